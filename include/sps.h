@@ -362,6 +362,115 @@ int64_t sps_linear_static_max_floats(void);
 /* floats of split-K scratch the shape needs on the current device; -1 for arguments sps_linear_static rejects */
 int64_t sps_linear_static_floats_needed(int32_t dtype, int32_t M, int32_t N, int32_t D);
 
+/* ---------------------------------------------------------------------------------------------------------------
+ * A paged key / value cache, for a serving program that runs many sequences of unlike lengths through the pieces of
+ * this library (sps_linear, sps_accept, sps_sample, ...) and keeps its own sequences: rotary positions, the append of
+ * new keys and values, and the attention of every sequence's new rows over its pages.  The paper serves one sequence
+ * from one dense cache; these calls change where keys and values live, not the method: a scoring pass of K + 1 rows
+ * is a batch whose sequences bring K + 1 new rows each, and the rollback after a rejection is a smaller kv_len.
+ *
+ * All three calls only enqueue (one kernel each) on `stream`, read lengths and page tables on the device -- so that a
+ * captured call can be replayed after these have moved -- and allocate nothing.  Pointers belong to the current
+ * device.  dtype here: 0 = fp32, 1 = bf16.
+ * ------------------------------------------------------------------------------------------------------------- */
+
+/* Activations by row and head: element e of head h of row r is p[r * row_stride + h * head_stride + e] (strides in
+ * elements; a head's elements are contiguous).  q, k and v may be slices of one q | k | v buffer. */
+typedef struct {
+  void* p;                         /* device */
+  int64_t row_stride, head_stride; /* elements */
+  int32_t dtype, heads;
+} sps_rows;
+
+#define SPS_ROTARY_PAIRS 0   /* rotated pairs are elements (2 i, 2 i + 1): what this library's models use */
+#define SPS_ROTARY_HALVES 1  /* rotated pairs are elements (i, i + rot_dim / 2)                            */
+typedef struct {
+  const double* freq; /* device [rot_dim / 2]: radians per position of each pair                            */
+  int32_t rot_dim;    /* the first rot_dim elements of a head are rotated (even, <= d_head), the rest kept   */
+  int32_t layout;     /* SPS_ROTARY_PAIRS or SPS_ROTARY_HALVES                                               */
+  float gain;         /* multiplies the rotated elements (1 = a pure rotation)                               */
+} sps_rotary_plan;
+
+/* Frequencies of the pairs, in 64 bits, into the HOST array out [rot_dim / 2]; no device work.  With
+ * f_i = base^(-2 i / rot_dim):
+ *   SPS_ROTARY_PLAIN   f_i
+ *   SPS_ROTARY_LINEAR  f_i / factor                       (positions squeezed into the trained length)
+ *   SPS_ROTARY_BASE    f_i with base * factor^(rot_dim / (rot_dim - 2)) in base's place (the fastest pair keeps its
+ *                      frequency, the slowest is divided by factor)
+ *   SPS_ROTARY_BANDS   a pair makes r_i = trained_len f_i / 2 pi turns within the trained length; with
+ *                      w_i = clamp((r_i - low_turns) / (high_turns - low_turns), 0, 1):  w_i f_i + (1 - w_i) f_i / factor
+ * factor >= 1 (ignored by PLAIN); trained_len >= 1 and 0 <= low_turns < high_turns for BANDS only. */
+#define SPS_ROTARY_PLAIN 0
+#define SPS_ROTARY_LINEAR 1
+#define SPS_ROTARY_BASE 2
+#define SPS_ROTARY_BANDS 3
+int sps_rotary_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, int32_t trained_len, double low_turns,
+                           double high_turns, double* out);
+
+/* y[r, h] = gain * R(positions[r]) x[r, h] over the first rot_dim elements, the others copied: the pair (a, b) at
+ * frequency f becomes gain * (a cos - b sin, a sin + b cos) of the angle position * f (worked out in 64 bits, so that
+ * far positions keep their phase).  transposed != 0 turns the other way -- gain * R^T: the operator's gradient, and
+ * for gain 1 its inverse.  positions device int32 [rows], any value.  x, y: [rows][heads] of d_head elements (even,
+ * 2 .. 1024) of one dtype; y may be x itself, other overlaps are not supported.  Rows, heads and strides of any
+ * alignment; 16-byte aligned ones are read and written 16 bytes at a time. */
+int sps_rotary(const sps_rotary_plan* plan, const sps_rows* x, const sps_rows* y, int32_t rows, int32_t d_head,
+               const int32_t* positions, int32_t transposed, void* stream);
+
+/* The cache of one layer: slot s of page p of key head h is k[p * page_stride + h * head_stride + s * pos_stride]
+ * and the d_head elements after it, v likewise.  k and v 16-byte aligned, strides multiples of 16 bytes, d_head 64 or
+ * 128, page_size a power of two, 8 .. 512. */
+typedef struct {
+  void *k, *v;                                  /* device, caller-owned */
+  int64_t page_stride, head_stride, pos_stride; /* elements             */
+  int32_t dtype, n_pages, page_size, n_kv_heads, d_head;
+} sps_paged_cache;
+
+/* The sequences of one call.  Sequence b owns rows q_start[b] .. q_start[b + 1] - 1 of the call's row buffers (none:
+ * q_start[b + 1] == q_start[b]) and has kv_len[b] tokens, these new ones included: its last row is at position
+ * kv_len[b] - 1.  Token j is in slot j % page_size of page pages[b * pages_ld + j / page_size]; table entries behind
+ * the last token's are never read, nor are slots behind it.  Rows behind the last sequence's are left as they were.
+ * Sequences may share pages that none of them appends to.
+ * The host sees none of these numbers.  What does not fit is skipped, never followed: row numbers outside the call's
+ * buffers, a kv_len above pages_ld * page_size (cut to it), a page number outside 0 .. n_pages - 1 (its tokens are
+ * not appended, and read as zeros); the last two also set a bit of *status, which the calls never clear. */
+#define SPS_PAGED_BAD_PAGE 1    /* bits of *status */
+#define SPS_PAGED_BAD_LENGTH 2
+#define SPS_PAGED_TIMEOUT 4     /* a bounded wait inside the attention kernel ran out: the call's outputs are meaningless */
+typedef struct {
+  const int32_t* q_start; /* device [B + 1], not decreasing      */
+  const int32_t* kv_len;  /* device [B]                          */
+  const int32_t* pages;   /* device [B][pages_ld]                */
+  int32_t* status;        /* device [1], may be NULL             */
+  int32_t B, pages_ld;
+  int32_t max_q;          /* the most rows a sequence brings, as far as the host knows (>= 1): picks the kernel, results
+                             hold for any q_start                */
+} sps_paged_batch;
+
+/* Append: for every row of every sequence, its keys -- rotated by the row's position under `plan`, unless plan is
+ * NULL -- and its values go to the row's slot, rounded to the cache's dtype.  With q (needs a plan; q_out too) the
+ * row's rotated queries go to q_out in the same kernel: q may be NULL, q_out may be q itself.  q, k, v share a dtype;
+ * q_out is fp32 or bf16 for fp32 q, bf16 for bf16 q; an fp32 cache takes fp32 rows only.  A row whose position is
+ * negative (more rows than kv_len) is skipped, its q_out too.  k, v, q: [rows] rows. */
+int sps_paged_append(const sps_paged_cache* cache, const sps_paged_batch* batch, const sps_rotary_plan* plan, int32_t rows,
+                     const sps_rows* k, const sps_rows* v, const sps_rows* q, const sps_rows* q_out, void* stream);
+
+/* Attention: row i of sequence b, at position p = kv_len[b] - (rows of b) + i, over the tokens 0 .. p of its sequence:
+ *   out[row, h] = sum_j softmax_j(scale q[row, h] . k[j, h / G]) v[j, h / G],   G = heads of q / n_kv_heads,
+ * scale 0 meaning 1 / sqrt(d_head).  A row at a negative position sees nothing: its output is 0.
+ * q and out: [rows] rows of the same heads; out has q's dtype, or is fp32; a bf16 cache takes fp32 or bf16 queries
+ * (fp32 queries and probabilities enter the tensor cores as three bf16 parts each, which keep their 24 bits; bf16
+ * queries leave the probabilities rounded to bf16), an fp32 cache fp32 ones.  lse: device fp32 [rows][heads], may be
+ * NULL: log sum_j exp(scale q . k_j), -inf for a row that sees nothing.
+ * What lies in slots behind a sequence's tokens never matters, whatever it is.  An infinite or NaN value (v) makes
+ * every element of the rows that see it NaN where its token is among the sequence's new rows, and follows
+ * sum p_j v_j elsewhere.
+ * workspace: device scratch of sps_paged_attention_workspace_bytes bytes, 16-byte aligned, zero-filled once before its
+ * first use (every call leaves it ready for the next; calls that share one must not run at the same time, captured
+ * ones included).  The size holds for every batch on this cache shape. */
+int sps_paged_attention(const sps_paged_cache* cache, const sps_paged_batch* batch, int32_t rows, const sps_rows* q,
+                        const sps_rows* out, float scale, float* lse, void* workspace, void* stream);
+int64_t sps_paged_attention_workspace_bytes(const sps_paged_cache* cache, int32_t n_heads, int32_t q_dtype);
+
 /* Tensor-parallel passes (section Conditional Scoring: the models are served Megatron-style over several chips, the
  * attention and feed-forward blocks sharded and each followed by an all-reduce of (K + 1) x d_model numbers, which
  * is latency-bound and about as costly for K + 1 rows as for one; section Choice of Draft Models: the draft is shaped

@@ -57,6 +57,24 @@ class sps_stats(C.Structure):
         return d
 
 
+class sps_rows(C.Structure):
+    _fields_ = [("p", C.c_void_p), ("row_stride", C.c_int64), ("head_stride", C.c_int64), ("dtype", C.c_int32), ("heads", C.c_int32)]
+
+
+class sps_rotary_plan(C.Structure):
+    _fields_ = [("freq", C.c_void_p), ("rot_dim", C.c_int32), ("layout", C.c_int32), ("gain", C.c_float)]
+
+
+class sps_paged_cache(C.Structure):
+    _fields_ = [("k", C.c_void_p), ("v", C.c_void_p), ("page_stride", C.c_int64), ("head_stride", C.c_int64), ("pos_stride", C.c_int64),
+                ("dtype", C.c_int32), ("n_pages", C.c_int32), ("page_size", C.c_int32), ("n_kv_heads", C.c_int32), ("d_head", C.c_int32)]
+
+
+class sps_paged_batch(C.Structure):
+    _fields_ = [("q_start", C.c_void_p), ("kv_len", C.c_void_p), ("pages", C.c_void_p), ("status", C.c_void_p),
+                ("B", C.c_int32), ("pages_ld", C.c_int32), ("max_q", C.c_int32)]
+
+
 _lib = None
 
 
@@ -111,6 +129,13 @@ def lib():
         L.sps_tp_group_prefill.argtypes = [vp, i32, vp, i32]
         L.sps_tp_group_score.argtypes = [vp, i32, i32, vp, i32, vp, C.POINTER(f32)]
         L.sps_tp_group_generate.argtypes = [vp, i32, vp, i32, i32, i32, f32, u64, vp, C.POINTER(sps_stats)]
+        f64 = C.c_double
+        L.sps_rotary_frequencies.argtypes = [i32, f64, i32, f64, i32, f64, f64, vp]
+        L.sps_rotary.argtypes = [vp, vp, vp, i32, i32, vp, i32, vp]
+        L.sps_paged_append.argtypes = [vp, vp, vp, i32, vp, vp, vp, vp, vp]
+        L.sps_paged_attention.argtypes = [vp, vp, i32, vp, vp, f32, vp, vp, vp]
+        L.sps_paged_attention_workspace_bytes.argtypes = [vp, i32, i32]
+        L.sps_paged_attention_workspace_bytes.restype = i64
         _lib = L
     return _lib
 
@@ -398,3 +423,154 @@ def sps_debug_set_wait(limit_us=0, drop_stage=-1):
     """Test hook: bound of the kernels' waits in microseconds (0 = the default 2 s) and the stage the first CTA's copy
     producer leaves out (-1 = none)."""
     _check(lib().sps_debug_set_wait(int(limit_us), int(drop_stage)))
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# rotary positions and the paged cache (see include/sps.h)
+# ---------------------------------------------------------------------------------------------------------------------
+PAGED_BAD_PAGE, PAGED_BAD_LENGTH, PAGED_TIMEOUT = 1, 2, 4
+ROTARY_LAYOUTS = {"pairs": 0, "halves": 1}
+ROTARY_SCALINGS = {"plain": 0, "linear": 1, "base": 2, "bands": 3}
+
+
+def sps_rotary_frequencies(rot_dim, base=10000.0, scaling="plain", factor=1.0, trained_len=0, low_turns=1.0, high_turns=32.0):
+    """The pairs' frequencies as a numpy float64 array [rot_dim / 2] (host arithmetic, no GPU needed)."""
+    if scaling not in ROTARY_SCALINGS:
+        raise ValueError("scaling is one of %s" % ", ".join(ROTARY_SCALINGS))
+    out = np.zeros(max(int(rot_dim) // 2, 1), dtype=np.float64)
+    _check(lib().sps_rotary_frequencies(int(rot_dim), base, ROTARY_SCALINGS[scaling], factor, trained_len, low_turns, high_turns, _np_ptr(out)))
+    return out
+
+
+def _dtype_of(t):
+    name = str(t.dtype)
+    if name == "torch.float32":
+        return 0
+    if name == "torch.bfloat16":
+        return 1
+    raise ValueError("tensors are float32 or bfloat16, got %s" % name)
+
+
+def _rows_of(t):
+    """A [rows, heads, d_head] tensor (any strides over contiguous heads) as an sps_rows."""
+    st = t.stride()
+    if len(st) != 3 or (st[2] != 1 and t.shape[2] > 1):
+        raise ValueError("rows are [rows, heads, d_head] with contiguous heads")
+    return sps_rows(t.data_ptr(), st[0], st[1], _dtype_of(t), t.shape[1])
+
+
+class Rotary:
+    """A rotary plan: `freq` CUDA float64 [rot_dim / 2] (e.g. torch.from_numpy(sps_rotary_frequencies(...)).cuda()),
+    `layout` "pairs" or "halves", `gain` the factor on the rotated elements."""
+
+    def __init__(self, freq, layout="pairs", gain=1.0):
+        if layout not in ROTARY_LAYOUTS:
+            raise ValueError("layout is one of %s" % ", ".join(ROTARY_LAYOUTS))
+        if str(freq.dtype) != "torch.float64" or freq.dim() != 1 or not freq.is_contiguous() or not freq.is_cuda:
+            raise ValueError("freq is a contiguous CUDA float64 vector")
+        self.freq, self.layout, self.gain, self.device = freq, layout, float(gain), freq.device
+        self._c = sps_rotary_plan(freq.data_ptr(), 2 * freq.shape[0], ROTARY_LAYOUTS[layout], self.gain)
+        self._p = C.addressof(self._c)
+
+
+class PagedCache:
+    """One layer's pages: k, v CUDA [n_pages, n_kv_heads, page_size, d_head], fp32 or bf16, of the same strides (any with
+    contiguous heads: a [n_pages, page_size, n_kv_heads, d_head] tensor goes in as its transpose(1, 2))."""
+
+    def __init__(self, k, v):
+        if k.dim() != 4 or k.shape != v.shape or k.stride() != v.stride() or k.dtype != v.dtype or k.device != v.device or not k.is_cuda:
+            raise ValueError("k and v are CUDA tensors [n_pages, n_kv_heads, page_size, d_head] of the same shape, strides and dtype")
+        if k.stride(3) != 1:
+            raise ValueError("a slot's d_head elements must be contiguous")
+        self.k, self.v, self.device = k, v, k.device
+        self._c = sps_paged_cache(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), _dtype_of(k), k.shape[0], k.shape[2],
+                                  k.shape[1], k.shape[3])
+        self._p = C.addressof(self._c)
+
+
+class PagedBatch:
+    """The sequences of a call: q_start CUDA int32 [B + 1], kv_len CUDA int32 [B], pages CUDA int32 [B, ...] (rows of the
+    page table), read by the kernels when they run.  max_q: the most new rows a sequence brings.  `status` (int32 [1],
+    made here unless given) collects PAGED_* bits and is never cleared by the calls."""
+
+    def __init__(self, q_start, kv_len, pages, max_q=1, status=None):
+        import torch
+        for t in (q_start, kv_len, pages):
+            if t.dtype != torch.int32 or t.device != q_start.device or not t.is_cuda:
+                raise ValueError("q_start, kv_len and pages are CUDA int32 tensors on one device")
+        B = kv_len.shape[0]
+        if kv_len.dim() != 1 or q_start.dim() != 1 or q_start.shape[0] != B + 1 or pages.dim() != 2 or pages.shape[0] != B:
+            raise ValueError("q_start [B + 1], kv_len [B], pages [B, ...]")
+        if not (q_start.is_contiguous() and kv_len.is_contiguous()) or (pages.numel() > 0 and pages.stride(1) != 1 and pages.shape[1] > 1):
+            raise ValueError("q_start, kv_len and the rows of pages must be contiguous")
+        if B > 1 and pages.stride(0) != pages.shape[1]:
+            raise ValueError("the rows of pages must follow one another")
+        if status is None:
+            status = torch.zeros(1, dtype=torch.int32, device=q_start.device)
+        if status.dtype != torch.int32 or status.numel() < 1 or status.device != q_start.device:
+            raise ValueError("status is a CUDA int32 tensor of one element")
+        self.q_start, self.kv_len, self.pages, self.status, self.device = q_start, kv_len, pages, status, q_start.device
+        self._c = sps_paged_batch(q_start.data_ptr(), kv_len.data_ptr(), pages.data_ptr(), status.data_ptr(), B, pages.shape[1], int(max_q))
+        self._p = C.addressof(self._c)
+
+
+def _on(device, fn, stream, *args):
+    """fn(*args, stream) with `device` current, on `stream` or that device's current one."""
+    import torch
+    if torch.cuda.current_device() == device.index:
+        _check(fn(*args, torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream))
+    else:
+        with torch.cuda.device(device):
+            _check(fn(*args, torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream))
+
+
+def _same_device(device, *tensors):
+    for t in tensors:
+        if t is not None and t.device != device:
+            raise ValueError("all tensors must be on one CUDA device")
+
+
+def sps_rotary(x, y, positions, plan, transposed=False, stream=None):
+    """y = gain R(positions) x over the plan's rotated elements, the others copied; x, y CUDA [rows, heads, d_head], fp32 or
+    bf16 (y may be x); positions CUDA int32 [rows].  transposed: gain R^T, the gradient."""
+    _same_device(plan.device, x, y, positions)
+    if x.shape != y.shape or positions.shape != x.shape[:1] or not positions.is_contiguous() or str(positions.dtype) != "torch.int32":
+        raise ValueError("x and y [rows, heads, d_head], positions contiguous int32 [rows]")
+    _on(plan.device, lib().sps_rotary, stream, plan._p, C.byref(_rows_of(x)), C.byref(_rows_of(y)), x.shape[0], x.shape[2],
+        positions.data_ptr(), 1 if transposed else 0)
+
+
+def sps_paged_append(cache, batch, k, v, plan=None, q=None, q_out=None, stream=None):
+    """Keys (rotated under `plan`) and values of the batch's rows into their slots; with q, its rotated rows into q_out.
+    k, v CUDA [rows, n_kv_heads, d_head]; q, q_out CUDA [rows, heads, d_head]."""
+    _same_device(cache.device, batch, k, v, plan, q, q_out)
+    if k.shape != v.shape or k.dim() != 3 or k.shape[2] != cache.k.shape[3]:
+        raise ValueError("k and v are [rows, n_kv_heads, d_head]")
+    if (q is None) != (q_out is None) or (q is not None and (q.shape != q_out.shape or q.shape[0] != k.shape[0] or q.shape[2] != k.shape[2])):
+        raise ValueError("q and q_out go together and are [rows, heads, d_head]")
+    _on(cache.device, lib().sps_paged_append, stream, cache._p, batch._p, plan._p if plan is not None else None, k.shape[0],
+        C.byref(_rows_of(k)), C.byref(_rows_of(v)), C.byref(_rows_of(q)) if q is not None else None,
+        C.byref(_rows_of(q_out)) if q is not None else None)
+
+
+def sps_paged_attention_workspace_bytes(cache, n_heads, q_dtype):
+    """q_dtype: torch.float32 or torch.bfloat16."""
+    n = int(lib().sps_paged_attention_workspace_bytes(cache._p, n_heads, {"torch.float32": 0, "torch.bfloat16": 1}.get(str(q_dtype), -1)))
+    if n < 0:
+        _check(SPS_EINVAL)
+    return n
+
+
+def sps_paged_attention(cache, batch, q, out, workspace, scale=0.0, lse=None, stream=None):
+    """Causal attention of the batch's rows over their sequences' pages.  q, out CUDA [rows, heads, d_head]; workspace CUDA
+    uint8 (zeroed once) of sps_paged_attention_workspace_bytes; scale 0 = 1 / sqrt(d_head); lse CUDA float32 [rows, heads]."""
+    _same_device(cache.device, batch, q, out, workspace, lse)
+    if q.shape != out.shape or q.dim() != 3 or q.shape[2] != cache.k.shape[3]:
+        raise ValueError("q and out are [rows, heads, d_head]")
+    if lse is not None and (lse.shape != q.shape[:2] or not lse.is_contiguous() or str(lse.dtype) != "torch.float32"):
+        raise ValueError("lse is contiguous float32 [rows, heads]")
+    need = lib().sps_paged_attention_workspace_bytes(cache._p, q.shape[1], _dtype_of(q))
+    if workspace.numel() * workspace.element_size() < need:
+        raise ValueError("workspace smaller than sps_paged_attention_workspace_bytes")
+    _on(cache.device, lib().sps_paged_attention, stream, cache._p, batch._p, q.shape[0], C.byref(_rows_of(q)), C.byref(_rows_of(out)), scale,
+        lse.data_ptr() if lse is not None else None, workspace.data_ptr())

@@ -1,0 +1,277 @@
+// Shared by the paged-cache kernels: argument blocks, where a sequence's rows and tokens are, and how the attention
+// kernels cut a ragged batch into equal pieces of work.
+#pragma once
+#include "../../include/sps.h"
+#include "common.cuh"
+
+// activations by row and head (sps_rows on the device side)
+struct RowsView {
+  void* p;
+  long long row, head;   // strides in elements
+};
+
+struct PagedSeqs {       // sps_paged_batch, with what bounds it on the host
+  const int32_t *q_start, *kv_len, *pages;
+  int32_t* status;
+  int B, pages_ld, rows;
+  int n_pages, page_size, page_shift;   // page_size = 1 << page_shift
+};
+
+__device__ __forceinline__ void paged_flag(int32_t* status, int bit) {
+  if (status) atomicOr(status, bit);
+}
+
+// tokens the page table of a sequence can hold (fits 32 bits: longer tables are cut)
+__device__ __forceinline__ int paged_capacity(const PagedSeqs& s) {
+  const long long c = (long long)s.pages_ld << s.page_shift;
+  return c > 0x7fff0000ll ? 0x7fff0000 : (int)c;
+}
+
+struct SeqGeom { int row0, nq, len; bool cut; };   // first row, rows, tokens; cut: kv_len did not fit the page table
+__device__ __forceinline__ SeqGeom paged_seq(const PagedSeqs& s, int b) {
+  SeqGeom g;
+  const int r0 = min(max(s.q_start[b], 0), s.rows), r1 = min(max(s.q_start[b + 1], r0), s.rows);
+  const int len = s.kv_len[b], cap = paged_capacity(s);
+  g.row0 = r0;
+  g.nq = r1 - r0;
+  g.cut = len > cap;
+  g.len = min(max(len, 0), cap);
+  return g;
+}
+
+// ------------------------------------------------------------------------------------------------------------------
+// The attention kernels' work.  A sequence's queries of one key head are nq * G rows (token-major: row r is token r / G,
+// head r % G of the group), taken NR at a time: an item is (sequence, key head, tile of NR rows), and its work is the
+// number of tiles of KT tokens its last row sees (at least one, so that empty rows get their zeros).  All items' tiles in
+// order -- sequences, key heads, row tiles -- are cut into equal runs, one per CTA: a ragged batch, one long sequence and
+// a prompt chunk are balanced alike, to one tile.  A CTA whose run begins or ends inside an item leaves that part's
+// (maximum, sum, unnormalised output) in its slot; the last CTA of the item to finish joins the parts in their order, so
+// results do not depend on timing.
+// ------------------------------------------------------------------------------------------------------------------
+struct PagedAttnArgs {
+  PagedSeqs s;
+  RowsView q, out;
+  int q_bf16, out_bf16, q_vec, out_vec;   // vec: 16-byte accesses are aligned
+  void *k, *v;
+  long long page_stride, head_stride, pos_stride;
+  int H, Hkv, G;
+  float scale_log2;         // scale * log2(e): scores are kept in base 2
+  float* lse;               // [rows][H] or null
+  int* counters;            // [grid] arrivals at an item, by the first CTA that works on it; zero between launches
+  float* slots;             // [2 * grid] parts: [NR] maxima, [NR] sums, [NR][d_head] outputs
+  unsigned long long wait_ns;
+};
+
+// tiles of KT tokens row tile t of a sequence has to read
+template <int NR, int KT>
+__device__ __forceinline__ int item_tiles(int nq, int len, int G, int t) {
+  const int last = min((t + 1) * NR, nq * G) - 1;
+  const int pos = len - nq + last / G;
+  return pos < 0 ? 1 : pos / KT + 1;
+}
+
+struct WorkCursor {       // a place in the list of items, and the run of tiles that is left
+  int b, hk, t;           // item
+  int row0, nq, len, nt;  // its sequence; nt = row tiles of the sequence
+  int n;                  // tiles of the item
+  int k0, k1;             // this CTA's tiles of it
+  long long u, u_end;     // tiles of the whole list: the next one after this part, the end of the run
+  long long item0;        // list index of the item's first tile
+  long long per;          // tiles per CTA
+  bool valid;
+};
+
+template <int NR, int KT>
+__device__ __forceinline__ void cursor_part(const PagedAttnArgs& a, WorkCursor& c) {   // the part of item (b, hk, t) that begins at c.u
+  c.n = item_tiles<NR, KT>(c.nq, c.len, a.G, c.t);
+  c.k0 = (int)(c.u - c.item0);
+  const long long left = c.u_end - c.u, rest = c.n - c.k0;
+  c.k1 = c.k0 + (int)(left < rest ? left : rest);
+  c.u += c.k1 - c.k0;
+}
+
+template <int NR, int KT>
+__device__ __forceinline__ void cursor_next(const PagedAttnArgs& a, WorkCursor& c) {
+  if (c.u >= c.u_end) { c.valid = false; return; }
+  c.item0 += c.n;
+  if (++c.t == c.nt) {
+    c.t = 0;
+    if (++c.hk == a.Hkv) {
+      c.hk = 0;
+      do {
+        if (++c.b >= a.s.B) { c.valid = false; return; }
+        const SeqGeom g = paged_seq(a.s, c.b);
+        c.row0 = g.row0; c.nq = g.nq; c.len = g.len;
+      } while (c.nq == 0);
+      c.nt = (c.nq * a.G + NR - 1) / NR;
+    }
+  }
+  cursor_part<NR, KT>(a, c);
+}
+
+// Sum of item_tiles over a sequence's row tiles, for the sequences of one warp (lane = sequence): short sequences by
+// their own lane, long ones by the whole warp.
+template <int NR, int KT>
+__device__ __forceinline__ long long warp_seq_units(const PagedAttnArgs& a, const SeqGeom& g, bool live) {
+  const int lane = threadIdx.x & 31;
+  const int nt = live ? (int)(((long long)g.nq * a.G + NR - 1) / NR) : 0;
+  long long sum = 0;
+  if (nt <= 4) for (int t = 0; t < nt; ++t) sum += item_tiles<NR, KT>(g.nq, g.len, a.G, t);
+  unsigned big = __ballot_sync(0xffffffffu, nt > 4);
+  while (big) {
+    const int src = __ffs(big) - 1;
+    big &= big - 1;
+    const int nq = __shfl_sync(0xffffffffu, g.nq, src), len = __shfl_sync(0xffffffffu, g.len, src), n = __shfl_sync(0xffffffffu, nt, src);
+    long long part = 0;
+    for (int t = lane; t < n; t += 32) part += item_tiles<NR, KT>(nq, len, a.G, t);
+#pragma unroll
+    for (int o = 16; o > 0; o >>= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
+    if (lane == src) sum = part;
+  }
+  return sum;
+}
+
+// Called by warp 0 alone; the result is for every thread of the CTA (through shared memory).  min_run: the fewest tiles a
+// CTA takes, so that a short list is not cut into parts that cost more to join than they save.
+template <int NR, int KT>
+__device__ __forceinline__ WorkCursor cursor_begin(const PagedAttnArgs& a, int min_run) {
+  const int lane = threadIdx.x & 31, B = a.s.B;
+  WorkCursor c;
+  c.valid = false;
+  long long total = 0;
+  bool cut = false;
+  for (int b0 = 0; b0 < B; b0 += 32) {
+    const int b = b0 + lane;
+    SeqGeom g{};
+    if (b < B) { g = paged_seq(a.s, b); cut = cut || (g.cut && g.nq > 0); }
+    total += warp_seq_units<NR, KT>(a, g, b < B);
+  }
+  if (cut && blockIdx.x == 0) paged_flag(a.s.status, SPS_PAGED_BAD_LENGTH);
+#pragma unroll
+  for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
+  total *= a.Hkv;
+  const long long grid = gridDim.x;
+  c.per = (total + grid - 1) / grid;
+  if (c.per < min_run) c.per = min_run;
+  c.u = (long long)blockIdx.x * c.per;
+  c.u_end = c.u + c.per < total ? c.u + c.per : total;
+  if (c.u >= c.u_end) return c;
+  // the sequence tile c.u falls into
+  long long base = 0;
+  for (int b0 = 0; b0 < B; b0 += 32) {
+    const int b = b0 + lane;
+    SeqGeom g{};
+    if (b < B) g = paged_seq(a.s, b);
+    const long long units = warp_seq_units<NR, KT>(a, g, b < B) * a.Hkv;
+    long long incl = units;
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long up = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += up;
+    }
+    const unsigned hit = __ballot_sync(0xffffffffu, base + incl > c.u);
+    if (hit) {
+      const int src = __ffs(hit) - 1;
+      c.b = b0 + src;
+      c.row0 = __shfl_sync(0xffffffffu, g.row0, src);
+      c.nq = __shfl_sync(0xffffffffu, g.nq, src);
+      c.len = __shfl_sync(0xffffffffu, g.len, src);
+      const long long first = __shfl_sync(0xffffffffu, base + incl - units, src), per_head = __shfl_sync(0xffffffffu, units, src) / a.Hkv;
+      c.nt = (int)(((long long)c.nq * a.G + NR - 1) / NR);
+      c.hk = (int)((c.u - first) / per_head);
+      long long at = first + c.hk * per_head;   // first tile of the key head
+      // the row tile: 32 at a time
+      for (int t0 = 0; t0 < c.nt; t0 += 32) {
+        const int t = t0 + lane;
+        const long long n = t < c.nt ? item_tiles<NR, KT>(c.nq, c.len, a.G, t) : 0;
+        long long in2 = n;
+#pragma unroll
+        for (int o = 1; o < 32; o <<= 1) {
+          const long long up = __shfl_up_sync(0xffffffffu, in2, o);
+          if (lane >= o) in2 += up;
+        }
+        const unsigned hit2 = __ballot_sync(0xffffffffu, at + in2 > c.u);
+        if (hit2) {
+          const int s2 = __ffs(hit2) - 1;
+          c.t = t0 + s2;
+          c.item0 = __shfl_sync(0xffffffffu, at + in2 - n, s2);
+          break;
+        }
+        at += __shfl_sync(0xffffffffu, in2, 31);
+      }
+      c.valid = true;
+      cursor_part<NR, KT>(a, c);
+      return c;
+    }
+    base += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  return c;
+}
+
+// parts an item is cut into: the CTAs first .. first + parts - 1 each hold one
+__device__ __forceinline__ void item_ctas(const WorkCursor& c, int& first, int& parts) {
+  first = (int)(c.item0 / c.per);
+  parts = (int)((c.item0 + c.n - 1) / c.per) - first + 1;
+}
+// the slot of this CTA's part: 2 c + 1 where the item begins in this CTA, else 2 c (a run holds at most one of each)
+__device__ __forceinline__ int part_slot(int cta, bool begins) { return 2 * cta + (begins ? 1 : 0); }
+template <int NR, int D> __host__ __device__ constexpr size_t slot_floats() { return (size_t)NR * (D + 2); }
+
+__device__ __forceinline__ void store_out(const PagedAttnArgs& a, long long at, float v) {
+  if (a.out_bf16) reinterpret_cast<__nv_bfloat16*>(a.out.p)[at] = __float2bfloat16_rn(v);
+  else reinterpret_cast<float*>(a.out.p)[at] = v;
+}
+
+// Joins the parts of an item and writes its rows: o = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c.  Run by all THREADS
+// threads of the last CTA to arrive; w is shared scratch of NR floats.
+template <int NR, int D, int THREADS>
+__device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCursor& c, int first, int parts, int tid, float* w_inv, float* w_max) {
+  const int R = c.nq * a.G, r0 = c.t * NR, live = min(NR, R - r0);
+  constexpr size_t SF = slot_floats<NR, D>();
+  auto slot = [&](int p) { return a.slots + SF * (size_t)part_slot(first + p, p == 0); };
+  if (tid < live) {
+    float M = -INFINITY, L = 0.f;
+    for (int p = 0; p < parts; ++p) M = fmaxf(M, __ldcg(slot(p) + tid));
+    for (int p = 0; p < parts; ++p) {
+      const float m = __ldcg(slot(p) + tid), l = __ldcg(slot(p) + NR + tid);
+      if (m != -INFINITY || l != l) L += l * exp2f(m - M);
+    }
+    w_max[tid] = M;
+    w_inv[tid] = M == -INFINITY && L == 0.f ? 0.f : 1.f / L;
+    if (a.lse) {
+      const int r = r0 + tid;
+      a.lse[(size_t)(c.row0 + r / a.G) * a.H + c.hk * a.G + r % a.G] = L > 0.f || L != L ? 0.6931471805599453f * (M + log2f(L)) : -INFINITY;
+    }
+  }
+  asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory");
+  for (int i = tid; i < live * D; i += THREADS) {
+    const int r = i / D, e = i - r * D;
+    const float M = w_max[r], inv = w_inv[r];
+    float o = 0.f;
+    for (int p = 0; p < parts; ++p) {
+      const float m = __ldcg(slot(p) + r);
+      if (m != -INFINITY) o += exp2f(m - M) * __ldcg(slot(p) + 2 * NR + i);
+    }
+    const int rr = r0 + r;
+    store_out(a, (long long)(c.row0 + rr / a.G) * a.out.row + (long long)(c.hk * a.G + rr % a.G) * a.out.head + e, inv != inv ? inv : (inv == 0.f ? 0.f : o * inv));
+  }
+  asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory");
+}
+
+// launchers
+struct RotaryArgs {
+  RowsView x[3], y[3];         // queries (or the rows of sps_rotary), keys, values; y[1], y[2]: page pools
+  int heads[3];
+  int d_head, rot, halves, transposed;
+  float gain;
+  const double* freq;          // null: nothing is rotated
+  const int32_t* positions;    // sps_rotary; null: from the batch
+  PagedSeqs s;
+  long long pos_stride;        // cache slots
+  int rows, rows_per_cta, units, units_per_cta, uh_rot, uh_flat;   // set by the launcher
+};
+cudaError_t rotary_launch(RotaryArgs a, int x_bf16, int yq_bf16, int cache_bf16, int num_sm, cudaStream_t st);
+// CTAs of an attention launch on a device of num_sm SMs, at most (counters and slots are laid out for as many)
+inline int paged_attn_grid(int num_sm) { return num_sm < 1024 ? num_sm : 1024; }
+size_t paged_attn_slot_bytes(int dtype, int q_dtype, int d_head);
+cudaError_t paged_attn_launch(const PagedAttnArgs& a, int cache_bf16, int d_head, int max_q, int num_sm, cudaStream_t st);

@@ -1,0 +1,239 @@
+"""sps_paged_attention on the GPU against per-row softmax attention in 64 bits."""
+import pytest
+import torch
+
+import paper_2302_01318_b200 as sps
+from paged_util import BF16, DEV, F32, Pages, attention64, attention_tol, check_attention, normal, run_attention, workspace
+
+pytestmark = pytest.mark.gpu
+
+TYPES = [(F32, F32, F32), (F32, BF16, F32), (BF16, BF16, BF16), (BF16, BF16, F32)]   # q, cache, out
+
+# lens, news, Hkv, G, page
+SHAPES = [
+    ([1], [1], 1, 1, 8),                                     # one token that sees itself
+    ([2, 1, 1], [1, 1, 1], 2, 1, 16),
+    ([127, 128, 129, 130], [1, 1, 1, 1], 1, 8, 16),          # contexts around a tile's end
+    ([64, 63, 65], [5, 5, 5], 2, 3, 32),                     # a group of three heads, 15 rows
+    ([0, 3, 0, 200], [0, 2, 0, 4], 1, 4, 8),                 # sequences without rows and without tokens
+    ([2, 40, 0], [5, 1, 3], 2, 2, 16),                       # rows at negative positions: they see nothing
+    ([700], [1], 1, 1, 64),                                  # one row over a long context: split over CTAs
+    ([1500, 3], [2, 3], 1, 5, 128),
+    ([257, 511], [33, 17], 2, 6, 512),                       # many rows: several row tiles, groups that do not divide them
+    ([150, 1, 90], [150, 1, 1], 1, 4, 16),                   # a prompt beside decode rows
+    ([1], [1], 3, 16, 8),
+    ([400], [7], 1, 20, 16),                                 # 140 rows of one key head
+]
+
+
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("types", range(len(TYPES)))
+@pytest.mark.parametrize("shape", range(len(SHAPES)))
+def test_matches_64_bits(d, types, shape):
+    lens, news, Hkv, G, page = SHAPES[shape]
+    qdt, cdt, odt = TYPES[types]
+    pages = Pages(lens, Hkv, d, page, cdt, seed=shape, order="head" if shape % 2 else "slot")   # every other slot is NaN
+    run_attention(pages, news, Hkv * G, qdt, odt, lead=shape % 3, tail=2)
+
+
+@pytest.mark.parametrize("types", range(3))
+@pytest.mark.parametrize("max_q", [1, 64, 100000])
+def test_max_q_is_a_hint_only(types, max_q):
+    qdt, cdt, odt = TYPES[types]
+    pages = Pages([300, 40], 2, 128, 16, cdt)
+    run_attention(pages, [70, 1], 8, qdt, odt, max_q=max_q)
+
+
+@pytest.mark.parametrize("types", range(3))
+@pytest.mark.parametrize("d", [64, 128])
+def test_one_workspace_serves_every_batch_in_turn(types, d):
+    """Counters and parts left by one call do not reach the next, whatever its shape; the same call twice gives the same bits."""
+    qdt, cdt, odt = TYPES[types]
+    pools = [Pages(lens, 2, d, 16, cdt, seed=i) for i, lens in enumerate(([2000], [5, 900, 31], [64] * 20, [1]))]
+    ws = workspace(pools[0].cache, 8, qdt)
+    news = ([3], [2, 1, 9], [1] * 20, [1])
+    for turn in range(2):
+        for p, n in zip(pools, news):
+            a = run_attention(p, n, 8, qdt, odt, ws=ws)
+            b = run_attention(p, n, 8, qdt, odt, ws=ws)
+            assert torch.equal(a[0], b[0]) and torch.equal(a[1], b[1])
+
+
+@pytest.mark.parametrize("types", range(3))
+def test_large_scores_small_scores_and_given_scale(types):
+    qdt, cdt, odt = TYPES[types]
+    pages = Pages([600, 90], 1, 64, 32, cdt)
+    run_attention(pages, [4, 30], 4, qdt, odt, std=40.0)       # one token takes nearly all the weight
+    run_attention(pages, [4, 30], 4, qdt, odt, std=1e-3)       # every token the same weight
+    run_attention(pages, [4, 30], 4, qdt, odt, scale=0.7)
+    run_attention(pages, [4, 30], 4, qdt, odt, scale=-0.25)
+
+
+@pytest.mark.parametrize("types", range(3))
+@pytest.mark.parametrize("rising", [False, True])
+def test_scores_that_rise_and_fall_along_the_context(types, rising):
+    """Maxima that keep moving: a key's score grows (or falls) by far more than a rescaling step from tile to tile."""
+    qdt, cdt, odt = TYPES[types]
+    pages = Pages([1000], 1, 64, 16, cdt)
+    k, v = pages.dense[0]
+    ramp = torch.linspace(0, 1, 1000, device=DEV)
+    if not rising:
+        ramp = ramp.flip(0)
+    k.copy_((ramp[:, None, None] * torch.ones_like(k).float() * 6).to(cdt))
+    j = torch.arange(1000)
+    pages.k[pages.table[0, j // 16].long().to(DEV), :, (j % 16).to(DEV)] = k
+    q = torch.ones((5, 4, 64), device=DEV).mul_(torch.tensor([1., 3., 0.2, -2.], device=DEV)[None, :, None]).to(qdt)
+    run_attention(pages, [5], 4, qdt, odt, q=q)
+
+
+@pytest.mark.parametrize("types", range(3))
+@pytest.mark.parametrize("bad", [float("nan"), float("inf"), float("-inf")])
+def test_what_a_row_does_not_see_never_reaches_it(types, bad):
+    """The last of the new tokens has a bad key and value: the rows before it are exact, its own is not finite."""
+    qdt, cdt, odt = TYPES[types]
+    pages = Pages([205, 70], 1, 64, 8, cdt, fill=bad)
+    news = [9, 3]
+    clean = [(k.clone(), v.clone()) for k, v in pages.dense]
+    pg, sl = int(pages.table[0, 204 // 8]), 204 % 8
+    pages.v[pg, 0, sl, 5] = bad
+    q = normal((12, 2, 64), qdt, 1)
+    out, ws = torch.empty((12, 2, 64), dtype=odt, device=DEV), workspace(pages.cache, 2, qdt)
+    for key in (False, True):
+        if key:
+            pages.k[pg, 0, sl, 7] = bad
+        sps.sps_paged_attention(pages.cache, pages.batch(news), q, out, ws)
+        torch.cuda.synchronize()
+        keep = [r for r in range(12) if r != 8]
+        assert not torch.isfinite(out[8].float()).all() or (key and bad == float("-inf"))
+        want, _, S = attention64(q, clean, news)
+
+        tol = attention_tol(want, S, 64, qdt, odt)
+        assert ((out.double() - want).abs() <= tol)[keep].all()
+
+
+@pytest.mark.parametrize("types", range(3))
+def test_bad_pages_and_lengths_are_flagged_and_harm_no_other_sequence(types):
+    qdt, cdt, odt = TYPES[types]
+    pages = Pages([100, 300, 50], 2, 64, 16, cdt)
+    batch = pages.batch([2, 2, 2])
+    batch.pages[0, 3] = pages.n_pages
+    batch.pages[2, 1] = -5
+    q, ws = normal((6, 4, 64), qdt, 1), workspace(pages.cache, 4, qdt)
+    out = torch.empty((6, 4, 64), dtype=odt, device=DEV)
+    sps.sps_paged_attention(pages.cache, batch, q, out, ws)
+    assert int(batch.status) == sps.PAGED_BAD_PAGE
+    assert torch.isfinite(out.float()).all()
+    check_attention(out[2:4], None, q[2:4], pages.dense[1:2], [2])
+    # a bad page's tokens read as zeros: score 0, value 0
+    zeroed = [(k.clone(), v.clone()) for k, v in pages.dense]
+    zeroed[0][0][48:64], zeroed[0][1][48:64] = 0, 0
+    zeroed[2][0][16:32], zeroed[2][1][16:32] = 0, 0
+    check_attention(out, None, q, zeroed, [2, 2, 2])
+    batch2 = pages.batch([2, 2, 2])
+    batch2.kv_len[1] = 10 ** 6
+    sps.sps_paged_attention(pages.cache, batch2, q, out, ws)
+    assert int(batch2.status) & sps.PAGED_BAD_LENGTH
+    check_attention(out[:2], None, q[:2], pages.dense[:1], [2])
+    check_attention(out[4:], None, q[4:], pages.dense[2:], [2])
+    # row numbers outside the buffers and out of order are cut, not followed
+    batch3 = pages.batch([2, 2, 2])
+    batch3.q_start.copy_(torch.tensor([-7, 2, 1, 5000], dtype=torch.int32))
+    sps.sps_paged_attention(pages.cache, batch3, q, out, ws)
+    torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("types", range(3))
+def test_strides_and_unaligned_rows(types):
+    qdt, cdt, odt = TYPES[types]
+    pages = Pages([77, 140], 2, 64, 8, cdt)
+    news, rows, H = [3, 20], 23, 4
+    big = normal((rows, H + 2, 67), qdt, 3)
+    for q in (big[:, 1:1 + H, :64], big[:, 1:1 + H, 3:67], normal((H, rows, 64), qdt, 4).transpose(0, 1)):
+        ob = torch.full((rows, H + 1, 69), 7.0, dtype=odt, device=DEV)
+        out = ob[:, 1:, 5:]
+        sps.sps_paged_attention(pages.cache, pages.batch(news), q, out, workspace(pages.cache, H, qdt))
+        check_attention(out, None, q, pages.dense, news)
+        assert (ob[:, 0] == 7).all() and (ob[..., :5] == 7).all()
+
+
+@pytest.mark.parametrize("types", range(3))
+def test_replayed_in_a_graph_with_moved_lengths(types):
+    qdt, cdt, odt = TYPES[types]
+    pages = Pages([900, 333], 1, 128, 16, cdt)
+    q, ws = normal((4, 4, 128), qdt, 1), workspace(pages.cache, 4, qdt)
+    out = torch.zeros((4, 4, 128), dtype=odt, device=DEV)
+    batch = pages.batch([2, 2])
+    sps.sps_paged_attention(pages.cache, batch, q, out, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sps.sps_paged_attention(pages.cache, batch, q, out, ws)
+    for lens, starts in (([900, 333], [0, 2, 4]), ([2, 300], [0, 1, 4]), ([513, 129], [0, 4, 4]), ([1, 0], [0, 1, 1])):
+        batch.kv_len.copy_(torch.tensor(lens, dtype=torch.int32))
+        batch.q_start.copy_(torch.tensor(starts, dtype=torch.int32))
+        q.copy_(normal((4, 4, 128), qdt, lens[0]))
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        check_attention(out, None, q, [(k[:L], v[:L]) for (k, v), L in zip(pages.dense, lens)], [b - a for a, b in zip(starts, starts[1:])])
+    assert int(batch.status) == 0
+
+
+def test_two_streams_with_two_workspaces():
+    pages = [Pages([1500, 20], 2, 128, 16, BF16, seed=s) for s in (0, 1)]
+    qs = [normal((3, 8, 128), F32, s) for s in (0, 1)]
+    outs = [torch.zeros_like(q) for q in qs]
+    wss = [workspace(p.cache, 8, F32) for p in pages]
+    batches = [p.batch([2, 1]) for p in pages]
+    streams = [torch.cuda.Stream() for _ in pages]
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for i, s in enumerate(streams):
+            with torch.cuda.stream(s):
+                sps.sps_paged_attention(pages[i].cache, batches[i], qs[i], outs[i], wss[i])
+    torch.cuda.synchronize()
+    for i in range(2):
+        check_attention(outs[i], None, qs[i], pages[i].dense, [2, 1])
+
+
+@pytest.mark.parametrize("types", range(3))
+def test_offsets_past_32_bits(types):
+    """The pool holds more than 2^31 elements; the sequences' pages lie at both of its ends."""
+    qdt, cdt, odt = TYPES[types]
+    n_pages, page, d = (2 ** 31 + 2 ** 20) // (64 * 128), 64, 128
+    k = torch.empty((n_pages, 1, page, d), dtype=cdt, device=DEV)
+    v = torch.empty((n_pages, 1, page, d), dtype=cdt, device=DEV)
+    lens = [200, 130]
+    ids = [n_pages - 1, 0, n_pages - 2, 5, 3, n_pages - 3, 1]
+    table = torch.tensor([ids[:4], ids[4:] + [0]], dtype=torch.int32)
+    dense = []
+    for b, L in enumerate(lens):
+        kk, vv = normal((L, 1, d), cdt, b), normal((L, 1, d), cdt, b + 9)
+        j = torch.arange(L)
+        p, s = table[b, j // page].long().to(DEV), (j % page).to(DEV)
+        k[p, :, s], v[p, :, s] = kk, vv
+        dense.append((kk, vv))
+    cache = sps.PagedCache(k, v)
+    news = [3, 2]
+    batch = sps.PagedBatch(torch.tensor([0, 3, 5], dtype=torch.int32, device=DEV), torch.tensor(lens, dtype=torch.int32, device=DEV), table.to(DEV), max_q=3)
+    kn, vn = torch.cat([dense[0][0][-3:], dense[1][0][-2:]]), torch.cat([dense[0][1][-3:], dense[1][1][-2:]])
+    for b, n in ((0, 3), (1, 2)):
+        for i in range(n):
+            at = lens[b] - n + i
+            k[int(table[b, at // page]), :, at % page] = 0
+    sps.sps_paged_append(cache, batch, kn.contiguous(), vn.contiguous())
+    q = normal((5, 4, d), qdt, 3)
+    out = torch.empty((5, 4, d), dtype=odt, device=DEV)
+    sps.sps_paged_attention(cache, batch, q, out, workspace(cache, 4, qdt))
+    check_attention(out, None, q, dense, news)
+    del k, v, cache
+    torch.cuda.empty_cache()
+
+
+def test_a_large_batch_and_a_long_context_against_sums_over_chunks():
+    """Many sequences of one token each, and one context of 70 000 tokens: every element against 64 bits, per head."""
+    pages = Pages([1 + 7 * i for i in range(150)], 1, 64, 16, BF16)
+    run_attention(pages, [1] * 150, 2, BF16)
+    L = 70000
+    pages = Pages([L], 1, 128, 64, BF16)
+    run_attention(pages, [2], 2, F32)
