@@ -138,13 +138,16 @@ __device__ __forceinline__ WorkCursor cursor_begin(const PagedAttnArgs& a, int m
   const int lane = threadIdx.x & 31, B = a.s.B;
   WorkCursor c;
   c.valid = false;
-  long long total = 0;
+  long long total = 0, units0 = 0;
+  SeqGeom g0{};              // the first 32 sequences, kept for the second sweep
   bool cut = false;
   for (int b0 = 0; b0 < B; b0 += 32) {
     const int b = b0 + lane;
     SeqGeom g{};
     if (b < B) { g = paged_seq(a.s, b); cut = cut || (g.cut && g.nq > 0); }
-    total += warp_seq_units<NR, KT>(a, g, b < B);
+    const long long units = warp_seq_units<NR, KT>(a, g, b < B);
+    if (b0 == 0) { g0 = g; units0 = units; }
+    total += units;
   }
   if (cut && blockIdx.x == 0) paged_flag(a.s.status, SPS_PAGED_BAD_LENGTH);
 #pragma unroll
@@ -160,9 +163,13 @@ __device__ __forceinline__ WorkCursor cursor_begin(const PagedAttnArgs& a, int m
   long long base = 0;
   for (int b0 = 0; b0 < B; b0 += 32) {
     const int b = b0 + lane;
-    SeqGeom g{};
-    if (b < B) g = paged_seq(a.s, b);
-    const long long units = warp_seq_units<NR, KT>(a, g, b < B) * a.Hkv;
+    SeqGeom g = g0;
+    long long units = units0;
+    if (b0 > 0) {
+      if (b < B) g = paged_seq(a.s, b);
+      units = warp_seq_units<NR, KT>(a, g, b < B);
+    }
+    units *= a.Hkv;
     long long incl = units;
 #pragma unroll
     for (int o = 1; o < 32; o <<= 1) {
@@ -273,5 +280,7 @@ struct RotaryArgs {
 cudaError_t rotary_launch(RotaryArgs a, int x_bf16, int yq_bf16, int cache_bf16, int num_sm, cudaStream_t st);
 // CTAs of an attention launch on a device of num_sm SMs, at most (counters and slots are laid out for as many)
 inline int paged_attn_grid(int num_sm) { return num_sm < 1024 ? num_sm : 1024; }
-size_t paged_attn_slot_bytes(int dtype, int q_dtype, int d_head);
+size_t paged_attn_slot_bytes(int dtype, int d_head);
+size_t paged_attn_tc_slot_bytes(int d_head);
+cudaError_t paged_attn_tc_launch(const PagedAttnArgs& a, int d_head, int max_q, int num_sm, cudaStream_t st);
 cudaError_t paged_attn_launch(const PagedAttnArgs& a, int cache_bf16, int d_head, int max_q, int num_sm, cudaStream_t st);

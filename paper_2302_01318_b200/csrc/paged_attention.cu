@@ -1,4 +1,5 @@
-// Attention over a paged cache, one kernel for every cache type and batch (see paged.cuh for how the work is cut).
+// Attention over a paged fp32 cache (see paged.cuh for how the work is cut; a bf16 cache runs on the tensor cores,
+// paged_attention_tc.cu).
 //
 //   s_j = scale q . k_j,  m = max s_j,  l = sum 2^(s_j - m),  o = sum 2^(s_j - m) v_j / l     (scores in base 2)
 //
@@ -13,15 +14,7 @@ namespace {
 
 constexpr int SIMT_NR = 16, SIMT_KT = 64, SIMT_THREADS = 256;
 
-template <typename TC> __device__ __forceinline__ float4 cache4(const TC* p);
-template <> __device__ __forceinline__ float4 cache4<float>(const float* p) { return *reinterpret_cast<const float4*>(p); }
-template <> __device__ __forceinline__ float4 cache4<__nv_bfloat16>(const __nv_bfloat16* p) {
-  const uint2 u = *reinterpret_cast<const uint2*>(p);
-  const float2 a = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.x)), b = __bfloat1622float2(*reinterpret_cast<const __nv_bfloat162*>(&u.y));
-  return make_float4(a.x, a.y, b.x, b.y);
-}
-
-template <typename TC, int D>
+template <int D>
 __global__ void __launch_bounds__(SIMT_THREADS) paged_attn_simt_kernel(const __grid_constant__ PagedAttnArgs a) {
   constexpr int NR = SIMT_NR, KT = SIMT_KT, LDK = D + 4;
   constexpr int RPT = NR / (SIMT_THREADS / (D / 2));   // rows a thread accumulates (4 or 2)
@@ -52,7 +45,7 @@ __global__ void __launch_bounds__(SIMT_THREADS) paged_attn_simt_kernel(const __g
       float v = 0.f;
       if (rr < R) {
         const long long at = (long long)(c.row0 + rr / a.G) * a.q.row + (long long)(c.hk * a.G + rr % a.G) * a.q.head + e;
-        v = a.q_bf16 ? __bfloat162float(reinterpret_cast<const __nv_bfloat16*>(a.q.p)[at]) : reinterpret_cast<const float*>(a.q.p)[at];
+        v = reinterpret_cast<const float*>(a.q.p)[at];
       }
       Qs[i] = v * a.scale_log2;
     }
@@ -75,8 +68,8 @@ __global__ void __launch_bounds__(SIMT_THREADS) paged_attn_simt_kernel(const __g
           const int page = a.s.pages[(long long)c.b * a.s.pages_ld + (pos >> a.s.page_shift)];
           if (page >= 0 && page < a.s.n_pages) {
             const long long at = page * a.page_stride + c.hk * a.head_stride + (pos & (a.s.page_size - 1)) * a.pos_stride + e;
-            k = cache4<TC>(reinterpret_cast<const TC*>(a.k) + at);
-            v = cache4<TC>(reinterpret_cast<const TC*>(a.v) + at);
+            k = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.k) + at);
+            v = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.v) + at);
           } else {
             paged_flag(a.s.status, SPS_PAGED_BAD_PAGE);
           }
@@ -182,24 +175,23 @@ __global__ void __launch_bounds__(SIMT_THREADS) paged_attn_simt_kernel(const __g
   }
 }
 
-template <typename TC, int D>
+template <int D>
 cudaError_t simt_go(const PagedAttnArgs& a, int num_sm, cudaStream_t st) {
   static DevSmemCache cached{};
   constexpr size_t smem = sizeof(float) * (SIMT_KT * (D + 4) + SIMT_KT * D + SIMT_NR * D + SIMT_NR * SIMT_KT);
-  const cudaError_t e = sps_ensure_smem(paged_attn_simt_kernel<TC, D>, smem, cached);
+  const cudaError_t e = sps_ensure_smem(paged_attn_simt_kernel<D>, smem, cached);
   if (e != cudaSuccess) return e;
-  return launch_k(paged_attn_simt_kernel<TC, D>, dim3(paged_attn_grid(num_sm)), dim3(SIMT_THREADS), smem, st, a);
+  return launch_k(paged_attn_simt_kernel<D>, dim3(paged_attn_grid(num_sm)), dim3(SIMT_THREADS), smem, st, a);
 }
 
 }  // namespace
 
-size_t paged_attn_slot_bytes(int dtype, int q_dtype, int d_head) {
-  (void)dtype; (void)q_dtype;
+size_t paged_attn_slot_bytes(int dtype, int d_head) {
+  if (dtype == 1) return paged_attn_tc_slot_bytes(d_head);
   return sizeof(float) * (d_head == 128 ? slot_floats<SIMT_NR, 128>() : slot_floats<SIMT_NR, 64>());
 }
 
 cudaError_t paged_attn_launch(const PagedAttnArgs& a, int cache_bf16, int d_head, int max_q, int num_sm, cudaStream_t st) {
-  (void)max_q;
-  if (cache_bf16) return d_head == 128 ? simt_go<__nv_bfloat16, 128>(a, num_sm, st) : simt_go<__nv_bfloat16, 64>(a, num_sm, st);
-  return d_head == 128 ? simt_go<float, 128>(a, num_sm, st) : simt_go<float, 64>(a, num_sm, st);
+  if (cache_bf16) return paged_attn_tc_launch(a, d_head, max_q, num_sm, st);
+  return d_head == 128 ? simt_go<128>(a, num_sm, st) : simt_go<64>(a, num_sm, st);
 }

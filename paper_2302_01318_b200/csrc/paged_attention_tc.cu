@@ -1,0 +1,657 @@
+// Attention over a paged bf16 cache on the 5th-generation tensor cores, for few query rows per key head (a decode step, a
+// scoring pass of K + 1 rows, their grouped heads) and for fp32 queries of any number.
+//
+// The tokens are the tensor cores' 128-row operand in both products, the query rows their narrow one:
+//
+//   S^T [128 tokens x NR rows]   = K [128 x d] Q^T              (K straight from the page copies, K-major)
+//   O^T [d x NR rows]           += V^T [d x 128] P^T            (V straight from the page copies, MN-major)
+//
+// so keys and values go from HBM to shared memory to the tensor cores and through no register, and a decode step of one
+// row costs a product 16 columns wide instead of 128.  A thread owns one token of the tile (a lane of tensor memory) and
+// all its rows' scores; it masks, exponentiates and stores its row of P^T.
+//
+// Running maximum.  The weights are 2^(s - m) with m fixed at the maximum of the part's first tile: P is bf16 (8 exponent
+// bits) or three bf16 parts of an fp32 number, sums are fp32, so m only has to keep the weights in range, not at most 1.
+// Only when a score exceeds m by 2^MAX_UP do the CTA's threads agree (a reducing barrier) to take the new maximum and
+// rescale sums and O^T.  That leaves a multiply-add, an exponential, an addition and the rounding per score, no
+// cross-lane reduction per tile.  Sums stay per thread (its token of every tile) until the part ends.
+//
+// Types.  bf16 queries: P rounds once to bf16 (2^-8 relative, and the sum is taken of the rounded weights).  fp32 queries:
+// Q and P enter as three bf16 parts (high, rest, rest of the rest: 24 bits), three products each, added up in fp32.
+//
+// What bounds it: HBM.  A tile of 128 tokens is 64 KB of keys and values (d = 128), 2760 clocks of an SM's share of
+// 6.5 TB/s; its products take 8 x 32 clocks each for 16 rows (x 3 for fp32), the softmax a few hundred.  One CTA per SM,
+// equal runs of tiles per CTA (paged.cuh), a ring of 4 to 6 half-tiles (K or V) of 32 KB in flight.
+//
+//   warp 0      copies: lane i asks for page i of the tile (TMA boxes of 64 elements x up to 128 slots, 128-byte swizzle)
+//   warp 1      one lane issues the products: S of tile i + 1 goes before O of tile i, so the softmax never waits
+//   warps 2..   softmax, 128 tokens x NR rows by 4 warps (16 rows) or 8 (two groups of columns)
+//
+// Every wait is bounded; on expiry the CTA sets SPS_PAGED_TIMEOUT, lets its copies and products finish, frees its tensor
+// memory and returns.
+#include <cuda.h>
+#include <cudaTypedefs.h>
+
+#include <mutex>
+
+#include "paged.cuh"
+
+namespace {
+
+constexpr int TILE = 128;            // tokens per tile
+constexpr float MAX_UP = 24.f;       // log2 of the largest weight that is let stand
+
+struct TcArgs {
+  CUtensorMap tm_k, tm_v;
+  PagedAttnArgs a;
+  int box;             // slots per copy: min(page_size, 128)
+  int head_first;      // the tensor maps' dimensions are (d, head, slot, page) instead of (d, slot, head, page)
+  int min_run;
+};
+
+__device__ __forceinline__ uint32_t p_smem(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
+__device__ __forceinline__ void p_bar_init(uint32_t bar, uint32_t count) { asm volatile("mbarrier.init.shared::cta.b64 [%0], %1;" ::"r"(bar), "r"(count) : "memory"); }
+__device__ __forceinline__ void p_arrive(uint32_t bar) { asm volatile("mbarrier.arrive.shared::cta.b64 _, [%0];" ::"r"(bar) : "memory"); }
+__device__ __forceinline__ void p_expect(uint32_t bar, uint32_t bytes) {
+  asm volatile("mbarrier.arrive.expect_tx.shared::cta.b64 _, [%0], %1;" ::"r"(bar), "r"(bytes) : "memory");
+}
+__device__ __forceinline__ uint32_t p_try(uint32_t bar, uint32_t parity) {
+  uint32_t ok;
+  asm volatile("{\n .reg .pred p;\n mbarrier.try_wait.parity.shared::cta.b64 p, [%1], %2, %3;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(ok) : "r"(bar), "r"(parity), "r"(1000u) : "memory");
+  return ok;
+}
+__device__ __forceinline__ unsigned long long p_timer() {
+  unsigned long long t;
+  asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
+  return t;
+}
+// bounded wait: false after wait_ns, or as soon as another thread of the CTA gave up
+__device__ __forceinline__ bool p_wait(uint32_t bar, uint32_t parity, unsigned long long wait_ns, int32_t* status, volatile int* abort_flag) {
+  if (p_try(bar, parity)) return true;
+  const unsigned long long t0 = p_timer();
+  for (;;) {
+#pragma unroll 1
+    for (int i = 0; i < 64; ++i) {
+      if (p_try(bar, parity)) return true;
+      if (*abort_flag) return false;
+    }
+    if (p_timer() - t0 > wait_ns) {
+      paged_flag(status, SPS_PAGED_TIMEOUT);
+      *abort_flag = 1;
+      return false;
+    }
+  }
+}
+__device__ __forceinline__ void p_copy(uint32_t dst, const CUtensorMap* tm, int c0, int c1, int c2, int c3, uint32_t bar) {
+  asm volatile("cp.async.bulk.tensor.4d.shared::cluster.global.tile.mbarrier::complete_tx::bytes [%0], [%1, {%2, %3, %4, %5}], [%6];" ::"r"(dst), "l"(tm),
+               "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar)
+               : "memory");
+}
+// shared-memory operand descriptor: layout 2 / 4 / 6 = 128- / 64- / 32-byte swizzle; sbo: bytes between groups of 8 rows,
+// lbo: bytes between 64-element blocks along the contiguous (MN) direction, unused for K-major operands
+__device__ __forceinline__ uint64_t p_desc(uint32_t addr, uint32_t lbo, uint32_t sbo, uint32_t layout) {
+  return (uint64_t)((addr & 0x3ffffu) >> 4) | (uint64_t)((lbo >> 4) & 0x3fffu) << 16 | (uint64_t)(sbo >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)layout << 61;
+}
+__device__ __forceinline__ void p_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+}
+__device__ __forceinline__ void p_commit(uint32_t bar) {
+  asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
+}
+#define P_FENCE_AFTER() asm volatile("tcgen05.fence::after_thread_sync;" ::: "memory")
+#define P_FENCE_BEFORE() asm volatile("tcgen05.fence::before_thread_sync;" ::: "memory")
+
+__device__ __forceinline__ void p_ld16(uint32_t t, float* v) {
+  uint32_t r[16];
+  asm volatile("tcgen05.ld.sync.aligned.32x32b.x16.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+               : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]),
+                 "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15])
+               : "r"(t)
+               : "memory");
+#pragma unroll
+  for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
+}
+__device__ __forceinline__ void p_st16(uint32_t t, const float* v) {
+  uint32_t r[16];
+#pragma unroll
+  for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(v[i]);
+  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]),
+               "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(t)
+               : "memory");
+}
+#define P_WAIT_LD() asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory")
+#define P_WAIT_ST() asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory")
+
+__device__ __forceinline__ float p_ex2(float x) {
+  float y;
+  asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
+  return y;
+}
+// two floats rounded to bf16, the first in the low half
+__device__ __forceinline__ uint32_t p_pack(float lo, float hi) {
+  uint32_t r;
+  asm("cvt.rn.bf16x2.f32 %0, %1, %2;" : "=r"(r) : "f"(hi), "f"(lo));
+  return r;
+}
+__device__ __forceinline__ float p_lo(uint32_t u) { return __uint_as_float(u << 16); }
+__device__ __forceinline__ float p_hi(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
+
+// Reduces v[c] over the 32 lanes for N columns (16 or 32), halving the columns a lane carries at every step; the lane ends
+// up with column lane >> 1 (16 columns) or lane (32).
+struct OpMax { static __device__ __forceinline__ float f(float a, float b) { return fmaxf(a, b); } };
+struct OpAdd { static __device__ __forceinline__ float f(float a, float b) { return a + b; } };
+template <class Op, int N> __device__ __forceinline__ float fold(float (&v)[N], int lane) {
+  int off = 16;
+#pragma unroll
+  for (int w = N / 2; w >= 1; w >>= 1, off >>= 1) {
+    const bool upper = (lane & off) != 0;
+#pragma unroll
+    for (int k = 0; k < w; ++k) {
+      const float send = upper ? v[k] : v[k + w], keep = upper ? v[k + w] : v[k];
+      v[k] = Op::f(keep, __shfl_xor_sync(0xffffffffu, send, off));
+    }
+  }
+  if (N == 16) v[0] = Op::f(v[0], __shfl_xor_sync(0xffffffffu, v[0], 1));
+  return v[0];
+}
+
+template <int D, int NR, int PARTS> struct Cfg {
+  static constexpr int GROUPS = NR == 16 ? 1 : 2;                   // column groups of four softmax warps each
+  static constexpr int COLS = NR / GROUPS;
+  static constexpr int SOFT = 128 * GROUPS;                         // softmax threads
+  static constexpr int THREADS = 64 + SOFT;
+  static constexpr uint32_t HALF = TILE * D * 2;                    // keys or values of a tile
+  static constexpr uint32_t QPART = NR * D * 2, PPART = TILE * NR * 2;
+  static constexpr uint32_t FIXED = PARTS * (QPART + PPART);
+  static constexpr uint32_t HDR = 2304;                             // barriers, small per-row arrays
+  static constexpr int STAGES_FIT = (232448 - (int)HDR - (int)FIXED) / (int)HALF;
+  static constexpr int STAGES = (STAGES_FIT > 8 ? 8 : STAGES_FIT) & ~1;   // even: K and V take turns
+  static constexpr size_t SMEM = FIXED + (size_t)STAGES * HALF + HDR;
+  static constexpr uint32_t TMEM = NR == 16 ? 64 : (NR == 32 ? 128 : 256);
+  // P^T is the B operand, MN-major: a token's NR weights side by side
+  static constexpr uint32_t P_ROW = NR >= 64 ? 128 : NR * 2;
+  static constexpr uint32_t P_LAYOUT = NR >= 64 ? 2 : (NR == 32 ? 4 : 6);
+  // kind::f16 instruction descriptors: fp32 accumulator, bf16 x bf16; S: both K-major, M = 128; O: both MN-major, M = d
+  static constexpr uint32_t IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(NR >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24);
+  static constexpr uint32_t IDESC_O = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(NR >> 3) << 17) | ((uint32_t)(D >> 4) << 24);
+  static_assert(STAGES >= 4, "ring too short");
+};
+
+template <int D, int NR, int PARTS>
+__global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_kernel(const __grid_constant__ TcArgs ta) {
+  using C = Cfg<D, NR, PARTS>;
+  constexpr int COLS = C::COLS, SOFT = C::SOFT, STAGES = C::STAGES;
+  extern __shared__ __align__(1024) unsigned char mem[];   // the ring, Q, P^T (swizzled operands: 1024-byte aligned), header
+  const PagedAttnArgs& a = ta.a;
+  const uint32_t ring = p_smem(mem), q_s = ring + STAGES * C::HALF, p_s = q_s + PARTS * C::QPART;
+  unsigned char* hdr = mem + STAGES * C::HALF + C::FIXED;
+  const uint32_t hb = p_smem(hdr);
+  const uint32_t full = hb, empty = hb + 64, s_full = hb + 128, s_free = hb + 144, p_full = hb + 160, pv_done = hb + 168, q_ready = hb + 176, drain = hb + 184;
+  volatile uint32_t* s_tmem = reinterpret_cast<volatile uint32_t*>(hdr + 192);
+  volatile int* s_abort = reinterpret_cast<volatile int*>(hdr + 196);
+  int* s_poison = reinterpret_cast<int*>(hdr + 200);
+  int* s_last = reinterpret_cast<int*>(hdr + 204);
+  WorkCursor* s_cur = reinterpret_cast<WorkCursor*>(hdr + 208);       // 96 bytes at most
+  int* s_lim = reinterpret_cast<int*>(hdr + 384);                      // [NR] last position a row sees
+  float* s_a = reinterpret_cast<float*>(hdr + 384 + NR * 4);           // [NR] maxima, and scratch of the join
+  float* s_b = s_a + NR;                                               // [NR] sums / factors
+  float* s_red = s_b + NR;                                             // [4][NR]
+  static_assert(384 + NR * 4 * 7 <= (int)C::HDR && sizeof(WorkCursor) <= 176, "header");
+  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+
+  if (tid == 0) {
+    for (int i = 0; i < STAGES; ++i) { p_bar_init(full + 8 * i, 1); p_bar_init(empty + 8 * i, 1); }
+    for (int i = 0; i < 2; ++i) { p_bar_init(s_full + 8 * i, 1); p_bar_init(s_free + 8 * i, SOFT); }
+    p_bar_init(p_full, SOFT); p_bar_init(pv_done, 1); p_bar_init(q_ready, SOFT); p_bar_init(drain, 1);
+    *s_abort = 0;
+    asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&ta.tm_k) : "memory");
+    asm volatile("prefetch.tensormap [%0];" ::"l"(&ta.tm_v) : "memory");
+  }
+  if (warp == 1) {
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(hb + 192), "n"(C::TMEM) : "memory");
+    asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+  }
+  pdl_launch_dependents();
+  pdl_wait();
+  if (warp == 0) {
+    const WorkCursor c0 = cursor_begin<NR, TILE>(a, ta.min_run);
+    if (lane == 0) *s_cur = c0;
+  }
+  P_FENCE_BEFORE();
+  __syncthreads();
+  P_FENCE_AFTER();
+  const uint32_t tmem = *s_tmem, tmem_o = tmem + 2 * NR;
+  WorkCursor c = *s_cur;
+
+  if (warp == 0) {
+    // ---------------------------------------------------------------------------------------------------- copies
+    bool ok = true;
+    int it = 0;   // half-tiles asked for so far
+    const int boxes = TILE / ta.box;
+    while (c.valid && ok) {
+      const int32_t* table = a.s.pages + (long long)c.b * a.s.pages_ld;
+      for (int kt = c.k0; kt < c.k1 && ok; ++kt) {
+        const int p0 = kt * TILE, pos = p0 + lane * ta.box;
+        const bool mine = lane < boxes && pos < c.len;
+        int page = 0;
+        if (mine) {
+          page = table[pos >> a.s.page_shift];
+          if (page < 0 || page >= a.s.n_pages) { paged_flag(a.s.status, SPS_PAGED_BAD_PAGE); page = a.s.n_pages; }   // outside the map: zeros
+        }
+        const int in_page = pos & (a.s.page_size - 1);
+        const int n = __popc(__ballot_sync(0xffffffffu, mine));
+#pragma unroll
+        for (int kv = 0; kv < 2; ++kv, ++it) {
+          const int slot = it % STAGES, use = it / STAGES;
+          if (use > 0) {
+            ok = p_wait(empty + 8 * slot, (uint32_t)(use - 1) & 1u, a.wait_ns, a.s.status, s_abort);
+            ok = __all_sync(0xffffffffu, ok) && !*s_abort;
+            if (!ok) break;
+          }
+          if (lane == 0) {
+            if (n > 0) p_expect(full + 8 * slot, (uint32_t)n * (uint32_t)ta.box * (uint32_t)(D * 2));
+            else p_arrive(full + 8 * slot);
+          }
+          __syncwarp();
+          if (mine) {
+            const CUtensorMap* tm = kv ? &ta.tm_v : &ta.tm_k;
+            const uint32_t dst = ring + slot * C::HALF + (uint32_t)(lane * ta.box) * 128u;
+#pragma unroll
+            for (int ch = 0; ch < D / 64; ++ch)
+              p_copy(dst + ch * (TILE * 128), tm, ch * 64, ta.head_first ? c.hk : in_page, ta.head_first ? in_page : c.hk, page, full + 8 * slot);
+          }
+          __syncwarp();
+        }
+      }
+      cursor_next<NR, TILE>(a, c);
+    }
+    if (lane == 0) {   // whatever happened, the copies in flight land before this CTA's shared memory goes away
+      if (!ok) *s_abort = 1;
+      for (int j = max(0, it - STAGES); j < it; ++j) {
+        const unsigned long long t0 = p_timer();
+        while (!p_try(full + 8 * (j % STAGES), (uint32_t)(j / STAGES) & 1u) && p_timer() - t0 <= a.wait_ns) {}
+      }
+    }
+  } else if (warp == 1) {
+    // ---------------------------------------------------------------------------------------------------- products
+    if (lane == 0) {
+      bool ok = true;
+      int it = 0, sn = 0, pn = 0, qn = 0;   // half-tiles, score products, output products, parts so far
+      auto score = [&](int e) {             // S of the tile whose keys are half-tile e
+        const int buf = sn & 1;
+        if (sn >= 2) ok = ok && p_wait(s_free + 8 * buf, (uint32_t)((sn >> 1) - 1) & 1u, a.wait_ns, a.s.status, s_abort);
+        ok = ok && p_wait(full + 8 * (e % STAGES), (uint32_t)(e / STAGES) & 1u, a.wait_ns, a.s.status, s_abort);
+        if (!ok) return;
+        P_FENCE_AFTER();
+        const uint32_t k_at = ring + (uint32_t)(e % STAGES) * C::HALF;
+        uint32_t acc = 0;
+#pragma unroll
+        for (int part = PARTS - 1; part >= 0; --part)      // smallest parts first
+#pragma unroll
+          for (int ch = 0; ch < D / 64; ++ch) {
+            const uint64_t da = p_desc(k_at + ch * (TILE * 128), 16, 1024, 2), db = p_desc(q_s + part * C::QPART + ch * (NR * 128), 16, 1024, 2);
+#pragma unroll
+            for (int k = 0; k < 4; ++k) { p_mma(tmem + buf * NR, da + 2 * k, db + 2 * k, C::IDESC_S, acc); acc = 1; }
+          }
+        p_commit(empty + 8 * (e % STAGES));
+        p_commit(s_full + 8 * buf);
+        ++sn;
+      };
+      while (c.valid && ok) {
+        const int n = c.k1 - c.k0;
+        ok = p_wait(q_ready, (uint32_t)qn & 1u, a.wait_ns, a.s.status, s_abort);
+        ++qn;
+        if (ok) score(it);
+        for (int i = 0; i < n && ok; ++i, it += 2) {
+          if (i + 1 < n) score(it + 2);
+          const int e = it + 1;
+          ok = ok && p_wait(p_full, (uint32_t)pn & 1u, a.wait_ns, a.s.status, s_abort);
+          ok = ok && p_wait(full + 8 * (e % STAGES), (uint32_t)(e / STAGES) & 1u, a.wait_ns, a.s.status, s_abort);
+          if (!ok) break;
+          P_FENCE_AFTER();
+          const uint32_t v_at = ring + (uint32_t)(e % STAGES) * C::HALF;
+          uint32_t acc = i > 0 ? 1u : 0u;
+#pragma unroll
+          for (int part = PARTS - 1; part >= 0; --part) {
+            const uint64_t da = p_desc(v_at, TILE * 128, 1024, 2), db = p_desc(p_s + part * C::PPART, 16, 8 * C::P_ROW, C::P_LAYOUT);
+#pragma unroll
+            for (int k = 0; k < TILE / 16; ++k) { p_mma(tmem_o, da + k * (16 * 128 >> 4), db + k * (16 * C::P_ROW >> 4), C::IDESC_O, acc); acc = 1; }
+          }
+          p_commit(empty + 8 * (e % STAGES));
+          p_commit(pv_done);
+          ++pn;
+        }
+        cursor_next<NR, TILE>(a, c);
+      }
+      if (!ok) {   // every product issued so far must be done before the ring and the tensor memory go away
+        *s_abort = 1;
+        p_commit(drain);
+        const unsigned long long t0 = p_timer();
+        while (!p_try(drain, 0u) && p_timer() - t0 <= a.wait_ns) {}
+      }
+    }
+  } else {
+    // ---------------------------------------------------------------------------------------------------- softmax
+    const int st = tid - 64, quarter = warp & 3, group = (warp - 2) >> 2, col0 = group * COLS;
+    const int my = quarter * 32 + lane;                       // token of the tile, and row of O^T (for d = 128)
+    const uint32_t t_lane = (uint32_t)(quarter * 32) << 16;
+    const int my_col = COLS == 32 ? lane : lane >> 1;         // the column a fold leaves here
+    // After a wait that ran out the softmax threads keep their common path -- barriers among them always meet -- and skip
+    // the waits, until they agree at the part's end to stop.
+    bool ok = true;
+    int sn = 0, pn = 0, it = 0;
+    auto soft_sync = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(SOFT) : "memory"); };
+    while (c.valid) {
+      const int R = c.nq * a.G, r0 = c.t * NR, n = c.k1 - c.k0, first_lim = c.len - c.nq + r0 / a.G;
+      // ---- Q, in PARTS bf16 parts, K-major: row r of block ch at r * 128, its 16-byte chunk k at chunk k ^ (r & 7)
+      for (int i = st; i < NR * (D / 8); i += SOFT) {
+        const int r = i / (D / 8), k8 = i - r * (D / 8), rr = r0 + r;
+        float f[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) f[j] = 0.f;
+        if (rr < R) {
+          const long long at = (long long)(c.row0 + rr / a.G) * a.q.row + (long long)(c.hk * a.G + rr % a.G) * a.q.head + k8 * 8;
+          if (PARTS == 3) {
+            const float* p = reinterpret_cast<const float*>(a.q.p) + at;
+            if (a.q_vec) {
+              const float4 x = *reinterpret_cast<const float4*>(p), y = *reinterpret_cast<const float4*>(p + 4);
+              f[0] = x.x; f[1] = x.y; f[2] = x.z; f[3] = x.w; f[4] = y.x; f[5] = y.y; f[6] = y.z; f[7] = y.w;
+            } else {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) f[j] = p[j];
+            }
+          } else {
+            const __nv_bfloat16* p = reinterpret_cast<const __nv_bfloat16*>(a.q.p) + at;
+            if (a.q_vec) {
+              const uint4 u = *reinterpret_cast<const uint4*>(p);
+              const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+              for (int j = 0; j < 4; ++j) { f[2 * j] = p_lo(w[j]); f[2 * j + 1] = p_hi(w[j]); }
+            } else {
+#pragma unroll
+              for (int j = 0; j < 8; ++j) f[j] = __bfloat162float(p[j]);
+            }
+          }
+        }
+        unsigned char* dst = mem + STAGES * C::HALF + (k8 >> 3) * (NR * 128) + r * 128 + (((k8 & 7) ^ (r & 7)) << 4);
+#pragma unroll
+        for (int part = 0; part < PARTS; ++part) {
+          uint32_t u[4];
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            u[j] = p_pack(f[2 * j], f[2 * j + 1]);
+            if (part + 1 < PARTS) { f[2 * j] -= p_lo(u[j]); f[2 * j + 1] -= p_hi(u[j]); }
+          }
+          *reinterpret_cast<uint4*>(dst + part * C::QPART) = make_uint4(u[0], u[1], u[2], u[3]);
+        }
+      }
+      if (st < NR) s_lim[st] = r0 + st < R ? c.len - c.nq + (r0 + st) / a.G : -1;
+      if (st == 0) *s_poison = 0x7fffffff;
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      p_arrive(q_ready);
+      soft_sync();
+      float m[COLS], l[COLS];
+#pragma unroll
+      for (int j = 0; j < COLS; ++j) { m[j] = 0.f; l[j] = 0.f; }
+      for (int i = 0; i < n; ++i, ++sn, it += 2) {
+        const int buf = sn & 1, p0 = (c.k0 + i) * TILE, pos = p0 + my;
+        const bool edge = p0 + TILE - 1 > first_lim;          // some row does not see all of this tile
+        ok = ok && p_wait(s_full + 8 * buf, (uint32_t)(sn >> 1) & 1u, a.wait_ns, a.s.status, s_abort);
+        __syncwarp();
+        P_FENCE_AFTER();
+        float x[COLS];
+#pragma unroll
+        for (int j = 0; j < COLS; j += 16) p_ld16(tmem + buf * NR + t_lane + col0 + j, x + j);
+        P_WAIT_LD();
+        P_FENCE_BEFORE();
+        p_arrive(s_free + 8 * buf);
+        // ---- the reference maximum: the first tile's, later only when a score has outgrown it
+        bool retake = i == 0;
+        if (i > 0) {
+          float up = -INFINITY;
+          if (edge) {
+#pragma unroll
+            for (int j = 0; j < COLS; ++j) up = fmaxf(up, pos <= s_lim[col0 + j] ? fmaf(x[j], a.scale_log2, -m[j]) : -INFINITY);
+          } else {
+#pragma unroll
+            for (int j = 0; j < COLS; ++j) up = fmaxf(up, fmaf(x[j], a.scale_log2, -m[j]));
+          }
+          uint32_t any;
+          asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.or.pred p, 1, %2, q;\n selp.u32 %0, 1, 0, p;\n}\n"
+                       : "=r"(any) : "r"(up > MAX_UP ? 1u : 0u), "n"(SOFT) : "memory");
+          retake = any != 0;
+        }
+        if (retake) {
+          float y[COLS];
+#pragma unroll
+          for (int j = 0; j < COLS; ++j) y[j] = pos <= s_lim[col0 + j] ? x[j] * a.scale_log2 : -INFINITY;
+          const float top = fold<OpMax, COLS>(y, lane);
+          s_red[quarter * NR + col0 + my_col] = top;
+          soft_sync();
+#pragma unroll
+          for (int j = 0; j < COLS; ++j) {
+            const int cc = col0 + j;
+            const float t = fmaxf(fmaxf(s_red[cc], s_red[NR + cc]), fmaxf(s_red[2 * NR + cc], s_red[3 * NR + cc]));
+            if (i == 0) {
+              m[j] = t == -INFINITY ? 0.f : t;                // a row that sees nothing here sees nothing in this part
+            } else {
+              const float nm = fmaxf(m[j], t), al = p_ex2(m[j] - nm);
+              l[j] *= al;
+              m[j] = nm;
+              if (my == 0) s_b[cc] = al;
+            }
+          }
+          if (i > 0) {
+            // O^T takes the factors: every product so far must be in it
+            ok = ok && p_wait(pv_done, (uint32_t)(pn - 1) & 1u, a.wait_ns, a.s.status, s_abort);
+            soft_sync();
+            P_FENCE_AFTER();
+#pragma unroll
+            for (int j = 0; j < COLS; j += 16) {
+              float o[16];
+              p_ld16(tmem_o + t_lane + col0 + j, o);
+              P_WAIT_LD();
+#pragma unroll
+              for (int q = 0; q < 16; ++q) o[q] *= s_b[col0 + j + q];
+              p_st16(tmem_o + t_lane + col0 + j, o);
+            }
+            P_WAIT_ST();
+            P_FENCE_BEFORE();
+          }
+          soft_sync();   // s_red and s_b may be written again
+        }
+        // ---- weights
+        if (edge) {
+#pragma unroll
+          for (int j = 0; j < COLS; ++j) x[j] = pos <= s_lim[col0 + j] ? p_ex2(fmaf(x[j], a.scale_log2, -m[j])) : 0.f;
+        } else {
+#pragma unroll
+          for (int j = 0; j < COLS; ++j) x[j] = p_ex2(fmaf(x[j], a.scale_log2, -m[j]));
+        }
+        if (PARTS == 3) {
+#pragma unroll
+          for (int j = 0; j < COLS; ++j) l[j] += x[j];
+        }
+        // P^T and, at the edge, V are written once the previous output product has read P^T
+        if (pn > 0) ok = ok && p_wait(pv_done, (uint32_t)(pn - 1) & 1u, a.wait_ns, a.s.status, s_abort);
+        if (edge) {
+          // slots behind the sequence hold anything: zero (0 x NaN is NaN in a product).  New tokens some rows do not see:
+          // a value that is not finite is taken out and remembered, its rows become NaN at the end.
+          const int e = it + 1;
+          ok = ok && p_wait(full + 8 * (e % STAGES), (uint32_t)(e / STAGES) & 1u, a.wait_ns, a.s.status, s_abort);
+          if (ok && group == 0 && pos > first_lim) {
+            unsigned char* vr = mem + (e % STAGES) * C::HALF + my * 128;
+            bool clear = pos >= c.len;
+            if (!clear) {
+#pragma unroll
+              for (int ch = 0; ch < D / 64; ++ch)
+#pragma unroll 2
+                for (int q = 0; q < 8; ++q) {
+                  const uint4 u = *reinterpret_cast<const uint4*>(vr + ch * (TILE * 128) + ((q ^ (my & 7)) << 4));
+                  const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+                  for (int z = 0; z < 4; ++z) clear = clear || (w[z] & 0x7f80u) == 0x7f80u || (w[z] & 0x7f800000u) == 0x7f800000u;
+                }
+              if (clear) atomicMin(s_poison, pos);
+            }
+            if (clear) {
+#pragma unroll
+              for (int ch = 0; ch < D / 64; ++ch)
+#pragma unroll 2
+                for (int q = 0; q < 8; ++q) *reinterpret_cast<uint4*>(vr + ch * (TILE * 128) + (q << 4)) = make_uint4(0, 0, 0, 0);
+            }
+          }
+        }
+        unsigned char* pr = mem + STAGES * C::HALF + PARTS * C::QPART + my * C::P_ROW;
+        const int sw = NR >= 64 ? my & 7 : (NR == 32 ? (my >> 1) & 3 : (my >> 2) & 1);
+#pragma unroll
+        for (int k = 0; k < COLS / 8; ++k) {
+          unsigned char* dst = pr + (((col0 / 8 + k) ^ sw) << 4);
+#pragma unroll
+          for (int part = 0; part < PARTS; ++part) {
+            uint32_t u[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              float &f0 = x[8 * k + 2 * j], &f1 = x[8 * k + 2 * j + 1];
+              u[j] = p_pack(f0, f1);
+              if (PARTS == 1) { l[8 * k + 2 * j] += p_lo(u[j]); l[8 * k + 2 * j + 1] += p_hi(u[j]); }
+              if (part + 1 < PARTS) { f0 -= p_lo(u[j]); f1 -= p_hi(u[j]); }
+            }
+            *reinterpret_cast<uint4*>(dst + part * C::PPART) = make_uint4(u[0], u[1], u[2], u[3]);
+          }
+        }
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+        P_FENCE_BEFORE();
+        p_arrive(p_full);
+        ++pn;
+      }
+      // ---- the part's end: sums over the tokens, then O^T
+#pragma unroll
+      for (int j = 0; j < COLS; ++j) if (my == 0) s_a[col0 + j] = m[j];
+      const float sum = fold<OpAdd, COLS>(l, lane);
+      s_red[quarter * NR + col0 + my_col] = sum;
+      ok = ok && p_wait(pv_done, (uint32_t)(pn - 1) & 1u, a.wait_ns, a.s.status, s_abort);
+      {
+        uint32_t all;
+        asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.and.pred p, 1, %2, q;\n selp.u32 %0, 1, 0, p;\n}\n"
+                     : "=r"(all) : "r"(ok ? 1u : 0u), "n"(SOFT) : "memory");
+        if (!all) break;
+      }
+      if (st < NR) {
+        float t = (s_red[st] + s_red[NR + st]) + (s_red[2 * NR + st] + s_red[3 * NR + st]);
+        if (s_lim[st] >= *s_poison) t = __int_as_float(0x7fffffff);
+        s_b[st] = t;
+        if (t == 0.f) s_a[st] = -INFINITY;
+      }
+      soft_sync();
+      int first, parts;
+      item_ctas(c, first, parts);
+      P_FENCE_AFTER();
+      const int e = D == 128 ? my : quarter * 16 + lane;      // element of the head (d = 64: 16 rows in each quarter's first 16 lanes)
+      const bool live_lane = D == 128 || lane < 16;
+      float* slot = a.slots + slot_floats<NR, D>() * (size_t)part_slot(blockIdx.x, c.k0 == 0);
+#pragma unroll 1
+      for (int j = 0; j < COLS; j += 16) {
+        float o[16];
+        p_ld16(tmem_o + t_lane + col0 + j, o);
+        P_WAIT_LD();
+#pragma unroll
+        for (int q = 0; q < 16; ++q) {
+          const int r = col0 + j + q, rr = r0 + r;
+          if (rr >= R || !live_lane) continue;
+          if (parts == 1) {
+            const float t = s_b[r];
+            store_out(a, (long long)(c.row0 + rr / a.G) * a.out.row + (long long)(c.hk * a.G + rr % a.G) * a.out.head + e, t == 0.f ? 0.f : o[q] * (1.f / t));
+          } else {
+            __stcg(slot + 2 * NR + r * D + e, o[q]);
+          }
+        }
+      }
+      P_FENCE_BEFORE();
+      if (parts == 1) {
+        if (a.lse && st < NR && r0 + st < R) {
+          const int rr = r0 + st;
+          a.lse[(size_t)(c.row0 + rr / a.G) * a.H + c.hk * a.G + rr % a.G] = s_b[st] == 0.f ? -INFINITY : 0.6931471805599453f * (s_a[st] + log2f(s_b[st]));
+        }
+      } else {
+        if (st < NR) { __stcg(slot + st, s_a[st]); __stcg(slot + NR + st, s_b[st]); }
+        __threadfence();
+        soft_sync();
+        if (st == 0) {
+          *s_last = atomicAdd(a.counters + first, 1) == parts - 1;
+          if (*s_last) { a.counters[first] = 0; __threadfence(); }
+        }
+        soft_sync();
+        if (*s_last) join_parts<NR, D, SOFT>(a, c, first, parts, st, s_b, s_a);
+      }
+      soft_sync();   // s_a, s_b, s_lim are free again
+      cursor_next<NR, TILE>(a, c);
+    }
+    if (!ok) *s_abort = 1;
+  }
+  P_FENCE_BEFORE();
+  __syncthreads();
+  if (warp == 1) {
+    P_FENCE_AFTER();
+    asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(C::TMEM) : "memory");
+  }
+}
+
+PFN_cuTensorMapEncodeTiled_v12000 encoder() {
+  static PFN_cuTensorMapEncodeTiled_v12000 encode = nullptr;
+  static std::mutex mu;
+  std::lock_guard<std::mutex> lock(mu);
+  if (!encode) {
+    void* fn = nullptr;
+    cudaDriverEntryPointQueryResult qres;
+    if (cudaGetDriverEntryPoint("cuTensorMapEncodeTiled", &fn, cudaEnableDefault, &qres) != cudaSuccess || qres != cudaDriverEntryPointSuccess || !fn) return nullptr;
+    encode = reinterpret_cast<PFN_cuTensorMapEncodeTiled_v12000>(fn);
+  }
+  return encode;
+}
+
+// the pages as a 4-D tensor, boxes of 64 elements x `box` slots under the 128-byte swizzle; pages outside it read as zeros
+cudaError_t page_map(PFN_cuTensorMapEncodeTiled_v12000 encode, const void* p, const PagedAttnArgs& a, int D, int box, bool head_first, CUtensorMap* out) {
+  const cuuint64_t head = (cuuint64_t)(a.Hkv > 1 ? a.head_stride : D) * 2, slot = (cuuint64_t)a.pos_stride * 2;
+  const cuuint64_t gdim[4] = {(cuuint64_t)D, (cuuint64_t)(head_first ? a.Hkv : a.s.page_size), (cuuint64_t)(head_first ? a.s.page_size : a.Hkv), (cuuint64_t)a.s.n_pages};
+  const cuuint64_t gstride[3] = {head_first ? head : slot, head_first ? slot : head, (cuuint64_t)a.page_stride * 2};
+  const cuuint32_t bx[4] = {64, (cuuint32_t)(head_first ? 1 : box), (cuuint32_t)(head_first ? box : 1), 1};
+  const cuuint32_t estr[4] = {1, 1, 1, 1};
+  return encode(out, CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 4, const_cast<void*>(p), gdim, gstride, bx, estr, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+                CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS
+             ? cudaSuccess
+             : cudaErrorInvalidValue;
+}
+
+template <int D, int NR, int PARTS>
+cudaError_t tc_go(const PagedAttnArgs& a, int num_sm, cudaStream_t st) {
+  static DevSmemCache cached{};
+  PFN_cuTensorMapEncodeTiled_v12000 encode = encoder();
+  if (!encode) return cudaErrorNotSupported;
+  TcArgs t;
+  t.a = a;
+  t.box = a.s.page_size < TILE ? a.s.page_size : TILE;
+  t.head_first = a.Hkv > 1 && a.head_stride < a.pos_stride;
+  t.min_run = 1;
+  cudaError_t e = page_map(encode, a.k, a, D, t.box, t.head_first, &t.tm_k);
+  if (e == cudaSuccess) e = page_map(encode, a.v, a, D, t.box, t.head_first, &t.tm_v);
+  if (e == cudaSuccess) e = sps_ensure_smem(paged_attn_tc_kernel<D, NR, PARTS>, Cfg<D, NR, PARTS>::SMEM, cached);
+  if (e != cudaSuccess) return e;
+  return launch_k(paged_attn_tc_kernel<D, NR, PARTS>, dim3(paged_attn_grid(num_sm)), dim3(Cfg<D, NR, PARTS>::THREADS), Cfg<D, NR, PARTS>::SMEM, st, t);
+}
+
+template <int D>
+cudaError_t tc_rows(const PagedAttnArgs& a, long long rows, int num_sm, cudaStream_t st) {
+  if (a.q_bf16) return rows <= 16 ? tc_go<D, 16, 1>(a, num_sm, st) : tc_go<D, 64, 1>(a, num_sm, st);
+  return rows <= 16 ? tc_go<D, 16, 3>(a, num_sm, st) : tc_go<D, 64, 3>(a, num_sm, st);
+}
+
+}  // namespace
+
+size_t paged_attn_tc_slot_bytes(int d_head) { return sizeof(float) * (d_head == 128 ? slot_floats<64, 128>() : slot_floats<64, 64>()); }
+
+cudaError_t paged_attn_tc_launch(const PagedAttnArgs& a, int d_head, int max_q, int num_sm, cudaStream_t st) {
+  const long long rows = (long long)max_q * a.G;
+  return d_head == 128 ? tc_rows<128>(a, rows, num_sm, st) : tc_rows<64>(a, rows, num_sm, st);
+}
