@@ -230,37 +230,59 @@ __device__ __forceinline__ void store_out(const PagedAttnArgs& a, long long at, 
 }
 
 // Joins the parts of an item and writes its rows: o = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c.  Run by all THREADS
-// threads of the last CTA to arrive; w is shared scratch of NR floats.
+// threads of the last CTA to arrive (named barrier 2 is theirs).  A part's slot is a trip to L2 away, so the loads of
+// several parts are in flight at once: maxima and sums by THREADS / NR threads per row, then four elements of a row at a
+// time, four parts per step.  w_max, w_inv: shared scratch of NR floats each, w_part of 2 * THREADS.
 template <int NR, int D, int THREADS>
-__device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCursor& c, int first, int parts, int tid, float* w_inv, float* w_max) {
+__device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCursor& c, int first, int parts, int tid, float* w_max, float* w_inv, float* w_part) {
   const int R = c.nq * a.G, r0 = c.t * NR, live = min(NR, R - r0);
   constexpr size_t SF = slot_floats<NR, D>();
-  auto slot = [&](int p) { return a.slots + SF * (size_t)part_slot(first + p, p == 0); };
+  constexpr int LANES = THREADS / NR;
+  const float* slots = a.slots + SF * (size_t)(2 * first);
+  auto slot = [&](int p) { return slots + SF * (size_t)(p == 0 ? 1 : 2 * p); };   // part 0 begins in its CTA: part_slot
+  {
+    const int r = tid % NR, p0 = tid / NR;
+    float M = -INFINITY, L = 0.f;
+    if (r < live) {
+#pragma unroll 4
+      for (int p = p0; p < parts; p += LANES) {
+        const float m = __ldcg(slot(p) + r), l = __ldcg(slot(p) + NR + r);
+        const float nm = fmaxf(M, m), base = nm == -INFINITY ? 0.f : nm;
+        L = L * exp2f(M - base) + l * exp2f(m - base);      // 2^-inf = 0 on either side that has nothing
+        M = nm;
+      }
+    }
+    w_part[2 * tid] = M;
+    w_part[2 * tid + 1] = L;
+  }
+  asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory");
   if (tid < live) {
     float M = -INFINITY, L = 0.f;
-    for (int p = 0; p < parts; ++p) M = fmaxf(M, __ldcg(slot(p) + tid));
-    for (int p = 0; p < parts; ++p) {
-      const float m = __ldcg(slot(p) + tid), l = __ldcg(slot(p) + NR + tid);
-      if (m != -INFINITY || l != l) L += l * exp2f(m - M);
-    }
-    w_max[tid] = M;
-    w_inv[tid] = M == -INFINITY && L == 0.f ? 0.f : 1.f / L;
+    for (int i = 0; i < LANES; ++i) M = fmaxf(M, w_part[2 * (i * NR + tid)]);
+    const float base = M == -INFINITY ? 0.f : M;
+    for (int i = 0; i < LANES; ++i) L += w_part[2 * (i * NR + tid) + 1] * exp2f(w_part[2 * (i * NR + tid)] - base);
+    w_max[tid] = base;
+    w_inv[tid] = L == 0.f ? 0.f : 1.f / L;
     if (a.lse) {
       const int r = r0 + tid;
-      a.lse[(size_t)(c.row0 + r / a.G) * a.H + c.hk * a.G + r % a.G] = L > 0.f || L != L ? 0.6931471805599453f * (M + log2f(L)) : -INFINITY;
+      a.lse[(size_t)(c.row0 + r / a.G) * a.H + c.hk * a.G + r % a.G] = L == 0.f ? -INFINITY : 0.6931471805599453f * (base + log2f(L));
     }
   }
   asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory");
-  for (int i = tid; i < live * D; i += THREADS) {
-    const int r = i / D, e = i - r * D;
+  for (int i = tid; i < live * (D / 4); i += THREADS) {
+    const int r = i / (D / 4), e = (i - r * (D / 4)) * 4;
     const float M = w_max[r], inv = w_inv[r];
-    float o = 0.f;
+    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll 4
     for (int p = 0; p < parts; ++p) {
-      const float m = __ldcg(slot(p) + r);
-      if (m != -INFINITY) o += exp2f(m - M) * __ldcg(slot(p) + 2 * NR + i);
+      const float w = exp2f(__ldcg(slot(p) + r) - M);
+      const float4 v = __ldcg(reinterpret_cast<const float4*>(slot(p) + 2 * NR + r * D + e));
+      o.x += w * v.x; o.y += w * v.y; o.z += w * v.z; o.w += w * v.w;
     }
     const int rr = r0 + r;
-    store_out(a, (long long)(c.row0 + rr / a.G) * a.out.row + (long long)(c.hk * a.G + rr % a.G) * a.out.head + e, inv != inv ? inv : (inv == 0.f ? 0.f : o * inv));
+    const long long at = (long long)(c.row0 + rr / a.G) * a.out.row + (long long)(c.hk * a.G + rr % a.G) * a.out.head + e;
+    if (inv == 0.f) o = make_float4(0.f, 0.f, 0.f, 0.f);
+    store_out(a, at, o.x * inv); store_out(a, at + 1, o.y * inv); store_out(a, at + 2, o.z * inv); store_out(a, at + 3, o.w * inv);
   }
   asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory");
 }

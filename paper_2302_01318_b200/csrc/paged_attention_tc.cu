@@ -13,8 +13,10 @@
 // Running maximum.  The weights are 2^(s - m) with m fixed at the maximum of the part's first tile: P is bf16 (8 exponent
 // bits) or three bf16 parts of an fp32 number, sums are fp32, so m only has to keep the weights in range, not at most 1.
 // Only when a score exceeds m by 2^MAX_UP do the CTA's threads agree (a reducing barrier) to take the new maximum and
-// rescale sums and O^T.  That leaves a multiply-add, an exponential, an addition and the rounding per score, no
-// cross-lane reduction per tile.  Sums stay per thread (its token of every tile) until the part ends.
+// rescale what they hold.  That leaves a multiply-add, an exponential, an addition and the rounding per score, no
+// cross-lane reduction per tile.  Sums stay per thread (its token of every tile) until the part ends.  Each tile's O^T
+// is a product of its own, added to fp32 registers: the tensor cores cut the low bits of a running sum instead of rounding
+// them, which over a context of 32 768 tokens cost 3.6e-5 of the result.
 //
 // Types.  bf16 queries: P rounds once to bf16 (2^-8 relative, and the sum is taken of the rounded weights).  fp32 queries:
 // Q and P enter as three bf16 parts (high, rest, rest of the rest: 24 bits), three products each, added up in fp32.
@@ -111,16 +113,7 @@ __device__ __forceinline__ void p_ld16(uint32_t t, float* v) {
 #pragma unroll
   for (int i = 0; i < 16; ++i) v[i] = __uint_as_float(r[i]);
 }
-__device__ __forceinline__ void p_st16(uint32_t t, const float* v) {
-  uint32_t r[16];
-#pragma unroll
-  for (int i = 0; i < 16; ++i) r[i] = __float_as_uint(v[i]);
-  asm volatile("tcgen05.st.sync.aligned.32x32b.x16.b32 [%16], {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15};" ::"r"(r[0]), "r"(r[1]), "r"(r[2]),
-               "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]), "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15]), "r"(t)
-               : "memory");
-}
 #define P_WAIT_LD() asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory")
-#define P_WAIT_ST() asm volatile("tcgen05.wait::st.sync.aligned;" ::: "memory")
 
 __device__ __forceinline__ float p_ex2(float x) {
   float y;
@@ -163,7 +156,7 @@ template <int D, int NR, int PARTS> struct Cfg {
   static constexpr uint32_t HALF = TILE * D * 2;                    // keys or values of a tile
   static constexpr uint32_t QPART = NR * D * 2, PPART = TILE * NR * 2;
   static constexpr uint32_t FIXED = PARTS * (QPART + PPART);
-  static constexpr uint32_t HDR = 2304;                             // barriers, small per-row arrays
+  static constexpr uint32_t HDR = 3072;                             // barriers, small per-row arrays
   static constexpr int STAGES_FIT = (232448 - (int)HDR - (int)FIXED) / (int)HALF;
   static constexpr int STAGES = (STAGES_FIT > 8 ? 8 : STAGES_FIT) & ~1;   // even: K and V take turns
   static constexpr size_t SMEM = FIXED + (size_t)STAGES * HALF + HDR;
@@ -196,7 +189,8 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
   float* s_a = reinterpret_cast<float*>(hdr + 384 + NR * 4);           // [NR] maxima, and scratch of the join
   float* s_b = s_a + NR;                                               // [NR] sums / factors
   float* s_red = s_b + NR;                                             // [4][NR]
-  static_assert(384 + NR * 4 * 7 <= (int)C::HDR && sizeof(WorkCursor) <= 176, "header");
+  long long* s_off = reinterpret_cast<long long*>(s_red + 4 * NR);     // [NR] where a row's output goes, -1: no such row
+  static_assert(384 + NR * 4 * 9 <= (int)C::HDR && sizeof(WorkCursor) <= 176, "header");
   const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
 
   if (tid == 0) {
@@ -311,7 +305,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
           if (!ok) break;
           P_FENCE_AFTER();
           const uint32_t v_at = ring + (uint32_t)(e % STAGES) * C::HALF;
-          uint32_t acc = i > 0 ? 1u : 0u;
+          uint32_t acc = 0;
 #pragma unroll
           for (int part = PARTS - 1; part >= 0; --part) {
             const uint64_t da = p_desc(v_at, TILE * 128, 1024, 2), db = p_desc(p_s + part * C::PPART, 16, 8 * C::P_ROW, C::P_LAYOUT);
@@ -386,14 +380,33 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
           *reinterpret_cast<uint4*>(dst + part * C::QPART) = make_uint4(u[0], u[1], u[2], u[3]);
         }
       }
-      if (st < NR) s_lim[st] = r0 + st < R ? c.len - c.nq + (r0 + st) / a.G : -1;
+      if (st < NR) {
+        const int rr = r0 + st, tok = rr / a.G;
+        s_lim[st] = rr < R ? c.len - c.nq + tok : -1;
+        s_off[st] = rr < R ? (long long)(c.row0 + tok) * a.out.row + (long long)(c.hk * a.G + rr - tok * a.G) * a.out.head : -1;
+      }
       if (st == 0) *s_poison = 0x7fffffff;
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       p_arrive(q_ready);
       soft_sync();
-      float m[COLS], l[COLS];
+      float l[COLS], o[COLS];
 #pragma unroll
-      for (int j = 0; j < COLS; ++j) { m[j] = 0.f; l[j] = 0.f; }
+      for (int j = 0; j < COLS; ++j) l[j] = o[j] = 0.f;
+      // o += O^T of the last tile multiplied, once that product is done
+      bool held = false;
+      auto collect = [&]() {
+        if (!held) return;
+        held = false;
+        ok = ok && p_wait(pv_done, (uint32_t)(pn - 1) & 1u, a.wait_ns, a.s.status, s_abort);
+        __syncwarp();
+        P_FENCE_AFTER();
+        float t[COLS];
+#pragma unroll
+        for (int j = 0; j < COLS; j += 16) p_ld16(tmem_o + t_lane + col0 + j, t + j);
+        P_WAIT_LD();
+#pragma unroll
+        for (int j = 0; j < COLS; ++j) o[j] += t[j];
+      };
       for (int i = 0; i < n; ++i, ++sn, it += 2) {
         const int buf = sn & 1, p0 = (c.k0 + i) * TILE, pos = p0 + my;
         const bool edge = p0 + TILE - 1 > first_lim;          // some row does not see all of this tile
@@ -410,12 +423,16 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
         bool retake = i == 0;
         if (i > 0) {
           float up = -INFINITY;
-          if (edge) {
 #pragma unroll
-            for (int j = 0; j < COLS; ++j) up = fmaxf(up, pos <= s_lim[col0 + j] ? fmaf(x[j], a.scale_log2, -m[j]) : -INFINITY);
-          } else {
-#pragma unroll
-            for (int j = 0; j < COLS; ++j) up = fmaxf(up, fmaf(x[j], a.scale_log2, -m[j]));
+          for (int j = 0; j < COLS; j += 4) {
+            const float4 m = *reinterpret_cast<const float4*>(s_a + col0 + j);
+            const float y[4] = {fmaf(x[j], a.scale_log2, -m.x), fmaf(x[j + 1], a.scale_log2, -m.y), fmaf(x[j + 2], a.scale_log2, -m.z), fmaf(x[j + 3], a.scale_log2, -m.w)};
+            if (edge) {
+              const int4 lim = *reinterpret_cast<const int4*>(s_lim + col0 + j);
+              up = fmaxf(up, fmaxf(fmaxf(pos <= lim.x ? y[0] : -INFINITY, pos <= lim.y ? y[1] : -INFINITY), fmaxf(pos <= lim.z ? y[2] : -INFINITY, pos <= lim.w ? y[3] : -INFINITY)));
+            } else {
+              up = fmaxf(up, fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])));
+            }
           }
           uint32_t any;
           asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.or.pred p, 1, %2, q;\n selp.u32 %0, 1, 0, p;\n}\n"
@@ -428,53 +445,50 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
           for (int j = 0; j < COLS; ++j) y[j] = pos <= s_lim[col0 + j] ? x[j] * a.scale_log2 : -INFINITY;
           const float top = fold<OpMax, COLS>(y, lane);
           s_red[quarter * NR + col0 + my_col] = top;
+          if (i > 0) collect();
           soft_sync();
 #pragma unroll
           for (int j = 0; j < COLS; ++j) {
             const int cc = col0 + j;
             const float t = fmaxf(fmaxf(s_red[cc], s_red[NR + cc]), fmaxf(s_red[2 * NR + cc], s_red[3 * NR + cc]));
             if (i == 0) {
-              m[j] = t == -INFINITY ? 0.f : t;                // a row that sees nothing here sees nothing in this part
+              y[j] = t == -INFINITY ? 0.f : t;                // a row that sees nothing here sees nothing in this part
             } else {
-              const float nm = fmaxf(m[j], t), al = p_ex2(m[j] - nm);
+              y[j] = fmaxf(s_a[cc], t);
+              const float al = p_ex2(s_a[cc] - y[j]);
               l[j] *= al;
-              m[j] = nm;
-              if (my == 0) s_b[cc] = al;
+              o[j] *= al;
             }
           }
-          if (i > 0) {
-            // O^T takes the factors: every product so far must be in it
-            ok = ok && p_wait(pv_done, (uint32_t)(pn - 1) & 1u, a.wait_ns, a.s.status, s_abort);
-            soft_sync();
-            P_FENCE_AFTER();
+          soft_sync();   // everyone has read s_red and the old maxima
+          if (my == 0) {
 #pragma unroll
-            for (int j = 0; j < COLS; j += 16) {
-              float o[16];
-              p_ld16(tmem_o + t_lane + col0 + j, o);
-              P_WAIT_LD();
-#pragma unroll
-              for (int q = 0; q < 16; ++q) o[q] *= s_b[col0 + j + q];
-              p_st16(tmem_o + t_lane + col0 + j, o);
-            }
-            P_WAIT_ST();
-            P_FENCE_BEFORE();
+            for (int j = 0; j < COLS; ++j) s_a[col0 + j] = y[j];
           }
-          soft_sync();   // s_red and s_b may be written again
+          soft_sync();
         }
         // ---- weights
-        if (edge) {
 #pragma unroll
-          for (int j = 0; j < COLS; ++j) x[j] = pos <= s_lim[col0 + j] ? p_ex2(fmaf(x[j], a.scale_log2, -m[j])) : 0.f;
-        } else {
-#pragma unroll
-          for (int j = 0; j < COLS; ++j) x[j] = p_ex2(fmaf(x[j], a.scale_log2, -m[j]));
+        for (int j = 0; j < COLS; j += 4) {
+          const float4 m = *reinterpret_cast<const float4*>(s_a + col0 + j);
+          x[j] = p_ex2(fmaf(x[j], a.scale_log2, -m.x));
+          x[j + 1] = p_ex2(fmaf(x[j + 1], a.scale_log2, -m.y));
+          x[j + 2] = p_ex2(fmaf(x[j + 2], a.scale_log2, -m.z));
+          x[j + 3] = p_ex2(fmaf(x[j + 3], a.scale_log2, -m.w));
+          if (edge) {
+            const int4 lim = *reinterpret_cast<const int4*>(s_lim + col0 + j);
+            x[j] = pos <= lim.x ? x[j] : 0.f;
+            x[j + 1] = pos <= lim.y ? x[j + 1] : 0.f;
+            x[j + 2] = pos <= lim.z ? x[j + 2] : 0.f;
+            x[j + 3] = pos <= lim.w ? x[j + 3] : 0.f;
+          }
         }
         if (PARTS == 3) {
 #pragma unroll
           for (int j = 0; j < COLS; ++j) l[j] += x[j];
         }
-        // P^T and, at the edge, V are written once the previous output product has read P^T
-        if (pn > 0) ok = ok && p_wait(pv_done, (uint32_t)(pn - 1) & 1u, a.wait_ns, a.s.status, s_abort);
+        // P^T is written once the previous output product has read it
+        if (i > 0) collect();
         if (edge) {
           // slots behind the sequence hold anything: zero (0 x NaN is NaN in a product).  New tokens some rows do not see:
           // a value that is not finite is taken out and remembered, its rows become NaN at the end.
@@ -525,13 +539,14 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
         P_FENCE_BEFORE();
         p_arrive(p_full);
         ++pn;
+        held = true;
       }
       // ---- the part's end: sums over the tokens, then O^T
-#pragma unroll
-      for (int j = 0; j < COLS; ++j) if (my == 0) s_a[col0 + j] = m[j];
       const float sum = fold<OpAdd, COLS>(l, lane);
       s_red[quarter * NR + col0 + my_col] = sum;
-      ok = ok && p_wait(pv_done, (uint32_t)(pn - 1) & 1u, a.wait_ns, a.s.status, s_abort);
+      collect();
+      int first, parts;
+      item_ctas(c, first, parts);
       {
         uint32_t all;
         asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.and.pred p, 1, %2, q;\n selp.u32 %0, 1, 0, p;\n}\n"
@@ -541,40 +556,35 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
       if (st < NR) {
         float t = (s_red[st] + s_red[NR + st]) + (s_red[2 * NR + st] + s_red[3 * NR + st]);
         if (s_lim[st] >= *s_poison) t = __int_as_float(0x7fffffff);
-        s_b[st] = t;
         if (t == 0.f) s_a[st] = -INFINITY;
+        s_b[st] = t;
+        if (parts == 1) {
+          if (a.lse && r0 + st < R) {
+            const int rr = r0 + st;
+            a.lse[(size_t)(c.row0 + rr / a.G) * a.H + c.hk * a.G + rr % a.G] = t == 0.f ? -INFINITY : 0.6931471805599453f * (s_a[st] + log2f(t));
+          }
+          s_b[st] = t == 0.f ? 0.f : 1.f / t;
+        }
       }
       soft_sync();
-      int first, parts;
-      item_ctas(c, first, parts);
-      P_FENCE_AFTER();
       const int e = D == 128 ? my : quarter * 16 + lane;      // element of the head (d = 64: 16 rows in each quarter's first 16 lanes)
       const bool live_lane = D == 128 || lane < 16;
       float* slot = a.slots + slot_floats<NR, D>() * (size_t)part_slot(blockIdx.x, c.k0 == 0);
-#pragma unroll 1
-      for (int j = 0; j < COLS; j += 16) {
-        float o[16];
-        p_ld16(tmem_o + t_lane + col0 + j, o);
-        P_WAIT_LD();
+      if (live_lane) {
 #pragma unroll
-        for (int q = 0; q < 16; ++q) {
-          const int r = col0 + j + q, rr = r0 + r;
-          if (rr >= R || !live_lane) continue;
+        for (int j = 0; j < COLS; ++j) {
+          const int r = col0 + j;
+          const long long at = s_off[r];
+          if (at < 0) continue;
           if (parts == 1) {
             const float t = s_b[r];
-            store_out(a, (long long)(c.row0 + rr / a.G) * a.out.row + (long long)(c.hk * a.G + rr % a.G) * a.out.head + e, t == 0.f ? 0.f : o[q] * (1.f / t));
+            store_out(a, at + e, t == 0.f ? 0.f : o[j] * t);
           } else {
-            __stcg(slot + 2 * NR + r * D + e, o[q]);
+            __stcg(slot + 2 * NR + r * D + e, o[j]);
           }
         }
       }
-      P_FENCE_BEFORE();
-      if (parts == 1) {
-        if (a.lse && st < NR && r0 + st < R) {
-          const int rr = r0 + st;
-          a.lse[(size_t)(c.row0 + rr / a.G) * a.H + c.hk * a.G + rr % a.G] = s_b[st] == 0.f ? -INFINITY : 0.6931471805599453f * (s_a[st] + log2f(s_b[st]));
-        }
-      } else {
+      if (parts > 1) {
         if (st < NR) { __stcg(slot + st, s_a[st]); __stcg(slot + NR + st, s_b[st]); }
         __threadfence();
         soft_sync();
@@ -583,7 +593,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
           if (*s_last) { a.counters[first] = 0; __threadfence(); }
         }
         soft_sync();
-        if (*s_last) join_parts<NR, D, SOFT>(a, c, first, parts, st, s_b, s_a);
+        if (*s_last) join_parts<NR, D, SOFT>(a, c, first, parts, st, s_b, s_a, reinterpret_cast<float*>(mem + STAGES * C::HALF + PARTS * C::QPART));
       }
       soft_sync();   // s_a, s_b, s_lim are free again
       cursor_next<NR, TILE>(a, c);
