@@ -230,16 +230,18 @@ __device__ __forceinline__ void store_out(const PagedAttnArgs& a, long long at, 
 }
 
 // Joins the parts of an item and writes its rows: o = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c.  Run by all THREADS
-// threads of the last CTA to arrive (named barrier 2 is theirs).  A part's slot is a trip to L2 away, so the loads of
-// several parts are in flight at once: maxima and sums by THREADS / NR threads per row, then four elements of a row at a
-// time, four parts per step.  w_max, w_inv: shared scratch of NR floats each, w_part of 2 * THREADS.
+// threads of the last CTA to arrive (named barrier 2 is theirs).  A part's slot is a trip to L2 away, so many loads are in
+// flight at once: maxima and sums by THREADS / NR threads per row; then every thread takes its four-element pieces of the
+// output through all parts, four parts at a time, their weights waiting in shared memory.  w_max, w_inv: shared scratch
+// of NR floats each; w: of w_floats >= 2 * THREADS.
 template <int NR, int D, int THREADS>
-__device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCursor& c, int first, int parts, int tid, float* w_max, float* w_inv, float* w_part) {
+__device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCursor& c, int first, int parts, int tid, float* w_max, float* w_inv, float* w, int w_floats) {
   const int R = c.nq * a.G, r0 = c.t * NR, live = min(NR, R - r0);
   constexpr size_t SF = slot_floats<NR, D>();
-  constexpr int LANES = THREADS / NR;
+  constexpr int LANES = THREADS / NR, PIECES = NR * (D / 4) / THREADS;
   const float* slots = a.slots + SF * (size_t)(2 * first);
   auto slot = [&](int p) { return slots + SF * (size_t)(p == 0 ? 1 : 2 * p); };   // part 0 begins in its CTA: part_slot
+  auto sync = [&]() { asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory"); };
   {
     const int r = tid % NR, p0 = tid / NR;
     float M = -INFINITY, L = 0.f;
@@ -252,15 +254,15 @@ __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCur
         M = nm;
       }
     }
-    w_part[2 * tid] = M;
-    w_part[2 * tid + 1] = L;
+    w[2 * tid] = M;
+    w[2 * tid + 1] = L;
   }
-  asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory");
+  sync();
   if (tid < live) {
     float M = -INFINITY, L = 0.f;
-    for (int i = 0; i < LANES; ++i) M = fmaxf(M, w_part[2 * (i * NR + tid)]);
+    for (int i = 0; i < LANES; ++i) M = fmaxf(M, w[2 * (i * NR + tid)]);
     const float base = M == -INFINITY ? 0.f : M;
-    for (int i = 0; i < LANES; ++i) L += w_part[2 * (i * NR + tid) + 1] * exp2f(w_part[2 * (i * NR + tid)] - base);
+    for (int i = 0; i < LANES; ++i) L += w[2 * (i * NR + tid) + 1] * exp2f(w[2 * (i * NR + tid)] - base);
     w_max[tid] = base;
     w_inv[tid] = L == 0.f ? 0.f : 1.f / L;
     if (a.lse) {
@@ -268,23 +270,42 @@ __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCur
       a.lse[(size_t)(c.row0 + r / a.G) * a.H + c.hk * a.G + r % a.G] = L == 0.f ? -INFINITY : 0.6931471805599453f * (base + log2f(L));
     }
   }
-  asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory");
-  for (int i = tid; i < live * (D / 4); i += THREADS) {
-    const int r = i / (D / 4), e = (i - r * (D / 4)) * 4;
-    const float M = w_max[r], inv = w_inv[r];
-    float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
-#pragma unroll 4
-    for (int p = 0; p < parts; ++p) {
-      const float w = exp2f(__ldcg(slot(p) + r) - M);
-      const float4 v = __ldcg(reinterpret_cast<const float4*>(slot(p) + 2 * NR + r * D + e));
-      o.x += w * v.x; o.y += w * v.y; o.z += w * v.z; o.w += w * v.w;
+  sync();
+  float4 o[PIECES];
+#pragma unroll
+  for (int k = 0; k < PIECES; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+  const int table = w_floats / NR;                             // parts whose weights fit at once
+  for (int pb = 0; pb < parts; pb += table) {
+    const int pn = min(table, parts - pb);
+    for (int i = tid; i < pn * NR; i += THREADS) {
+      const int p = i / NR, r = i - p * NR;
+      if (r < live) w[i] = exp2f(__ldcg(slot(pb + p) + r) - w_max[r]) * w_inv[r];
     }
-    const int rr = r0 + r;
-    const long long at = (long long)(c.row0 + rr / a.G) * a.out.row + (long long)(c.hk * a.G + rr % a.G) * a.out.head + e;
-    if (inv == 0.f) o = make_float4(0.f, 0.f, 0.f, 0.f);
-    store_out(a, at, o.x * inv); store_out(a, at + 1, o.y * inv); store_out(a, at + 2, o.z * inv); store_out(a, at + 3, o.w * inv);
+    sync();
+#pragma unroll 4
+    for (int p = 0; p < pn; ++p) {
+      const float* s = slot(pb + p) + 2 * NR;
+#pragma unroll
+      for (int k = 0; k < PIECES; ++k) {
+        const int i = tid + k * THREADS;
+        if (i < live * (D / 4)) {
+          const float f = w[p * NR + i / (D / 4)];
+          const float4 v = __ldcg(reinterpret_cast<const float4*>(s) + i);
+          o[k].x += f * v.x; o[k].y += f * v.y; o[k].z += f * v.z; o[k].w += f * v.w;
+        }
+      }
+    }
+    sync();
   }
-  asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory");
+#pragma unroll
+  for (int k = 0; k < PIECES; ++k) {
+    const int i = tid + k * THREADS;
+    if (i < live * (D / 4)) {
+      const int r = i / (D / 4), e = (i - r * (D / 4)) * 4, rr = r0 + r;
+      const long long at = (long long)(c.row0 + rr / a.G) * a.out.row + (long long)(c.hk * a.G + rr % a.G) * a.out.head + e;
+      store_out(a, at, o[k].x); store_out(a, at + 1, o[k].y); store_out(a, at + 2, o[k].z); store_out(a, at + 3, o[k].w);
+    }
+  }
 }
 
 // launchers

@@ -169,7 +169,7 @@ __global__ void __launch_bounds__(SIMT_THREADS) paged_attn_simt_kernel(const __g
         if (s_last) { a.counters[first] = 0; __threadfence(); }
       }
       __syncthreads();
-      if (s_last) join_parts<NR, D, SIMT_THREADS>(a, c, first, parts, tid, s_alpha, s_m, Ps);
+      if (s_last) join_parts<NR, D, SIMT_THREADS>(a, c, first, parts, tid, s_alpha, s_m, Ps, NR * KT);
     }
     cursor_next<NR, KT>(a, c);
   }

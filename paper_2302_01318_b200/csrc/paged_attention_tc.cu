@@ -19,15 +19,20 @@
 // them, which over a context of 32 768 tokens cost 3.6e-5 of the result.
 //
 // Types.  bf16 queries: P rounds once to bf16 (2^-8 relative, and the sum is taken of the rounded weights).  fp32 queries:
-// Q and P enter as three bf16 parts (high, rest, rest of the rest: 24 bits), three products each, added up in fp32.
+// Q and P enter as three bf16 parts (high, rest, rest of the rest: 24 bits), side by side as columns of one product -- a
+// product reads its 128-row operand in 32 clocks however few its columns, 16 columns cost 39 and 48 cost 44 -- and the
+// three columns of a row are added in fp32.
 //
 // What bounds it: HBM.  A tile of 128 tokens is 64 KB of keys and values (d = 128), 2760 clocks of an SM's share of
-// 6.5 TB/s; its products take 8 x 32 clocks each for 16 rows (x 3 for fp32), the softmax a few hundred.  One CTA per SM,
-// equal runs of tiles per CTA (paged.cuh), a ring of 4 to 6 half-tiles (K or V) of 32 KB in flight.
+// 6.5 TB/s; its 16 products take 39 to 72 clocks each, the softmax a few hundred.  One CTA per SM, equal runs of tiles per
+// CTA (paged.cuh), a ring of 4 to 6 half-tiles (K or V) of 32 KB in flight.
 //
 //   warp 0      copies: lane i asks for page i of the tile (TMA boxes of 64 elements x up to 128 slots, 128-byte swizzle)
-//   warp 1      one lane issues the products: S of tile i + 1 goes before O of tile i, so the softmax never waits
-//   warps 2..   softmax, 128 tokens x NR rows by 4 warps (16 rows) or 8 (two groups of columns)
+//   warp 1      products: S of the next tile, the next part's included, goes before O of this one.  The warp runs as one
+//               with an elected lane issuing and constant offsets: descriptors stay in uniform registers (40 clocks a
+//               product; issued from a divergent lane they took 130)
+//   warps 2, 3  Q of the parts to come, into shared memory in bf16 parts
+//   warps 4..   softmax and outputs, 16 rows per group of four warps
 //
 // Every wait is bounded; on expiry the CTA sets SPS_PAGED_TIMEOUT, lets its copies and products finish, frees its tensor
 // memory and returns.
@@ -89,13 +94,21 @@ __device__ __forceinline__ void p_copy(uint32_t dst, const CUtensorMap* tm, int 
                "r"(c0), "r"(c1), "r"(c2), "r"(c3), "r"(bar)
                : "memory");
 }
-// shared-memory operand descriptor: layout 2 / 4 / 6 = 128- / 64- / 32-byte swizzle; sbo: bytes between groups of 8 rows,
-// lbo: bytes between 64-element blocks along the contiguous (MN) direction, unused for K-major operands
-__device__ __forceinline__ uint64_t p_desc(uint32_t addr, uint32_t lbo, uint32_t sbo, uint32_t layout) {
-  return (uint64_t)((addr & 0x3ffffu) >> 4) | (uint64_t)((lbo >> 4) & 0x3fffu) << 16 | (uint64_t)(sbo >> 4) << 32 | (uint64_t)1 << 46 | (uint64_t)layout << 61;
+// shared-memory operand descriptors: the low word holds the address and, for MN-major operands, the bytes between blocks
+// along the contiguous direction (lbo); the high word the bytes between groups of 8 rows (sbo), version 1 and the swizzle
+// (layout 2 / 6 = 128 / 32 bytes)
+__device__ __forceinline__ uint32_t p_desc_lo(uint32_t addr, uint32_t lbo) { return ((addr & 0x3ffffu) >> 4) | (lbo >> 4) << 16; }
+__host__ __device__ constexpr uint32_t p_desc_hi(uint32_t sbo, uint32_t layout) { return (sbo >> 4) | 1u << 14 | layout << 29; }
+__device__ __forceinline__ void p_mma(uint32_t d, uint32_t a_lo, uint32_t a_hi, uint32_t b_lo, uint32_t b_hi, uint32_t idesc, bool accumulate) {
+  asm volatile(
+      "{\n .reg .pred p;\n .reg .b64 a, b;\n mov.b64 a, {%1, %2};\n mov.b64 b, {%3, %4};\n setp.ne.b32 p, %6, 0;\n"
+      " tcgen05.mma.cta_group::1.kind::f16 [%0], a, b, %5, p;\n}\n" ::"r"(d), "r"(a_lo), "r"(a_hi), "r"(b_lo), "r"(b_hi), "r"(idesc), "r"(accumulate ? 1u : 0u)
+      : "memory");
 }
-__device__ __forceinline__ void p_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
-  asm volatile("{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n tcgen05.mma.cta_group::1.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d), "l"(a), "l"(b), "r"(idesc), "r"(accumulate) : "memory");
+__device__ __forceinline__ bool p_elect() {
+  uint32_t r;
+  asm volatile("{\n .reg .pred p;\n elect.sync _|p, 0xffffffff;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(r));
+  return r != 0;
 }
 __device__ __forceinline__ void p_commit(uint32_t bar) {
   asm volatile("tcgen05.commit.cta_group::1.mbarrier::arrive::one.shared::cluster.b64 [%0];" ::"r"(bar) : "memory");
@@ -129,14 +142,14 @@ __device__ __forceinline__ uint32_t p_pack(float lo, float hi) {
 __device__ __forceinline__ float p_lo(uint32_t u) { return __uint_as_float(u << 16); }
 __device__ __forceinline__ float p_hi(uint32_t u) { return __uint_as_float(u & 0xffff0000u); }
 
-// Reduces v[c] over the 32 lanes for N columns (16 or 32), halving the columns a lane carries at every step; the lane ends
-// up with column lane >> 1 (16 columns) or lane (32).
+// Reduces v[c] over the 32 lanes for 16 columns, halving the columns a lane carries at every step; the lane ends up with
+// column lane >> 1.
 struct OpMax { static __device__ __forceinline__ float f(float a, float b) { return fmaxf(a, b); } };
 struct OpAdd { static __device__ __forceinline__ float f(float a, float b) { return a + b; } };
-template <class Op, int N> __device__ __forceinline__ float fold(float (&v)[N], int lane) {
+template <class Op> __device__ __forceinline__ float fold16(float (&v)[16], int lane) {
   int off = 16;
 #pragma unroll
-  for (int w = N / 2; w >= 1; w >>= 1, off >>= 1) {
+  for (int w = 8; w >= 1; w >>= 1, off >>= 1) {
     const bool upper = (lane & off) != 0;
 #pragma unroll
     for (int k = 0; k < w; ++k) {
@@ -144,66 +157,65 @@ template <class Op, int N> __device__ __forceinline__ float fold(float (&v)[N], 
       v[k] = Op::f(keep, __shfl_xor_sync(0xffffffffu, send, off));
     }
   }
-  if (N == 16) v[0] = Op::f(v[0], __shfl_xor_sync(0xffffffffu, v[0], 1));
-  return v[0];
+  return Op::f(v[0], __shfl_xor_sync(0xffffffffu, v[0], 1));
 }
 
 template <int D, int NR, int PARTS> struct Cfg {
-  static constexpr int GROUPS = NR == 16 ? 1 : 2;                   // column groups of four softmax warps each
-  static constexpr int COLS = NR / GROUPS;
+  static constexpr int GROUPS = NR / 16;                            // column groups of four softmax warps each
   static constexpr int SOFT = 128 * GROUPS;                         // softmax threads
-  static constexpr int THREADS = 64 + SOFT;
+  static constexpr int THREADS = 128 + SOFT;
+  static constexpr int N = PARTS * NR;                              // columns of a product
   static constexpr uint32_t HALF = TILE * D * 2;                    // keys or values of a tile
-  static constexpr uint32_t QPART = NR * D * 2, PPART = TILE * NR * 2;
-  static constexpr uint32_t FIXED = PARTS * (QPART + PPART);
+  static constexpr uint32_t Q_BYTES = N * D * 2, P_BYTES = TILE * N * 2;
   static constexpr uint32_t HDR = 3072;                             // barriers, small per-row arrays
-  static constexpr int STAGES_FIT = (232448 - (int)HDR - (int)FIXED) / (int)HALF;
-  static constexpr int STAGES = (STAGES_FIT > 8 ? 8 : STAGES_FIT) & ~1;   // even: K and V take turns
-  static constexpr size_t SMEM = FIXED + (size_t)STAGES * HALF + HDR;
-  static constexpr uint32_t TMEM = NR == 16 ? 64 : (NR == 32 ? 128 : 256);
-  // P^T is the B operand, MN-major: a token's NR weights side by side
-  static constexpr uint32_t P_ROW = NR >= 64 ? 128 : NR * 2;
-  static constexpr uint32_t P_LAYOUT = NR >= 64 ? 2 : (NR == 32 ? 4 : 6);
+  static constexpr int BUDGET = 232448 - (int)HDR - (int)P_BYTES;
+  static constexpr int QBUF = (BUDGET - 2 * (int)Q_BYTES) / (int)HALF >= 4 ? 2 : 1;
+  static constexpr int STAGES_FIT = (BUDGET - QBUF * (int)Q_BYTES) / (int)HALF;
+  static constexpr int STAGES = STAGES_FIT > 8 ? 8 : STAGES_FIT;
+  static constexpr uint32_t Q_AT = STAGES * HALF, P_AT = Q_AT + QBUF * Q_BYTES, HDR_AT = P_AT + P_BYTES;
+  static constexpr size_t SMEM = HDR_AT + HDR;
+  static constexpr uint32_t TMEM = 3 * N <= 64 ? 64 : (3 * N <= 128 ? 128 : (3 * N <= 256 ? 256 : 512));   // S twice, O once
+  // P^T is the B operand of O, MN-major under the 32-byte swizzle: blocks of 16 columns x 128 tokens, 32 bytes per token
+  static constexpr uint32_t P_BLOCK = TILE * 32;
   // kind::f16 instruction descriptors: fp32 accumulator, bf16 x bf16; S: both K-major, M = 128; O: both MN-major, M = d
-  static constexpr uint32_t IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(NR >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24);
-  static constexpr uint32_t IDESC_O = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(NR >> 3) << 17) | ((uint32_t)(D >> 4) << 24);
-  static_assert(STAGES >= 4, "ring too short");
+  static constexpr uint32_t IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24);
+  static constexpr uint32_t IDESC_O = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(D >> 4) << 24);
+  static_assert(STAGES >= 4 && 3 * N <= 512 && N <= 256, "shape");
 };
 
 template <int D, int NR, int PARTS>
 __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_kernel(const __grid_constant__ TcArgs ta) {
   using C = Cfg<D, NR, PARTS>;
-  constexpr int COLS = C::COLS, SOFT = C::SOFT, STAGES = C::STAGES;
+  constexpr int SOFT = C::SOFT, STAGES = C::STAGES, N = C::N;
   extern __shared__ __align__(1024) unsigned char mem[];   // the ring, Q, P^T (swizzled operands: 1024-byte aligned), header
   const PagedAttnArgs& a = ta.a;
-  const uint32_t ring = p_smem(mem), q_s = ring + STAGES * C::HALF, p_s = q_s + PARTS * C::QPART;
-  unsigned char* hdr = mem + STAGES * C::HALF + C::FIXED;
-  const uint32_t hb = p_smem(hdr);
-  const uint32_t full = hb, empty = hb + 64, s_full = hb + 128, s_free = hb + 144, p_full = hb + 160, pv_done = hb + 168, q_ready = hb + 176, drain = hb + 184;
-  volatile uint32_t* s_tmem = reinterpret_cast<volatile uint32_t*>(hdr + 192);
-  volatile int* s_abort = reinterpret_cast<volatile int*>(hdr + 196);
-  int* s_poison = reinterpret_cast<int*>(hdr + 200);
-  int* s_last = reinterpret_cast<int*>(hdr + 204);
-  WorkCursor* s_cur = reinterpret_cast<WorkCursor*>(hdr + 208);       // 96 bytes at most
+  const uint32_t ring = p_smem(mem), hb = ring + C::HDR_AT;
+  unsigned char* hdr = mem + C::HDR_AT;
+  const uint32_t full = hb, empty = hb + 64, s_full = hb + 128, s_free = hb + 144, p_full = hb + 160, pv_done = hb + 168, q_ready = hb + 176, q_free = hb + 192, drain = hb + 208;
+  volatile uint32_t* s_tmem = reinterpret_cast<volatile uint32_t*>(hdr + 216);
+  volatile int* s_abort = reinterpret_cast<volatile int*>(hdr + 220);
+  int* s_poison = reinterpret_cast<int*>(hdr + 224);
+  int* s_last = reinterpret_cast<int*>(hdr + 228);
+  WorkCursor* s_cur = reinterpret_cast<WorkCursor*>(hdr + 232);
   int* s_lim = reinterpret_cast<int*>(hdr + 384);                      // [NR] last position a row sees
-  float* s_a = reinterpret_cast<float*>(hdr + 384 + NR * 4);           // [NR] maxima, and scratch of the join
+  float* s_a = reinterpret_cast<float*>(hdr + 384 + NR * 4);           // [NR] maxima
   float* s_b = s_a + NR;                                               // [NR] sums / factors
   float* s_red = s_b + NR;                                             // [4][NR]
   long long* s_off = reinterpret_cast<long long*>(s_red + 4 * NR);     // [NR] where a row's output goes, -1: no such row
-  static_assert(384 + NR * 4 * 9 <= (int)C::HDR && sizeof(WorkCursor) <= 176, "header");
-  const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+  static_assert(384 + NR * 4 * 9 <= (int)C::HDR && sizeof(WorkCursor) <= 152, "header");
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
 
   if (tid == 0) {
     for (int i = 0; i < STAGES; ++i) { p_bar_init(full + 8 * i, 1); p_bar_init(empty + 8 * i, 1); }
-    for (int i = 0; i < 2; ++i) { p_bar_init(s_full + 8 * i, 1); p_bar_init(s_free + 8 * i, SOFT); }
-    p_bar_init(p_full, SOFT); p_bar_init(pv_done, 1); p_bar_init(q_ready, SOFT); p_bar_init(drain, 1);
+    for (int i = 0; i < 2; ++i) { p_bar_init(s_full + 8 * i, 1); p_bar_init(s_free + 8 * i, SOFT); p_bar_init(q_ready + 8 * i, 64); p_bar_init(q_free + 8 * i, 1); }
+    p_bar_init(p_full, SOFT); p_bar_init(pv_done, 1); p_bar_init(drain, 1);
     *s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&ta.tm_k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&ta.tm_v) : "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(hb + 192), "n"(C::TMEM) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(hb + 216), "n"(C::TMEM) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
   }
   pdl_launch_dependents();
@@ -215,7 +227,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
   P_FENCE_BEFORE();
   __syncthreads();
   P_FENCE_AFTER();
-  const uint32_t tmem = *s_tmem, tmem_o = tmem + 2 * NR;
+  const uint32_t tmem = __shfl_sync(0xffffffffu, *s_tmem, 0), tmem_o = tmem + 2 * N;
   WorkCursor c = *s_cur;
 
   if (warp == 0) {
@@ -241,6 +253,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
           if (use > 0) {
             ok = p_wait(empty + 8 * slot, (uint32_t)(use - 1) & 1u, a.wait_ns, a.s.status, s_abort);
             ok = __all_sync(0xffffffffu, ok) && !*s_abort;
+            ok = __all_sync(0xffffffffu, ok);
             if (!ok) break;
           }
           if (lane == 0) {
@@ -269,83 +282,83 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
     }
   } else if (warp == 1) {
     // ---------------------------------------------------------------------------------------------------- products
-    if (lane == 0) {
-      bool ok = true;
-      int it = 0, sn = 0, pn = 0, qn = 0;   // half-tiles, score products, output products, parts so far
-      auto score = [&](int e) {             // S of the tile whose keys are half-tile e
-        const int buf = sn & 1;
-        if (sn >= 2) ok = ok && p_wait(s_free + 8 * buf, (uint32_t)((sn >> 1) - 1) & 1u, a.wait_ns, a.s.status, s_abort);
-        ok = ok && p_wait(full + 8 * (e % STAGES), (uint32_t)(e / STAGES) & 1u, a.wait_ns, a.s.status, s_abort);
-        if (!ok) return;
-        P_FENCE_AFTER();
-        const uint32_t k_at = ring + (uint32_t)(e % STAGES) * C::HALF;
-        uint32_t acc = 0;
-#pragma unroll
-        for (int part = PARTS - 1; part >= 0; --part)      // smallest parts first
-#pragma unroll
-          for (int ch = 0; ch < D / 64; ++ch) {
-            const uint64_t da = p_desc(k_at + ch * (TILE * 128), 16, 1024, 2), db = p_desc(q_s + part * C::QPART + ch * (NR * 128), 16, 1024, 2);
-#pragma unroll
-            for (int k = 0; k < 4; ++k) { p_mma(tmem + buf * NR, da + 2 * k, db + 2 * k, C::IDESC_S, acc); acc = 1; }
-          }
-        p_commit(empty + 8 * (e % STAGES));
-        p_commit(s_full + 8 * buf);
-        ++sn;
-      };
-      while (c.valid && ok) {
-        const int n = c.k1 - c.k0;
-        ok = p_wait(q_ready, (uint32_t)qn & 1u, a.wait_ns, a.s.status, s_abort);
-        ++qn;
-        if (ok) score(it);
-        for (int i = 0; i < n && ok; ++i, it += 2) {
-          if (i + 1 < n) score(it + 2);
-          const int e = it + 1;
-          ok = ok && p_wait(p_full, (uint32_t)pn & 1u, a.wait_ns, a.s.status, s_abort);
-          ok = ok && p_wait(full + 8 * (e % STAGES), (uint32_t)(e / STAGES) & 1u, a.wait_ns, a.s.status, s_abort);
-          if (!ok) break;
-          P_FENCE_AFTER();
-          const uint32_t v_at = ring + (uint32_t)(e % STAGES) * C::HALF;
-          uint32_t acc = 0;
-#pragma unroll
-          for (int part = PARTS - 1; part >= 0; --part) {
-            const uint64_t da = p_desc(v_at, TILE * 128, 1024, 2), db = p_desc(p_s + part * C::PPART, 16, 8 * C::P_ROW, C::P_LAYOUT);
-#pragma unroll
-            for (int k = 0; k < TILE / 16; ++k) { p_mma(tmem_o, da + k * (16 * 128 >> 4), db + k * (16 * C::P_ROW >> 4), C::IDESC_O, acc); acc = 1; }
-          }
-          p_commit(empty + 8 * (e % STAGES));
-          p_commit(pv_done);
-          ++pn;
-        }
-        cursor_next<NR, TILE>(a, c);
-      }
-      if (!ok) {   // every product issued so far must be done before the ring and the tensor memory go away
-        *s_abort = 1;
-        p_commit(drain);
-        const unsigned long long t0 = p_timer();
-        while (!p_try(drain, 0u) && p_timer() - t0 <= a.wait_ns) {}
-      }
-    }
-  } else {
-    // ---------------------------------------------------------------------------------------------------- softmax
-    const int st = tid - 64, quarter = warp & 3, group = (warp - 2) >> 2, col0 = group * COLS;
-    const int my = quarter * 32 + lane;                       // token of the tile, and row of O^T (for d = 128)
-    const uint32_t t_lane = (uint32_t)(quarter * 32) << 16;
-    const int my_col = COLS == 32 ? lane : lane >> 1;         // the column a fold leaves here
-    // After a wait that ran out the softmax threads keep their common path -- barriers among them always meet -- and skip
-    // the waits, until they agree at the part's end to stop.
+    const bool leader = p_elect();
     bool ok = true;
-    int sn = 0, pn = 0, it = 0;
-    auto soft_sync = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(SOFT) : "memory"); };
-    while (c.valid) {
-      const int R = c.nq * a.G, r0 = c.t * NR, n = c.k1 - c.k0, first_lim = c.len - c.nq + r0 / a.G;
-      // ---- Q, in PARTS bf16 parts, K-major: row r of block ch at r * 128, its 16-byte chunk k at chunk k ^ (r & 7)
-      for (int i = st; i < NR * (D / 8); i += SOFT) {
+    int e_s = 0, e_o = 1, sn = 0, pn = 0, qn = 0, s_i = 0;   // half-tiles of the next S and O, products so far, parts so far, S's tile in its part
+    WorkCursor cs = c;                                         // the part S is at; c is the part O is at
+    auto wait = [&](uint32_t bar, uint32_t parity) {
+      if (ok) ok = __all_sync(0xffffffffu, p_wait(bar, parity & 1u, a.wait_ns, a.s.status, s_abort));
+    };
+    auto score = [&]() {                                       // S of the next tile
+      if (!cs.valid) return;
+      const int buf = sn & 1, qb = qn % C::QBUF;
+      if (s_i == 0) wait(q_ready + 8 * qb, (uint32_t)(qn / C::QBUF));
+      if (sn >= 2) wait(s_free + 8 * buf, (uint32_t)((sn >> 1) - 1));
+      wait(full + 8 * (e_s % STAGES), (uint32_t)(e_s / STAGES));
+      if (!ok) return;
+      P_FENCE_AFTER();
+      const bool last = ++s_i == cs.k1 - cs.k0;
+      if (leader) {
+        const uint32_t ka = p_desc_lo(ring + (uint32_t)(e_s % STAGES) * C::HALF, 16), qa = p_desc_lo(ring + C::Q_AT + qb * C::Q_BYTES, 16), d = tmem + buf * N;
+#pragma unroll
+        for (int k = 0; k < D / 16; ++k)
+          p_mma(d, ka + (k >> 2) * (TILE * 128 >> 4) + (k & 3) * 2, p_desc_hi(1024, 2), qa + (k >> 2) * (N * 128 >> 4) + (k & 3) * 2, p_desc_hi(1024, 2), C::IDESC_S, k > 0);
+        p_commit(empty + 8 * (e_s % STAGES));
+        p_commit(s_full + 8 * buf);
+        if (last) p_commit(q_free + 8 * qb);
+      }
+      __syncwarp();
+      e_s += 2;
+      ++sn;
+      if (last) { cursor_next<NR, TILE>(a, cs); s_i = 0; ++qn; }
+    };
+    score();
+    while (c.valid && ok) {
+      for (int n = c.k1 - c.k0; n > 0 && ok; --n) {
+        score();
+        wait(p_full, (uint32_t)pn);
+        wait(full + 8 * (e_o % STAGES), (uint32_t)(e_o / STAGES));
+        if (!ok) break;
+        P_FENCE_AFTER();
+        if (leader) {
+          const uint32_t va = p_desc_lo(ring + (uint32_t)(e_o % STAGES) * C::HALF, TILE * 128), pa = p_desc_lo(ring + C::P_AT, C::P_BLOCK);
+#pragma unroll
+          for (int k = 0; k < TILE / 16; ++k)
+            p_mma(tmem_o, va + k * (16 * 128 >> 4), p_desc_hi(1024, 2), pa + k * (16 * 32 >> 4), p_desc_hi(256, 6), C::IDESC_O, k > 0);
+          p_commit(empty + 8 * (e_o % STAGES));
+          p_commit(pv_done);
+        }
+        __syncwarp();
+        e_o += 2;
+        ++pn;
+      }
+      cursor_next<NR, TILE>(a, c);
+    }
+    if (!ok) {   // every product issued so far must be done before the ring and the tensor memory go away
+      *s_abort = 1;
+      if (leader) p_commit(drain);
+      __syncwarp();
+      const unsigned long long t0 = p_timer();
+      while (!p_try(drain, 0u) && p_timer() - t0 <= a.wait_ns) {}
+    }
+  } else if (warp < 4) {
+    // ---------------------------------------------------------------------------------------------------- Q
+    const int qt = tid - 64;
+    bool ok = true;
+    for (int qn = 0; c.valid && ok; ++qn) {
+      const int qb = qn % C::QBUF, use = qn / C::QBUF, R = c.nq * a.G, r0 = c.t * NR;
+      if (use > 0) ok = p_wait(q_free + 8 * qb, (uint32_t)(use - 1) & 1u, a.wait_ns, a.s.status, s_abort);
+      if (!ok) break;
+      // K-major: row (part, r) of 64-element block ch at (part NR + r) * 128, its 16-byte chunk k at chunk k ^ (r & 7)
+#pragma unroll 2
+      for (int i = qt; i < NR * (D / 8); i += 64) {
         const int r = i / (D / 8), k8 = i - r * (D / 8), rr = r0 + r;
         float f[8];
 #pragma unroll
         for (int j = 0; j < 8; ++j) f[j] = 0.f;
         if (rr < R) {
-          const long long at = (long long)(c.row0 + rr / a.G) * a.q.row + (long long)(c.hk * a.G + rr % a.G) * a.q.head + k8 * 8;
+          const int tok = rr / a.G;
+          const long long at = (long long)(c.row0 + tok) * a.q.row + (long long)(c.hk * a.G + rr - tok * a.G) * a.q.head + k8 * 8;
           if (PARTS == 3) {
             const float* p = reinterpret_cast<const float*>(a.q.p) + at;
             if (a.q_vec) {
@@ -368,7 +381,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
             }
           }
         }
-        unsigned char* dst = mem + STAGES * C::HALF + (k8 >> 3) * (NR * 128) + r * 128 + (((k8 & 7) ^ (r & 7)) << 4);
+        unsigned char* dst = mem + C::Q_AT + qb * C::Q_BYTES + (k8 >> 3) * (N * 128) + r * 128 + (((k8 & 7) ^ (r & 7)) << 4);
 #pragma unroll
         for (int part = 0; part < PARTS; ++part) {
           uint32_t u[4];
@@ -377,21 +390,36 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
             u[j] = p_pack(f[2 * j], f[2 * j + 1]);
             if (part + 1 < PARTS) { f[2 * j] -= p_lo(u[j]); f[2 * j + 1] -= p_hi(u[j]); }
           }
-          *reinterpret_cast<uint4*>(dst + part * C::QPART) = make_uint4(u[0], u[1], u[2], u[3]);
+          *reinterpret_cast<uint4*>(dst + part * (NR * 128)) = make_uint4(u[0], u[1], u[2], u[3]);
         }
       }
+      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+      p_arrive(q_ready + 8 * qb);
+      cursor_next<NR, TILE>(a, c);
+    }
+  } else {
+    // ---------------------------------------------------------------------------------------------------- softmax
+    const int st = tid - 128, quarter = warp & 3, group = (warp - 4) >> 2, col0 = group * 16;
+    const int my = quarter * 32 + lane;                       // token of the tile, and row of O^T (for d = 128)
+    const uint32_t t_lane = (uint32_t)(quarter * 32) << 16;
+    // After a wait that ran out the softmax threads keep their common path -- barriers among them always meet -- and skip
+    // the waits, until they agree at the part's end to stop.
+    bool ok = true;
+    int sn = 0, pn = 0, it = 0;
+    auto all_sync = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(SOFT) : "memory"); };
+    auto group_sync = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(3 + group) : "memory"); };
+    while (c.valid) {
+      const int R = c.nq * a.G, r0 = c.t * NR, n = c.k1 - c.k0, first_lim = c.len - c.nq + r0 / a.G;
       if (st < NR) {
         const int rr = r0 + st, tok = rr / a.G;
         s_lim[st] = rr < R ? c.len - c.nq + tok : -1;
         s_off[st] = rr < R ? (long long)(c.row0 + tok) * a.out.row + (long long)(c.hk * a.G + rr - tok * a.G) * a.out.head : -1;
       }
       if (st == 0) *s_poison = 0x7fffffff;
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
-      p_arrive(q_ready);
-      soft_sync();
-      float l[COLS], o[COLS];
+      all_sync();
+      float l[16], o[16];
 #pragma unroll
-      for (int j = 0; j < COLS; ++j) l[j] = o[j] = 0.f;
+      for (int j = 0; j < 16; ++j) l[j] = o[j] = 0.f;
       // o += O^T of the last tile multiplied, once that product is done
       bool held = false;
       auto collect = [&]() {
@@ -400,12 +428,12 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
         ok = ok && p_wait(pv_done, (uint32_t)(pn - 1) & 1u, a.wait_ns, a.s.status, s_abort);
         __syncwarp();
         P_FENCE_AFTER();
-        float t[COLS];
+        float t[PARTS][16];
 #pragma unroll
-        for (int j = 0; j < COLS; j += 16) p_ld16(tmem_o + t_lane + col0 + j, t + j);
+        for (int part = 0; part < PARTS; ++part) p_ld16(tmem_o + t_lane + part * NR + col0, t[part]);
         P_WAIT_LD();
 #pragma unroll
-        for (int j = 0; j < COLS; ++j) o[j] += t[j];
+        for (int j = 0; j < 16; ++j) o[j] += PARTS == 3 ? t[0][j] + (t[PARTS / 2][j] + t[PARTS - 1][j]) : t[0][j];
       };
       for (int i = 0; i < n; ++i, ++sn, it += 2) {
         const int buf = sn & 1, p0 = (c.k0 + i) * TILE, pos = p0 + my;
@@ -413,10 +441,15 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
         ok = ok && p_wait(s_full + 8 * buf, (uint32_t)(sn >> 1) & 1u, a.wait_ns, a.s.status, s_abort);
         __syncwarp();
         P_FENCE_AFTER();
-        float x[COLS];
+        float x[16];
+        {
+          float t[PARTS][16];
 #pragma unroll
-        for (int j = 0; j < COLS; j += 16) p_ld16(tmem + buf * NR + t_lane + col0 + j, x + j);
-        P_WAIT_LD();
+          for (int part = 0; part < PARTS; ++part) p_ld16(tmem + buf * N + t_lane + part * NR + col0, t[part]);
+          P_WAIT_LD();
+#pragma unroll
+          for (int j = 0; j < 16; ++j) x[j] = PARTS == 3 ? t[0][j] + (t[PARTS / 2][j] + t[PARTS - 1][j]) : t[0][j];
+        }
         P_FENCE_BEFORE();
         p_arrive(s_free + 8 * buf);
         // ---- the reference maximum: the first tile's, later only when a score has outgrown it
@@ -424,7 +457,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
         if (i > 0) {
           float up = -INFINITY;
 #pragma unroll
-          for (int j = 0; j < COLS; j += 4) {
+          for (int j = 0; j < 16; j += 4) {
             const float4 m = *reinterpret_cast<const float4*>(s_a + col0 + j);
             const float y[4] = {fmaf(x[j], a.scale_log2, -m.x), fmaf(x[j + 1], a.scale_log2, -m.y), fmaf(x[j + 2], a.scale_log2, -m.z), fmaf(x[j + 3], a.scale_log2, -m.w)};
             if (edge) {
@@ -435,20 +468,20 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
             }
           }
           uint32_t any;
-          asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.or.pred p, 1, %2, q;\n selp.u32 %0, 1, 0, p;\n}\n"
-                       : "=r"(any) : "r"(up > MAX_UP ? 1u : 0u), "n"(SOFT) : "memory");
+          asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.or.pred p, %2, 128, q;\n selp.u32 %0, 1, 0, p;\n}\n"
+                       : "=r"(any) : "r"(up > MAX_UP ? 1u : 0u), "r"(3 + group) : "memory");
           retake = any != 0;
         }
         if (retake) {
-          float y[COLS];
+          float y[16];
 #pragma unroll
-          for (int j = 0; j < COLS; ++j) y[j] = pos <= s_lim[col0 + j] ? x[j] * a.scale_log2 : -INFINITY;
-          const float top = fold<OpMax, COLS>(y, lane);
-          s_red[quarter * NR + col0 + my_col] = top;
+          for (int j = 0; j < 16; ++j) y[j] = pos <= s_lim[col0 + j] ? x[j] * a.scale_log2 : -INFINITY;
+          const float top = fold16<OpMax>(y, lane);
+          s_red[quarter * NR + col0 + (lane >> 1)] = top;
           if (i > 0) collect();
-          soft_sync();
+          group_sync();
 #pragma unroll
-          for (int j = 0; j < COLS; ++j) {
+          for (int j = 0; j < 16; ++j) {
             const int cc = col0 + j;
             const float t = fmaxf(fmaxf(s_red[cc], s_red[NR + cc]), fmaxf(s_red[2 * NR + cc], s_red[3 * NR + cc]));
             if (i == 0) {
@@ -460,16 +493,16 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
               o[j] *= al;
             }
           }
-          soft_sync();   // everyone has read s_red and the old maxima
+          group_sync();   // everyone has read s_red and the old maxima
           if (my == 0) {
 #pragma unroll
-            for (int j = 0; j < COLS; ++j) s_a[col0 + j] = y[j];
+            for (int j = 0; j < 16; ++j) s_a[col0 + j] = y[j];
           }
-          soft_sync();
+          group_sync();
         }
         // ---- weights
 #pragma unroll
-        for (int j = 0; j < COLS; j += 4) {
+        for (int j = 0; j < 16; j += 4) {
           const float4 m = *reinterpret_cast<const float4*>(s_a + col0 + j);
           x[j] = p_ex2(fmaf(x[j], a.scale_log2, -m.x));
           x[j + 1] = p_ex2(fmaf(x[j + 1], a.scale_log2, -m.y));
@@ -485,7 +518,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
         }
         if (PARTS == 3) {
 #pragma unroll
-          for (int j = 0; j < COLS; ++j) l[j] += x[j];
+          for (int j = 0; j < 16; ++j) l[j] += x[j];
         }
         // P^T is written once the previous output product has read it
         if (i > 0) collect();
@@ -517,11 +550,10 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
             }
           }
         }
-        unsigned char* pr = mem + STAGES * C::HALF + PARTS * C::QPART + my * C::P_ROW;
-        const int sw = NR >= 64 ? my & 7 : (NR == 32 ? (my >> 1) & 3 : (my >> 2) & 1);
+        unsigned char* pr = mem + C::P_AT + group * C::P_BLOCK + my * 32;
+        const int sw = (my >> 2) & 1;                          // 32-byte swizzle: a token's two 16-byte chunks swap in every other group of 4
 #pragma unroll
-        for (int k = 0; k < COLS / 8; ++k) {
-          unsigned char* dst = pr + (((col0 / 8 + k) ^ sw) << 4);
+        for (int k = 0; k < 2; ++k) {
 #pragma unroll
           for (int part = 0; part < PARTS; ++part) {
             uint32_t u[4];
@@ -532,7 +564,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
               if (PARTS == 1) { l[8 * k + 2 * j] += p_lo(u[j]); l[8 * k + 2 * j + 1] += p_hi(u[j]); }
               if (part + 1 < PARTS) { f0 -= p_lo(u[j]); f1 -= p_hi(u[j]); }
             }
-            *reinterpret_cast<uint4*>(dst + part * C::PPART) = make_uint4(u[0], u[1], u[2], u[3]);
+            *reinterpret_cast<uint4*>(pr + part * C::GROUPS * C::P_BLOCK + ((k ^ sw) << 4)) = make_uint4(u[0], u[1], u[2], u[3]);
           }
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
@@ -542,8 +574,8 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
         held = true;
       }
       // ---- the part's end: sums over the tokens, then O^T
-      const float sum = fold<OpAdd, COLS>(l, lane);
-      s_red[quarter * NR + col0 + my_col] = sum;
+      const float sum = fold16<OpAdd>(l, lane);
+      s_red[quarter * NR + col0 + (lane >> 1)] = sum;
       collect();
       int first, parts;
       item_ctas(c, first, parts);
@@ -566,13 +598,13 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
           s_b[st] = t == 0.f ? 0.f : 1.f / t;
         }
       }
-      soft_sync();
+      all_sync();
       const int e = D == 128 ? my : quarter * 16 + lane;      // element of the head (d = 64: 16 rows in each quarter's first 16 lanes)
       const bool live_lane = D == 128 || lane < 16;
       float* slot = a.slots + slot_floats<NR, D>() * (size_t)part_slot(blockIdx.x, c.k0 == 0);
       if (live_lane) {
 #pragma unroll
-        for (int j = 0; j < COLS; ++j) {
+        for (int j = 0; j < 16; ++j) {
           const int r = col0 + j;
           const long long at = s_off[r];
           if (at < 0) continue;
@@ -587,15 +619,15 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
       if (parts > 1) {
         if (st < NR) { __stcg(slot + st, s_a[st]); __stcg(slot + NR + st, s_b[st]); }
         __threadfence();
-        soft_sync();
+        all_sync();
         if (st == 0) {
           *s_last = atomicAdd(a.counters + first, 1) == parts - 1;
           if (*s_last) { a.counters[first] = 0; __threadfence(); }
         }
-        soft_sync();
-        if (*s_last) join_parts<NR, D, SOFT>(a, c, first, parts, st, s_b, s_a, reinterpret_cast<float*>(mem + STAGES * C::HALF + PARTS * C::QPART));
+        all_sync();
+        if (*s_last) join_parts<NR, D, SOFT>(a, c, first, parts, st, s_b, s_a, reinterpret_cast<float*>(mem + C::P_AT), C::P_BYTES / 4);
       }
-      soft_sync();   // s_a, s_b, s_lim are free again
+      all_sync();   // s_a, s_b, s_lim are free again
       cursor_next<NR, TILE>(a, c);
     }
     if (!ok) *s_abort = 1;
@@ -651,10 +683,17 @@ cudaError_t tc_go(const PagedAttnArgs& a, int num_sm, cudaStream_t st) {
   return launch_k(paged_attn_tc_kernel<D, NR, PARTS>, dim3(paged_attn_grid(num_sm)), dim3(Cfg<D, NR, PARTS>::THREADS), Cfg<D, NR, PARTS>::SMEM, st, t);
 }
 
+// The fewest rows per tile that hold a sequence's rows of one key head; more rows go in tiles of the largest width.
 template <int D>
 cudaError_t tc_rows(const PagedAttnArgs& a, long long rows, int num_sm, cudaStream_t st) {
-  if (a.q_bf16) return rows <= 16 ? tc_go<D, 16, 1>(a, num_sm, st) : tc_go<D, 64, 1>(a, num_sm, st);
-  return rows <= 16 ? tc_go<D, 16, 3>(a, num_sm, st) : tc_go<D, 64, 3>(a, num_sm, st);
+  if (a.q_bf16) {
+    if (rows <= 16) return tc_go<D, 16, 1>(a, num_sm, st);
+    if (rows <= 32) return tc_go<D, 32, 1>(a, num_sm, st);
+    return tc_go<D, 64, 1>(a, num_sm, st);
+  }
+  if (rows <= 16) return tc_go<D, 16, 3>(a, num_sm, st);
+  if (rows <= 32) return tc_go<D, 32, 3>(a, num_sm, st);
+  return tc_go<D, 48, 3>(a, num_sm, st);
 }
 
 }  // namespace
