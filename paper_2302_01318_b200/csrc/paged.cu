@@ -440,6 +440,7 @@ int sps_paged_attention(const sps_paged_cache* cache, const sps_paged_batch* bat
   a.k = cache->k; a.v = cache->v;
   a.page_stride = cache->page_stride; a.head_stride = cache->head_stride; a.pos_stride = cache->pos_stride;
   a.H = q->heads; a.Hkv = cache->n_kv_heads; a.G = a.H / a.Hkv;
+  a.g_magic = a.G > 1 ? ~0ull / (unsigned long long)a.G + 1 : 0;   // ceil(2^64 / G), powers of two included
   a.scale_log2 = (scale == 0.f ? 1.f / std::sqrt((float)cache->d_head) : scale) * 1.4426950408889634f;
   a.lse = lse;
   a.counters = (int*)workspace;

@@ -55,6 +55,7 @@ struct PagedAttnArgs {
   void *k, *v;
   long long page_stride, head_stride, pos_stride;
   int H, Hkv, G;
+  unsigned long long g_magic;   // ceil(2^64 / G) for G > 1: row / G is a high product
   float scale_log2;         // scale * log2(e): scores are kept in base 2
   float* lse;               // [rows][H] or null
   int* counters;            // [grid] arrivals at an item, by the first CTA that works on it; zero between launches
@@ -62,11 +63,14 @@ struct PagedAttnArgs {
   unsigned long long wait_ns;
 };
 
+// r / G for a row of a group of G heads
+__device__ __forceinline__ int row_token(const PagedAttnArgs& a, int r) { return a.G == 1 ? r : (int)__umul64hi((unsigned long long)r, a.g_magic); }
+
 // tiles of KT tokens row tile t of a sequence has to read
 template <int NR, int KT>
-__device__ __forceinline__ int item_tiles(int nq, int len, int G, int t) {
-  const int last = min((t + 1) * NR, nq * G) - 1;
-  const int pos = len - nq + last / G;
+__device__ __forceinline__ int item_tiles(const PagedAttnArgs& a, int nq, int len, int t) {
+  const int last = min((t + 1) * NR, nq * a.G) - 1;
+  const int pos = len - nq + row_token(a, last);
   return pos < 0 ? 1 : pos / KT + 1;
 }
 
@@ -83,7 +87,7 @@ struct WorkCursor {       // a place in the list of items, and the run of tiles 
 
 template <int NR, int KT>
 __device__ __forceinline__ void cursor_part(const PagedAttnArgs& a, WorkCursor& c) {   // the part of item (b, hk, t) that begins at c.u
-  c.n = item_tiles<NR, KT>(c.nq, c.len, a.G, c.t);
+  c.n = item_tiles<NR, KT>(a, c.nq, c.len, c.t);
   c.k0 = (int)(c.u - c.item0);
   const long long left = c.u_end - c.u, rest = c.n - c.k0;
   c.k1 = c.k0 + (int)(left < rest ? left : rest);
@@ -116,14 +120,14 @@ __device__ __forceinline__ long long warp_seq_units(const PagedAttnArgs& a, cons
   const int lane = threadIdx.x & 31;
   const int nt = live ? (int)(((long long)g.nq * a.G + NR - 1) / NR) : 0;
   long long sum = 0;
-  if (nt <= 4) for (int t = 0; t < nt; ++t) sum += item_tiles<NR, KT>(g.nq, g.len, a.G, t);
+  if (nt <= 4) for (int t = 0; t < nt; ++t) sum += item_tiles<NR, KT>(a, g.nq, g.len, t);
   unsigned big = __ballot_sync(0xffffffffu, nt > 4);
   while (big) {
     const int src = __ffs(big) - 1;
     big &= big - 1;
     const int nq = __shfl_sync(0xffffffffu, g.nq, src), len = __shfl_sync(0xffffffffu, g.len, src), n = __shfl_sync(0xffffffffu, nt, src);
     long long part = 0;
-    for (int t = lane; t < n; t += 32) part += item_tiles<NR, KT>(nq, len, a.G, t);
+    for (int t = lane; t < n; t += 32) part += item_tiles<NR, KT>(a, nq, len, t);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
     if (lane == src) sum = part;
@@ -190,7 +194,7 @@ __device__ __forceinline__ WorkCursor cursor_begin(const PagedAttnArgs& a, int m
       // the row tile: 32 at a time
       for (int t0 = 0; t0 < c.nt; t0 += 32) {
         const int t = t0 + lane;
-        const long long n = t < c.nt ? item_tiles<NR, KT>(c.nq, c.len, a.G, t) : 0;
+        const long long n = t < c.nt ? item_tiles<NR, KT>(a, c.nq, c.len, t) : 0;
         long long in2 = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
@@ -217,6 +221,9 @@ __device__ __forceinline__ WorkCursor cursor_begin(const PagedAttnArgs& a, int m
 
 // parts an item is cut into: the CTAs first .. first + parts - 1 each hold one
 __device__ __forceinline__ void item_ctas(const WorkCursor& c, int& first, int& parts) {
+  first = blockIdx.x;
+  parts = 1;
+  if (c.k0 == 0 && c.k1 == c.n) return;
   first = (int)(c.item0 / c.per);
   parts = (int)((c.item0 + c.n - 1) / c.per) - first + 1;
 }
@@ -267,7 +274,7 @@ __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCur
     w_inv[tid] = L == 0.f ? 0.f : 1.f / L;
     if (a.lse) {
       const int r = r0 + tid;
-      a.lse[(size_t)(c.row0 + r / a.G) * a.H + c.hk * a.G + r % a.G] = L == 0.f ? -INFINITY : 0.6931471805599453f * (base + log2f(L));
+      a.lse[(size_t)(c.row0 + row_token(a, r)) * a.H + c.hk * a.G + r - row_token(a, r) * a.G] = L == 0.f ? -INFINITY : 0.6931471805599453f * (base + log2f(L));
     }
   }
   sync();
@@ -301,8 +308,8 @@ __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCur
   for (int k = 0; k < PIECES; ++k) {
     const int i = tid + k * THREADS;
     if (i < live * (D / 4)) {
-      const int r = i / (D / 4), e = (i - r * (D / 4)) * 4, rr = r0 + r;
-      const long long at = (long long)(c.row0 + rr / a.G) * a.out.row + (long long)(c.hk * a.G + rr % a.G) * a.out.head + e;
+      const int r = i / (D / 4), e = (i - r * (D / 4)) * 4, rr = r0 + r, tok = row_token(a, rr);
+      const long long at = (long long)(c.row0 + tok) * a.out.row + (long long)(c.hk * a.G + rr - tok * a.G) * a.out.head + e;
       store_out(a, at, o[k].x); store_out(a, at + 1, o[k].y); store_out(a, at + 2, o[k].z); store_out(a, at + 3, o[k].w);
     }
   }

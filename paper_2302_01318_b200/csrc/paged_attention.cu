@@ -44,20 +44,21 @@ __global__ void __launch_bounds__(SIMT_THREADS) paged_attn_simt_kernel(const __g
       const int r = i / D, e = i - r * D, rr = r0 + r;
       float v = 0.f;
       if (rr < R) {
-        const long long at = (long long)(c.row0 + rr / a.G) * a.q.row + (long long)(c.hk * a.G + rr % a.G) * a.q.head + e;
+        const int tok = row_token(a, rr);
+        const long long at = (long long)(c.row0 + tok) * a.q.row + (long long)(c.hk * a.G + rr - tok * a.G) * a.q.head + e;
         v = reinterpret_cast<const float*>(a.q.p)[at];
       }
       Qs[i] = v * a.scale_log2;
     }
     if (tid < NR) {
-      s_lim[tid] = r0 + tid < R ? c.len - c.nq + (r0 + tid) / a.G : -1;
+      s_lim[tid] = r0 + tid < R ? c.len - c.nq + row_token(a, r0 + tid) : -1;
       s_m[tid] = -INFINITY;
       s_l[tid] = 0.f;
     }
     float o[RPT][2];
 #pragma unroll
     for (int i = 0; i < RPT; ++i) o[i][0] = o[i][1] = 0.f;
-    const int first_lim = c.len - c.nq + r0 / a.G;
+    const int first_lim = c.len - c.nq + row_token(a, r0);
     for (int kt = c.k0; kt < c.k1; ++kt) {
       const int p0 = kt * KT;
       __syncthreads();
@@ -146,13 +147,14 @@ __global__ void __launch_bounds__(SIMT_THREADS) paged_attn_simt_kernel(const __g
         const int r = rg * RPT + i, rr = r0 + r;
         if (rr >= R) continue;
         const float l = s_l[r], inv = l == 0.f ? 0.f : 1.f / l;
-        const long long at = (long long)(c.row0 + rr / a.G) * a.out.row + (long long)(c.hk * a.G + rr % a.G) * a.out.head + 2 * dp;
+        const int tok = row_token(a, rr);
+        const long long at = (long long)(c.row0 + tok) * a.out.row + (long long)(c.hk * a.G + rr - tok * a.G) * a.out.head + 2 * dp;
         store_out(a, at, o[i][0] * inv);
         store_out(a, at + 1, o[i][1] * inv);
       }
       if (a.lse && tid < NR && r0 + tid < R) {
-        const int rr = r0 + tid;
-        a.lse[(size_t)(c.row0 + rr / a.G) * a.H + c.hk * a.G + rr % a.G] = s_l[tid] == 0.f ? -INFINITY : 0.6931471805599453f * (s_m[tid] + log2f(s_l[tid]));
+        const int rr = r0 + tid, tok = row_token(a, rr);
+        a.lse[(size_t)(c.row0 + tok) * a.H + c.hk * a.G + rr - tok * a.G] = s_l[tid] == 0.f ? -INFINITY : 0.6931471805599453f * (s_m[tid] + log2f(s_l[tid]));
       }
     } else {
       float* slot = a.slots + slot_floats<NR, D>() * (size_t)part_slot(blockIdx.x, c.k0 == 0);
@@ -162,9 +164,9 @@ __global__ void __launch_bounds__(SIMT_THREADS) paged_attn_simt_kernel(const __g
         const int r = rg * RPT + i;
         if (r0 + r < R) __stcg(reinterpret_cast<float2*>(slot + 2 * NR + r * D + 2 * dp), make_float2(o[i][0], o[i][1]));
       }
-      __threadfence();
       __syncthreads();
       if (tid == 0) {
+        __threadfence();   // the CTA's parts are out before its arrival is
         s_last = atomicAdd(a.counters + first, 1) == parts - 1;
         if (s_last) { a.counters[first] = 0; __threadfence(); }
       }

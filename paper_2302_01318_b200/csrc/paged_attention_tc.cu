@@ -10,9 +10,10 @@
 // row costs a product 16 columns wide instead of 128.  A thread owns one token of the tile (a lane of tensor memory) and
 // all its rows' scores; it masks, exponentiates and stores its row of P^T.
 //
-// Running maximum.  The weights are 2^(s - m) with m fixed at the maximum of the part's first tile: P is bf16 (8 exponent
-// bits) or three bf16 parts of an fp32 number, sums are fp32, so m only has to keep the weights in range, not at most 1.
-// Only when a score exceeds m by 2^MAX_UP do the CTA's threads agree (a reducing barrier) to take the new maximum and
+// Running maximum.  The weights are 2^(s - m) with m fixed at the score of the part's first token, which every row that sees
+// anything of the part sees: P is bf16 (8 exponent bits) or three bf16 parts of an fp32 number, sums are fp32, so m only
+// has to keep the weights in range, not at most 1, and a weight of 1 is among them.  Only when a score exceeds m by
+// MAX_UP (in base 2) do the threads of a column group agree (a reducing barrier) to take the new maximum and
 // rescale what they hold.  That leaves a multiply-add, an exponential, an addition and the rounding per score, no
 // cross-lane reduction per tile.  Sums stay per thread (its token of every tile) until the part ends.  Each tile's O^T
 // is a product of its own, added to fp32 registers: the tensor cores cut the low bits of a running sum instead of rounding
@@ -133,6 +134,14 @@ __device__ __forceinline__ float p_ex2(float x) {
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
 }
+// two fp32 operations in one instruction
+__device__ __forceinline__ void p_add2(float& x, float& y, float a, float b) {
+  asm("{\n .reg .b64 s, t;\n mov.b64 s, {%0, %1};\n mov.b64 t, {%2, %3};\n add.rn.f32x2 s, s, t;\n mov.b64 {%0, %1}, s;\n}\n" : "+f"(x), "+f"(y) : "f"(a), "f"(b));
+}
+__device__ __forceinline__ void p_fma2(float& x, float& y, float f, float a, float b) {   // (x, y) f + (a, b)
+  asm("{\n .reg .b64 s, t, u;\n mov.b64 s, {%0, %1};\n mov.b64 t, {%2, %2};\n mov.b64 u, {%3, %4};\n fma.rn.f32x2 s, s, t, u;\n mov.b64 {%0, %1}, s;\n}\n"
+      : "+f"(x), "+f"(y) : "f"(f), "f"(a), "f"(b));
+}
 // two floats rounded to bf16, the first in the low half
 __device__ __forceinline__ uint32_t p_pack(float lo, float hi) {
   uint32_t r;
@@ -167,7 +176,7 @@ template <int D, int NR, int PARTS> struct Cfg {
   static constexpr int N = PARTS * NR;                              // columns of a product
   static constexpr uint32_t HALF = TILE * D * 2;                    // keys or values of a tile
   static constexpr uint32_t Q_BYTES = N * D * 2, P_BYTES = TILE * N * 2;
-  static constexpr uint32_t HDR = 3072;                             // barriers, small per-row arrays
+  static constexpr uint32_t HDR = 3328;                             // barriers, small per-row arrays
   static constexpr int BUDGET = 232448 - (int)HDR - (int)P_BYTES;
   static constexpr int QBUF = (BUDGET - 2 * (int)Q_BYTES) / (int)HALF >= 4 ? 2 : 1;
   static constexpr int STAGES_FIT = (BUDGET - QBUF * (int)Q_BYTES) / (int)HALF;
@@ -201,8 +210,9 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
   float* s_a = reinterpret_cast<float*>(hdr + 384 + NR * 4);           // [NR] maxima
   float* s_b = s_a + NR;                                               // [NR] sums / factors
   float* s_red = s_b + NR;                                             // [4][NR]
-  long long* s_off = reinterpret_cast<long long*>(s_red + 4 * NR);     // [NR] where a row's output goes, -1: no such row
-  static_assert(384 + NR * 4 * 9 <= (int)C::HDR && sizeof(WorkCursor) <= 152, "header");
+  long long* s_off = reinterpret_cast<long long*>(s_red + 4 * NR);     // [NR] where a row's output goes
+  long long* s_qat = s_off + NR;                                       // [NR] where a row of Q is
+  static_assert(384 + NR * 4 * 11 <= (int)C::HDR && sizeof(WorkCursor) <= 152, "header");
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
 
   if (tid == 0) {
@@ -237,12 +247,13 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
     const int boxes = TILE / ta.box;
     while (c.valid && ok) {
       const int32_t* table = a.s.pages + (long long)c.b * a.s.pages_ld;
+      int next = lane < boxes && c.k0 * TILE + lane * ta.box < c.len ? table[(c.k0 * TILE + lane * ta.box) >> a.s.page_shift] : 0;
       for (int kt = c.k0; kt < c.k1 && ok; ++kt) {
-        const int p0 = kt * TILE, pos = p0 + lane * ta.box;
+        const int pos = kt * TILE + lane * ta.box;
         const bool mine = lane < boxes && pos < c.len;
-        int page = 0;
+        int page = next;
+        if (kt + 1 < c.k1 && lane < boxes && pos + TILE < c.len) next = table[(pos + TILE) >> a.s.page_shift];   // under way while this tile waits
         if (mine) {
-          page = table[pos >> a.s.page_shift];
           if (page < 0 || page >= a.s.n_pages) { paged_flag(a.s.status, SPS_PAGED_BAD_PAGE); page = a.s.n_pages; }   // outside the map: zeros
         }
         const int in_page = pos & (a.s.page_size - 1);
@@ -343,56 +354,72 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
     }
   } else if (warp < 4) {
     // ---------------------------------------------------------------------------------------------------- Q
+    constexpr int CHUNKS = NR * (D / 8) / 64, BATCH = CHUNKS % 4 == 0 ? 4 : (CHUNKS % 3 == 0 ? 3 : 2);   // 8-element chunks per thread; loads in flight
+    static_assert(NR * (D / 8) % 64 == 0 && CHUNKS % BATCH == 0, "every chunk belongs to a row of the tile");
     const int qt = tid - 64;
     bool ok = true;
     for (int qn = 0; c.valid && ok; ++qn) {
-      const int qb = qn % C::QBUF, use = qn / C::QBUF, R = c.nq * a.G, r0 = c.t * NR;
-      if (use > 0) ok = p_wait(q_free + 8 * qb, (uint32_t)(use - 1) & 1u, a.wait_ns, a.s.status, s_abort);
-      if (!ok) break;
+      const int qb = qn % C::QBUF, use = qn / C::QBUF, live = c.nq * a.G - c.t * NR;
+      if (qt < NR) {
+        const int rr = c.t * NR + qt, tok = row_token(a, rr);
+        s_qat[qt] = (long long)(c.row0 + tok) * a.q.row + (long long)(c.hk * a.G + rr - tok * a.G) * a.q.head;
+      }
+      asm volatile("bar.sync 7, 64;" ::: "memory");
       // K-major: row (part, r) of 64-element block ch at (part NR + r) * 128, its 16-byte chunk k at chunk k ^ (r & 7)
-#pragma unroll 2
-      for (int i = qt; i < NR * (D / 8); i += 64) {
-        const int r = i / (D / 8), k8 = i - r * (D / 8), rr = r0 + r;
-        float f[8];
+#pragma unroll 1
+      for (int b0 = 0; b0 < CHUNKS; b0 += BATCH) {
+        float f[BATCH][8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) f[j] = 0.f;
-        if (rr < R) {
-          const int tok = rr / a.G;
-          const long long at = (long long)(c.row0 + tok) * a.q.row + (long long)(c.hk * a.G + rr - tok * a.G) * a.q.head + k8 * 8;
-          if (PARTS == 3) {
-            const float* p = reinterpret_cast<const float*>(a.q.p) + at;
-            if (a.q_vec) {
-              const float4 x = *reinterpret_cast<const float4*>(p), y = *reinterpret_cast<const float4*>(p + 4);
-              f[0] = x.x; f[1] = x.y; f[2] = x.z; f[3] = x.w; f[4] = y.x; f[5] = y.y; f[6] = y.z; f[7] = y.w;
+        for (int b = 0; b < BATCH; ++b) {
+          const int i = qt + (b0 + b) * 64, r = i / (D / 8), k8 = i - r * (D / 8);
+#pragma unroll
+          for (int j = 0; j < 8; ++j) f[b][j] = 0.f;
+          if (r < live) {
+            const long long at = s_qat[r] + k8 * 8;
+            if (PARTS == 3) {
+              const float* p = reinterpret_cast<const float*>(a.q.p) + at;
+              if (a.q_vec) {
+                const float4 x = *reinterpret_cast<const float4*>(p), y = *reinterpret_cast<const float4*>(p + 4);
+                f[b][0] = x.x; f[b][1] = x.y; f[b][2] = x.z; f[b][3] = x.w; f[b][4] = y.x; f[b][5] = y.y; f[b][6] = y.z; f[b][7] = y.w;
+              } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j) f[b][j] = p[j];
+              }
             } else {
+              const __nv_bfloat16* p = reinterpret_cast<const __nv_bfloat16*>(a.q.p) + at;
+              if (a.q_vec) {
+                const uint4 u = *reinterpret_cast<const uint4*>(p);
+                const uint32_t w[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
-              for (int j = 0; j < 8; ++j) f[j] = p[j];
-            }
-          } else {
-            const __nv_bfloat16* p = reinterpret_cast<const __nv_bfloat16*>(a.q.p) + at;
-            if (a.q_vec) {
-              const uint4 u = *reinterpret_cast<const uint4*>(p);
-              const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+                for (int j = 0; j < 4; ++j) { f[b][2 * j] = p_lo(w[j]); f[b][2 * j + 1] = p_hi(w[j]); }
+              } else {
 #pragma unroll
-              for (int j = 0; j < 4; ++j) { f[2 * j] = p_lo(w[j]); f[2 * j + 1] = p_hi(w[j]); }
-            } else {
-#pragma unroll
-              for (int j = 0; j < 8; ++j) f[j] = __bfloat162float(p[j]);
+                for (int j = 0; j < 8; ++j) f[b][j] = __bfloat162float(p[j]);
+              }
             }
           }
         }
-        unsigned char* dst = mem + C::Q_AT + qb * C::Q_BYTES + (k8 >> 3) * (N * 128) + r * 128 + (((k8 & 7) ^ (r & 7)) << 4);
+        if (b0 == 0 && use > 0) ok = p_wait(q_free + 8 * qb, (uint32_t)(use - 1) & 1u, a.wait_ns, a.s.status, s_abort);   // the first loads are under way
+        if (!ok) break;
 #pragma unroll
-        for (int part = 0; part < PARTS; ++part) {
-          uint32_t u[4];
+        for (int b = 0; b < BATCH; ++b) {
+          const int i = qt + (b0 + b) * 64, r = i / (D / 8), k8 = i - r * (D / 8);
+          unsigned char* dst = mem + C::Q_AT + qb * C::Q_BYTES + (k8 >> 3) * (N * 128) + r * 128 + (((k8 & 7) ^ (r & 7)) << 4);
 #pragma unroll
-          for (int j = 0; j < 4; ++j) {
-            u[j] = p_pack(f[2 * j], f[2 * j + 1]);
-            if (part + 1 < PARTS) { f[2 * j] -= p_lo(u[j]); f[2 * j + 1] -= p_hi(u[j]); }
+          for (int part = 0; part < PARTS; ++part) {
+            uint32_t u[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+              u[j] = p_pack(f[b][2 * j], f[b][2 * j + 1]);
+              if (part + 1 < PARTS) { f[b][2 * j] -= p_lo(u[j]); f[b][2 * j + 1] -= p_hi(u[j]); }
+            }
+            *reinterpret_cast<uint4*>(dst + part * (NR * 128)) = make_uint4(u[0], u[1], u[2], u[3]);
           }
-          *reinterpret_cast<uint4*>(dst + part * (NR * 128)) = make_uint4(u[0], u[1], u[2], u[3]);
         }
       }
+      uint32_t both;   // (and s_qat may be written again)
+      asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.and.pred p, 7, 64, q;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(both) : "r"(ok ? 1u : 0u) : "memory");
+      if (!both) break;
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       p_arrive(q_ready + 8 * qb);
       cursor_next<NR, TILE>(a, c);
@@ -409,11 +436,11 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
     auto all_sync = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(SOFT) : "memory"); };
     auto group_sync = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(3 + group) : "memory"); };
     while (c.valid) {
-      const int R = c.nq * a.G, r0 = c.t * NR, n = c.k1 - c.k0, first_lim = c.len - c.nq + r0 / a.G;
+      const int R = c.nq * a.G, r0 = c.t * NR, n = c.k1 - c.k0, first_lim = c.len - c.nq + row_token(a, r0);
       if (st < NR) {
-        const int rr = r0 + st, tok = rr / a.G;
+        const int rr = r0 + st, tok = row_token(a, rr);
         s_lim[st] = rr < R ? c.len - c.nq + tok : -1;
-        s_off[st] = rr < R ? (long long)(c.row0 + tok) * a.out.row + (long long)(c.hk * a.G + rr - tok * a.G) * a.out.head : -1;
+        s_off[st] = rr < R ? (long long)(c.row0 + tok) * a.out.row + (long long)(c.hk * a.G + rr - tok * a.G) * a.out.head : 0;
       }
       if (st == 0) *s_poison = 0x7fffffff;
       all_sync();
@@ -433,7 +460,13 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
         for (int part = 0; part < PARTS; ++part) p_ld16(tmem_o + t_lane + part * NR + col0, t[part]);
         P_WAIT_LD();
 #pragma unroll
-        for (int j = 0; j < 16; ++j) o[j] += PARTS == 3 ? t[0][j] + (t[PARTS / 2][j] + t[PARTS - 1][j]) : t[0][j];
+        for (int j = 0; j < 16; j += 2) {
+          if (PARTS == 3) {
+            p_add2(t[PARTS / 2][j], t[PARTS / 2][j + 1], t[PARTS - 1][j], t[PARTS - 1][j + 1]);
+            p_add2(t[0][j], t[0][j + 1], t[PARTS / 2][j], t[PARTS / 2][j + 1]);
+          }
+          p_add2(o[j], o[j + 1], t[0][j], t[0][j + 1]);
+        }
       };
       for (int i = 0; i < n; ++i, ++sn, it += 2) {
         const int buf = sn & 1, p0 = (c.k0 + i) * TILE, pos = p0 + my;
@@ -448,77 +481,75 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
           for (int part = 0; part < PARTS; ++part) p_ld16(tmem + buf * N + t_lane + part * NR + col0, t[part]);
           P_WAIT_LD();
 #pragma unroll
-          for (int j = 0; j < 16; ++j) x[j] = PARTS == 3 ? t[0][j] + (t[PARTS / 2][j] + t[PARTS - 1][j]) : t[0][j];
+          for (int j = 0; j < 16; j += 2) {
+            if (PARTS == 3) {
+              p_add2(t[PARTS / 2][j], t[PARTS / 2][j + 1], t[PARTS - 1][j], t[PARTS - 1][j + 1]);
+              p_add2(t[0][j], t[0][j + 1], t[PARTS / 2][j], t[PARTS / 2][j + 1]);
+            }
+            x[j] = t[0][j];
+            x[j + 1] = t[0][j + 1];
+          }
         }
         P_FENCE_BEFORE();
         p_arrive(s_free + 8 * buf);
-        // ---- the reference maximum: the first tile's, later only when a score has outgrown it
-        bool retake = i == 0;
-        if (i > 0) {
-          float up = -INFINITY;
+        // ---- the reference maximum: the part's first token's score, a new one only when a score has outgrown it
+        if (i == 0) {
+          if (my == 0) {
 #pragma unroll
-          for (int j = 0; j < 16; j += 4) {
-            const float4 m = *reinterpret_cast<const float4*>(s_a + col0 + j);
-            const float y[4] = {fmaf(x[j], a.scale_log2, -m.x), fmaf(x[j + 1], a.scale_log2, -m.y), fmaf(x[j + 2], a.scale_log2, -m.z), fmaf(x[j + 3], a.scale_log2, -m.w)};
-            if (edge) {
-              const int4 lim = *reinterpret_cast<const int4*>(s_lim + col0 + j);
-              up = fmaxf(up, fmaxf(fmaxf(pos <= lim.x ? y[0] : -INFINITY, pos <= lim.y ? y[1] : -INFINITY), fmaxf(pos <= lim.z ? y[2] : -INFINITY, pos <= lim.w ? y[3] : -INFINITY)));
-            } else {
-              up = fmaxf(up, fmaxf(fmaxf(y[0], y[1]), fmaxf(y[2], y[3])));
+            for (int j = 0; j < 16; ++j) {
+              const float s = x[j] * a.scale_log2;
+              s_a[col0 + j] = s_lim[col0 + j] < pos || s == -INFINITY ? 0.f : s;
             }
           }
-          uint32_t any;
-          asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.or.pred p, %2, 128, q;\n selp.u32 %0, 1, 0, p;\n}\n"
-                       : "=r"(any) : "r"(up > MAX_UP ? 1u : 0u), "r"(3 + group) : "memory");
-          retake = any != 0;
+          group_sync();
         }
+        float up = -INFINITY;
+#pragma unroll
+        for (int j = 0; j < 16; j += 4) {   // x becomes s - m
+          const float4 m = *reinterpret_cast<const float4*>(s_a + col0 + j);
+          p_fma2(x[j], x[j + 1], a.scale_log2, -m.x, -m.y);
+          p_fma2(x[j + 2], x[j + 3], a.scale_log2, -m.z, -m.w);
+          if (edge) {
+            const int4 lim = *reinterpret_cast<const int4*>(s_lim + col0 + j);
+            x[j] = pos <= lim.x ? x[j] : -INFINITY;
+            x[j + 1] = pos <= lim.y ? x[j + 1] : -INFINITY;
+            x[j + 2] = pos <= lim.z ? x[j + 2] : -INFINITY;
+            x[j + 3] = pos <= lim.w ? x[j + 3] : -INFINITY;
+          }
+          up = fmaxf(up, fmaxf(fmaxf(x[j], x[j + 1]), fmaxf(x[j + 2], x[j + 3])));
+        }
+        uint32_t retake;
+        asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.or.pred p, %2, 128, q;\n selp.u32 %0, 1, 0, p;\n}\n"
+                     : "=r"(retake) : "r"(up > MAX_UP ? 1u : 0u), "r"(3 + group) : "memory");
         if (retake) {
           float y[16];
 #pragma unroll
-          for (int j = 0; j < 16; ++j) y[j] = pos <= s_lim[col0 + j] ? x[j] * a.scale_log2 : -INFINITY;
+          for (int j = 0; j < 16; ++j) y[j] = x[j];
           const float top = fold16<OpMax>(y, lane);
           s_red[quarter * NR + col0 + (lane >> 1)] = top;
-          if (i > 0) collect();
+          collect();
           group_sync();
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {
+          for (int j = 0; j < 16; ++j) {   // what the maximum rises by, if anything
             const int cc = col0 + j;
-            const float t = fmaxf(fmaxf(s_red[cc], s_red[NR + cc]), fmaxf(s_red[2 * NR + cc], s_red[3 * NR + cc]));
-            if (i == 0) {
-              y[j] = t == -INFINITY ? 0.f : t;                // a row that sees nothing here sees nothing in this part
-            } else {
-              y[j] = fmaxf(s_a[cc], t);
-              const float al = p_ex2(s_a[cc] - y[j]);
-              l[j] *= al;
-              o[j] *= al;
-            }
+            y[j] = fmaxf(fmaxf(fmaxf(s_red[cc], s_red[NR + cc]), fmaxf(s_red[2 * NR + cc], s_red[3 * NR + cc])), 0.f);
+            const float al = p_ex2(-y[j]);
+            l[j] *= al;
+            o[j] *= al;
+            x[j] -= y[j];
           }
-          group_sync();   // everyone has read s_red and the old maxima
           if (my == 0) {
 #pragma unroll
-            for (int j = 0; j < 16; ++j) s_a[col0 + j] = y[j];
+            for (int j = 0; j < 16; ++j) s_a[col0 + j] += y[j];
           }
-          group_sync();
+          group_sync();   // s_red may be written again, s_a read
         }
         // ---- weights
 #pragma unroll
-        for (int j = 0; j < 16; j += 4) {
-          const float4 m = *reinterpret_cast<const float4*>(s_a + col0 + j);
-          x[j] = p_ex2(fmaf(x[j], a.scale_log2, -m.x));
-          x[j + 1] = p_ex2(fmaf(x[j + 1], a.scale_log2, -m.y));
-          x[j + 2] = p_ex2(fmaf(x[j + 2], a.scale_log2, -m.z));
-          x[j + 3] = p_ex2(fmaf(x[j + 3], a.scale_log2, -m.w));
-          if (edge) {
-            const int4 lim = *reinterpret_cast<const int4*>(s_lim + col0 + j);
-            x[j] = pos <= lim.x ? x[j] : 0.f;
-            x[j + 1] = pos <= lim.y ? x[j + 1] : 0.f;
-            x[j + 2] = pos <= lim.z ? x[j + 2] : 0.f;
-            x[j + 3] = pos <= lim.w ? x[j + 3] : 0.f;
-          }
-        }
+        for (int j = 0; j < 16; ++j) x[j] = p_ex2(x[j]);
         if (PARTS == 3) {
 #pragma unroll
-          for (int j = 0; j < 16; ++j) l[j] += x[j];
+          for (int j = 0; j < 16; j += 2) p_add2(l[j], l[j + 1], x[j], x[j + 1]);
         }
         // P^T is written once the previous output product has read it
         if (i > 0) collect();
@@ -561,8 +592,8 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
             for (int j = 0; j < 4; ++j) {
               float &f0 = x[8 * k + 2 * j], &f1 = x[8 * k + 2 * j + 1];
               u[j] = p_pack(f0, f1);
-              if (PARTS == 1) { l[8 * k + 2 * j] += p_lo(u[j]); l[8 * k + 2 * j + 1] += p_hi(u[j]); }
-              if (part + 1 < PARTS) { f0 -= p_lo(u[j]); f1 -= p_hi(u[j]); }
+              if (PARTS == 1) p_add2(l[8 * k + 2 * j], l[8 * k + 2 * j + 1], p_lo(u[j]), p_hi(u[j]));
+              if (part + 1 < PARTS) p_add2(f0, f1, -p_lo(u[j]), -p_hi(u[j]));
             }
             *reinterpret_cast<uint4*>(pr + part * C::GROUPS * C::P_BLOCK + ((k ^ sw) << 4)) = make_uint4(u[0], u[1], u[2], u[3]);
           }
@@ -592,8 +623,8 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
         s_b[st] = t;
         if (parts == 1) {
           if (a.lse && r0 + st < R) {
-            const int rr = r0 + st;
-            a.lse[(size_t)(c.row0 + rr / a.G) * a.H + c.hk * a.G + rr % a.G] = t == 0.f ? -INFINITY : 0.6931471805599453f * (s_a[st] + log2f(t));
+            const int rr = r0 + st, tok = row_token(a, rr);
+            a.lse[(size_t)(c.row0 + tok) * a.H + c.hk * a.G + rr - tok * a.G] = t == 0.f ? -INFINITY : 0.6931471805599453f * (s_a[st] + log2f(t));
           }
           s_b[st] = t == 0.f ? 0.f : 1.f / t;
         }
@@ -602,25 +633,25 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
       const int e = D == 128 ? my : quarter * 16 + lane;      // element of the head (d = 64: 16 rows in each quarter's first 16 lanes)
       const bool live_lane = D == 128 || lane < 16;
       float* slot = a.slots + slot_floats<NR, D>() * (size_t)part_slot(blockIdx.x, c.k0 == 0);
-      if (live_lane) {
+      const int rows = min(max(R - r0 - col0, 0), live_lane ? 16 : 0);
+      if (parts == 1) {
+        long long at[16];
+        float f[16];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) {
-          const int r = col0 + j;
-          const long long at = s_off[r];
-          if (at < 0) continue;
-          if (parts == 1) {
-            const float t = s_b[r];
-            store_out(a, at + e, t == 0.f ? 0.f : o[j] * t);
-          } else {
-            __stcg(slot + 2 * NR + r * D + e, o[j]);
-          }
-        }
+        for (int j = 0; j < 16; ++j) { at[j] = s_off[col0 + j] + e; f[j] = s_b[col0 + j]; }
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          if (j < rows) store_out(a, at[j], f[j] == 0.f ? 0.f : o[j] * f[j]);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 16; ++j)
+          if (j < rows) __stcg(slot + 2 * NR + (col0 + j) * D + e, o[j]);
       }
       if (parts > 1) {
         if (st < NR) { __stcg(slot + st, s_a[st]); __stcg(slot + NR + st, s_b[st]); }
-        __threadfence();
         all_sync();
         if (st == 0) {
+          __threadfence();   // the CTA's parts are out before its arrival is
           *s_last = atomicAdd(a.counters + first, 1) == parts - 1;
           if (*s_last) { a.counters[first] = 0; __threadfence(); }
         }
