@@ -11,14 +11,15 @@
 //
 // Bound by HBM: every element is read once and written once, 6 operations per pair.  The angles would not be cheap per
 // element -- a 64-bit product and reduction and a sine and cosine each --, so a CTA works them out once per row, shares
-// them through shared memory, and rotates many heads of that row by them.  A unit is 16 bytes of x (both 16-byte halves
-// of a pair in the halves layout); consecutive threads take consecutive units, UPT of them per thread in flight.
+// them through shared memory, and rotates many heads of that row by them.  A unit is 16 bytes of x (two of them, both
+// halves of its pairs, in the halves layout); consecutive threads take consecutive units, 64 bytes per thread.  The units
+// are on their way before positions, page table and angles are looked at: the two latencies overlap.
 // E = elements per access: 16 bytes of x when addresses, strides and the rotated part allow, else single elements.
 // ------------------------------------------------------------------------------------------------------------------
 namespace {
 
 constexpr int ROT_THREADS = 256;
-constexpr int ROT_UPT = 4;        // units per thread and turn
+constexpr int ROT_PASSES = 4;
 constexpr int ROT_MAX_ROWS = 32;  // rows a CTA may share (small rows)
 
 template <typename T> struct Elem;
@@ -32,11 +33,7 @@ template <> struct Elem<__nv_bfloat16> {
 };
 
 template <typename T, int E> struct alignas(sizeof(T) * E) Pack { T v[E]; };
-template <typename T, int E> __device__ __forceinline__ void load_e(const T* p, float (&f)[E]) {
-  const Pack<T, E> k = *reinterpret_cast<const Pack<T, E>*>(p);
-#pragma unroll
-  for (int i = 0; i < E; ++i) f[i] = Elem<T>::get(k.v[i]);
-}
+template <typename T, int E> __device__ __forceinline__ Pack<T, E> load_e(const T* p) { return *reinterpret_cast<const Pack<T, E>*>(p); }
 template <typename T, int E> __device__ __forceinline__ void store_e(T* p, const float (&f)[E]) {
   Pack<T, E> k;
 #pragma unroll
@@ -57,23 +54,17 @@ __device__ __forceinline__ float2 turn(double p, double f) {
   return make_float2(fmaf(-d, s, c), fmaf(d, c, s));
 }
 
-// E: elements per access.  In the pairs layout a unit of E >= 2 holds E / 2 pairs; single-element access (E = 1) takes
-// the two elements of one pair as a unit.
-template <typename TX, typename TQ, typename TC, int E, bool HALVES>
-__global__ void __launch_bounds__(ROT_THREADS) rotary_kernel(const __grid_constant__ RotaryArgs a) {
-  extern __shared__ float2 s_turn[];                 // [rows_per_cta][rot / 2]
-  __shared__ int s_pos[ROT_MAX_ROWS];
-  __shared__ long long s_slot[ROT_MAX_ROWS];         // element offset of the row's slot in the cache, -1: skip the row
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  const int row0 = blockIdx.x * a.rows_per_cta, nr = min(a.rows_per_cta, a.rows - row0);
-  pdl_launch_dependents();
-  pdl_wait();
-  for (int i = warp; i < nr; i += ROT_THREADS / 32) {
+__device__ __forceinline__ int magic_div(int n, uint32_t magic) { return magic ? (int)__umulhi((uint32_t)n, magic) : n; }   // magic 0: by 1
+
+// positions and cache slots (element offsets; -1: the row is skipped) of the CTA's rows, a row per warp
+__device__ __forceinline__ void row_places(const RotaryArgs& a, int row0, int nr, int* s_pos, long long* s_slot) {
+  const int lane = threadIdx.x & 31;
+  if (a.positions) {
+    for (int i = threadIdx.x; i < nr; i += ROT_THREADS) { s_pos[i] = a.positions[row0 + i]; s_slot[i] = 0; }
+    return;
+  }
+  for (int i = threadIdx.x >> 5; i < nr; i += ROT_THREADS / 32) {
     const int row = row0 + i;
-    if (a.positions) {
-      if (lane == 0) { s_pos[i] = a.positions[row]; s_slot[i] = 0; }
-      continue;
-    }
     // the sequence: as many as end at or before this row precede it
     int before = 0;
     for (int b0 = 0; b0 < a.s.B; b0 += 32) {
@@ -95,131 +86,153 @@ __global__ void __launch_bounds__(ROT_THREADS) rotary_kernel(const __grid_consta
       s_pos[i] = (int)pos;
     }
   }
-  __syncthreads();
+}
+
+__device__ __forceinline__ void row_turns(const RotaryArgs& a, int nr, const int* s_pos, float2* s_turn) {
   const int hr = a.rot >> 1;
-  if (a.freq) {
-    for (int i = tid; i < nr * hr; i += ROT_THREADS) {
-      const int r = i / hr, k = i - r * hr;
-      float2 t = turn((double)s_pos[r], a.freq[k]);
-      t.x *= a.gain;
-      t.y *= a.transposed ? -a.gain : a.gain;
-      s_turn[i] = t;
-    }
+  for (int i = threadIdx.x; i < nr * hr; i += ROT_THREADS) {
+    const int r = i / hr, k = i - r * hr;
+    float2 t = turn((double)s_pos[r], a.freq[k]);
+    t.x *= a.gain;
+    t.y *= a.transposed ? -a.gain : a.gain;
+    s_turn[i] = t;
   }
-  __syncthreads();
-  constexpr int EU = (!HALVES && E == 1) ? 2 : E;    // elements of a unit's first access(es) that lie side by side
-  const int rot_units = a.freq ? (HALVES ? hr / EU : a.rot / EU) : 0;   // of a head: units that are rotated
+}
+
+// A unit's first access is at element e0 of its head, in the halves layout the second rot / 2 further (when it is rotated);
+// in the pairs layout single-element access (E = 1) takes both elements of a pair.  UPT: units per thread.
+template <typename TX, typename TQ, typename TC, int E, bool HALVES, int UPT>
+__global__ void __launch_bounds__(ROT_THREADS) rotary_kernel(const __grid_constant__ RotaryArgs a) {
+  extern __shared__ float2 s_turn[];                 // [rows_per_cta][rot / 2]
+  __shared__ int s_pos[ROT_MAX_ROWS];
+  __shared__ long long s_slot[ROT_MAX_ROWS];
+  constexpr int EU = (!HALVES && E == 1) ? 2 : E;    // elements a unit holds side by side
+  const int tid = threadIdx.x, hr = a.rot >> 1;
+  const int rot_units = a.freq ? (HALVES ? hr : a.rot) / EU : 0;       // of a head: units that are rotated
   const int n_rot = (a.heads[0] + a.heads[1]) * a.uh_rot;              // units of a row: queries and keys, then values
-  const int u0 = blockIdx.y * a.units_per_cta, u1 = min(u0 + a.units_per_cta, a.units);
-  const int span = u1 - u0, all = nr * span;
-  for (int base = tid; base < all; base += ROT_THREADS * ROT_UPT) {
-    float lo[ROT_UPT][EU], hi[ROT_UPT][HALVES ? E : 1];
-    int where[ROT_UPT];       // unit of the head, -1: nothing to do
-    int kind[ROT_UPT], head[ROT_UPT], rr[ROT_UPT];
+  const int row0 = blockIdx.x * a.rows_per_cta, nr = min(a.rows_per_cta, a.rows - row0);
+  const int u0 = blockIdx.y * a.units_per_cta, span = min(a.units_per_cta, a.units - u0), all = nr * span;
+  pdl_launch_dependents();
+  pdl_wait();
+  for (int base = 0; base < all; base += ROT_THREADS * UPT) {
+    int e0[UPT], kind[UPT], head[UPT], rr[UPT];      // kind: 0 queries, 1 keys, 2 values, -1 nothing; + 4 when rotated
+    Pack<TX, E> lo[UPT], hi[UPT];                    // hi: the second half of the pairs (of the pair, for E = 1)
 #pragma unroll
-    for (int j = 0; j < ROT_UPT; ++j) {
-      const int i = base + j * ROT_THREADS;
-      where[j] = -1;
+    for (int j = 0; j < UPT; ++j) {
+      const int i = base + tid + j * ROT_THREADS;
+      kind[j] = -1;
       if (i >= all) continue;
-      const int r = i / span;
-      int u = u0 + i - r * span;
-      if (s_slot[r] < 0) continue;
-      rr[j] = r;
+      rr[j] = a.rows_per_cta == 1 ? 0 : magic_div(i, a.span_magic);    // several rows: span is units, in every CTA
+      int u = u0 + i - rr[j] * span, h, w;
       if (u < n_rot) {
-        head[j] = u / a.uh_rot;
-        where[j] = u - head[j] * a.uh_rot;
-        kind[j] = head[j] >= a.heads[0] ? 1 : 0;
-        if (kind[j]) head[j] -= a.heads[0];
+        h = magic_div(u, a.uh_rot_magic);
+        w = u - h * a.uh_rot;
+        kind[j] = h >= a.heads[0] ? 1 : 0;
+        if (kind[j]) h -= a.heads[0];
+        if (w < rot_units) kind[j] += 4;
+        e0[j] = HALVES && a.freq && w >= rot_units ? a.rot + (w - rot_units) * E : w * EU;
       } else {
         u -= n_rot;
-        head[j] = u / a.uh_flat;
-        where[j] = u - head[j] * a.uh_flat;
+        h = magic_div(u, a.uh_flat_magic);
+        e0[j] = (u - h * a.uh_flat) * EU;
         kind[j] = 2;
       }
-      const RowsView& x = a.x[kind[j]];
-      const TX* src = reinterpret_cast<const TX*>(x.p) + (long long)(row0 + r) * x.row + (long long)head[j] * x.head;
-      const bool turned = kind[j] < 2 && where[j] < rot_units;
-      if constexpr (HALVES) {
-        // rotated units: elements where E .. and rot / 2 further; the rest: one access of E elements behind the rotated part
-        const int e = turned || kind[j] == 2 || !a.freq ? where[j] * E : a.rot + (where[j] - rot_units) * E;
-        load_e<TX, E>(src + e, lo[j]);
-        if (turned) load_e<TX, E>(src + e + hr, hi[j]);
-      } else if constexpr (E == 1) {
-        float t[1];
-        load_e<TX, 1>(src + 2 * where[j], t);
-        lo[j][0] = t[0];
-        load_e<TX, 1>(src + 2 * where[j] + 1, t);
-        lo[j][EU - 1] = t[0];
-      } else {
-        load_e<TX, E>(src + where[j] * E, lo[j]);
+      head[j] = h;
+      const RowsView& x = a.x[kind[j] & 3];
+      const TX* src = reinterpret_cast<const TX*>(x.p) + (long long)(row0 + rr[j]) * x.row + (long long)h * x.head + e0[j];
+      lo[j] = load_e<TX, E>(src);
+      if constexpr (HALVES) { if (kind[j] >= 4) hi[j] = load_e<TX, E>(src + hr); }
+      if constexpr (!HALVES && E == 1) hi[j] = load_e<TX, E>(src + 1);
+    }
+    if (base == 0) {
+      row_places(a, row0, nr, s_pos, s_slot);
+      __syncthreads();
+      if (a.freq) {
+        row_turns(a, nr, s_pos, s_turn);
+        __syncthreads();
       }
     }
 #pragma unroll
-    for (int j = 0; j < ROT_UPT; ++j) {
-      if (where[j] < 0) continue;
-      const bool turned = kind[j] < 2 && where[j] < rot_units;
-      const float2* tr = s_turn + rr[j] * hr;
-      int e0;   // first element of the (first) store
-      if constexpr (HALVES) {
-        e0 = turned || kind[j] == 2 || !a.freq ? where[j] * E : a.rot + (where[j] - rot_units) * E;
-        if (turned) {
+    for (int j = 0; j < UPT; ++j) {
+      if (kind[j] < 0) continue;
+      const long long slot = s_slot[rr[j]];
+      if (slot < 0) continue;
+      float f[EU], g[E];
+#pragma unroll
+      for (int q = 0; q < E; ++q) f[q] = Elem<TX>::get(lo[j].v[q]);
+      if constexpr (!HALVES && E == 1) f[EU - 1] = Elem<TX>::get(hi[j].v[0]);
+      if (kind[j] >= 4) {
+        const float2* tr = s_turn + rr[j] * hr + (HALVES ? e0[j] : e0[j] >> 1);
+        if constexpr (HALVES) {
 #pragma unroll
           for (int q = 0; q < E; ++q) {
-            const float2 t = tr[e0 + q];
-            const float p = lo[j][q], s = hi[j][q];
-            lo[j][q] = p * t.x - s * t.y;
-            hi[j][q] = p * t.y + s * t.x;
+            const float2 t = tr[q];
+            const float p = f[q], s = Elem<TX>::get(hi[j].v[q]);
+            f[q] = p * t.x - s * t.y;
+            g[q] = p * t.y + s * t.x;
           }
-        }
-      } else {
-        e0 = where[j] * EU;
-        if (turned) {
+        } else {
 #pragma unroll
           for (int q = 0; q < EU; q += 2) {
-            const float2 t = tr[(e0 + q) >> 1];
-            const float p = lo[j][q], s = lo[j][q + 1];
-            lo[j][q] = p * t.x - s * t.y;
-            lo[j][q + 1] = p * t.y + s * t.x;
+            const float2 t = tr[q >> 1];
+            const float p = f[q], s = f[q + 1];
+            f[q] = p * t.x - s * t.y;
+            f[q + 1] = p * t.y + s * t.x;
           }
         }
       }
       auto put = [&](auto* dst) {
         using T = typename std::remove_reference<decltype(*dst)>::type;
+        dst += e0[j];
         if constexpr (!HALVES && E == 1) {
-          dst[e0] = Elem<T>::put(lo[j][0]);
-          dst[e0 + 1] = Elem<T>::put(lo[j][EU - 1]);
+          dst[0] = Elem<T>::put(f[0]);
+          dst[1] = Elem<T>::put(f[EU - 1]);
         } else {
-          store_e<T, E>(dst + e0, lo[j]);
-          if constexpr (HALVES) { if (turned) store_e<T, E>(dst + e0 + hr, hi[j]); }
+          store_e<T, E>(dst, f);
+          if constexpr (HALVES) { if (kind[j] >= 4) store_e<T, E>(dst + hr, g); }
         }
       };
-      if (kind[j] == 0) put(reinterpret_cast<TQ*>(a.y[0].p) + (long long)(row0 + rr[j]) * a.y[0].row + (long long)head[j] * a.y[0].head);
-      else put(reinterpret_cast<TC*>(a.y[kind[j]].p) + s_slot[rr[j]] + (long long)head[j] * a.y[kind[j]].head);
+      const int what = kind[j] & 3;
+      if (what == 0) put(reinterpret_cast<TQ*>(a.y[0].p) + (long long)(row0 + rr[j]) * a.y[0].row + (long long)head[j] * a.y[0].head);
+      else put(reinterpret_cast<TC*>(a.y[what].p) + slot + (long long)head[j] * a.y[what].head);
     }
   }
 }
 
+// ceil(2^32 / d): n / d is the high word of a product for n d < 2^32 (units of a row times units of a head are below that)
+uint32_t magic_of(int d) { return d > 1 ? (uint32_t)(((1ull << 32) + (unsigned)d - 1) / (unsigned)d) : 0; }
+
+template <typename TX, typename TQ, typename TC, int E, bool HALVES, int UPT>
+cudaError_t rotary_cut(RotaryArgs& a, int num_sm, cudaStream_t st) {
+  const int hr = a.rot / 2;
+  // passes per CTA: as many as leave every SM 8 CTAs, up to ROT_PASSES
+  long long passes = (long long)a.rows * a.units / ((long long)num_sm * 8 * ROT_THREADS * UPT);
+  passes = passes < 1 ? 1 : (passes > ROT_PASSES ? ROT_PASSES : passes);
+  const int want = ROT_THREADS * UPT * (int)passes;
+  a.units_per_cta = a.units < want ? a.units : want;
+  int rpc = want / a.units_per_cta;
+  const int fit = hr > 0 ? 2048 / hr : ROT_MAX_ROWS;   // rows whose angles fit 16 KB
+  if (rpc > ROT_MAX_ROWS) rpc = ROT_MAX_ROWS;
+  if (rpc > fit) rpc = fit;
+  a.rows_per_cta = rpc < 1 ? 1 : rpc;
+  a.span_magic = magic_of(a.units_per_cta);
+  const size_t smem = sizeof(float2) * (size_t)a.rows_per_cta * (hr > 0 ? hr : 1);
+  const dim3 grid((a.rows + a.rows_per_cta - 1) / a.rows_per_cta, (a.units + a.units_per_cta - 1) / a.units_per_cta);
+  return launch_k(rotary_kernel<TX, TQ, TC, E, HALVES, UPT>, grid, dim3(ROT_THREADS), smem, st, a);
+}
+
 template <typename TX, typename TQ, typename TC, int E, bool HALVES>
 cudaError_t rotary_go(RotaryArgs& a, int num_sm, cudaStream_t st) {
-  constexpr int EU = (!HALVES && E == 1) ? 2 : E;
+  constexpr int EU = (!HALVES && E == 1) ? 2 : E, UPT = HALVES ? 2 : 4;
   const int hr = a.rot / 2;
   a.uh_flat = a.d_head / EU;
   a.uh_rot = HALVES && a.freq ? hr / EU + (a.d_head - a.rot) / EU : a.uh_flat;
   a.units = (a.heads[0] + a.heads[1]) * a.uh_rot + a.heads[2] * a.uh_flat;
-  // A CTA takes up to ROT_UPT units per thread.  Few rows (a decode step) are spread thinner, one unit per thread, so that
-  // more SMs share the latency; short rows share a CTA.
-  int upt = ROT_UPT;
-  while (upt > 1 && (long long)a.rows * a.units < (long long)num_sm * ROT_THREADS * upt) upt >>= 1;
-  const int want = ROT_THREADS * upt;
-  a.units_per_cta = a.units < want ? a.units : want;
-  int rpc = want / a.units_per_cta;
-  const int smem_rows = hr > 0 ? 4096 / hr : ROT_MAX_ROWS;
-  if (rpc > ROT_MAX_ROWS) rpc = ROT_MAX_ROWS;
-  if (rpc > smem_rows) rpc = smem_rows;
-  a.rows_per_cta = rpc < 1 ? 1 : rpc;
-  const size_t smem = sizeof(float2) * (size_t)a.rows_per_cta * (hr > 0 ? hr : 1);
-  const dim3 grid((a.rows + a.rows_per_cta - 1) / a.rows_per_cta, (a.units + a.units_per_cta - 1) / a.units_per_cta);
-  return launch_k(rotary_kernel<TX, TQ, TC, E, HALVES>, grid, dim3(ROT_THREADS), smem, st, a);
+  a.uh_rot_magic = magic_of(a.uh_rot);
+  a.uh_flat_magic = magic_of(a.uh_flat);
+  // few rows (a decode step) are spread thinner, one unit per thread, so that more SMs share the latency
+  if ((long long)a.rows * a.units < (long long)num_sm * ROT_THREADS * UPT) return rotary_cut<TX, TQ, TC, E, HALVES, 1>(a, num_sm, st);
+  return rotary_cut<TX, TQ, TC, E, HALVES, UPT>(a, num_sm, st);
 }
 
 bool aligned(const RowsView& v, int heads, int bytes, int esize) {
@@ -273,7 +286,7 @@ RowsView view(const sps_rows* r) { return RowsView{r->p, (long long)r->row_strid
 const char* bad_rows(const sps_rows* r, int rows) {
   if (!r) return "null rows";
   if (r->dtype != 0 && r->dtype != 1) return "rows: dtype must be 0 (fp32) or 1 (bf16)";
-  if (r->heads < 1 || r->heads > 65536) return "rows: heads out of range";
+  if (r->heads < 1 || r->heads > 4096) return "rows: heads out of range";
   if (r->row_stride < 0 || r->head_stride < 0) return "rows: negative stride";
   if (rows > 0 && !r->p) return "rows: null pointer";
   if ((uintptr_t)r->p & (r->dtype == 0 ? 3 : 1)) return "rows: pointer not aligned to its elements";
@@ -292,7 +305,7 @@ const char* bad_cache(const sps_paged_cache* c) {
   if (c->dtype != 0 && c->dtype != 1) return "cache: dtype must be 0 (fp32) or 1 (bf16)";
   if (c->d_head != 64 && c->d_head != 128) return "cache: d_head must be 64 or 128";
   if (c->page_size < 8 || c->page_size > 512 || (c->page_size & (c->page_size - 1))) return "cache: page_size must be a power of two, 8 .. 512";
-  if (c->n_pages < 1 || c->n_kv_heads < 1 || c->n_kv_heads > 65536) return "cache: n_pages or n_kv_heads out of range";
+  if (c->n_pages < 1 || c->n_kv_heads < 1 || c->n_kv_heads > 4096) return "cache: n_pages or n_kv_heads out of range";
   if (!c->k || !c->v) return "cache: null pointer";
   const int64_t m = c->dtype == 0 ? 4 : 8;
   if ((((uintptr_t)c->k | (uintptr_t)c->v) & 15) || c->page_stride % m || c->head_stride % m || c->pos_stride % m)
@@ -400,7 +413,7 @@ int sps_paged_append(const sps_paged_cache* cache, const sps_paged_batch* batch,
 }
 
 static const char* bad_heads(const sps_paged_cache* c, int n_heads, int q_dtype) {
-  if (n_heads < 1 || n_heads > 65536 || n_heads % c->n_kv_heads) return "heads of q must be a multiple of the cache's";
+  if (n_heads < 1 || n_heads > 4096 || n_heads % c->n_kv_heads) return "heads of q must be a multiple of the cache's";
   if (q_dtype != 0 && q_dtype != 1) return "q: dtype must be 0 (fp32) or 1 (bf16)";
   if (q_dtype == 1 && c->dtype == 0) return "an fp32 cache takes fp32 queries";
   return nullptr;

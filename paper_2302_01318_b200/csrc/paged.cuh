@@ -325,7 +325,10 @@ struct RotaryArgs {
   const int32_t* positions;    // sps_rotary; null: from the batch
   PagedSeqs s;
   long long pos_stride;        // cache slots
-  int rows, rows_per_cta, units, units_per_cta, uh_rot, uh_flat;   // set by the launcher
+  int rows;
+  // set by the launcher: units of a row, of a rotated head and of a plain one, a CTA's rows and units of each; reciprocals
+  int units, uh_rot, uh_flat, rows_per_cta, units_per_cta;
+  uint32_t span_magic, uh_rot_magic, uh_flat_magic;
 };
 cudaError_t rotary_launch(RotaryArgs a, int x_bf16, int yq_bf16, int cache_bf16, int num_sm, cudaStream_t st);
 // CTAs of an attention launch on a device of num_sm SMs, at most (counters and slots are laid out for as many)
