@@ -11,15 +11,17 @@
 //
 // Bound by HBM: every element is read once and written once, 6 operations per pair.  The angles would not be cheap per
 // element -- a 64-bit product and reduction and a sine and cosine each --, so a CTA works them out once per row, shares
-// them through shared memory, and rotates many heads of that row by them.  A unit is 16 bytes of x (two of them, both
-// halves of its pairs, in the halves layout); consecutive threads take consecutive units, 64 bytes per thread.  The units
-// are on their way before positions, page table and angles are looked at: the two latencies overlap.
+// them through shared memory, and rotates many heads of that row by them.  A unit is 16 bytes of x, two of them in the
+// halves layout (both halves of its pairs; two 16-byte pieces where nothing is rotated); a thread keeps its place in the
+// head and goes from head to head, 64 bytes of loads in flight, through queries, keys and values and the rows of its CTA.
+// The first units are on their way before positions, page table and angles are looked at; what is left of that latency
+// hides behind the SM's other CTAs.
 // E = elements per access: 16 bytes of x when addresses, strides and the rotated part allow, else single elements.
 // ------------------------------------------------------------------------------------------------------------------
 namespace {
 
 constexpr int ROT_THREADS = 256;
-constexpr int ROT_PASSES = 4;
+constexpr int ROT_PASSES = 4;     // batches of loads per thread, at most
 constexpr int ROT_MAX_ROWS = 32;  // rows a CTA may share (small rows)
 
 template <typename T> struct Elem;
@@ -54,8 +56,6 @@ __device__ __forceinline__ float2 turn(double p, double f) {
   return make_float2(fmaf(-d, s, c), fmaf(d, c, s));
 }
 
-__device__ __forceinline__ int magic_div(int n, uint32_t magic) { return magic ? (int)__umulhi((uint32_t)n, magic) : n; }   // magic 0: by 1
-
 // positions and cache slots (element offsets; -1: the row is skipped) of the CTA's rows, a row per warp
 __device__ __forceinline__ void row_places(const RotaryArgs& a, int row0, int nr, int* s_pos, long long* s_slot) {
   const int lane = threadIdx.x & 31;
@@ -88,150 +88,155 @@ __device__ __forceinline__ void row_places(const RotaryArgs& a, int row0, int nr
   }
 }
 
+// the turns of the CTA's rows; pair k of a row at (k % PU) units + k / PU, PU pairs to a unit: neighbouring units read
+// neighbouring words
+template <int PU>
 __device__ __forceinline__ void row_turns(const RotaryArgs& a, int nr, const int* s_pos, float2* s_turn) {
-  const int hr = a.rot >> 1;
+  const int hr = a.rot >> 1, units = hr / PU;
   for (int i = threadIdx.x; i < nr * hr; i += ROT_THREADS) {
     const int r = i / hr, k = i - r * hr;
     float2 t = turn((double)s_pos[r], a.freq[k]);
     t.x *= a.gain;
     t.y *= a.transposed ? -a.gain : a.gain;
-    s_turn[i] = t;
+    s_turn[r * hr + (k % PU) * units + k / PU] = t;
   }
 }
 
-// A unit's first access is at element e0 of its head, in the halves layout the second rot / 2 further (when it is rotated);
-// in the pairs layout single-element access (E = 1) takes both elements of a pair.  UPT: units per thread.
+__device__ __forceinline__ int magic_div(int n, uint32_t magic) { return magic ? (int)__umulhi((uint32_t)n, magic) : n; }   // magic 0: by 1
+
+// UPT: units per thread and batch.  Single-element access (E = 1) takes the two elements of a pair as a unit.
 template <typename TX, typename TQ, typename TC, int E, bool HALVES, int UPT>
-__global__ void __launch_bounds__(ROT_THREADS) rotary_kernel(const __grid_constant__ RotaryArgs a) {
+__global__ void __launch_bounds__(ROT_THREADS, 4) rotary_kernel(const __grid_constant__ RotaryArgs a) {
   extern __shared__ float2 s_turn[];                 // [rows_per_cta][rot / 2]
   __shared__ int s_pos[ROT_MAX_ROWS];
   __shared__ long long s_slot[ROT_MAX_ROWS];
-  constexpr int EU = (!HALVES && E == 1) ? 2 : E;    // elements a unit holds side by side
-  const int tid = threadIdx.x, hr = a.rot >> 1;
-  const int rot_units = a.freq ? (HALVES ? hr : a.rot) / EU : 0;       // of a head: units that are rotated
-  const int n_rot = (a.heads[0] + a.heads[1]) * a.uh_rot;              // units of a row: queries and keys, then values
+  constexpr bool TWO = HALVES || E == 1;             // two accesses to a unit
+  constexpr int PU = HALVES ? E : (E == 1 ? 1 : E / 2);   // pairs of a rotated unit
+  const int tid = threadIdx.x, hr = a.rot >> 1, uh = a.uh;
+  const int rot_units = a.freq ? hr / PU : 0;        // of a head's units: the rotated ones
   const int row0 = blockIdx.x * a.rows_per_cta, nr = min(a.rows_per_cta, a.rows - row0);
-  const int u0 = blockIdx.y * a.units_per_cta, span = min(a.units_per_cta, a.units - u0), all = nr * span;
+  const int h_lo = blockIdx.y * a.heads_per_cta, span = min(a.heads_per_cta, a.vheads - h_lo);   // this CTA's heads of each row
+  const int all = nr * span;                         // (row, head) pairs
+  const int slice = magic_div(tid, a.uh_magic);      // a thread's first pair, among the per_pass that a pass takes
+  const int active = slice < a.per_pass;
   pdl_launch_dependents();
   pdl_wait();
-  for (int base = 0; base < all; base += ROT_THREADS * UPT) {
-    int e0[UPT], kind[UPT], head[UPT], rr[UPT];      // kind: 0 queries, 1 keys, 2 values, -1 nothing; + 4 when rotated
-    Pack<TX, E> lo[UPT], hi[UPT];                    // hi: the second half of the pairs (of the pair, for E = 1)
-#pragma unroll
-    for (int j = 0; j < UPT; ++j) {
-      const int i = base + tid + j * ROT_THREADS;
-      kind[j] = -1;
-      if (i >= all) continue;
-      rr[j] = a.rows_per_cta == 1 ? 0 : magic_div(i, a.span_magic);    // several rows: span is units, in every CTA
-      int u = u0 + i - rr[j] * span, h, w;
-      if (u < n_rot) {
-        h = magic_div(u, a.uh_rot_magic);
-        w = u - h * a.uh_rot;
-        kind[j] = h >= a.heads[0] ? 1 : 0;
-        if (kind[j]) h -= a.heads[0];
-        if (w < rot_units) kind[j] += 4;
-        e0[j] = HALVES && a.freq && w >= rot_units ? a.rot + (w - rot_units) * E : w * EU;
-      } else {
-        u -= n_rot;
-        h = magic_div(u, a.uh_flat_magic);
-        e0[j] = (u - h * a.uh_flat) * EU;
-        kind[j] = 2;
-      }
-      head[j] = h;
-      const RowsView& x = a.x[kind[j] & 3];
-      const TX* src = reinterpret_cast<const TX*>(x.p) + (long long)(row0 + rr[j]) * x.row + (long long)h * x.head + e0[j];
-      lo[j] = load_e<TX, E>(src);
-      if constexpr (HALVES) { if (kind[j] >= 4) hi[j] = load_e<TX, E>(src + hr); }
-      if constexpr (!HALVES && E == 1) hi[j] = load_e<TX, E>(src + 1);
+  bool ready = false;
+  for (int w = tid - slice * uh; w < uh; w += ROT_THREADS) {   // (once, unless a head has more units than the CTA threads)
+    const bool turned = w < rot_units;
+    int e0, e1 = 0;                                  // the unit's elements
+    if (HALVES) {
+      e0 = turned ? w * E : a.flat0 + (w - rot_units) * E;
+      e1 = e0 + (turned ? hr : a.flat_half);
+    } else {
+      e0 = w * (E == 1 ? 2 : E);
+      e1 = e0 + 1;
     }
-    if (base == 0) {
-      row_places(a, row0, nr, s_pos, s_slot);
-      __syncthreads();
-      if (a.freq) {
-        row_turns(a, nr, s_pos, s_turn);
+    for (int i0 = slice; i0 - slice < all; i0 += a.per_pass * UPT) {
+      Pack<TX, E> lo[UPT], hi[UPT];
+      int rr[UPT], vh[UPT];                          // row of the CTA (-1: none) and head among queries, keys and values
+#pragma unroll
+      for (int j = 0; j < UPT; ++j) {
+        const int i = i0 + j * a.per_pass;
+        rr[j] = -1;
+        if (i >= all || !active) continue;
+        rr[j] = a.rows_per_cta == 1 ? 0 : magic_div(i, a.span_magic);   // several rows: the CTA has all of their heads
+        vh[j] = h_lo + i - rr[j] * span;
+        const int kind = vh[j] < a.heads[0] ? 0 : (vh[j] < a.heads[0] + a.heads[1] ? 1 : 2);
+        const int h = vh[j] - (kind > 0 ? a.heads[0] : 0) - (kind > 1 ? a.heads[1] : 0);
+        const RowsView& x = a.x[kind];
+        const TX* src = reinterpret_cast<const TX*>(x.p) + (long long)(row0 + rr[j]) * x.row + (long long)h * x.head;
+        lo[j] = load_e<TX, E>(src + e0);
+        if constexpr (TWO) hi[j] = load_e<TX, E>(src + e1);
+      }
+      if (!ready) {
+        ready = true;
+        row_places(a, row0, nr, s_pos, s_slot);
         __syncthreads();
-      }
-    }
-#pragma unroll
-    for (int j = 0; j < UPT; ++j) {
-      if (kind[j] < 0) continue;
-      const long long slot = s_slot[rr[j]];
-      if (slot < 0) continue;
-      float f[EU], g[E];
-#pragma unroll
-      for (int q = 0; q < E; ++q) f[q] = Elem<TX>::get(lo[j].v[q]);
-      if constexpr (!HALVES && E == 1) f[EU - 1] = Elem<TX>::get(hi[j].v[0]);
-      if (kind[j] >= 4) {
-        const float2* tr = s_turn + rr[j] * hr + (HALVES ? e0[j] : e0[j] >> 1);
-        if constexpr (HALVES) {
-#pragma unroll
-          for (int q = 0; q < E; ++q) {
-            const float2 t = tr[q];
-            const float p = f[q], s = Elem<TX>::get(hi[j].v[q]);
-            f[q] = p * t.x - s * t.y;
-            g[q] = p * t.y + s * t.x;
-          }
-        } else {
-#pragma unroll
-          for (int q = 0; q < EU; q += 2) {
-            const float2 t = tr[q >> 1];
-            const float p = f[q], s = f[q + 1];
-            f[q] = p * t.x - s * t.y;
-            f[q + 1] = p * t.y + s * t.x;
-          }
+        if (a.freq) {
+          row_turns<PU>(a, nr, s_pos, s_turn);
+          __syncthreads();
         }
       }
-      auto put = [&](auto* dst) {
-        using T = typename std::remove_reference<decltype(*dst)>::type;
-        dst += e0[j];
-        if constexpr (!HALVES && E == 1) {
-          dst[0] = Elem<T>::put(f[0]);
-          dst[1] = Elem<T>::put(f[EU - 1]);
-        } else {
-          store_e<T, E>(dst, f);
-          if constexpr (HALVES) { if (kind[j] >= 4) store_e<T, E>(dst + hr, g); }
+#pragma unroll
+      for (int j = 0; j < UPT; ++j) {
+        if (rr[j] < 0) continue;
+        const long long slot = s_slot[rr[j]];
+        if (slot < 0) continue;
+        const int kind = vh[j] < a.heads[0] ? 0 : (vh[j] < a.heads[0] + a.heads[1] ? 1 : 2);
+        const int h = vh[j] - (kind > 0 ? a.heads[0] : 0) - (kind > 1 ? a.heads[1] : 0);
+        float f[E], g[E];
+#pragma unroll
+        for (int q = 0; q < E; ++q) f[q] = Elem<TX>::get(lo[j].v[q]);
+        if constexpr (TWO) {
+#pragma unroll
+          for (int q = 0; q < E; ++q) g[q] = Elem<TX>::get(hi[j].v[q]);
         }
-      };
-      const int what = kind[j] & 3;
-      if (what == 0) put(reinterpret_cast<TQ*>(a.y[0].p) + (long long)(row0 + rr[j]) * a.y[0].row + (long long)head[j] * a.y[0].head);
-      else put(reinterpret_cast<TC*>(a.y[what].p) + slot + (long long)head[j] * a.y[what].head);
+        if (turned && kind < 2) {
+          const float2* tr = s_turn + rr[j] * hr + w;
+          if constexpr (TWO) {
+#pragma unroll
+            for (int q = 0; q < E; ++q) {
+              const float2 t = tr[q * rot_units];
+              const float p = f[q], s = g[q];
+              f[q] = p * t.x - s * t.y;
+              g[q] = p * t.y + s * t.x;
+            }
+          } else {
+#pragma unroll
+            for (int q = 0; q < E; q += 2) {
+              const float2 t = tr[(q >> 1) * rot_units];
+              const float p = f[q], s = f[q + 1];
+              f[q] = p * t.x - s * t.y;
+              f[q + 1] = p * t.y + s * t.x;
+            }
+          }
+        }
+        auto put = [&](auto* dst) {
+          using T = typename std::remove_reference<decltype(*dst)>::type;
+          store_e<T, E>(dst + e0, f);
+          if constexpr (TWO) store_e<T, E>(dst + e1, g);
+        };
+        if (kind == 0) put(reinterpret_cast<TQ*>(a.y[0].p) + (long long)(row0 + rr[j]) * a.y[0].row + (long long)h * a.y[0].head);
+        else put(reinterpret_cast<TC*>(a.y[kind].p) + slot + (long long)h * a.y[kind].head);
+      }
     }
   }
 }
 
-// ceil(2^32 / d): n / d is the high word of a product for n d < 2^32 (units of a row times units of a head are below that)
+// ceil(2^32 / d): n / d is the high word of a product for n d < 2^32
 uint32_t magic_of(int d) { return d > 1 ? (uint32_t)(((1ull << 32) + (unsigned)d - 1) / (unsigned)d) : 0; }
 
 template <typename TX, typename TQ, typename TC, int E, bool HALVES, int UPT>
 cudaError_t rotary_cut(RotaryArgs& a, int num_sm, cudaStream_t st) {
   const int hr = a.rot / 2;
-  // passes per CTA: as many as leave every SM 8 CTAs, up to ROT_PASSES
-  long long passes = (long long)a.rows * a.units / ((long long)num_sm * 8 * ROT_THREADS * UPT);
+  // batches per thread: as many as leave every SM 8 CTAs, up to ROT_PASSES
+  long long passes = (long long)a.rows * a.vheads * a.uh / ((long long)num_sm * 8 * ROT_THREADS * UPT);
   passes = passes < 1 ? 1 : (passes > ROT_PASSES ? ROT_PASSES : passes);
-  const int want = ROT_THREADS * UPT * (int)passes;
-  a.units_per_cta = a.units < want ? a.units : want;
-  int rpc = want / a.units_per_cta;
+  const int want = a.per_pass * UPT * (int)passes;   // (row, head) pairs of a CTA
+  a.heads_per_cta = a.vheads < want ? a.vheads : want;
+  int rpc = want / a.heads_per_cta;
   const int fit = hr > 0 ? 2048 / hr : ROT_MAX_ROWS;   // rows whose angles fit 16 KB
   if (rpc > ROT_MAX_ROWS) rpc = ROT_MAX_ROWS;
   if (rpc > fit) rpc = fit;
   a.rows_per_cta = rpc < 1 ? 1 : rpc;
-  a.span_magic = magic_of(a.units_per_cta);
+  a.span_magic = magic_of(a.heads_per_cta);          // pairs of a CTA: at most 4096
   const size_t smem = sizeof(float2) * (size_t)a.rows_per_cta * (hr > 0 ? hr : 1);
-  const dim3 grid((a.rows + a.rows_per_cta - 1) / a.rows_per_cta, (a.units + a.units_per_cta - 1) / a.units_per_cta);
+  const dim3 grid((a.rows + a.rows_per_cta - 1) / a.rows_per_cta, (a.vheads + a.heads_per_cta - 1) / a.heads_per_cta);
   return launch_k(rotary_kernel<TX, TQ, TC, E, HALVES, UPT>, grid, dim3(ROT_THREADS), smem, st, a);
 }
 
 template <typename TX, typename TQ, typename TC, int E, bool HALVES>
 cudaError_t rotary_go(RotaryArgs& a, int num_sm, cudaStream_t st) {
-  constexpr int EU = (!HALVES && E == 1) ? 2 : E, UPT = HALVES ? 2 : 4;
-  const int hr = a.rot / 2;
-  a.uh_flat = a.d_head / EU;
-  a.uh_rot = HALVES && a.freq ? hr / EU + (a.d_head - a.rot) / EU : a.uh_flat;
-  a.units = (a.heads[0] + a.heads[1]) * a.uh_rot + a.heads[2] * a.uh_flat;
-  a.uh_rot_magic = magic_of(a.uh_rot);
-  a.uh_flat_magic = magic_of(a.uh_flat);
+  constexpr int UPT = HALVES ? 2 : 4;
+  a.uh = HALVES || E == 1 ? a.d_head / (2 * E) : a.d_head / E;
+  a.uh_magic = magic_of(a.uh);
+  a.flat0 = a.freq ? a.rot : 0;
+  a.flat_half = (a.d_head - a.flat0) / 2;
+  a.vheads = a.heads[0] + a.heads[1] + a.heads[2];
+  a.per_pass = a.uh < ROT_THREADS ? ROT_THREADS / a.uh : 1;
   // few rows (a decode step) are spread thinner, one unit per thread, so that more SMs share the latency
-  if ((long long)a.rows * a.units < (long long)num_sm * ROT_THREADS * UPT) return rotary_cut<TX, TQ, TC, E, HALVES, 1>(a, num_sm, st);
+  if ((long long)a.rows * a.vheads * a.uh < (long long)num_sm * ROT_THREADS * UPT) return rotary_cut<TX, TQ, TC, E, HALVES, 1>(a, num_sm, st);
   return rotary_cut<TX, TQ, TC, E, HALVES, UPT>(a, num_sm, st);
 }
 
@@ -242,8 +247,8 @@ bool aligned(const RowsView& v, int heads, int bytes, int esize) {
 template <typename TX, typename TQ, typename TC>
 cudaError_t rotary_types(RotaryArgs& a, int num_sm, cudaStream_t st) {
   constexpr int E = 16 / (int)sizeof(TX);
-  bool vec = a.d_head % E == 0;
-  if (a.freq) vec = vec && (a.halves ? (a.rot / 2) % E == 0 && (a.d_head - a.rot) % E == 0 : a.rot % E == 0);
+  const int whole = a.halves ? 2 * E : E;   // a head and its rotated part must be whole units
+  bool vec = a.d_head % whole == 0 && (!a.freq || a.rot % whole == 0);
   for (int i = 0; i < 3 && vec; ++i) {
     if (!a.heads[i]) continue;
     vec = vec && aligned(a.x[i], a.heads[i], 16, (int)sizeof(TX));

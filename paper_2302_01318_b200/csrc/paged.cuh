@@ -326,9 +326,10 @@ struct RotaryArgs {
   PagedSeqs s;
   long long pos_stride;        // cache slots
   int rows;
-  // set by the launcher: units of a row, of a rotated head and of a plain one, a CTA's rows and units of each; reciprocals
-  int units, uh_rot, uh_flat, rows_per_cta, units_per_cta;
-  uint32_t span_magic, uh_rot_magic, uh_flat_magic;
+  // set by the launcher: heads of all three, units of a head, (row, head) pairs the threads of a CTA take at once, a CTA's
+  // rows and heads of each, where a head's unrotated part starts and half its length; reciprocals for divisions
+  int vheads, uh, per_pass, rows_per_cta, heads_per_cta, flat0, flat_half;
+  uint32_t uh_magic, span_magic;
 };
 cudaError_t rotary_launch(RotaryArgs a, int x_bf16, int yq_bf16, int cache_bf16, int num_sm, cudaStream_t st);
 // CTAs of an attention launch on a device of num_sm SMs, at most (counters and slots are laid out for as many)
