@@ -7,8 +7,8 @@ import subprocess
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 LIB = os.path.join(HERE, "libsps_b200.so")
-SOURCES = ["engine.cu", "linear.cu", "linear_tc.cu", "attention.cu", "sampler.cu", "wide.cu", "tp.cu", "paged.cu", "paged_attention.cu", "paged_attention_tc.cu"]
-HEADERS = ["common.cuh", "paged.cuh", os.path.join("..", "..", "include", "sps.h")]
+SOURCES = ["engine.cu", "linear.cu", "linear_tc.cu", "attention.cu", "sampler.cu", "wide.cu", "tp.cu", "paged.cu", "paged_attention.cu", "paged_attention_tc.cu", "paged_attention_wide.cu"]
+HEADERS = ["common.cuh", "paged.cuh", "paged_tc.cuh", os.path.join("..", "..", "include", "sps.h")]
 NVCC_FLAGS = ["-gencode", "arch=compute_100a,code=sm_100a", "-O3", "-lineinfo", "-std=c++17", "-Xcompiler", "-fPIC",
               "-shared"]
 

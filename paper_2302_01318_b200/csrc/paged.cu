@@ -431,7 +431,7 @@ int64_t sps_paged_attention_workspace_bytes(const sps_paged_cache* cache, int32_
   const char* why = bad_cache(cache);
   if (!why) why = bad_heads(cache, n_heads, q_dtype);
   if (why) { no(SPS_EINVAL, why); return -1; }
-  return PAGED_COUNTER_BYTES + (int64_t)2 * paged_attn_grid(sms()) * (int64_t)paged_attn_slot_bytes(cache->dtype, cache->d_head);
+  return PAGED_COUNTER_BYTES + (int64_t)2 * paged_attn_grid(sms()) * (int64_t)paged_attn_slot_bytes(cache->dtype, q_dtype, cache->d_head);
 }
 
 int sps_paged_attention(const sps_paged_cache* cache, const sps_paged_batch* batch, int32_t rows, const sps_rows* q, const sps_rows* out,

@@ -278,39 +278,45 @@ __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCur
     }
   }
   sync();
-  float4 o[PIECES];
-#pragma unroll
-  for (int k = 0; k < PIECES; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
   const int table = w_floats / NR;                             // parts whose weights fit at once
-  for (int pb = 0; pb < parts; pb += table) {
-    const int pn = min(table, parts - pb);
-    for (int i = tid; i < pn * NR; i += THREADS) {
-      const int p = i / NR, r = i - p * NR;
-      if (r < live) w[i] = exp2f(__ldcg(slot(pb + p) + r) - w_max[r]) * w_inv[r];
-    }
-    sync();
-#pragma unroll 4
-    for (int p = 0; p < pn; ++p) {
-      const float* s = slot(pb + p) + 2 * NR;
+  constexpr int BLOCK = PIECES < 4 ? PIECES : 4;
+#pragma unroll 1
+  for (int kb = 0; kb < PIECES; kb += BLOCK) {
+    float4 o[BLOCK];
 #pragma unroll
-      for (int k = 0; k < PIECES; ++k) {
-        const int i = tid + k * THREADS;
-        if (i < live * (D / 4)) {
-          const float f = w[p * NR + i / (D / 4)];
-          const float4 v = __ldcg(reinterpret_cast<const float4*>(s) + i);
-          o[k].x += f * v.x; o[k].y += f * v.y; o[k].z += f * v.z; o[k].w += f * v.w;
+    for (int k = 0; k < BLOCK; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int pb = 0; pb < parts; pb += table) {
+      const int pn = min(table, parts - pb);
+      if (kb == 0 || parts > table) {
+        for (int i = tid; i < pn * NR; i += THREADS) {
+          const int p = i / NR, r = i - p * NR;
+          if (r < live) w[i] = exp2f(__ldcg(slot(pb + p) + r) - w_max[r]) * w_inv[r];
+        }
+        sync();
+      }
+#pragma unroll 4
+      for (int p = 0; p < pn; ++p) {
+        const float* s = slot(pb + p) + 2 * NR;
+#pragma unroll
+        for (int k = 0; k < BLOCK; ++k) {
+          const int i = tid + (kb + k) * THREADS;
+          if (i < live * (D / 4)) {
+            const float f = w[p * NR + i / (D / 4)];
+            const float4 v = __ldcg(reinterpret_cast<const float4*>(s) + i);
+            o[k].x += f * v.x; o[k].y += f * v.y; o[k].z += f * v.z; o[k].w += f * v.w;
+          }
         }
       }
+      if (parts > table) sync();   // the table may be written again
     }
-    sync();
-  }
 #pragma unroll
-  for (int k = 0; k < PIECES; ++k) {
-    const int i = tid + k * THREADS;
-    if (i < live * (D / 4)) {
-      const int r = i / (D / 4), e = (i - r * (D / 4)) * 4, rr = r0 + r, tok = row_token(a, rr);
-      const long long at = (long long)(c.row0 + tok) * a.out.row + (long long)(c.hk * a.G + rr - tok * a.G) * a.out.head + e;
-      store_out(a, at, o[k].x); store_out(a, at + 1, o[k].y); store_out(a, at + 2, o[k].z); store_out(a, at + 3, o[k].w);
+    for (int k = 0; k < BLOCK; ++k) {
+      const int i = tid + (kb + k) * THREADS;
+      if (i < live * (D / 4)) {
+        const int r = i / (D / 4), e = (i - r * (D / 4)) * 4, rr = r0 + r, tok = row_token(a, rr);
+        const long long at = (long long)(c.row0 + tok) * a.out.row + (long long)(c.hk * a.G + rr - tok * a.G) * a.out.head + e;
+        store_out(a, at, o[k].x); store_out(a, at + 1, o[k].y); store_out(a, at + 2, o[k].z); store_out(a, at + 3, o[k].w);
+      }
     }
   }
 }
@@ -334,7 +340,9 @@ struct RotaryArgs {
 cudaError_t rotary_launch(RotaryArgs a, int x_bf16, int yq_bf16, int cache_bf16, int num_sm, cudaStream_t st);
 // CTAs of an attention launch on a device of num_sm SMs, at most (counters and slots are laid out for as many)
 inline int paged_attn_grid(int num_sm) { return num_sm < 1024 ? num_sm : 1024; }
-size_t paged_attn_slot_bytes(int dtype, int d_head);
+size_t paged_attn_slot_bytes(int dtype, int q_dtype, int d_head);
 size_t paged_attn_tc_slot_bytes(int d_head);
+size_t paged_attn_wide_slot_bytes(int d_head);
+cudaError_t paged_attn_wide_launch(const PagedAttnArgs& a, int d_head, int num_sm, cudaStream_t st);
 cudaError_t paged_attn_tc_launch(const PagedAttnArgs& a, int d_head, int max_q, int num_sm, cudaStream_t st);
 cudaError_t paged_attn_launch(const PagedAttnArgs& a, int cache_bf16, int d_head, int max_q, int num_sm, cudaStream_t st);

@@ -188,8 +188,8 @@ cudaError_t simt_go(const PagedAttnArgs& a, int num_sm, cudaStream_t st) {
 
 }  // namespace
 
-size_t paged_attn_slot_bytes(int dtype, int d_head) {
-  if (dtype == 1) return paged_attn_tc_slot_bytes(d_head);
+size_t paged_attn_slot_bytes(int dtype, int q_dtype, int d_head) {
+  if (dtype == 1) return q_dtype == 1 ? paged_attn_wide_slot_bytes(d_head) : paged_attn_tc_slot_bytes(d_head);
   return sizeof(float) * (d_head == 128 ? slot_floats<SIMT_NR, 128>() : slot_floats<SIMT_NR, 64>());
 }
 
