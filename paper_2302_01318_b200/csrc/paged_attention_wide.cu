@@ -13,10 +13,6 @@
 // base 2): bf16 weights and fp32 sums keep their relative precision at any size, so this loses nothing, and O stays
 // untouched in tensor memory from tile to tile.  A warp whose rows do outgrow m rescales their O itself.
 //
-// Exponentials.  16 a clock and SM (2^x on the special function unit) would take 2048 clocks for the two tiles -- as long as
-// their four products.  So a quarter of them are worked out on the fp32 pipes: 2^x = 2^n 2^f with n the nearest
-// integer, f in [-1/2, 1/2] and a cubic for 2^f (least maximal relative error 7.5e-5, a fiftieth of a bf16 rounding).
-//
 // What bounds it: the tensor cores, 4 x 8 products of 64 clocks per pair of tiles (d = 128); they work on one tile while
 // the other one's softmax runs.
 //
@@ -59,25 +55,6 @@ __device__ __forceinline__ float w_max3(float a, float b, float c) {
   asm("max.NaN.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(a), "f"(b), "f"(c));
   return r;
 }
-// 2^x for two x on the fp32 pipes, for bf16 results (see above); x at most MAX_UP.  Below -126, and for a NaN, it gives
-// 2^-126: the caller clears what a row does not see and looks for NaN in the maximum.
-__device__ __forceinline__ void w_ex2_poly(float& x, float& y) {
-  x = fmaxf(x, -126.f);
-  y = fmaxf(y, -126.f);
-  float nx = x, ny = y;
-  p_add2(nx, ny, 12582912.f, 12582912.f);                    // 1.5 * 2^23: the sum's low bits are the nearest integer
-  const int ix = __float_as_int(nx), iy = __float_as_int(ny);
-  p_add2(nx, ny, -12582912.f, -12582912.f);
-  p_add2(x, y, -nx, -ny);                                    // f
-  float a = 0.0551716685f, b = 0.0551716685f;
-  asm("{\n .reg .b64 f, r, k;\n mov.b64 f, {%2, %3};\n mov.b64 r, {%0, %1};\n"
-      " mov.b64 k, {%4, %4};\n fma.rn.f32x2 r, r, f, k;\n mov.b64 k, {%5, %5};\n fma.rn.f32x2 r, r, f, k;\n mov.b64 k, {%6, %6};\n fma.rn.f32x2 r, r, f, k;\n"
-      " mov.b64 {%0, %1}, r;\n}\n"
-      : "+f"(a), "+f"(b) : "f"(x), "f"(y), "f"(0.242611125f), "f"(0.693260968f), "f"(0.999928057f));
-  x = __int_as_float(__float_as_int(a) + (ix << 23));
-  y = __int_as_float(__float_as_int(b) + (iy << 23));
-}
-
 template <int D>
 __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __grid_constant__ TcArgs ta) {
   using C = WCfg<D>;
@@ -86,7 +63,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
   const PagedAttnArgs& a = ta.a;
   const uint32_t ring = p_smem(wmem), q_s = ring + C::Q_AT, hb = ring + C::HDR_AT;
   unsigned char* hdr = wmem + C::HDR_AT;
-  const uint32_t full = hb, empty = hb + 64, s_full = hb + 128, p_full = hb + 144, pv_done = hb + 160, q_ready = hb + 176, q_free = hb + 184, drain = hb + 192;
+  const uint32_t full = hb, empty = hb + 64, s_full = hb + 128, p_full = hb + 144, pv_done = hb + 160, q_ready = hb + 176, q_free = hb + 184, drain = hb + 192, p_half = hb + 480;
   volatile uint32_t* s_tmem = reinterpret_cast<volatile uint32_t*>(hdr + 200);
   volatile int* s_abort = reinterpret_cast<volatile int*>(hdr + 204);
   int* s_poison = reinterpret_cast<int*>(hdr + 208);
@@ -101,7 +78,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
 
   if (tid == 0) {
     for (int i = 0; i < STAGES; ++i) { p_bar_init(full + 8 * i, 1); p_bar_init(empty + 8 * i, 1); }
-    for (int i = 0; i < 2; ++i) { p_bar_init(s_full + 8 * i, 1); p_bar_init(p_full + 8 * i, 128); p_bar_init(pv_done + 8 * i, 1); }
+    for (int i = 0; i < 2; ++i) { p_bar_init(s_full + 8 * i, 1); p_bar_init(p_full + 8 * i, 128); p_bar_init(p_half + 8 * i, 128); p_bar_init(pv_done + 8 * i, 1); }
     p_bar_init(q_ready, 128); p_bar_init(q_free, 1); p_bar_init(drain, 1);
     *s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
@@ -158,15 +135,24 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
         __syncwarp();
       };
       auto output = [&](int w, int e, bool first, bool frees_v) {    // O_w += P_w V
-        wait(p_full + 8 * w, pn[w]);
-        ++pn[w];
         wait(full + 8 * (e % STAGES), (uint32_t)(e / STAGES));
+        const uint32_t va = p_desc_lo(ring + (uint32_t)(e % STAGES) * C::HALF, TILE * 128);
+        wait(p_half + 8 * w, pn[w]);
         if (!ok) return;
         P_FENCE_AFTER();
         if (leader) {
-          const uint32_t va = p_desc_lo(ring + (uint32_t)(e % STAGES) * C::HALF, TILE * 128);
 #pragma unroll
-          for (int k = 0; k < TILE / 16; ++k)
+          for (int k = 0; k < TILE / 32; ++k)
+            w_mma_ts(tmem + 256 + w * 128, tmem + w * 128 + k * 8, va + k * (16 * 128 >> 4), p_desc_hi(1024, 2), C::IDESC_O, k > 0 || !first);
+        }
+        __syncwarp();
+        wait(p_full + 8 * w, pn[w]);
+        ++pn[w];
+        if (!ok) return;
+        P_FENCE_AFTER();
+        if (leader) {
+#pragma unroll
+          for (int k = TILE / 32; k < TILE / 16; ++k)
             w_mma_ts(tmem + 256 + w * 128, tmem + w * 128 + k * 8, va + k * (16 * 128 >> 4), p_desc_hi(1024, 2), C::IDESC_O, k > 0 || !first);
           if (frees_v) p_commit(empty + 8 * (e % STAGES));
           p_commit(pv_done + 8 * w);
@@ -305,9 +291,8 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
           P_WAIT_LD();
 #pragma unroll
           for (int j = 0; j < 128; j += 2) p_fma2(x[j], x[j + 1], a.scale_log2, -m, -m);
-          const bool edge = p0 + TILE - 1 > warp_lim || r >= R;
-          const int d = lim - p0;                               // last token of the tile this row sees
-          if (edge) {
+          if (p0 + TILE - 1 > warp_lim || r >= R) {
+            const int d = lim - p0;                             // last token of the tile this row sees
 #pragma unroll
             for (int j = 0; j < 128; ++j) x[j] = j <= d ? x[j] : -INFINITY;
           }
@@ -353,18 +338,18 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
 #pragma unroll
             for (int j = 0; j < 32; j += 2) {
               float &x0 = x[b + j], &x1 = x[b + j + 1];
-              if (j % 8 == 6) {
-                w_ex2_poly(x0, x1);
-                if (edge) { x0 = b + j <= d ? x0 : 0.f; x1 = b + j + 1 <= d ? x1 : 0.f; }
-              } else {
-                x0 = p_ex2(x0);
-                x1 = p_ex2(x1);
-              }
+              x0 = p_ex2(x0);
+              x1 = p_ex2(x1);
               if (j & 2) p_add2(l2, l3, x0, x1);
               else p_add2(l, l1, x0, x1);
               u[j >> 1] = p_pack(x0, x1);
             }
             p_st16(t_s + b / 2, u);
+            if (b == 32) {
+              P_WAIT_ST();
+              P_FENCE_BEFORE();
+              p_arrive(p_half + 8 * w);
+            }
           }
           l += l1 + (l2 + l3);
           P_WAIT_ST();
