@@ -42,9 +42,10 @@ __device__ __forceinline__ SeqGeom paged_seq(const PagedSeqs& s, int b) {
 // ------------------------------------------------------------------------------------------------------------------
 // The attention kernels' work.  A sequence's queries of one key head are nq * G rows (token-major: row r is token r / G,
 // head r % G of the group), taken NR at a time: an item is (sequence, key head, tile of NR rows), and its work is the
-// number of tiles of KT tokens its last row sees (at least one, so that empty rows get their zeros).  All items' tiles in
-// order -- sequences, key heads, row tiles -- are cut into equal runs, one per CTA: a ragged batch, one long sequence and
-// a prompt chunk are balanced alike, to one tile.  A CTA whose run begins or ends inside an item leaves that part's
+// number of tiles of KT tokens its last row sees (at least one, so that empty rows get their zeros), plus `lead` for what an
+// item costs before its first tile.  All items' work in order -- sequences, key heads, row tiles -- is cut into equal runs,
+// one per CTA: a ragged batch, one long sequence and a prompt chunk are balanced alike, to one tile.  A CTA whose run
+// begins or ends inside an item leaves that part's
 // (maximum, sum, unnormalised output) in its slot; the last CTA of the item to finish joins the parts in their order, so
 // results do not depend on timing.
 // ------------------------------------------------------------------------------------------------------------------
@@ -59,6 +60,7 @@ struct PagedAttnArgs {
   float scale_log2;         // scale * log2(e): scores are kept in base 2
   float* lse;               // [rows][H] or null
   int* counters;            // [grid] arrivals at an item, by the first CTA that works on it; zero between launches
+  int lead, min_run;        // set by the launcher: an item's cost ahead of its tiles, the least run, in tiles
   float* slots;             // [2 * grid] parts: [NR] maxima, [NR] sums, [NR][d_head] outputs
   unsigned long long wait_ns;
 };
@@ -74,60 +76,63 @@ __device__ __forceinline__ int item_tiles(const PagedAttnArgs& a, int nq, int le
   return pos < 0 ? 1 : pos / KT + 1;
 }
 
-struct WorkCursor {       // a place in the list of items, and the run of tiles that is left
+struct WorkCursor {       // a place in the list of items, and the run that is left
   int b, hk, t;           // item
   int row0, nq, len, nt;  // its sequence; nt = row tiles of the sequence
   int n;                  // tiles of the item
   int k0, k1;             // this CTA's tiles of it
-  long long u, u_end;     // tiles of the whole list: the next one after this part, the end of the run
-  long long item0;        // list index of the item's first tile
-  long long per;          // tiles per CTA
+  int b0;                 // the run's first sequence: geo[] holds it and those behind it
+  long long u_end;        // the end of the run in the whole list
+  long long item0;        // place of the item's first tile in the list (its lead lies before it)
+  long long per;          // length of a run
   bool valid;
 };
+constexpr int GEO = 32;   // sequences a CTA keeps in shared memory, from its first on
 
+// the part of item (b, hk, t) that lies in the run, which enters it at place u
 template <int NR, int KT>
-__device__ __forceinline__ void cursor_part(const PagedAttnArgs& a, WorkCursor& c) {   // the part of item (b, hk, t) that begins at c.u
+__device__ __forceinline__ void cursor_part(const PagedAttnArgs& a, WorkCursor& c, long long u) {
   c.n = item_tiles<NR, KT>(a, c.nq, c.len, c.t);
-  c.k0 = (int)(c.u - c.item0);
-  const long long left = c.u_end - c.u, rest = c.n - c.k0;
-  c.k1 = c.k0 + (int)(left < rest ? left : rest);
-  c.u += c.k1 - c.k0;
+  c.k0 = u > c.item0 ? (int)(u - c.item0) : 0;
+  c.k1 = c.u_end - c.item0 < c.n ? (int)(c.u_end - c.item0) : c.n;
+  c.valid = c.k1 > c.k0;  // (a run that ends in an item's lead has no part of it)
 }
 
 template <int NR, int KT>
-__device__ __forceinline__ void cursor_next(const PagedAttnArgs& a, WorkCursor& c) {
-  if (c.u >= c.u_end) { c.valid = false; return; }
-  c.item0 += c.n;
+__device__ __forceinline__ void cursor_next(const PagedAttnArgs& a, WorkCursor& c, const SeqGeom* geo) {
+  const long long u = c.item0 + c.n;
+  if (u >= c.u_end) { c.valid = false; return; }
+  c.item0 = u + a.lead;
   if (++c.t == c.nt) {
     c.t = 0;
     if (++c.hk == a.Hkv) {
       c.hk = 0;
       do {
         if (++c.b >= a.s.B) { c.valid = false; return; }
-        const SeqGeom g = paged_seq(a.s, c.b);
+        const SeqGeom g = c.b - c.b0 < GEO ? geo[c.b - c.b0] : paged_seq(a.s, c.b);
         c.row0 = g.row0; c.nq = g.nq; c.len = g.len;
       } while (c.nq == 0);
       c.nt = (c.nq * a.G + NR - 1) / NR;
     }
   }
-  cursor_part<NR, KT>(a, c);
+  cursor_part<NR, KT>(a, c, u);
 }
 
-// Sum of item_tiles over a sequence's row tiles, for the sequences of one warp (lane = sequence): short sequences by
+// The work of one key head of a sequence, for the sequences of one warp (lane = sequence): short sequences by
 // their own lane, long ones by the whole warp.
 template <int NR, int KT>
 __device__ __forceinline__ long long warp_seq_units(const PagedAttnArgs& a, const SeqGeom& g, bool live) {
   const int lane = threadIdx.x & 31;
   const int nt = live ? (int)(((long long)g.nq * a.G + NR - 1) / NR) : 0;
   long long sum = 0;
-  if (nt <= 4) for (int t = 0; t < nt; ++t) sum += item_tiles<NR, KT>(a, g.nq, g.len, t);
+  if (nt <= 4) for (int t = 0; t < nt; ++t) sum += a.lead + item_tiles<NR, KT>(a, g.nq, g.len, t);
   unsigned big = __ballot_sync(0xffffffffu, nt > 4);
   while (big) {
     const int src = __ffs(big) - 1;
     big &= big - 1;
     const int nq = __shfl_sync(0xffffffffu, g.nq, src), len = __shfl_sync(0xffffffffu, g.len, src), n = __shfl_sync(0xffffffffu, nt, src);
     long long part = 0;
-    for (int t = lane; t < n; t += 32) part += item_tiles<NR, KT>(a, nq, len, t);
+    for (int t = lane; t < n; t += 32) part += a.lead + item_tiles<NR, KT>(a, nq, len, t);
 #pragma unroll
     for (int o = 16; o > 0; o >>= 1) part += __shfl_xor_sync(0xffffffffu, part, o);
     if (lane == src) sum = part;
@@ -135,10 +140,10 @@ __device__ __forceinline__ long long warp_seq_units(const PagedAttnArgs& a, cons
   return sum;
 }
 
-// Called by warp 0 alone; the result is for every thread of the CTA (through shared memory).  min_run: the fewest tiles a
+// Called by warp 0 alone; the result and geo are for every thread of the CTA (in shared memory).  a.min_run: the least work a
 // CTA takes, so that a short list is not cut into parts that cost more to join than they save.
 template <int NR, int KT>
-__device__ __forceinline__ WorkCursor cursor_begin(const PagedAttnArgs& a, int min_run) {
+__device__ __forceinline__ WorkCursor cursor_begin(const PagedAttnArgs& a, SeqGeom* geo) {
   const int lane = threadIdx.x & 31, B = a.s.B;
   WorkCursor c;
   c.valid = false;
@@ -159,11 +164,11 @@ __device__ __forceinline__ WorkCursor cursor_begin(const PagedAttnArgs& a, int m
   total *= a.Hkv;
   const long long grid = gridDim.x;
   c.per = (total + grid - 1) / grid;
-  if (c.per < min_run) c.per = min_run;
-  c.u = (long long)blockIdx.x * c.per;
-  c.u_end = c.u + c.per < total ? c.u + c.per : total;
-  if (c.u >= c.u_end) return c;
-  // the sequence tile c.u falls into
+  if (c.per < a.min_run) c.per = a.min_run;
+  const long long u = (long long)blockIdx.x * c.per;
+  c.u_end = u + c.per < total ? u + c.per : total;
+  if (u >= c.u_end) return c;
+  // the sequence that place u falls into
   long long base = 0;
   for (int b0 = 0; b0 < B; b0 += 32) {
     const int b = b0 + lane;
@@ -180,7 +185,7 @@ __device__ __forceinline__ WorkCursor cursor_begin(const PagedAttnArgs& a, int m
       const long long up = __shfl_up_sync(0xffffffffu, incl, o);
       if (lane >= o) incl += up;
     }
-    const unsigned hit = __ballot_sync(0xffffffffu, base + incl > c.u);
+    const unsigned hit = __ballot_sync(0xffffffffu, base + incl > u);
     if (hit) {
       const int src = __ffs(hit) - 1;
       c.b = b0 + src;
@@ -189,29 +194,30 @@ __device__ __forceinline__ WorkCursor cursor_begin(const PagedAttnArgs& a, int m
       c.len = __shfl_sync(0xffffffffu, g.len, src);
       const long long first = __shfl_sync(0xffffffffu, base + incl - units, src), per_head = __shfl_sync(0xffffffffu, units, src) / a.Hkv;
       c.nt = (int)(((long long)c.nq * a.G + NR - 1) / NR);
-      c.hk = (int)((c.u - first) / per_head);
-      long long at = first + c.hk * per_head;   // first tile of the key head
+      c.hk = (int)((u - first) / per_head);
+      long long at = first + c.hk * per_head;   // where the key head's work begins
       // the row tile: 32 at a time
       for (int t0 = 0; t0 < c.nt; t0 += 32) {
         const int t = t0 + lane;
-        const long long n = t < c.nt ? item_tiles<NR, KT>(a, c.nq, c.len, t) : 0;
+        const long long n = t < c.nt ? a.lead + item_tiles<NR, KT>(a, c.nq, c.len, t) : 0;
         long long in2 = n;
 #pragma unroll
         for (int o = 1; o < 32; o <<= 1) {
           const long long up = __shfl_up_sync(0xffffffffu, in2, o);
           if (lane >= o) in2 += up;
         }
-        const unsigned hit2 = __ballot_sync(0xffffffffu, at + in2 > c.u);
+        const unsigned hit2 = __ballot_sync(0xffffffffu, at + in2 > u);
         if (hit2) {
           const int s2 = __ffs(hit2) - 1;
           c.t = t0 + s2;
-          c.item0 = __shfl_sync(0xffffffffu, at + in2 - n, s2);
+          c.item0 = __shfl_sync(0xffffffffu, at + in2 - n, s2) + a.lead;
           break;
         }
         at += __shfl_sync(0xffffffffu, in2, 31);
       }
-      c.valid = true;
-      cursor_part<NR, KT>(a, c);
+      c.b0 = c.b;
+      if (c.b + lane < B) geo[lane] = paged_seq(a.s, c.b + lane);
+      cursor_part<NR, KT>(a, c, u);
       return c;
     }
     base += __shfl_sync(0xffffffffu, incl, 31);
@@ -240,8 +246,9 @@ __device__ __forceinline__ void store_out(const PagedAttnArgs& a, long long at, 
 // threads of the last CTA to arrive (named barrier 2 is theirs).  A part's slot is a trip to L2 away, so many loads are in
 // flight at once: maxima and sums by THREADS / NR threads per row; then every thread takes its four-element pieces of the
 // output through all parts, four parts at a time, their weights waiting in shared memory.  w_max, w_inv: shared scratch
-// of NR floats each; w: of w_floats >= 2 * THREADS.
-template <int NR, int D, int THREADS>
+// of NR floats each; w: of w_floats >= 2 * THREADS.  A part's outputs lie row by row, or (BY_PIECE) piece by piece: piece k
+// (four elements) of row r at k * NR + r, for a kernel whose threads own rows.
+template <int NR, int D, int THREADS, bool BY_PIECE = false>
 __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCursor& c, int first, int parts, int tid, float* w_max, float* w_inv, float* w, int w_floats) {
   const int R = c.nq * a.G, r0 = c.t * NR, live = min(NR, R - r0);
   constexpr size_t SF = slot_floats<NR, D>();
@@ -299,9 +306,9 @@ __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCur
         const float* s = slot(pb + p) + 2 * NR;
 #pragma unroll
         for (int k = 0; k < BLOCK; ++k) {
-          const int i = tid + (kb + k) * THREADS;
-          if (i < live * (D / 4)) {
-            const float f = w[p * NR + i / (D / 4)];
+          const int i = tid + (kb + k) * THREADS, r = BY_PIECE ? i % NR : i / (D / 4);
+          if (r < live) {
+            const float f = w[p * NR + r];
             const float4 v = __ldcg(reinterpret_cast<const float4*>(s) + i);
             o[k].x += f * v.x; o[k].y += f * v.y; o[k].z += f * v.z; o[k].w += f * v.w;
           }
@@ -311,9 +318,9 @@ __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCur
     }
 #pragma unroll
     for (int k = 0; k < BLOCK; ++k) {
-      const int i = tid + (kb + k) * THREADS;
-      if (i < live * (D / 4)) {
-        const int r = i / (D / 4), e = (i - r * (D / 4)) * 4, rr = r0 + r, tok = row_token(a, rr);
+      const int i = tid + (kb + k) * THREADS, r = BY_PIECE ? i % NR : i / (D / 4);
+      if (r < live) {
+        const int e = (BY_PIECE ? i / NR : i - r * (D / 4)) * 4, rr = r0 + r, tok = row_token(a, rr);
         const long long at = (long long)(c.row0 + tok) * a.out.row + (long long)(c.hk * a.G + rr - tok * a.G) * a.out.head + e;
         store_out(a, at, o[k].x); store_out(a, at + 1, o[k].y); store_out(a, at + 2, o[k].z); store_out(a, at + 3, o[k].w);
       }

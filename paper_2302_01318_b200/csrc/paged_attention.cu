@@ -26,12 +26,13 @@ __global__ void __launch_bounds__(SIMT_THREADS) paged_attn_simt_kernel(const __g
   __shared__ float s_m[NR], s_l[NR], s_alpha[NR];
   __shared__ int s_lim[NR];
   __shared__ WorkCursor s_cur;
+  __shared__ SeqGeom s_geo[GEO];
   __shared__ int s_last;
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_launch_dependents();
   pdl_wait();
   if (warp == 0) {
-    const WorkCursor c0 = cursor_begin<NR, KT>(a, 1);
+    const WorkCursor c0 = cursor_begin<NR, KT>(a, s_geo);
     if (lane == 0) s_cur = c0;
   }
   __syncthreads();
@@ -173,13 +174,15 @@ __global__ void __launch_bounds__(SIMT_THREADS) paged_attn_simt_kernel(const __g
       __syncthreads();
       if (s_last) join_parts<NR, D, SIMT_THREADS>(a, c, first, parts, tid, s_alpha, s_m, Ps, NR * KT);
     }
-    cursor_next<NR, KT>(a, c);
+    cursor_next<NR, KT>(a, c, s_geo);
   }
 }
 
 template <int D>
-cudaError_t simt_go(const PagedAttnArgs& a, int num_sm, cudaStream_t st) {
+cudaError_t simt_go(PagedAttnArgs a, int num_sm, cudaStream_t st) {
   static DevSmemCache cached{};
+  a.lead = 1;
+  a.min_run = 1;
   constexpr size_t smem = sizeof(float) * (SIMT_KT * (D + 4) + SIMT_KT * D + SIMT_NR * D + SIMT_NR * SIMT_KT);
   const cudaError_t e = sps_ensure_smem(paged_attn_simt_kernel<D>, smem, cached);
   if (e != cudaSuccess) return e;

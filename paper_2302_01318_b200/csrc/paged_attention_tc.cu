@@ -68,7 +68,7 @@ template <int D, int NR, int PARTS> struct Cfg {
   static constexpr int N = PARTS * NR;                              // columns of a product
   static constexpr uint32_t HALF = TILE * D * 2;                    // keys or values of a tile
   static constexpr uint32_t Q_BYTES = N * D * 2, P_BYTES = TILE * N * 2;
-  static constexpr uint32_t HDR = 3328;                             // barriers, small per-row arrays
+  static constexpr uint32_t HDR = 3840;                             // barriers, small per-row arrays
   static constexpr int BUDGET = 232448 - (int)HDR - (int)P_BYTES;
   static constexpr int QBUF = (BUDGET - 2 * (int)Q_BYTES) / (int)HALF >= 4 ? 2 : 1;
   static constexpr int STAGES_FIT = (BUDGET - QBUF * (int)Q_BYTES) / (int)HALF;
@@ -98,13 +98,14 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
   int* s_poison = reinterpret_cast<int*>(hdr + 224);
   int* s_last = reinterpret_cast<int*>(hdr + 228);
   WorkCursor* s_cur = reinterpret_cast<WorkCursor*>(hdr + 232);
-  int* s_lim = reinterpret_cast<int*>(hdr + 384);                      // [NR] last position a row sees
-  float* s_a = reinterpret_cast<float*>(hdr + 384 + NR * 4);           // [NR] maxima
+  SeqGeom* geo = reinterpret_cast<SeqGeom*>(hdr + 384);                // [GEO]
+  int* s_lim = reinterpret_cast<int*>(hdr + 896);                      // [NR] last position a row sees
+  float* s_a = reinterpret_cast<float*>(hdr + 896 + NR * 4);           // [NR] maxima
   float* s_b = s_a + NR;                                               // [NR] sums / factors
   float* s_red = s_b + NR;                                             // [4][NR]
   long long* s_off = reinterpret_cast<long long*>(s_red + 4 * NR);     // [NR] where a row's output goes
   long long* s_qat = s_off + NR;                                       // [NR] where a row of Q is
-  static_assert(384 + NR * 4 * 11 <= (int)C::HDR && sizeof(WorkCursor) <= 152, "header");
+  static_assert(896 + NR * 4 * 11 <= (int)C::HDR && sizeof(WorkCursor) <= 152 && sizeof(SeqGeom) * GEO <= 512, "header");
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
 
   if (tid == 0) {
@@ -123,7 +124,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
   pdl_launch_dependents();
   pdl_wait();
   if (warp == 0) {
-    const WorkCursor c0 = cursor_begin<NR, TILE>(a, ta.min_run);
+    const WorkCursor c0 = cursor_begin<NR, TILE>(a, geo);
     if (lane == 0) *s_cur = c0;
   }
   P_FENCE_BEFORE();
@@ -133,7 +134,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
   WorkCursor c = *s_cur;
 
   if (warp == 0) {
-    copy_pages<D, NR, STAGES>(ta, c, ring, full, empty, s_abort);
+    copy_pages<D, NR, STAGES>(ta, c, geo, ring, full, empty, s_abort);
   } else if (warp == 1) {
     // ---------------------------------------------------------------------------------------------------- products
     const bool leader = p_elect();
@@ -164,7 +165,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
       __syncwarp();
       e_s += 2;
       ++sn;
-      if (last) { cursor_next<NR, TILE>(a, cs); s_i = 0; ++qn; }
+      if (last) { cursor_next<NR, TILE>(a, cs, geo); s_i = 0; ++qn; }
     };
     score();
     while (c.valid && ok) {
@@ -186,7 +187,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
         e_o += 2;
         ++pn;
       }
-      cursor_next<NR, TILE>(a, c);
+      cursor_next<NR, TILE>(a, c, geo);
     }
     if (!ok) {   // every product issued so far must be done before the ring and the tensor memory go away
       *s_abort = 1;
@@ -265,7 +266,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
       if (!both) break;
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       p_arrive(q_ready + 8 * qb);
-      cursor_next<NR, TILE>(a, c);
+      cursor_next<NR, TILE>(a, c, geo);
     }
   } else {
     // ---------------------------------------------------------------------------------------------------- softmax
@@ -502,7 +503,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
         if (*s_last) join_parts<NR, D, SOFT>(a, c, first, parts, st, s_b, s_a, reinterpret_cast<float*>(mem + C::P_AT), C::P_BYTES / 4);
       }
       all_sync();   // s_a, s_b, s_lim are free again
-      cursor_next<NR, TILE>(a, c);
+      cursor_next<NR, TILE>(a, c, geo);
     }
     if (!ok) *s_abort = 1;
   }
@@ -515,8 +516,12 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
 }
 
 template <int D, int NR, int PARTS>
-cudaError_t tc_go(const PagedAttnArgs& a, int num_sm, cudaStream_t st) {
+cudaError_t tc_go(PagedAttnArgs a, int num_sm, cudaStream_t st) {
   static DevSmemCache cached{};
+  // An item costs about two tiles before its first one (Q, the first scores, its outputs): 64 ragged sequences of one token
+  // took 103 / 82 / 61 / 62 / 65 us at 0 / 1 / 2 / 3 / 4; longer least runs than one tile only slowed short calls down.
+  a.lead = 2;
+  a.min_run = 1;
   TcArgs t;
   cudaError_t e = tc_args(a, D, &t);
   if (e == cudaSuccess) e = sps_ensure_smem(paged_attn_tc_kernel<D, NR, PARTS>, Cfg<D, NR, PARTS>::SMEM, cached);

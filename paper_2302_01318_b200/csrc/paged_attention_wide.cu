@@ -37,7 +37,7 @@ template <int D> struct WCfg {
   static constexpr int STAGES = D == 128 ? 4 : 8;
   static constexpr uint32_t Q_AT = STAGES * HALF, HDR_AT = Q_AT + Q_BYTES;
   static constexpr int JOIN_FLOATS = 1024;
-  static constexpr uint32_t HDR = 512 + W_ROWS * (8 + 4 + 4) + JOIN_FLOATS * 4;
+  static constexpr uint32_t HDR = 1024 + W_ROWS * (8 + 4 + 4) + JOIN_FLOATS * 4;
   static constexpr size_t SMEM = HDR_AT + HDR;
   // kind::f16 instruction descriptors: fp32 accumulator, bf16 x bf16, M = 128; S: both K-major, N = 128; O: B MN-major, N = d
   static constexpr uint32_t IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TILE >> 3) << 17) | (8u << 24);
@@ -69,11 +69,12 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
   int* s_poison = reinterpret_cast<int*>(hdr + 208);
   int* s_last = reinterpret_cast<int*>(hdr + 212);
   WorkCursor* s_cur = reinterpret_cast<WorkCursor*>(hdr + 216);
-  long long* s_qat = reinterpret_cast<long long*>(hdr + 512);           // [256] where a row of Q is
-  float* s_max = reinterpret_cast<float*>(hdr + 512 + NR * 8);          // [256] scratch of the join
+  SeqGeom* geo = reinterpret_cast<SeqGeom*>(hdr + 512);                 // [GEO]
+  long long* s_qat = reinterpret_cast<long long*>(hdr + 1024);          // [256] where a row of Q is
+  float* s_max = reinterpret_cast<float*>(hdr + 1024 + NR * 8);          // [256] scratch of the join
   float* s_inv = s_max + NR;
   float* s_join = s_inv + NR;                                           // [JOIN_FLOATS]
-  static_assert(sizeof(WorkCursor) <= 296, "header");
+  static_assert(sizeof(WorkCursor) <= 264 && sizeof(SeqGeom) * GEO <= 512, "header");
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
 
   if (tid == 0) {
@@ -92,7 +93,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
   pdl_launch_dependents();
   pdl_wait();
   if (warp == 0) {
-    const WorkCursor c0 = cursor_begin<NR, TILE>(a, ta.min_run);
+    const WorkCursor c0 = cursor_begin<NR, TILE>(a, geo);
     if (lane == 0) *s_cur = c0;
   }
   P_FENCE_BEFORE();
@@ -108,7 +109,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
   if (warp < 4) {
     W_GIVE();
     if (warp == 0) {
-      copy_pages<D, NR, STAGES>(ta, c, ring, full, empty, s_abort);
+      copy_pages<D, NR, STAGES>(ta, c, geo, ring, full, empty, s_abort);
     } else if (warp == 1) {
       // ---------------------------------------------------------------------------------------------------- products
       const bool leader = p_elect();
@@ -176,7 +177,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
           }
         }
         it += 2 * n;
-        cursor_next<NR, TILE>(a, c);
+        cursor_next<NR, TILE>(a, c, geo);
       }
       if (!ok) {   // every product issued so far must be done before the ring and the tensor memory go away
         *s_abort = 1;
@@ -189,8 +190,6 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
   } else if (warp < 8) {
     W_GIVE();
     // ---------------------------------------------------------------------------------------------------- Q
-    constexpr int CHUNKS = NR * (D / 8) / 128, BATCH = 8;      // 16-byte chunks per thread; loads in flight
-    static_assert(CHUNKS % BATCH == 0, "every chunk belongs to a row of the tiles");
     const int qt = tid - 128;
     bool ok = true;
     for (int qn = 0; c.valid && ok; ++qn) {
@@ -201,30 +200,33 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
         s_qat[r] = (long long)(c.row0 + tok) * a.q.row + (long long)(c.hk * a.G + rr - tok * a.G) * a.q.head;
       }
       asm volatile("bar.sync 7, 128;" ::: "memory");
-#pragma unroll 1
-      for (int b0 = 0; b0 < CHUNKS; b0 += BATCH) {
-        uint4 f[BATCH];
+      // K-major: row r of tile w, 64-element block ch at ((w D / 64 + ch) * 128 + r) * 128, its 16-byte chunk k at chunk k ^ (r & 7)
+      auto place = [&](int r, int k8) { return C::Q_AT + (((r >> 7) * (D / 64) + (k8 >> 3)) * 128 + (r & 127)) * 128 + (((k8 & 7) ^ (r & 7)) << 4); };
+      const __nv_bfloat16* q = reinterpret_cast<const __nv_bfloat16*>(a.q.p);
+      if (qn > 0) {   // into L2 while the part before still needs the buffer
+        for (int r = qt; r < min(live, NR); r += 128)
 #pragma unroll
-        for (int b = 0; b < BATCH; ++b) {
-          const int i = qt + (b0 + b) * 128, r = i / (D / 8), k8 = i - r * (D / 8);
-          f[b] = make_uint4(0u, 0u, 0u, 0u);
-          if (r < live) {
-            const __nv_bfloat16* p = reinterpret_cast<const __nv_bfloat16*>(a.q.p) + s_qat[r] + k8 * 8;
-            if (a.q_vec) {
-              f[b] = *reinterpret_cast<const uint4*>(p);
-            } else {
-              const unsigned short* u = reinterpret_cast<const unsigned short*>(p);
-              f[b] = make_uint4(u[0] | (uint32_t)u[1] << 16, u[2] | (uint32_t)u[3] << 16, u[4] | (uint32_t)u[5] << 16, u[6] | (uint32_t)u[7] << 16);
-            }
-          }
+          for (int e = 0; e < D; e += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + s_qat[r] + e));
+        ok = p_wait(q_free, (uint32_t)(qn - 1) & 1u, a.wait_ns, a.s.status, s_abort);
+      }
+      if (ok && a.q_vec) {
+        // straight to shared memory, all of a thread's 16-byte chunks in flight; rows that do not exist become zeros
+#pragma unroll 4
+        for (int i = qt; i < NR * (D / 8); i += 128) {
+          const int r = i / (D / 8), k8 = i - r * (D / 8);
+          const __nv_bfloat16* src = r < live ? q + s_qat[r] + k8 * 8 : q;
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16, %2;" ::"r"(ring + place(r, k8)), "l"(src), "r"(r < live ? 16 : 0) : "memory");
         }
-        if (b0 == 0 && qn > 0) ok = p_wait(q_free, (uint32_t)(qn - 1) & 1u, a.wait_ns, a.s.status, s_abort);   // the first loads are under way
-        if (!ok) break;
-        // K-major: row r of tile w, 64-element block ch at ((w D / 64 + ch) * 128 + r) * 128, its 16-byte chunk k at chunk k ^ (r & 7)
-#pragma unroll
-        for (int b = 0; b < BATCH; ++b) {
-          const int i = qt + (b0 + b) * 128, r = i / (D / 8), k8 = i - r * (D / 8);
-          *reinterpret_cast<uint4*>(wmem + C::Q_AT + (((r >> 7) * (D / 64) + (k8 >> 3)) * 128 + (r & 127)) * 128 + (((k8 & 7) ^ (r & 7)) << 4)) = f[b];
+        asm volatile("cp.async.wait_all;" ::: "memory");
+      } else if (ok) {
+        for (int i = qt; i < NR * (D / 8); i += 128) {
+          const int r = i / (D / 8), k8 = i - r * (D / 8);
+          uint4 f = make_uint4(0u, 0u, 0u, 0u);
+          if (r < live) {
+            const unsigned short* u = reinterpret_cast<const unsigned short*>(q + s_qat[r] + k8 * 8);
+            f = make_uint4(u[0] | (uint32_t)u[1] << 16, u[2] | (uint32_t)u[3] << 16, u[4] | (uint32_t)u[5] << 16, u[6] | (uint32_t)u[7] << 16);
+          }
+          *reinterpret_cast<uint4*>(wmem + place(r, k8)) = f;
         }
       }
       uint32_t all;   // (and s_qat may be written again)
@@ -232,7 +234,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
       if (!all) break;
       asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
       p_arrive(q_ready);
-      cursor_next<NR, TILE>(a, c);
+      cursor_next<NR, TILE>(a, c, geo);
     }
   } else {
     W_TAKE();
@@ -382,7 +384,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
           if (r >= R) continue;
           if (parts > 1) {
 #pragma unroll
-            for (int q = 0; q < 32; q += 4) __stcg(reinterpret_cast<float4*>(slot + 2 * NR + sr * D + j + q), make_float4(o[q], o[q + 1], o[q + 2], o[q + 3]));
+            for (int q = 0; q < 32; q += 4) __stcg(reinterpret_cast<float4*>(slot + 2 * NR) + ((j + q) >> 2) * NR + sr, make_float4(o[q], o[q + 1], o[q + 2], o[q + 3]));
           } else {
 #pragma unroll
             for (int q = 0; q < 32; ++q) o[q] = l == 0.f ? 0.f : o[q] * inv;
@@ -416,10 +418,10 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
           if (*s_last) { a.counters[first] = 0; __threadfence(); }
         }
         asm volatile("bar.sync 1, 256;" ::: "memory");
-        if (*s_last) join_parts<NR, D, W_SOFT>(a, c, first, parts, st, s_max, s_inv, s_join, C::JOIN_FLOATS);
+        if (*s_last) join_parts<NR, D, W_SOFT, true>(a, c, first, parts, st, s_max, s_inv, s_join, C::JOIN_FLOATS);
       }
       asm volatile("bar.sync 1, 256;" ::: "memory");   // s_poison and s_last may be written again
-      cursor_next<NR, TILE>(a, c);
+      cursor_next<NR, TILE>(a, c, geo);
     }
     if (!ok) *s_abort = 1;
   }
@@ -432,8 +434,10 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
 }
 
 template <int D>
-cudaError_t wide_go(const PagedAttnArgs& a, int num_sm, cudaStream_t st) {
+cudaError_t wide_go(PagedAttnArgs a, int num_sm, cudaStream_t st) {
   static DevSmemCache cached{};
+  a.lead = 1;
+  a.min_run = 2;
   TcArgs t;
   cudaError_t e = tc_args(a, D, &t);
   if (e == cudaSuccess) e = sps_ensure_smem(paged_attn_wide_kernel<D>, WCfg<D>::SMEM, cached);

@@ -15,7 +15,6 @@ struct TcArgs {
   PagedAttnArgs a;
   int box;             // slots per copy: min(page_size, 128)
   int head_first;      // the tensor maps' dimensions are (d, head, slot, page) instead of (d, slot, head, page)
-  int min_run;
 };
 
 __device__ __forceinline__ uint32_t p_smem(const void* p) { return (uint32_t)__cvta_generic_to_shared(p); }
@@ -136,24 +135,29 @@ __device__ __forceinline__ void p_st16(uint32_t t, const uint32_t* r) {
 // STAGES of them.  Lane i asks for page i of the tile (or its only page): boxes of 64 elements x ta.box slots, 128-byte
 // swizzle, so a half-tile is d / 64 blocks of 128 tokens x 128 bytes.
 template <int D, int NR, int STAGES>
-__device__ __forceinline__ void copy_pages(const TcArgs& ta, WorkCursor c, uint32_t ring, uint32_t full, uint32_t empty, volatile int* s_abort) {
+__device__ __forceinline__ void copy_pages(const TcArgs& ta, WorkCursor c, const SeqGeom* geo, uint32_t ring, uint32_t full, uint32_t empty, volatile int* s_abort) {
   constexpr uint32_t HALF = TILE * D * 2;
   const PagedAttnArgs& a = ta.a;
   const int lane = threadIdx.x & 31;
   bool ok = true;
   int it = 0;   // half-tiles asked for so far
   const int boxes = TILE / ta.box;
+  auto page_of = [&](const WorkCursor& c, int kt) {   // this lane's page of a tile
+    const int pos = kt * TILE + lane * ta.box;
+    return lane < boxes && pos < c.len ? a.s.pages[(long long)c.b * a.s.pages_ld + (pos >> a.s.page_shift)] : 0;
+  };
+  int next = c.valid ? page_of(c, c.k0) : 0;
   while (c.valid && ok) {
-    const int32_t* table = a.s.pages + (long long)c.b * a.s.pages_ld;
-    int next = lane < boxes && c.k0 * TILE + lane * ta.box < c.len ? table[(c.k0 * TILE + lane * ta.box) >> a.s.page_shift] : 0;
+    WorkCursor after = c;
+    cursor_next<NR, TILE>(a, after, geo);
     for (int kt = c.k0; kt < c.k1 && ok; ++kt) {
       const int pos = kt * TILE + lane * ta.box;
       const bool mine = lane < boxes && pos < c.len;
       int page = next;
-      if (kt + 1 < c.k1 && lane < boxes && pos + TILE < c.len) next = table[(pos + TILE) >> a.s.page_shift];   // under way while this tile waits
-      if (mine) {
-        if (page < 0 || page >= a.s.n_pages) { paged_flag(a.s.status, SPS_PAGED_BAD_PAGE); page = a.s.n_pages; }   // outside the map: zeros
-      }
+      // the next tile's page numbers, the next part's included, are under way while this tile waits
+      if (kt + 1 < c.k1) next = page_of(c, kt + 1);
+      else if (after.valid) next = page_of(after, after.k0);
+      if (mine && (page < 0 || page >= a.s.n_pages)) { paged_flag(a.s.status, SPS_PAGED_BAD_PAGE); page = a.s.n_pages; }   // outside the map: zeros
       const int in_page = pos & (a.s.page_size - 1);
       const int n = __popc(__ballot_sync(0xffffffffu, mine));
 #pragma unroll
@@ -180,7 +184,7 @@ __device__ __forceinline__ void copy_pages(const TcArgs& ta, WorkCursor c, uint3
         __syncwarp();
       }
     }
-    cursor_next<NR, TILE>(a, c);
+    c = after;
   }
   if (lane == 0) {   // whatever happened, the copies in flight land before this CTA's shared memory goes away
     if (!ok) *s_abort = 1;
@@ -224,7 +228,6 @@ inline cudaError_t tc_args(const PagedAttnArgs& a, int D, TcArgs* t) {
   t->a = a;
   t->box = a.s.page_size < TILE ? a.s.page_size : TILE;
   t->head_first = a.Hkv > 1 && a.head_stride < a.pos_stride;
-  t->min_run = 1;
   const cudaError_t e = page_map(encode, a.k, a, D, t->box, t->head_first, &t->tm_k);
   return e != cudaSuccess ? e : page_map(encode, a.v, a, D, t->box, t->head_first, &t->tm_v);
 }
