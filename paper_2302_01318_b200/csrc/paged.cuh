@@ -140,30 +140,39 @@ __device__ __forceinline__ long long warp_seq_units(const PagedAttnArgs& a, cons
   return sum;
 }
 
+__device__ __forceinline__ long long list_div(long long n, long long d) {   // n, d >= 0; almost always 32 bits wide
+  if (((unsigned long long)(n | d) >> 32) == 0) return (long long)((unsigned)n / (unsigned)d);
+  return n / d;
+}
+
 // Called by warp 0 alone; the result and geo are for every thread of the CTA (in shared memory).  a.min_run: the least work a
-// CTA takes, so that a short list is not cut into parts that cost more to join than they save.
+// CTA takes, so that a short list is not cut into parts that cost more to join than they save.  Up to 32 sequences are
+// read once, more of them twice (their number of tiles first, then the place of this CTA's run among them).
 template <int NR, int KT>
 __device__ __forceinline__ WorkCursor cursor_begin(const PagedAttnArgs& a, SeqGeom* geo) {
   const int lane = threadIdx.x & 31, B = a.s.B;
   WorkCursor c;
   c.valid = false;
-  long long total = 0, units0 = 0;
-  SeqGeom g0{};              // the first 32 sequences, kept for the second sweep
-  bool cut = false;
-  for (int b0 = 0; b0 < B; b0 += 32) {
+  SeqGeom g{};                   // the sequences of one block of 32, a lane each; their work, and the sum up to each
+  long long units = 0, incl = 0, total = 0;
+  auto block = [&](int b0) {
     const int b = b0 + lane;
-    SeqGeom g{};
-    if (b < B) { g = paged_seq(a.s, b); cut = cut || (g.cut && g.nq > 0); }
-    const long long units = warp_seq_units<NR, KT>(a, g, b < B);
-    if (b0 == 0) { g0 = g; units0 = units; }
-    total += units;
-  }
-  if (cut && blockIdx.x == 0) paged_flag(a.s.status, SPS_PAGED_BAD_LENGTH);
+    g = SeqGeom{};
+    if (b < B) g = paged_seq(a.s, b);
+    units = warp_seq_units<NR, KT>(a, g, b < B) * a.Hkv;
+    incl = units;
 #pragma unroll
-  for (int o = 16; o > 0; o >>= 1) total += __shfl_xor_sync(0xffffffffu, total, o);
-  total *= a.Hkv;
-  const long long grid = gridDim.x;
-  c.per = (total + grid - 1) / grid;
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long up = __shfl_up_sync(0xffffffffu, incl, o);
+      if (lane >= o) incl += up;
+    }
+  };
+  for (int b0 = 0; b0 < B; b0 += 32) {
+    block(b0);
+    if (blockIdx.x == 0 && g.cut && g.nq > 0) paged_flag(a.s.status, SPS_PAGED_BAD_LENGTH);
+    total += __shfl_sync(0xffffffffu, incl, 31);
+  }
+  c.per = list_div(total + gridDim.x - 1, gridDim.x);
   if (c.per < a.min_run) c.per = a.min_run;
   const long long u = (long long)blockIdx.x * c.per;
   c.u_end = u + c.per < total ? u + c.per : total;
@@ -171,52 +180,46 @@ __device__ __forceinline__ WorkCursor cursor_begin(const PagedAttnArgs& a, SeqGe
   // the sequence that place u falls into
   long long base = 0;
   for (int b0 = 0; b0 < B; b0 += 32) {
-    const int b = b0 + lane;
-    SeqGeom g = g0;
-    long long units = units0;
-    if (b0 > 0) {
-      if (b < B) g = paged_seq(a.s, b);
-      units = warp_seq_units<NR, KT>(a, g, b < B);
-    }
-    units *= a.Hkv;
-    long long incl = units;
-#pragma unroll
-    for (int o = 1; o < 32; o <<= 1) {
-      const long long up = __shfl_up_sync(0xffffffffu, incl, o);
-      if (lane >= o) incl += up;
-    }
+    if (B > 32) block(b0);
     const unsigned hit = __ballot_sync(0xffffffffu, base + incl > u);
     if (hit) {
       const int src = __ffs(hit) - 1;
-      c.b = b0 + src;
+      c.b = c.b0 = b0 + src;
       c.row0 = __shfl_sync(0xffffffffu, g.row0, src);
       c.nq = __shfl_sync(0xffffffffu, g.nq, src);
       c.len = __shfl_sync(0xffffffffu, g.len, src);
-      const long long first = __shfl_sync(0xffffffffu, base + incl - units, src), per_head = __shfl_sync(0xffffffffu, units, src) / a.Hkv;
-      c.nt = (int)(((long long)c.nq * a.G + NR - 1) / NR);
-      c.hk = (int)((u - first) / per_head);
-      long long at = first + c.hk * per_head;   // where the key head's work begins
-      // the row tile: 32 at a time
-      for (int t0 = 0; t0 < c.nt; t0 += 32) {
-        const int t = t0 + lane;
-        const long long n = t < c.nt ? a.lead + item_tiles<NR, KT>(a, c.nq, c.len, t) : 0;
-        long long in2 = n;
-#pragma unroll
-        for (int o = 1; o < 32; o <<= 1) {
-          const long long up = __shfl_up_sync(0xffffffffu, in2, o);
-          if (lane >= o) in2 += up;
-        }
-        const unsigned hit2 = __ballot_sync(0xffffffffu, at + in2 > u);
-        if (hit2) {
-          const int s2 = __ffs(hit2) - 1;
-          c.t = t0 + s2;
-          c.item0 = __shfl_sync(0xffffffffu, at + in2 - n, s2) + a.lead;
-          break;
-        }
-        at += __shfl_sync(0xffffffffu, in2, 31);
+      if (B <= 32) {
+        if (lane >= src && lane < B) geo[lane - src] = g;
+      } else if (c.b + lane < B) {
+        geo[lane] = paged_seq(a.s, c.b + lane);
       }
-      c.b0 = c.b;
-      if (c.b + lane < B) geo[lane] = paged_seq(a.s, c.b + lane);
+      const long long first = base + __shfl_sync(0xffffffffu, incl - units, src), per_head = list_div(__shfl_sync(0xffffffffu, units, src), a.Hkv);
+      c.nt = (int)(((long long)c.nq * a.G + NR - 1) / NR);
+      c.hk = (int)list_div(u - first, per_head);
+      long long at = first + c.hk * per_head;   // where the key head's work begins
+      c.t = 0;
+      if (c.nt > 1) {
+        // the row tile: 32 at a time
+        for (int t0 = 0; t0 < c.nt; t0 += 32) {
+          const int t = t0 + lane;
+          const long long n = t < c.nt ? a.lead + item_tiles<NR, KT>(a, c.nq, c.len, t) : 0;
+          long long in2 = n;
+#pragma unroll
+          for (int o = 1; o < 32; o <<= 1) {
+            const long long up = __shfl_up_sync(0xffffffffu, in2, o);
+            if (lane >= o) in2 += up;
+          }
+          const unsigned hit2 = __ballot_sync(0xffffffffu, at + in2 > u);
+          if (hit2) {
+            const int s2 = __ffs(hit2) - 1;
+            c.t = t0 + s2;
+            at += __shfl_sync(0xffffffffu, in2 - n, s2);
+            break;
+          }
+          at += __shfl_sync(0xffffffffu, in2, 31);
+        }
+      }
+      c.item0 = at + a.lead;
       cursor_part<NR, KT>(a, c, u);
       return c;
     }
@@ -230,12 +233,22 @@ __device__ __forceinline__ void item_ctas(const WorkCursor& c, int& first, int& 
   first = blockIdx.x;
   parts = 1;
   if (c.k0 == 0 && c.k1 == c.n) return;
-  first = (int)(c.item0 / c.per);
-  parts = (int)((c.item0 + c.n - 1) / c.per) - first + 1;
+  first = (int)list_div(c.item0, c.per);
+  parts = (int)list_div(c.item0 + c.n - 1, c.per) - first + 1;
 }
 // the slot of this CTA's part: 2 c + 1 where the item begins in this CTA, else 2 c (a run holds at most one of each)
 __device__ __forceinline__ int part_slot(int cta, bool begins) { return 2 * cta + (begins ? 1 : 0); }
 template <int NR, int D> __host__ __device__ constexpr size_t slot_floats() { return (size_t)NR * (D + 2); }
+
+// One thread's word that its CTA's part is out (the CTA's threads have met since): true for the last part of the item, which
+// may then read the others'; the counter is left at zero for the next call.
+__device__ __forceinline__ bool part_arrive(int* counter, int parts) {
+  int old;
+  asm volatile("atom.acq_rel.gpu.global.add.s32 %0, [%1], 1;" : "=r"(old) : "l"(counter) : "memory");
+  if (old != parts - 1) return false;
+  *counter = 0;
+  return true;
+}
 
 __device__ __forceinline__ void store_out(const PagedAttnArgs& a, long long at, float v) {
   if (a.out_bf16) reinterpret_cast<__nv_bfloat16*>(a.out.p)[at] = __float2bfloat16_rn(v);
@@ -244,18 +257,28 @@ __device__ __forceinline__ void store_out(const PagedAttnArgs& a, long long at, 
 
 // Joins the parts of an item and writes its rows: o = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c.  Run by all THREADS
 // threads of the last CTA to arrive (named barrier 2 is theirs).  A part's slot is a trip to L2 away, so many loads are in
-// flight at once: maxima and sums by THREADS / NR threads per row; then every thread takes its four-element pieces of the
-// output through all parts, four parts at a time, their weights waiting in shared memory.  w_max, w_inv: shared scratch
-// of NR floats each; w: of w_floats >= 2 * THREADS.  A part's outputs lie row by row, or (BY_PIECE) piece by piece: piece k
-// (four elements) of row r at k * NR + r, for a kernel whose threads own rows.
+// flight at once: every thread first asks for its four-element pieces of the first AHEAD parts' outputs, then for maxima and
+// sums (THREADS / NR threads to a row), and goes on four parts at a time, their weights in shared memory.  s_max, s_inv: shared
+// scratch of NR floats each; w: of w_floats >= 2 * THREADS.  A part's outputs lie row by row, or (BY_PIECE) piece by piece:
+// piece k (four elements) of row r at k * NR + r, for a kernel whose threads own rows.
 template <int NR, int D, int THREADS, bool BY_PIECE = false>
-__device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCursor& c, int first, int parts, int tid, float* w_max, float* w_inv, float* w, int w_floats) {
+__device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCursor& c, int first, int parts, int tid, float* s_max, float* s_inv, float* w, int w_floats) {
   const int R = c.nq * a.G, r0 = c.t * NR, live = min(NR, R - r0);
   constexpr size_t SF = slot_floats<NR, D>();
-  constexpr int LANES = THREADS / NR, PIECES = NR * (D / 4) / THREADS;
+  constexpr int LANES = THREADS / NR, PIECES = NR * (D / 4) / THREADS, BLOCK = PIECES < 4 ? PIECES : 4, AHEAD = 2;
   const float* slots = a.slots + SF * (size_t)(2 * first);
   auto slot = [&](int p) { return slots + SF * (size_t)(p == 0 ? 1 : 2 * p); };   // part 0 begins in its CTA: part_slot
   auto sync = [&]() { asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory"); };
+  auto row = [&](int i) { return BY_PIECE ? i % NR : i / (D / 4); };
+  auto fetch = [&](int p, int i) { return __ldcg(reinterpret_cast<const float4*>(slot(p) + 2 * NR) + i); };
+  float4 early[AHEAD][BLOCK];
+#pragma unroll
+  for (int p = 0; p < AHEAD; ++p)
+#pragma unroll
+    for (int k = 0; k < BLOCK; ++k) {
+      const int i = tid + k * THREADS;
+      early[p][k] = row(i) < live ? fetch(p, i) : make_float4(0.f, 0.f, 0.f, 0.f);    // (an item that is joined has at least two)
+    }
   {
     const int r = tid % NR, p0 = tid / NR;
     float M = -INFINITY, L = 0.f;
@@ -277,8 +300,8 @@ __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCur
     for (int i = 0; i < LANES; ++i) M = fmaxf(M, w[2 * (i * NR + tid)]);
     const float base = M == -INFINITY ? 0.f : M;
     for (int i = 0; i < LANES; ++i) L += w[2 * (i * NR + tid) + 1] * exp2f(w[2 * (i * NR + tid)] - base);
-    w_max[tid] = base;
-    w_inv[tid] = L == 0.f ? 0.f : 1.f / L;
+    s_max[tid] = base;
+    s_inv[tid] = L == 0.f ? 0.f : 1.f / L;
     if (a.lse) {
       const int r = r0 + tid;
       a.lse[(size_t)(c.row0 + row_token(a, r)) * a.H + c.hk * a.G + r - row_token(a, r) * a.G] = L == 0.f ? -INFINITY : 0.6931471805599453f * (base + log2f(L));
@@ -286,7 +309,6 @@ __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCur
   }
   sync();
   const int table = w_floats / NR;                             // parts whose weights fit at once
-  constexpr int BLOCK = PIECES < 4 ? PIECES : 4;
 #pragma unroll 1
   for (int kb = 0; kb < PIECES; kb += BLOCK) {
     float4 o[BLOCK];
@@ -297,28 +319,34 @@ __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCur
       if (kb == 0 || parts > table) {
         for (int i = tid; i < pn * NR; i += THREADS) {
           const int p = i / NR, r = i - p * NR;
-          if (r < live) w[i] = exp2f(__ldcg(slot(pb + p) + r) - w_max[r]) * w_inv[r];
+          if (r < live) w[i] = exp2f(__ldcg(slot(pb + p) + r) - s_max[r]) * s_inv[r];
         }
         sync();
       }
+      auto add = [&](int k, float f, const float4& v) { o[k].x += f * v.x; o[k].y += f * v.y; o[k].z += f * v.z; o[k].w += f * v.w; };
+      int p = 0;
+      if (kb == 0 && pb == 0) {
+#pragma unroll
+        for (; p < AHEAD; ++p)
+#pragma unroll
+          for (int k = 0; k < BLOCK; ++k) {
+            const int r = row(tid + k * THREADS);
+            if (r < live) add(k, w[p * NR + r], early[p][k]);
+          }
+      }
 #pragma unroll 4
-      for (int p = 0; p < pn; ++p) {
-        const float* s = slot(pb + p) + 2 * NR;
+      for (; p < pn; ++p) {
 #pragma unroll
         for (int k = 0; k < BLOCK; ++k) {
-          const int i = tid + (kb + k) * THREADS, r = BY_PIECE ? i % NR : i / (D / 4);
-          if (r < live) {
-            const float f = w[p * NR + r];
-            const float4 v = __ldcg(reinterpret_cast<const float4*>(s) + i);
-            o[k].x += f * v.x; o[k].y += f * v.y; o[k].z += f * v.z; o[k].w += f * v.w;
-          }
+          const int i = tid + (kb + k) * THREADS, r = row(i);
+          if (r < live) add(k, w[p * NR + r], fetch(pb + p, i));
         }
       }
       if (parts > table) sync();   // the table may be written again
     }
 #pragma unroll
     for (int k = 0; k < BLOCK; ++k) {
-      const int i = tid + (kb + k) * THREADS, r = BY_PIECE ? i % NR : i / (D / 4);
+      const int i = tid + (kb + k) * THREADS, r = row(i);
       if (r < live) {
         const int e = (BY_PIECE ? i / NR : i - r * (D / 4)) * 4, rr = r0 + r, tok = row_token(a, rr);
         const long long at = (long long)(c.row0 + tok) * a.out.row + (long long)(c.hk * a.G + rr - tok * a.G) * a.out.head + e;

@@ -167,9 +167,7 @@ __global__ void __launch_bounds__(SIMT_THREADS) paged_attn_simt_kernel(const __g
       }
       __syncthreads();
       if (tid == 0) {
-        __threadfence();   // the CTA's parts are out before its arrival is
-        s_last = atomicAdd(a.counters + first, 1) == parts - 1;
-        if (s_last) { a.counters[first] = 0; __threadfence(); }
+        s_last = part_arrive(a.counters + first, parts);
       }
       __syncthreads();
       if (s_last) join_parts<NR, D, SIMT_THREADS>(a, c, first, parts, tid, s_alpha, s_m, Ps, NR * KT);

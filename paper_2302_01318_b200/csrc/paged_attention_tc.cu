@@ -198,7 +198,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
     }
   } else if (warp < 4) {
     // ---------------------------------------------------------------------------------------------------- Q
-    constexpr int CHUNKS = NR * (D / 8) / 64, BATCH = CHUNKS % 4 == 0 ? 4 : (CHUNKS % 3 == 0 ? 3 : 2);   // 8-element chunks per thread; loads in flight
+    constexpr int CHUNKS = NR * (D / 8) / 64, BATCH = CHUNKS % 6 == 0 ? 6 : (CHUNKS % 4 == 0 ? 4 : 2);   // 8-element chunks per thread; loads in flight
     static_assert(NR * (D / 8) % 64 == 0 && CHUNKS % BATCH == 0, "every chunk belongs to a row of the tile");
     const int qt = tid - 64;
     bool ok = true;
@@ -479,25 +479,34 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
       float* slot = a.slots + slot_floats<NR, D>() * (size_t)part_slot(blockIdx.x, c.k0 == 0);
       const int rows = min(max(R - r0 - col0, 0), live_lane ? 16 : 0);
       if (parts == 1) {
-        long long at[16];
-        float f[16];
 #pragma unroll
-        for (int j = 0; j < 16; ++j) { at[j] = s_off[col0 + j] + e; f[j] = s_b[col0 + j]; }
+        for (int j0 = 0; j0 < 16; j0 += 4) {
+          if (j0 >= rows) break;
+          long long at[4];
+          float f[4];
 #pragma unroll
-        for (int j = 0; j < 16; ++j)
-          if (j < rows) store_out(a, at[j], f[j] == 0.f ? 0.f : o[j] * f[j]);
+          for (int j = 0; j < 4; ++j) { at[j] = s_off[col0 + j0 + j] + e; f[j] = s_b[col0 + j0 + j]; }
+#pragma unroll
+          for (int j = 0; j < 4; ++j) f[j] = f[j] == 0.f ? 0.f : o[j0 + j] * f[j];
+          if (a.out_bf16) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) if (j0 + j < rows) reinterpret_cast<__nv_bfloat16*>(a.out.p)[at[j]] = __float2bfloat16_rn(f[j]);
+          } else {
+#pragma unroll
+            for (int j = 0; j < 4; ++j) if (j0 + j < rows) reinterpret_cast<float*>(a.out.p)[at[j]] = f[j];
+          }
+        }
       } else {
+        float* s = slot + 2 * NR + col0 * D + e;
 #pragma unroll
         for (int j = 0; j < 16; ++j)
-          if (j < rows) __stcg(slot + 2 * NR + (col0 + j) * D + e, o[j]);
+          if (j < rows) __stcg(s + j * D, o[j]);
       }
       if (parts > 1) {
         if (st < NR) { __stcg(slot + st, s_a[st]); __stcg(slot + NR + st, s_b[st]); }
         all_sync();
         if (st == 0) {
-          __threadfence();   // the CTA's parts are out before its arrival is
-          *s_last = atomicAdd(a.counters + first, 1) == parts - 1;
-          if (*s_last) { a.counters[first] = 0; __threadfence(); }
+          *s_last = part_arrive(a.counters + first, parts);
         }
         all_sync();
         if (*s_last) join_parts<NR, D, SOFT>(a, c, first, parts, st, s_b, s_a, reinterpret_cast<float*>(mem + C::P_AT), C::P_BYTES / 4);

@@ -413,9 +413,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
       if (parts > 1) {
         asm volatile("bar.sync 1, 256;" ::: "memory");
         if (st == 0) {
-          __threadfence();   // the CTA's parts are out before its arrival is
-          *s_last = atomicAdd(a.counters + first, 1) == parts - 1;
-          if (*s_last) { a.counters[first] = 0; __threadfence(); }
+          *s_last = part_arrive(a.counters + first, parts);
         }
         asm volatile("bar.sync 1, 256;" ::: "memory");
         if (*s_last) join_parts<NR, D, W_SOFT, true>(a, c, first, parts, st, s_max, s_inv, s_join, C::JOIN_FLOATS);
