@@ -68,7 +68,7 @@ template <int D, int NR, int PARTS> struct Cfg {
   static constexpr int N = PARTS * NR;                              // columns of a product
   static constexpr uint32_t HALF = TILE * D * 2;                    // keys or values of a tile
   static constexpr uint32_t Q_BYTES = N * D * 2, P_BYTES = TILE * N * 2;
-  static constexpr uint32_t HDR = 3840;                             // barriers, small per-row arrays
+  static constexpr uint32_t HDR = 4224;                             // barriers, small per-row arrays
   static constexpr int BUDGET = 232448 - (int)HDR - (int)P_BYTES;
   static constexpr int QBUF = (BUDGET - 2 * (int)Q_BYTES) / (int)HALF >= 4 ? 2 : 1;
   static constexpr int STAGES_FIT = (BUDGET - QBUF * (int)Q_BYTES) / (int)HALF;
@@ -84,6 +84,78 @@ template <int D, int NR, int PARTS> struct Cfg {
   static_assert(STAGES >= 4 && 3 * N <= 512 && N <= 256, "shape");
 };
 
+// Q of the cursor's item into shared memory, in PARTS bf16 parts, by THREADS threads (named barrier `bar` is theirs): K-major,
+// row (part, r) of 64-element block ch at (part NR + r) * 128, its 16-byte chunk k at chunk k ^ (r & 7); rows that do not
+// exist are zeros.  s_at: scratch of NR places.  may_write: whether the buffer is free, asked with the first loads under way.
+template <int D, int NR, int PARTS, int THREADS, class F>
+__device__ __forceinline__ bool load_q(const PagedAttnArgs& a, const WorkCursor& c, unsigned char* q_mem, long long* s_at, int qt, int bar, F may_write) {
+  constexpr int CHUNKS = NR * (D / 8) / THREADS, BATCH = CHUNKS % 6 == 0 ? 6 : (CHUNKS % 4 == 0 ? 4 : (CHUNKS % 2 == 0 ? 2 : 1));   // 8-element chunks per thread; in flight
+  static_assert(NR * (D / 8) % THREADS == 0 && CHUNKS % BATCH == 0 && THREADS >= NR, "every chunk belongs to a row of the tile");
+  const int live = c.nq * a.G - c.t * NR;
+  if (qt < NR) {
+    const int rr = c.t * NR + qt, tok = row_token(a, rr);
+    s_at[qt] = (long long)(c.row0 + tok) * a.q.row + (long long)(c.hk * a.G + rr - tok * a.G) * a.q.head;
+  }
+  asm volatile("bar.sync %0, %1;" ::"r"(bar), "n"(THREADS) : "memory");
+  bool ok = true;
+#pragma unroll 1
+  for (int b0 = 0; b0 < CHUNKS; b0 += BATCH) {
+    float f[BATCH][8];
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) {
+      const int i = qt + (b0 + b) * THREADS, r = i / (D / 8), k8 = i - r * (D / 8);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) f[b][j] = 0.f;
+      if (r < live) {
+        const long long at = s_at[r] + k8 * 8;
+        if (PARTS == 3) {
+          const float* p = reinterpret_cast<const float*>(a.q.p) + at;
+          if (a.q_vec) {
+            const float4 x = *reinterpret_cast<const float4*>(p), y = *reinterpret_cast<const float4*>(p + 4);
+            f[b][0] = x.x; f[b][1] = x.y; f[b][2] = x.z; f[b][3] = x.w; f[b][4] = y.x; f[b][5] = y.y; f[b][6] = y.z; f[b][7] = y.w;
+          } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[b][j] = p[j];
+          }
+        } else {
+          const __nv_bfloat16* p = reinterpret_cast<const __nv_bfloat16*>(a.q.p) + at;
+          if (a.q_vec) {
+            const uint4 u = *reinterpret_cast<const uint4*>(p);
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int j = 0; j < 4; ++j) { f[b][2 * j] = p_lo(w[j]); f[b][2 * j + 1] = p_hi(w[j]); }
+          } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) f[b][j] = __bfloat162float(p[j]);
+          }
+        }
+      }
+    }
+    if (b0 == 0) ok = may_write();
+    if (!ok) break;
+#pragma unroll
+    for (int b = 0; b < BATCH; ++b) {
+      const int i = qt + (b0 + b) * THREADS, r = i / (D / 8), k8 = i - r * (D / 8);
+      unsigned char* dst = q_mem + (k8 >> 3) * (PARTS * NR * 128) + r * 128 + (((k8 & 7) ^ (r & 7)) << 4);
+#pragma unroll
+      for (int part = 0; part < PARTS; ++part) {
+        uint32_t u[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          u[j] = p_pack(f[b][2 * j], f[b][2 * j + 1]);
+          if (part + 1 < PARTS) { f[b][2 * j] -= p_lo(u[j]); f[b][2 * j + 1] -= p_hi(u[j]); }
+        }
+        *reinterpret_cast<uint4*>(dst + part * (NR * 128)) = make_uint4(u[0], u[1], u[2], u[3]);
+      }
+    }
+  }
+  uint32_t all;   // (and s_at may be written again)
+  asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.and.pred p, %2, %3, q;\n selp.u32 %0, 1, 0, p;\n}\n"
+               : "=r"(all) : "r"(ok ? 1u : 0u), "r"(bar), "n"(THREADS) : "memory");
+  asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+  return all != 0;
+}
+
 template <int D, int NR, int PARTS>
 __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_kernel(const __grid_constant__ TcArgs ta) {
   using C = Cfg<D, NR, PARTS>;
@@ -92,7 +164,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
   const PagedAttnArgs& a = ta.a;
   const uint32_t ring = p_smem(mem), hb = ring + C::HDR_AT;
   unsigned char* hdr = mem + C::HDR_AT;
-  const uint32_t full = hb, empty = hb + 64, s_full = hb + 128, s_free = hb + 144, p_full = hb + 160, pv_done = hb + 168, q_ready = hb + 176, q_free = hb + 192, drain = hb + 208;
+  const uint32_t full = hb, empty = hb + 64, s_full = hb + 128, s_free = hb + 144, p_full = hb + 160, pv_done = hb + 168, q_ready = hb + 176, q_free = hb + 192, drain = hb + 208, q_first = hb + 376;
   volatile uint32_t* s_tmem = reinterpret_cast<volatile uint32_t*>(hdr + 216);
   volatile int* s_abort = reinterpret_cast<volatile int*>(hdr + 220);
   int* s_poison = reinterpret_cast<int*>(hdr + 224);
@@ -104,14 +176,14 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
   float* s_b = s_a + NR;                                               // [NR] sums / factors
   float* s_red = s_b + NR;                                             // [4][NR]
   long long* s_off = reinterpret_cast<long long*>(s_red + 4 * NR);     // [NR] where a row's output goes
-  long long* s_qat = s_off + NR;                                       // [NR] where a row of Q is
-  static_assert(896 + NR * 4 * 11 <= (int)C::HDR && sizeof(WorkCursor) <= 152 && sizeof(SeqGeom) * GEO <= 512, "header");
+  long long* s_qat = s_off + NR;                                       // [2][NR] where a row of Q is (loader, first part)
+  static_assert(896 + NR * 4 * 13 <= (int)C::HDR && sizeof(WorkCursor) <= 144 && sizeof(SeqGeom) * GEO <= 512, "header");
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
 
   if (tid == 0) {
     for (int i = 0; i < STAGES; ++i) { p_bar_init(full + 8 * i, 1); p_bar_init(empty + 8 * i, 1); }
     for (int i = 0; i < 2; ++i) { p_bar_init(s_full + 8 * i, 1); p_bar_init(s_free + 8 * i, SOFT); p_bar_init(q_ready + 8 * i, 64); p_bar_init(q_free + 8 * i, 1); }
-    p_bar_init(p_full, SOFT); p_bar_init(pv_done, 1); p_bar_init(drain, 1);
+    p_bar_init(p_full, SOFT); p_bar_init(q_first, SOFT); p_bar_init(pv_done, 1); p_bar_init(drain, 1);
     *s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&ta.tm_k) : "memory");
@@ -147,7 +219,10 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
     auto score = [&]() {                                       // S of the next tile
       if (!cs.valid) return;
       const int buf = sn & 1, qb = qn % C::QBUF;
-      if (s_i == 0) wait(q_ready + 8 * qb, (uint32_t)(qn / C::QBUF));
+      if (s_i == 0) {
+        if (qn == 0) wait(q_first, 0);
+        else wait(q_ready + 8 * qb, (uint32_t)(qn / C::QBUF - (qb == 0 ? 1 : 0)));   // (the first part did not use it)
+      }
       if (sn >= 2) wait(s_free + 8 * buf, (uint32_t)((sn >> 1) - 1));
       wait(full + 8 * (e_s % STAGES), (uint32_t)(e_s / STAGES));
       if (!ok) return;
@@ -198,73 +273,14 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
     }
   } else if (warp < 4) {
     // ---------------------------------------------------------------------------------------------------- Q
-    constexpr int CHUNKS = NR * (D / 8) / 64, BATCH = CHUNKS % 6 == 0 ? 6 : (CHUNKS % 4 == 0 ? 4 : 2);   // 8-element chunks per thread; loads in flight
-    static_assert(NR * (D / 8) % 64 == 0 && CHUNKS % BATCH == 0, "every chunk belongs to a row of the tile");
     const int qt = tid - 64;
     bool ok = true;
-    for (int qn = 0; c.valid && ok; ++qn) {
-      const int qb = qn % C::QBUF, use = qn / C::QBUF, live = c.nq * a.G - c.t * NR;
-      if (qt < NR) {
-        const int rr = c.t * NR + qt, tok = row_token(a, rr);
-        s_qat[qt] = (long long)(c.row0 + tok) * a.q.row + (long long)(c.hk * a.G + rr - tok * a.G) * a.q.head;
-      }
-      asm volatile("bar.sync 7, 64;" ::: "memory");
-      // K-major: row (part, r) of 64-element block ch at (part NR + r) * 128, its 16-byte chunk k at chunk k ^ (r & 7)
-#pragma unroll 1
-      for (int b0 = 0; b0 < CHUNKS; b0 += BATCH) {
-        float f[BATCH][8];
-#pragma unroll
-        for (int b = 0; b < BATCH; ++b) {
-          const int i = qt + (b0 + b) * 64, r = i / (D / 8), k8 = i - r * (D / 8);
-#pragma unroll
-          for (int j = 0; j < 8; ++j) f[b][j] = 0.f;
-          if (r < live) {
-            const long long at = s_qat[r] + k8 * 8;
-            if (PARTS == 3) {
-              const float* p = reinterpret_cast<const float*>(a.q.p) + at;
-              if (a.q_vec) {
-                const float4 x = *reinterpret_cast<const float4*>(p), y = *reinterpret_cast<const float4*>(p + 4);
-                f[b][0] = x.x; f[b][1] = x.y; f[b][2] = x.z; f[b][3] = x.w; f[b][4] = y.x; f[b][5] = y.y; f[b][6] = y.z; f[b][7] = y.w;
-              } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) f[b][j] = p[j];
-              }
-            } else {
-              const __nv_bfloat16* p = reinterpret_cast<const __nv_bfloat16*>(a.q.p) + at;
-              if (a.q_vec) {
-                const uint4 u = *reinterpret_cast<const uint4*>(p);
-                const uint32_t w[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-                for (int j = 0; j < 4; ++j) { f[b][2 * j] = p_lo(w[j]); f[b][2 * j + 1] = p_hi(w[j]); }
-              } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j) f[b][j] = __bfloat162float(p[j]);
-              }
-            }
-          }
-        }
-        if (b0 == 0 && use > 0) ok = p_wait(q_free + 8 * qb, (uint32_t)(use - 1) & 1u, a.wait_ns, a.s.status, s_abort);   // the first loads are under way
-        if (!ok) break;
-#pragma unroll
-        for (int b = 0; b < BATCH; ++b) {
-          const int i = qt + (b0 + b) * 64, r = i / (D / 8), k8 = i - r * (D / 8);
-          unsigned char* dst = mem + C::Q_AT + qb * C::Q_BYTES + (k8 >> 3) * (N * 128) + r * 128 + (((k8 & 7) ^ (r & 7)) << 4);
-#pragma unroll
-          for (int part = 0; part < PARTS; ++part) {
-            uint32_t u[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-              u[j] = p_pack(f[b][2 * j], f[b][2 * j + 1]);
-              if (part + 1 < PARTS) { f[b][2 * j] -= p_lo(u[j]); f[b][2 * j + 1] -= p_hi(u[j]); }
-            }
-            *reinterpret_cast<uint4*>(dst + part * (NR * 128)) = make_uint4(u[0], u[1], u[2], u[3]);
-          }
-        }
-      }
-      uint32_t both;   // (and s_qat may be written again)
-      asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.and.pred p, 7, 64, q;\n selp.u32 %0, 1, 0, p;\n}\n" : "=r"(both) : "r"(ok ? 1u : 0u) : "memory");
-      if (!both) break;
-      asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    if (c.valid) cursor_next<NR, TILE>(a, c, geo);   // the first part's are loaded by the softmax warps, which have nothing else to do yet
+    for (int qn = 1; c.valid && ok; ++qn) {
+      const int qb = qn % C::QBUF, use = qn / C::QBUF;
+      ok = load_q<D, NR, PARTS, 64>(a, c, mem + C::Q_AT + qb * C::Q_BYTES, s_qat, qt, 7,
+                                    [&]() { return use == 0 || p_wait(q_free + 8 * qb, (uint32_t)(use - 1) & 1u, a.wait_ns, a.s.status, s_abort); });
+      if (!ok) break;
       p_arrive(q_ready + 8 * qb);
       cursor_next<NR, TILE>(a, c, geo);
     }
@@ -279,6 +295,10 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
     int sn = 0, pn = 0, it = 0;
     auto all_sync = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(SOFT) : "memory"); };
     auto group_sync = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(3 + group) : "memory"); };
+    if (c.valid) {
+      ok = load_q<D, NR, PARTS, SOFT>(a, c, mem + C::Q_AT, s_qat + NR, st, 1, []() { return true; });
+      p_arrive(q_first);
+    }
     while (c.valid) {
       const int R = c.nq * a.G, r0 = c.t * NR, n = c.k1 - c.k0, first_lim = c.len - c.nq + row_token(a, r0);
       if (st < NR) {
@@ -288,6 +308,8 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
       }
       if (st == 0) *s_poison = 0x7fffffff;
       all_sync();
+      int first, parts;
+      item_ctas(c, first, parts);
       float l[16], o[16];
 #pragma unroll
       for (int j = 0; j < 16; ++j) l[j] = o[j] = 0.f;
@@ -452,8 +474,6 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
       const float sum = fold16<OpAdd>(l, lane);
       s_red[quarter * NR + col0 + (lane >> 1)] = sum;
       collect();
-      int first, parts;
-      item_ctas(c, first, parts);
       {
         uint32_t all;
         asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.and.pred p, 1, %2, q;\n selp.u32 %0, 1, 0, p;\n}\n"

@@ -36,7 +36,7 @@ template <int D> struct WCfg {
   static constexpr uint32_t Q_BYTES = W_ROWS * D * 2;
   static constexpr int STAGES = D == 128 ? 4 : 8;
   static constexpr uint32_t Q_AT = STAGES * HALF, HDR_AT = Q_AT + Q_BYTES;
-  static constexpr int JOIN_FLOATS = 1024;
+  static constexpr int JOIN_FLOATS = 2 * W_SOFT + 4 * W_ROWS;   // see join_parts
   static constexpr uint32_t HDR = 1024 + W_ROWS * (8 + 4 + 4) + JOIN_FLOATS * 4;
   static constexpr size_t SMEM = HDR_AT + HDR;
   // kind::f16 instruction descriptors: fp32 accumulator, bf16 x bf16, M = 128; S: both K-major, N = 128; O: B MN-major, N = d
