@@ -442,21 +442,39 @@ def sps_rotary_frequencies(rot_dim, base=10000.0, scaling="plain", factor=1.0, t
     return out
 
 
+class _Torch:
+    """What the calls below need of torch, looked up once (importing this module does not import torch)."""
+    codes = None
+
+    @classmethod
+    def load(cls):
+        import torch
+        cls.float64, cls.float32, cls.int32, cls.cuda_device = torch.float64, torch.float32, torch.int32, torch.cuda.device
+        cls.current_device, cls.raw_stream = torch._C._cuda_getDevice, torch._C._cuda_getCurrentRawStream
+        cls.codes = {torch.float32: 0, torch.bfloat16: 1}
+
+
 def _dtype_of(t):
-    name = str(t.dtype)
-    if name == "torch.float32":
-        return 0
-    if name == "torch.bfloat16":
-        return 1
-    raise ValueError("tensors are float32 or bfloat16, got %s" % name)
+    if _Torch.codes is None:
+        _Torch.load()
+    code = _Torch.codes.get(t.dtype)
+    if code is None:
+        raise ValueError("tensors are float32 or bfloat16, got %s" % t.dtype)
+    return code
 
 
-def _rows_of(t):
-    """A [rows, heads, d_head] tensor (any strides over contiguous heads) as an sps_rows."""
-    st = t.stride()
-    if len(st) != 3 or (st[2] != 1 and t.shape[2] > 1):
-        raise ValueError("rows are [rows, heads, d_head] with contiguous heads")
-    return sps_rows(t.data_ptr(), st[0], st[1], _dtype_of(t), t.shape[1])
+def _rows_of(t, index):
+    """A [rows, heads, d_head] tensor (any strides over contiguous heads) on device `index` as an sps_rows, and its shape."""
+    shape = t.shape
+    if len(shape) != 3 or t.get_device() != index:
+        raise ValueError("rows are [rows, heads, d_head] tensors, all on one CUDA device")
+    row, head, one = t.stride()
+    if one != 1 and shape[2] > 1:
+        raise ValueError("a head's elements must be contiguous")
+    code = _Torch.codes.get(t.dtype)
+    if code is None:
+        raise ValueError("tensors are float32 or bfloat16, got %s" % t.dtype)
+    return sps_rows(t.data_ptr(), row, head, code, shape[1]), shape
 
 
 class Rotary:
@@ -466,9 +484,11 @@ class Rotary:
     def __init__(self, freq, layout="pairs", gain=1.0):
         if layout not in ROTARY_LAYOUTS:
             raise ValueError("layout is one of %s" % ", ".join(ROTARY_LAYOUTS))
-        if str(freq.dtype) != "torch.float64" or freq.dim() != 1 or not freq.is_contiguous() or not freq.is_cuda:
+        if _Torch.codes is None:
+            _Torch.load()
+        if freq.dtype is not _Torch.float64 or freq.dim() != 1 or not freq.is_contiguous() or not freq.is_cuda:
             raise ValueError("freq is a contiguous CUDA float64 vector")
-        self.freq, self.layout, self.gain, self.device = freq, layout, float(gain), freq.device
+        self.freq, self.layout, self.gain, self.device, self.index = freq, layout, float(gain), freq.device, freq.get_device()
         self._c = sps_rotary_plan(freq.data_ptr(), 2 * freq.shape[0], ROTARY_LAYOUTS[layout], self.gain)
         self._p = C.addressof(self._c)
 
@@ -482,7 +502,8 @@ class PagedCache:
             raise ValueError("k and v are CUDA tensors [n_pages, n_kv_heads, page_size, d_head] of the same shape, strides and dtype")
         if k.stride(3) != 1:
             raise ValueError("a slot's d_head elements must be contiguous")
-        self.k, self.v, self.device = k, v, k.device
+        self.k, self.v, self.device, self.index = k, v, k.device, k.get_device()
+        self.d_head = k.shape[3]
         self._c = sps_paged_cache(k.data_ptr(), v.data_ptr(), k.stride(0), k.stride(1), k.stride(2), _dtype_of(k), k.shape[0], k.shape[2],
                                   k.shape[1], k.shape[3])
         self._p = C.addressof(self._c)
@@ -509,48 +530,54 @@ class PagedBatch:
             status = torch.zeros(1, dtype=torch.int32, device=q_start.device)
         if status.dtype != torch.int32 or status.numel() < 1 or status.device != q_start.device:
             raise ValueError("status is a CUDA int32 tensor of one element")
-        self.q_start, self.kv_len, self.pages, self.status, self.device = q_start, kv_len, pages, status, q_start.device
+        self.q_start, self.kv_len, self.pages, self.status = q_start, kv_len, pages, status
+        self.device, self.index = q_start.device, q_start.get_device()
         self._c = sps_paged_batch(q_start.data_ptr(), kv_len.data_ptr(), pages.data_ptr(), status.data_ptr(), B, pages.shape[1], int(max_q))
         self._p = C.addressof(self._c)
 
 
-def _on(device, fn, stream, *args):
-    """fn(*args, stream) with `device` current, on `stream` or that device's current one."""
-    import torch
-    if torch.cuda.current_device() == device.index:
-        _check(fn(*args, torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream))
+def _on(index, fn, stream, *args):
+    """fn(*args, stream) with device `index` current, on `stream` or that device's current one."""
+    if _Torch.current_device() == index:
+        rc = fn(*args, _Torch.raw_stream(index) if stream is None else stream)
     else:
-        with torch.cuda.device(device):
-            _check(fn(*args, torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream))
-
-
-def _same_device(device, *tensors):
-    for t in tensors:
-        if t is not None and t.device != device:
-            raise ValueError("all tensors must be on one CUDA device")
+        with _Torch.cuda_device(index):
+            rc = fn(*args, _Torch.raw_stream(index) if stream is None else stream)
+    if rc:
+        _check(rc)
 
 
 def sps_rotary(x, y, positions, plan, transposed=False, stream=None):
     """y = gain R(positions) x over the plan's rotated elements, the others copied; x, y CUDA [rows, heads, d_head], fp32 or
     bf16 (y may be x); positions CUDA int32 [rows].  transposed: gain R^T, the gradient."""
-    _same_device(plan.device, x, y, positions)
-    if x.shape != y.shape or positions.shape != x.shape[:1] or not positions.is_contiguous() or str(positions.dtype) != "torch.int32":
-        raise ValueError("x and y [rows, heads, d_head], positions contiguous int32 [rows]")
-    _on(plan.device, lib().sps_rotary, stream, plan._p, C.byref(_rows_of(x)), C.byref(_rows_of(y)), x.shape[0], x.shape[2],
-        positions.data_ptr(), 1 if transposed else 0)
+    rx, shape = _rows_of(x, plan.index)
+    ry, other = _rows_of(y, plan.index)
+    if shape != other or positions.dtype is not _Torch.int32 or positions.dim() != 1 or positions.numel() != shape[0] or \
+            not positions.is_contiguous() or positions.get_device() != plan.index:
+        raise ValueError("x and y [rows, heads, d_head], positions contiguous int32 [rows], all on one CUDA device")
+    _on(plan.index, lib().sps_rotary, stream, plan._p, C.byref(rx), C.byref(ry), shape[0], shape[2], positions.data_ptr(), 1 if transposed else 0)
 
 
 def sps_paged_append(cache, batch, k, v, plan=None, q=None, q_out=None, stream=None):
     """Keys (rotated under `plan`) and values of the batch's rows into their slots; with q, its rotated rows into q_out.
     k, v CUDA [rows, n_kv_heads, d_head]; q, q_out CUDA [rows, heads, d_head]."""
-    _same_device(cache.device, batch, k, v, plan, q, q_out)
-    if k.shape != v.shape or k.dim() != 3 or k.shape[2] != cache.k.shape[3]:
+    index = cache.index
+    rk, shape = _rows_of(k, index)
+    rv, other = _rows_of(v, index)
+    if shape != other or shape[2] != cache.d_head:
         raise ValueError("k and v are [rows, n_kv_heads, d_head]")
-    if (q is None) != (q_out is None) or (q is not None and (q.shape != q_out.shape or q.shape[0] != k.shape[0] or q.shape[2] != k.shape[2])):
-        raise ValueError("q and q_out go together and are [rows, heads, d_head]")
-    _on(cache.device, lib().sps_paged_append, stream, cache._p, batch._p, plan._p if plan is not None else None, k.shape[0],
-        C.byref(_rows_of(k)), C.byref(_rows_of(v)), C.byref(_rows_of(q)) if q is not None else None,
-        C.byref(_rows_of(q_out)) if q is not None else None)
+    if batch.index != index or (plan is not None and plan.index != index):
+        raise ValueError("all tensors must be on one CUDA device")
+    rq = ro = None
+    if q is not None and q_out is not None:
+        rq, qs = _rows_of(q, index)
+        ro, other = _rows_of(q_out, index)
+        if qs != other or qs[0] != shape[0] or qs[2] != shape[2]:
+            raise ValueError("q and q_out are [rows, heads, d_head]")
+        rq, ro = C.byref(rq), C.byref(ro)
+    elif q is not None or q_out is not None:
+        raise ValueError("q and q_out go together")
+    _on(index, lib().sps_paged_append, stream, cache._p, batch._p, plan._p if plan is not None else None, shape[0], C.byref(rk), C.byref(rv), rq, ro)
 
 
 def sps_paged_attention_workspace_bytes(cache, n_heads, q_dtype):
@@ -564,13 +591,18 @@ def sps_paged_attention_workspace_bytes(cache, n_heads, q_dtype):
 def sps_paged_attention(cache, batch, q, out, workspace, scale=0.0, lse=None, stream=None):
     """Causal attention of the batch's rows over their sequences' pages.  q, out CUDA [rows, heads, d_head]; workspace CUDA
     uint8 (zeroed once) of sps_paged_attention_workspace_bytes; scale 0 = 1 / sqrt(d_head); lse CUDA float32 [rows, heads]."""
-    _same_device(cache.device, batch, q, out, workspace, lse)
-    if q.shape != out.shape or q.dim() != 3 or q.shape[2] != cache.k.shape[3]:
+    index = cache.index
+    rq, shape = _rows_of(q, index)
+    ro, other = _rows_of(out, index)
+    if shape != other or shape[2] != cache.d_head:
         raise ValueError("q and out are [rows, heads, d_head]")
-    if lse is not None and (lse.shape != q.shape[:2] or not lse.is_contiguous() or str(lse.dtype) != "torch.float32"):
-        raise ValueError("lse is contiguous float32 [rows, heads]")
-    need = lib().sps_paged_attention_workspace_bytes(cache._p, q.shape[1], _dtype_of(q))
-    if workspace.numel() * workspace.element_size() < need:
+    if batch.index != index or workspace.get_device() != index:
+        raise ValueError("all tensors must be on one CUDA device")
+    lse_p = None
+    if lse is not None:
+        if lse.shape != shape[:2] or not lse.is_contiguous() or lse.get_device() != index or lse.dtype is not _Torch.float32:
+            raise ValueError("lse is contiguous float32 [rows, heads] on the same device")
+        lse_p = lse.data_ptr()
+    if workspace.nbytes < lib().sps_paged_attention_workspace_bytes(cache._p, shape[1], rq.dtype):
         raise ValueError("workspace smaller than sps_paged_attention_workspace_bytes")
-    _on(cache.device, lib().sps_paged_attention, stream, cache._p, batch._p, q.shape[0], C.byref(_rows_of(q)), C.byref(_rows_of(out)), scale,
-        lse.data_ptr() if lse is not None else None, workspace.data_ptr())
+    _on(index, lib().sps_paged_attention, stream, cache._p, batch._p, shape[0], C.byref(rq), C.byref(ro), scale, lse_p, workspace.data_ptr())
