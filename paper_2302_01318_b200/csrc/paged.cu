@@ -11,9 +11,10 @@
 //
 // Bound by HBM: every element is read once and written once, 6 operations per pair.  The angles would not be cheap per
 // element -- a 64-bit product and reduction and a sine and cosine each --, so a CTA works them out once per row, shares
-// them through shared memory, and rotates many heads of that row by them.  A unit is 16 bytes of x, two of them in the
-// halves layout (both halves of its pairs; two 16-byte pieces where nothing is rotated); a thread keeps its place in the
+// them through shared memory, and rotates many heads of that row by them.  A unit is two 16-byte pieces of x half a head
+// apart -- in the halves layout both halves of its pairs, apart by half the rotated part --; a thread keeps its place in the
 // head and goes from head to head, 64 bytes of loads in flight, through queries, keys and values and the rows of its CTA.
+// What a unit costs beside its bytes (where it is, what is done to it) counts: one piece to a unit took a tenth longer.
 // The first units are on their way before positions, page table and angles are looked at; what is left of that latency
 // hides behind the SM's other CTAs.
 // E = elements per access: 16 bytes of x when addresses, strides and the rotated part allow, else single elements.
@@ -36,10 +37,32 @@ template <> struct Elem<__nv_bfloat16> {
 
 template <typename T, int E> struct alignas(sizeof(T) * E) Pack { T v[E]; };
 template <typename T, int E> __device__ __forceinline__ Pack<T, E> load_e(const T* p) { return *reinterpret_cast<const Pack<T, E>*>(p); }
+// (pairs of bf16 in one instruction each way: element by element their conversions, not HBM, bound the kernel)
+template <typename T, int E> __device__ __forceinline__ void unpack(const Pack<T, E>& k, float (&f)[E]) {
+  if constexpr (sizeof(T) == 2 && E % 2 == 0) {
+#pragma unroll
+    for (int i = 0; i < E; i += 2) {
+      const uint32_t u = reinterpret_cast<const uint32_t*>(&k)[i / 2];
+      f[i] = __uint_as_float(u << 16);
+      f[i + 1] = __uint_as_float(u & 0xffff0000u);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; ++i) f[i] = Elem<T>::get(k.v[i]);
+  }
+}
 template <typename T, int E> __device__ __forceinline__ void store_e(T* p, const float (&f)[E]) {
   Pack<T, E> k;
+  if constexpr (sizeof(T) == 2 && E % 2 == 0) {
 #pragma unroll
-  for (int i = 0; i < E; ++i) k.v[i] = Elem<T>::put(f[i]);
+    for (int i = 0; i < E; i += 2) {
+      const __nv_bfloat162 h = __floats2bfloat162_rn(f[i], f[i + 1]);
+      reinterpret_cast<uint32_t*>(&k)[i / 2] = *reinterpret_cast<const uint32_t*>(&h);
+    }
+  } else {
+#pragma unroll
+    for (int i = 0; i < E; ++i) k.v[i] = Elem<T>::put(f[i]);
+  }
   *reinterpret_cast<Pack<T, E>*>(p) = k;
 }
 
@@ -88,7 +111,7 @@ __device__ __forceinline__ void row_places(const RotaryArgs& a, int row0, int nr
   }
 }
 
-// the turns of the CTA's rows; pair k of a row at (k % PU) units + k / PU, PU pairs to a unit: neighbouring units read
+// the turns of the CTA's rows; pair k of a row at (k % PU) (hr / PU) + k / PU, PU pairs to a piece: neighbouring pieces read
 // neighbouring words
 template <int PU>
 __device__ __forceinline__ void row_turns(const RotaryArgs& a, int nr, const int* s_pos, float2* s_turn) {
@@ -110,10 +133,9 @@ __global__ void __launch_bounds__(ROT_THREADS, 4) rotary_kernel(const __grid_con
   extern __shared__ float2 s_turn[];                 // [rows_per_cta][rot / 2]
   __shared__ int s_pos[ROT_MAX_ROWS];
   __shared__ long long s_slot[ROT_MAX_ROWS];
-  constexpr bool TWO = HALVES || E == 1;             // two accesses to a unit
-  constexpr int PU = HALVES ? E : (E == 1 ? 1 : E / 2);   // pairs of a rotated unit
+  constexpr int PU = HALVES ? E : (E == 1 ? 1 : E / 2);   // pairs of a rotated unit (halves, single pair) or piece (pairs)
   const int tid = threadIdx.x, hr = a.rot >> 1, uh = a.uh;
-  const int rot_units = a.freq ? hr / PU : 0;        // of a head's units: the rotated ones
+  const int rot_units = a.freq ? hr / PU : 0;        // of a head's units, or pieces: the rotated ones
   const int row0 = blockIdx.x * a.rows_per_cta, nr = min(a.rows_per_cta, a.rows - row0);
   const int h_lo = blockIdx.y * a.heads_per_cta, span = min(a.heads_per_cta, a.vheads - h_lo);   // this CTA's heads of each row
   const int all = nr * span;                         // (row, head) pairs
@@ -123,31 +145,38 @@ __global__ void __launch_bounds__(ROT_THREADS, 4) rotary_kernel(const __grid_con
   pdl_wait();
   bool ready = false;
   for (int w = tid - slice * uh; w < uh; w += ROT_THREADS) {   // (once, unless a head has more units than the CTA threads)
-    const bool turned = w < rot_units;
-    int e0, e1 = 0;                                  // the unit's elements
+    const bool turned = w < rot_units, turned1 = !HALVES && E > 1 && w + uh < rot_units;   // (turned1: the second piece)
+    int e0, e1;                                      // the unit's pieces
     if (HALVES) {
       e0 = turned ? w * E : a.flat0 + (w - rot_units) * E;
       e1 = e0 + (turned ? hr : a.flat_half);
-    } else {
-      e0 = w * (E == 1 ? 2 : E);
+    } else if (E == 1) {
+      e0 = 2 * w;
       e1 = e0 + 1;
+    } else {
+      e0 = w * E;
+      e1 = e0 + uh * E;
     }
     for (int i0 = slice; i0 - slice < all; i0 += a.per_pass * UPT) {
       Pack<TX, E> lo[UPT], hi[UPT];
-      int rr[UPT], vh[UPT];                          // row of the CTA (-1: none) and head among queries, keys and values
+      int rr[UPT], kind[UPT], head[UPT];             // row of the CTA (-1: none); 0 queries, 1 keys, 2 values; head of them
 #pragma unroll
       for (int j = 0; j < UPT; ++j) {
         const int i = i0 + j * a.per_pass;
         rr[j] = -1;
         if (i >= all || !active) continue;
         rr[j] = a.rows_per_cta == 1 ? 0 : magic_div(i, a.span_magic);   // several rows: the CTA has all of their heads
-        vh[j] = h_lo + i - rr[j] * span;
-        const int kind = vh[j] < a.heads[0] ? 0 : (vh[j] < a.heads[0] + a.heads[1] ? 1 : 2);
-        const int h = vh[j] - (kind > 0 ? a.heads[0] : 0) - (kind > 1 ? a.heads[1] : 0);
-        const RowsView& x = a.x[kind];
-        const TX* src = reinterpret_cast<const TX*>(x.p) + (long long)(row0 + rr[j]) * x.row + (long long)h * x.head;
+        head[j] = h_lo + i - rr[j] * span;
+        kind[j] = 0;
+        if (head[j] >= a.heads[0]) {
+          head[j] -= a.heads[0];
+          kind[j] = 1;
+          if (head[j] >= a.heads[1]) { head[j] -= a.heads[1]; kind[j] = 2; }
+        }
+        const RowsView& x = a.x[kind[j]];
+        const TX* src = reinterpret_cast<const TX*>(x.p) + (long long)(row0 + rr[j]) * x.row + (long long)head[j] * x.head;
         lo[j] = load_e<TX, E>(src + e0);
-        if constexpr (TWO) hi[j] = load_e<TX, E>(src + e1);
+        hi[j] = load_e<TX, E>(src + e1);
       }
       if (!ready) {
         ready = true;
@@ -163,42 +192,42 @@ __global__ void __launch_bounds__(ROT_THREADS, 4) rotary_kernel(const __grid_con
         if (rr[j] < 0) continue;
         const long long slot = s_slot[rr[j]];
         if (slot < 0) continue;
-        const int kind = vh[j] < a.heads[0] ? 0 : (vh[j] < a.heads[0] + a.heads[1] ? 1 : 2);
-        const int h = vh[j] - (kind > 0 ? a.heads[0] : 0) - (kind > 1 ? a.heads[1] : 0);
         float f[E], g[E];
-#pragma unroll
-        for (int q = 0; q < E; ++q) f[q] = Elem<TX>::get(lo[j].v[q]);
-        if constexpr (TWO) {
-#pragma unroll
-          for (int q = 0; q < E; ++q) g[q] = Elem<TX>::get(hi[j].v[q]);
-        }
-        if (turned && kind < 2) {
+        unpack<TX, E>(lo[j], f);
+        unpack<TX, E>(hi[j], g);
+        if (kind[j] < 2) {
           const float2* tr = s_turn + rr[j] * hr + w;
-          if constexpr (TWO) {
+          if constexpr (HALVES || E == 1) {
+            if (turned) {
 #pragma unroll
-            for (int q = 0; q < E; ++q) {
-              const float2 t = tr[q * rot_units];
-              const float p = f[q], s = g[q];
-              f[q] = p * t.x - s * t.y;
-              g[q] = p * t.y + s * t.x;
+              for (int q = 0; q < E; ++q) {
+                const float2 t = tr[q * rot_units];
+                const float p = f[q], s = g[q];
+                f[q] = p * t.x - s * t.y;
+                g[q] = p * t.y + s * t.x;
+              }
             }
           } else {
+            auto turn_piece = [&](float (&v)[E], const float2* at) {
 #pragma unroll
-            for (int q = 0; q < E; q += 2) {
-              const float2 t = tr[(q >> 1) * rot_units];
-              const float p = f[q], s = f[q + 1];
-              f[q] = p * t.x - s * t.y;
-              f[q + 1] = p * t.y + s * t.x;
-            }
+              for (int q = 0; q < E; q += 2) {
+                const float2 t = at[(q >> 1) * rot_units];
+                const float p = v[q], s = v[q + 1];
+                v[q] = p * t.x - s * t.y;
+                v[q + 1] = p * t.y + s * t.x;
+              }
+            };
+            if (turned) turn_piece(f, tr);
+            if (turned1) turn_piece(g, tr + uh);
           }
         }
         auto put = [&](auto* dst) {
           using T = typename std::remove_reference<decltype(*dst)>::type;
           store_e<T, E>(dst + e0, f);
-          if constexpr (TWO) store_e<T, E>(dst + e1, g);
+          store_e<T, E>(dst + e1, g);
         };
-        if (kind == 0) put(reinterpret_cast<TQ*>(a.y[0].p) + (long long)(row0 + rr[j]) * a.y[0].row + (long long)h * a.y[0].head);
-        else put(reinterpret_cast<TC*>(a.y[kind].p) + slot + (long long)h * a.y[kind].head);
+        if (kind[j] == 0) put(reinterpret_cast<TQ*>(a.y[0].p) + (long long)(row0 + rr[j]) * a.y[0].row + (long long)head[j] * a.y[0].head);
+        else put(reinterpret_cast<TC*>(a.y[kind[j]].p) + slot + (long long)head[j] * a.y[kind[j]].head);
       }
     }
   }
@@ -228,8 +257,8 @@ cudaError_t rotary_cut(RotaryArgs& a, int num_sm, cudaStream_t st) {
 
 template <typename TX, typename TQ, typename TC, int E, bool HALVES>
 cudaError_t rotary_go(RotaryArgs& a, int num_sm, cudaStream_t st) {
-  constexpr int UPT = HALVES ? 2 : 4;
-  a.uh = HALVES || E == 1 ? a.d_head / (2 * E) : a.d_head / E;
+  constexpr int UPT = 2;
+  a.uh = a.d_head / (2 * E);
   a.uh_magic = magic_of(a.uh);
   a.flat0 = a.freq ? a.rot : 0;
   a.flat_half = (a.d_head - a.flat0) / 2;
@@ -247,8 +276,8 @@ bool aligned(const RowsView& v, int heads, int bytes, int esize) {
 template <typename TX, typename TQ, typename TC>
 cudaError_t rotary_types(RotaryArgs& a, int num_sm, cudaStream_t st) {
   constexpr int E = 16 / (int)sizeof(TX);
-  const int whole = a.halves ? 2 * E : E;   // a head and its rotated part must be whole units
-  bool vec = a.d_head % whole == 0 && (!a.freq || a.rot % whole == 0);
+  // a head must be whole units, its rotated part whole units (halves) or pieces (pairs)
+  bool vec = a.d_head % (2 * E) == 0 && (!a.freq || a.rot % (a.halves ? 2 * E : E) == 0);
   for (int i = 0; i < 3 && vec; ++i) {
     if (!a.heads[i]) continue;
     vec = vec && aligned(a.x[i], a.heads[i], 16, (int)sizeof(TX));
