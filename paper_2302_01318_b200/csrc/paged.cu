@@ -453,14 +453,15 @@ static const char* bad_heads(const sps_paged_cache* c, int n_heads, int q_dtype)
   return nullptr;
 }
 
-// workspace: the arrival counters of up to PAGED_MAX_CTAS CTAs, then two part slots each
+// workspace: arrival counters and records of up to 1024 CTAs, then two part slots for each CTA
 #define PAGED_COUNTER_BYTES 4096
+#define PAGED_RECORD_BYTES (1024 * sizeof(PartRecord))
 
 int64_t sps_paged_attention_workspace_bytes(const sps_paged_cache* cache, int32_t n_heads, int32_t q_dtype) {
   const char* why = bad_cache(cache);
   if (!why) why = bad_heads(cache, n_heads, q_dtype);
   if (why) { no(SPS_EINVAL, why); return -1; }
-  return PAGED_COUNTER_BYTES + (int64_t)2 * paged_attn_grid(sms()) * (int64_t)paged_attn_slot_bytes(cache->dtype, q_dtype, cache->d_head);
+  return (int64_t)(PAGED_COUNTER_BYTES + PAGED_RECORD_BYTES) + (int64_t)2 * paged_attn_grid(sms()) * (int64_t)paged_attn_slot_bytes(cache->dtype, q_dtype, cache->d_head);
 }
 
 int sps_paged_attention(const sps_paged_cache* cache, const sps_paged_batch* batch, int32_t rows, const sps_rows* q, const sps_rows* out,
@@ -491,7 +492,8 @@ int sps_paged_attention(const sps_paged_cache* cache, const sps_paged_batch* bat
   a.scale_log2 = (scale == 0.f ? 1.f / std::sqrt((float)cache->d_head) : scale) * 1.4426950408889634f;
   a.lse = lse;
   a.counters = (int*)workspace;
-  a.slots = (float*)((char*)workspace + PAGED_COUNTER_BYTES);
+  a.records = (PartRecord*)((char*)workspace + PAGED_COUNTER_BYTES);
+  a.slots = (float*)((char*)workspace + PAGED_COUNTER_BYTES + PAGED_RECORD_BYTES);
   a.wait_ns = sps_wait_knobs().limit_ns;
   const cudaError_t e = paged_attn_launch(a, cache->dtype, cache->d_head, batch->max_q, sms(), (cudaStream_t)stream);
   return e == cudaSuccess ? SPS_OK : no(SPS_ECUDA, cudaGetErrorString(e));

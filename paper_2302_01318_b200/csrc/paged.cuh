@@ -49,6 +49,9 @@ __device__ __forceinline__ SeqGeom paged_seq(const PagedSeqs& s, int b) {
 // (maximum, sum, unnormalised output) in its slot; the last CTA of the item to finish joins the parts in their order, so
 // results do not depend on timing.
 // ------------------------------------------------------------------------------------------------------------------
+// an item cut into parts, left for the join by the CTA that has its first part
+struct PartRecord { int row0, nq, hk, t, first, parts; };
+
 struct PagedAttnArgs {
   PagedSeqs s;
   RowsView q, out;
@@ -60,6 +63,7 @@ struct PagedAttnArgs {
   float scale_log2;         // scale * log2(e): scores are kept in base 2
   float* lse;               // [rows][H] or null
   int* counters;            // [grid] arrivals at an item, by the first CTA that works on it; zero between launches
+  PartRecord* records;      // [grid] (kernels whose parts another kernel joins)
   int lead, min_run;        // set by the launcher: an item's cost ahead of its tiles, the least run, in tiles
   float* slots;             // [2 * grid] parts: [NR] maxima, [NR] sums, [NR][d_head] outputs
   unsigned long long wait_ns;
@@ -269,19 +273,18 @@ __device__ __forceinline__ void store_out(const PagedAttnArgs& a, long long at, 
 // threads of the last CTA to arrive (named barrier 2 is theirs).  A part's slot is a trip to L2 away, so many loads are in
 // flight at once: every thread first asks for its four-element pieces of the first AHEAD parts' outputs, then for maxima and
 // sums (THREADS / NR threads to a row), and goes on four parts at a time, their weights in shared memory.  s_max, s_inv: shared
-// scratch of NR floats each; w: of w_floats >= 2 * THREADS + 2 * NR.  A part's outputs lie row by row, or (BY_PIECE) piece by
-// piece: piece k (four elements) of row r at k * NR + r, for a kernel whose threads own rows.
-template <int NR, int D, int THREADS, bool BY_PIECE = false>
+// scratch of NR floats each; w: of w_floats >= 2 * THREADS + 2 * NR. 
+template <int NR, int D, int THREADS>
 __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCursor& c, int first, int parts, int tid, float* s_max, float* s_inv, float* w, int w_floats) {
   const int R = c.nq * a.G, r0 = c.t * NR, live = min(NR, R - r0);
   constexpr size_t SF = slot_floats<NR, D>();
-  constexpr int LANES = THREADS / NR, PIECES = NR * (D / 4) / THREADS, BLOCK = PIECES < 4 ? PIECES : 4, AHEAD = BY_PIECE ? 2 : 4;
+  constexpr int LANES = THREADS / NR, PIECES = NR * (D / 4) / THREADS, BLOCK = PIECES < 4 ? PIECES : 4, AHEAD = 4;
   float* pair = w + w_floats - 2 * THREADS;                    // (maximum, sum) by thread; ahead of it the table of weights
   const int table = (w_floats - 2 * THREADS) / NR;             // parts whose weights fit at once
   const float* slots = a.slots + SF * (size_t)(2 * first);
   auto slot = [&](int p) { return slots + SF * (size_t)(p == 0 ? 1 : 2 * p); };   // part 0 begins in its CTA: part_slot
   auto sync = [&]() { asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory"); };
-  auto row = [&](int i) { return BY_PIECE ? i % NR : i / (D / 4); };
+  auto row = [&](int i) { return i / (D / 4); };
   auto fetch = [&](int p, int i) { return __ldcg(reinterpret_cast<const float4*>(slot(p) + 2 * NR) + i); };
   float4 early[AHEAD][BLOCK];
 #pragma unroll
@@ -361,7 +364,7 @@ __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCur
     for (int k = 0; k < BLOCK; ++k) {
       const int i = tid + (kb + k) * THREADS, r = row(i);
       if (r < live) {
-        const int e = (BY_PIECE ? i / NR : i - r * (D / 4)) * 4, rr = r0 + r, tok = row_token(a, rr);
+        const int e = (i - r * (D / 4)) * 4, rr = r0 + r, tok = row_token(a, rr);
         const long long at = (long long)(c.row0 + tok) * a.out.row + (long long)(c.hk * a.G + rr - tok * a.G) * a.out.head + e;
         store_out(a, at, o[k].x); store_out(a, at + 1, o[k].y); store_out(a, at + 2, o[k].z); store_out(a, at + 3, o[k].w);
       }

@@ -11,18 +11,18 @@
 // all its rows' scores; it masks, exponentiates and stores its row of P^T.
 //
 // Running maximum.  The weights are 2^(s - m) with m fixed at the score of the part's first token, which every row that sees
-// anything of the part sees: P is bf16 (8 exponent bits) or three bf16 parts of an fp32 number, sums are fp32, so m only
-// has to keep the weights in range, not at most 1, and a weight of 1 is among them.  Only when a score exceeds m by
-// MAX_UP (in base 2) do the threads of a column group agree (a reducing barrier) to take the new maximum and
-// rescale what they hold.  That leaves a multiply-add, an exponential, an addition and the rounding per score, no
+// anything of the part sees: P is bf16 parts (8 exponent bits) of an fp32 number, sums are fp32, so m only has to keep the
+// weights in range, not at most 1, and a weight of 1 is among them.  Only when a score exceeds m by MAX_UP (in base 2) do
+// the threads of a column group agree (a reducing barrier) to take the new maximum and rescale what they hold.  That leaves a multiply-add, an exponential, an addition and the rounding per score, no
 // cross-lane reduction per tile.  Sums stay per thread (its token of every tile) until the part ends.  Each tile's O^T
 // is a product of its own, added to fp32 registers: the tensor cores cut the low bits of a running sum instead of rounding
 // them, which over a context of 32 768 tokens cost 3.6e-5 of the result.
 //
-// Types.  bf16 queries: P rounds once to bf16 (2^-8 relative, and the sum is taken of the rounded weights).  fp32 queries:
-// Q and P enter as three bf16 parts (high, rest, rest of the rest: 24 bits), side by side as columns of one product -- a
-// product reads its 128-row operand in 32 clocks however few its columns, 16 columns cost 39 and 48 cost 44 -- and the
-// three columns of a row are added in fp32.
+// Types.  bf16 queries: P enters as two bf16 parts (high, rest: 2^-17 relative), so that the output's own rounding is the
+// only one of its size; here, bound by HBM, the second part costs nothing.  fp32 queries: Q and P enter as three bf16 parts
+// (high, rest, rest of the rest: 24 bits).  Parts lie side by side as columns of one product -- a product reads its
+// 128-row operand in 32 clocks however few its columns: 16 columns cost 39 and 48 cost 44 -- and a row's columns are added
+// in fp32.
 //
 // What bounds it: HBM.  A tile of 128 tokens is 64 KB of keys and values (d = 128), 2760 clocks of an SM's share of
 // 6.5 TB/s; its 16 products take 39 to 72 clocks each, the softmax a few hundred.  One CTA per SM, equal runs of tiles per
@@ -61,13 +61,14 @@ template <class Op> __device__ __forceinline__ float fold16(float (&v)[16], int 
   return Op::f(v[0], __shfl_xor_sync(0xffffffffu, v[0], 1));
 }
 
-template <int D, int NR, int PARTS> struct Cfg {
+template <int D, int NR, int PARTS> struct Cfg {   // PARTS: of Q (1 or 3)
+  static constexpr int PP = PARTS == 3 ? 3 : 2;                     // parts of P
   static constexpr int GROUPS = NR / 16;                            // column groups of four softmax warps each
   static constexpr int SOFT = 128 * GROUPS;                         // softmax threads
   static constexpr int THREADS = 128 + SOFT;
-  static constexpr int N = PARTS * NR;                              // columns of a product
+  static constexpr int N = PARTS * NR, NO = PP * NR;                // columns of S and O
   static constexpr uint32_t HALF = TILE * D * 2;                    // keys or values of a tile
-  static constexpr uint32_t Q_BYTES = N * D * 2, P_BYTES = TILE * N * 2;
+  static constexpr uint32_t Q_BYTES = N * D * 2, P_BYTES = TILE * NO * 2;
   static constexpr uint32_t HDR = 4224;                             // barriers, small per-row arrays
   static constexpr int BUDGET = 232448 - (int)HDR - (int)P_BYTES;
   static constexpr int QBUF = (BUDGET - 2 * (int)Q_BYTES) / (int)HALF >= 4 ? 2 : 1;
@@ -75,13 +76,14 @@ template <int D, int NR, int PARTS> struct Cfg {
   static constexpr int STAGES = STAGES_FIT > 8 ? 8 : STAGES_FIT;
   static constexpr uint32_t Q_AT = STAGES * HALF, P_AT = Q_AT + QBUF * Q_BYTES, HDR_AT = P_AT + P_BYTES;
   static constexpr size_t SMEM = HDR_AT + HDR;
-  static constexpr uint32_t TMEM = 3 * N <= 64 ? 64 : (3 * N <= 128 ? 128 : (3 * N <= 256 ? 256 : 512));   // S twice, O once
+  static constexpr int COLUMNS = 2 * N + NO;                        // of tensor memory: S twice, O once
+  static constexpr uint32_t TMEM = COLUMNS <= 64 ? 64 : (COLUMNS <= 128 ? 128 : (COLUMNS <= 256 ? 256 : 512));
   // P^T is the B operand of O, MN-major under the 32-byte swizzle: blocks of 16 columns x 128 tokens, 32 bytes per token
   static constexpr uint32_t P_BLOCK = TILE * 32;
   // kind::f16 instruction descriptors: fp32 accumulator, bf16 x bf16; S: both K-major, M = 128; O: both MN-major, M = d
   static constexpr uint32_t IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(TILE >> 4) << 24);
-  static constexpr uint32_t IDESC_O = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(N >> 3) << 17) | ((uint32_t)(D >> 4) << 24);
-  static_assert(STAGES >= 4 && 3 * N <= 512 && N <= 256, "shape");
+  static constexpr uint32_t IDESC_O = (1u << 4) | (1u << 7) | (1u << 10) | (1u << 15) | (1u << 16) | ((uint32_t)(NO >> 3) << 17) | ((uint32_t)(D >> 4) << 24);
+  static_assert(STAGES >= 4 && COLUMNS <= 512 && NO <= 256 && N % 16 == 0, "shape");
 };
 
 // Q of the cursor's item into shared memory, in PARTS bf16 parts, by THREADS threads (named barrier `bar` is theirs): K-major,
@@ -159,7 +161,7 @@ __device__ __forceinline__ bool load_q(const PagedAttnArgs& a, const WorkCursor&
 template <int D, int NR, int PARTS>
 __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_kernel(const __grid_constant__ TcArgs ta) {
   using C = Cfg<D, NR, PARTS>;
-  constexpr int SOFT = C::SOFT, STAGES = C::STAGES, N = C::N;
+  constexpr int SOFT = C::SOFT, STAGES = C::STAGES, N = C::N, PP = C::PP;
   extern __shared__ __align__(1024) unsigned char mem[];   // the ring, Q, P^T (swizzled operands: 1024-byte aligned), header
   const PagedAttnArgs& a = ta.a;
   const uint32_t ring = p_smem(mem), hb = ring + C::HDR_AT;
@@ -321,16 +323,14 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
         ok = ok && p_wait(pv_done, (uint32_t)(pn - 1) & 1u, a.wait_ns, a.s.status, s_abort);
         __syncwarp();
         P_FENCE_AFTER();
-        float t[PARTS][16];
+        float t[PP][16];
 #pragma unroll
-        for (int part = 0; part < PARTS; ++part) p_ld16(tmem_o + t_lane + part * NR + col0, t[part]);
+        for (int part = 0; part < PP; ++part) p_ld16(tmem_o + t_lane + part * NR + col0, t[part]);
         P_WAIT_LD();
 #pragma unroll
         for (int j = 0; j < 16; j += 2) {
-          if (PARTS == 3) {
-            p_add2(t[PARTS / 2][j], t[PARTS / 2][j + 1], t[PARTS - 1][j], t[PARTS - 1][j + 1]);
-            p_add2(t[0][j], t[0][j + 1], t[PARTS / 2][j], t[PARTS / 2][j + 1]);
-          }
+          if (PP == 3) p_add2(t[1][j], t[1][j + 1], t[PP - 1][j], t[PP - 1][j + 1]);
+          p_add2(t[0][j], t[0][j + 1], t[1][j], t[1][j + 1]);
           p_add2(o[j], o[j + 1], t[0][j], t[0][j + 1]);
         }
       };
@@ -413,10 +413,8 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
         // ---- weights
 #pragma unroll
         for (int j = 0; j < 16; ++j) x[j] = p_ex2(x[j]);
-        if (PARTS == 3) {
 #pragma unroll
-          for (int j = 0; j < 16; j += 2) p_add2(l[j], l[j + 1], x[j], x[j + 1]);
-        }
+        for (int j = 0; j < 16; j += 2) p_add2(l[j], l[j + 1], x[j], x[j + 1]);
         // P^T is written once the previous output product has read it
         if (i > 0) collect();
         if (edge) {
@@ -452,14 +450,13 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
 #pragma unroll
-          for (int part = 0; part < PARTS; ++part) {
+          for (int part = 0; part < PP; ++part) {
             uint32_t u[4];
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
               float &f0 = x[8 * k + 2 * j], &f1 = x[8 * k + 2 * j + 1];
               u[j] = p_pack(f0, f1);
-              if (PARTS == 1) p_add2(l[8 * k + 2 * j], l[8 * k + 2 * j + 1], p_lo(u[j]), p_hi(u[j]));
-              if (part + 1 < PARTS) p_add2(f0, f1, -p_lo(u[j]), -p_hi(u[j]));
+              if (part + 1 < PP) p_add2(f0, f1, -p_lo(u[j]), -p_hi(u[j]));
             }
             *reinterpret_cast<uint4*>(pr + part * C::GROUPS * C::P_BLOCK + ((k ^ sw) << 4)) = make_uint4(u[0], u[1], u[2], u[3]);
           }
@@ -558,12 +555,15 @@ cudaError_t tc_go(PagedAttnArgs a, int num_sm, cudaStream_t st) {
   return launch_k(paged_attn_tc_kernel<D, NR, PARTS>, dim3(paged_attn_grid(num_sm)), dim3(Cfg<D, NR, PARTS>::THREADS), Cfg<D, NR, PARTS>::SMEM, st, t);
 }
 
-// The fewest rows per tile that hold a sequence's rows of one key head; more rows go in tiles of the largest width.
+// The narrowest tile that holds a sequence's rows of one key head (18 sequences of 4096 tokens, bf16: 24 rows 52 us in tiles of
+// 32, 40 rows 54 us in tiles of 48 and 61 us in tiles of 64).  More rows than the widest: fp32 ones in several tiles of it,
+// bf16 ones on the kernel for many rows (64 rows, one sequence of 18 944 tokens: 41 us here, 102 us there).
 template <int D>
 cudaError_t tc_rows(const PagedAttnArgs& a, long long rows, int num_sm, cudaStream_t st) {
   if (a.q_bf16) {
     if (rows <= 16) return tc_go<D, 16, 1>(a, num_sm, st);
     if (rows <= 32) return tc_go<D, 32, 1>(a, num_sm, st);
+    if (rows <= 48) return tc_go<D, 48, 1>(a, num_sm, st);
     return tc_go<D, 64, 1>(a, num_sm, st);
   }
   if (rows <= 16) return tc_go<D, 16, 3>(a, num_sm, st);

@@ -21,23 +21,25 @@
 //   warps 4-7    Q of the part to come: its loads under way while the last scores of this part are multiplied
 //   warps 8-15   softmax of tile 0 (8-11) and tile 1 (12-15), and their outputs
 //
+// Parts of an item are 256 rows x d floats each: they are joined by a kernel of its own (paged_join_kernel) that spreads every
+// item's rows over several CTAs; one CTA joining all of them took 60 us for 18 parts of 64 rows.
+//
 // Waits are bounded and end as in paged_attention_tc.cu.
 #include "paged_tc.cuh"
+
 
 namespace {
 
 constexpr float MAX_UP = 24.f;       // log2 of the largest weight that is let stand
 constexpr int W_ROWS = 256;          // rows of an item: two tiles
 constexpr int W_THREADS = 512;
-constexpr int W_SOFT = 256;
 
 template <int D> struct WCfg {
   static constexpr uint32_t HALF = TILE * D * 2;
   static constexpr uint32_t Q_BYTES = W_ROWS * D * 2;
   static constexpr int STAGES = D == 128 ? 4 : 8;
   static constexpr uint32_t Q_AT = STAGES * HALF, HDR_AT = Q_AT + Q_BYTES;
-  static constexpr int JOIN_FLOATS = 2 * W_SOFT + 4 * W_ROWS;   // see join_parts
-  static constexpr uint32_t HDR = 1024 + W_ROWS * (8 + 4 + 4) + JOIN_FLOATS * 4;
+  static constexpr uint32_t HDR = 1024 + W_ROWS * 8;
   static constexpr size_t SMEM = HDR_AT + HDR;
   // kind::f16 instruction descriptors: fp32 accumulator, bf16 x bf16, M = 128; S: both K-major, N = 128; O: B MN-major, N = d
   static constexpr uint32_t IDESC_S = (1u << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(TILE >> 3) << 17) | (8u << 24);
@@ -67,13 +69,9 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
   volatile uint32_t* s_tmem = reinterpret_cast<volatile uint32_t*>(hdr + 200);
   volatile int* s_abort = reinterpret_cast<volatile int*>(hdr + 204);
   int* s_poison = reinterpret_cast<int*>(hdr + 208);
-  int* s_last = reinterpret_cast<int*>(hdr + 212);
   WorkCursor* s_cur = reinterpret_cast<WorkCursor*>(hdr + 216);
   SeqGeom* geo = reinterpret_cast<SeqGeom*>(hdr + 512);                 // [GEO]
   long long* s_qat = reinterpret_cast<long long*>(hdr + 1024);          // [256] where a row of Q is
-  float* s_max = reinterpret_cast<float*>(hdr + 1024 + NR * 8);          // [256] scratch of the join
-  float* s_inv = s_max + NR;
-  float* s_join = s_inv + NR;                                           // [JOIN_FLOATS]
   static_assert(sizeof(WorkCursor) <= 264 && sizeof(SeqGeom) * GEO <= 512, "header");
   const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
 
@@ -246,6 +244,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
     bool ok = true;
     uint32_t sn = 0, on = 0;                                   // scores taken; outputs awaited
     int it = 0;
+    if (st == 0) a.records[blockIdx.x].parts = 0;
     while (c.valid) {
       const int R = c.nq * a.G, r = c.t * NR + w * 128 + my, n = c.k1 - c.k0;
       const int tok = row_token(a, r);
@@ -410,15 +409,8 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
           a.lse[(size_t)(c.row0 + tok) * a.H + c.hk * a.G + r - tok * a.G] = l == 0.f ? -INFINITY : 0.6931471805599453f * (m + log2f(l));
         }
       }
-      if (parts > 1) {
-        asm volatile("bar.sync 1, 256;" ::: "memory");
-        if (st == 0) {
-          *s_last = part_arrive(a.counters + first, parts);
-        }
-        asm volatile("bar.sync 1, 256;" ::: "memory");
-        if (*s_last) join_parts<NR, D, W_SOFT, true>(a, c, first, parts, st, s_max, s_inv, s_join, C::JOIN_FLOATS);
-      }
-      asm volatile("bar.sync 1, 256;" ::: "memory");   // s_poison and s_last may be written again
+      if (parts > 1 && c.k0 == 0 && st == 0) a.records[blockIdx.x] = PartRecord{c.row0, c.nq, c.hk, c.t, first, parts};
+      asm volatile("bar.sync 1, 256;" ::: "memory");   // s_poison may be written again
       cursor_next<NR, TILE>(a, c, geo);
     }
     if (!ok) *s_abort = 1;
@@ -431,6 +423,72 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
   }
 }
 
+// Joins the parts of the items that the attention kernel cut: o = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c.  CTA (c, s)
+// takes 32 rows of the item whose first part CTA c left, a lane per row, d / 32 pieces of four elements per warp; the pieces
+// of four parts are in flight at once.  Bound by the parts' bytes, out of L2.
+constexpr int JOIN_PARTS = 256;   // weights held at once
+template <int D>
+__global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttnArgs a) {
+  constexpr int NR = W_ROWS, PIECES = D / 4 / 8;
+  __shared__ float s_w[JOIN_PARTS][32];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  pdl_launch_dependents();
+  pdl_wait();
+  const PartRecord rec = a.records[blockIdx.x];
+  const int r = blockIdx.y * 32 + lane, rr = rec.t * NR + r, R = rec.nq * a.G;
+  if (rec.parts < 2 || rec.t * NR + (int)blockIdx.y * 32 >= R) return;
+  const bool live = rr < R;
+  constexpr size_t SF = slot_floats<NR, D>();
+  const float* slots = a.slots + SF * (size_t)(2 * rec.first);
+  auto slot = [&](int p) { return slots + SF * (size_t)(p == 0 ? 1 : 2 * p); };   // part 0 begins in its CTA: part_slot
+  float M = -INFINITY, L = 0.f;
+  if (live) {
+#pragma unroll 4
+    for (int p = 0; p < rec.parts; ++p) {
+      const float m = __ldcg(slot(p) + r), l = __ldcg(slot(p) + NR + r);
+      const float nm = fmaxf(M, m), base = nm == -INFINITY ? 0.f : nm;
+      L = L * exp2f(M - base) + l * exp2f(m - base);        // 2^-inf = 0 on either side that has nothing
+      M = nm;
+    }
+  }
+  const float base = M == -INFINITY ? 0.f : M, inv = L == 0.f ? 0.f : 1.f / L;
+  float4 o[PIECES];
+#pragma unroll
+  for (int k = 0; k < PIECES; ++k) o[k] = make_float4(0.f, 0.f, 0.f, 0.f);
+  for (int p0 = 0; p0 < rec.parts; p0 += JOIN_PARTS) {
+    const int n = min(JOIN_PARTS, rec.parts - p0);
+    __syncthreads();
+    for (int p = warp; p < n; p += 8) s_w[p][lane] = live ? exp2f(__ldcg(slot(p0 + p) + r) - base) * inv : 0.f;
+    __syncthreads();
+    if (live) {
+#pragma unroll 4
+      for (int p = 0; p < n; ++p) {
+        const float w = s_w[p][lane];
+        const float4* s = reinterpret_cast<const float4*>(slot(p0 + p) + 2 * NR) + (size_t)(warp * PIECES) * NR + r;
+#pragma unroll
+        for (int k = 0; k < PIECES; ++k) {
+          const float4 v = __ldcg(s + k * NR);
+          o[k].x += w * v.x; o[k].y += w * v.y; o[k].z += w * v.z; o[k].w += w * v.w;
+        }
+      }
+    }
+  }
+  if (!live) return;
+  const int tok = row_token(a, rr), head = rec.hk * a.G + rr - tok * a.G;
+  const long long at = (long long)(rec.row0 + tok) * a.out.row + (long long)head * a.out.head + warp * PIECES * 4;
+#pragma unroll
+  for (int k = 0; k < PIECES; ++k) {
+    if (a.out_vec && a.out_bf16) {
+      *reinterpret_cast<uint2*>(reinterpret_cast<__nv_bfloat16*>(a.out.p) + at + 4 * k) = make_uint2(p_pack(o[k].x, o[k].y), p_pack(o[k].z, o[k].w));
+    } else if (a.out_vec) {
+      *reinterpret_cast<float4*>(reinterpret_cast<float*>(a.out.p) + at + 4 * k) = o[k];
+    } else {
+      store_out(a, at + 4 * k, o[k].x); store_out(a, at + 4 * k + 1, o[k].y); store_out(a, at + 4 * k + 2, o[k].z); store_out(a, at + 4 * k + 3, o[k].w);
+    }
+  }
+  if (a.lse && warp == 0) a.lse[(size_t)(rec.row0 + tok) * a.H + head] = L == 0.f ? -INFINITY : 0.6931471805599453f * (base + log2f(L));
+}
+
 template <int D>
 cudaError_t wide_go(PagedAttnArgs a, int num_sm, cudaStream_t st) {
   static DevSmemCache cached{};
@@ -440,7 +498,9 @@ cudaError_t wide_go(PagedAttnArgs a, int num_sm, cudaStream_t st) {
   cudaError_t e = tc_args(a, D, &t);
   if (e == cudaSuccess) e = sps_ensure_smem(paged_attn_wide_kernel<D>, WCfg<D>::SMEM, cached);
   if (e != cudaSuccess) return e;
-  return launch_k(paged_attn_wide_kernel<D>, dim3(paged_attn_grid(num_sm)), dim3(W_THREADS), WCfg<D>::SMEM, st, t);
+  e = launch_k(paged_attn_wide_kernel<D>, dim3(paged_attn_grid(num_sm)), dim3(W_THREADS), WCfg<D>::SMEM, st, t);
+  if (e != cudaSuccess) return e;
+  return launch_k(paged_join_kernel<D>, dim3(paged_attn_grid(num_sm), W_ROWS / 32), dim3(256), 0, st, a);
 }
 
 }  // namespace
