@@ -273,14 +273,12 @@ __device__ __forceinline__ void store_out(const PagedAttnArgs& a, long long at, 
 // threads of the last CTA to arrive (named barrier 2 is theirs).  A part's slot is a trip to L2 away, so many loads are in
 // flight at once: every thread first asks for its four-element pieces of the first AHEAD parts' outputs, then for maxima and
 // sums (THREADS / NR threads to a row), and goes on four parts at a time, their weights in shared memory.  s_max, s_inv: shared
-// scratch of NR floats each; w: of w_floats >= 2 * THREADS + 2 * NR. 
+// scratch of NR floats each; w: of w_floats >= 2 * THREADS.
 template <int NR, int D, int THREADS>
 __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCursor& c, int first, int parts, int tid, float* s_max, float* s_inv, float* w, int w_floats) {
   const int R = c.nq * a.G, r0 = c.t * NR, live = min(NR, R - r0);
   constexpr size_t SF = slot_floats<NR, D>();
-  constexpr int LANES = THREADS / NR, PIECES = NR * (D / 4) / THREADS, BLOCK = PIECES < 4 ? PIECES : 4, AHEAD = 4;
-  float* pair = w + w_floats - 2 * THREADS;                    // (maximum, sum) by thread; ahead of it the table of weights
-  const int table = (w_floats - 2 * THREADS) / NR;             // parts whose weights fit at once
+  constexpr int LANES = THREADS / NR, PIECES = NR * (D / 4) / THREADS, BLOCK = PIECES < 4 ? PIECES : 4, AHEAD = 2;
   const float* slots = a.slots + SF * (size_t)(2 * first);
   auto slot = [&](int p) { return slots + SF * (size_t)(p == 0 ? 1 : 2 * p); };   // part 0 begins in its CTA: part_slot
   auto sync = [&]() { asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory"); };
@@ -292,7 +290,7 @@ __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCur
 #pragma unroll
     for (int k = 0; k < BLOCK; ++k) {
       const int i = tid + k * THREADS;
-      early[p][k] = p < parts && row(i) < live ? fetch(p, i) : make_float4(0.f, 0.f, 0.f, 0.f);
+      early[p][k] = row(i) < live ? fetch(p, i) : make_float4(0.f, 0.f, 0.f, 0.f);    // (an item that is joined has at least two)
     }
   {
     const int r = tid % NR, p0 = tid / NR;
@@ -301,21 +299,20 @@ __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCur
 #pragma unroll 4
       for (int p = p0; p < parts; p += LANES) {
         const float m = __ldcg(slot(p) + r), l = __ldcg(slot(p) + NR + r);
-        if (p < table) w[p * NR + r] = m;
         const float nm = fmaxf(M, m), base = nm == -INFINITY ? 0.f : nm;
         L = L * exp2f(M - base) + l * exp2f(m - base);      // 2^-inf = 0 on either side that has nothing
         M = nm;
       }
     }
-    pair[2 * tid] = M;
-    pair[2 * tid + 1] = L;
+    w[2 * tid] = M;
+    w[2 * tid + 1] = L;
   }
   sync();
   if (tid < live) {
     float M = -INFINITY, L = 0.f;
-    for (int i = 0; i < LANES; ++i) M = fmaxf(M, pair[2 * (i * NR + tid)]);
+    for (int i = 0; i < LANES; ++i) M = fmaxf(M, w[2 * (i * NR + tid)]);
     const float base = M == -INFINITY ? 0.f : M;
-    for (int i = 0; i < LANES; ++i) L += pair[2 * (i * NR + tid) + 1] * exp2f(pair[2 * (i * NR + tid)] - base);
+    for (int i = 0; i < LANES; ++i) L += w[2 * (i * NR + tid) + 1] * exp2f(w[2 * (i * NR + tid)] - base);
     s_max[tid] = base;
     s_inv[tid] = L == 0.f ? 0.f : 1.f / L;
     if (a.lse) {
@@ -324,6 +321,7 @@ __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCur
     }
   }
   sync();
+  const int table = w_floats / NR;                             // parts whose weights fit at once
 #pragma unroll 1
   for (int kb = 0; kb < PIECES; kb += BLOCK) {
     float4 o[BLOCK];
@@ -334,7 +332,7 @@ __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCur
       if (kb == 0 || parts > table) {
         for (int i = tid; i < pn * NR; i += THREADS) {
           const int p = i / NR, r = i - p * NR;
-          if (r < live) w[i] = exp2f((kb == 0 && pb == 0 ? w[i] : __ldcg(slot(pb + p) + r)) - s_max[r]) * s_inv[r];
+          if (r < live) w[i] = exp2f(__ldcg(slot(pb + p) + r) - s_max[r]) * s_inv[r];
         }
         sync();
       }
@@ -342,13 +340,12 @@ __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCur
       int p = 0;
       if (kb == 0 && pb == 0) {
 #pragma unroll
-        for (int q = 0; q < AHEAD; ++q)
+        for (; p < AHEAD; ++p)
 #pragma unroll
           for (int k = 0; k < BLOCK; ++k) {
             const int r = row(tid + k * THREADS);
-            if (q < pn && r < live) add(k, w[q * NR + r], early[q][k]);
+            if (r < live) add(k, w[p * NR + r], early[p][k]);
           }
-        p = min(AHEAD, pn);
       }
 #pragma unroll 4
       for (; p < pn; ++p) {

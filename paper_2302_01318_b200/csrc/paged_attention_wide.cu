@@ -27,7 +27,6 @@
 // Waits are bounded and end as in paged_attention_tc.cu.
 #include "paged_tc.cuh"
 
-
 namespace {
 
 constexpr float MAX_UP = 24.f;       // log2 of the largest weight that is let stand
