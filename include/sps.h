@@ -457,7 +457,7 @@ int sps_paged_append(const sps_paged_cache* cache, const sps_paged_batch* batch,
 /* Attention: row i of sequence b, at position p = kv_len[b] - (rows of b) + i, over the tokens 0 .. p of its sequence:
  *   out[row, h] = sum_j softmax_j(scale q[row, h] . k[j, h / G]) v[j, h / G],   G = heads of q / n_kv_heads,
  * scale 0 meaning 1 / sqrt(d_head).  A row at a negative position sees nothing: its output is 0.
- * q and out: [rows] rows of the same heads; out has q's dtype, or is fp32; a bf16 cache takes fp32 or bf16 queries
+ * q and out: [rows] rows of the same heads, rows x heads below 2^31; out has q's dtype, or is fp32; a bf16 cache takes fp32 or bf16 queries
  * (fp32 queries and probabilities enter the tensor cores as three bf16 parts each, which keep their 24 bits; bf16
  * queries leave the probabilities rounded to bf16), an fp32 cache fp32 ones.  lse: device fp32 [rows][heads], may be
  * NULL: log sum_j exp(scale q . k_j), -inf for a row that sees nothing.

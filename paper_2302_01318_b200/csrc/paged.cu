@@ -475,6 +475,7 @@ int sps_paged_attention(const sps_paged_cache* cache, const sps_paged_batch* bat
   if (why) return no(SPS_EINVAL, why);
   if (out->heads != q->heads) return no(SPS_EINVAL, "q and out must have the same heads");
   if (q->dtype == 0 && out->dtype == 1) return no(SPS_EINVAL, "out has q's dtype or is fp32");
+  if ((int64_t)rows * q->heads > 0x7fff0000) return no(SPS_EINVAL, "rows x heads must stay below 2^31");
   if (!std::isfinite(scale)) return no(SPS_EINVAL, "scale must be finite");
   if (!workspace || ((uintptr_t)workspace & 15)) return no(SPS_EINVAL, "workspace null or not 16-byte aligned");
   if ((uintptr_t)lse & 3) return no(SPS_EINVAL, "lse not 4-byte aligned");
@@ -495,6 +496,9 @@ int sps_paged_attention(const sps_paged_cache* cache, const sps_paged_batch* bat
   a.records = (PartRecord*)((char*)workspace + PAGED_COUNTER_BYTES);
   a.slots = (float*)((char*)workspace + PAGED_COUNTER_BYTES + PAGED_RECORD_BYTES);
   a.wait_ns = sps_wait_knobs().limit_ns;
+  const unsigned grid = (unsigned)paged_attn_grid(sms());
+  a.grid_magic = grid > 1 ? (uint32_t)(((1ull << 32) + grid - 1) / grid) : 0;   // one CTA: never used
+  a.grid_magic_to = grid > 1 ? (int)((1ull << 31) / grid) : 0;
   const cudaError_t e = paged_attn_launch(a, cache->dtype, cache->d_head, batch->max_q, sms(), (cudaStream_t)stream);
   return e == cudaSuccess ? SPS_OK : no(SPS_ECUDA, cudaGetErrorString(e));
 }

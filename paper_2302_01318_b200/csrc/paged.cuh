@@ -64,6 +64,8 @@ struct PagedAttnArgs {
   float* lse;               // [rows][H] or null
   int* counters;            // [grid] arrivals at an item, by the first CTA that works on it; zero between launches
   PartRecord* records;      // [grid] (kernels whose parts another kernel joins)
+  uint32_t grid_magic;      // ceil(2^32 / CTAs), and the numbers below which its high product divides by them
+  int grid_magic_to;
   int lead, min_run;        // set by the launcher: an item's cost ahead of its tiles, the least run, in tiles
   float* slots;             // [2 * grid] parts: [NR] maxima, [NR] sums, [NR][d_head] outputs
   unsigned long long wait_ns;
@@ -116,7 +118,7 @@ __device__ __forceinline__ void cursor_next(const PagedAttnArgs& a, WorkCursor& 
         const SeqGeom g = c.b - c.b0 < GEO ? geo[c.b - c.b0] : paged_seq(a.s, c.b);
         c.row0 = g.row0; c.nq = g.nq; c.len = g.len;
       } while (c.nq == 0);
-      c.nt = (c.nq * a.G + NR - 1) / NR;
+      c.nt = (int)((unsigned)(c.nq * a.G + NR - 1) / NR);
     }
   }
   cursor_part<NR, KT>(a, c, u);
@@ -127,9 +129,10 @@ __device__ __forceinline__ void cursor_next(const PagedAttnArgs& a, WorkCursor& 
 template <int NR, int KT>
 __device__ __forceinline__ long long warp_seq_units(const PagedAttnArgs& a, const SeqGeom& g, bool live) {
   const int lane = threadIdx.x & 31;
-  const int nt = live ? (int)(((long long)g.nq * a.G + NR - 1) / NR) : 0;
+  const int nt = live ? (int)((unsigned)(g.nq * a.G + NR - 1) / NR) : 0;
   long long sum = 0;
-  if (nt <= 4) for (int t = 0; t < nt; ++t) sum += a.lead + item_tiles<NR, KT>(a, g.nq, g.len, t);
+  if (nt == 1) sum = a.lead + item_tiles<NR, KT>(a, g.nq, g.len, 0);
+  else if (nt <= 4) for (int t = 0; t < nt; ++t) sum += a.lead + item_tiles<NR, KT>(a, g.nq, g.len, t);
   unsigned big = __ballot_sync(0xffffffffu, nt > 4);
   while (big) {
     const int src = __ffs(big) - 1;
@@ -158,12 +161,13 @@ __device__ __forceinline__ WorkCursor cursor_begin(const PagedAttnArgs& a, SeqGe
   WorkCursor c;
   c.valid = false;
   SeqGeom g{};                   // the sequences of one block of 32, a lane each; their work, and the sum up to each
-  long long units = 0, incl = 0, total = 0;
+  long long head = 0, units = 0, incl = 0, total = 0;   // head: of one key head
   auto block = [&](int b0) {
     const int b = b0 + lane;
     g = SeqGeom{};
     if (b < B) g = paged_seq(a.s, b);
-    units = warp_seq_units<NR, KT>(a, g, b < B) * a.Hkv;
+    head = warp_seq_units<NR, KT>(a, g, b < B);
+    units = head * a.Hkv;
     incl = units;
     if (__any_sync(0xffffffffu, units >= (1ll << 26))) {
 #pragma unroll 1
@@ -186,7 +190,9 @@ __device__ __forceinline__ WorkCursor cursor_begin(const PagedAttnArgs& a, SeqGe
     if (blockIdx.x == 0 && g.cut && g.nq > 0) paged_flag(a.s.status, SPS_PAGED_BAD_LENGTH);
     total += __shfl_sync(0xffffffffu, incl, 31);
   }
-  c.per = list_div(total + gridDim.x - 1, gridDim.x);
+  // ceil(total / CTAs): a high product for lists of up to 2^31 / CTAs tiles
+  const long long up = total + gridDim.x - 1;
+  c.per = up < a.grid_magic_to ? (long long)__umulhi((unsigned)up, a.grid_magic) : up / gridDim.x;
   if (c.per < a.min_run) c.per = a.min_run;
   const long long u = (long long)blockIdx.x * c.per;
   c.u_end = u + c.per < total ? u + c.per : total;
@@ -207,8 +213,8 @@ __device__ __forceinline__ WorkCursor cursor_begin(const PagedAttnArgs& a, SeqGe
       } else if (c.b + lane < B) {
         geo[lane] = paged_seq(a.s, c.b + lane);
       }
-      const long long first = base + __shfl_sync(0xffffffffu, incl - units, src), per_head = list_div(__shfl_sync(0xffffffffu, units, src), a.Hkv);
-      c.nt = (int)(((long long)c.nq * a.G + NR - 1) / NR);
+      const long long first = base + __shfl_sync(0xffffffffu, incl - units, src), per_head = __shfl_sync(0xffffffffu, head, src);
+      c.nt = (int)((unsigned)(c.nq * a.G + NR - 1) / NR);
       c.hk = (int)list_div(u - first, per_head);
       long long at = first + c.hk * per_head;   // where the key head's work begins
       c.t = 0;

@@ -116,6 +116,7 @@ def test_combinations():
     refused(append(k=rows(heads=2, dtype=1), v=rows(heads=2, dtype=1), q=rows(dtype=1), qo=rows(2 * P)), "q_out")
     refused(append(q=rows(), qo=rows(dtype=1)), "in place")
     refused(attend(n=-2), "rows")
+    refused(attend(n=1 << 29), "2^31")
     refused(attend(q=rows(heads=3), o=rows(heads=3)), "multiple")
     refused(attend(o=rows(heads=2)), "heads")
     refused(attend(cache(dtype=0), q=rows(dtype=1)), "fp32 cache")
