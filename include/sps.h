@@ -435,7 +435,8 @@ typedef struct {
  * not appended, and read as zeros); the last two also set a bit of *status, which the calls never clear. */
 #define SPS_PAGED_BAD_PAGE 1    /* bits of *status */
 #define SPS_PAGED_BAD_LENGTH 2
-#define SPS_PAGED_TIMEOUT 4     /* a bounded wait inside the attention kernel ran out: the call's outputs are meaningless */
+#define SPS_PAGED_TIMEOUT 4     /* a bounded wait inside the attention kernel ran out: the call's outputs are meaningless,
+                                   and its workspace wants zeroes again */
 typedef struct {
   const int32_t* q_start; /* device [B + 1], not decreasing      */
   const int32_t* kv_len;  /* device [B]                          */
@@ -458,8 +459,9 @@ int sps_paged_append(const sps_paged_cache* cache, const sps_paged_batch* batch,
  *   out[row, h] = sum_j softmax_j(scale q[row, h] . k[j, h / G]) v[j, h / G],   G = heads of q / n_kv_heads,
  * scale 0 meaning 1 / sqrt(d_head).  A row at a negative position sees nothing: its output is 0.
  * q and out: [rows] rows of the same heads, rows x heads below 2^31; out has q's dtype, or is fp32; a bf16 cache takes fp32 or bf16 queries
- * (fp32 queries and probabilities enter the tensor cores as three bf16 parts each, which keep their 24 bits; bf16
- * queries leave the probabilities rounded to bf16), an fp32 cache fp32 ones.  lse: device fp32 [rows][heads], may be
+ * (fp32 queries and probabilities enter the tensor cores as three bf16 parts each, which keep their 24 bits; with bf16
+ * queries the probabilities are two bf16 parts, or, for more than 64 rows of a key head, one), an fp32 cache fp32 ones.
+ * out may be q itself (same dtype and strides), other overlaps are not supported.  lse: device fp32 [rows][heads], may be
  * NULL: log sum_j exp(scale q . k_j), -inf for a row that sees nothing.
  * What lies in slots behind a sequence's tokens never matters, whatever it is.  An infinite or NaN value (v) makes
  * every element of the rows that see it NaN where its token is among the sequence's new rows, and follows
@@ -516,8 +518,8 @@ int sps_tp_group_score(sps_handle* const* ranks, int32_t world, int32_t which, c
  * it has in flight land, frees what it holds and returns, and the host call
  * reports SPS_ETIMEOUT.  limit_us shortens that bound (0 = the default of 2 s;
  * at most 2 s), and drop_stage >= 0 makes the copy producer of the first CTA
- * of sps_linear / sps_linear_wide leave out that stage of its ring, so that a
- * wait runs out on purpose with nothing left in flight (-1 = leave nothing
+ * of sps_linear / sps_linear_wide / sps_paged_attention (bf16 cache) leave out
+ * that stage of its ring, so that a wait runs out on purpose with nothing left in flight (-1 = leave nothing
  * out).  Process-wide; not thread-safe; meant for tests only. */
 int sps_debug_set_wait(int64_t limit_us, int32_t drop_stage);
 

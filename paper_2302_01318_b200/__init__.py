@@ -580,9 +580,17 @@ def sps_paged_append(cache, batch, k, v, plan=None, q=None, q_out=None, stream=N
     _on(index, lib().sps_paged_append, stream, cache._p, batch._p, plan._p if plan is not None else None, shape[0], C.byref(rk), C.byref(rv), rq, ro)
 
 
+def _workspace_bytes(cache, n_heads, code):
+    """On the cache's device: its number of SMs counts."""
+    if _Torch.current_device() == cache.index:
+        return int(lib().sps_paged_attention_workspace_bytes(cache._p, n_heads, code))
+    with _Torch.cuda_device(cache.index):
+        return int(lib().sps_paged_attention_workspace_bytes(cache._p, n_heads, code))
+
+
 def sps_paged_attention_workspace_bytes(cache, n_heads, q_dtype):
     """q_dtype: torch.float32 or torch.bfloat16."""
-    n = int(lib().sps_paged_attention_workspace_bytes(cache._p, n_heads, {"torch.float32": 0, "torch.bfloat16": 1}.get(str(q_dtype), -1)))
+    n = _workspace_bytes(cache, n_heads, _Torch.codes.get(q_dtype, -1))
     if n < 0:
         _check(SPS_EINVAL)
     return n
@@ -603,6 +611,6 @@ def sps_paged_attention(cache, batch, q, out, workspace, scale=0.0, lse=None, st
         if lse.shape != shape[:2] or not lse.is_contiguous() or lse.get_device() != index or lse.dtype is not _Torch.float32:
             raise ValueError("lse is contiguous float32 [rows, heads] on the same device")
         lse_p = lse.data_ptr()
-    if workspace.nbytes < lib().sps_paged_attention_workspace_bytes(cache._p, shape[1], rq.dtype):
+    if workspace.nbytes < _workspace_bytes(cache, shape[1], rq.dtype):
         raise ValueError("workspace smaller than sps_paged_attention_workspace_bytes")
     _on(index, lib().sps_paged_attention, stream, cache._p, batch._p, shape[0], C.byref(rq), C.byref(ro), scale, lse_p, workspace.data_ptr())

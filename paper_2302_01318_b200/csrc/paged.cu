@@ -496,6 +496,7 @@ int sps_paged_attention(const sps_paged_cache* cache, const sps_paged_batch* bat
   a.records = (PartRecord*)((char*)workspace + PAGED_COUNTER_BYTES);
   a.slots = (float*)((char*)workspace + PAGED_COUNTER_BYTES + PAGED_RECORD_BYTES);
   a.wait_ns = sps_wait_knobs().limit_ns;
+  a.drop_stage = sps_wait_knobs().drop_stage;
   const unsigned grid = (unsigned)paged_attn_grid(sms());
   a.grid_magic = grid > 1 ? (uint32_t)(((1ull << 32) + grid - 1) / grid) : 0;   // one CTA: never used
   a.grid_magic_to = grid > 1 ? (int)((1ull << 31) / grid) : 0;

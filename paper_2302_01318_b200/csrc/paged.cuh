@@ -69,6 +69,7 @@ struct PagedAttnArgs {
   int lead, min_run;        // set by the launcher: an item's cost ahead of its tiles, the least run, in tiles
   float* slots;             // [2 * grid] parts: [NR] maxima, [NR] sums, [NR][d_head] outputs
   unsigned long long wait_ns;
+  int drop_stage;           // test hook: the half-tile that the copies of the list's first CTA leave out, -1 = none
 };
 
 // r / G for a row of a group of G heads

@@ -270,8 +270,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
       *s_abort = 1;
       if (leader) p_commit(drain);
       __syncwarp();
-      const unsigned long long t0 = p_timer();
-      while (!p_try(drain, 0u) && p_timer() - t0 <= a.wait_ns) {}
+      p_drain(drain, 0u);
     }
   } else if (warp < 4) {
     // ---------------------------------------------------------------------------------------------------- Q

@@ -180,8 +180,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
         *s_abort = 1;
         if (leader) p_commit(drain);
         __syncwarp();
-        const unsigned long long t0 = p_timer();
-        while (!p_try(drain, 0u) && p_timer() - t0 <= a.wait_ns) {}
+        p_drain(drain, 0u);
       }
     }
   } else if (warp < 8) {

@@ -237,3 +237,60 @@ def test_a_large_batch_and_a_long_context_against_sums_over_chunks():
     L = 70000
     pages = Pages([L], 1, 128, 64, BF16)
     run_attention(pages, [2], 2, F32)
+
+
+@pytest.mark.parametrize("types", range(3))
+@pytest.mark.parametrize("new", [1, 40])
+def test_in_place(types, new):
+    qdt, cdt, odt = TYPES[types]
+    pages = Pages([700, 90], 2, 64, 16, cdt)
+    q = normal((2 * new, 8, 64), qdt, 1)
+    buf = q.clone()
+    sps.sps_paged_attention(pages.cache, pages.batch([new, new]), buf, buf, workspace(pages.cache, 8, qdt))
+    check_attention(buf, None, q, pages.dense, [new, new])
+
+
+@pytest.mark.parametrize("types", range(3))
+@pytest.mark.parametrize("order", [(0, 1, 2), (0, 2, 1), (1, 0, 2), (1, 2, 0), (2, 0, 1), (2, 1, 0)])
+def test_pools_of_any_order(types, order):
+    """Pages, heads and slots in any order of strides, with gaps: the pool is a view of a larger tensor."""
+    qdt, cdt, odt = TYPES[types]
+    src = Pages([100, 37], 3, 64, 8, cdt)
+    size = [src.k.shape[i] for i in order]
+    back = [order.index(i) for i in range(3)] + [3]
+    pools = []
+    for t in (src.k, src.v):
+        big = torch.full([s + 1 for s in size] + [72], float("nan"), dtype=cdt, device=DEV)
+        view = big[:size[0], :size[1], :size[2], :64]
+        view.copy_(t.permute(*order, 3))
+        pools.append(view.permute(*back))
+    cache = sps.PagedCache(*pools)
+    news = [5, 2]
+    q = normal((7, 6, 64), qdt, 2)
+    out = torch.empty((7, 6, 64), dtype=odt, device=DEV)
+    sps.sps_paged_attention(cache, src.batch(news), q, out, workspace(cache, 6, qdt))
+    check_attention(out, None, q, src.dense, news)
+
+
+@pytest.mark.parametrize("qdt,new,lens", [(F32, 2, [60000, 90]), (BF16, 2, [60000, 90]), (F32, 6, [30000, 90]), (BF16, 100, [6000, 300])])
+@pytest.mark.parametrize("stage", [0, 1, 2])
+def test_a_wait_that_runs_out_ends_the_call_with_a_status(qdt, new, lens, stage):
+    """The first CTA's copies leave out one half-tile (keys of its first tile, values of it, keys of the next): the call gives
+    up within the bound, says so, and the next one on a fresh workspace is right."""
+    pages = Pages(lens, 2, 128, 16, BF16)
+    news = [new, new]
+    q = normal((2 * new, 16, 128), qdt, 1)
+    out, ws, batch = torch.empty_like(q), workspace(pages.cache, 16, qdt), pages.batch(news)
+    try:
+        sps.sps_debug_set_wait(20000, stage)
+        sps.sps_paged_attention(pages.cache, batch, q, out, ws)
+        torch.cuda.synchronize()
+    finally:
+        sps.sps_debug_set_wait()
+    assert int(batch.status) == sps.PAGED_TIMEOUT
+    batch.status.zero_()
+    ws.zero_()
+    sps.sps_paged_attention(pages.cache, batch, q, out, ws)
+    torch.cuda.synchronize()
+    assert int(batch.status) == 0
+    check_attention(out, None, q, pages.dense, news)
