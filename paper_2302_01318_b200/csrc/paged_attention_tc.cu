@@ -326,6 +326,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
 #pragma unroll
         for (int part = 0; part < PP; ++part) p_ld16(tmem_o + t_lane + part * NR + col0, t[part]);
         P_WAIT_LD();
+        p_landed<PP * 16>(t[0]);
 #pragma unroll
         for (int j = 0; j < 16; j += 2) {
           if (PP == 3) p_add2(t[1][j], t[1][j + 1], t[PP - 1][j], t[PP - 1][j + 1]);
@@ -345,6 +346,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
 #pragma unroll
           for (int part = 0; part < PARTS; ++part) p_ld16(tmem + buf * N + t_lane + part * NR + col0, t[part]);
           P_WAIT_LD();
+          p_landed<PARTS * 16>(t[0]);
 #pragma unroll
           for (int j = 0; j < 16; j += 2) {
             if (PARTS == 3) {

@@ -288,6 +288,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
 #pragma unroll
           for (int j = 0; j < 128; j += 32) p_ld32(t_s + j, x + j);
           P_WAIT_LD();
+          p_landed<128>(x);
 #pragma unroll
           for (int j = 0; j < 128; j += 2) p_fma2(x[j], x[j + 1], a.scale_log2, -m, -m);
           if (p0 + TILE - 1 > warp_lim || r >= R) {
@@ -324,6 +325,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
               float o[16];
               p_ld16(t_o + j, o);
               P_WAIT_LD();
+              p_landed<16>(o);
               uint32_t u[16];
 #pragma unroll
               for (int q = 0; q < 16; ++q) u[q] = __float_as_uint(o[q] * f);
@@ -378,6 +380,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
           float o[32];
           p_ld32(t_o + j, o);
           P_WAIT_LD();
+          p_landed<32>(o);
           if (r >= R) continue;
           if (parts > 1) {
 #pragma unroll
