@@ -4,7 +4,7 @@
 //   s_j = scale q . k_j,  m = max s_j,  l = sum 2^(s_j - m),  o = sum 2^(s_j - m) v_j / l     (scores in base 2)
 //
 // One pass over keys and values with the running maximum and sum; everything in fp32.  A CTA of 256 threads takes 16 query
-// rows against tiles of 64 tokens staged in shared memory as fp32: scores by (token, four rows) per thread, the softmax
+// rows against tiles of 64 tokens, fetched into registers a tile ahead and staged in shared memory: scores by (token, four rows) per thread, the softmax
 // by a warp per two rows, outputs by (two elements, a few rows) per thread in registers.
 #include <type_traits>
 
@@ -18,6 +18,7 @@ template <int D>
 __global__ void __launch_bounds__(SIMT_THREADS) paged_attn_simt_kernel(const __grid_constant__ PagedAttnArgs a) {
   constexpr int NR = SIMT_NR, KT = SIMT_KT, LDK = D + 4;
   constexpr int RPT = NR / (SIMT_THREADS / (D / 2));   // rows a thread accumulates (4 or 2)
+  constexpr int LOADS = KT * (D / 4) / SIMT_THREADS;   // four-element pieces of a tile's keys (and values) per thread
   extern __shared__ __align__(16) float simt_smem[];
   float* Ks = simt_smem;             // [KT][D + 4]
   float* Vs = Ks + KT * LDK;         // [KT][D]
@@ -40,6 +41,30 @@ __global__ void __launch_bounds__(SIMT_THREADS) paged_attn_simt_kernel(const __g
   const int dp = tid % (D / 2), rg = tid / (D / 2);
   while (c.valid) {
     const int R = c.nq * a.G, r0 = c.t * NR;
+    // keys and values of a tile into registers: this thread's four elements of LOADS tokens; zeros where there is no token or page
+    float4 kr[LOADS], vr[LOADS];
+    auto fetch = [&](int kt) {
+      long long at[LOADS];
+#pragma unroll
+      for (int x = 0; x < LOADS; ++x) {
+        const int i = tid + x * SIMT_THREADS, j = i / (D / 4), e = (i - j * (D / 4)) * 4, pos = kt * KT + j;
+        at[x] = -1;
+        if (pos < c.len) {
+          const int page = a.s.pages[(long long)c.b * a.s.pages_ld + (pos >> a.s.page_shift)];
+          if (page >= 0 && page < a.s.n_pages) at[x] = page * a.page_stride + c.hk * a.head_stride + (pos & (a.s.page_size - 1)) * a.pos_stride + e;
+          else paged_flag(a.s.status, SPS_PAGED_BAD_PAGE);
+        }
+      }
+#pragma unroll
+      for (int x = 0; x < LOADS; ++x) {
+        kr[x] = vr[x] = make_float4(0.f, 0.f, 0.f, 0.f);
+        if (at[x] >= 0) {
+          kr[x] = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.k) + at[x]);
+          vr[x] = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.v) + at[x]);
+        }
+      }
+    };
+    fetch(c.k0);
     __syncthreads();   // the previous part's rows have been read
     for (int i = tid; i < NR * D; i += SIMT_THREADS) {
       const int r = i / D, e = i - r * D, rr = r0 + r;
@@ -63,23 +88,14 @@ __global__ void __launch_bounds__(SIMT_THREADS) paged_attn_simt_kernel(const __g
     for (int kt = c.k0; kt < c.k1; ++kt) {
       const int p0 = kt * KT;
       __syncthreads();
-      for (int i = tid; i < KT * (D / 4); i += SIMT_THREADS) {
-        const int j = i / (D / 4), e = (i - j * (D / 4)) * 4, pos = p0 + j;
-        float4 k = make_float4(0.f, 0.f, 0.f, 0.f), v = k;
-        if (pos < c.len) {
-          const int page = a.s.pages[(long long)c.b * a.s.pages_ld + (pos >> a.s.page_shift)];
-          if (page >= 0 && page < a.s.n_pages) {
-            const long long at = page * a.page_stride + c.hk * a.head_stride + (pos & (a.s.page_size - 1)) * a.pos_stride + e;
-            k = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.k) + at);
-            v = *reinterpret_cast<const float4*>(reinterpret_cast<const float*>(a.v) + at);
-          } else {
-            paged_flag(a.s.status, SPS_PAGED_BAD_PAGE);
-          }
-        }
-        *reinterpret_cast<float4*>(Ks + j * LDK + e) = k;
-        *reinterpret_cast<float4*>(Vs + j * D + e) = v;
+#pragma unroll
+      for (int x = 0; x < LOADS; ++x) {
+        const int i = tid + x * SIMT_THREADS, j = i / (D / 4), e = (i - j * (D / 4)) * 4;
+        *reinterpret_cast<float4*>(Ks + j * LDK + e) = kr[x];
+        *reinterpret_cast<float4*>(Vs + j * D + e) = vr[x];
       }
       __syncthreads();
+      if (kt + 1 < c.k1) fetch(kt + 1);   // under way while this tile is worked on
       {
         const int j = tid & 63, g = tid >> 6;
         float s[4] = {0.f, 0.f, 0.f, 0.f};
