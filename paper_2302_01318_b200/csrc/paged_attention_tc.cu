@@ -194,8 +194,8 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
   if (warp == 1) {
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(hb + 216), "n"(C::TMEM) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    pdl_launch_dependents();   // with the tensor memory in hand: a dependent on this SM that took it first would wait for this CTA
   }
-  pdl_launch_dependents();
   pdl_wait();
   if (warp == 0) {
     const WorkCursor c0 = cursor_begin<NR, TILE>(a, geo);

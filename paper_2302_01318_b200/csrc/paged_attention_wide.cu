@@ -86,8 +86,8 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
   if (warp == 1) {   // S_0, S_1 and O_0, O_1: all 512 columns
     asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], 512;" ::"r"(hb + 200) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    pdl_launch_dependents();   // with the tensor memory in hand: a dependent on this SM that took it first would wait for this CTA
   }
-  pdl_launch_dependents();
   pdl_wait();
   if (warp == 0) {
     const WorkCursor c0 = cursor_begin<NR, TILE>(a, geo);
