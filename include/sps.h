@@ -463,9 +463,9 @@ int sps_paged_append(const sps_paged_cache* cache, const sps_paged_batch* batch,
  * queries the probabilities are two bf16 parts, or, for more than 64 rows of a key head, one), an fp32 cache fp32 ones.
  * out may be q itself (same dtype and strides), other overlaps are not supported.  lse: device fp32 [rows][heads], may be
  * NULL: log sum_j exp(scale q . k_j), -inf for a row that sees nothing.
- * What lies in slots behind a sequence's tokens never matters, whatever it is.  An infinite or NaN value (v) makes
- * every element of the rows that see it NaN where its token is among the sequence's new rows, and follows
- * sum p_j v_j elsewhere.
+ * What lies in slots behind a sequence's tokens never matters, whatever it is.  An infinite or NaN value (v) makes its
+ * element of the rows that give it weight infinite or NaN (which of the two is left open); over a bf16 cache, where its
+ * token is among the sequence's new ones, every element of the rows that see it is NaN.
  * workspace: device scratch of sps_paged_attention_workspace_bytes bytes, 16-byte aligned, zero-filled once before its
  * first use (every call leaves it ready for the next; calls that share one must not run at the same time, captured
  * ones included).  The size holds for every batch on this cache shape. */

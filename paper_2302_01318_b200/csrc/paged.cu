@@ -251,7 +251,7 @@ cudaError_t rotary_cut(RotaryArgs& a, int num_sm, cudaStream_t st) {
   a.rows_per_cta = rpc < 1 ? 1 : rpc;
   a.span_magic = magic_of(a.heads_per_cta);          // pairs of a CTA: at most 4096
   const size_t smem = sizeof(float2) * (size_t)a.rows_per_cta * (hr > 0 ? hr : 1);
-  const dim3 grid((a.rows + a.rows_per_cta - 1) / a.rows_per_cta, (a.vheads + a.heads_per_cta - 1) / a.heads_per_cta);
+  const dim3 grid(((unsigned)a.rows + a.rows_per_cta - 1) / a.rows_per_cta, (a.vheads + a.heads_per_cta - 1) / a.heads_per_cta);
   return launch_k(rotary_kernel<TX, TQ, TC, E, HALVES, UPT>, grid, dim3(ROT_THREADS), smem, st, a);
 }
 
@@ -474,9 +474,11 @@ int sps_paged_attention(const sps_paged_cache* cache, const sps_paged_batch* bat
   if (!why) why = bad_heads(cache, q->heads, q->dtype);
   if (why) return no(SPS_EINVAL, why);
   if (out->heads != q->heads) return no(SPS_EINVAL, "q and out must have the same heads");
+  if (out->p == q->p && rows > 0 && (out->dtype != q->dtype || out->row_stride != q->row_stride || out->head_stride != q->head_stride))
+    return no(SPS_EINVAL, "in place, q and out must have the same dtype and strides");
   if (q->dtype == 0 && out->dtype == 1) return no(SPS_EINVAL, "out has q's dtype or is fp32");
   if ((int64_t)rows * q->heads > 0x7fff0000) return no(SPS_EINVAL, "rows x heads must stay below 2^31");
-  if (!std::isfinite(scale)) return no(SPS_EINVAL, "scale must be finite");
+  if (!std::isfinite(scale * 1.4426950408889634f)) return no(SPS_EINVAL, "scale must be finite, in base 2 too");
   if (!workspace || ((uintptr_t)workspace & 15)) return no(SPS_EINVAL, "workspace null or not 16-byte aligned");
   if ((uintptr_t)lse & 3) return no(SPS_EINVAL, "lse not 4-byte aligned");
   if (rows == 0 || batch->B == 0) return SPS_OK;

@@ -112,6 +112,34 @@ def test_what_a_row_does_not_see_never_reaches_it(types, bad):
 
 
 @pytest.mark.parametrize("types", range(3))
+@pytest.mark.parametrize("new", [2, 150])
+def test_an_infinite_value_stays_in_its_element(types, new):
+    """Of an older token: every row sees it, and every other element is what it is without it."""
+    qdt, cdt, odt = TYPES[types]
+    pages = Pages([600], 1, 64, 16, cdt)
+    q = normal((new, 2, 64), qdt, 1)
+    ws, batch = workspace(pages.cache, 2, qdt), pages.batch([new])
+    out, clean = (torch.empty((new, 2, 64), dtype=odt, device=DEV) for _ in range(2))
+    sps.sps_paged_attention(pages.cache, batch, q, clean, ws)
+    pages.v[int(pages.table[0, 5]), 0, 3, 21] = float("inf")    # token 83
+    sps.sps_paged_attention(pages.cache, batch, q, out, ws)
+    others = [e for e in range(64) if e != 21]
+    assert not torch.isfinite(out[..., 21].float()).any()
+    assert torch.equal(out[..., others], clean[..., others]) and torch.isfinite(out[..., others].float()).all()
+
+
+@pytest.mark.parametrize("types", range(3))
+def test_sequences_that_share_a_prefix(types):
+    """Two sequences whose tables begin with the same pages, each with a last page of its own."""
+    qdt, cdt, odt = TYPES[types]
+    pages = Pages([160, 150], 2, 128, 16, cdt)
+    pages.table[1, :8] = pages.table[0, :8]
+    for own, other in zip(pages.dense[1], pages.dense[0]):
+        own[:128] = other[:128]
+    run_attention(pages, [5, 3], 8, qdt, odt)
+
+
+@pytest.mark.parametrize("types", range(3))
 def test_bad_pages_and_lengths_are_flagged_and_harm_no_other_sequence(types):
     qdt, cdt, odt = TYPES[types]
     pages = Pages([100, 300, 50], 2, 64, 16, cdt)

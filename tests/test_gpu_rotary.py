@@ -1,4 +1,6 @@
 """sps_rotary and sps_paged_append on the GPU against 64-bit restatements."""
+import math
+
 import pytest
 import torch
 
@@ -256,3 +258,17 @@ def test_append_replayed_in_a_graph_follows_lengths_and_tables():
         for b, L in ((0, 10 + step), (1, 30 + step)):
             assert torch.equal(pages.k[int(pages.table[b, (L - 1) // 8]), 0, (L - 1) % 8], k[b, 0])
     assert int(batch.status) == 0
+
+
+def test_rotary_as_many_rows_as_an_int_counts():
+    """2^31 - 1 rows of one pair, in place (8.6 GB, and as much for the positions): a quarter turn at odd positions."""
+    n = 2 ** 31 - 1
+    plan = sps.Rotary(torch.tensor([math.pi / 2], dtype=torch.float64, device=DEV))
+    x = torch.empty((n, 1, 2), dtype=BF16, device=DEV)
+    x[..., 0], x[..., 1] = 1.0, 2.0
+    pos = torch.zeros(n, dtype=torch.int32, device=DEV)
+    pos[1::2] = 1
+    sps.sps_rotary(x, x, pos, plan)
+    for at, want in ((slice(0, None, 2), (1.0, 2.0)), (slice(1, None, 2), (-2.0, 1.0))):
+        for e in range(2):
+            assert bool((x[at, 0, e] == want[e]).all())

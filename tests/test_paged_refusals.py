@@ -134,6 +134,17 @@ def test_combinations():
     assert L.sps_paged_attention_workspace_bytes(C.byref(cache(dtype=0)), 4, 1) == -1
 
 
+def test_attention_in_place_wants_the_same_layout():
+    refused(attend(q=rows(row=256), o=rows(row=512)), "in place")
+    refused(attend(q=rows(head=64), o=rows(head=128)), "in place")
+    refused(attend(q=rows(dtype=1), o=rows(dtype=0)), "in place")
+
+
+def test_a_scale_that_overflows_in_base_2_is_refused():
+    """Scores are kept in base 2: scale / ln 2 has to be a number too."""
+    refused(attend(scale=3e38), "scale")
+
+
 def test_nothing_to_do_is_no_error_and_launches_nothing():
     assert rotary(n=0) == sps.SPS_OK and append(n=0) == sps.SPS_OK and attend(n=0) == sps.SPS_OK
     assert append(b=batch(B=0, q_start=None, kv_len=None, pages=None)) == sps.SPS_OK
