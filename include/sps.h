@@ -442,7 +442,7 @@ typedef struct {
   const int32_t* kv_len;  /* device [B]                          */
   const int32_t* pages;   /* device [B][pages_ld]                */
   int32_t* status;        /* device [1], may be NULL             */
-  int32_t B, pages_ld;
+  int32_t B, pages_ld;    /* B: up to 2^27                       */
   int32_t max_q;          /* the most rows a sequence brings, as far as the host knows (>= 1): picks the kernel, results
                              hold for any q_start                */
 } sps_paged_batch;

@@ -349,7 +349,7 @@ const char* bad_cache(const sps_paged_cache* c) {
 }
 const char* bad_batch(const sps_paged_batch* b) {
   if (!b) return "null batch";
-  if (b->B < 0 || b->pages_ld < 0 || b->max_q < 1) return "batch: B, pages_ld or max_q out of range";
+  if (b->B < 0 || b->B > 1 << 27 || b->pages_ld < 0 || b->max_q < 1) return "batch: B, pages_ld or max_q out of range";
   if (b->B > 0 && (!b->q_start || !b->kv_len || (!b->pages && b->pages_ld > 0))) return "batch: null pointer";
   if (((uintptr_t)b->q_start | (uintptr_t)b->kv_len | (uintptr_t)b->pages | (uintptr_t)b->status) & 3) return "batch: pointers must be 4-byte aligned";
   return nullptr;

@@ -153,12 +153,14 @@ __device__ __forceinline__ long long list_div(long long n, long long d) {   // n
   return n / d;
 }
 
-// Called by warp 0 alone; the result and geo are for every thread of the CTA (in shared memory).  a.min_run: the least work a
-// CTA takes, so that a short list is not cut into parts that cost more to join than they save.  Up to 32 sequences are
-// read once, more of them twice (their number of tiles first, then the place of this CTA's run among them).
+// Called by every warp of the CTA; the result is warp 0's, and with geo for every thread (in shared memory).  a.min_run: the
+// least work a CTA takes, so that a short list is not cut into parts that cost more to join than they save.  Up to 32
+// sequences are read by warp 0, once.  More of them are summed by all warps, in 32 stretches of whole blocks of 32
+// (sums: shared, [32]), before warp 0 reads the stretch that this CTA's run begins in; with one warp reading all of them
+// twice 512 (2048) sequences of one token took 34 (123) us, this way 18 (56).
 template <int NR, int KT>
-__device__ __forceinline__ WorkCursor cursor_begin(const PagedAttnArgs& a, SeqGeom* geo) {
-  const int lane = threadIdx.x & 31, B = a.s.B;
+__device__ __forceinline__ WorkCursor cursor_begin(const PagedAttnArgs& a, SeqGeom* geo, long long* sums) {
+  const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, B = a.s.B;
   WorkCursor c;
   c.valid = false;
   SeqGeom g{};                   // the sequences of one block of 32, a lane each; their work, and the sum up to each
@@ -186,10 +188,32 @@ __device__ __forceinline__ WorkCursor cursor_begin(const PagedAttnArgs& a, SeqGe
       incl = sum;
     }
   };
-  for (int b0 = 0; b0 < B; b0 += 32) {
-    block(b0);
+  const long long stretch = 32ll * (((unsigned)B + 1023u) >> 10);   // sequences of one
+  long long mine = 0, upto = 0;   // lane's stretch, and the sum up to it
+  if (B <= 32) {
+    if (warp != 0) return c;
+    block(0);
     if (blockIdx.x == 0 && g.cut && g.nq > 0) paged_flag(a.s.status, SPS_PAGED_BAD_LENGTH);
-    total += __shfl_sync(0xffffffffu, incl, 31);
+    total = __shfl_sync(0xffffffffu, incl, 31);
+  } else {
+    for (int x = warp; x < 32; x += (int)(blockDim.x >> 5)) {
+      long long sum = 0;
+      for (long long b0 = x * stretch; b0 < (x + 1) * stretch && b0 < B; b0 += 32) {
+        block((int)b0);
+        if (blockIdx.x == 0 && g.cut && g.nq > 0) paged_flag(a.s.status, SPS_PAGED_BAD_LENGTH);
+        sum += __shfl_sync(0xffffffffu, incl, 31);
+      }
+      if (lane == 0) sums[x] = sum;
+    }
+    __syncthreads();
+    if (warp != 0) return c;
+    mine = upto = sums[lane];
+#pragma unroll
+    for (int o = 1; o < 32; o <<= 1) {
+      const long long up = __shfl_up_sync(0xffffffffu, upto, o);
+      if (lane >= o) upto += up;
+    }
+    total = __shfl_sync(0xffffffffu, upto, 31);
   }
   // ceil(total / CTAs): a high product for lists of up to 2^31 / CTAs tiles
   const long long up = total + gridDim.x - 1;
@@ -200,7 +224,13 @@ __device__ __forceinline__ WorkCursor cursor_begin(const PagedAttnArgs& a, SeqGe
   if (u >= c.u_end) return c;
   // the sequence that place u falls into
   long long base = 0;
-  for (int b0 = 0; b0 < B; b0 += 32) {
+  int from = 0;
+  if (B > 32) {
+    const int x = __ffs(__ballot_sync(0xffffffffu, upto > u)) - 1;
+    base = __shfl_sync(0xffffffffu, upto - mine, x);
+    from = (int)(x * stretch);
+  }
+  for (int b0 = from; b0 < B; b0 += 32) {
     if (B > 32) block(b0);
     const unsigned hit = __ballot_sync(0xffffffffu, base + incl > u);
     if (hit) {
@@ -277,18 +307,18 @@ __device__ __forceinline__ void store_out(const PagedAttnArgs& a, long long at, 
 }
 
 // Joins the parts of an item and writes its rows: o = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c.  Run by all THREADS
-// threads of the last CTA to arrive (named barrier 2 is theirs).  A part's slot is a trip to L2 away, so many loads are in
+// threads that finished the item's last part to arrive (named barrier `bar` is theirs).  A part's slot is a trip to L2 away, so many loads are in
 // flight at once: every thread first asks for its four-element pieces of the first AHEAD parts' outputs, then for maxima and
 // sums (THREADS / NR threads to a row), and goes on four parts at a time, their weights in shared memory.  s_max, s_inv: shared
 // scratch of NR floats each; w: of w_floats >= 2 * THREADS.
 template <int NR, int D, int THREADS>
-__device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCursor& c, int first, int parts, int tid, float* s_max, float* s_inv, float* w, int w_floats) {
+__device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCursor& c, int first, int parts, int tid, float* s_max, float* s_inv, float* w, int w_floats, int bar = 2) {
   const int R = c.nq * a.G, r0 = c.t * NR, live = min(NR, R - r0);
   constexpr size_t SF = slot_floats<NR, D>();
   constexpr int LANES = THREADS / NR, PIECES = NR * (D / 4) / THREADS, BLOCK = PIECES < 4 ? PIECES : 4, AHEAD = 2;
   const float* slots = a.slots + SF * (size_t)(2 * first);
   auto slot = [&](int p) { return slots + SF * (size_t)(p == 0 ? 1 : 2 * p); };   // part 0 begins in its CTA: part_slot
-  auto sync = [&]() { asm volatile("bar.sync 2, %0;" ::"n"(THREADS) : "memory"); };
+  auto sync = [&]() { asm volatile("bar.sync %0, %1;" ::"r"(bar), "n"(THREADS) : "memory"); };
   auto row = [&](int i) { return i / (D / 4); };
   auto fetch = [&](int p, int i) { return __ldcg(reinterpret_cast<const float4*>(slot(p) + 2 * NR) + i); };
   float4 early[AHEAD][BLOCK];

@@ -32,10 +32,8 @@ __global__ void __launch_bounds__(SIMT_THREADS) paged_attn_simt_kernel(const __g
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   pdl_launch_dependents();
   pdl_wait();
-  if (warp == 0) {
-    const WorkCursor c0 = cursor_begin<NR, KT>(a, s_geo);
-    if (lane == 0) s_cur = c0;
-  }
+  const WorkCursor c0 = cursor_begin<NR, KT>(a, s_geo, reinterpret_cast<long long*>(Ps));
+  if (tid == 0) s_cur = c0;
   __syncthreads();
   WorkCursor c = s_cur;
   const int dp = tid % (D / 2), rg = tid / (D / 2);

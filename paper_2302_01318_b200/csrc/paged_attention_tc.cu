@@ -197,10 +197,8 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
     pdl_launch_dependents();   // with the tensor memory in hand: a dependent on this SM that took it first would wait for this CTA
   }
   pdl_wait();
-  if (warp == 0) {
-    const WorkCursor c0 = cursor_begin<NR, TILE>(a, geo);
-    if (lane == 0) *s_cur = c0;
-  }
+  const WorkCursor c0 = cursor_begin<NR, TILE>(a, geo, s_qat);
+  if (tid == 0) *s_cur = c0;
   P_FENCE_BEFORE();
   __syncthreads();
   P_FENCE_AFTER();

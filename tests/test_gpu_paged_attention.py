@@ -129,6 +129,30 @@ def test_an_infinite_value_stays_in_its_element(types, new):
 
 
 @pytest.mark.parametrize("types", range(3))
+@pytest.mark.parametrize("B,max_q", [(33, 2), (150, 64), (1100, 2)])
+def test_batches_of_many_sequences(types, B, max_q):
+    """More than a warp reads at once, and more than 32 blocks of 32: ragged lengths, sequences without rows or tokens among
+    them; then one whose length does not fit the table."""
+    qdt, cdt, odt = TYPES[types]
+    g = torch.Generator().manual_seed(B)
+    lens = torch.randint(0, 40, (B,), generator=g).tolist()
+    lens[B // 2] = 1000                                          # cut between CTAs
+    news = [min(n, L + 1) for n, L in zip(torch.randint(0, 3, (B,), generator=g).tolist(), lens)]
+    pages = Pages(lens, 1, 64, 16, cdt)
+    out, lse, _, ws = run_attention(pages, news, 4, qdt, odt, max_q=max_q, lead=1, tail=1)
+    batch = pages.batch(news, 1, max_q)
+    last = max(b for b in range(B) if news[b])
+    batch.kv_len[last] = 10 ** 6
+    rows = out.shape[0]
+    q, again = normal((rows, 4, 64), qdt, 5, 1.5), out.clone()   # run_attention's queries
+    sps.sps_paged_attention(pages.cache, batch, q, again, ws)
+    assert int(batch.status) & sps.PAGED_BAD_LENGTH
+    end = 1 + sum(news[:last])
+    want, _, S = attention64(q, pages.dense, news, 1)
+    assert ((again.double() - want).abs() <= attention_tol(want, S, 64, qdt, odt))[1:end].all()
+
+
+@pytest.mark.parametrize("types", range(3))
 def test_sequences_that_share_a_prefix(types):
     """Two sequences whose tables begin with the same pages, each with a last page of its own."""
     qdt, cdt, odt = TYPES[types]

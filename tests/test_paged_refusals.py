@@ -140,6 +140,10 @@ def test_attention_in_place_wants_the_same_layout():
     refused(attend(q=rows(dtype=1), o=rows(dtype=0)), "in place")
 
 
+def test_more_sequences_than_the_list_of_work_counts_are_refused():
+    refused(attend(b=batch(B=(1 << 27) + 1)), "B")
+
+
 def test_a_scale_that_overflows_in_base_2_is_refused():
     """Scores are kept in base 2: scale / ln 2 has to be a number too."""
     refused(attend(scale=3e38), "scale")
