@@ -33,7 +33,10 @@
 //               with an elected lane issuing and constant offsets: descriptors stay in uniform registers (40 clocks a
 //               product; issued from a divergent lane they took 130)
 //   warps 2, 3  Q of the parts to come, into shared memory in bf16 parts
-//   warps 4..   softmax and outputs, 16 rows per group of four warps
+//   warps 4..   softmax and outputs, 16 rows per group of four warps; for tiles of 16 rows two sets of four warps, each with
+//               its own P, O and row arrays, that take the CTA's parts in turn, so that one part's outputs and join go on
+//               beside the next part's scores (64 sequences of 300 tokens, 8 key heads: 27.7 -> 24.9 us; batches of short
+//               sequences are bound by what a part costs at its ends, not by HBM)
 //
 // Every wait is bounded; on expiry the CTA sets SPS_PAGED_TIMEOUT, lets its copies and products finish, frees its tensor
 // memory and returns.
@@ -64,19 +67,21 @@ template <class Op> __device__ __forceinline__ float fold16(float (&v)[16], int 
 template <int D, int NR, int PARTS> struct Cfg {   // PARTS: of Q (1 or 3)
   static constexpr int PP = PARTS == 3 ? 3 : 2;                     // parts of P
   static constexpr int GROUPS = NR / 16;                            // column groups of four softmax warps each
-  static constexpr int SOFT = 128 * GROUPS;                         // softmax threads
-  static constexpr int THREADS = 128 + SOFT;
+  static constexpr int SETS = NR == 16 ? 2 : 1;                     // sets of softmax warps, taking parts in turn
+  static constexpr int SOFT = 128 * GROUPS;                         // softmax threads of a set
+  static constexpr int THREADS = 128 + SETS * SOFT;
   static constexpr int N = PARTS * NR, NO = PP * NR;                // columns of S and O
   static constexpr uint32_t HALF = TILE * D * 2;                    // keys or values of a tile
-  static constexpr uint32_t Q_BYTES = N * D * 2, P_BYTES = TILE * NO * 2;
-  static constexpr uint32_t HDR = 4224;                             // barriers, small per-row arrays
-  static constexpr int BUDGET = 232448 - (int)HDR - (int)P_BYTES;
+  static constexpr uint32_t Q_BYTES = N * D * 2, P_BYTES = TILE * NO * 2;   // (P: of a set)
+  static constexpr uint32_t HDR = 4352;                             // barriers, small per-row arrays
+  static constexpr int SET_BYTES = NR * 4 * 9 + 16;                 // a set's share of them
+  static constexpr int BUDGET = 232448 - (int)HDR - SETS * (int)P_BYTES;
   static constexpr int QBUF = (BUDGET - 2 * (int)Q_BYTES) / (int)HALF >= 4 ? 2 : 1;
   static constexpr int STAGES_FIT = (BUDGET - QBUF * (int)Q_BYTES) / (int)HALF;
   static constexpr int STAGES = STAGES_FIT > 8 ? 8 : STAGES_FIT;
-  static constexpr uint32_t Q_AT = STAGES * HALF, P_AT = Q_AT + QBUF * Q_BYTES, HDR_AT = P_AT + P_BYTES;
+  static constexpr uint32_t Q_AT = STAGES * HALF, P_AT = Q_AT + QBUF * Q_BYTES, HDR_AT = P_AT + SETS * P_BYTES;
   static constexpr size_t SMEM = HDR_AT + HDR;
-  static constexpr int COLUMNS = 2 * N + NO;                        // of tensor memory: S twice, O once
+  static constexpr int COLUMNS = 2 * N + SETS * NO;                 // of tensor memory: S twice, O once for each set
   static constexpr uint32_t TMEM = COLUMNS <= 64 ? 64 : (COLUMNS <= 128 ? 128 : (COLUMNS <= 256 ? 256 : 512));
   // P^T is the B operand of O, MN-major under the 32-byte swizzle: blocks of 16 columns x 128 tokens, 32 bytes per token
   static constexpr uint32_t P_BLOCK = TILE * 32;
@@ -166,33 +171,37 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
   const PagedAttnArgs& a = ta.a;
   const uint32_t ring = p_smem(mem), hb = ring + C::HDR_AT;
   unsigned char* hdr = mem + C::HDR_AT;
-  const uint32_t full = hb, empty = hb + 64, s_full = hb + 128, s_free = hb + 144, p_full = hb + 160, pv_done = hb + 168, q_ready = hb + 176, q_free = hb + 192, drain = hb + 208, q_first = hb + 376;
-  volatile uint32_t* s_tmem = reinterpret_cast<volatile uint32_t*>(hdr + 216);
-  volatile int* s_abort = reinterpret_cast<volatile int*>(hdr + 220);
-  int* s_poison = reinterpret_cast<int*>(hdr + 224);
-  int* s_last = reinterpret_cast<int*>(hdr + 228);
-  WorkCursor* s_cur = reinterpret_cast<WorkCursor*>(hdr + 232);
-  SeqGeom* geo = reinterpret_cast<SeqGeom*>(hdr + 384);                // [GEO]
-  int* s_lim = reinterpret_cast<int*>(hdr + 896);                      // [NR] last position a row sees
-  float* s_a = reinterpret_cast<float*>(hdr + 896 + NR * 4);           // [NR] maxima
+  // s_full: by set and buffer of S; p_full, pv_done: by set
+  const uint32_t full = hb, empty = hb + 64, s_full = hb + 128, s_free = hb + 160, p_full = hb + 176, pv_done = hb + 192, q_ready = hb + 208, q_free = hb + 224, drain = hb + 240, q_first = hb + 248;
+  volatile uint32_t* s_tmem = reinterpret_cast<volatile uint32_t*>(hdr + 256);
+  volatile int* s_abort = reinterpret_cast<volatile int*>(hdr + 260);
+  WorkCursor* s_cur = reinterpret_cast<WorkCursor*>(hdr + 272);
+  SeqGeom* geo = reinterpret_cast<SeqGeom*>(hdr + 416);                // [GEO]
+  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  const int set = C::SETS > 1 && warp >= 4 + SOFT / 32 ? 1 : 0;
+  unsigned char* own = hdr + 928 + set * C::SET_BYTES;                 // the set's arrays
+  int* s_lim = reinterpret_cast<int*>(own);                            // [NR] last position a row sees
+  float* s_a = reinterpret_cast<float*>(own + NR * 4);                 // [NR] maxima
   float* s_b = s_a + NR;                                               // [NR] sums / factors
   float* s_red = s_b + NR;                                             // [4][NR]
   long long* s_off = reinterpret_cast<long long*>(s_red + 4 * NR);     // [NR] where a row's output goes
-  long long* s_qat = s_off + NR;                                       // [2][NR] where a row of Q is (loader, first part)
-  static_assert(896 + NR * 4 * 13 <= (int)C::HDR && sizeof(WorkCursor) <= 144 && sizeof(SeqGeom) * GEO <= 512, "header");
-  const int tid = threadIdx.x, warp = __shfl_sync(0xffffffffu, tid >> 5, 0), lane = tid & 31;
+  int* s_poison = reinterpret_cast<int*>(s_off + NR);
+  int* s_last = s_poison + 1;
+  long long* s_qat = reinterpret_cast<long long*>(hdr + 928 + C::SETS * C::SET_BYTES);   // [2][NR] where a row of Q is (loader, first part)
+  static_assert(928 + C::SETS * C::SET_BYTES + 16 * NR <= (int)C::HDR && sizeof(WorkCursor) <= 144 && sizeof(SeqGeom) * GEO <= 512, "header");
 
   if (tid == 0) {
     for (int i = 0; i < STAGES; ++i) { p_bar_init(full + 8 * i, 1); p_bar_init(empty + 8 * i, 1); }
-    for (int i = 0; i < 2; ++i) { p_bar_init(s_full + 8 * i, 1); p_bar_init(s_free + 8 * i, SOFT); p_bar_init(q_ready + 8 * i, 64); p_bar_init(q_free + 8 * i, 1); }
-    p_bar_init(p_full, SOFT); p_bar_init(q_first, SOFT); p_bar_init(pv_done, 1); p_bar_init(drain, 1);
+    for (int i = 0; i < 2; ++i) { p_bar_init(s_free + 8 * i, SOFT); p_bar_init(q_ready + 8 * i, 64); p_bar_init(q_free + 8 * i, 1); p_bar_init(p_full + 8 * i, SOFT); p_bar_init(pv_done + 8 * i, 1); }
+    for (int i = 0; i < 4; ++i) p_bar_init(s_full + 8 * i, 1);
+    p_bar_init(q_first, SOFT); p_bar_init(drain, 1);
     *s_abort = 0;
     asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&ta.tm_k) : "memory");
     asm volatile("prefetch.tensormap [%0];" ::"l"(&ta.tm_v) : "memory");
   }
   if (warp == 1) {
-    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(hb + 216), "n"(C::TMEM) : "memory");
+    asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(hb + 256), "n"(C::TMEM) : "memory");
     asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
     pdl_launch_dependents();   // with the tensor memory in hand: a dependent on this SM that took it first would wait for this CTA
   }
@@ -211,7 +220,9 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
     // ---------------------------------------------------------------------------------------------------- products
     const bool leader = p_elect();
     bool ok = true;
-    int e_s = 0, e_o = 1, sn = 0, pn = 0, qn = 0, s_i = 0;   // half-tiles of the next S and O, products so far, parts so far, S's tile in its part
+    int e_s = 0, e_o = 1, sn = 0, qn = 0, s_i = 0;             // half-tiles of the next S and O, scores so far, parts so far, S's tile in its part
+    int on = 0;                                                // parts whose O is done
+    uint32_t p_phase = 0;                                      // parity of p_full, a bit for each set
     WorkCursor cs = c;                                         // the part S is at; c is the part O is at
     auto wait = [&](uint32_t bar, uint32_t parity) {
       if (ok) ok = __all_sync(0xffffffffu, p_wait(bar, parity & 1u, a.wait_ns, a.s.status, s_abort));
@@ -234,7 +245,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
         for (int k = 0; k < D / 16; ++k)
           p_mma(d, ka + (k >> 2) * (TILE * 128 >> 4) + (k & 3) * 2, p_desc_hi(1024, 2), qa + (k >> 2) * (N * 128 >> 4) + (k & 3) * 2, p_desc_hi(1024, 2), C::IDESC_S, k > 0);
         p_commit(empty + 8 * (e_s % STAGES));
-        p_commit(s_full + 8 * buf);
+        p_commit(s_full + 16 * (qn % C::SETS) + 8 * buf);
         if (last) p_commit(q_free + 8 * qb);
       }
       __syncwarp();
@@ -244,24 +255,26 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
     };
     score();
     while (c.valid && ok) {
+      const int g = on % C::SETS;
       for (int n = c.k1 - c.k0; n > 0 && ok; --n) {
         score();
-        wait(p_full, (uint32_t)pn);
+        wait(p_full + 8 * g, p_phase >> g);
         wait(full + 8 * (e_o % STAGES), (uint32_t)(e_o / STAGES));
         if (!ok) break;
         P_FENCE_AFTER();
         if (leader) {
-          const uint32_t va = p_desc_lo(ring + (uint32_t)(e_o % STAGES) * C::HALF, TILE * 128), pa = p_desc_lo(ring + C::P_AT, C::P_BLOCK);
+          const uint32_t va = p_desc_lo(ring + (uint32_t)(e_o % STAGES) * C::HALF, TILE * 128), pa = p_desc_lo(ring + C::P_AT + g * C::P_BYTES, C::P_BLOCK);
 #pragma unroll
           for (int k = 0; k < TILE / 16; ++k)
-            p_mma(tmem_o, va + k * (16 * 128 >> 4), p_desc_hi(1024, 2), pa + k * (16 * 32 >> 4), p_desc_hi(256, 6), C::IDESC_O, k > 0);
+            p_mma(tmem_o + g * C::NO, va + k * (16 * 128 >> 4), p_desc_hi(1024, 2), pa + k * (16 * 32 >> 4), p_desc_hi(256, 6), C::IDESC_O, k > 0);
           p_commit(empty + 8 * (e_o % STAGES));
-          p_commit(pv_done);
+          p_commit(pv_done + 8 * g);
         }
         __syncwarp();
         e_o += 2;
-        ++pn;
+        p_phase ^= 1u << g;
       }
+      ++on;
       cursor_next<NR, TILE>(a, c, geo);
     }
     if (!ok) {   // every product issued so far must be done before the ring and the tensor memory go away
@@ -285,19 +298,25 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
     }
   } else {
     // ---------------------------------------------------------------------------------------------------- softmax
-    const int st = tid - 128, quarter = warp & 3, group = (warp - 4) >> 2, col0 = group * 16;
+    const int st = tid - 128 - set * SOFT, quarter = warp & 3, group = C::SETS > 1 ? 0 : (warp - 4) >> 2, col0 = group * 16;
     const int my = quarter * 32 + lane;                       // token of the tile, and row of O^T (for d = 128)
     const uint32_t t_lane = (uint32_t)(quarter * 32) << 16;
     // After a wait that ran out the softmax threads keep their common path -- barriers among them always meet -- and skip
     // the waits, until they agree at the part's end to stop.
     bool ok = true;
-    int sn = 0, pn = 0, it = 0;
-    auto all_sync = [&]() { asm volatile("bar.sync 1, %0;" ::"n"(SOFT) : "memory"); };
-    auto group_sync = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(3 + group) : "memory"); };
-    if (c.valid) {
+    int pn = 0, it = 0;                                       // outputs awaited (the set's); half-tiles of the parts before (both sets')
+    uint32_t s_phase = 0;                                     // parity of s_full, a bit for each buffer
+    auto all_sync = [&]() { asm volatile("bar.sync %0, %1;" ::"r"(1 + 8 * set), "n"(SOFT) : "memory"); };
+    auto group_sync = [&]() { asm volatile("bar.sync %0, 128;" ::"r"(3 + group + 8 * set) : "memory"); };
+    if (c.valid && set == 0) {
       ok = load_q<D, NR, PARTS, SOFT>(a, c, mem + C::Q_AT, s_qat + NR, st, 1, []() { return true; });
       p_arrive(q_first);
     }
+    auto next_part = [&]() {
+      it += 2 * (c.k1 - c.k0);
+      cursor_next<NR, TILE>(a, c, geo);
+    };
+    if (set == 1 && c.valid) next_part();
     while (c.valid) {
       const int R = c.nq * a.G, r0 = c.t * NR, n = c.k1 - c.k0, first_lim = c.len - c.nq + row_token(a, r0);
       if (st < NR) {
@@ -317,12 +336,12 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
       auto collect = [&]() {
         if (!held) return;
         held = false;
-        ok = ok && p_wait(pv_done, (uint32_t)(pn - 1) & 1u, a.wait_ns, a.s.status, s_abort);
+        ok = ok && p_wait(pv_done + 8 * set, (uint32_t)(pn - 1) & 1u, a.wait_ns, a.s.status, s_abort);
         __syncwarp();
         P_FENCE_AFTER();
         float t[PP][16];
 #pragma unroll
-        for (int part = 0; part < PP; ++part) p_ld16(tmem_o + t_lane + part * NR + col0, t[part]);
+        for (int part = 0; part < PP; ++part) p_ld16(tmem_o + set * C::NO + t_lane + part * NR + col0, t[part]);
         P_WAIT_LD();
         p_landed<PP * 16>(t[0]);
 #pragma unroll
@@ -332,10 +351,11 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
           p_add2(o[j], o[j + 1], t[0][j], t[0][j + 1]);
         }
       };
-      for (int i = 0; i < n; ++i, ++sn, it += 2) {
-        const int buf = sn & 1, p0 = (c.k0 + i) * TILE, pos = p0 + my;
+      for (int i = 0; i < n; ++i) {
+        const int buf = ((it >> 1) + i) & 1, p0 = (c.k0 + i) * TILE, pos = p0 + my;
         const bool edge = p0 + TILE - 1 > first_lim;          // some row does not see all of this tile
-        ok = ok && p_wait(s_full + 8 * buf, (uint32_t)(sn >> 1) & 1u, a.wait_ns, a.s.status, s_abort);
+        ok = ok && p_wait(s_full + 16 * set + 8 * buf, (s_phase >> buf) & 1u, a.wait_ns, a.s.status, s_abort);
+        s_phase ^= 1u << buf;
         __syncwarp();
         P_FENCE_AFTER();
         float x[16];
@@ -385,7 +405,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
         }
         uint32_t retake;
         asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.or.pred p, %2, 128, q;\n selp.u32 %0, 1, 0, p;\n}\n"
-                     : "=r"(retake) : "r"(up > MAX_UP ? 1u : 0u), "r"(3 + group) : "memory");
+                     : "=r"(retake) : "r"(up > MAX_UP ? 1u : 0u), "r"(3 + group + 8 * set) : "memory");
         if (retake) {
           float y[16];
 #pragma unroll
@@ -419,7 +439,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
         if (edge) {
           // slots behind the sequence hold anything: zero (0 x NaN is NaN in a product).  New tokens some rows do not see:
           // a value that is not finite is taken out and remembered, its rows become NaN at the end.
-          const int e = it + 1;
+          const int e = it + 2 * i + 1;
           ok = ok && p_wait(full + 8 * (e % STAGES), (uint32_t)(e / STAGES) & 1u, a.wait_ns, a.s.status, s_abort);
           if (ok && group == 0 && pos > first_lim) {
             unsigned char* vr = mem + (e % STAGES) * C::HALF + my * 128;
@@ -444,7 +464,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
             }
           }
         }
-        unsigned char* pr = mem + C::P_AT + group * C::P_BLOCK + my * 32;
+        unsigned char* pr = mem + C::P_AT + set * C::P_BYTES + group * C::P_BLOCK + my * 32;
         const int sw = (my >> 2) & 1;                          // 32-byte swizzle: a token's two 16-byte chunks swap in every other group of 4
 #pragma unroll
         for (int k = 0; k < 2; ++k) {
@@ -462,7 +482,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
         }
         asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         P_FENCE_BEFORE();
-        p_arrive(p_full);
+        p_arrive(p_full + 8 * set);
         ++pn;
         held = true;
       }
@@ -472,8 +492,8 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
       collect();
       {
         uint32_t all;
-        asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.and.pred p, 1, %2, q;\n selp.u32 %0, 1, 0, p;\n}\n"
-                     : "=r"(all) : "r"(ok ? 1u : 0u), "n"(SOFT) : "memory");
+        asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.and.pred p, %2, %3, q;\n selp.u32 %0, 1, 0, p;\n}\n"
+                     : "=r"(all) : "r"(ok ? 1u : 0u), "r"(1 + 8 * set), "n"(SOFT) : "memory");
         if (!all) break;
       }
       if (st < NR) {
@@ -525,10 +545,11 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
           *s_last = part_arrive(a.counters + first, parts);
         }
         all_sync();
-        if (*s_last) join_parts<NR, D, SOFT>(a, c, first, parts, st, s_b, s_a, reinterpret_cast<float*>(mem + C::P_AT), C::P_BYTES / 4);
+        if (*s_last) join_parts<NR, D, SOFT>(a, c, first, parts, st, s_b, s_a, reinterpret_cast<float*>(mem + C::P_AT + set * C::P_BYTES), C::P_BYTES / 4, 2 + 8 * set);
       }
       all_sync();   // s_a, s_b, s_lim are free again
-      cursor_next<NR, TILE>(a, c, geo);
+      next_part();
+      if (C::SETS > 1 && c.valid) next_part();   // the other set's
     }
     if (!ok) *s_abort = 1;
   }
@@ -544,8 +565,9 @@ template <int D, int NR, int PARTS>
 cudaError_t tc_go(PagedAttnArgs a, int num_sm, cudaStream_t st) {
   static DevSmemCache cached{};
   // An item costs about two tiles before its first one (Q, the first scores, its outputs): 64 ragged sequences of one token
-  // took 103 / 82 / 61 / 62 / 65 us at 0 / 1 / 2 / 3 / 4; longer least runs than one tile only slowed short calls down.
-  a.lead = 2;
+  // took 103 / 82 / 61 / 62 / 65 us at 0 / 1 / 2 / 3 / 4 with one set of softmax warps, 57 / 60 / 64 at 1 / 2 / 3 with two;
+  // longer least runs than one tile only slowed short calls down.
+  a.lead = Cfg<D, NR, PARTS>::SETS == 2 ? 1 : 2;
   a.min_run = 1;
   TcArgs t;
   cudaError_t e = tc_args(a, D, &t);
