@@ -13,7 +13,10 @@
 // Running maximum.  The weights are 2^(s - m) with m fixed at the score of the part's first token, which every row that sees
 // anything of the part sees: P is bf16 parts (8 exponent bits) of an fp32 number, sums are fp32, so m only has to keep the
 // weights in range, not at most 1, and a weight of 1 is among them.  Only when a score exceeds m by MAX_UP (in base 2) do
-// the threads of a column group agree (a reducing barrier) to take the new maximum and rescale what they hold.  That leaves a multiply-add, an exponential, an addition and the rounding per score, no
+// the threads of a column group agree (a reducing barrier) to take the new maximum and rescale what they hold.  The tile's
+// differences are then taken again from its raw scores: those to a first token that scored far below the others were
+// rounded at its size.  A first score of -inf leaves the least finite number as m, which any finite score outgrows.  That
+// leaves a multiply-add, an exponential, an addition and the rounding per score, no
 // cross-lane reduction per tile.  Sums stay per thread (its token of every tile) until the part ends.  Each tile's O^T
 // is a product of its own, added to fp32 registers: the tensor cores cut the low bits of a running sum instead of rounding
 // them, which over a context of 32 768 tokens cost 3.6e-5 of the result.
@@ -45,6 +48,7 @@
 namespace {
 
 constexpr float MAX_UP = 24.f;       // log2 of the largest weight that is let stand
+constexpr float LEAST = -3.402823466e38f;   // the reference of rows that have seen no finite score yet
 
 // Reduces v[c] over the 32 lanes for 16 columns, halving the columns a lane carries at every step; the lane ends up with
 // column lane >> 1.
@@ -359,7 +363,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
         __syncwarp();
         P_FENCE_AFTER();
         float x[16];
-        {
+        auto scores = [&]() {                                 // x = S of this thread's token
           float t[PARTS][16];
 #pragma unroll
           for (int part = 0; part < PARTS; ++part) p_ld16(tmem + buf * N + t_lane + part * NR + col0, t[part]);
@@ -374,61 +378,70 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
             x[j] = t[0][j];
             x[j + 1] = t[0][j + 1];
           }
-        }
-        P_FENCE_BEFORE();
-        p_arrive(s_free + 8 * buf);
+        };
+        scores();
         // ---- the reference maximum: the part's first token's score, a new one only when a score has outgrown it
         if (i == 0) {
           if (my == 0) {
 #pragma unroll
             for (int j = 0; j < 16; ++j) {
               const float s = x[j] * a.scale_log2;
-              s_a[col0 + j] = s_lim[col0 + j] < pos || s == -INFINITY ? 0.f : s;
+              s_a[col0 + j] = s_lim[col0 + j] < pos ? 0.f : (fabsf(s) == INFINITY ? LEAST : s);
             }
           }
           group_sync();
         }
+        // x -> scale x - m, rounded once, -inf where a row does not see the token
+        auto relative = [&](const float* ref) {
+#pragma unroll
+          for (int j = 0; j < 16; j += 4) {
+            const float4 m = *reinterpret_cast<const float4*>(ref + j);
+            p_fma2(x[j], x[j + 1], a.scale_log2, -m.x, -m.y);
+            p_fma2(x[j + 2], x[j + 3], a.scale_log2, -m.z, -m.w);
+            if (edge) {
+              const int4 lim = *reinterpret_cast<const int4*>(s_lim + col0 + j);
+              x[j] = pos <= lim.x ? x[j] : -INFINITY;
+              x[j + 1] = pos <= lim.y ? x[j + 1] : -INFINITY;
+              x[j + 2] = pos <= lim.z ? x[j + 2] : -INFINITY;
+              x[j + 3] = pos <= lim.w ? x[j + 3] : -INFINITY;
+            }
+          }
+        };
+        relative(s_a + col0);
         float up = -INFINITY;
 #pragma unroll
-        for (int j = 0; j < 16; j += 4) {   // x becomes s - m
-          const float4 m = *reinterpret_cast<const float4*>(s_a + col0 + j);
-          p_fma2(x[j], x[j + 1], a.scale_log2, -m.x, -m.y);
-          p_fma2(x[j + 2], x[j + 3], a.scale_log2, -m.z, -m.w);
-          if (edge) {
-            const int4 lim = *reinterpret_cast<const int4*>(s_lim + col0 + j);
-            x[j] = pos <= lim.x ? x[j] : -INFINITY;
-            x[j + 1] = pos <= lim.y ? x[j + 1] : -INFINITY;
-            x[j + 2] = pos <= lim.z ? x[j + 2] : -INFINITY;
-            x[j + 3] = pos <= lim.w ? x[j + 3] : -INFINITY;
-          }
-          up = fmaxf(up, fmaxf(fmaxf(x[j], x[j + 1]), fmaxf(x[j + 2], x[j + 3])));
-        }
+        for (int j = 0; j < 16; j += 4) up = fmaxf(up, fmaxf(fmaxf(x[j], x[j + 1]), fmaxf(x[j + 2], x[j + 3])));
         uint32_t retake;
         asm volatile("{\n .reg .pred p, q;\n setp.ne.u32 q, %1, 0;\n bar.red.or.pred p, %2, 128, q;\n selp.u32 %0, 1, 0, p;\n}\n"
                      : "=r"(retake) : "r"(up > MAX_UP ? 1u : 0u), "r"(3 + group + 8 * set) : "memory");
         if (retake) {
-          float y[16];
+          scores();
+          {
+            float y[16];
 #pragma unroll
-          for (int j = 0; j < 16; ++j) y[j] = x[j];
-          const float top = fold16<OpMax>(y, lane);
-          s_red[quarter * NR + col0 + (lane >> 1)] = top;
+            for (int j = 0; j < 16; ++j) y[j] = !edge || pos <= s_lim[col0 + j] ? x[j] * a.scale_log2 : -INFINITY;
+            const float top = fold16<OpMax>(y, lane);
+            s_red[quarter * NR + col0 + (lane >> 1)] = top;
+          }
           collect();
           group_sync();
+          float m_new = 0.f;                                  // (of column col0 + my, for the group's first 16 threads)
 #pragma unroll
-          for (int j = 0; j < 16; ++j) {   // what the maximum rises by, if anything
+          for (int j = 0; j < 16; ++j) {
             const int cc = col0 + j;
-            y[j] = fmaxf(fmaxf(fmaxf(s_red[cc], s_red[NR + cc]), fmaxf(s_red[2 * NR + cc], s_red[3 * NR + cc])), 0.f);
-            const float al = p_ex2(-y[j]);
-            l[j] *= al;
+            const float was = s_a[cc], m = fmaxf(fmaxf(fmaxf(s_red[cc], s_red[NR + cc]), fmaxf(s_red[2 * NR + cc], s_red[3 * NR + cc])), was);
+            const float al = p_ex2(was - m);
+            l[j] = m == INFINITY ? __int_as_float(0x7fffffff) : l[j] * al;   // an infinite score that the row sees
             o[j] *= al;
-            x[j] -= y[j];
+            if (my == j) m_new = m;
           }
-          if (my == 0) {
-#pragma unroll
-            for (int j = 0; j < 16; ++j) s_a[col0 + j] += y[j];
-          }
-          group_sync();   // s_red may be written again, s_a read
+          group_sync();                                       // s_a has been read
+          if (my < 16) s_a[col0 + my] = m_new;
+          group_sync();                                       // ... written, s_red may be
+          relative(s_a + col0);
         }
+        P_FENCE_BEFORE();
+        p_arrive(s_free + 8 * buf);
         // ---- weights
 #pragma unroll
         for (int j = 0; j < 16; ++j) x[j] = p_ex2(x[j]);
