@@ -11,7 +11,9 @@
 //
 // Running maximum.  m is fixed at the maximum of the part's first tile and raised only when a score exceeds it by MAX_UP (in
 // base 2): bf16 weights and fp32 sums keep their relative precision at any size, so this loses nothing, and O stays
-// untouched in tensor memory from tile to tile.  A warp whose rows do outgrow m rescales their O itself.
+// untouched in tensor memory from tile to tile.  A warp whose rows do outgrow m rescales their O itself, and takes the tile's
+// raw scores from tensor memory once more: their differences to an m far below them were rounded at its size.  Until a row
+// has a finite score m is the least finite number, which any such score outgrows.
 //
 // What bounds it: the tensor cores, 4 x 8 products of 64 clocks per pair of tiles (d = 128); they work on one tile while
 // the other one's softmax runs.
@@ -30,6 +32,7 @@
 namespace {
 
 constexpr float MAX_UP = 24.f;       // log2 of the largest weight that is let stand
+constexpr float LEAST = -3.402823466e38f;   // the reference of a row that has seen no finite score yet
 constexpr int W_ROWS = 256;          // rows of an item: two tiles
 constexpr int W_THREADS = 512;
 
@@ -249,7 +252,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
       const bool work = w == 0 || R - c.t * NR > 128;          // the second tile may be empty
       if (st == 0) *s_poison = 0x7fffffff;
       asm volatile("bar.sync 1, 256;" ::: "memory");
-      float m = 0.f, l = 0.f;
+      float m = LEAST, l = 0.f;
       if (work) {
         const int warp_lim = __shfl_sync(0xffffffffu, lim < 0 && r >= R ? 0x7fffffff : lim, 0);   // the least of the warp's live rows' (rows ascend)
         for (int i = 0; i < n; ++i, ++sn) {
@@ -282,53 +285,57 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
           ok = ok && p_wait(s_full + 8 * w, sn & 1u, a.wait_ns, a.s.status, s_abort);
           __syncwarp();
           P_FENCE_AFTER();
-          float x[128];
+          float x[128], up;
+          bool fresh = i == 0;                                  // x is scale s, from which a new m is taken, not scale s - m
+          for (;;) {
+            const float ref = fresh ? 0.f : -m;
 #pragma unroll
-          for (int j = 0; j < 128; j += 32) p_ld32(t_s + j, x + j);
-          P_WAIT_LD();
-          p_landed<128>(x);
+            for (int j = 0; j < 128; j += 32) p_ld32(t_s + j, x + j);
+            P_WAIT_LD();
+            p_landed<128>(x);
 #pragma unroll
-          for (int j = 0; j < 128; j += 2) p_fma2(x[j], x[j + 1], a.scale_log2, -m, -m);
-          if (p0 + TILE - 1 > warp_lim || r >= R) {
-            const int d = lim - p0;                             // last token of the tile this row sees
+            for (int j = 0; j < 128; j += 2) p_fma2(x[j], x[j + 1], a.scale_log2, ref, ref);
+            if (p0 + TILE - 1 > warp_lim || r >= R) {
+              const int d = lim - p0;                             // last token of the tile this row sees
 #pragma unroll
-            for (int j = 0; j < 128; ++j) x[j] = j <= d ? x[j] : -INFINITY;
+              for (int j = 0; j < 128; ++j) x[j] = j <= d ? x[j] : -INFINITY;
+            }
+            float u0 = x[0], u1 = x[1], u2 = x[2], u3 = x[3];
+#pragma unroll
+            for (int j = 4; j < 124; j += 8) {
+              u0 = w_max3(u0, x[j], x[j + 1]);
+              u1 = w_max3(u1, x[j + 2], x[j + 3]);
+              u2 = w_max3(u2, x[j + 4], x[j + 5]);
+              u3 = w_max3(u3, x[j + 6], x[j + 7]);
+            }
+            u0 = w_max3(u0, x[124], x[125]);
+            u1 = w_max3(u1, x[126], x[127]);
+            up = w_max3(w_max3(u0, u1, u2), u3, u3);
+            if (fresh || !__any_sync(0xffffffffu, !(up <= MAX_UP))) break;
+            fresh = true;
           }
-          float u0 = x[0], u1 = x[1], u2 = x[2], u3 = x[3];
-#pragma unroll
-          for (int j = 4; j < 124; j += 8) {
-            u0 = w_max3(u0, x[j], x[j + 1]);
-            u1 = w_max3(u1, x[j + 2], x[j + 3]);
-            u2 = w_max3(u2, x[j + 4], x[j + 5]);
-            u3 = w_max3(u3, x[j + 6], x[j + 7]);
-          }
-          u0 = w_max3(u0, x[124], x[125]);
-          u1 = w_max3(u1, x[126], x[127]);
-          const float up = w_max3(w_max3(u0, u1, u2), u3, u3);
-          if (i == 0) {
-            m = up == -INFINITY ? 0.f : up;
-            if (!(up < INFINITY)) l = __int_as_float(0x7fffffff);   // an infinite or NaN score that the row sees
+          if (fresh) {
+            const float was = m;
+            m = up > m ? up : m;
 #pragma unroll
             for (int j = 0; j < 128; j += 2) p_add2(x[j], x[j + 1], -m, -m);
-          } else if (__any_sync(0xffffffffu, !(up <= MAX_UP))) {
-            // these rows' O takes the factor too; every product so far is in it: S of this tile came after them
-            const float rise = up > MAX_UP ? up : 0.f, f = p_ex2(-rise);
-            if (!(up < INFINITY)) l = __int_as_float(0x7fffffff);
-            m += rise;
-            l *= f;
-#pragma unroll
-            for (int j = 0; j < 128; j += 2) p_add2(x[j], x[j + 1], -rise, -rise);
+            if (i > 0) {
+              // these rows' O takes the factor too; every product so far is in it: S of this tile came after them
+              const float f = p_ex2(was - m);
+              l *= f;
 #pragma unroll 1
-            for (int j = 0; j < D; j += 16) {
-              float o[16];
-              p_ld16(t_o + j, o);
-              P_WAIT_LD();
-              p_landed<16>(o);
-              uint32_t u[16];
+              for (int j = 0; j < D; j += 16) {
+                float o[16];
+                p_ld16(t_o + j, o);
+                P_WAIT_LD();
+                p_landed<16>(o);
+                uint32_t u[16];
 #pragma unroll
-              for (int q = 0; q < 16; ++q) u[q] = __float_as_uint(o[q] * f);
-              p_st16(t_o + j, u);
+                for (int q = 0; q < 16; ++q) u[q] = __float_as_uint(o[q] * f);
+                p_st16(t_o + j, u);
+              }
             }
+            if (!(up < INFINITY)) l = __int_as_float(0x7fffffff);   // an infinite or NaN score that the row sees
           }
           float l1 = 0.f, l2 = 0.f, l3 = 0.f;
 #pragma unroll

@@ -74,3 +74,27 @@ def test_a_score_of_minus_infinity_ahead_of_very_low_ones(types, d, new):
     q[..., -1] = 2.0
     out, lse = attend(pages, q, [new, new], odt)
     check_precision(out, lse, q, pages.dense, [new, new])
+
+
+@pytest.mark.parametrize("score", LOW)
+@pytest.mark.parametrize("below", [0.0, -300.0])             # of the other scores
+@pytest.mark.parametrize("new", [9, 40])                     # 72 and 320 rows of a key head: one or both tiles of 128, several items
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("types", range(len(TYPES)))
+def test_whole_tiles_of_low_scores_ahead_of_the_others(types, d, new, below, score):
+    """The first 128 tokens, and in the second sequence every other tile of 128."""
+    qdt, cdt, odt = TYPES[types]
+    pages = Pages([700, 5000], 1, d, 16, cdt)
+    q = normal((2 * new, 8, d), qdt, 1, 1.5)
+    for b in range(2):
+        L = pages.dense[b][0].shape[0]
+        j = torch.arange(L, device=DEV)
+        k = pages.dense[b][0].clone()
+        lower(k, j // 128 % 2 == 0 if b else j < 128, score, q)
+        if below:
+            q[..., -2] = 16.0
+            k[..., -2] = below / 16 * d ** 0.5
+        put(pages, b, k)
+    q[..., -1] = 2.0
+    out, lse = attend(pages, q, [new, new], odt)
+    check_precision(out, lse, q, pages.dense, [new, new])
