@@ -435,8 +435,9 @@ typedef struct {
  * not appended, and read as zeros); the last two also set a bit of *status, which the calls never clear. */
 #define SPS_PAGED_BAD_PAGE 1    /* bits of *status */
 #define SPS_PAGED_BAD_LENGTH 2
-#define SPS_PAGED_TIMEOUT 4     /* a bounded wait inside the attention kernel ran out: the call's outputs are meaningless,
-                                   and its workspace wants zeroes again */
+#define SPS_PAGED_TIMEOUT 4     /* a bounded wait inside the attention kernel ran out: rows the call did not finish are NaN
+                                   (log-sum-exp too), others may be; until its workspace is zero-filled again every
+                                   call on it sets this bit and makes its rows NaN */
 typedef struct {
   const int32_t* q_start; /* device [B + 1], not decreasing      */
   const int32_t* kv_len;  /* device [B]                          */

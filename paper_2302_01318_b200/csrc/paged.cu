@@ -453,8 +453,9 @@ static const char* bad_heads(const sps_paged_cache* c, int n_heads, int q_dtype)
   return nullptr;
 }
 
-// workspace: arrival counters and records of up to 1024 CTAs, then two part slots for each CTA
-#define PAGED_COUNTER_BYTES 4096
+// workspace: arrival counters of up to 1024 CTAs, a line for the word that a call leaves which gave up, records of up to 1024
+// CTAs, then two part slots for each CTA
+#define PAGED_COUNTER_BYTES (4096 + 128)
 #define PAGED_RECORD_BYTES (1024 * sizeof(PartRecord))
 
 int64_t sps_paged_attention_workspace_bytes(const sps_paged_cache* cache, int32_t n_heads, int32_t q_dtype) {
@@ -495,6 +496,7 @@ int sps_paged_attention(const sps_paged_cache* cache, const sps_paged_batch* bat
   a.scale_log2 = (scale == 0.f ? 1.f / std::sqrt((float)cache->d_head) : scale) * 1.4426950408889634f;
   a.lse = lse;
   a.counters = (int*)workspace;
+  a.gave_up = a.counters + 1024;
   a.records = (PartRecord*)((char*)workspace + PAGED_COUNTER_BYTES);
   a.slots = (float*)((char*)workspace + PAGED_COUNTER_BYTES + PAGED_RECORD_BYTES);
   a.wait_ns = sps_wait_knobs().limit_ns;

@@ -64,6 +64,7 @@ struct PagedAttnArgs {
   float* lse;               // [rows][H] or null
   int* counters;            // [grid] arrivals at an item, by the first CTA that works on it; zero between launches
   PartRecord* records;      // [grid] (kernels whose parts another kernel joins)
+  int* gave_up;             // not 0: a wait of this call, or of an earlier one on this workspace, ran out
   uint32_t grid_magic;      // ceil(2^32 / CTAs), and the numbers below which its high product divides by them
   int grid_magic_to;
   int lead, min_run;        // set by the launcher: an item's cost ahead of its tiles, the least run, in tiles
@@ -93,6 +94,7 @@ struct WorkCursor {       // a place in the list of items, and the run that is l
   long long item0;        // place of the item's first tile in the list (its lead lies before it)
   long long per;          // length of a run
   bool valid;
+  int spoilt;             // not 0: the workspace holds what a call left that gave up, nothing is worked on
 };
 constexpr int GEO = 32;   // sequences a CTA keeps in shared memory, from its first on
 
@@ -163,6 +165,8 @@ __device__ __forceinline__ WorkCursor cursor_begin(const PagedAttnArgs& a, SeqGe
   const int warp = __shfl_sync(0xffffffffu, threadIdx.x >> 5, 0), lane = threadIdx.x & 31, B = a.s.B;
   WorkCursor c;
   c.valid = false;
+  c.spoilt = 0;
+  if (warp == 0) c.spoilt = __ldcg(a.gave_up);   // (one request a CTA: all of them ask for the same word)
   SeqGeom g{};                   // the sequences of one block of 32, a lane each; their work, and the sum up to each
   long long head = 0, units = 0, incl = 0, total = 0;   // head: of one key head
   auto block = [&](int b0) {
@@ -404,6 +408,19 @@ __device__ __forceinline__ void join_parts(const PagedAttnArgs& a, const WorkCur
       }
     }
   }
+}
+
+// The rows of a call that gave up, or that found its workspace spoilt by one: NaN, so that no caller takes them for answers.
+// Share `share` of `shares`, by all threads of a CTA.
+template <int D> __device__ __forceinline__ void nan_rows(const PagedAttnArgs& a, int share, int shares) {
+  const int r0 = min(max(a.s.q_start[0], 0), a.s.rows), r1 = min(max(a.s.q_start[a.s.B], r0), a.s.rows);
+  const float nan = __int_as_float(0x7fffffff);
+  for (int row = r0 + share; row < r1; row += shares)
+    for (int head = 0; head < a.H; ++head) {
+      const long long at = (long long)row * a.out.row + (long long)head * a.out.head;
+      for (int e = threadIdx.x; e < D; e += blockDim.x) store_out(a, at + e, nan);
+      if (threadIdx.x == 0 && a.lse) a.lse[(size_t)row * a.H + head] = nan;
+    }
 }
 
 // launchers

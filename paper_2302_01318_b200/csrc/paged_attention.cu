@@ -36,6 +36,11 @@ __global__ void __launch_bounds__(SIMT_THREADS) paged_attn_simt_kernel(const __g
   if (tid == 0) s_cur = c0;
   __syncthreads();
   WorkCursor c = s_cur;
+  if (c.spoilt) {
+    if (tid == 0) paged_flag(a.s.status, SPS_PAGED_TIMEOUT);
+    nan_rows<D>(a, blockIdx.x, gridDim.x);
+    return;
+  }
   const int dp = tid % (D / 2), rg = tid / (D / 2);
   while (c.valid) {
     const int R = c.nq * a.G, r0 = c.t * NR;

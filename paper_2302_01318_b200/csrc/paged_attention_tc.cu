@@ -42,7 +42,7 @@
 //               sequences are bound by what a part costs at its ends, not by HBM)
 //
 // Every wait is bounded; on expiry the CTA sets SPS_PAGED_TIMEOUT, lets its copies and products finish, frees its tensor
-// memory and returns.
+// memory, leaves NaN in the call's rows and a word in the workspace, whose counters are part-way, and returns.
 #include "paged_tc.cuh"
 
 namespace {
@@ -211,7 +211,10 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
   }
   pdl_wait();
   const WorkCursor c0 = cursor_begin<NR, TILE>(a, geo, s_qat);
-  if (tid == 0) *s_cur = c0;
+  if (tid == 0) {
+    *s_cur = c0;
+    if (c0.spoilt) { s_cur->valid = false; *s_abort = 2; paged_flag(a.s.status, SPS_PAGED_TIMEOUT); }
+  }
   P_FENCE_BEFORE();
   __syncthreads();
   P_FENCE_AFTER();
@@ -229,7 +232,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
     uint32_t p_phase = 0;                                      // parity of p_full, a bit for each set
     WorkCursor cs = c;                                         // the part S is at; c is the part O is at
     auto wait = [&](uint32_t bar, uint32_t parity) {
-      if (ok) ok = __all_sync(0xffffffffu, p_wait(bar, parity & 1u, a.wait_ns, a.s.status, s_abort));
+      if (ok) ok = __all_sync(0xffffffffu, p_wait(bar, parity & 1u, a, s_abort));
     };
     auto score = [&]() {                                       // S of the next tile
       if (!cs.valid) return;
@@ -295,7 +298,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
     for (int qn = 1; c.valid && ok; ++qn) {
       const int qb = qn % C::QBUF, use = qn / C::QBUF;
       ok = load_q<D, NR, PARTS, 64>(a, c, mem + C::Q_AT + qb * C::Q_BYTES, s_qat, qt, 7,
-                                    [&]() { return use == 0 || p_wait(q_free + 8 * qb, (uint32_t)(use - 1) & 1u, a.wait_ns, a.s.status, s_abort); });
+                                    [&]() { return use == 0 || p_wait(q_free + 8 * qb, (uint32_t)(use - 1) & 1u, a, s_abort); });
       if (!ok) break;
       p_arrive(q_ready + 8 * qb);
       cursor_next<NR, TILE>(a, c, geo);
@@ -340,7 +343,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
       auto collect = [&]() {
         if (!held) return;
         held = false;
-        ok = ok && p_wait(pv_done + 8 * set, (uint32_t)(pn - 1) & 1u, a.wait_ns, a.s.status, s_abort);
+        ok = ok && p_wait(pv_done + 8 * set, (uint32_t)(pn - 1) & 1u, a, s_abort);
         __syncwarp();
         P_FENCE_AFTER();
         float t[PP][16];
@@ -358,7 +361,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
       for (int i = 0; i < n; ++i) {
         const int buf = ((it >> 1) + i) & 1, p0 = (c.k0 + i) * TILE, pos = p0 + my;
         const bool edge = p0 + TILE - 1 > first_lim;          // some row does not see all of this tile
-        ok = ok && p_wait(s_full + 16 * set + 8 * buf, (s_phase >> buf) & 1u, a.wait_ns, a.s.status, s_abort);
+        ok = ok && p_wait(s_full + 16 * set + 8 * buf, (s_phase >> buf) & 1u, a, s_abort);
         s_phase ^= 1u << buf;
         __syncwarp();
         P_FENCE_AFTER();
@@ -453,7 +456,7 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
           // slots behind the sequence hold anything: zero (0 x NaN is NaN in a product).  New tokens some rows do not see:
           // a value that is not finite is taken out and remembered, its rows become NaN at the end.
           const int e = it + 2 * i + 1;
-          ok = ok && p_wait(full + 8 * (e % STAGES), (uint32_t)(e / STAGES) & 1u, a.wait_ns, a.s.status, s_abort);
+          ok = ok && p_wait(full + 8 * (e % STAGES), (uint32_t)(e / STAGES) & 1u, a, s_abort);
           if (ok && group == 0 && pos > first_lim) {
             unsigned char* vr = mem + (e % STAGES) * C::HALF + my * 128;
             bool clear = pos >= c.len;
@@ -572,6 +575,8 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
     P_FENCE_AFTER();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "n"(C::TMEM) : "memory");
   }
+  // (items that this CTA leaves unfinished are never joined: what other CTAs write over these rows is whole)
+  if (const int gave_up = *s_abort) nan_rows<D>(a, gave_up == 2 ? blockIdx.x : 0, gave_up == 2 ? gridDim.x : 1);
 }
 
 template <int D, int NR, int PARTS>

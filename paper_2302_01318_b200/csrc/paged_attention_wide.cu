@@ -26,7 +26,7 @@
 // Parts of an item are 256 rows x d floats each: they are joined by a kernel of its own (paged_join_kernel) that spreads every
 // item's rows over several CTAs; one CTA joining all of them took 60 us for 18 parts of 64 rows.
 //
-// Waits are bounded and end as in paged_attention_tc.cu.
+// Waits are bounded and end as in paged_attention_tc.cu; the join then makes the rows that it writes NaN.
 #include "paged_tc.cuh"
 
 namespace {
@@ -93,7 +93,10 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
   }
   pdl_wait();
   const WorkCursor c0 = cursor_begin<NR, TILE>(a, geo, s_qat);
-  if (tid == 0) *s_cur = c0;
+  if (tid == 0) {
+    *s_cur = c0;
+    if (c0.spoilt) { s_cur->valid = false; *s_abort = 2; paged_flag(a.s.status, SPS_PAGED_TIMEOUT); }
+  }
   P_FENCE_BEFORE();
   __syncthreads();
   P_FENCE_AFTER();
@@ -115,7 +118,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
       int it = 0, qn = 0;                  // half-tiles of the parts before, parts
       uint32_t pn[2] = {0, 0};             // weights taken, by tile
       auto wait = [&](uint32_t bar, uint32_t parity) {
-        if (ok) ok = __all_sync(0xffffffffu, p_wait(bar, parity & 1u, a.wait_ns, a.s.status, s_abort));
+        if (ok) ok = __all_sync(0xffffffffu, p_wait(bar, parity & 1u, a, s_abort));
       };
       auto score = [&](int w, int e, bool frees_k, bool frees_q) {   // S_w of the tile whose keys are half-tile e
         wait(full + 8 * (e % STAGES), (uint32_t)(e / STAGES));
@@ -204,7 +207,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
         for (int r = qt; r < min(live, NR); r += 128)
 #pragma unroll
           for (int e = 0; e < D; e += 64) asm volatile("prefetch.global.L2 [%0];" ::"l"(q + s_qat[r] + e));
-        ok = p_wait(q_free, (uint32_t)(qn - 1) & 1u, a.wait_ns, a.s.status, s_abort);
+        ok = p_wait(q_free, (uint32_t)(qn - 1) & 1u, a, s_abort);
       }
       if (ok && a.q_vec) {
         // straight to shared memory, all of a thread's 16-byte chunks in flight; rows that do not exist become zeros
@@ -261,7 +264,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
             // slots behind the sequence hold anything: zero (0 x NaN is NaN in a product).  New tokens some rows do not
             // see: a value that is not finite is taken out and remembered, its rows become NaN at the end.
             const int e = it + 2 * i + 1, pos = p0 + my;
-            ok = ok && p_wait(full + 8 * (e % STAGES), (uint32_t)(e / STAGES) & 1u, a.wait_ns, a.s.status, s_abort);
+            ok = ok && p_wait(full + 8 * (e % STAGES), (uint32_t)(e / STAGES) & 1u, a, s_abort);
             if (ok && pos > item_lim) {
               unsigned char* vr = wmem + (e % STAGES) * C::HALF + my * 128;
               bool clear = pos >= c.len;
@@ -282,7 +285,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
             }
             asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
           }
-          ok = ok && p_wait(s_full + 8 * w, sn & 1u, a.wait_ns, a.s.status, s_abort);
+          ok = ok && p_wait(s_full + 8 * w, sn & 1u, a, s_abort);
           __syncwarp();
           P_FENCE_AFTER();
           float x[128], up;
@@ -363,7 +366,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
           p_arrive(p_full + 8 * w);
         }
         on += n;
-        ok = ok && p_wait(pv_done + 8 * w, (on - 1) & 1u, a.wait_ns, a.s.status, s_abort);
+        ok = ok && p_wait(pv_done + 8 * w, (on - 1) & 1u, a, s_abort);
         __syncwarp();
       }
       it += 2 * n;
@@ -427,6 +430,7 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
     P_FENCE_AFTER();
     asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, 512;" ::"r"(tmem));
   }
+  if (const int gave_up = *s_abort) nan_rows<D>(a, gave_up == 2 ? blockIdx.x : 0, gave_up == 2 ? gridDim.x : 1);
 }
 
 // Joins the parts of the items that the attention kernel cut: o = sum_c 2^(m_c - M) o_c / sum_c 2^(m_c - M) l_c.  CTA (c, s)
@@ -437,6 +441,7 @@ template <int D>
 __global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttnArgs a) {
   constexpr int NR = W_ROWS, PIECES = D / 4 / 8;
   __shared__ float s_w[JOIN_PARTS][32];
+  __shared__ int s_gave_up;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
   pdl_launch_dependents();
   pdl_wait();
@@ -444,6 +449,7 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttnArgs a) 
   const int r = blockIdx.y * 32 + lane, rr = rec.t * NR + r, R = rec.nq * a.G;
   if (rec.parts < 2 || rec.t * NR + (int)blockIdx.y * 32 >= R) return;
   const bool live = rr < R;
+  if (threadIdx.x == 0) s_gave_up = __ldcg(a.gave_up);       // some part may be missing: NaN (s_w's barriers are between)
   constexpr size_t SF = slot_floats<NR, D>();
   const float* slots = a.slots + SF * (size_t)(2 * rec.first);
   auto slot = [&](int p) { return slots + SF * (size_t)(p == 0 ? 1 : 2 * p); };   // part 0 begins in its CTA: part_slot
@@ -480,6 +486,11 @@ __global__ void __launch_bounds__(256) paged_join_kernel(const PagedAttnArgs a) 
     }
   }
   if (!live) return;
+  if (s_gave_up) {
+    L = __int_as_float(0x7fffffff);
+#pragma unroll
+    for (int k = 0; k < PIECES; ++k) o[k] = make_float4(L, L, L, L);
+  }
   const int tok = row_token(a, rr), head = rec.hk * a.G + rr - tok * a.G;
   const long long at = (long long)(rec.row0 + tok) * a.out.row + (long long)head * a.out.head + warp * PIECES * 4;
 #pragma unroll

@@ -33,8 +33,8 @@ __device__ __forceinline__ unsigned long long p_timer() {
   asm volatile("mov.u64 %0, %globaltimer;" : "=l"(t));
   return t;
 }
-// bounded wait: false after wait_ns, or as soon as another thread of the CTA gave up
-__device__ __forceinline__ bool p_wait(uint32_t bar, uint32_t parity, unsigned long long wait_ns, int32_t* status, volatile int* abort_flag) {
+// bounded wait: false after a.wait_ns, or as soon as another thread of the CTA gave up
+__device__ __forceinline__ bool p_wait(uint32_t bar, uint32_t parity, const PagedAttnArgs& a, volatile int* abort_flag) {
   if (p_try(bar, parity)) return true;
   const unsigned long long t0 = p_timer();
   for (;;) {
@@ -43,8 +43,9 @@ __device__ __forceinline__ bool p_wait(uint32_t bar, uint32_t parity, unsigned l
       if (p_try(bar, parity)) return true;
       if (*abort_flag) return false;
     }
-    if (p_timer() - t0 > wait_ns) {
-      paged_flag(status, SPS_PAGED_TIMEOUT);
+    if (p_timer() - t0 > a.wait_ns) {
+      paged_flag(a.s.status, SPS_PAGED_TIMEOUT);
+      *reinterpret_cast<volatile int*>(a.gave_up) = 1;
       *abort_flag = 1;
       return false;
     }
@@ -172,7 +173,7 @@ __device__ __forceinline__ void copy_pages(const TcArgs& ta, WorkCursor c, const
       for (int kv = 0; kv < 2; ++kv, ++it) {
         const int slot = it % STAGES, use = it / STAGES;
         if (use > 0) {
-          ok = p_wait(empty + 8 * slot, (uint32_t)(use - 1) & 1u, a.wait_ns, a.s.status, s_abort);
+          ok = p_wait(empty + 8 * slot, (uint32_t)(use - 1) & 1u, a, s_abort);
           ok = __all_sync(0xffffffffu, ok) && !*s_abort;
           ok = __all_sync(0xffffffffu, ok);
           if (!ok) break;

@@ -346,3 +346,52 @@ def test_a_wait_that_runs_out_ends_the_call_with_a_status(qdt, new, lens, stage)
     torch.cuda.synchronize()
     assert int(batch.status) == 0
     check_attention(out, None, q, pages.dense, news)
+
+
+@pytest.mark.parametrize("qdt,new,lens", [(F32, 2, [60000, 90]), (BF16, 2, [60000, 90]), (BF16, 100, [6000, 300])])
+@pytest.mark.parametrize("watched", [True, False])
+def test_a_call_that_gave_up_is_seen_without_its_status(qdt, new, lens, watched):
+    """Whether or not the caller passes a status: what the call did not finish is NaN, and so is everything of the next calls on
+    the same workspace, whose arrival counters are part-way, until it is zeroed."""
+    pages = Pages(lens, 2, 128, 16, BF16)
+    news, rows = [new, new], 2 * new + 3
+    q = normal((rows, 16, 128), qdt, 1)
+    ws, batch = workspace(pages.cache, 16, qdt), pages.batch(news, lead=1)
+    status = batch.status
+    if not watched:
+        batch._c.status = None
+    want, _, S = attention64(q, pages.dense, news, 1)
+    tol = attention_tol(want, S, 128, qdt, qdt)
+    inside = slice(1, 1 + 2 * new)
+
+    def call(cache=pages.cache, over=batch, x=q):
+        out, lse = torch.full_like(x, 7.0), torch.full((rows, 16), 7.0, device=DEV)
+        sps.sps_paged_attention(cache, over, x, out, ws, lse=lse)
+        torch.cuda.synchronize()
+        for t in (out, lse):
+            assert (t[:1] == 7).all() and (t[1 + 2 * new:] == 7).all()
+        return out[inside], lse[inside]
+
+    try:
+        sps.sps_debug_set_wait(20000, 1)
+        out, _ = call()
+    finally:
+        sps.sps_debug_set_wait()
+    lost = torch.isnan(out.float())
+    assert lost.any() and ((out.double() - want[inside]).abs() <= tol[inside])[~lost].all()
+    for _ in range(2):
+        status.zero_()
+        out, lse = call()
+        assert torch.isnan(out.float()).all() and torch.isnan(lse).all()
+        assert int(status) == (sps.PAGED_TIMEOUT if watched else 0)
+    # the kernels over an fp32 cache read the same counters
+    other = Pages([70, 20], 2, 64, 16, F32)
+    x = normal((rows, 16, 64), F32, 2)
+    if ws.nbytes >= workspace(other.cache, 16, F32).nbytes and new < 20:
+        small = other.batch(news, lead=1)
+        out, lse = call(other.cache, small, x)
+        assert torch.isnan(out).all() and torch.isnan(lse).all() and int(small.status) == sps.PAGED_TIMEOUT
+    ws.zero_()
+    status.zero_()
+    out, _ = call()
+    assert int(status) == 0 and ((out.double() - want[inside]).abs() <= tol[inside]).all()
