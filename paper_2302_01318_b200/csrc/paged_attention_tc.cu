@@ -284,12 +284,12 @@ __global__ void __launch_bounds__(Cfg<D, NR, PARTS>::THREADS, 1) paged_attn_tc_k
       ++on;
       cursor_next<NR, TILE>(a, c, geo);
     }
-    if (!ok) {   // every product issued so far must be done before the ring and the tensor memory go away
-      *s_abort = 1;
-      if (leader) p_commit(drain);
-      __syncwarp();
-      p_drain(drain, 0u);
-    }
+    // Every product issued must be done before the ring and the tensor memory go away.  After a part that was worked to its
+    // end they are; but softmax warps that gave up go on to the end without waiting for them, and this warp need not notice.
+    if (!ok) *s_abort = 1;
+    if (leader) p_commit(drain);
+    __syncwarp();
+    p_drain(drain, 0u);
   } else if (warp < 4) {
     // ---------------------------------------------------------------------------------------------------- Q
     const int qt = tid - 64;

@@ -180,12 +180,12 @@ __global__ void __launch_bounds__(W_THREADS, 1) paged_attn_wide_kernel(const __g
         it += 2 * n;
         cursor_next<NR, TILE>(a, c, geo);
       }
-      if (!ok) {   // every product issued so far must be done before the ring and the tensor memory go away
-        *s_abort = 1;
-        if (leader) p_commit(drain);
-        __syncwarp();
-        p_drain(drain, 0u);
-      }
+      // Every product issued must be done before the ring and the tensor memory go away.  After a part that was worked to its
+      // end they are; but softmax warps that gave up go on to the end without waiting for them, and this warp need not notice.
+      if (!ok) *s_abort = 1;
+      if (leader) p_commit(drain);
+      __syncwarp();
+      p_drain(drain, 0u);
     }
   } else if (warp < 8) {
     W_GIVE();
