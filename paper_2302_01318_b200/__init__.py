@@ -611,6 +611,6 @@ def sps_paged_attention(cache, batch, q, out, workspace, scale=0.0, lse=None, st
         if lse.shape != shape[:2] or not lse.is_contiguous() or lse.get_device() != index or lse.dtype is not _Torch.float32:
             raise ValueError("lse is contiguous float32 [rows, heads] on the same device")
         lse_p = lse.data_ptr()
-    if workspace.nbytes < _workspace_bytes(cache, shape[1], rq.dtype):
-        raise ValueError("workspace smaller than sps_paged_attention_workspace_bytes")
+    if workspace.nbytes < _workspace_bytes(cache, shape[1], rq.dtype) or not workspace.is_contiguous():
+        raise ValueError("workspace not contiguous, or smaller than sps_paged_attention_workspace_bytes")
     _on(index, lib().sps_paged_attention, stream, cache._p, batch._p, shape[0], C.byref(rq), C.byref(ro), scale, lse_p, workspace.data_ptr())

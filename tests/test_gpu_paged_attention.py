@@ -395,3 +395,14 @@ def test_a_call_that_gave_up_is_seen_without_its_status(qdt, new, lens, watched)
     status.zero_()
     out, _ = call()
     assert int(status) == 0 and ((out.double() - want[inside]).abs() <= tol[inside]).all()
+
+
+def test_a_workspace_that_repeats_its_bytes_is_refused():
+    """An expanded tensor claims more bytes than it has."""
+    pages = Pages([20], 1, 64, 8, F32)
+    q = normal((1, 2, 64), F32, 1)
+    n = workspace(pages.cache, 2, F32).nbytes
+    for ws in (torch.zeros((1, 16), dtype=torch.uint8, device=DEV).expand(n // 16 + 1, 16), torch.zeros((n, 2), dtype=torch.uint8, device=DEV)[:, 0],
+               torch.zeros(n - 1, dtype=torch.uint8, device=DEV)):
+        with pytest.raises(ValueError, match="workspace"):
+            sps.sps_paged_attention(pages.cache, pages.batch([1]), q, torch.empty_like(q), ws)
