@@ -6,7 +6,7 @@ import pytest
 import torch
 
 import paper_2302_01318_b200 as sps
-from paged_precision import check_precision, lower
+from paged_precision import check_precision, equal_weights, hardest_query, hardest_weight, lower, one_query_number
 from paged_util import BF16, DEV, F32, Pages, normal, workspace
 
 pytestmark = pytest.mark.gpu
@@ -98,3 +98,54 @@ def test_whole_tiles_of_low_scores_ahead_of_the_others(types, d, new, below, sco
     q[..., -1] = 2.0
     out, lse = attend(pages, q, [new, new], odt)
     check_precision(out, lse, q, pages.dense, [new, new])
+
+
+# rows of a key head: every width of the few-row tiles, one and two tiles of 128, several items
+ROWS = [(1, 4), (3, 8), (5, 8), (8, 8), (9, 8), (40, 8)]     # new rows, query heads (on one key head)
+
+
+@pytest.mark.parametrize("new,H", ROWS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("types", range(len(TYPES)))
+def test_as_exact_as_a_plain_evaluation_in_32_bits(types, d, new, H):
+    qdt, cdt, odt = TYPES[types]
+    pages = Pages([50, 129, 9000], 1, d, 16, cdt)
+    news = [new, min(new, 100), new]
+    q = normal((sum(news), H, d), qdt, 2, 1.5)
+    out, lse = attend(pages, q, news, odt)
+    check_precision(out, lse, q, pages.dense, news)
+
+
+@pytest.mark.parametrize("new,H", ROWS)
+@pytest.mark.parametrize("L", [50, 700, 9000])
+@pytest.mark.parametrize("types", range(len(TYPES)))
+def test_no_part_of_the_probabilities_is_missing(types, L, new, H):
+    qdt, cdt, odt = TYPES[types]
+    parts = 3 if qdt == F32 else (1 if new * H > 64 else 2)
+    pages = Pages([L], 1, 64, 16, cdt)
+    q, k, v = equal_weights(new, H, 64, L, hardest_weight(max(parts - 1, 1), qdt), qdt, cdt, DEV)
+    put(pages, 0, k, v)
+    out, _ = attend(pages, q, [new], odt, scale=math.log(2.0))
+    check_precision(out, None, q, pages.dense, [new], scale=math.log(2.0), together=True)
+
+
+@pytest.mark.parametrize("new,H", ROWS)
+@pytest.mark.parametrize("d", [64, 128])
+@pytest.mark.parametrize("cdt", [F32, BF16])
+def test_no_part_of_the_queries_is_missing(cdt, d, new, H):
+    pages = Pages([700], 1, d, 16, cdt)
+    q, k, v = one_query_number(new, H, d, 700, hardest_query(2), F32, cdt, DEV)
+    put(pages, 0, k, v)
+    out, _ = attend(pages, q, [new], F32, scale=1.0)
+    check_precision(out, None, q, pages.dense, [new], scale=1.0, together=True)
+
+
+@pytest.mark.parametrize("types", range(len(TYPES)))
+def test_long_sums_are_not_cut(types):
+    qdt, cdt, odt = TYPES[types]
+    pages = Pages([32768], 1, 64, 64, cdt)
+    v = torch.rand((32768, 1, 64), generator=torch.Generator().manual_seed(4)) * 0.5 + 0.5
+    put(pages, 0, v=v.to(DEV).to(cdt))
+    q = normal((1, 2, 64), qdt, 3)
+    out, _ = attend(pages, q, [1], odt)
+    check_precision(out, None, q, pages.dense, [1], together=True)
