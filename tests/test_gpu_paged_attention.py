@@ -406,3 +406,48 @@ def test_a_workspace_that_repeats_its_bytes_is_refused():
                torch.zeros(n - 1, dtype=torch.uint8, device=DEV)):
         with pytest.raises(ValueError, match="workspace"):
             sps.sps_paged_attention(pages.cache, pages.batch([1]), q, torch.empty_like(q), ws)
+
+
+@pytest.mark.parametrize("types", range(len(TYPES)))
+@pytest.mark.parametrize("d", [64, 128])
+def test_many_rows_with_strides_and_unaligned_rows(types, d):
+    """More than 64 rows of a key head, of short sequences (items in one piece) and a long one (cut between CTAs and joined)."""
+    qdt, cdt, odt = TYPES[types]
+    pages = Pages([77, 6000, 150], 2, d, 8, cdt)
+    news, rows, H = [3, 150, 90], 243, 4
+    big = normal((rows, H + 2, d + 3), qdt, 3)
+    for q in (big[:, 1:1 + H, :d], big[:, 1:1 + H, 3:], normal((H, rows, d), qdt, 4).transpose(0, 1)):
+        for shift in (5, 8):                                     # outputs element by element, and whole pieces
+            ob = torch.full((rows, H + 1, d + 8), 7.0, dtype=odt, device=DEV)
+            out = ob[:, 1:, shift:shift + d]
+            lse = torch.full((rows, H), 7.0, device=DEV)
+            sps.sps_paged_attention(pages.cache, pages.batch(news), q, out, workspace(pages.cache, H, qdt), lse=lse)
+            check_attention(out, lse, q, pages.dense, news)
+            assert (ob[:, 0] == 7).all() and (ob[..., :shift] == 7).all() and (ob[..., shift + d:] == 7).all()
+
+
+@pytest.mark.parametrize("types", range(len(TYPES)))
+def test_many_rows_replayed_in_a_graph_with_moved_lengths(types):
+    """Attention and the join of its parts, captured together; two captured calls that take turns on one workspace."""
+    qdt, cdt, odt = TYPES[types]
+    pages = Pages([5000, 333], 1, 128, 16, cdt)
+    rows = 200
+    q, ws = normal((rows, 4, 128), qdt, 1), workspace(pages.cache, 4, qdt)
+    out, second = (torch.zeros((rows, 4, 128), dtype=odt, device=DEV) for _ in range(2))
+    batch, other = pages.batch([150, 50]), pages.batch([1, 1], max_q=1)
+    sps.sps_paged_attention(pages.cache, batch, q, out, ws)
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        sps.sps_paged_attention(pages.cache, batch, q, out, ws)
+        sps.sps_paged_attention(pages.cache, other, q, second, ws)
+    for lens, starts in (([5000, 333], [0, 150, 200]), ([200, 300], [0, 1, 200]), ([4000, 129], [0, 71, 200]), ([170, 0], [0, 170, 170]), ([1, 333], [0, 1, 140])):
+        batch.kv_len.copy_(torch.tensor(lens, dtype=torch.int32))
+        batch.q_start.copy_(torch.tensor(starts, dtype=torch.int32))
+        q.copy_(normal((rows, 4, 128), qdt, lens[0]))
+        out.fill_(7.0)
+        graph.replay()
+        torch.cuda.synchronize()
+        check_attention(out, None, q, [(k[:L], v[:L]) for (k, v), L in zip(pages.dense, lens)], [b - a for a, b in zip(starts, starts[1:])])
+        check_attention(second[:2], None, q[:2], pages.dense, [1, 1])
+    assert int(batch.status) == 0 and int(other.status) == 0
