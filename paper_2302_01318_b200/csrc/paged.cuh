@@ -27,15 +27,17 @@ __device__ __forceinline__ int paged_capacity(const PagedSeqs& s) {
   return c > 0x7fff0000ll ? 0x7fff0000 : (int)c;
 }
 
-struct SeqGeom { int row0, nq, len; bool cut; };   // first row, rows, tokens; cut: kv_len did not fit the page table
+// first row and rows, of those inside the call's buffers; tokens up to the last such row's own (rows behind the buffers take
+// theirs with them); cut: kv_len did not fit the page table
+struct SeqGeom { int row0, nq, len; bool cut; };
 __device__ __forceinline__ SeqGeom paged_seq(const PagedSeqs& s, int b) {
   SeqGeom g;
-  const int r0 = min(max(s.q_start[b], 0), s.rows), r1 = min(max(s.q_start[b + 1], r0), s.rows);
+  const int end = s.q_start[b + 1], r0 = min(max(s.q_start[b], 0), s.rows), r1 = min(max(end, r0), s.rows);
   const int len = s.kv_len[b], cap = paged_capacity(s);
   g.row0 = r0;
   g.nq = r1 - r0;
   g.cut = len > cap;
-  g.len = min(max(len, 0), cap);
+  g.len = max(min(max(len, 0), cap) - (max(end, r1) - r1), 0);
   return g;
 }
 

@@ -451,3 +451,22 @@ def test_many_rows_replayed_in_a_graph_with_moved_lengths(types):
         check_attention(out, None, q, [(k[:L], v[:L]) for (k, v), L in zip(pages.dense, lens)], [b - a for a, b in zip(starts, starts[1:])])
         check_attention(second[:2], None, q[:2], pages.dense, [1, 1])
     assert int(batch.status) == 0 and int(other.status) == 0
+
+
+@pytest.mark.parametrize("types", range(3))
+@pytest.mark.parametrize("news,lead", [([4, 3, 9], 0), ([4, 3, 90], -2), ([40, 3, 7], -5)])
+def test_rows_outside_the_buffers_are_skipped_and_move_no_other(types, news, lead):
+    """A call on the first rows only, row numbers before and behind them: a row's position goes by its sequence's rows, there or
+    not, and what it sees with it."""
+    qdt, cdt, odt = TYPES[types]
+    lens = [300, 40, 260]
+    pages = Pages(lens, 2, 64, 16, cdt)
+    total = lead + sum(news)
+    q, ws = normal((total, 8, 64), qdt, 1), workspace(pages.cache, 8, qdt)
+    want, _, S = attention64(torch.cat([q[:1].expand(-lead, -1, -1), q]), pages.dense, news)
+    tol = attention_tol(want, S, 64, qdt, odt)
+    batch = pages.batch(news, lead=lead)
+    for rows in (total, total - 2, total - news[2], total - news[2] - 1, 1):
+        out, lse = torch.full((rows, 8, 64), 7.0, dtype=odt, device=DEV), torch.empty((rows, 8), device=DEV)
+        sps.sps_paged_attention(pages.cache, batch, q[:rows], out, ws, lse=lse)
+        assert ((out.double() - want[-lead:][:rows]).abs() <= tol[-lead:][:rows]).all()
