@@ -369,8 +369,8 @@ int64_t sps_linear_static_floats_needed(int32_t dtype, int32_t M, int32_t N, int
  * from one dense cache; these calls change where keys and values live, not the method: a scoring pass of K + 1 rows
  * is a batch whose sequences bring K + 1 new rows each, and the rollback after a rejection is a smaller kv_len.
  *
- * All three calls only enqueue (one kernel each) on `stream`, read lengths and page tables on the device -- so that a
- * captured call can be replayed after these have moved -- and allocate nothing.  Pointers belong to the current
+ * All three calls only enqueue (one kernel; attention of many bf16 rows two) on `stream`, read lengths and page tables on
+ * the device -- so that a captured call can be replayed after these have moved -- and allocate nothing.  Pointers belong to the current
  * device.  dtype here: 0 = fp32, 1 = bf16.
  * ------------------------------------------------------------------------------------------------------------- */
 
@@ -428,11 +428,13 @@ typedef struct {
 /* The sequences of one call.  Sequence b owns rows q_start[b] .. q_start[b + 1] - 1 of the call's row buffers (none:
  * q_start[b + 1] == q_start[b]) and has kv_len[b] tokens, these new ones included: its last row is at position
  * kv_len[b] - 1.  Token j is in slot j % page_size of page pages[b * pages_ld + j / page_size]; table entries behind
- * the last token's are never read, nor are slots behind it.  Rows behind the last sequence's are left as they were.
- * Sequences may share pages that none of them appends to.
+ * the last token's are never read; slots behind it are never used, though a page that holds any of the sequence's tokens
+ * may be read whole.  Rows behind the last sequence's are left as they were.  Sequences may share pages that none of
+ * them appends to.
  * The host sees none of these numbers.  What does not fit is skipped, never followed: row numbers outside the call's
- * buffers, a kv_len above pages_ld * page_size (cut to it), a page number outside 0 .. n_pages - 1 (its tokens are
- * not appended, and read as zeros); the last two also set a bit of *status, which the calls never clear. */
+ * buffers (the other rows of their sequence keep their positions), tokens behind pages_ld * page_size (not appended;
+ * attention takes a kv_len above it as if it were that), a page number outside 0 .. n_pages - 1 (its tokens are not
+ * appended, and read as zeros); the last two also set a bit of *status, which the calls never clear. */
 #define SPS_PAGED_BAD_PAGE 1    /* bits of *status */
 #define SPS_PAGED_BAD_LENGTH 2
 #define SPS_PAGED_TIMEOUT 4     /* a bounded wait inside the attention kernel ran out: rows the call did not finish are NaN
@@ -444,8 +446,9 @@ typedef struct {
   const int32_t* pages;   /* device [B][pages_ld]                */
   int32_t* status;        /* device [1], may be NULL             */
   int32_t B, pages_ld;    /* B: up to 2^27                       */
-  int32_t max_q;          /* the most rows a sequence brings, as far as the host knows (>= 1): picks the kernel, results
-                             hold for any q_start                */
+  int32_t max_q;          /* the most rows a sequence brings, as far as the host knows (>= 1): picks the kernel for the whole
+                             call, results hold for any q_start; for bf16 queries it decides the probabilities' bits,
+                             see sps_paged_attention             */
 } sps_paged_batch;
 
 /* Append: for every row of every sequence, its keys -- rotated by the row's position under `plan`, unless plan is
@@ -459,14 +462,18 @@ int sps_paged_append(const sps_paged_cache* cache, const sps_paged_batch* batch,
 /* Attention: row i of sequence b, at position p = kv_len[b] - (rows of b) + i, over the tokens 0 .. p of its sequence:
  *   out[row, h] = sum_j softmax_j(scale q[row, h] . k[j, h / G]) v[j, h / G],   G = heads of q / n_kv_heads,
  * scale 0 meaning 1 / sqrt(d_head).  A row at a negative position sees nothing: its output is 0.
- * q and out: [rows] rows of the same heads, rows x heads below 2^31; out has q's dtype, or is fp32; a bf16 cache takes fp32 or bf16 queries
- * (fp32 queries and probabilities enter the tensor cores as three bf16 parts each, which keep their 24 bits; with bf16
- * queries the probabilities are two bf16 parts, or, for more than 64 rows of a key head, one), an fp32 cache fp32 ones.
+ * q and out: [rows] rows of the same heads, rows x heads below 2^31; out has q's dtype, or is fp32; a bf16 cache takes fp32 or
+ * bf16 queries, an fp32 cache fp32 ones.  Sums and scores are fp32, whatever the scores' size.  Over a bf16 cache fp32 queries
+ * and their probabilities enter the tensor cores as three bf16 parts each, which keep their 24 bits.  With bf16 queries
+ * the probabilities are two bf16 parts (16 bits) where max_q * G is at most 64, and one (8 bits) where it is more, in all
+ * rows of the call, an fp32 out's too: a max_q below the truth keeps 16 bits, at the cost of a prompt's speed.
  * out may be q itself (same dtype and strides), other overlaps are not supported.  lse: device fp32 [rows][heads], may be
- * NULL: log sum_j exp(scale q . k_j), -inf for a row that sees nothing.
- * What lies in slots behind a sequence's tokens never matters, whatever it is.  An infinite or NaN value (v) makes its
- * element of the rows that give it weight infinite or NaN (which of the two is left open); over a bf16 cache, where its
- * token is among the sequence's new ones, every element of the rows that see it is NaN.
+ * NULL: log sum_j exp(scale q . k_j), -inf for a row that sees nothing or whose scores are all -inf (its output is 0 too).
+ * What lies in slots behind a sequence's tokens never matters, whatever it is, nor do tokens behind a row's own.  An infinite
+ * or NaN value (v) makes its element of the rows that see it infinite or NaN (which of the two is left open; where its weight is 0
+ * it may be left out); over a bf16 cache, where its token is among the sequence's new ones, it may make every element of
+ * those rows NaN, and values beyond 2^80 may overflow to infinite ones.  An infinite or NaN key makes the rows that see it NaN,
+ * or is left out where its score is -inf.
  * workspace: device scratch of sps_paged_attention_workspace_bytes bytes, 16-byte aligned, zero-filled once before its
  * first use (every call leaves it ready for the next; calls that share one must not run at the same time, captured
  * ones included).  The size holds for every batch on this cache shape. */
