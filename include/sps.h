@@ -369,7 +369,7 @@ int64_t sps_linear_static_floats_needed(int32_t dtype, int32_t M, int32_t N, int
  * from one dense cache; these calls change where keys and values live, not the method: a scoring pass of K + 1 rows
  * is a batch whose sequences bring K + 1 new rows each, and the rollback after a rejection is a smaller kv_len.
  *
- * All three calls only enqueue (one kernel; attention of many bf16 rows two) on `stream`, read lengths and page tables on
+ * These three calls only enqueue (one kernel; attention of many bf16 rows two) on `stream`, read lengths and page tables on
  * the device -- so that a captured call can be replayed after these have moved -- and allocate nothing.  Pointers belong to the current
  * device.  dtype here: 0 = fp32, 1 = bf16.
  * ------------------------------------------------------------------------------------------------------------- */
@@ -480,6 +480,103 @@ int sps_paged_append(const sps_paged_cache* cache, const sps_paged_batch* batch,
 int sps_paged_attention(const sps_paged_cache* cache, const sps_paged_batch* batch, int32_t rows, const sps_rows* q,
                         const sps_rows* out, float scale, float* lse, void* workspace, void* stream);
 int64_t sps_paged_attention_workspace_bytes(const sps_paged_cache* cache, int32_t n_heads, int32_t q_dtype);
+
+/* ---------------------------------------------------------------------------------------------------------------
+ * Which pages a sequence has.  A pool counts, page by page, the table rows that hold it; a table has a row per sequence
+ * (or per beam of one).  Rows may share pages: a prompt's pages are held once by all that continue it, and a row gets a page of
+ * its own only where it is about to write (sps_paged_append) into one that others hold too.  The paper decodes one
+ * sequence; these calls serve programs that decode several continuations of a prompt, admit and drop sequences, and roll
+ * rejected drafts back.  One table serves all layers: page p is page p of every layer's cache.
+ *
+ * All calls only enqueue on `stream` (one kernel each, sps_paged_compact two, sps_paged_copy one per 64 layers), read and write
+ * their state on the device -- so that a captured call can be replayed -- and allocate nothing.  A pool's, a table's or a
+ * workspace's calls must not run at the same time.  Results do not depend on timing: of free pages the lowest are taken, rows are
+ * served in their order.  What does not fit is skipped, never followed, and sets a bit of the pool's status: page numbers
+ * outside the pool (SPS_PAGED_BAD_PAGE; a fork and a compaction keep such an entry), counts outside their row
+ * (SPS_PAGED_BAD_LENGTH; they are clipped), parents outside their table (SPS_PAGED_BAD_ROW; none).
+ * ------------------------------------------------------------------------------------------------------------- */
+#define SPS_PAGED_NO_PAGE 8    /* more bits of *status: a row was left without the pages that it wanted */
+#define SPS_PAGED_BAD_ROW 16
+typedef struct {
+  int32_t* refs;     /* device [n_pages]: table rows that hold the page, 0 = free           */
+  int32_t* status;   /* device [1], SPS_PAGED_* bits, never cleared by the calls; may be NULL */
+  int32_t n_pages, page_size;   /* page_size: tokens, a power of two, 8 .. 512               */
+} sps_page_pool;
+
+/* Row r holds the pages in entries 0 .. held[r] - 1 of pages[r * ld ...], for len[r] tokens (len[r] <= held[r] * page_size).
+ * Entries behind held[r] are never read, and stay as they are unless pages are taken.  pages, with len as kv_len, is what
+ * sps_paged_batch takes; its append and attention need held to cover kv_len. */
+typedef struct {
+  int32_t* pages;    /* device [B][ld] */
+  int32_t *held, *len;   /* device [B]  */
+  int32_t B, ld;     /* B: up to 8192, B x ld below 2^31 */
+} sps_page_table;
+
+/* Pages to be copied, as a call leaves them: list[i] = (from, to, slots), the first `slots` of page `from`, *count of them. */
+typedef struct {
+  int32_t* list;     /* device [capacity][3] */
+  int32_t* count;    /* device [1]           */
+  int32_t capacity;
+} sps_page_moves;
+
+/* Fork / reorder: row i of dst becomes row parents[i] of src (its entries, held and len); parents[i] = -1 makes an empty row.
+ * Several children share their parent's pages.  dst takes src's place: src's rows give up their references, pages without a child
+ * become free, and src is not to be used as a table again before it has been a dst (a beam search takes two in turn).  parents:
+ * device [dst->B].  src and dst share no array; dst->ld >= src->ld. */
+int sps_paged_fork(const sps_page_pool* pool, const sps_page_table* src, const sps_page_table* dst, const int32_t* parents, void* stream);
+
+/* Roll back, free and make room, for every row of the table; want: device [B].  With n = min(len, want) tokens kept, first of all rows:
+ *   the entries behind ceil(n / page_size) are given up (want = 0: the whole row);
+ * then, where want > n, row after row:
+ *   the page of token n, if n is inside it and other rows hold it too, is exchanged for a fresh one, and (old, fresh, n % page_size)
+ *   is added to `moves` -- unless all who hold it exchange it in this call: then the first of them keeps it;
+ *   fresh pages are appended up to ceil(want / page_size) entries.
+ * Fresh pages are the free ones in ascending order.  A row whose pages are no longer to be had gets none of them, nor does any
+ * row behind it that needs some: it keeps its n tokens, held tells so, and SPS_PAGED_NO_PAGE is set.  held and len (= n) are
+ * written.  Before the row's new tokens are appended, the moves are to be carried out (sps_paged_copy).
+ * moves->capacity >= B.  workspace: device scratch of sps_paged_pool_workspace_bytes(n_pages) bytes, 16-byte aligned, zero-filled
+ * once before its first use (every call leaves it ready for the next). */
+int sps_paged_reserve(const sps_page_pool* pool, const sps_page_table* table, const int32_t* want, const sps_page_moves* moves, void* workspace,
+                      void* stream);
+int64_t sps_paged_pool_workspace_bytes(int32_t n_pages);
+
+/* Compact: with U pages in use, those numbered U and above move to the free ones below U, the i-th such page to the i-th such
+ * hole, at most moves->capacity of them, lowest first; afterwards (without that limit) pages 0 .. U - 1 are in use and the rest
+ * of the pool can be given back.  src must be the only table that holds pages of the pool.  dst receives the table, refs_out
+ * (device [n_pages]) the references, `moves` the copies to carry out, whole pages.  In place: dst may share src's arrays (the same ld), refs_out may be
+ * pool->refs; else src and pool->refs stay as they are.  workspace: as for sps_paged_reserve (the same one will do). */
+int sps_paged_compact(const sps_page_pool* pool, const sps_page_table* src, const sps_page_table* dst, int32_t* refs_out, const sps_page_moves* moves,
+                      void* workspace, void* stream);
+
+/* Copy: the listed pages' first slots, in the keys and values of every layer; slots behind them are left as they were.  layers: HOST array of n_layers caches of
+ * one shape, dtype and strides.  Items of the list outside the caches are skipped, slots clipped to page_size.  No page may be
+ * the destination of two items, or a source and a destination (what the calls above list is of that kind). */
+int sps_paged_copy(const sps_paged_cache* layers, int32_t n_layers, const sps_page_moves* moves, void* stream);
+
+/* The selection of a beam step: for each of B sequences the N best continuations of its W beams, best first,
+ *   c[w, v] = scores[w] + logits[w, v] / T - log sum_u exp(logits[w, u] / T),
+ * equal ones in the order of w V + v.  The paper samples; this is the search its Related Work's decoding methods set beside it, over the
+ * same logits, and with sps_paged_fork over the same cache.
+ *   logits        device, dtype 0 fp32 / 1 bf16: row b W + w at logits + (b W + w) row_stride (elements), V of them; any alignment
+ *                 (16-byte aligned rows are read 16 bytes at a time)
+ *   scores        device fp32 [B][W]: log-probability of each beam so far; -inf: there is no such beam (the first step after
+ *                 a prompt has one beam, or one score that is not -inf)
+ *   done          device int32 [B][W], may be NULL: a beam that has ended (not 0) is not continued; it offers itself as one candidate,
+ *                 (end_token, its score), and its logits are not read
+ *   end_token     -1: none; else candidates with it are done
+ *   out_scores    device fp32 [B][N]: c, rounded once (candidates are compared before)
+ *   out_parents   device int32 [B][N]: row b W + w of the continued beam -- the parents of sps_paged_fork when N = W
+ *   out_tokens    device int32 [B][N]
+ *   out_done      device int32 [B][N], may be NULL: 1 where the token is end_token, else 0
+ * A logit of -inf is no candidate.  A beam whose score is not finite, or whose logits hold a NaN or +inf or nothing above -inf, offers
+ * none; a sequence that has fewer than N candidates gets (-inf, -1, -1, 0) for the rest.
+ * With N = W, out_scores may be scores and out_done may be done.  B up to 2^16, W and N up to 128, V up to 2^24, W V below 2^31.
+ * workspace: device scratch of sps_beam_select_workspace_bytes bytes, 16-byte aligned, zero-filled once before its first use (every
+ * call leaves it ready for the next; calls that share one must not run at the same time, captured ones included). */
+int sps_beam_select(const void* logits, int32_t dtype, int64_t row_stride, int32_t B, int32_t W, int32_t V, double temperature,
+                    const float* scores, const int32_t* done, int32_t end_token, int32_t N, float* out_scores, int32_t* out_parents,
+                    int32_t* out_tokens, int32_t* out_done, void* workspace, void* stream);
+int64_t sps_beam_select_workspace_bytes(int32_t B, int32_t W, int32_t V);
 
 /* Tensor-parallel passes (section Conditional Scoring: the models are served Megatron-style over several chips, the
  * attention and feed-forward blocks sharded and each followed by an all-reduce of (K + 1) x d_model numbers, which

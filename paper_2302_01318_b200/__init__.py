@@ -75,6 +75,18 @@ class sps_paged_batch(C.Structure):
                 ("B", C.c_int32), ("pages_ld", C.c_int32), ("max_q", C.c_int32)]
 
 
+class sps_page_pool(C.Structure):
+    _fields_ = [("refs", C.c_void_p), ("status", C.c_void_p), ("n_pages", C.c_int32), ("page_size", C.c_int32)]
+
+
+class sps_page_table(C.Structure):
+    _fields_ = [("pages", C.c_void_p), ("held", C.c_void_p), ("len", C.c_void_p), ("B", C.c_int32), ("ld", C.c_int32)]
+
+
+class sps_page_moves(C.Structure):
+    _fields_ = [("list", C.c_void_p), ("count", C.c_void_p), ("capacity", C.c_int32)]
+
+
 _lib = None
 
 
@@ -136,6 +148,15 @@ def lib():
         L.sps_paged_attention.argtypes = [vp, vp, i32, vp, vp, f32, vp, vp, vp]
         L.sps_paged_attention_workspace_bytes.argtypes = [vp, i32, i32]
         L.sps_paged_attention_workspace_bytes.restype = i64
+        L.sps_paged_fork.argtypes = [vp, vp, vp, vp, vp]
+        L.sps_paged_reserve.argtypes = [vp, vp, vp, vp, vp, vp]
+        L.sps_paged_pool_workspace_bytes.argtypes = [i32]
+        L.sps_paged_pool_workspace_bytes.restype = i64
+        L.sps_paged_compact.argtypes = [vp, vp, vp, vp, vp, vp, vp]
+        L.sps_paged_copy.argtypes = [vp, i32, vp, vp]
+        L.sps_beam_select.argtypes = [vp, i32, i64, i32, i32, i32, f64, vp, vp, i32, i32, vp, vp, vp, vp, vp, vp]
+        L.sps_beam_select_workspace_bytes.argtypes = [i32, i32, i32]
+        L.sps_beam_select_workspace_bytes.restype = i64
         _lib = L
     return _lib
 
@@ -614,3 +635,153 @@ def sps_paged_attention(cache, batch, q, out, workspace, scale=0.0, lse=None, st
     if workspace.nbytes < _workspace_bytes(cache, shape[1], rq.dtype) or not workspace.is_contiguous():
         raise ValueError("workspace not contiguous, or smaller than sps_paged_attention_workspace_bytes")
     _on(index, lib().sps_paged_attention, stream, cache._p, batch._p, shape[0], C.byref(rq), C.byref(ro), scale, lse_p, workspace.data_ptr())
+
+
+# ---------------------------------------------------------------------------------------------------------------------
+# a paged cache's pages, and the selection of a beam step (see include/sps.h)
+# ---------------------------------------------------------------------------------------------------------------------
+PAGED_NO_PAGE, PAGED_BAD_ROW = 8, 16
+
+
+def _ints(t, shape, index, what):
+    """A contiguous CUDA int32 tensor of that shape on device `index`."""
+    if t.dtype is not _Torch.int32 or t.get_device() != index or tuple(t.shape) != shape or not t.is_contiguous():
+        raise ValueError("%s is contiguous int32 %s on the same CUDA device" % (what, list(shape)))
+    return t.data_ptr()
+
+
+class PagePool:
+    """A pool's state: refs CUDA int32 [n_pages], the table rows that hold each page (all zeros: an empty pool).  `status` (int32
+    [1], made here unless given) collects PAGED_* bits and is never cleared by the calls."""
+
+    def __init__(self, refs, page_size, status=None):
+        import torch
+        if _Torch.codes is None:
+            _Torch.load()
+        if refs.dim() != 1 or not refs.is_cuda:
+            raise ValueError("refs is a CUDA int32 tensor [n_pages]")
+        self.refs, self.page_size, self.index = refs, int(page_size), refs.get_device()
+        p = _ints(refs, (refs.shape[0],), self.index, "refs")
+        self.status = torch.zeros(1, dtype=torch.int32, device=refs.device) if status is None else status
+        self._c = sps_page_pool(p, _ints(self.status, (1,), self.index, "status"), refs.shape[0], self.page_size)
+        self._p = C.addressof(self._c)
+
+
+class PageTable:
+    """Rows of pages: pages CUDA int32 [B, ld], held (pages of each row) and lens (tokens) CUDA int32 [B]."""
+
+    def __init__(self, pages, held, lens):
+        if _Torch.codes is None:
+            _Torch.load()
+        if pages.dim() != 2 or not pages.is_cuda:
+            raise ValueError("pages is a CUDA int32 tensor [B, ld]")
+        B, ld = pages.shape
+        self.pages, self.held, self.lens, self.index, self.B = pages, held, lens, pages.get_device(), B
+        self._c = sps_page_table(_ints(pages, (B, ld), self.index, "pages"), _ints(held, (B,), self.index, "held"), _ints(lens, (B,), self.index, "lens"), B, ld)
+        self._p = C.addressof(self._c)
+
+
+class PageMoves:
+    """Pages to be copied: list CUDA int32 [capacity, 3] of (from, to, slots), count CUDA int32 [1]."""
+
+    def __init__(self, list, count):
+        if _Torch.codes is None:
+            _Torch.load()
+        if list.dim() != 2 or not list.is_cuda:
+            raise ValueError("list is a CUDA int32 tensor [capacity, 3]")
+        self.list, self.count, self.index = list, count, list.get_device()
+        self._c = sps_page_moves(_ints(list, (list.shape[0], 3), self.index, "list"), _ints(count, (1,), self.index, "count"), list.shape[0])
+        self._p = C.addressof(self._c)
+
+
+class PagedLayers:
+    """The caches of a model's layers (PagedCache, all of one shape, dtype and strides), as sps_paged_copy takes them."""
+
+    def __init__(self, caches):
+        if _Torch.codes is None:
+            _Torch.load()
+        self.caches = list(caches)
+        if not self.caches or any(c.index != self.caches[0].index for c in self.caches):
+            raise ValueError("caches of one CUDA device, at least one")
+        self.index = self.caches[0].index
+        self._c = (sps_paged_cache * len(self.caches))(*[c._c for c in self.caches])
+        self._p = C.addressof(self._c)
+
+
+def sps_paged_pool_workspace_bytes(n_pages):
+    n = int(lib().sps_paged_pool_workspace_bytes(n_pages))
+    if n < 0:
+        _check(SPS_EINVAL)
+    return n
+
+
+def _pool_workspace(pool, workspace):
+    if workspace.get_device() != pool.index or not workspace.is_contiguous() or workspace.nbytes < lib().sps_paged_pool_workspace_bytes(pool._c.n_pages):
+        raise ValueError("workspace: on the pool's device, contiguous, of sps_paged_pool_workspace_bytes")
+    return workspace.data_ptr()
+
+
+def sps_paged_fork(pool, src, dst, parents, stream=None):
+    """Row i of dst becomes row parents[i] of src (-1: an empty row); dst takes src's place in the pool."""
+    index = pool.index
+    if src.index != index or dst.index != index:
+        raise ValueError("all tensors must be on one CUDA device")
+    _on(index, lib().sps_paged_fork, stream, pool._p, src._p, dst._p, _ints(parents, (dst.B,), index, "parents"))
+
+
+def sps_paged_reserve(pool, table, want, moves, workspace, stream=None):
+    """Every row keeps min(len, want) tokens and gets room for want of them; `moves` are then to be copied."""
+    index = pool.index
+    if table.index != index or moves.index != index:
+        raise ValueError("all tensors must be on one CUDA device")
+    _on(index, lib().sps_paged_reserve, stream, pool._p, table._p, _ints(want, (table.B,), index, "want"), moves._p, _pool_workspace(pool, workspace))
+
+
+def sps_paged_compact(pool, src, dst, refs_out, moves, workspace, stream=None):
+    """Pages above the number in use move below it; dst, refs_out and `moves` receive the result (dst may be src, refs_out pool.refs)."""
+    index = pool.index
+    if src.index != index or dst.index != index or moves.index != index:
+        raise ValueError("all tensors must be on one CUDA device")
+    _on(index, lib().sps_paged_compact, stream, pool._p, src._p, dst._p, _ints(refs_out, (pool._c.n_pages,), index, "refs_out"), moves._p,
+        _pool_workspace(pool, workspace))
+
+
+def sps_paged_copy(layers, moves, stream=None):
+    """The listed pages' first slots, in every layer's keys and values."""
+    if moves.index != layers.index:
+        raise ValueError("all tensors must be on one CUDA device")
+    _on(layers.index, lib().sps_paged_copy, stream, layers._p, len(layers._c), moves._p)
+
+
+def sps_beam_select_workspace_bytes(B, W, V):
+    n = int(lib().sps_beam_select_workspace_bytes(B, W, V))
+    if n < 0:
+        _check(SPS_EINVAL)
+    return n
+
+
+def sps_beam_select(logits, scores, out_scores, out_parents, out_tokens, workspace, done=None, out_done=None, end_token=-1,
+                    temperature=1.0, stream=None):
+    """The N best continuations of each sequence's beams.  logits CUDA [B, W, V], fp32 or bf16 (rows of any one stride); scores CUDA
+    float32 [B, W]; done CUDA int32 [B, W]; out_scores float32, out_parents (rows b W + w), out_tokens, out_done int32, all
+    [B, N]; workspace CUDA uint8 (zeroed once) of sps_beam_select_workspace_bytes."""
+    code = _dtype_of(logits)
+    index = logits.get_device()
+    if logits.dim() != 3 or index < 0:
+        raise ValueError("logits is a CUDA tensor [B, W, V]")
+    B, W, V = logits.shape
+    sb, sw, sv = logits.stride()
+    row = sw if W > 1 else sb
+    if (sv != 1 and V > 1) or (W > 1 and B > 1 and sb != W * sw):
+        raise ValueError("the rows of logits must be contiguous, one stride apart")
+    N = out_scores.shape[1] if out_scores.dim() == 2 else 0
+    for t, n, what in ((scores, W, "scores"), (out_scores, N, "out_scores")):
+        if t.dtype is not _Torch.float32 or t.get_device() != index or tuple(t.shape) != (B, n) or not t.is_contiguous():
+            raise ValueError("%s is contiguous float32 %s on the logits' device" % (what, [B, n]))
+    need = lib().sps_beam_select_workspace_bytes(B, W, V)
+    if workspace.get_device() != index or not workspace.is_contiguous() or workspace.nbytes < need:
+        raise ValueError("workspace: on the logits' device, contiguous, of sps_beam_select_workspace_bytes")
+    _on(index, lib().sps_beam_select, stream, logits.data_ptr(), code, row, B, W, V, temperature, scores.data_ptr(),
+        _ints(done, (B, W), index, "done") if done is not None else None, end_token, N, out_scores.data_ptr(),
+        _ints(out_parents, (B, N), index, "out_parents"), _ints(out_tokens, (B, N), index, "out_tokens"),
+        _ints(out_done, (B, N), index, "out_done") if out_done is not None else None, workspace.data_ptr())

@@ -364,6 +364,9 @@ PagedSeqs seqs(const sps_paged_cache* c, const sps_paged_batch* b, int rows) {
 
 }  // namespace
 
+const char* paged_bad_cache(const sps_paged_cache* c) { return bad_cache(c); }
+int paged_sms() { return sms(); }
+
 extern "C" {
 
 int sps_rotary_frequencies(int32_t rot_dim, double base, int32_t scaling, double factor, int32_t trained_len, double low_turns,

@@ -27,6 +27,10 @@ __device__ __forceinline__ int paged_capacity(const PagedSeqs& s) {
   return c > 0x7fff0000ll ? 0x7fff0000 : (int)c;
 }
 
+// argument check of a cache (null: good) and SMs of the current device, for the other files' entry points
+const char* paged_bad_cache(const sps_paged_cache* c);
+int paged_sms();
+
 // first row and rows, of those inside the call's buffers; tokens up to the last such row's own (rows behind the buffers take
 // theirs with them); cut: kv_len did not fit the page table
 struct SeqGeom { int row0, nq, len; bool cut; };
