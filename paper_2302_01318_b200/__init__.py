@@ -645,7 +645,7 @@ PAGED_NO_PAGE, PAGED_BAD_ROW = 8, 16
 
 def _ints(t, shape, index, what):
     """A contiguous CUDA int32 tensor of that shape on device `index`."""
-    if t.dtype is not _Torch.int32 or t.get_device() != index or tuple(t.shape) != shape or not t.is_contiguous():
+    if t.dtype is not _Torch.int32 or t.shape != shape or not t.is_contiguous() or t.get_device() != index:
         raise ValueError("%s is contiguous int32 %s on the same CUDA device" % (what, list(shape)))
     return t.data_ptr()
 
@@ -767,21 +767,33 @@ def sps_beam_select(logits, scores, out_scores, out_parents, out_tokens, workspa
     [B, N]; workspace CUDA uint8 (zeroed once) of sps_beam_select_workspace_bytes."""
     code = _dtype_of(logits)
     index = logits.get_device()
-    if logits.dim() != 3 or index < 0:
+    shape = logits.shape
+    if len(shape) != 3 or index < 0:
         raise ValueError("logits is a CUDA tensor [B, W, V]")
-    B, W, V = logits.shape
+    B, W, V = shape
     sb, sw, sv = logits.stride()
-    row = sw if W > 1 else sb
     if (sv != 1 and V > 1) or (W > 1 and B > 1 and sb != W * sw):
         raise ValueError("the rows of logits must be contiguous, one stride apart")
-    N = out_scores.shape[1] if out_scores.dim() == 2 else 0
-    for t, n, what in ((scores, W, "scores"), (out_scores, N, "out_scores")):
-        if t.dtype is not _Torch.float32 or t.get_device() != index or tuple(t.shape) != (B, n) or not t.is_contiguous():
-            raise ValueError("%s is contiguous float32 %s on the logits' device" % (what, [B, n]))
-    need = lib().sps_beam_select_workspace_bytes(B, W, V)
-    if workspace.get_device() != index or not workspace.is_contiguous() or workspace.nbytes < need:
+    out = out_scores.shape
+    ints, f32 = _Torch.int32, _Torch.float32
+    if scores.dtype is not f32 or scores.shape != shape[:2] or not scores.is_contiguous() or scores.get_device() != index:
+        raise ValueError("scores is contiguous float32 [B, W] on the logits' device")
+    if out_scores.dtype is not f32 or len(out) != 2 or out[0] != B or not out_scores.is_contiguous() or out_scores.get_device() != index:
+        raise ValueError("out_scores is contiguous float32 [B, N] on the logits' device")
+    if out_parents.dtype is not ints or out_parents.shape != out or not out_parents.is_contiguous() or out_parents.get_device() != index or \
+            out_tokens.dtype is not ints or out_tokens.shape != out or not out_tokens.is_contiguous() or out_tokens.get_device() != index:
+        raise ValueError("out_parents and out_tokens are contiguous int32 [B, N] on the logits' device")
+    done_p = over_p = None
+    if done is not None:
+        if done.dtype is not ints or done.shape != shape[:2] or not done.is_contiguous() or done.get_device() != index:
+            raise ValueError("done is contiguous int32 [B, W] on the logits' device")
+        done_p = done.data_ptr()
+    if out_done is not None:
+        if out_done.dtype is not ints or out_done.shape != out or not out_done.is_contiguous() or out_done.get_device() != index:
+            raise ValueError("out_done is contiguous int32 [B, N] on the logits' device")
+        over_p = out_done.data_ptr()
+    L = lib()
+    if workspace.nbytes < L.sps_beam_select_workspace_bytes(B, W, V) or workspace.get_device() != index or not workspace.is_contiguous():
         raise ValueError("workspace: on the logits' device, contiguous, of sps_beam_select_workspace_bytes")
-    _on(index, lib().sps_beam_select, stream, logits.data_ptr(), code, row, B, W, V, temperature, scores.data_ptr(),
-        _ints(done, (B, W), index, "done") if done is not None else None, end_token, N, out_scores.data_ptr(),
-        _ints(out_parents, (B, N), index, "out_parents"), _ints(out_tokens, (B, N), index, "out_tokens"),
-        _ints(out_done, (B, N), index, "out_done") if out_done is not None else None, workspace.data_ptr())
+    _on(index, L.sps_beam_select, stream, logits.data_ptr(), code, sw if W > 1 else sb, B, W, V, temperature, scores.data_ptr(), done_p, end_token, out[1],
+        out_scores.data_ptr(), out_parents.data_ptr(), out_tokens.data_ptr(), over_p, workspace.data_ptr())

@@ -2,7 +2,11 @@
 #include <climits>
 #include <cmath>
 
+#include <cooperative_groups.h>
+
 #include "paged.cuh"
+
+namespace cg = cooperative_groups;
 
 // ------------------------------------------------------------------------------------------------------------------
 // c[w, v] = s[w] + l[w, v] / T - log sum_u exp(l[w, u] / T); the N best (w, v) of each sequence, ties to the lowest w V + v.
@@ -17,25 +21,25 @@
 // ------------------------------------------------------------------------------------------------------------------
 namespace {
 
-constexpr int SCAN_THREADS = 256, SCAN_WARPS = 8, SCAN_SEGS = 4;      // segments a warp loads at a time
-constexpr int SCAN_PART = SCAN_WARPS * SCAN_SEGS;                     // the least segments of a part (a CTA's)
-constexpr int PICK_THREADS = 256, PICK_WARPS = 8, PICK_CAP = 512;
-constexpr int BEAM_MAX_W = 128, BEAM_MAX_N = 128;
+constexpr int SCAN_THREADS = 256, SCAN_WARPS = 8, SCAN_SEGS = 4;       // segments of a group: a warp's load
+constexpr int ONE_RUN = 8, ONE_CTAS = 8, ONE_THREADS = 512, ONE_WARPS = ONE_CTAS * ONE_THREADS / 32;                         // the kernel for little work
+constexpr int PICK_CAP = 1024, PICK_SPLIT = 8, PICK_PER = 8;           // entries of a list, threads that rank one, segments a thread holds
+constexpr int BEAM_MAX_B = 8192, BEAM_MAX_W = 128, BEAM_MAX_N = 128;
 
 struct BeamArgs {
   const void* logits;
   long long row_stride;
   int B, W, V, N;
-  double inv_t;
-  float c;                   // log2(e) / T
+  double inv_t, t;
+  float c, inv_t32;          // log2(e) / T, 1 / T
   const float* scores;
   const int32_t* done;       // or null
   int end_token;
   float* out_scores;
   int32_t *out_parents, *out_tokens, *out_done;   // out_done: or null
   float* seg_max;            // [B W][n_seg]
-  float2* parts;             // [B W][n_parts]: maximum, sum of exponentials
-  int n_seg, n_parts, part_segs;
+  float2* parts;             // [B W][max_parts]: maximum, sum of exponentials
+  int n_seg, groups, run, max_parts;   // segments and groups of a row, groups of a run, parts a row may have
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -50,12 +54,19 @@ __device__ __forceinline__ int ordered(float x) {
 }
 __device__ __forceinline__ float unordered(int i) { return __int_as_float(i ^ ((i >> 31) & 0x7fffffff)); }
 
+// E logits in 16 bytes
 template <typename T> struct Logit;
 template <> struct Logit<float> {
   static constexpr int E = 4;
   static __device__ __forceinline__ float get(const float* p) { return *p; }
   static __device__ __forceinline__ void unpack(uint4 u, float (&f)[4]) {
     f[0] = __uint_as_float(u.x); f[1] = __uint_as_float(u.y); f[2] = __uint_as_float(u.z); f[3] = __uint_as_float(u.w);
+  }
+  static __device__ __forceinline__ uint4 pack(const float (&f)[4]) {
+    return make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+  }
+  static __device__ __forceinline__ float top(uint4 u) {   // NaN left out, by this one and the next
+    return fmaxf(fmaxf(fmaxf(__uint_as_float(u.x), -INFINITY), __uint_as_float(u.y)), fmaxf(__uint_as_float(u.z), __uint_as_float(u.w)));
   }
 };
 template <> struct Logit<__nv_bfloat16> {
@@ -69,6 +80,17 @@ template <> struct Logit<__nv_bfloat16> {
       f[2 * i + 1] = __uint_as_float(w[i] & 0xffff0000u);
     }
   }
+  static __device__ __forceinline__ uint4 pack(const float (&f)[8]) {   // (of numbers that are bf16)
+    uint32_t w[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) w[i] = __float_as_uint(f[2 * i]) >> 16 | (__float_as_uint(f[2 * i + 1]) & 0xffff0000u);
+    return make_uint4(w[0], w[1], w[2], w[3]);
+  }
+  static __device__ __forceinline__ float top(uint4 u) {
+    auto two = [](uint32_t w) { return *reinterpret_cast<const __nv_bfloat162*>(&w); };
+    const __nv_bfloat162 m = __hmax2(__hmax2(two(u.x), two(u.y)), __hmax2(two(u.z), two(u.w)));
+    return fmaxf(fmaxf(__low2float(m), -INFINITY), __high2float(m));
+  }
 };
 
 // a beam that reads its logits: it has a score, and is not done
@@ -76,195 +98,434 @@ __device__ __forceinline__ bool beam_reads(const BeamArgs& a, int row) {
   return !(a.done && a.done[row]) && isfinite(a.scores[row]);
 }
 
-// (m, s) of a set and of another: sums are relative to the maxima
-__device__ __forceinline__ void merge(float& m, float& s, float m1, float s1, float c) {
-  const float t = fmaxf(m, m1), r = t == -INFINITY ? 0.f : t;
-  s = s * ex2((m - r) * c) + s1 * ex2((m1 - r) * c);
-  m = t;
+// (m, s) of the warp from its lanes': sums are relative to the maxima
+__device__ __forceinline__ void warp_merge(float& m, float& s, float c) {
+  const float all = unordered(__reduce_max_sync(0xffffffffu, ordered(m))), r = all == -INFINITY ? 0.f : all;
+  s = warp_sum(s * ex2((m - r) * c));
+  m = all;
 }
 
+// A lane's running maximum m and sum of 2^(c l - R), R = c m rounded: one fused operation per exponent, whose rounding is the
+// difference's alone; what R's own rounding leaves, R - c m, is exact in one more and put right at the end.  With maxima beyond
+// 2^20 / c (`far`, for the rest of the part) differences are taken first: c l might overflow.
+struct Running {
+  float m, R, s;
+  bool far;
+};
+template <typename T>
+__device__ __forceinline__ void running_add(Running& r, const uint4 (&u)[SCAN_SEGS], float top, float c) {
+  constexpr int E = Logit<T>::E;
+  const float m1 = fmaxf(r.m, top), R1 = m1 == -INFINITY ? 0.f : m1 * c;
+  if (!r.far && __any_sync(0xffffffffu, !(fabsf(R1) < 1048576.f))) {
+    r.far = true;
+    if (r.m > -INFINITY) r.s *= ex2(-fmaf(r.m, c, -r.R));
+  }
+  float s0 = 0.f, s1 = 0.f;
+  if (r.far) {
+    const float ref = m1 == -INFINITY ? 0.f : m1;
+    r.s *= ex2((r.m - ref) * c);
+#pragma unroll
+    for (int j = 0; j < SCAN_SEGS; ++j) {
+      float f[E];
+      Logit<T>::unpack(u[j], f);
+#pragma unroll
+      for (int e = 0; e < E; ++e) s0 += ex2((f[e] - ref) * c);
+    }
+  } else {
+    r.s *= ex2(r.R - R1);
+#pragma unroll
+    for (int j = 0; j < SCAN_SEGS; ++j) {
+      float f[E];
+      Logit<T>::unpack(u[j], f);
+#pragma unroll
+      for (int e = 0; e < E; e += 2) {
+        s0 += ex2(fmaf(f[e], c, -R1));
+        s1 += ex2(fmaf(f[e + 1], c, -R1));
+      }
+    }
+    r.R = m1 == -INFINITY ? -INFINITY : R1;
+  }
+  r.s += s0 + s1;
+  r.m = m1;
+}
+
+// A run of the list of `rows` rows' groups (SCAN_SEGS segments; the last of a row may be short), from group x0 of the list on, by
+// one warp: its next group is under way while it works on this one, whatever the rows' number and length.  A run's share of a
+// row is a part of it; beams that are done or dead are skipped.  seg_max, parts: the list's.
 template <typename T, bool VEC>
-__global__ void __launch_bounds__(SCAN_THREADS) beam_scan_kernel(const __grid_constant__ BeamArgs a) {
-  constexpr int E = Logit<T>::E, SEG = 32 * E;
-  __shared__ float s_m[SCAN_WARPS], s_s[SCAN_WARPS];
-  pdl_launch_dependents();
-  const int row = blockIdx.x / a.n_parts, part = blockIdx.x - row * a.n_parts;
-  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
-  pdl_wait();
-  if (!beam_reads(a, row)) return;
-  const T* x = reinterpret_cast<const T*>(a.logits) + (long long)row * a.row_stride;
-  const int s0 = part * a.part_segs, s1 = min(s0 + a.part_segs, a.n_seg);
-  float m = -INFINITY, s = 0.f;
-  for (int seg = s0 + warp * SCAN_SEGS; seg < s1; seg += SCAN_PART) {
-    float f[SCAN_SEGS][E];
-    const bool whole = (long long)(seg + SCAN_SEGS) * SEG <= a.V;
-    if (VEC && whole) {
-      uint4 u[SCAN_SEGS];
+__device__ __forceinline__ void beam_scan(const BeamArgs& a, int first_row, int rows, int me, float* seg_max, float2* parts) {
+  constexpr int E = Logit<T>::E, SEG = 32 * E, GROUP = SCAN_SEGS * SEG;
+  const int lane = threadIdx.x & 31;
+  const long long x0 = (long long)me * a.run;
+  const int whole = a.V / GROUP;   // groups of a row that are inside it
+  if (x0 >= (long long)rows * a.groups) return;
+  int row = (int)x0 / a.groups, g = (int)x0 - row * a.groups, left = (int)min((long long)a.run, (long long)rows * a.groups - x0);
+  const T* x = reinterpret_cast<const T*>(a.logits) + (long long)(first_row + row) * a.row_stride;
+  uint4 u[SCAN_SEGS];
+  auto fetch = [&](const T* p, int group) {
 #pragma unroll
-      for (int j = 0; j < SCAN_SEGS; ++j) u[j] = *reinterpret_cast<const uint4*>(x + (seg + j) * SEG + lane * E);
+    for (int j = 0; j < SCAN_SEGS; ++j) u[j] = *reinterpret_cast<const uint4*>(p + (long long)group * GROUP + j * SEG + lane * E);
+  };
+  bool fetched = VEC && g < whole;
+  if (fetched) fetch(x, g);   // (before its row is known to be read)
+  int row0 = row;
+  unsigned live = __ballot_sync(0xffffffffu, row + lane < rows && beam_reads(a, first_row + min(row + lane, rows - 1)));
+  Running run{-INFINITY, -INFINITY, 0.f, false};
+  while (left > 0) {
+    if (row - row0 >= 32) {
+      row0 = row;
+      live = __ballot_sync(0xffffffffu, row + lane < rows && beam_reads(a, first_row + min(row + lane, rows - 1)));
+    }
+    if (!((live >> (row - row0)) & 1)) {
+      left -= a.groups - g;
+      ++row;
+      x += a.row_stride;
+      g = 0;
+      fetched = VEC && left > 0 && whole > 0 && row - row0 < 32 && ((live >> (row - row0)) & 1);
+      if (fetched) fetch(x, 0);
+      continue;
+    }
+    uint4 now[SCAN_SEGS];
+    if (VEC && g < whole) {
+      if (!fetched) fetch(x, g);
 #pragma unroll
-      for (int j = 0; j < SCAN_SEGS; ++j) Logit<T>::unpack(u[j], f[j]);
+      for (int j = 0; j < SCAN_SEGS; ++j) now[j] = u[j];
     } else {
 #pragma unroll
-      for (int j = 0; j < SCAN_SEGS; ++j)
+      for (int j = 0; j < SCAN_SEGS; ++j) {
+        float f[E];
 #pragma unroll
         for (int e = 0; e < E; ++e) {
-          const int v = (seg + j) * SEG + e * 32 + lane;
-          f[j][e] = v < a.V ? Logit<T>::get(x + v) : -INFINITY;
+          const int v = g * GROUP + j * SEG + e * 32 + lane;
+          f[e] = v < a.V ? Logit<T>::get(x + v) : -INFINITY;
         }
+        now[j] = Logit<T>::pack(f);
+      }
     }
+    const bool ends = g + 1 == a.groups || left == 1;
+    if (g + 1 < a.groups) fetched = VEC && left > 1 && g + 1 < whole;
+    else fetched = VEC && left > 1 && whole > 0 && row + 1 - row0 < 32 && ((live >> (row + 1 - row0)) & 1);
+    if (fetched) { if (g + 1 < a.groups) fetch(x, g + 1); else fetch(x + a.row_stride, 0); }
     float top = -INFINITY;
     int best = 0;
 #pragma unroll
     for (int j = 0; j < SCAN_SEGS; ++j) {
-      float t = f[j][0];
-#pragma unroll
-      for (int e = 1; e < E; ++e) t = fmaxf(t, f[j][e]);
-      t = fmaxf(t, -INFINITY);      // (NaN left out)
+      const float t = Logit<T>::top(now[j]);
       top = fmaxf(top, t);
       const int w = __reduce_max_sync(0xffffffffu, ordered(t));
       if (lane == j) best = w;
     }
-    if (lane < SCAN_SEGS && seg + lane < s1) a.seg_max[(long long)row * a.n_seg + seg + lane] = unordered(best);
-    const float m1 = fmaxf(m, top), r = m1 == -INFINITY ? 0.f : m1;
-    s *= ex2((m - r) * a.c);
-    m = m1;
-#pragma unroll
-    for (int j = 0; j < SCAN_SEGS; ++j)
-#pragma unroll
-      for (int e = 0; e < E; ++e) s += ex2((f[j][e] - r) * a.c);
-  }
-#pragma unroll
-  for (int o = 16; o > 0; o >>= 1) {
-    const float m1 = __shfl_xor_sync(0xffffffffu, m, o), v1 = __shfl_xor_sync(0xffffffffu, s, o);
-    merge(m, s, m1, v1, a.c);
-  }
-  if (lane == 0) { s_m[warp] = m; s_s[warp] = s; }
-  __syncthreads();
-  if (threadIdx.x == 0) {
-    for (int w = 1; w < SCAN_WARPS; ++w) merge(m, s, s_m[w], s_s[w], a.c);
-    a.parts[(long long)row * a.n_parts + part] = make_float2(m, s);
+    if (lane < SCAN_SEGS && g * SCAN_SEGS + lane < a.n_seg) seg_max[(long long)row * a.n_seg + g * SCAN_SEGS + lane] = unordered(best);
+    running_add<T>(run, now, top, a.c);
+    if (ends) {
+      float m = run.m, s = run.s;
+      if (!run.far && m > -INFINITY) s *= ex2(-fmaf(m, a.c, -run.R));
+      warp_merge(m, s, a.c);
+      if (lane == 0) parts[(long long)row * a.max_parts + me - row * a.groups / a.run] = make_float2(m, s);
+      run = Running{-INFINITY, -INFINITY, 0.f, false};
+    }
+    --left;
+    if (++g == a.groups) { g = 0; ++row; x += a.row_stride; }
   }
 }
 
-// The N best of a stream of (score, place), places falling ties to the lowest: a buffer of PICK_CAP and the bound below which
-// nothing is taken, the N-th best so far once there are N.
+// Picking: candidates are (score, place) pairs, ties falling to the lowest place, so that all differ.  A list takes those that
+// reach a bound which at least N reach; only where more reach it than the list holds (ties by the hundred, rising rows) is the
+// stream taken in rounds, the list cut to its N best whenever it might overflow.
 struct Best {
-  double* key[2];
-  int* at[2];
+  double* key;        // [PICK_CAP]
+  int* at;
+  double* keep_key;   // [BEAM_MAX_N]: the N best, in order
+  int* keep_at;
   int* count;
-  int side;
-  double bound;
-  int bound_at;
 };
 __device__ __forceinline__ bool better(double k, int i, double k1, int i1) { return k > k1 || (k == k1 && i < i1); }
-__device__ __forceinline__ void best_push(Best& b, double k, int i) {
-  if (!better(k, i, b.bound, b.bound_at)) return;
+__device__ __forceinline__ void best_push(const Best& b, double k, int i) {
   const int n = atomicAdd(b.count, 1);
-  b.key[b.side][n] = k;
-  b.at[b.side][n] = i;
+  if (n < PICK_CAP) { b.key[n] = k; b.at[n] = i; }
 }
-// leaves the N best in order and raises the bound (every thread of the CTA calls it); the buffer's count is returned
-__device__ __forceinline__ int best_prune(Best& b, int N) {
-  __syncthreads();
-  const int n = *b.count, keep = min(n, N);
-  const double* key = b.key[b.side];
-  const int* at = b.at[b.side];
-  for (int i = threadIdx.x; i < n; i += PICK_THREADS) {
-    const double k = key[i];
-    const int p = at[i];
+// the list's N best to keep_key / keep_at in order, every entry counting those before it, PICK_SPLIT threads to an entry;
+// returns how many there are (every thread of the CTA calls it, the list is complete)
+template <int THREADS>
+__device__ __forceinline__ int best_rank(const Best& b, int N) {
+  const int n = min(*b.count, PICK_CAP), sub = threadIdx.x % PICK_SPLIT;
+  for (int i0 = 0; i0 < n; i0 += THREADS / PICK_SPLIT) {
+    const int i = i0 + threadIdx.x / PICK_SPLIT;
+    const double k = i < n ? b.key[i] : 0.0;
+    const int p = i < n ? b.at[i] : 0;
     int r = 0;
-    for (int j = 0; j < n; ++j) r += better(key[j], at[j], k, p);
-    if (r < N) { b.key[b.side ^ 1][r] = k; b.at[b.side ^ 1][r] = p; }
+    if (i < n)
+#pragma unroll 4
+      for (int j = sub; j < n; j += PICK_SPLIT) r += better(b.key[j], b.at[j], k, p);
+#pragma unroll
+    for (int o = PICK_SPLIT / 2; o > 0; o >>= 1) r += __shfl_xor_sync(0xffffffffu, r, o);
+    if (i < n && sub == 0 && r < N) { b.keep_key[r] = k; b.keep_at[r] = p; }
   }
   __syncthreads();
-  if (threadIdx.x == 0) *b.count = keep;
-  b.side ^= 1;
-  if (n >= N) { b.bound = b.key[b.side][N - 1]; b.bound_at = b.at[b.side][N - 1]; }
-  __syncthreads();
-  return keep;
+  return min(n, N);
 }
-__device__ __forceinline__ void best_room(Best& b, int N) {   // room for a push by every thread
+// the N best of item(0 .. all - 1) -> (key, place), -inf keys left out, in rounds
+template <int THREADS, class Item>
+__device__ __noinline__ int best_rounds(const Best& b, int N, int all, Item item) {
+  int have = 0;
   __syncthreads();
-  const int n = *b.count;
-  if (n > PICK_CAP - PICK_THREADS) best_prune(b, N);
-  else __syncthreads();
+  for (int i0 = 0; i0 < all; i0 += PICK_CAP - BEAM_MAX_N) {
+    for (int i = threadIdx.x; i < have; i += THREADS) { b.key[i] = b.keep_key[i]; b.at[i] = b.keep_at[i]; }
+    if (threadIdx.x == 0) *b.count = have;
+    __syncthreads();
+    const double bound = have == N ? b.key[N - 1] : -INFINITY;
+    const int bound_at = have == N ? b.at[N - 1] : 0;
+    for (int i = i0 + threadIdx.x; i < min(i0 + PICK_CAP - BEAM_MAX_N, all); i += THREADS) {
+      int at;
+      const double k = item(i, &at);
+      if (better(k, at, bound, bound_at)) best_push(b, k, at);
+    }
+    __syncthreads();
+    have = best_rank<THREADS>(b, N);
+  }
+  return have;
 }
 
-template <typename T>
-__global__ void __launch_bounds__(PICK_THREADS) beam_pick_kernel(const __grid_constant__ BeamArgs a) {
-  constexpr int E = Logit<T>::E, SEG = 32 * E;
-  __shared__ double s_key[2][PICK_CAP], s_base[BEAM_MAX_W];
-  __shared__ float s_max[BEAM_MAX_W];
-  __shared__ int s_at[2][PICK_CAP], s_seg[BEAM_MAX_N], s_done[BEAM_MAX_W], s_count;
-  const int b = blockIdx.x, tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
-  pdl_launch_dependents();
-  pdl_wait();
-  // a beam's part of its candidates' scores, -inf where it has none: c = base + (l - max) / T
-  for (int w = warp; w < a.W; w += PICK_WARPS) {
-    const int row = b * a.W + w;
-    double base = -INFINITY;
-    float m = -INFINITY;
-    if (beam_reads(a, row)) {
-      for (int p = lane; p < a.n_parts; p += 32) m = fmaxf(m, a.parts[(long long)row * a.n_parts + p].x);
-      m = warp_max(m);
-      const float r = m == -INFINITY ? 0.f : m;
-      double s = 0.0;
-      for (int p = lane; p < a.n_parts; p += 32) {
-        const float2 v = a.parts[(long long)row * a.n_parts + p];
-        s += (double)v.y * exp(((double)v.x - (double)r) * a.inv_t);
-      }
-#pragma unroll
-      for (int o = 16; o > 0; o >>= 1) s += __shfl_xor_sync(0xffffffffu, s, o);
-      if (isfinite(m) && s > 0.0 && s < INFINITY) base = (double)a.scores[row] - log(s);
-    }
-    if (lane == 0) { s_base[w] = base; s_max[w] = m; s_done[w] = a.done ? a.done[row] : 0; }   // (out_done may be done)
+// a sequence's beams, where the pick finds them
+struct Beams {
+  float score[BEAM_MAX_W];
+  int done[BEAM_MAX_W];
+};
+template <int THREADS>
+__device__ __forceinline__ void beams_load(const BeamArgs& a, int b, Beams& beams) {
+  for (int w = threadIdx.x; w < a.W; w += THREADS) {
+    beams.score[w] = a.scores[b * a.W + w];
+    beams.done[w] = a.done ? a.done[b * a.W + w] : 0;
   }
-  Best best{{s_key[0], s_key[1]}, {s_at[0], s_at[1]}, &s_count, 0, -INFINITY, 0};   // (-inf is not taken)
-  if (tid == 0) s_count = 0;
-  __syncthreads();
-  // the N best segments
+}
+
+// the pick of sequence b by a CTA; first: its first row in the list that was cut into runs, seg_max and parts: from there on
+template <typename T, bool VEC, int THREADS>
+__device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, const Beams& beams, const float* seg_max, const float2* all_parts) {
+  constexpr int E = Logit<T>::E, SEG = 32 * E, WARPS = THREADS / 32, PER = PICK_PER;
+  __shared__ double s_key[PICK_CAP], s_keep[BEAM_MAX_N], s_base[BEAM_MAX_W];
+  __shared__ float s_max[BEAM_MAX_W], s_base32[BEAM_MAX_W];
+  __shared__ int s_thread[THREADS + WARPS], s_at[PICK_CAP], s_keep_at[BEAM_MAX_N], s_top[BEAM_MAX_N + 2 * WARPS], s_count, s_bound;
+  __shared__ int2 s_seg[BEAM_MAX_N];
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, N = a.N;
+  const Best best{s_key, s_at, s_keep, s_keep_at, &s_count};
   const int all = a.W * a.n_seg;
-  for (int i0 = 0; i0 < all; i0 += PICK_THREADS) {
-    const int i = i0 + tid;
-    best_room(best, a.N);
-    if (i < all) {
-      const int w = i / a.n_seg;
-      if (s_base[w] > -INFINITY) best_push(best, s_base[w] + ((double)a.seg_max[(long long)b * all + i] - (double)s_max[w]) * a.inv_t, i);
+  float held[PER];   // the first segments' maxima are on their way while the beams are looked at
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int i = tid + j * THREADS;
+    held[j] = i < all ? seg_max[i] : -INFINITY;
+  }
+  // a beam's part of its candidates' scores, -inf where it has none: c = base + (l - max) / T
+  for (int w = warp; w < a.W; w += WARPS) {
+    const float2* parts = all_parts + (long long)w * a.max_parts;
+    const int at = (first + w) * a.groups, n_parts = (at + a.groups - 1) / a.run - at / a.run + 1;
+    float m = -INFINITY, s = 0.f;
+    for (int p0 = 0; p0 < n_parts; p0 += 32) {   // (one round, but for few rows that are long)
+      float2 v = make_float2(-INFINITY, 0.f);
+      if (p0 + lane < n_parts) v = parts[p0 + lane];
+      warp_merge(v.x, v.y, a.c);
+      const float t = fmaxf(m, v.x), r = t == -INFINITY ? 0.f : t;
+      s = s * ex2((m - r) * a.c) + v.y * ex2((v.x - r) * a.c);
+      m = t;
+    }
+    if (lane == 0) {
+      const float score = beams.score[w];
+      const bool live = !beams.done[w] && isfinite(score) && isfinite(m) && s > 0.f && s < INFINITY;   // (else its parts were not written)
+      const double base = live ? (double)score - log((double)s) : -INFINITY;
+      s_base[w] = base;
+      s_base32[w] = (float)base;
+      s_max[w] = m;
     }
   }
-  const int segs = best_prune(best, a.N);
-  for (int i = tid; i < segs; i += PICK_THREADS) s_seg[i] = best.at[best.side][i];
+  if (tid == 0) { s_count = 0; s_bound = INT_MIN; }
+  __syncthreads();
+  auto score_of = [&](int w, float l) { return s_base[w] > -INFINITY ? s_base[w] + ((double)l - (double)s_max[w]) * a.inv_t : -INFINITY; };
+  // score_of in fp32, less and more than what its roundings (base, difference, 1 / T, product, sum: 2^-24 each of a term, once more
+  // of the sum) may come to; where the product leaves fp32's range, anything below the base
+  auto about = [&](int w, float l) {
+    const float base = s_base32[w], t = (l - s_max[w]) * a.inv_t32;
+    if (!(base > -INFINITY) || !(l > -INFINITY)) return make_float2(-INFINITY, -INFINITY);
+    const float v = base + t, e = fmaf(fabsf(base) + fabsf(t), 4.7683716e-7f, 1e-36f);   // 2^-21
+    return t > -INFINITY ? make_float2(v - e, v + e) : make_float2(-INFINITY, fmaf(fabsf(base), 4.7683716e-7f, base));
+  };
+  const int step_w = THREADS / a.n_seg, step_r = THREADS - step_w * a.n_seg;
+  // The N best segments.  Scores are first taken in fp32 with what these may be off by, below and above: at least N reach the
+  // bound with what they have at least, and only those that may reach it are scored in 64 bits.  The bound is the N-th of
+  // the groups' best threads, k from each group: a group is every WARPS-th thread, whose segments are of all beams
+  const int k = (N + WARPS - 1) / WARPS + 1;
+  const int w_first = tid / a.n_seg, r_first = tid - w_first * a.n_seg;
+  float high[PER], top = -INFINITY;
+  {
+    int w = w_first, r = r_first;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      high[j] = -INFINITY;
+      if (j * THREADS >= all) continue;
+      if (tid + j * THREADS < all) {
+        const float2 v = about(w, held[j]);
+        high[j] = v.y;
+        top = fmaxf(top, v.x);
+      }
+      w += step_w; r += step_r;
+      if (r >= a.n_seg) { r -= a.n_seg; ++w; }
+    }
+    for (int i = tid + PER * THREADS; i < all; i += THREADS) {
+      top = fmaxf(top, about(w, seg_max[i]).x);
+      w += step_w; r += step_r;
+      if (r >= a.n_seg) { r -= a.n_seg; ++w; }
+    }
+  }
+  s_thread[tid + tid / 32] = ordered(top);
+  __syncthreads();
+  int mine = s_thread[(lane * WARPS + warp) + (lane * WARPS + warp) / 32];
+  for (int j = 0; j < k; ++j) {
+    const int v = __reduce_max_sync(0xffffffffu, mine);
+    if (lane == 0) s_top[warp * k + j] = v;
+    if (__ffs(__ballot_sync(0xffffffffu, mine == v)) - 1 == lane) mine = INT_MIN;
+  }
+  __syncthreads();
+  for (int i = tid; i < k * WARPS; i += THREADS) {
+    const int v = s_top[i];
+    int r = 0;
+#pragma unroll 8
+    for (int j = 0; j < k * WARPS; ++j) r += s_top[j] > v || (s_top[j] == v && j < i);
+    if (r == N - 1) s_bound = v;
+  }
+  __syncthreads();
+  const float least = unordered(max(s_bound, ordered(-INFINITY)));
+  {
+    int w = w_first, r = r_first;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      if (j * THREADS >= all) continue;
+      if (high[j] >= least && high[j] > -INFINITY) best_push(best, score_of(w, held[j]), tid + j * THREADS);
+      w += step_w; r += step_r;
+      if (r >= a.n_seg) { r -= a.n_seg; ++w; }
+    }
+    for (int i = tid + PER * THREADS; i < all; i += THREADS) {
+      const float l = seg_max[i], h = about(w, l).y;
+      if (h >= least && h > -INFINITY) best_push(best, score_of(w, l), i);
+      w += step_w; r += step_r;
+      if (r >= a.n_seg) { r -= a.n_seg; ++w; }
+    }
+  }
+  __syncthreads();
+  // few more than N: all are read, else the N best
+  int segs = s_count;
+  double bound = least;
+  if (segs > BEAM_MAX_N) {
+    segs = segs > PICK_CAP ? best_rounds<THREADS>(best, N, all, [&](int i, int* at) { *at = i; return score_of(i / a.n_seg, seg_max[i]); })
+                           : best_rank<THREADS>(best, N);
+    bound = segs == N ? s_keep[N - 1] : -INFINITY;
+  }
+  const int* const from = s_count > BEAM_MAX_N ? s_keep_at : s_at;
+  for (int i = tid; i < segs; i += THREADS) {
+    const int w = from[i] / a.n_seg;
+    s_seg[i] = make_int2(w, (from[i] - w * a.n_seg) * SEG);
+  }
   __syncthreads();
   if (tid == 0) s_count = 0;
-  // their elements that reach the N-th segment's maximum, and the beams that are done
-  best.bound_at = INT_MAX;
-  for (int i0 = 0; i0 < segs; i0 += PICK_WARPS) {
-    const int i = i0 + warp;
-    const int w = i < segs ? s_seg[i] / a.n_seg : 0, v0 = i < segs ? (s_seg[i] - w * a.n_seg) * SEG : a.V;
-    const T* x = reinterpret_cast<const T*>(a.logits) + (long long)(b * a.W + w) * a.row_stride;
-    float f[E];
+  __syncthreads();
+  // their elements that reach the bound, and the beams that are done
+  auto row_of = [&](int w) { return reinterpret_cast<const T*>(a.logits) + (long long)(b * a.W + w) * a.row_stride; };
+  auto ended = [&](int w, int* at) {            // beam w's candidate, if it is done
+    const float s = beams.done[w] ? beams.score[w] : -INFINITY;
+    *at = w * a.V + a.end_token;
+    return isfinite(s) ? (double)s : -(double)INFINITY;
+  };
+  for (int i0 = warp; i0 < segs; i0 += 4 * WARPS) {
+    uint4 u[4];
+    int2 sg[4];
 #pragma unroll
-    for (int e = 0; e < E; ++e) f[e] = v0 + e * 32 + lane < a.V ? Logit<T>::get(x + v0 + e * 32 + lane) : -INFINITY;
+    for (int j = 0; j < 4; ++j) {
+      if (i0 + j * WARPS >= segs) continue;
+      sg[j] = s_seg[i0 + j * WARPS];
+      const T* x = row_of(sg[j].x) + sg[j].y + lane * E;
+      if (VEC && sg[j].y + SEG <= a.V) {
+        u[j] = *reinterpret_cast<const uint4*>(x);
+      } else {
+        float f[E];
 #pragma unroll
-    for (int e = 0; e < E; ++e) {
-      best_room(best, a.N);
-      if (f[e] > -INFINITY) best_push(best, s_base[w] + ((double)f[e] - (double)s_max[w]) * a.inv_t, w * a.V + v0 + e * 32 + lane);
+        for (int e = 0; e < E; ++e) f[e] = sg[j].y + lane * E + e < a.V ? Logit<T>::get(x + e) : -INFINITY;
+        u[j] = Logit<T>::pack(f);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      if (i0 + j * WARPS >= segs) continue;
+      float f[E];
+      Logit<T>::unpack(u[j], f);
+      // the least logit that may reach the bound, rounded down: nearly all are told from it by one comparison
+      const double base = s_base[sg[j].x], m = s_max[sg[j].x], off = (bound - base) * a.t;
+      const float low = __double2float_rd(m + off - (fabs(m) + fabs(off) + fabs(base) * a.t) * 1e-12);
+#pragma unroll
+      for (int e = 0; e < E; ++e) {
+        if (!(f[e] >= low)) continue;
+        const double v = score_of(sg[j].x, f[e]);
+        if (v >= bound && v > -INFINITY) best_push(best, v, sg[j].x * a.V + sg[j].y + lane * E + e);
+      }
     }
   }
-  best_room(best, a.N);
-  if (tid < a.W && s_done[tid] && isfinite(a.scores[b * a.W + tid]))
-    best_push(best, (double)a.scores[b * a.W + tid], tid * a.V + a.end_token);
-  const int n = best_prune(best, a.N);
-  for (int i = tid; i < a.N; i += PICK_THREADS) {
+  if (a.done && tid < a.W) {
+    int at;
+    const double v = ended(tid, &at);
+    if (v >= bound && v > -INFINITY) best_push(best, v, at);
+  }
+  __syncthreads();
+  auto element = [&](int i, int* at) {          // element i of the segments, one behind the other, then the done beams
+    if (i >= segs * SEG) return ended(i - segs * SEG, at);
+    const int2 sg = s_seg[i / SEG];
+    const int v = sg.y + i % SEG;
+    *at = sg.x * a.V + v;
+    return v < a.V ? score_of(sg.x, Logit<T>::get(row_of(sg.x) + v)) : -(double)INFINITY;
+  };
+  const int n = s_count > PICK_CAP ? best_rounds<THREADS>(best, N, segs * SEG + (a.done ? a.W : 0), element) : best_rank<THREADS>(best, N);
+  for (int i = tid; i < N; i += THREADS) {
     const bool there = i < n;
-    const int at = there ? best.at[best.side][i] : 0, w = at / a.V, v = at - w * a.V;
-    const long long o = (long long)b * a.N + i;
-    a.out_scores[o] = there ? (float)best.key[best.side][i] : -INFINITY;
+    const int at = there ? s_keep_at[i] : 0, w = at / a.V, v = at - w * a.V;
+    const long long o = (long long)b * N + i;
+    a.out_scores[o] = there ? (float)s_keep[i] : -INFINITY;
     a.out_parents[o] = there ? b * a.W + w : -1;
     a.out_tokens[o] = there ? v : -1;
-    if (a.out_done) a.out_done[o] = there && (v == a.end_token || s_done[w]);
+    if (a.out_done) a.out_done[o] = there && (v == a.end_token || beams.done[w]);
   }
+}
+
+// With a CTA to each part of a row 64 x 4 rows of 131071 took 20 us, as runs 15.  Neighbouring runs go to different CTAs, so that
+// beams that are skipped are spread over all.
+template <typename T, bool VEC>
+__global__ void __launch_bounds__(SCAN_THREADS, 4) beam_scan_kernel(const __grid_constant__ BeamArgs a) {
+  pdl_launch_dependents();
+  pdl_wait();
+  beam_scan<T, VEC>(a, 0, a.B * a.W, (threadIdx.x >> 5) * gridDim.x + blockIdx.x, a.seg_max, a.parts);
+}
+template <typename T, bool VEC, int THREADS>
+__global__ void __launch_bounds__(THREADS) beam_pick_kernel(const __grid_constant__ BeamArgs a) {
+  __shared__ Beams s_beams;
+  const int row = blockIdx.x * a.W;
+  pdl_launch_dependents();
+  pdl_wait();
+  beams_load<THREADS>(a, blockIdx.x, s_beams);
+  __syncthreads();
+  beam_pick<T, VEC, THREADS>(a, blockIdx.x, row, s_beams, a.seg_max + (long long)row * a.n_seg, a.parts + (long long)row * a.max_parts);
+}
+// Both for little work, a cluster to a sequence: what the scan finds goes straight to the shared memory of the CTA that picks.
+// One prompt of 4 x 32000: 8.6 us as two launches in a graph and 16 one by one (the host's), 9.9 and 12 this way through L2.
+template <typename T, bool VEC>
+__global__ void __cluster_dims__(ONE_CTAS, 1, 1) __launch_bounds__(ONE_THREADS, 2) beam_one_kernel(const __grid_constant__ BeamArgs a) {
+  __shared__ Beams s_beams;
+  __shared__ float s_segs[ONE_RUN * ONE_WARPS * SCAN_SEGS];
+  __shared__ float2 s_parts[ONE_WARPS + 2 * BEAM_MAX_W];
+  cg::cluster_group cl = cg::this_cluster();
+  const int rank = (int)cl.block_rank(), b = blockIdx.x / ONE_CTAS;
+  pdl_launch_dependents();
+  cl.sync();   // (the CTA that picks has to be there before others write to it)
+  pdl_wait();
+  if (rank == 0) beams_load<ONE_THREADS>(a, b, s_beams);
+  beam_scan<T, VEC>(a, b * a.W, a.W, (threadIdx.x >> 5) * ONE_CTAS + rank, cl.map_shared_rank(s_segs, 0), cl.map_shared_rank(s_parts, 0));
+  cl.sync();
+  if (rank == 0) beam_pick<T, VEC, ONE_THREADS>(a, b, 0, s_beams, s_segs, s_parts);
 }
 
 int no(int code, const char* msg) {
@@ -272,25 +533,38 @@ int no(int code, const char* msg) {
   return code;
 }
 const char* bad_shape(int B, int W, int V) {
-  if (B < 0 || B > 1 << 16 || W < 1 || W > BEAM_MAX_W || V < 1 || V > 1 << 24) return "beams: B must be 0 .. 2^16, W 1 .. 128, V 1 .. 2^24";
-  const int64_t parts = ((int64_t)V + 128 * SCAN_PART - 1) / (128 * SCAN_PART);
-  if ((int64_t)W * V > INT_MAX || (int64_t)B * W * parts > INT_MAX) return "beams: W x V must stay below 2^31, B x W x V below 2^43";
+  if (B < 0 || B > BEAM_MAX_B || W < 1 || W > BEAM_MAX_W || V < 1 || V > 1 << 24) return "beams: B must be 0 .. 8192, W 1 .. 128, V 1 .. 2^24";
+  if ((int64_t)W * V > INT_MAX || (int64_t)B * W * ((V + 511) / 512) > INT_MAX) return "beams: W x V must stay below 2^31, B x W x V below 2^40";
   return nullptr;
 }
 int64_t up(int64_t n) { return (n + 255) / 256 * 256; }
 
-template <typename T>
-cudaError_t beam_launch(BeamArgs& a, cudaStream_t st) {
+int max_parts(int V) { return (V + 511) / 512 + 1; }   // of fp32 rows, which have the most groups; a run is one group at least
+template <typename T, bool VEC>
+cudaError_t beam_launch(BeamArgs& a, int num_sm, cudaStream_t st) {
   constexpr int SEG = 32 * Logit<T>::E;
   a.n_seg = (a.V + SEG - 1) / SEG;
-  const int rows = a.B * a.W;
-  a.part_segs = SCAN_PART;
-  a.n_parts = (a.n_seg + a.part_segs - 1) / a.part_segs;
+  a.groups = (a.n_seg + SCAN_SEGS - 1) / SCAN_SEGS;
+  a.max_parts = max_parts(a.V);
+  const long long all = (long long)a.B * a.W * a.groups, warps = (long long)num_sm * 4 * SCAN_WARPS;
+  // little work, no more than ONE_RUN groups to a warp and clusters that fit beside one another: one launch
+  if ((long long)a.W * a.groups <= ONE_RUN * ONE_WARPS && a.B * ONE_CTAS <= num_sm) {
+    a.run = (a.W * a.groups + ONE_WARPS - 1) / ONE_WARPS;
+    a.max_parts = (a.groups + a.run - 1) / a.run + 1;   // W of them: ONE_WARPS + 2 W at most
+    return launch_k(beam_one_kernel<T, VEC>, dim3(a.B * ONE_CTAS), dim3(ONE_THREADS), 0, st, a);
+  }
+  a.run = (int)((all + warps - 1) / warps);
+  const long long runs = (all + a.run - 1) / a.run;
+  cudaError_t e = launch_k(beam_scan_kernel<T, VEC>, dim3((unsigned)((runs + SCAN_WARPS - 1) / SCAN_WARPS)), dim3(SCAN_THREADS), 0, st, a);
+  if (e != cudaSuccess) return e;
+  // a small CTA for few segments: what each warp does for itself then costs less than the walk over them
+  if ((long long)a.W * a.n_seg <= 256 * PICK_PER) return launch_k(beam_pick_kernel<T, VEC, 256>, dim3(a.B), dim3(256), 0, st, a);
+  return launch_k(beam_pick_kernel<T, VEC, 1024>, dim3(a.B), dim3(1024), 0, st, a);
+}
+template <typename T>
+cudaError_t beam_types(BeamArgs& a, int num_sm, cudaStream_t st) {
   const bool vec = (((uintptr_t)a.logits | (uintptr_t)(a.row_stride * (int64_t)sizeof(T))) & 15) == 0;
-  const dim3 grid((unsigned)((long long)rows * a.n_parts));
-  cudaError_t e = vec ? launch_k(beam_scan_kernel<T, true>, grid, dim3(SCAN_THREADS), 0, st, a) : launch_k(beam_scan_kernel<T, false>, grid, dim3(SCAN_THREADS), 0, st, a);
-  if (e == cudaSuccess) e = launch_k(beam_pick_kernel<T>, dim3(a.B), dim3(PICK_THREADS), 0, st, a);
-  return e;
+  return vec ? beam_launch<T, true>(a, num_sm, st) : beam_launch<T, false>(a, num_sm, st);
 }
 
 }  // namespace
@@ -299,8 +573,8 @@ extern "C" {
 
 int64_t sps_beam_select_workspace_bytes(int32_t B, int32_t W, int32_t V) {
   if (const char* why = bad_shape(B, W, V)) { no(SPS_EINVAL, why); return -1; }
-  const int64_t segs = ((int64_t)V + 127) / 128, parts = (segs + SCAN_PART - 1) / SCAN_PART;
-  return 256 + up((int64_t)B * W * segs * 4) + up((int64_t)B * W * parts * 8);
+  const int64_t rows = (int64_t)B * W;
+  return up(rows * (((int64_t)V + 127) / 128) * 4) + up(rows * max_parts(V) * 8);
 }
 
 int sps_beam_select(const void* logits, int32_t dtype, int64_t row_stride, int32_t B, int32_t W, int32_t V, double temperature,
@@ -323,12 +597,11 @@ int sps_beam_select(const void* logits, int32_t dtype, int64_t row_stride, int32
   if (!workspace || ((uintptr_t)workspace & 15)) return no(SPS_EINVAL, "workspace null or not 16-byte aligned");
   BeamArgs a{};
   a.logits = logits; a.row_stride = row_stride; a.B = B; a.W = W; a.V = V; a.N = N;
-  a.inv_t = 1.0 / temperature; a.c = c; a.scores = scores; a.done = done; a.end_token = end_token;
+  a.t = temperature; a.inv_t = 1.0 / temperature; a.inv_t32 = (float)a.inv_t; a.c = c; a.scores = scores; a.done = done; a.end_token = end_token;
   a.out_scores = out_scores; a.out_parents = out_parents; a.out_tokens = out_tokens; a.out_done = out_done;
-  const int64_t segs = ((int64_t)V + 127) / 128;
-  a.seg_max = (float*)((char*)workspace + 256);
-  a.parts = (float2*)((char*)workspace + 256 + up((int64_t)B * W * segs * 4));
-  const cudaError_t e = dtype == 0 ? beam_launch<float>(a, (cudaStream_t)stream) : beam_launch<__nv_bfloat16>(a, (cudaStream_t)stream);
+  a.seg_max = (float*)workspace;
+  a.parts = (float2*)((char*)workspace + up((int64_t)B * W * (((int64_t)V + 127) / 128) * 4));
+  const cudaError_t e = dtype == 0 ? beam_types<float>(a, paged_sms(), (cudaStream_t)stream) : beam_types<__nv_bfloat16>(a, paged_sms(), (cudaStream_t)stream);
   return e == cudaSuccess ? SPS_OK : no(SPS_ECUDA, cudaGetErrorString(e));
 }
 

@@ -168,6 +168,14 @@ def test_one_workspace_serves_calls_of_any_shape_and_results_repeat():
             assert all(torch.equal(a, b) for a, b in zip(o, first[(B, W, V)]))
 
 
+def test_one_workspace_serves_few_and_many_sequences_in_turn():
+    """Arrivals are counted at the same place whatever the shape: what a call of few sequences leaves is no count of one of many."""
+    ws = torch.zeros(sps.sps_beam_select_workspace_bytes(600, 2, 500), dtype=torch.uint8, device=DEV)
+    for B, W, V in ((1, 8, 5000), (600, 2, 500), (2, 2, 9000), (600, 2, 500)):
+        x, s = normal((B, W, V), seed=B + V), beams(B, W)
+        check_select(run_select(x, s, N=3, ws=ws), x, s, N=3)
+
+
 def test_captured_and_replayed_on_another_stream():
     B, W, V = 3, 4, 32000
     x, s = normal((B, W, V), seed=12), beams(B, W)

@@ -122,8 +122,8 @@ def test_layers():
     refused(copy([c], n=-1), "layers")
 
 
-@pytest.mark.parametrize("kw,word", [(dict(B=-1), "B"), (dict(B=65537), "B"), (dict(W=0), "W"), (dict(W=129), "W"), (dict(V=0), "V"), (dict(V=(1 << 24) + 1), "V"),
-                                     (dict(W=128, V=1 << 24), "2^31"), (dict(B=65536, W=128, V=1 << 23), "W x V"), (dict(dtype=2), "dtype"), (dict(N=0), "N"),
+@pytest.mark.parametrize("kw,word", [(dict(B=-1), "B"), (dict(B=8193), "B"), (dict(W=0), "W"), (dict(W=129), "W"), (dict(V=0), "V"), (dict(V=(1 << 24) + 1), "V"),
+                                     (dict(W=128, V=1 << 24), "2^31"), (dict(B=8192, W=128, V=(1 << 24) - 1), "W x V"), (dict(dtype=2), "dtype"), (dict(N=0), "N"),
                                      (dict(N=129), "N"), (dict(row=-1), "stride"), (dict(T=0.0), "temperature"), (dict(T=-1.0), "temperature"),
                                      (dict(T=math.nan), "temperature"), (dict(T=math.inf), "temperature"), (dict(T=1e-39), "temperature"), (dict(T=1e39), "temperature"),
                                      (dict(end=-2), "end_token"), (dict(end=100), "end_token"), (dict(done=P), "end_token"), (dict(logits=None), "null"),
