@@ -500,7 +500,7 @@ int64_t sps_paged_attention_workspace_bytes(const sps_paged_cache* cache, int32_
 typedef struct {
   int32_t* refs;     /* device [n_pages]: table rows that hold the page, 0 = free           */
   int32_t* status;   /* device [1], SPS_PAGED_* bits, never cleared by the calls; may be NULL */
-  int32_t n_pages, page_size;   /* page_size: tokens, a power of two, 8 .. 512               */
+  int32_t n_pages, page_size;   /* n_pages: up to 2^20; page_size: tokens, a power of two, 8 .. 512 */
 } sps_page_pool;
 
 /* Row r holds the pages in entries 0 .. held[r] - 1 of pages[r * ld ...], for len[r] tokens (len[r] <= held[r] * page_size).

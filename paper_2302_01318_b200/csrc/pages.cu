@@ -8,7 +8,8 @@
 
 namespace cg = cooperative_groups;
 
-#define PAGES_MAX_ROWS 8192   // rows of a table: their prefix sums fit a CTA's shared memory
+#define PAGES_MAX (1 << 20)    // pages of a pool: their bits fit the shared memory of eight CTAs
+#define PAGES_MAX_ROWS 8192   // rows of a table: a thread each of a cluster of eight CTAs
 
 namespace {
 
@@ -87,58 +88,121 @@ __global__ void __launch_bounds__(FORK_THREADS) fork_kernel(const __grid_constan
 }
 
 // ------------------------------------------------------------------------------------------------------------------
-// Block-wide helpers of the pool kernels (1024 threads)
+// Helpers of the pool kernels: one cluster, 1024 threads to a CTA
 // ------------------------------------------------------------------------------------------------------------------
 constexpr int POOL_THREADS = 1024, POOL_WARPS = POOL_THREADS / 32;
+constexpr int POOL_WORDS = 4096;   // of 32 pages each, that a CTA may have: pools of 2^20 pages in a cluster of eight
 
-// inclusive sum over the block's threads, in thread order; s_warp: [POOL_WARPS]; total: the block's
-__device__ __forceinline__ int block_scan(int v, int* s_warp, int* total) {
+// inclusive sums over the block's threads, in thread order; s_warp: [POOL_WARPS]; total: the block's
+__device__ __forceinline__ int2 block_scan(int2 v, int2* s_warp, int2* total) {
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  auto scan = [&](int2 x) {
 #pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int u = __shfl_up_sync(0xffffffffu, v, o);
-    if (lane >= o) v += u;
-  }
+    for (int o = 1; o < 32; o <<= 1) {
+      const int u0 = __shfl_up_sync(0xffffffffu, x.x, o), u1 = __shfl_up_sync(0xffffffffu, x.y, o);
+      if (lane >= o) { x.x += u0; x.y += u1; }
+    }
+    return x;
+  };
+  v = scan(v);
   __syncthreads();   // (s_warp may still be read from the last call)
   if (lane == 31) s_warp[warp] = v;
   __syncthreads();
-  int w = s_warp[lane];
-#pragma unroll
-  for (int o = 1; o < 32; o <<= 1) {
-    const int u = __shfl_up_sync(0xffffffffu, w, o);
-    if (lane >= o) w += u;
-  }
-  *total = __shfl_sync(0xffffffffu, w, 31);
-  const int before = __shfl_sync(0xffffffffu, w, (warp + 31) & 31);
-  return v + (warp > 0 ? before : 0);
+  const int2 w = scan(s_warp[lane]);
+  total->x = __shfl_sync(0xffffffffu, w.x, 31);
+  total->y = __shfl_sync(0xffffffffu, w.y, 31);
+  const int b0 = __shfl_sync(0xffffffffu, w.x, (warp + 31) & 31), b1 = __shfl_sync(0xffffffffu, w.y, (warp + 31) & 31);
+  return warp > 0 ? make_int2(v.x + b0, v.y + b1) : v;
+}
+__device__ __forceinline__ void block_add(int v, int* s_sum) {   // *s_sum is complete after the next barrier
+  v = __reduce_add_sync(0xffffffffu, v);
+  if ((threadIdx.x & 31) == 0 && v) atomicAdd(s_sum, v);
 }
 
-// this CTA's pages of the pool, in whole tiles of 4 pages a thread
-__device__ __forceinline__ void pool_part(int n_pages, unsigned rank, unsigned parts, int* lo, int* hi) {
-  const long long tiles = ((long long)n_pages + POOL_THREADS * 4 - 1) / (POOL_THREADS * 4), per = (tiles + parts - 1) / parts;
-  const long long a = per * rank * (POOL_THREADS * 4), b = a + per * (POOL_THREADS * 4);
-  *lo = (int)(a < n_pages ? a : n_pages);
-  *hi = (int)(b < n_pages ? b : n_pages);
+// The pool's references as bits in shared memory, a page's set where it is in use; a CTA has the pages lo .. hi - 1, whole words
+// of them.  A warp reads 32 neighbouring references and votes; words go round the warps.
+struct PoolPart { int lo, hi, words; };
+__device__ __forceinline__ PoolPart pool_part(int n_pages, int rank, int parts) {
+  const int per = ((n_pages + 31) / 32 + parts - 1) / parts * 32;
+  PoolPart p;
+  p.lo = min(per * rank, n_pages);
+  p.hi = min(p.lo + per, n_pages);
+  p.words = (p.hi - p.lo + 31) / 32;
+  return p;
 }
-// references of pages p .. p + 3, `outside` behind hi (read from L2: other CTAs changed them)
-__device__ __forceinline__ int4 refs4(const int32_t* refs, int p, int hi, int outside) {
-  int4 r = make_int4(outside, outside, outside, outside);
-  if (p < hi) r.x = __ldcg(refs + p);
-  if (p + 1 < hi) r.y = __ldcg(refs + p + 1);
-  if (p + 2 < hi) r.z = __ldcg(refs + p + 2);
-  if (p + 3 < hi) r.w = __ldcg(refs + p + 3);
-  return r;
+// references are read from L2 (other CTAs changed them), and copied to `copy` if that is given
+__device__ __forceinline__ void used_bits(const int32_t* refs, const PoolPart& p, uint32_t* s_bits, int32_t* copy = nullptr) {
+  const int lane = threadIdx.x & 31;
+  for (int w0 = threadIdx.x >> 5; w0 < p.words; w0 += 8 * POOL_WARPS) {
+    int r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int page = p.lo + (w0 + i * POOL_WARPS) * 32 + lane;
+      r[i] = page < p.hi ? __ldcg(refs + page) : 0;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int w = w0 + i * POOL_WARPS, page = p.lo + w * 32 + lane;
+      if (w >= p.words) break;
+      const uint32_t v = __ballot_sync(0xffffffffu, r[i] != 0);
+      if (lane == 0) s_bits[w] = v;
+      if (copy && page < p.hi) copy[page] = r[i];
+    }
+  }
+}
+__device__ __forceinline__ uint32_t existing_bits(int page, int hi) {   // of the 32 pages from `page` on, those below hi
+  return page + 32 <= hi ? 0xffffffffu : (page < hi ? (1u << (hi - page)) - 1u : 0u);
+}
+// fn(word, its bits, page, lane) for every page of this CTA's words w0 .. w0 + 1023, a warp to a word
+template <class Fn>
+__device__ __forceinline__ void for_pages(const PoolPart& p, const uint32_t* s_bits, int w0, Fn fn) {
+  const int lane = threadIdx.x & 31;
+  for (int w = w0 + (threadIdx.x >> 5); w < min(w0 + POOL_THREADS, p.words); w += POOL_WARPS) fn(w, s_bits[w], p.lo + w * 32 + lane, lane);
+}
+
+// use(row, i, load(row, i)) for i < count of every row of the CTA (a row per thread), by threads of a warp for neighbouring i: rows of
+// one or two by their own thread, the others in runs of 256 that go round the warps
+template <class Load, class Use>
+__device__ __forceinline__ void for_entries(int count, int* s_end, int* s_count, int2* s_warp, Load load, Use use) {
+  const int tid = threadIdx.x;
+  const bool few = count <= 2;
+  if (few && count > 0) {
+    const int v0 = load(tid, 0), v1 = count > 1 ? load(tid, 1) : 0;
+    use(tid, 0, v0);
+    if (count > 1) use(tid, 1, v1);
+  }
+  const int runs = few ? 0 : (count + 255) / 256;
+  if (!__syncthreads_or(runs)) return;
+  int2 all;
+  s_end[tid] = block_scan(make_int2(runs, 0), s_warp, &all).x;
+  s_count[tid] = count;
+  __syncthreads();
+  for (int u = tid >> 5; u < all.x; u += POOL_WARPS) {
+    int x = 0, y = POOL_THREADS - 1;   // the row of the u-th run: the first whose runs end behind it
+    while (x < y) {
+      const int m = (x + y) >> 1;
+      if (s_end[m] > u) y = m; else x = m + 1;
+    }
+    const int i0 = (u - (x ? s_end[x - 1] : 0)) * 256 + (tid & 31), n = s_count[x];
+    int v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = i0 + 32 * j < n ? load(x, i0 + 32 * j) : 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (i0 + 32 * j < n) use(x, i0 + 32 * j, v[j]);
+  }
 }
 
 // ------------------------------------------------------------------------------------------------------------------
 // Reserve.  With n = min(len, want) tokens kept in k = ceil(n / page) pages, a row (1) gives up its entries behind k, (2)
 // exchanges entry k - 1 for a fresh page if it is partly filled, about to be written and held by others too -- unless all who
 // hold it write to it and this row is the first of them --, and (3) takes fresh pages up to want tokens.  Fresh pages are the
-// lowest free ones, handed out row after row: a prefix sum over the rows' needs and one over the pool's free pages meet.
+// lowest free ones, handed out row after row: a prefix sum over the rows' needs and one over the pool's free pages meet in
+// a list of the pages handed out.
 //
-// One cluster does it all (its CTAs share the pool's scan and the rows; needs are summed by every CTA for itself), the
-// steps divided by cluster barriers: giving up -> marks at shared last pages -> needs and counts -> pages handed out.  What
-// it costs is those steps' trips to L2, one behind the other; the references are read once or twice (4 bytes a page).
+// One cluster does it all, a thread to a row (its state stays in registers), a part of the pool to a CTA, the steps divided by
+// cluster barriers: giving up -> marks at shared last pages, free pages -> needs -> list -> entries.  What it costs is those
+// steps' trips to L2, one behind the other; the references are read once (4 bytes a page).
 // Marks: per page the number of rows about to write to it and B - (the first of them), in the workspace, zero between calls.
 // ------------------------------------------------------------------------------------------------------------------
 struct ReserveArgs {
@@ -147,165 +211,135 @@ struct ReserveArgs {
   const int32_t* want;
   Moves moves;
   int32_t *writers, *first;   // [n_pages], zero
+  int32_t* fresh;             // [n_pages]: the pages handed out
 };
 
-struct RowPlan { int n, k, held, to; };   // tokens and pages kept, entries held, pages wanted
-__device__ __forceinline__ RowPlan row_plan(const ReserveArgs& a, int b) {
-  RowPlan r;
-  const int cap = (int)min((long long)a.t.ld << a.pool.page_shift, (long long)INT_MAX - a.pool.page_size);
-  const int held = a.t.held[b], len = a.t.len[b], want = a.want[b];
-  r.held = min(max(held, 0), a.t.ld);
-  const int room = (int)min((long long)r.held << a.pool.page_shift, (long long)cap);
-  if (held != r.held || len > room || want > cap) paged_flag(a.pool.status, SPS_PAGED_BAD_LENGTH);
-  const int w = min(max(want, 0), cap);
-  r.n = min(min(max(len, 0), room), w);
-  r.k = (r.n + a.pool.page_size - 1) >> a.pool.page_shift;
-  r.to = (w + a.pool.page_size - 1) >> a.pool.page_shift;
-  return r;
-}
-// the page of a row's last kept entry if the row is about to write into it, else -1
-__device__ __forceinline__ int written_page(const ReserveArgs& a, int b, const RowPlan& r) {
-  if (!(r.n & (a.pool.page_size - 1)) || a.want[b] <= r.n) return -1;
-  const int q = a.t.pages[(long long)b * a.t.ld + r.k - 1];
-  if (q < 0 || q >= a.pool.n_pages) { paged_flag(a.pool.status, SPS_PAGED_BAD_PAGE); return -1; }
-  return q;
-}
-
 __global__ void __launch_bounds__(POOL_THREADS) reserve_kernel(const __grid_constant__ ReserveArgs a) {
-  extern __shared__ int s_rows[];
-  __shared__ int s_warp[POOL_WARPS], s_free;
-  int *s_end = s_rows, *s_keep = s_rows + a.t.B, *s_moves = s_keep + a.t.B, *s_page = s_moves + a.t.B;   // each [B]
-  cg::cluster_group cl = cg::this_cluster();
-  const unsigned rank = cl.block_rank(), parts = cl.num_blocks();
-  const int tid = threadIdx.x, B = a.t.B;
+  __shared__ int s_end[POOL_THREADS], s_count[POOL_THREADS], s_from[POOL_THREADS], s_at[POOL_THREADS];
+  __shared__ int2 s_warp[POOL_WARPS];
+  __shared__ uint32_t s_bits[POOL_WORDS];
+  __shared__ int s_free, s_met, s_sums[3][8];   // this CTA's free pages; what is met where not all is; every CTA's free pages, needs and moves
+  cg::cluster_group cl = cg::this_cluster();   // (at the first barrier every CTA is there to be written to)
+  const int rank = (int)cl.block_rank(), parts = (int)cl.num_blocks(), tid = threadIdx.x, B = a.t.B;
+  const int per = (B + parts - 1) / parts, b = rank * per + tid;
+  const bool row = tid < per && b < B;
+  int32_t* const entries = a.t.pages + (long long)(row ? b : 0) * a.t.ld;
+  const PoolPart part = pool_part(a.pool.n_pages, rank, parts);
   pdl_launch_dependents();
   pdl_wait();
 
-  // (1) entries behind the kept ones, a row per warp
-  for (int b = rank * POOL_WARPS + (tid >> 5); b < B; b += parts * POOL_WARPS) {
-    const RowPlan r = row_plan(a, b);
-    const int32_t* row = a.t.pages + (long long)b * a.t.ld;
-    for (int i0 = r.k + (tid & 31); i0 < r.held; i0 += 32 * 8) {
-      int p[8];
-#pragma unroll
-      for (int j = 0; j < 8; ++j) p[j] = i0 + 32 * j < r.held ? row[i0 + 32 * j] : INT_MIN;
-#pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        if (i0 + 32 * j >= r.held) continue;
-        if (p[j] < 0 || p[j] >= a.pool.n_pages) paged_flag(a.pool.status, SPS_PAGED_BAD_PAGE);
-        else atomicAdd(a.pool.refs + p[j], -1);
-      }
+  // (1) the row's plan, and what it gives up
+  int n = 0, keep = 0, to = 0, q = -1, give = 0;   // tokens and pages kept, pages wanted, the page about to be written
+  if (row) {
+    const int held0 = a.t.held[b], len0 = a.t.len[b], want0 = a.want[b];
+    const int cap = (int)min((long long)a.t.ld << a.pool.page_shift, (long long)INT_MAX - a.pool.page_size);
+    const int held = min(max(held0, 0), a.t.ld), room = (int)min((long long)held << a.pool.page_shift, (long long)cap), want = min(max(want0, 0), cap);
+    if (held != held0 || len0 > room || want0 > cap) paged_flag(a.pool.status, SPS_PAGED_BAD_LENGTH);
+    n = min(min(max(len0, 0), room), want);
+    keep = (n + a.pool.page_size - 1) >> a.pool.page_shift;
+    to = (want + a.pool.page_size - 1) >> a.pool.page_shift;
+    give = held - keep;
+    if ((n & (a.pool.page_size - 1)) && want > n) {
+      q = entries[keep - 1];
+      if (q < 0 || q >= a.pool.n_pages) { paged_flag(a.pool.status, SPS_PAGED_BAD_PAGE); q = -1; }
     }
+  }
+  s_from[tid] = keep;
+  if (tid == 0) s_free = 0;
+  for_entries(give, s_end, s_count, s_warp, [&](int r, int i) { return a.t.pages[(long long)(rank * per + r) * a.t.ld + s_from[r] + i]; }, [&](int, int, int p) {
+    if (p < 0 || p >= a.pool.n_pages) paged_flag(a.pool.status, SPS_PAGED_BAD_PAGE);
+    else atomicAdd(a.pool.refs + p, -1);
+  });
+  cl.sync();
+  // (2) marks at pages that are shared and about to be written; the free pages
+  const int shared = q >= 0 ? __ldcg(a.pool.refs + q) : 0;
+  if (shared > 1) {
+    atomicAdd(a.writers + q, 1);
+    atomicMax(a.first + q, B - b);
+  }
+  used_bits(a.pool.refs, part, s_bits);
+  __syncthreads();
+  int free_pages = 0;
+  for (int w = tid; w < part.words; w += POOL_THREADS) {
+    const uint32_t v = ~s_bits[w] & existing_bits(part.lo + w * 32, part.hi);
+    s_bits[w] = v;   // (the free ones from here on)
+    free_pages += __popc(v);
+  }
+  block_add(free_pages, &s_free);
+  cl.sync();
+  // (3) needs, summed in the rows' order, and every CTA told the others' sums
+  const bool swap = shared > 1 && !(__ldcg(a.writers + q) == shared && __ldcg(a.first + q) == B - b);
+  const int need = row ? max(to - keep, 0) + swap : 0;
+  int2 sum;
+  const int2 ends = block_scan(make_int2(need, swap), s_warp, &sum);
+  if (tid < parts) {
+    int* const s = cl.map_shared_rank(&s_sums[0][0], tid);
+    s[rank] = s_free; s[8 + rank] = sum.x; s[16 + rank] = sum.y;
   }
   cl.sync();
-  // (2) marks at the pages that are shared and about to be written
-  for (int b = rank * POOL_THREADS + tid; b < B; b += parts * POOL_THREADS) {
-    const int q = written_page(a, b, row_plan(a, b));
-    if (q >= 0 && __ldcg(a.pool.refs + q) > 1) {
-      atomicAdd(a.writers + q, 1);
-      atomicMax(a.first + q, B - b);
-    }
-  }
-  cl.sync();
-  // (3) needs and their sums, in every CTA
-  const int per = (B + POOL_THREADS - 1) / POOL_THREADS, b0 = min(tid * per, B), b1 = min(b0 + per, B);
-  int need = 0, fresh = 0;
-  for (int b = b0; b < b1; ++b) {
-    const RowPlan r = row_plan(a, b);
-    const int q = written_page(a, b, r);
-    int swap = 0;
-    if (q >= 0) {
-      const int refs = __ldcg(a.pool.refs + q);
-      swap = refs > 1 && !(__ldcg(a.writers + q) == refs && __ldcg(a.first + q) == B - b);
-    }
-    need += max(r.to - r.k, 0) + swap;
-    fresh += swap;
-    s_end[b] = need;
-    s_moves[b] = fresh;
-    s_keep[b] = r.k;
-    s_page[b] = q;
-  }
-  int total_need, total_moves;
-  const int need0 = block_scan(need, s_warp, &total_need) - need, fresh0 = block_scan(fresh, s_warp, &total_moves) - fresh;
-  for (int b = b0; b < b1; ++b) { s_end[b] += need0; s_moves[b] += fresh0; }
-  int lo, hi, mine = 0;
-  pool_part(a.pool.n_pages, rank, parts, &lo, &hi);
-  for (int p = lo + tid * 4; p < hi; p += POOL_THREADS * 4) {
-    const int4 r = refs4(a.pool.refs, p, hi, 1);
-    mine += (r.x == 0) + (r.y == 0) + (r.z == 0) + (r.w == 0);
-  }
-  int free_here;
-  block_scan(mine, s_warp, &free_here);
-  if (tid == 0) s_free = free_here;
-  cl.sync();
-  int before = 0, free_all = 0;
-  for (unsigned c = 0; c < parts; ++c) {
-    const int n = *cl.map_shared_rank(&s_free, c);
-    if (c < rank) before += n;
-    free_all += n;
-  }
-  // (4) rows' new state and the pages given up for fresh ones (CTA 0), then the fresh pages
-  if (rank == 0) {
-    for (int b = tid; b < B; b += POOL_THREADS) {
-      const RowPlan r = row_plan(a, b);
-      const int start = b ? s_end[b - 1] : 0, swap = s_moves[b] - (b ? s_moves[b - 1] : 0), q = s_page[b];
-      const bool wants = s_end[b] > start, served = wants && s_end[b] <= free_all;
-      if (wants && !served) paged_flag(a.pool.status, SPS_PAGED_NO_PAGE);
-      if (q >= 0) { a.writers[q] = 0; a.first[q] = 0; }
-      if (served && swap) {
-        atomicAdd(a.pool.refs + q, -1);
-        int32_t* m = a.moves.list + 3ll * (s_moves[b] - 1);
-        m[0] = q;
-        m[2] = r.n & (a.pool.page_size - 1);
-      }
-      a.t.held[b] = served ? max(r.to, r.k) : r.k;
-      a.t.len[b] = r.n;
-    }
-    // moves of the rows that were served: those end with the last row whose need fits
-    if (tid == 0) {
-      int lo_b = 0, hi_b = B;   // the first row whose needs do not fit
-      while (lo_b < hi_b) {
-        const int m = (lo_b + hi_b) >> 1;
-        if (s_end[m] > free_all) hi_b = m; else lo_b = m + 1;
-      }
-      a.moves.count[0] = lo_b ? s_moves[lo_b - 1] : 0;
-    }
-  }
-  int at = before;
-  for (int p0 = lo; p0 < hi && at < total_need; p0 += POOL_THREADS * 4) {
-    const int p = p0 + tid * 4;
-    const int4 r = refs4(a.pool.refs, p, hi, 1);
-    const int free4[4] = {r.x == 0, r.y == 0, r.z == 0, r.w == 0};
-    const int n = free4[0] + free4[1] + free4[2] + free4[3];
-    int tile;
-    int j = at + block_scan(n, s_warp, &tile) - n;
+  int end = ends.x, moves_end = ends.y, free_before = 0, free_all = 0, need_all = 0, moves_all = 0;
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      if (!free4[i]) continue;
-      if (j < total_need) {
-        int x = 0, y = B - 1;   // the row that the j-th free page goes to: the first whose needs end behind j
-        while (x < y) {
-          const int m = (x + y) >> 1;
-          if (s_end[m] > j) y = m; else x = m + 1;
-        }
-        if (s_end[x] <= free_all) {
-          const int swap = s_moves[x] - (x ? s_moves[x - 1] : 0), e = s_keep[x] - swap + j - (x ? s_end[x - 1] : 0);
-          a.t.pages[(long long)x * a.t.ld + e] = p + i;
-          a.pool.refs[p + i] = 1;
-          if (swap && e == s_keep[x] - 1) a.moves.list[3ll * (s_moves[x] - 1) + 1] = p + i;
-        }
-      }
-      ++j;
-    }
-    at += tile;
+  for (int c = 0; c < 8; ++c) {
+    if (c >= parts) break;
+    const int f = s_sums[0][c], n0 = s_sums[1][c], m = s_sums[2][c];
+    if (c < rank) { free_before += f; end += n0; moves_end += m; }
+    free_all += f; need_all += n0; moves_all += m;
   }
-  cl.sync();   // (a CTA's counts are read by the others until here)
+  if (need_all > free_all) {   // the rows behind the first that goes without do so too: what the ones before it need, and their moves
+    if (row && need > 0 && end > free_all) paged_flag(a.pool.status, SPS_PAGED_NO_PAGE);
+    s_met = 0;
+    __syncthreads();
+    if (row && end <= free_all) atomicMax(&s_met, end);
+    cl.sync();
+    need_all = 0;
+    for (int c = 0; c < parts; ++c) need_all = max(need_all, *cl.map_shared_rank(&s_met, c));
+    cl.sync();
+    if (tid == 0) s_met = 0;
+    __syncthreads();
+    if (row && end <= free_all) atomicMax(&s_met, moves_end);
+    cl.sync();
+    moves_all = 0;
+    for (int c = 0; c < parts; ++c) moves_all = max(moves_all, *cl.map_shared_rank(&s_met, c));
+  }
+  // (4) the rows' new state, the pages that they exchange, and the list of fresh pages
+  const bool served = need > 0 && end <= need_all;
+  if (row) {
+    a.t.held[b] = served ? max(to, keep) : keep;
+    a.t.len[b] = n;
+    if (served && swap) {
+      atomicAdd(a.pool.refs + q, -1);
+      int32_t* m = a.moves.list + 3ll * (moves_end - 1);
+      m[0] = q;
+      m[2] = n & (a.pool.page_size - 1);
+    }
+    if (shared > 1) { a.writers[q] = 0; a.first[q] = 0; }
+  }
+  if (b == 0 && tid == 0) a.moves.count[0] = moves_all;
+  for (int w0 = 0, at = free_before; w0 < part.words && at < need_all; w0 += POOL_THREADS) {
+    const int count = w0 + tid < part.words ? __popc(s_bits[w0 + tid]) : 0;
+    s_count[tid] = at - count + block_scan(make_int2(count, 0), s_warp, &sum).x;   // (for_entries is done with it)
+    __syncthreads();
+    at += sum.x;
+    for_pages(part, s_bits, w0, [&](int w, uint32_t v, int page, int lane) {
+      const int j = s_count[w - w0] + __popc(v & ((1u << lane) - 1u));
+      if ((v >> lane & 1) && j < need_all) { a.fresh[j] = page; a.pool.refs[page] = 1; }
+    });
+    __syncthreads();
+  }
+  cl.sync();
+  // (5) the rows' entries from the list
+  const int take = served ? need : 0;
+  s_from[tid] = end - need;
+  s_at[tid] = keep - swap;
+  for_entries(take, s_end, s_count, s_warp, [&](int r, int i) { return __ldcg(a.fresh + s_from[r] + i); },
+              [&](int r, int i, int p) { a.t.pages[(long long)(rank * per + r) * a.t.ld + s_at[r] + i] = p; });
+  if (served && swap) a.moves.list[3ll * (moves_end - 1) + 1] = __ldcg(a.fresh + end - need);
 }
 
 // ------------------------------------------------------------------------------------------------------------------
 // Compact: of U pages in use, those numbered U and above go to the free ones below U, the i-th to the i-th.
-// First a cluster over the pool: U, the number of holes, then each page's place among the holes or among those that move
-// (references read twice); then a grid over the table's entries and the list.  map[p]: where page p >= U stands in the list, -1 if
+// First a cluster over the pool, its references read once: U, the holes below it, then each page's place among the holes or
+// among those that move; then a grid over the table's entries and the list.  map[p]: where page p >= U stands in the list, -1 if
 // it stays (nothing in use, or the list is full).
 // ------------------------------------------------------------------------------------------------------------------
 struct CompactArgs {
@@ -317,73 +351,66 @@ struct CompactArgs {
 };
 
 __global__ void __launch_bounds__(POOL_THREADS) compact_scan_kernel(const __grid_constant__ CompactArgs a) {
-  __shared__ int s_warp[POOL_WARPS], s_n[2];
+  __shared__ int2 s_warp[POOL_WARPS];
+  __shared__ uint32_t s_bits[POOL_WORDS];
+  __shared__ int s_rank[POOL_THREADS], s_n[2], s_sums[2][8];
   cg::cluster_group cl = cg::this_cluster();
-  const unsigned rank = cl.block_rank(), parts = cl.num_blocks();
-  const int tid = threadIdx.x;
+  const int rank = (int)cl.block_rank(), parts = (int)cl.num_blocks(), tid = threadIdx.x;
+  const PoolPart part = pool_part(a.pool.n_pages, rank, parts);
+  if (tid < 2) s_n[tid] = 0;
   pdl_launch_dependents();
   pdl_wait();
-  int lo, hi, mine = 0, n_used;
-  pool_part(a.pool.n_pages, rank, parts, &lo, &hi);
-  for (int p = lo + tid * 4; p < hi; p += POOL_THREADS * 4) {
-    const int4 r = refs4(a.pool.refs, p, hi, 0);
-    mine += (r.x != 0) + (r.y != 0) + (r.z != 0) + (r.w != 0);
-  }
-  block_scan(mine, s_warp, &n_used);
-  if (tid == 0) s_n[0] = n_used;
-  cl.sync();
-  int used = 0, before = 0;
-  for (unsigned c = 0; c < parts; ++c) {
-    const int n = *cl.map_shared_rank(&s_n[0], c);
-    if (c < rank) before += n;
-    used += n;
-  }
-  // pages in use below U: all of a part's that lies below, part of one's
-  int below = hi <= used ? n_used : 0;
-  if (lo < used && used < hi) {
-    mine = 0;
-    for (int p = lo + tid * 4; p < used; p += POOL_THREADS * 4) {
-      const int4 r = refs4(a.pool.refs, p, used, 0);
-      mine += (r.x != 0) + (r.y != 0) + (r.z != 0) + (r.w != 0);
+  cl.sync();   // (every CTA is there to be written to)
+  auto tell = [&](int i) {   // this CTA's sum to all, everyone's from all
+    __syncthreads();
+    if (tid < parts) cl.map_shared_rank(&s_sums[i][0], tid)[rank] = s_n[i];
+    cl.sync();
+    int2 all = make_int2(0, 0);   // of the CTAs before this one, of all
+    for (int c = 0; c < parts; ++c) {
+      if (c < rank) all.x += s_sums[i][c];
+      all.y += s_sums[i][c];
     }
-    block_scan(mine, s_warp, &below);
-  }
-  if (tid == 0) s_n[1] = below;
-  cl.sync();
-  int stay = 0;   // pages in use below U
-  for (unsigned c = 0; c < parts; ++c) stay += *cl.map_shared_rank(&s_n[1], c);
+    return all;
+  };
+  used_bits(a.pool.refs, part, s_bits, a.refs_out != a.pool.refs ? a.refs_out : nullptr);
+  __syncthreads();
+  int mine = 0;
+  for (int w = tid; w < part.words; w += POOL_THREADS) mine += __popc(s_bits[w]);
+  block_add(mine, &s_n[0]);
+  const int2 in_use = tell(0);
+  const int used = in_use.y;
+  mine = 0;
+  for (int w = tid; w < part.words; w += POOL_THREADS) mine += __popc(s_bits[w] & existing_bits(part.lo + w * 32, used));
+  block_add(mine, &s_n[1]);
+  const int stay = tell(1).y;   // pages in use below U
   if (rank == 0 && tid == 0) {
     a.used[0] = used;
     a.moves.count[0] = min(used - stay, a.moves.capacity);
   }
-  int at = before;
-  for (int p0 = lo; p0 < hi; p0 += POOL_THREADS * 4) {
-    const int p = p0 + tid * 4;
-    const int4 r = refs4(a.pool.refs, p, hi, 0);
-    const int ref[4] = {r.x, r.y, r.z, r.w};
-    const int n = (ref[0] != 0) + (ref[1] != 0) + (ref[2] != 0) + (ref[3] != 0);
-    int tile;
-    int u = at + block_scan(n, s_warp, &tile) - n;   // pages in use before p
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int q = p + i;
-      if (q >= hi) break;
-      if (a.refs_out != a.pool.refs) a.refs_out[q] = ref[i];
-      if (q < used) {
-        if (ref[i] == 0 && q - u < a.moves.capacity) a.moves.list[3ll * (q - u) + 1] = q;
+  for (int w0 = 0, at = in_use.x; w0 < part.words; w0 += POOL_THREADS) {
+    const int count = w0 + tid < part.words ? __popc(s_bits[w0 + tid]) : 0;
+    int2 sum;
+    s_rank[tid] = at - count + block_scan(make_int2(count, 0), s_warp, &sum).x;   // pages in use before the word's
+    __syncthreads();
+    at += sum.x;
+    for_pages(part, s_bits, w0, [&](int w, uint32_t v, int page, int lane) {
+      if (page >= part.hi) return;
+      const bool in = v >> lane & 1;
+      const int before = s_rank[w - w0] + __popc(v & ((1u << lane) - 1u));
+      if (page < used) {
+        if (!in && page - before < a.moves.capacity) a.moves.list[3ll * (page - before) + 1] = page;
       } else {
-        const int m = ref[i] != 0 && u - stay < a.moves.capacity ? u - stay : -1;
-        a.map[q] = m;
-        if (m >= 0) {
-          a.moves.list[3ll * m] = q;
-          a.moves.list[3ll * m + 2] = a.pool.page_size;
+        const int j = before - stay;
+        const bool goes = in && j < a.moves.capacity;
+        a.map[page] = goes ? j : -1;
+        if (goes) {
+          a.moves.list[3ll * j] = page;
+          a.moves.list[3ll * j + 2] = a.pool.page_size;
         }
       }
-      u += ref[i] != 0;
-    }
-    at += tile;
+    });
+    __syncthreads();
   }
-  cl.sync();
 }
 
 __global__ void __launch_bounds__(FORK_THREADS) compact_apply_kernel(const __grid_constant__ CompactArgs a) {
@@ -479,9 +506,9 @@ int no(int code, const char* msg) {
 int done(cudaError_t e) { return e == cudaSuccess ? SPS_OK : no(SPS_ECUDA, cudaGetErrorString(e)); }
 
 template <class Args>
-cudaError_t launch_cluster(void (*kern)(Args), int ctas, size_t smem, cudaStream_t st, const Args& a) {
+cudaError_t launch_cluster(void (*kern)(Args), int ctas, cudaStream_t st, const Args& a) {
   cudaLaunchConfig_t cfg{};
-  cfg.gridDim = dim3(ctas); cfg.blockDim = dim3(POOL_THREADS); cfg.dynamicSmemBytes = smem; cfg.stream = st;
+  cfg.gridDim = dim3(ctas); cfg.blockDim = dim3(POOL_THREADS); cfg.stream = st;
   cudaLaunchAttribute at[2];
   at[0].id = cudaLaunchAttributeClusterDimension;
   at[0].val.clusterDim.x = ctas; at[0].val.clusterDim.y = 1; at[0].val.clusterDim.z = 1;
@@ -491,16 +518,16 @@ cudaError_t launch_cluster(void (*kern)(Args), int ctas, size_t smem, cudaStream
   cfg.numAttrs = sps_pdl_enabled() ? 2 : 1;
   return cudaLaunchKernelEx(&cfg, kern, a);
 }
-// CTAs for a pool: a tile of 4096 pages each, up to a portable cluster
-int pool_ctas(int n_pages) {
+// CTAs for a pool and a table: up to 4096 pages and a row to a thread, until the cluster has eight
+int pool_ctas(int n_pages, int rows) {
   int c = 1;
-  while (c < 8 && (long long)c * POOL_THREADS * 4 < n_pages) c *= 2;
+  while (c < 8 && ((long long)c * 4096 < n_pages || c * POOL_THREADS < rows)) c *= 2;
   return c;
 }
 
 const char* bad_pool(const sps_page_pool* p) {
   if (!p) return "null pool";
-  if (p->n_pages < 1) return "pool: n_pages out of range";
+  if (p->n_pages < 1 || p->n_pages > PAGES_MAX) return "pool: n_pages must be 1 .. 2^20";
   if (p->page_size < 8 || p->page_size > 512 || (p->page_size & (p->page_size - 1))) return "pool: page_size must be a power of two, 8 .. 512";
   if (!p->refs) return "pool: null pointer";
   if (((uintptr_t)p->refs | (uintptr_t)p->status) & 3) return "pool: pointers must be 4-byte aligned";
@@ -537,7 +564,8 @@ dim3 table_grid(int rows, int ld) { return dim3(rows, ld > 0 ? (ld + FORK_THREAD
 extern "C" {
 
 int64_t sps_paged_pool_workspace_bytes(int32_t n_pages) {
-  if (n_pages < 1) { no(SPS_EINVAL, "n_pages must be at least 1"); return -1; }
+  if (n_pages < 1 || n_pages > PAGES_MAX) { no(SPS_EINVAL, "n_pages must be 1 .. 2^20"); return -1; }
+  // the number of pages in use; writers, the first of them, pages handed out (or a compaction's map), a word each
   return 256 + 3 * 4 * (((int64_t)n_pages + 63) / 64 * 64);
 }
 
@@ -570,11 +598,8 @@ int sps_paged_reserve(const sps_page_pool* pool, const sps_page_table* table, co
   const int64_t n = ((int64_t)pool->n_pages + 63) / 64 * 64;
   a.writers = (int32_t*)((char*)workspace + 256);
   a.first = a.writers + n;
-  const size_t smem = sizeof(int) * 4 * (size_t)table->B;
-  static DevSmemCache attr;
-  cudaError_t e = sps_ensure_smem(reserve_kernel, smem, attr);
-  if (e == cudaSuccess) e = launch_cluster(reserve_kernel, pool_ctas(pool->n_pages), smem, (cudaStream_t)stream, a);
-  return done(e);
+  a.fresh = a.writers + 2 * n;
+  return done(launch_cluster(reserve_kernel, pool_ctas(pool->n_pages, table->B), (cudaStream_t)stream, a));
 }
 
 int sps_paged_compact(const sps_page_pool* pool, const sps_page_table* src, const sps_page_table* dst, int32_t* refs_out, const sps_page_moves* moves,
@@ -593,7 +618,7 @@ int sps_paged_compact(const sps_page_pool* pool, const sps_page_table* src, cons
   const int64_t n = ((int64_t)pool->n_pages + 63) / 64 * 64;
   a.used = (int32_t*)workspace;
   a.map = (int32_t*)((char*)workspace + 256) + 2 * n;
-  cudaError_t e = launch_cluster(compact_scan_kernel, pool_ctas(pool->n_pages), 0, (cudaStream_t)stream, a);
+  cudaError_t e = launch_cluster(compact_scan_kernel, pool_ctas(pool->n_pages, 0), (cudaStream_t)stream, a);
   if (e == cudaSuccess) e = launch_k(compact_apply_kernel, table_grid(src->B > 0 ? src->B : 1, src->ld), dim3(FORK_THREADS), 0, (cudaStream_t)stream, a);
   return done(e);
 }

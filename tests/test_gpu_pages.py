@@ -196,6 +196,27 @@ def test_many_rows(B, n_pages):
         d.t.lens.copy_(ints(m.lens))
 
 
+def test_a_pool_of_several_rounds():
+    """More pages than a CTA has threads for words of them (8 x 32768)."""
+    n_pages = 600_001
+    m, d = Model(n_pages, 8, 40), Device(n_pages, 8, 40, 60000)
+    d.load(m)
+    lens = [8 * 14900 + 3 * i for i in range(40)]
+    status = 0
+    for want in (lens, [0 if i % 3 == 0 else n + 1 for i, n in enumerate(lens)], [n + 90000 * (i % 3 == 0) for i, n in enumerate(lens)], [i % 2 * n for i, n in enumerate(lens)]):
+        moves, short = m.reserve(want)
+        status |= sps.PAGED_NO_PAGE if short else 0
+        d.reserve(want)
+        d.check(m, status)
+        m.lens = [min(w, 8 * len(r)) for w, r in zip(want, m.rows)]
+        d.t.lens.copy_(ints(m.lens))
+    assert status == sps.PAGED_NO_PAGE
+    moves = m.compact(10 ** 9)
+    d.compact()
+    assert d.listed() == moves and len(moves) > 100_000
+    d.check(m, status)
+
+
 def test_long_rows():
     """Thousands of pages to a row, taken and given up; the first call asks for one page more than there are."""
     m, d = Model(30000, 8, 3), Device(30000, 8, 3, 20000)

@@ -66,7 +66,7 @@ def refused(rc, word):
     assert rc == sps.SPS_EINVAL and word in msg, (rc, msg)
 
 
-@pytest.mark.parametrize("kw,word", [(dict(refs=None), "null"), (dict(refs=P + 2), "aligned"), (dict(status=P + 1), "aligned"), (dict(n_pages=0), "n_pages"),
+@pytest.mark.parametrize("kw,word", [(dict(refs=None), "null"), (dict(refs=P + 2), "aligned"), (dict(status=P + 1), "aligned"), (dict(n_pages=0), "n_pages"), (dict(n_pages=(1 << 20) + 1), "n_pages"),
                                      (dict(page_size=12), "power of two"), (dict(page_size=4), "power of two"), (dict(page_size=1024), "power of two")])
 def test_pools(kw, word):
     for rc in (fork(pool(**kw)), reserve(pool(**kw)), compact(pool(**kw))):
@@ -108,7 +108,7 @@ def test_combinations():
     assert L.sps_paged_reserve(None, None, None, None, None, None) == sps.SPS_EINVAL
     assert L.sps_paged_compact(None, None, None, None, None, None, None) == sps.SPS_EINVAL
     assert L.sps_paged_copy(None, 1, None, None) == sps.SPS_EINVAL
-    assert L.sps_paged_pool_workspace_bytes(0) == -1
+    assert L.sps_paged_pool_workspace_bytes(0) == -1 and L.sps_paged_pool_workspace_bytes((1 << 20) + 1) == -1
     with pytest.raises(sps.SpsError):
         sps.sps_paged_pool_workspace_bytes(-1)
 
