@@ -130,18 +130,43 @@ __device__ __forceinline__ PoolPart pool_part(int n_pages, int rank, int parts) 
   p.words = (p.hi - p.lo + 31) / 32;
   return p;
 }
-// references are read from L2 (other CTAs changed them), and copied to `copy` if that is given
+// references are read from L2 (other CTAs changed them), four to a lane if they are aligned, and copied to `copy` if that is given
 __device__ __forceinline__ void used_bits(const int32_t* refs, const PoolPart& p, uint32_t* s_bits, int32_t* copy = nullptr) {
-  const int lane = threadIdx.x & 31;
-  for (int w0 = threadIdx.x >> 5; w0 < p.words; w0 += 8 * POOL_WARPS) {
-    int r[8];
+  const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+  int w0 = 0;   // words done
+  if (((uintptr_t)refs & 15) == 0) {
+    const int fours = (p.hi - p.lo) / 128;   // four words to a load
+    for (int f0 = warp; f0 < fours; f0 += 8 * POOL_WARPS) {
+      int4 r[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+      for (int i = 0; i < 8; ++i)
+        if (f0 + i * POOL_WARPS < fours) r[i] = __ldcg(reinterpret_cast<const int4*>(refs + p.lo) + (f0 + i * POOL_WARPS) * 32 + lane);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int f = f0 + i * POOL_WARPS;
+        if (f >= fours) break;
+        uint32_t v = ((r[i].x != 0) | (r[i].y != 0) << 1 | (r[i].z != 0) << 2 | (r[i].w != 0) << 3) << (lane & 7) * 4;
+        v |= __shfl_xor_sync(0xffffffffu, v, 1);
+        v |= __shfl_xor_sync(0xffffffffu, v, 2);
+        v |= __shfl_xor_sync(0xffffffffu, v, 4);
+        if ((lane & 7) == 0) s_bits[f * 4 + (lane >> 3)] = v;
+        if (copy) {
+          int32_t* const c = copy + p.lo + (f * 32 + lane) * 4;
+          c[0] = r[i].x; c[1] = r[i].y; c[2] = r[i].z; c[3] = r[i].w;
+        }
+      }
+    }
+    w0 = fours * 4;
+  }
+  for (w0 += warp; w0 < p.words; w0 += 4 * POOL_WARPS) {
+    int r[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
       const int page = p.lo + (w0 + i * POOL_WARPS) * 32 + lane;
       r[i] = page < p.hi ? __ldcg(refs + page) : 0;
     }
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 4; ++i) {
       const int w = w0 + i * POOL_WARPS, page = p.lo + w * 32 + lane;
       if (w >= p.words) break;
       const uint32_t v = __ballot_sync(0xffffffffu, r[i] != 0);
@@ -156,8 +181,9 @@ __device__ __forceinline__ uint32_t existing_bits(int page, int hi) {   // of th
 // fn(word, its bits, page, lane) for every page of this CTA's words w0 .. w0 + 1023, a warp to a word
 template <class Fn>
 __device__ __forceinline__ void for_pages(const PoolPart& p, const uint32_t* s_bits, int w0, Fn fn) {
-  const int lane = threadIdx.x & 31;
-  for (int w = w0 + (threadIdx.x >> 5); w < min(w0 + POOL_THREADS, p.words); w += POOL_WARPS) fn(w, s_bits[w], p.lo + w * 32 + lane, lane);
+  const int lane = threadIdx.x & 31, end = min(w0 + POOL_THREADS, p.words);
+#pragma unroll 4
+  for (int w = w0 + (threadIdx.x >> 5); w < end; w += POOL_WARPS) fn(w, s_bits[w], p.lo + w * 32 + lane, lane);
 }
 
 // use(row, i, load(row, i)) for i < count of every row of the CTA (a row per thread), by threads of a warp for neighbouring i: rows of
@@ -446,54 +472,71 @@ __global__ void __launch_bounds__(FORK_THREADS) compact_apply_kernel(const __gri
 }
 
 // ------------------------------------------------------------------------------------------------------------------
-// Copy: the first `slots` slots of page `from` to page `to`, of every layer's keys and values.  Bound by HBM.  An item is up
-// to 32 KB of one page of one layer's keys or values (COPY_PER 16-byte pieces per thread, all on their way before the first is
-// stored); items go round a grid that fills the SMs.  Pieces run along whichever of heads and slots lies closer together.
+// Copy: the first `slots` slots of page `from` to page `to`, of every layer's keys and values.  Bound by HBM, which likes long
+// runs of reads and of writes: a thread has PER 16-byte pieces on their way before the first is stored.  805 MB in whole pages of
+// 32 KB take 248 us with PER 16 and 258 with 8; a beam step with 64 rows' partly filled pages in 24 layers takes 31 us with 16 and 26
+// with 4, where CTAs without an item are the cost: the list's capacity, all that the host knows, decides.  A unit is such a run at one
+// place of a page of one layer's keys or values; a CTA keeps to its unit and goes from page to page.  Pieces run along
+// whichever of heads and slots lies closer together.
 // ------------------------------------------------------------------------------------------------------------------
-constexpr int COPY_THREADS = 256, COPY_PER = 8, COPY_LAYERS = 64;   // layers per launch
+constexpr int COPY_THREADS = 256, COPY_LAYERS = 64;   // layers: per launch
+constexpr long long COPY_MUCH = 512ll << 20;          // bytes of a full list that are much
 
 struct CopyArgs {
   Moves moves;
   char* base[2 * COPY_LAYERS];            // keys, values, layer after layer
   long long page, head, slot;             // strides in 16-byte pieces
-  int tensors, n_pages, page_size, heads, row_shift;   // row_shift: log2 of a slot's pieces
-  int slot_first, chunks;                 // heads lie closer than slots; items of a whole page
+  int units, chunks;                      // tensors x chunks; chunks: of a whole page
+  int n_pages, page_size, heads, row_shift;   // row_shift: log2 of a slot's pieces
+  int slot_first;                         // heads lie closer than slots
 };
 
+template <int PER>
 __global__ void __launch_bounds__(COPY_THREADS) copy_kernel(const __grid_constant__ CopyArgs a) {
   pdl_launch_dependents();
+  const int first = blockIdx.x / a.units, unit = blockIdx.x - first * a.units, step = gridDim.x / a.units;
+  const int tensor = unit / a.chunks, chunk = unit - tensor * a.chunks;
+  const int piece = chunk * (COPY_THREADS * PER) + threadIdx.x;
+  uint4* const base = reinterpret_cast<uint4*>(a.base[tensor]) + (piece & ((1 << a.row_shift) - 1));
   pdl_wait();
   const int count = min(max(a.moves.count[0], 0), a.moves.capacity);
-  const long long items = (long long)count * a.tensors * a.chunks;
-  const int pr = 1 << a.row_shift;
-  for (long long it = blockIdx.x; it < items; it += gridDim.x) {
-    const int chunk = (int)(it % a.chunks);
-    const long long r = it / a.chunks;
-    const int tensor = (int)(r % a.tensors);
-    const int32_t* m = a.moves.list + 3 * (r / a.tensors);
+  int had = -1, n = 0;
+  long long off[PER];   // of this thread's pieces in a page, for `had` slots
+  for (int i = first; i < count; i += step) {
+    const int32_t* m = a.moves.list + 3ll * i;
     const int from = m[0], to = m[1], slots = min(max(m[2], 0), a.page_size);
     if (from < 0 || from >= a.n_pages || to < 0 || to >= a.n_pages) continue;
-    const long long n = (long long)slots * a.heads << a.row_shift;
-    uint4* const base = reinterpret_cast<uint4*>(a.base[tensor]);
+    if (slots != had) {
+      had = slots;
+      n = slots * a.heads << a.row_shift;
+      const unsigned inner = a.slot_first ? (unsigned)a.heads : (unsigned)max(slots, 1);
+      const long long so = a.slot_first ? a.slot : a.head, si = a.slot_first ? a.head : a.slot;
+#pragma unroll
+      for (int j = 0; j < PER; ++j) {
+        const unsigned row = (unsigned)(piece + j * COPY_THREADS) >> a.row_shift, o = row / inner;
+        off[j] = o * so + (row - o * inner) * si;
+      }
+    }
     const uint4* const src = base + (long long)from * a.page;
     uint4* const dst = base + (long long)to * a.page;
-    const long long i0 = (long long)chunk * (COPY_THREADS * COPY_PER) + threadIdx.x;
-    uint4 v[COPY_PER];
-    long long off[COPY_PER];
+    uint4 v[PER];
 #pragma unroll
-    for (int j = 0; j < COPY_PER; ++j) {
-      const long long i = i0 + j * COPY_THREADS;
-      off[j] = -1;
-      if (i >= n) continue;
-      const unsigned row = (unsigned)(i >> a.row_shift), inner = a.slot_first ? (unsigned)a.heads : (unsigned)slots;
-      const unsigned o = row / inner, k = row - o * inner;
-      off[j] = (a.slot_first ? o * a.slot + k * a.head : o * a.head + k * a.slot) + (i & (pr - 1));
-      v[j] = src[off[j]];
-    }
+    for (int j = 0; j < PER; ++j)
+      if (piece + j * COPY_THREADS < n) v[j] = src[off[j]];
 #pragma unroll
-    for (int j = 0; j < COPY_PER; ++j)
-      if (off[j] >= 0) dst[off[j]] = v[j];
+    for (int j = 0; j < PER; ++j)
+      if (piece + j * COPY_THREADS < n) dst[off[j]] = v[j];
   }
+}
+
+template <int PER, int CTAS>   // CTAs: per SM
+cudaError_t copy_launch(CopyArgs& a, int tensors, int num_sm, cudaStream_t st) {
+  const int pieces = a.page_size * a.heads << a.row_shift;   // at most 512 x 4096 x 32
+  a.chunks = (pieces + COPY_THREADS * PER - 1) / (COPY_THREADS * PER);
+  a.units = tensors * a.chunks;
+  int at_once = num_sm * CTAS / a.units;   // pages: as many as fill the SMs
+  at_once = at_once < 1 ? 1 : (at_once < a.moves.capacity ? at_once : a.moves.capacity);
+  return launch_k(copy_kernel<PER>, dim3((unsigned)(at_once * a.units)), dim3(COPY_THREADS), 0, st, a);
 }
 
 // ------------------------------------------------------------------------------------------------------------------
@@ -643,14 +686,11 @@ int sps_paged_copy(const sps_paged_cache* layers, int32_t n_layers, const sps_pa
   a.n_pages = f.n_pages; a.page_size = f.page_size; a.heads = f.n_kv_heads;
   while ((per16 << a.row_shift) < f.d_head) ++a.row_shift;
   a.slot_first = f.n_kv_heads > 1 && f.head_stride < f.pos_stride;
-  const long long pieces = (long long)f.page_size * f.n_kv_heads << a.row_shift;
-  a.chunks = (int)((pieces + COPY_THREADS * COPY_PER - 1) / (COPY_THREADS * COPY_PER));
   for (int l = 0; l < n_layers; l += COPY_LAYERS) {
     const int n = n_layers - l < COPY_LAYERS ? n_layers - l : COPY_LAYERS;
     for (int i = 0; i < n; ++i) { a.base[2 * i] = (char*)layers[l + i].k; a.base[2 * i + 1] = (char*)layers[l + i].v; }
-    a.tensors = 2 * n;
-    const long long items = (long long)moves->capacity * a.tensors * a.chunks, most = (long long)paged_sms() * 6;
-    const cudaError_t e = launch_k(copy_kernel, dim3((unsigned)(items < most ? items : most)), dim3(COPY_THREADS), 0, (cudaStream_t)stream, a);
+    const bool much = (long long)moves->capacity * 2 * n * ((long long)a.page_size * a.heads << a.row_shift) * 16 >= COPY_MUCH;
+    const cudaError_t e = much ? copy_launch<16, 3>(a, 2 * n, paged_sms(), (cudaStream_t)stream) : copy_launch<4, 8>(a, 2 * n, paged_sms(), (cudaStream_t)stream);
     if (e != cudaSuccess) return done(e);
   }
   return SPS_OK;
