@@ -317,13 +317,18 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
     held[j] = i < all ? seg_max[i] : -INFINITY;
   }
   // a beam's part of its candidates' scores, -inf where it has none: c = base + (l - max) / T
+  auto parts_of = [&](int w) { return ((first + w) * a.groups + a.groups - 1) / a.run - (first + w) * a.groups / a.run + 1; };
+  float2 ahead = make_float2(-INFINITY, 0.f);   // (so is a warp's first part)
+  if (warp < a.W && lane < parts_of(warp)) ahead = all_parts[(long long)warp * a.max_parts + lane];
+  __syncthreads();   // (`beams` is there)
   for (int w = warp; w < a.W; w += WARPS) {
     const float2* parts = all_parts + (long long)w * a.max_parts;
-    const int at = (first + w) * a.groups, n_parts = (at + a.groups - 1) / a.run - at / a.run + 1;
+    const int n_parts = parts_of(w);
     float m = -INFINITY, s = 0.f;
     for (int p0 = 0; p0 < n_parts; p0 += 32) {   // (one round, but for few rows that are long)
       float2 v = make_float2(-INFINITY, 0.f);
-      if (p0 + lane < n_parts) v = parts[p0 + lane];
+      if (w == warp && p0 == 0) v = ahead;
+      else if (p0 + lane < n_parts) v = parts[p0 + lane];
       warp_merge(v.x, v.y, a.c);
       const float t = fmaxf(m, v.x), r = t == -INFINITY ? 0.f : t;
       s = s * ex2((m - r) * a.c) + v.y * ex2((v.x - r) * a.c);
@@ -507,7 +512,6 @@ __global__ void __launch_bounds__(THREADS) beam_pick_kernel(const __grid_constan
   pdl_launch_dependents();
   pdl_wait();
   beams_load<THREADS>(a, blockIdx.x, s_beams);
-  __syncthreads();
   beam_pick<T, VEC, THREADS>(a, blockIdx.x, row, s_beams, a.seg_max + (long long)row * a.n_seg, a.parts + (long long)row * a.max_parts);
 }
 // Both for little work, a cluster to a sequence: what the scan finds goes straight to the shared memory of the CTA that picks.
@@ -558,7 +562,7 @@ cudaError_t beam_launch(BeamArgs& a, int num_sm, cudaStream_t st) {
   cudaError_t e = launch_k(beam_scan_kernel<T, VEC>, dim3((unsigned)((runs + SCAN_WARPS - 1) / SCAN_WARPS)), dim3(SCAN_THREADS), 0, st, a);
   if (e != cudaSuccess) return e;
   // a small CTA for few segments: what each warp does for itself then costs less than the walk over them
-  if ((long long)a.W * a.n_seg <= 256 * PICK_PER) return launch_k(beam_pick_kernel<T, VEC, 256>, dim3(a.B), dim3(256), 0, st, a);
+  if ((long long)a.W * a.n_seg <= 2048) return launch_k(beam_pick_kernel<T, VEC, 512>, dim3(a.B), dim3(512), 0, st, a);
   return launch_k(beam_pick_kernel<T, VEC, 1024>, dim3(a.B), dim3(1024), 0, st, a);
 }
 template <typename T>

@@ -196,6 +196,44 @@ def test_many_rows(B, n_pages):
         d.t.lens.copy_(ints(m.lens))
 
 
+@pytest.mark.parametrize("n_pages", [31, 33, 2999, 3071, 3500, 4095, 4600, 5121, 24575, 24576, 24577, 32769])
+def test_pools_of_any_size(n_pages):
+    """Both kernels and every request for shared memory: pages at both ends of the pool, taken, shared, exchanged and given up."""
+    page, top = 8, min(60, n_pages // 8)
+    m, d = Model(n_pages, page, 9), Device(n_pages, page, 9, n_pages)
+    d.load(m)
+    status = 0
+    for want in ([8 * top] * 8 + [8 * (n_pages - 8 * top)], [8 * top + 3] * 4 + [0] * 4 + [8 * (n_pages - 8 * top)], [5] * 8 + [0], [7] * 9):
+        moves, short = m.reserve(want)
+        status |= sps.PAGED_NO_PAGE if short else 0
+        d.reserve(want)
+        assert d.listed() == moves
+        d.check(m, status)
+        m.lens = [min(w, page * len(r)) for w, r in zip(want, m.rows)]
+        d.t.lens.copy_(ints(m.lens))
+        parents = [0, 0, 2, 3, 3, 5, 6, 7, 8]
+        m.fork(parents)
+        d.fork(parents)
+        d.check(m, status)
+
+
+@pytest.mark.parametrize("offset", [1, 2, 3])
+def test_references_of_any_alignment(offset):
+    m, d = grown(300, 8, [90, 41, 7, 500], ld=120)
+    store = torch.zeros(300 + offset, dtype=I32, device=DEV)
+    store[offset:] = d.pool.refs
+    d.pool = sps.PagePool(store[offset:], 8)
+    for want in ([91, 60, 0, 900], [3, 3, 3, 3]):
+        m.reserve(want)
+        d.reserve(want)
+        d.check(m)
+    assert d.listed() == []
+    moves = m.compact(10 ** 9)
+    d.compact()
+    assert d.listed() == moves
+    d.check(m)
+
+
 def test_a_pool_of_several_rounds():
     """More pages than a CTA has threads for words of them (8 x 32768)."""
     n_pages = 600_001
