@@ -488,7 +488,7 @@ int64_t sps_paged_attention_workspace_bytes(const sps_paged_cache* cache, int32_
  * sequence; these calls serve programs that decode several continuations of a prompt, admit and drop sequences, and roll
  * rejected drafts back.  One table serves all layers: page p is page p of every layer's cache.
  *
- * All calls only enqueue on `stream` (one kernel each, sps_paged_compact two, sps_paged_copy one per 64 layers), read and write
+ * All calls only enqueue on `stream` (one kernel each, sps_paged_compact of a large pool or table two, sps_paged_copy one per 64 layers), read and write
  * their state on the device -- so that a captured call can be replayed -- and allocate nothing.  A pool's, a table's or a
  * workspace's calls must not run at the same time.  Results do not depend on timing: of free pages the lowest are taken, rows are
  * served in their order.  What does not fit is skipped, never followed, and sets a bit of the pool's status: page numbers

@@ -663,6 +663,7 @@ class PagePool:
         self.refs, self.page_size, self.index = refs, int(page_size), refs.get_device()
         p = _ints(refs, (refs.shape[0],), self.index, "refs")
         self.status = torch.zeros(1, dtype=torch.int32, device=refs.device) if status is None else status
+        self._need = lib().sps_paged_pool_workspace_bytes(refs.shape[0])
         self._c = sps_page_pool(p, _ints(self.status, (1,), self.index, "status"), refs.shape[0], self.page_size)
         self._p = C.addressof(self._c)
 
@@ -716,7 +717,7 @@ def sps_paged_pool_workspace_bytes(n_pages):
 
 
 def _pool_workspace(pool, workspace):
-    if workspace.get_device() != pool.index or not workspace.is_contiguous() or workspace.nbytes < lib().sps_paged_pool_workspace_bytes(pool._c.n_pages):
+    if workspace.nbytes < pool._need or workspace.get_device() != pool.index or not workspace.is_contiguous():
         raise ValueError("workspace: on the pool's device, contiguous, of sps_paged_pool_workspace_bytes")
     return workspace.data_ptr()
 

@@ -344,6 +344,20 @@ def test_compact_in_steps_of_a_short_list():
     assert not moves and sorted(p for r in m.rows for p in r) == list(range(240))
 
 
+@pytest.mark.parametrize("n_pages", [50, 20000])
+def test_compact_without_rows_moves_what_is_in_use(n_pages):
+    """Pages that no table of this call names: their references and contents move all the same."""
+    d = Device(n_pages, 8, 0, 0)
+    d.pool.refs[n_pages - 7:] = 3
+    d.compact()
+    assert d.listed() == [[n_pages - 7 + i, i, 8] for i in range(7)]
+    assert d.pool.refs[:7].tolist() == [3] * 7 and not d.pool.refs[7:].any()
+    d = Device(n_pages, 8, 2, 0)
+    d.pool.refs[n_pages - 1] = 1
+    d.compact()
+    assert d.listed() == [[n_pages - 1, 0, 8]] and d.t.held.tolist() == [0, 0]
+
+
 def test_compact_keeps_entries_that_name_no_page():
     m, d = grown(40, 8, [30, 30], seed=2)
     d.t.pages[0, 0], d.t.pages[1, 2] = 40, -2
