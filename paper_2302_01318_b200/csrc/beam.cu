@@ -40,12 +40,21 @@ struct BeamArgs {
   float* seg_max;            // [B W][n_seg]
   float2* parts;             // [B W][max_parts]: maximum, sum of exponentials
   int n_seg, groups, run, max_parts;   // segments and groups of a row, groups of a run, parts a row may have
+  int step_w, step_r;        // the picking CTA's threads over n_seg, and what is left
 };
 
 __device__ __forceinline__ float ex2(float x) {
   float y;
   asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(y) : "f"(x));
   return y;
+}
+// two fp32 operations in one instruction: (x, y) f + (g, g); (x, y) += (a, b)
+__device__ __forceinline__ void fma2(float& x, float& y, float f, float g) {
+  asm("{\n .reg .b64 s, t, u;\n mov.b64 s, {%0, %1};\n mov.b64 t, {%2, %2};\n mov.b64 u, {%3, %3};\n fma.rn.f32x2 s, s, t, u;\n mov.b64 {%0, %1}, s;\n}\n"
+      : "+f"(x), "+f"(y) : "f"(f), "f"(g));
+}
+__device__ __forceinline__ void add2(float& x, float& y, float a, float b) {
+  asm("{\n .reg .b64 s, t;\n mov.b64 s, {%0, %1};\n mov.b64 t, {%2, %3};\n add.rn.f32x2 s, s, t;\n mov.b64 {%0, %1}, s;\n}\n" : "+f"(x), "+f"(y) : "f"(a), "f"(b));
 }
 // numbers in the order of floats; NaN never comes here (maxima leave it out)
 __device__ __forceinline__ int ordered(float x) {
@@ -139,8 +148,8 @@ __device__ __forceinline__ void running_add(Running& r, const uint4 (&u)[SCAN_SE
       Logit<T>::unpack(u[j], f);
 #pragma unroll
       for (int e = 0; e < E; e += 2) {
-        s0 += ex2(fmaf(f[e], c, -R1));
-        s1 += ex2(fmaf(f[e + 1], c, -R1));
+        fma2(f[e], f[e + 1], c, -R1);
+        add2(s0, s1, ex2(f[e]), ex2(f[e + 1]));
       }
     }
     r.R = m1 == -INFINITY ? -INFINITY : R1;
@@ -319,7 +328,7 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
   // a beam's part of its candidates' scores, -inf where it has none: c = base + (l - max) / T
   auto parts_of = [&](int w) { return ((first + w) * a.groups + a.groups - 1) / a.run - (first + w) * a.groups / a.run + 1; };
   float2 ahead = make_float2(-INFINITY, 0.f);   // (so is a warp's first part)
-  if (warp < a.W && lane < parts_of(warp)) ahead = all_parts[(long long)warp * a.max_parts + lane];
+  if (warp < a.W && lane < a.max_parts) ahead = all_parts[(long long)warp * a.max_parts + lane];   // (those behind its own are not used)
   __syncthreads();   // (`beams` is there)
   for (int w = warp; w < a.W; w += WARPS) {
     const float2* parts = all_parts + (long long)w * a.max_parts;
@@ -327,8 +336,7 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
     float m = -INFINITY, s = 0.f;
     for (int p0 = 0; p0 < n_parts; p0 += 32) {   // (one round, but for few rows that are long)
       float2 v = make_float2(-INFINITY, 0.f);
-      if (w == warp && p0 == 0) v = ahead;
-      else if (p0 + lane < n_parts) v = parts[p0 + lane];
+      if (p0 + lane < n_parts) v = w == warp && p0 == 0 ? ahead : parts[p0 + lane];
       warp_merge(v.x, v.y, a.c);
       const float t = fmaxf(m, v.x), r = t == -INFINITY ? 0.f : t;
       s = s * ex2((m - r) * a.c) + v.y * ex2((v.x - r) * a.c);
@@ -354,7 +362,6 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
     const float v = base + t, e = fmaf(fabsf(base) + fabsf(t), 4.7683716e-7f, 1e-36f);   // 2^-21
     return t > -INFINITY ? make_float2(v - e, v + e) : make_float2(-INFINITY, fmaf(fabsf(base), 4.7683716e-7f, base));
   };
-  const int step_w = THREADS / a.n_seg, step_r = THREADS - step_w * a.n_seg;
   // The N best segments.  Scores are first taken in fp32 with what these may be off by, below and above: at least N reach the
   // bound with what they have at least, and only those that may reach it are scored in 64 bits.  The bound is the N-th of
   // the groups' best threads, k from each group: a group is every WARPS-th thread, whose segments are of all beams
@@ -372,12 +379,12 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
         high[j] = v.y;
         top = fmaxf(top, v.x);
       }
-      w += step_w; r += step_r;
+      w += a.step_w; r += a.step_r;
       if (r >= a.n_seg) { r -= a.n_seg; ++w; }
     }
     for (int i = tid + PER * THREADS; i < all; i += THREADS) {
       top = fmaxf(top, about(w, seg_max[i]).x);
-      w += step_w; r += step_r;
+      w += a.step_w; r += a.step_r;
       if (r >= a.n_seg) { r -= a.n_seg; ++w; }
     }
   }
@@ -405,13 +412,13 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
     for (int j = 0; j < PER; ++j) {
       if (j * THREADS >= all) continue;
       if (high[j] >= least && high[j] > -INFINITY) best_push(best, score_of(w, held[j]), tid + j * THREADS);
-      w += step_w; r += step_r;
+      w += a.step_w; r += a.step_r;
       if (r >= a.n_seg) { r -= a.n_seg; ++w; }
     }
     for (int i = tid + PER * THREADS; i < all; i += THREADS) {
       const float l = seg_max[i], h = about(w, l).y;
       if (h >= least && h > -INFINITY) best_push(best, score_of(w, l), i);
-      w += step_w; r += step_r;
+      w += a.step_w; r += a.step_r;
       if (r >= a.n_seg) { r -= a.n_seg; ++w; }
     }
   }
@@ -550,11 +557,13 @@ cudaError_t beam_launch(BeamArgs& a, int num_sm, cudaStream_t st) {
   a.n_seg = (a.V + SEG - 1) / SEG;
   a.groups = (a.n_seg + SCAN_SEGS - 1) / SCAN_SEGS;
   a.max_parts = max_parts(a.V);
+  auto steps = [&](int threads) { a.step_w = threads / a.n_seg; a.step_r = threads % a.n_seg; };
   const long long all = (long long)a.B * a.W * a.groups, warps = (long long)num_sm * 4 * SCAN_WARPS;
   // little work, no more than ONE_RUN groups to a warp and clusters that fit beside one another: one launch
   if ((long long)a.W * a.groups <= ONE_RUN * ONE_WARPS && a.B * ONE_CTAS <= num_sm) {
     a.run = (a.W * a.groups + ONE_WARPS - 1) / ONE_WARPS;
     a.max_parts = (a.groups + a.run - 1) / a.run + 1;   // W of them: ONE_WARPS + 2 W at most
+    steps(ONE_THREADS);
     return launch_k(beam_one_kernel<T, VEC>, dim3(a.B * ONE_CTAS), dim3(ONE_THREADS), 0, st, a);
   }
   a.run = (int)((all + warps - 1) / warps);
@@ -562,7 +571,11 @@ cudaError_t beam_launch(BeamArgs& a, int num_sm, cudaStream_t st) {
   cudaError_t e = launch_k(beam_scan_kernel<T, VEC>, dim3((unsigned)((runs + SCAN_WARPS - 1) / SCAN_WARPS)), dim3(SCAN_THREADS), 0, st, a);
   if (e != cudaSuccess) return e;
   // a small CTA for few segments: what each warp does for itself then costs less than the walk over them
-  if ((long long)a.W * a.n_seg <= 2048) return launch_k(beam_pick_kernel<T, VEC, 512>, dim3(a.B), dim3(512), 0, st, a);
+  if ((long long)a.W * a.n_seg <= 2048) {
+    steps(512);
+    return launch_k(beam_pick_kernel<T, VEC, 512>, dim3(a.B), dim3(512), 0, st, a);
+  }
+  steps(1024);
   return launch_k(beam_pick_kernel<T, VEC, 1024>, dim3(a.B), dim3(1024), 0, st, a);
 }
 template <typename T>
