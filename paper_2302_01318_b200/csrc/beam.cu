@@ -14,15 +14,16 @@ namespace cg = cooperative_groups;
 // Two kernels.  The scan reads every logit once: per row running maxima and sums of exponentials, and the maximum of every
 // segment of 512 bytes.  A row's order is its logits', so the N best elements lie in the N segments whose maxima score
 // best (ties to the lower segment: any element outside has N better ones in them) -- whatever the numbers are.  The pick, a
-// CTA per sequence, finds those segments, reads them again (N x 512 bytes, from L2) and picks the N best elements.
-// Bound by HBM with many rows, by latency with few.
+// CTA per sequence, finds those segments (or a few more), reads them again (N x 512 bytes, from L2) and picks the N best elements.
+// The scan is bound by HBM with many rows; the pick by latency, a chain of a dozen short steps between barriers (7 us): 256 rows of
+// 131071 in bf16 (67 MB) 23 us, 512 of 32000 in fp32 20 us, of which the bytes' floor is 10.
 // Candidates are compared in 64 bits, from exact logits and a sum of fp32 exponentials (relative error about 2^-22), so that
 // far scores keep the order of their last bits; results are rounded once.
 // ------------------------------------------------------------------------------------------------------------------
 namespace {
 
 constexpr int SCAN_THREADS = 256, SCAN_WARPS = 8, SCAN_SEGS = 4;       // segments of a group: a warp's load
-constexpr int ONE_RUN = 8, ONE_CTAS = 8, ONE_THREADS = 512, ONE_WARPS = ONE_CTAS * ONE_THREADS / 32;                         // the kernel for little work
+constexpr int ONE_RUN = 8, ONE_CTAS = 8, ONE_THREADS = 512, ONE_WARPS = ONE_CTAS * ONE_THREADS / 32;   // the kernel for little work
 constexpr int PICK_CAP = 1024, PICK_SPLIT = 8, PICK_PER = 8;           // entries of a list, threads that rank one, segments a thread holds
 constexpr int BEAM_MAX_B = 8192, BEAM_MAX_W = 128, BEAM_MAX_N = 128;
 
@@ -425,13 +426,14 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
   __syncthreads();
   // few more than N: all are read, else the N best
   int segs = s_count;
+  const bool all_read = segs <= BEAM_MAX_N;
   double bound = least;
-  if (segs > BEAM_MAX_N) {
+  if (!all_read) {
     segs = segs > PICK_CAP ? best_rounds<THREADS>(best, N, all, [&](int i, int* at) { *at = i; return score_of(i / a.n_seg, seg_max[i]); })
                            : best_rank<THREADS>(best, N);
     bound = segs == N ? s_keep[N - 1] : -INFINITY;
   }
-  const int* const from = s_count > BEAM_MAX_N ? s_keep_at : s_at;
+  const int* const from = all_read ? s_at : s_keep_at;
   for (int i = tid; i < segs; i += THREADS) {
     const int w = from[i] / a.n_seg;
     s_seg[i] = make_int2(w, (from[i] - w * a.n_seg) * SEG);
@@ -522,7 +524,8 @@ __global__ void __launch_bounds__(THREADS) beam_pick_kernel(const __grid_constan
   beam_pick<T, VEC, THREADS>(a, blockIdx.x, row, s_beams, a.seg_max + (long long)row * a.n_seg, a.parts + (long long)row * a.max_parts);
 }
 // Both for little work, a cluster to a sequence: what the scan finds goes straight to the shared memory of the CTA that picks.
-// One prompt of 4 x 32000: 8.6 us as two launches in a graph and 16 one by one (the host's), 9.9 and 12 this way through L2.
+// One prompt of 4 x 32000: 8.6 us as two launches in a graph and 16 one by one (the host's), 8.9 and 11.5 this way (through L2 9.9
+// and 12); eight of 8 x 32000 14.6 and 16.6 against 11.9 and 12.2.
 template <typename T, bool VEC>
 __global__ void __cluster_dims__(ONE_CTAS, 1, 1) __launch_bounds__(ONE_THREADS, 2) beam_one_kernel(const __grid_constant__ BeamArgs a) {
   __shared__ Beams s_beams;

@@ -67,6 +67,28 @@ def test_rising_and_falling_rows():
         run_and_check(x.view(1, 1, -1).repeat(1, 2, 1), torch.tensor([[-1.0, -1.5]], device=DEV), N=50)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("V,N", [(200_000, 5), (150_001, 128)])
+def test_more_equal_segments_than_the_list_holds(dtype, V, N):
+    """Thousands of segments tie: they are taken in rounds, as are their elements."""
+    flat = torch.full((2, 3, V), -0.75, dtype=dtype, device=DEV)
+    o = run_and_check(flat, torch.full((2, 3), -2.0, device=DEV), N=N, exact_ties=True)
+    assert o[2][1].tolist() == list(range(N)) and (o[1][1] == 3).all()
+    flat[0, 1, V - 9:] = 0.5
+    flat[1, 2, 7] = 0.5
+    run_and_check(flat, torch.full((2, 3), -2.0, device=DEV), N=N)
+    flat[:, 2, V - 3:] = 0.5                                   # (better ones in the last round alone)
+    run_and_check(flat, torch.full((2, 3), -2.0, device=DEV), N=N)
+
+
+def test_long_rising_and_falling_rows():
+    """The same with every segment better than all before it, or worse: each round brings better ones, or none."""
+    up = torch.arange(400_000, device=DEV, dtype=F32) * 2.0 ** -20
+    for x in (up, up.flip(0)):
+        for N in (1, 33, 128):
+            run_and_check(x.view(1, 1, -1).repeat(1, 2, 1), torch.tensor([[-1.0, -1.125]], device=DEV), N=N)
+
+
 def test_the_best_ones_in_one_segment_and_in_the_last_element():
     x = normal((2, 2, 5000), seed=3)
     x[:, 1, 1024:1088] += 30
