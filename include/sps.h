@@ -509,7 +509,7 @@ typedef struct {
 typedef struct {
   int32_t* pages;    /* device [B][ld] */
   int32_t *held, *len;   /* device [B]  */
-  int32_t B, ld;     /* B: up to 8192, B x ld below 2^31 */
+  int32_t B, ld;     /* B: up to 8192, ld: up to 2^20, B x ld below 2^31 */
 } sps_page_table;
 
 /* Pages to be copied, as a call leaves them: list[i] = (from, to, slots), the first `slots` of page `from`, *count of them. */

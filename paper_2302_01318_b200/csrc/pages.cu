@@ -51,38 +51,39 @@ __global__ void __launch_bounds__(FORK_THREADS) fork_kernel(const __grid_constan
   pdl_launch_dependents();
   pdl_wait();
   const int row = blockIdx.x, tid = threadIdx.x, e0 = blockIdx.y * FORK_THREADS * FORK_PER + tid;
-  if (row < a.dst.B) {
-    const int parent = a.parents[row];
-    const bool there = parent >= 0 && parent < a.src.B;
-    const int held = there ? row_held(a.src, a.pool, parent) : 0;
+  // as a row of src: what it gives up or hands on; as a row of dst: what it gets (both on their way before either is looked at)
+  const bool is_src = row < a.src.B, is_dst = row < a.dst.B;
+  const int gives = is_src ? row_held(a.src, a.pool, row) : 0, parent = is_dst ? a.parents[row] : -1;
+  const bool there = parent >= 0 && parent < a.src.B;
+  const int gets = there ? row_held(a.src, a.pool, parent) : 0;
+  const int32_t* const mine = a.src.pages + (long long)(is_src ? row : 0) * a.src.ld;
+  const int32_t* const from = a.src.pages + (long long)(there ? parent : 0) * a.src.ld;
+  int v[FORK_PER], u[FORK_PER], children = 0;
+#pragma unroll
+  for (int i = 0; i < FORK_PER; ++i) {
+    const int e = e0 + i * FORK_THREADS;
+    u[i] = e < gives ? mine[e] : 0;
+    v[i] = e < gets ? from[e] : 0;
+  }
+  if (is_src)
+    for (int b0 = 0; b0 < a.dst.B; b0 += FORK_THREADS) children += __syncthreads_count(b0 + tid < a.dst.B && a.parents[b0 + tid] == row);
+  if (is_dst) {
     if (blockIdx.y == 0 && tid == 0) {
       if (parent >= a.src.B) paged_flag(a.pool.status, SPS_PAGED_BAD_ROW);
-      a.dst.held[row] = held;
+      a.dst.held[row] = gets;
       a.dst.len[row] = there ? a.src.len[parent] : 0;
     }
-    const int32_t* from = a.src.pages + (long long)(there ? parent : 0) * a.src.ld;
-    int32_t* to = a.dst.pages + (long long)row * a.dst.ld;
-    int v[FORK_PER];
-#pragma unroll
-    for (int i = 0; i < FORK_PER; ++i) v[i] = e0 + i * FORK_THREADS < held ? from[e0 + i * FORK_THREADS] : 0;
+    int32_t* const to = a.dst.pages + (long long)row * a.dst.ld;
 #pragma unroll
     for (int i = 0; i < FORK_PER; ++i)
-      if (e0 + i * FORK_THREADS < held) to[e0 + i * FORK_THREADS] = v[i];
+      if (e0 + i * FORK_THREADS < gets) to[e0 + i * FORK_THREADS] = v[i];
   }
-  if (row < a.src.B) {
-    int children = 0;
-    for (int b0 = 0; b0 < a.dst.B; b0 += FORK_THREADS) children += __syncthreads_count(b0 + tid < a.dst.B && a.parents[b0 + tid] == row);
-    if (children == 1) return;
-    const int held = row_held(a.src, a.pool, row);
-    const int32_t* from = a.src.pages + (long long)row * a.src.ld;
-    int v[FORK_PER];
-#pragma unroll
-    for (int i = 0; i < FORK_PER; ++i) v[i] = e0 + i * FORK_THREADS < held ? from[e0 + i * FORK_THREADS] : -2;
+  if (is_src && children != 1) {
 #pragma unroll
     for (int i = 0; i < FORK_PER; ++i) {
-      if (v[i] == -2 && e0 + i * FORK_THREADS >= held) continue;
-      if (v[i] < 0 || v[i] >= a.pool.n_pages) paged_flag(a.pool.status, SPS_PAGED_BAD_PAGE);
-      else atomicAdd(a.pool.refs + v[i], children - 1);
+      if (e0 + i * FORK_THREADS >= gives) continue;
+      if (u[i] < 0 || u[i] >= a.pool.n_pages) paged_flag(a.pool.status, SPS_PAGED_BAD_PAGE);
+      else atomicAdd(a.pool.refs + u[i], children - 1);
     }
   }
 }
@@ -685,7 +686,7 @@ const char* bad_pool(const sps_page_pool* p) {
 const char* bad_table(const sps_page_table* t) {
   if (!t) return "null table";
   if (t->B < 0 || t->B > PAGES_MAX_ROWS) return "table: B must be 0 .. 8192";
-  if (t->ld < 0 || (int64_t)t->B * t->ld > INT_MAX) return "table: ld negative, or B x ld not below 2^31";
+  if (t->ld < 0 || t->ld > PAGES_MAX || (int64_t)t->B * t->ld > INT_MAX) return "table: ld must be 0 .. 2^20, B x ld below 2^31";
   if (t->B > 0 && (!t->held || !t->len || (!t->pages && t->ld > 0))) return "table: null pointer";
   if (((uintptr_t)t->pages | (uintptr_t)t->held | (uintptr_t)t->len) & 3) return "table: pointers must be 4-byte aligned";
   return nullptr;

@@ -73,7 +73,7 @@ def test_pools(kw, word):
         refused(rc, word)
 
 
-@pytest.mark.parametrize("kw,word", [(dict(B=-1), "B"), (dict(B=8193), "B"), (dict(ld=-1), "ld"), (dict(B=8192, ld=262144), "2^31"), (dict(pages=None), "null"),
+@pytest.mark.parametrize("kw,word", [(dict(B=-1), "B"), (dict(B=8193), "B"), (dict(ld=-1), "ld"), (dict(ld=(1 << 20) + 1), "ld"), (dict(B=8192, ld=262144), "2^31"), (dict(pages=None), "null"),
                                      (dict(held=None), "null"), (dict(len=None), "null"), (dict(len=P + 2), "aligned")])
 def test_tables(kw, word):
     for rc in (fork(s=table(**kw)), fork(d=other(**kw)), reserve(t=table(**kw)), compact(s=table(**kw)), compact(d=other(**kw))):
