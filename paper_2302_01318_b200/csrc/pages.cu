@@ -609,9 +609,14 @@ __global__ void __launch_bounds__(COPY_THREADS) copy_kernel(const __grid_constan
   const int count = min(max(a.moves.count[0], 0), a.moves.capacity);
   int had = -1, n = 0;
   long long off[PER];   // of this thread's pieces in a page, for `had` slots
+  int next[3] = {0, 0, 0};   // the next item, read while this one is copied
+  auto read = [&](int i) {
+    if (i < count) { next[0] = a.moves.list[3ll * i]; next[1] = a.moves.list[3ll * i + 1]; next[2] = a.moves.list[3ll * i + 2]; }
+  };
+  read(first);
   for (int i = first; i < count; i += step) {
-    const int32_t* m = a.moves.list + 3ll * i;
-    const int from = m[0], to = m[1], slots = min(max(m[2], 0), a.page_size);
+    const int from = next[0], to = next[1], slots = min(max(next[2], 0), a.page_size);
+    read(i + step);
     if (from < 0 || from >= a.n_pages || to < 0 || to >= a.n_pages) continue;
     if (slots != had) {
       had = slots;

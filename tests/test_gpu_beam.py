@@ -36,6 +36,43 @@ def test_against_64_bits(B, W, V, N, dtype, pad, T):
     run_and_check(normal((B, W, V), dtype, B + V, pad=pad), beams(B, W, V), N=N, T=T)
 
 
+@pytest.mark.parametrize("B,W,V,N,dtype,pad", [(8192, 1, 33, 2, F32, 0), (1, 128, 32000, 128, F32, 0), (20, 4, 32001, 6, BF16, 3), (19, 5, 8001, 64, F32, 1),
+                                               (40, 3, 515, 5, BF16, 0), (3, 7, 90_001, 100, BF16, 7)])
+def test_many_sequences_wide_beams_and_unaligned_rows_in_both_forms(B, W, V, N, dtype, pad):
+    run_and_check(normal((B, W, V), dtype, B + V, pad=pad), beams(B, W, V), N=N)
+
+
+def test_sequences_of_which_many_beams_are_dead_or_done():
+    """Whole runs of rows are skipped, and parts begin and end beside them."""
+    B, W, V = 60, 16, 3001
+    x, s = normal((B, W, V), seed=31), beams(B, W, 3)
+    g = torch.Generator().manual_seed(9)
+    s[(torch.rand((B, W), generator=g) < 0.5).to(DEV)] = -INF
+    s[7:25] = -INF
+    s[25, 15] = -1.0
+    done = (torch.rand((B, W), generator=g) < 0.3).to(I32).to(DEV)
+    done[40:44] = 1
+    run_and_check(x, s, done, 11, N=9)
+
+
+def test_two_calls_at_once_on_streams_and_workspaces_of_their_own():
+    shapes = [(2, 4, 32000), (70, 4, 32000)]
+    data = [(normal(sh, seed=i), beams(*sh[:2], i)) for i, sh in enumerate(shapes)]
+    want = [run_select(x, s, N=4) for x, s in data]
+    streams = [torch.cuda.Stream() for _ in shapes]
+    got, ws = [], []
+    for x, s in data:
+        got.append([torch.zeros((x.shape[0], 4), device=DEV)] + [torch.zeros((x.shape[0], 4), dtype=I32, device=DEV) for _ in range(2)])
+        ws.append(torch.zeros(sps.sps_beam_select_workspace_bytes(*x.shape), dtype=torch.uint8, device=DEV))
+    torch.cuda.synchronize()
+    for _ in range(20):
+        for (x, s), o, w, st in zip(data, got, ws, streams):
+            sps.sps_beam_select(x, s, *o, w, stream=st.cuda_stream)
+    torch.cuda.synchronize()
+    for a, b in zip(got, want):
+        assert all(torch.equal(p, q) for p, q in zip(a, b))
+
+
 @pytest.mark.parametrize("offset", [1, 2, 3, 5])
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_rows_of_any_alignment(offset, dtype):

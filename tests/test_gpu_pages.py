@@ -96,6 +96,38 @@ def test_fork_of_nothing_and_into_nothing():
     assert dst.held.tolist() == [0, 0] and int(d.pool.status) == sps.PAGED_BAD_ROW
 
 
+@pytest.mark.parametrize("n_pages", [12, 30000])
+def test_tables_without_rows(n_pages):
+    d = Device(n_pages, 8, 0, 4, capacity=3)
+    d.moves.count.fill_(9)
+    d.reserve([])
+    assert int(d.moves.count) == 0 and not d.pool.refs.any() and int(d.pool.status) == 0
+    d = Device(n_pages, 8, 3, 0)
+    d.reserve([0, 0, 0])
+    assert int(d.pool.status) == 0
+    d.reserve([0, 1, 0])                                       # rows without entries have room for nothing
+    assert int(d.pool.status) == sps.PAGED_BAD_LENGTH and d.t.held.tolist() == [0, 0, 0]
+
+
+def test_two_pools_at_once_on_streams_of_their_own():
+    ms = [grown(n, 8, [60, 41, 7, 0], ld=16, seed=n) for n in (200, 40000)]
+    streams = [torch.cuda.Stream() for _ in ms]
+    wants = [ints([w + 3 * i for w in (60, 41, 7, 1)]) for i in range(8)]
+    parents = ints([0, 1, 1, 2])
+    torch.cuda.synchronize()
+    for want in wants:
+        for (m, d), st in zip(ms, streams):
+            sps.sps_paged_reserve(d.pool, d.t, want, d.moves, d.ws, stream=st.cuda_stream)
+            sps.sps_paged_fork(d.pool, d.t, d.tables[1 - d.at], parents, stream=st.cuda_stream)
+            d.at = 1 - d.at
+    torch.cuda.synchronize()
+    for m, d in ms:
+        for want in wants:
+            m.reserve(want.tolist())
+            m.fork([0, 1, 1, 2])
+        d.check(m)
+
+
 def test_fork_skips_what_does_not_fit():
     m, d = grown(20, 8, [30, 9, 17])
     d.t.pages[0, 1] = 20
@@ -398,6 +430,36 @@ def test_copy(L, H, page, d, dtype, order, gap):
     sps.sps_paged_copy(layers, sps.PageMoves(ints(moves + [[0, 1, page]]), ints([len(moves)])))
     for got, w in zip(k + v, want[0] + want[1]):
         assert torch.equal(got, w)
+
+
+@pytest.mark.parametrize("L,H,page,d,dtype,order,gap", [(2, 3, 16, 128, BF16, "head", 0), (2, 3, 16, 128, BF16, "slot", 0), (1, 9, 64, 128, F32, "head", 8),
+                                                        (66, 2, 8, 64, BF16, "slot", 0)])
+def test_copy_of_a_long_list_little_of_which_is_used(L, H, page, d, dtype, order, gap):
+    """A list that could hold more than half a gigabyte: the other kernel."""
+    n_pages = 40
+    k, v = caches(L, n_pages, H, page, d, dtype, order, gap=gap)
+    capacity = 600_000_000 // (2 * min(L, 2) * H * page * d * k[0].element_size())
+    perm = torch.randperm(n_pages, generator=torch.Generator().manual_seed(L)).tolist()
+    slots = [1, page, page - 1, 0, page // 2, 3, page]
+    moves = [[perm[2 * i], perm[2 * i + 1], n] for i, n in enumerate(slots)]
+    want = [copied(t, moves) for t in k + v]
+    layers = sps.PagedLayers([sps.PagedCache(a, b) for a, b in zip(k, v)])
+    list_ = torch.full((capacity, 3), -1, dtype=I32, device=DEV)
+    list_[:len(moves)] = ints(moves)
+    sps.sps_paged_copy(layers, sps.PageMoves(list_, ints([len(moves)])))
+    assert all(torch.equal(a, b) for a, b in zip(k + v, want))
+
+
+def test_copy_of_pages_of_more_places_than_ctas():
+    k, v = caches(40, 6, 8, 512, 64, BF16, "head")
+    moves = [[5, 0, 512], [3, 1, 77], [4, 2, 511]]
+    want = [copied(t, moves) for t in k + v]
+    layers = sps.PagedLayers([sps.PagedCache(a, b) for a, b in zip(k, v)])
+    for capacity in (3, 9):
+        list_ = torch.zeros((capacity, 3), dtype=I32, device=DEV)
+        list_[:3] = ints(moves)
+        sps.sps_paged_copy(layers, sps.PageMoves(list_, ints([3])))
+        assert all(torch.equal(a, b) for a, b in zip(k + v, want))
 
 
 def test_copy_skips_what_does_not_fit():
