@@ -24,7 +24,7 @@ namespace {
 
 constexpr int SCAN_THREADS = 256, SCAN_WARPS = 8, SCAN_SEGS = 4;       // segments of a group: a warp's load
 constexpr int ONE_RUN = 8, ONE_CTAS = 8, ONE_THREADS = 512, ONE_WARPS = ONE_CTAS * ONE_THREADS / 32;   // the kernel for little work
-constexpr int PICK_CAP = 1024, PICK_SPLIT = 8, PICK_PER = 8;           // entries of a list, threads that rank one, segments a thread holds
+constexpr int PICK_CAP = 1024, PICK_COUNTED = 128, PICK_SPLIT = 8, PICK_PER = 8;   // entries of a list, of one ranked by counting, threads that rank one; segments a thread holds
 constexpr int BEAM_MAX_B = 8192, BEAM_MAX_W = 128, BEAM_MAX_N = 128;
 
 struct BeamArgs {
@@ -248,31 +248,106 @@ struct Best {
   double* keep_key;   // [BEAM_MAX_N]: the N best, in order
   int* keep_at;
   int* count;
+  int *thread, *tops, *bound;   // [THREADS + WARPS], [BEAM_MAX_N + 2 WARPS], [1]: for best_bound
 };
 __device__ __forceinline__ bool better(double k, int i, double k1, int i1) { return k > k1 || (k == k1 && i < i1); }
 __device__ __forceinline__ void best_push(const Best& b, double k, int i) {
   const int n = atomicAdd(b.count, 1);
   if (n < PICK_CAP) { b.key[n] = k; b.at[n] = i; }
 }
-// the list's N best to keep_key / keep_at in order, every entry counting those before it, PICK_SPLIT threads to an entry;
-// returns how many there are (every thread of the CTA calls it, the list is complete)
+// a number that at least N of the threads' numbers reach (-inf: they may be fewer): the N-th of the groups' best, k from each, a
+// group being every WARPS-th thread (so that neighbours, which may all be of one beam, are in groups of their own)
 template <int THREADS>
-__device__ __forceinline__ int best_rank(const Best& b, int N) {
-  const int n = min(*b.count, PICK_CAP), sub = threadIdx.x % PICK_SPLIT;
-  for (int i0 = 0; i0 < n; i0 += THREADS / PICK_SPLIT) {
-    const int i = i0 + threadIdx.x / PICK_SPLIT;
-    const double k = i < n ? b.key[i] : 0.0;
-    const int p = i < n ? b.at[i] : 0;
-    int r = 0;
-    if (i < n)
-#pragma unroll 4
-      for (int j = sub; j < n; j += PICK_SPLIT) r += better(b.key[j], b.at[j], k, p);
-#pragma unroll
-    for (int o = PICK_SPLIT / 2; o > 0; o >>= 1) r += __shfl_xor_sync(0xffffffffu, r, o);
-    if (i < n && sub == 0 && r < N) { b.keep_key[r] = k; b.keep_at[r] = p; }
+__device__ __forceinline__ float best_bound(const Best& b, float top, int N) {
+  constexpr int WARPS = THREADS / 32;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, k = (N + WARPS - 1) / WARPS + 1, mine_at = lane * WARPS + warp;
+  b.thread[tid + tid / 32] = ordered(top);
+  if (tid == 0) *b.bound = INT_MIN;
+  __syncthreads();
+  int mine = b.thread[mine_at + mine_at / 32];
+  for (int j = 0; j < k; ++j) {
+    const int v = __reduce_max_sync(0xffffffffu, mine);
+    if (lane == 0) b.tops[warp * k + j] = v;
+    if (__ffs(__ballot_sync(0xffffffffu, mine == v)) - 1 == lane) mine = INT_MIN;
   }
   __syncthreads();
-  return min(n, N);
+  for (int i = tid; i < k * WARPS; i += THREADS) {
+    const int v = b.tops[i];
+    int r = 0;
+#pragma unroll 8
+    for (int j = 0; j < k * WARPS; ++j) r += b.tops[j] > v || (b.tops[j] == v && j < i);
+    if (r == N - 1) *b.bound = v;
+  }
+  __syncthreads();
+  return unordered(max(*b.bound, ordered(-INFINITY)));
+}
+
+// The list's N best to keep_key / keep_at in order; returns how many there are (every thread of the CTA calls it, the list is
+// complete).  Every entry counts those before it, PICK_SPLIT threads to an entry.  A long list (few segments with many candidates)
+// is first cut to what reaches a bound; what is long even then (ties by the hundred) is sorted, a bitonic network over the next power
+// of two, of which a warp has 64 neighbours to itself.  Counting 1000 entries would take 50 us, sorting them 10, the cut 1.
+template <int THREADS>
+__device__ __forceinline__ int best_rank(const Best& b, int N) {
+  const int tid = threadIdx.x;
+  int n = min(*b.count, PICK_CAP);
+  const int found = min(n, N);
+  if (n > PICK_COUNTED) {
+    constexpr int PER = (PICK_CAP + THREADS - 1) / THREADS;
+    double k[PER];
+    int p[PER];
+    float top = -INFINITY;
+#pragma unroll
+    for (int j = 0; j < PER; ++j) {
+      const int i = tid + j * THREADS;
+      k[j] = i < n ? b.key[i] : -INFINITY;
+      p[j] = i < n ? b.at[i] : 0;
+      top = fmaxf(top, __double2float_rd(k[j]));
+    }
+    const float least = best_bound<THREADS>(b, top, N);
+    if (tid == 0) *b.count = 0;
+    __syncthreads();
+#pragma unroll
+    for (int j = 0; j < PER; ++j)
+      if (k[j] > -INFINITY && k[j] >= (double)least) best_push(b, k[j], p[j]);
+    __syncthreads();
+    n = *b.count;
+  }
+  if (n <= 2 * PICK_COUNTED) {
+    const int sub = tid % PICK_SPLIT;
+    for (int i0 = 0; i0 < n; i0 += THREADS / PICK_SPLIT) {
+      const int i = i0 + tid / PICK_SPLIT;
+      const double k = i < n ? b.key[i] : 0.0;
+      const int p = i < n ? b.at[i] : 0;
+      int r = 0;
+      if (i < n)
+#pragma unroll 4
+        for (int j = sub; j < n; j += PICK_SPLIT) r += better(b.key[j], b.at[j], k, p);
+#pragma unroll
+      for (int o = PICK_SPLIT / 2; o > 0; o >>= 1) r += __shfl_xor_sync(0xffffffffu, r, o);
+      if (i < n && sub == 0 && r < N) { b.keep_key[r] = k; b.keep_at[r] = p; }
+    }
+  } else {
+    int size = 4 * PICK_COUNTED;
+    while (size < n) size *= 2;
+    for (int i = n + tid; i < size; i += THREADS) { b.key[i] = -INFINITY; b.at[i] = INT_MAX; }
+    __syncthreads();
+    for (int run = 2; run <= size; run *= 2)
+      for (int step = run / 2; step > 0; step /= 2) {
+        if (tid < size / 2) {
+          const int i = 2 * tid - (tid & (step - 1)), j = i + step;
+          const double ki = b.key[i], kj = b.key[j];
+          const int ai = b.at[i], aj = b.at[j];
+          if (better(kj, aj, ki, ai) == ((i & run) == 0)) { b.key[i] = kj; b.at[i] = aj; b.key[j] = ki; b.at[j] = ai; }
+        }
+        // the next step's pairs lie within what a warp has, unless its step is above 32
+        if (step > 32 || (step == 1 && run > 32)) __syncthreads();
+        else __syncwarp();
+      }
+    __syncthreads();
+    for (int i = tid; i < N; i += THREADS) { b.keep_key[i] = b.key[i]; b.keep_at[i] = b.at[i]; }   // (N <= PICK_COUNTED < n)
+  }
+  __syncthreads();
+  return found;
 }
 // the N best of item(0 .. all - 1) -> (key, place), -inf keys left out, in rounds
 template <int THREADS, class Item>
@@ -315,10 +390,10 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
   constexpr int E = Logit<T>::E, SEG = 32 * E, WARPS = THREADS / 32, PER = PICK_PER;
   __shared__ double s_key[PICK_CAP], s_keep[BEAM_MAX_N], s_base[BEAM_MAX_W];
   __shared__ float s_max[BEAM_MAX_W], s_base32[BEAM_MAX_W];
-  __shared__ int s_thread[THREADS + WARPS], s_at[PICK_CAP], s_keep_at[BEAM_MAX_N], s_top[BEAM_MAX_N + 2 * WARPS], s_count, s_bound;
+  __shared__ int s_thread[THREADS + WARPS], s_at[PICK_CAP], s_keep_at[BEAM_MAX_N], s_tops[BEAM_MAX_N + 2 * WARPS], s_count, s_bound;
   __shared__ int2 s_seg[BEAM_MAX_N];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, N = a.N;
-  const Best best{s_key, s_at, s_keep, s_keep_at, &s_count};
+  const Best best{s_key, s_at, s_keep, s_keep_at, &s_count, s_thread, s_tops, &s_bound};
   const int all = a.W * a.n_seg;
   float held[PER];   // the first segments' maxima are on their way while the beams are looked at
 #pragma unroll
@@ -352,7 +427,7 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
       s_max[w] = m;
     }
   }
-  if (tid == 0) { s_count = 0; s_bound = INT_MIN; }
+  if (tid == 0) s_count = 0;
   __syncthreads();
   auto score_of = [&](int w, float l) { return s_base[w] > -INFINITY ? s_base[w] + ((double)l - (double)s_max[w]) * a.inv_t : -INFINITY; };
   // score_of in fp32, less and more than what its roundings (base, difference, 1 / T, product, sum: 2^-24 each of a term, once more
@@ -364,9 +439,7 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
     return t > -INFINITY ? make_float2(v - e, v + e) : make_float2(-INFINITY, fmaf(fabsf(base), 4.7683716e-7f, base));
   };
   // The N best segments.  Scores are first taken in fp32 with what these may be off by, below and above: at least N reach the
-  // bound with what they have at least, and only those that may reach it are scored in 64 bits.  The bound is the N-th of
-  // the groups' best threads, k from each group: a group is every WARPS-th thread, whose segments are of all beams
-  const int k = (N + WARPS - 1) / WARPS + 1;
+  // bound with what they have at least, and only those that may reach it are scored in 64 bits
   const int w_first = tid / a.n_seg, r_first = tid - w_first * a.n_seg;
   float high[PER], top = -INFINITY;
   {
@@ -389,24 +462,7 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
       if (r >= a.n_seg) { r -= a.n_seg; ++w; }
     }
   }
-  s_thread[tid + tid / 32] = ordered(top);
-  __syncthreads();
-  int mine = s_thread[(lane * WARPS + warp) + (lane * WARPS + warp) / 32];
-  for (int j = 0; j < k; ++j) {
-    const int v = __reduce_max_sync(0xffffffffu, mine);
-    if (lane == 0) s_top[warp * k + j] = v;
-    if (__ffs(__ballot_sync(0xffffffffu, mine == v)) - 1 == lane) mine = INT_MIN;
-  }
-  __syncthreads();
-  for (int i = tid; i < k * WARPS; i += THREADS) {
-    const int v = s_top[i];
-    int r = 0;
-#pragma unroll 8
-    for (int j = 0; j < k * WARPS; ++j) r += s_top[j] > v || (s_top[j] == v && j < i);
-    if (r == N - 1) s_bound = v;
-  }
-  __syncthreads();
-  const float least = unordered(max(s_bound, ordered(-INFINITY)));
+  const float least = best_bound<THREADS>(best, top, N);
   {
     int w = w_first, r = r_first;
 #pragma unroll
