@@ -558,11 +558,11 @@ int sps_paged_copy(const sps_paged_cache* layers, int32_t n_layers, const sps_pa
  * equal ones in the order of w V + v.  The paper samples; this is the search its Related Work's decoding methods set beside it, over the
  * same logits, and with sps_paged_fork over the same cache.
  *   logits        device, dtype 0 fp32 / 1 bf16: row b W + w at logits + (b W + w) row_stride (elements), V of them; any alignment
- *                 (16-byte aligned rows are read 16 bytes at a time)
+ *                 of the rows
  *   scores        device fp32 [B][W]: log-probability of each beam so far; -inf: there is no such beam (the first step after
  *                 a prompt has one beam, or one score that is not -inf)
  *   done          device int32 [B][W], may be NULL: a beam that has ended (not 0) is not continued; it offers itself as one candidate,
- *                 (end_token, its score), and its logits are not read
+ *                 (end_token, its score), whatever its logits are
  *   end_token     -1: none; else candidates with it are done
  *   out_scores    device fp32 [B][N]: c, rounded once (candidates are compared before)
  *   out_parents   device int32 [B][N]: row b W + w of the continued beam -- the parents of sps_paged_fork when N = W

@@ -103,6 +103,25 @@ template <> struct Logit<__nv_bfloat16> {
   }
 };
 
+// Rows need not begin at 16 bytes: segments are counted from the 16-byte boundary at or before a row's first logit, `shift` elements
+// ahead of it, so that all but the pieces at its ends are read 16 bytes at a time.
+template <typename T>
+__device__ __forceinline__ const T* row_begin(const BeamArgs& a, int row, int* shift) {
+  const T* x = reinterpret_cast<const T*>(a.logits) + (long long)row * a.row_stride;
+  *shift = (int)(((uintptr_t)x & 15) / sizeof(T));
+  return x - *shift;
+}
+// the piece at place v of such a row (a multiple of E), -inf what is not of the row
+template <typename T>
+__device__ __forceinline__ uint4 load_piece(const T* x, int v, int shift, int V) {
+  constexpr int E = Logit<T>::E;
+  if (v >= shift && v + E <= V + shift) return *reinterpret_cast<const uint4*>(x + v);
+  float f[E];
+#pragma unroll
+  for (int e = 0; e < E; ++e) f[e] = v + e >= shift && v + e < V + shift ? Logit<T>::get(x + v + e) : -INFINITY;
+  return Logit<T>::pack(f);
+}
+
 // a beam that reads its logits: it has a score, and is not done
 __device__ __forceinline__ bool beam_reads(const BeamArgs& a, int row) {
   return !(a.done && a.done[row]) && isfinite(a.scores[row]);
@@ -162,21 +181,22 @@ __device__ __forceinline__ void running_add(Running& r, const uint4 (&u)[SCAN_SE
 // A run of the list of `rows` rows' groups (SCAN_SEGS segments; the last of a row may be short), from group x0 of the list on, by
 // one warp: its next group is under way while it works on this one, whatever the rows' number and length.  A run's share of a
 // row is a part of it; beams that are done or dead are skipped.  seg_max, parts: the list's.
-template <typename T, bool VEC>
+template <typename T>
 __device__ __forceinline__ void beam_scan(const BeamArgs& a, int first_row, int rows, int me, float* seg_max, float2* parts) {
   constexpr int E = Logit<T>::E, SEG = 32 * E, GROUP = SCAN_SEGS * SEG;
   const int lane = threadIdx.x & 31;
   const long long x0 = (long long)me * a.run;
-  const int whole = a.V / GROUP;   // groups of a row that are inside it
   if (x0 >= (long long)rows * a.groups) return;
   int row = (int)x0 / a.groups, g = (int)x0 - row * a.groups, left = (int)min((long long)a.run, (long long)rows * a.groups - x0);
-  const T* x = reinterpret_cast<const T*>(a.logits) + (long long)(first_row + row) * a.row_stride;
+  int shift;
+  const T* x = row_begin<T>(a, first_row + row, &shift);
   uint4 u[SCAN_SEGS];
   auto fetch = [&](const T* p, int group) {
 #pragma unroll
     for (int j = 0; j < SCAN_SEGS; ++j) u[j] = *reinterpret_cast<const uint4*>(p + (long long)group * GROUP + j * SEG + lane * E);
   };
-  bool fetched = VEC && g < whole;
+  auto inside = [&](int group) { return (group > 0 || shift == 0) && (group + 1) * GROUP <= a.V + shift; };   // all of it in the row
+  bool fetched = inside(g);
   if (fetched) fetch(x, g);   // (before its row is known to be read)
   int row0 = row;
   unsigned live = __ballot_sync(0xffffffffu, row + lane < rows && beam_reads(a, first_row + min(row + lane, rows - 1)));
@@ -189,33 +209,25 @@ __device__ __forceinline__ void beam_scan(const BeamArgs& a, int first_row, int 
     if (!((live >> (row - row0)) & 1)) {
       left -= a.groups - g;
       ++row;
-      x += a.row_stride;
       g = 0;
-      fetched = VEC && left > 0 && whole > 0 && row - row0 < 32 && ((live >> (row - row0)) & 1);
+      if (left <= 0) break;
+      x = row_begin<T>(a, first_row + row, &shift);
+      fetched = row - row0 < 32 && ((live >> (row - row0)) & 1) && inside(0);
       if (fetched) fetch(x, 0);
       continue;
     }
     uint4 now[SCAN_SEGS];
-    if (VEC && g < whole) {
-      if (!fetched) fetch(x, g);
 #pragma unroll
-      for (int j = 0; j < SCAN_SEGS; ++j) now[j] = u[j];
-    } else {
-#pragma unroll
-      for (int j = 0; j < SCAN_SEGS; ++j) {
-        float f[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) {
-          const int v = g * GROUP + j * SEG + e * 32 + lane;
-          f[e] = v < a.V ? Logit<T>::get(x + v) : -INFINITY;
-        }
-        now[j] = Logit<T>::pack(f);
-      }
+    for (int j = 0; j < SCAN_SEGS; ++j) now[j] = fetched ? u[j] : load_piece(x, g * GROUP + j * SEG + lane * E, shift, a.V);
+    const int now_row = row, now_g = g;
+    --left;
+    if (++g == a.groups) {
+      g = 0;
+      ++row;
+      if (left > 0) x = row_begin<T>(a, first_row + row, &shift);
     }
-    const bool ends = g + 1 == a.groups || left == 1;
-    if (g + 1 < a.groups) fetched = VEC && left > 1 && g + 1 < whole;
-    else fetched = VEC && left > 1 && whole > 0 && row + 1 - row0 < 32 && ((live >> (row + 1 - row0)) & 1);
-    if (fetched) { if (g + 1 < a.groups) fetch(x, g + 1); else fetch(x + a.row_stride, 0); }
+    fetched = left > 0 && row - row0 < 32 && ((live >> (row - row0)) & 1) && inside(g);
+    if (fetched) fetch(x, g);
     float top = -INFINITY;
     int best = 0;
 #pragma unroll
@@ -225,17 +237,15 @@ __device__ __forceinline__ void beam_scan(const BeamArgs& a, int first_row, int 
       const int w = __reduce_max_sync(0xffffffffu, ordered(t));
       if (lane == j) best = w;
     }
-    if (lane < SCAN_SEGS && g * SCAN_SEGS + lane < a.n_seg) seg_max[(long long)row * a.n_seg + g * SCAN_SEGS + lane] = unordered(best);
+    if (lane < SCAN_SEGS && now_g * SCAN_SEGS + lane < a.n_seg) seg_max[(long long)now_row * a.n_seg + now_g * SCAN_SEGS + lane] = unordered(best);
     running_add<T>(run, now, top, a.c);
-    if (ends) {
+    if (g == 0 || left == 0) {   // the end of the row, or of the run
       float m = run.m, s = run.s;
       if (!run.far && m > -INFINITY) s *= ex2(-fmaf(m, a.c, -run.R));
       warp_merge(m, s, a.c);
-      if (lane == 0) parts[(long long)row * a.max_parts + me - row * a.groups / a.run] = make_float2(m, s);
+      if (lane == 0) parts[(long long)now_row * a.max_parts + me - now_row * a.groups / a.run] = make_float2(m, s);
       run = Running{-INFINITY, -INFINITY, 0.f, false};
     }
-    --left;
-    if (++g == a.groups) { g = 0; ++row; x += a.row_stride; }
   }
 }
 
@@ -385,7 +395,7 @@ __device__ __forceinline__ void beams_load(const BeamArgs& a, int b, Beams& beam
 }
 
 // the pick of sequence b by a CTA; first: its first row in the list that was cut into runs, seg_max and parts: from there on
-template <typename T, bool VEC, int THREADS>
+template <typename T, int THREADS>
 __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, const Beams& beams, const float* seg_max, const float2* all_parts) {
   constexpr int E = Logit<T>::E, SEG = 32 * E, WARPS = THREADS / 32, PER = PICK_PER;
   __shared__ double s_key[PICK_CAP], s_keep[BEAM_MAX_N], s_base[BEAM_MAX_W];
@@ -498,7 +508,6 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
   if (tid == 0) s_count = 0;
   __syncthreads();
   // their elements that reach the bound, and the beams that are done
-  auto row_of = [&](int w) { return reinterpret_cast<const T*>(a.logits) + (long long)(b * a.W + w) * a.row_stride; };
   auto ended = [&](int w, int* at) {            // beam w's candidate, if it is done
     const float s = beams.done[w] ? beams.score[w] : -INFINITY;
     *at = w * a.V + a.end_token;
@@ -507,19 +516,13 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
   for (int i0 = warp; i0 < segs; i0 += 4 * WARPS) {
     uint4 u[4];
     int2 sg[4];
+    int shift[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       if (i0 + j * WARPS >= segs) continue;
       sg[j] = s_seg[i0 + j * WARPS];
-      const T* x = row_of(sg[j].x) + sg[j].y + lane * E;
-      if (VEC && sg[j].y + SEG <= a.V) {
-        u[j] = *reinterpret_cast<const uint4*>(x);
-      } else {
-        float f[E];
-#pragma unroll
-        for (int e = 0; e < E; ++e) f[e] = sg[j].y + lane * E + e < a.V ? Logit<T>::get(x + e) : -INFINITY;
-        u[j] = Logit<T>::pack(f);
-      }
+      const T* x = row_begin<T>(a, b * a.W + sg[j].x, &shift[j]);
+      u[j] = load_piece(x, sg[j].y + lane * E, shift[j], a.V);
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
@@ -533,7 +536,7 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
       for (int e = 0; e < E; ++e) {
         if (!(f[e] >= low)) continue;
         const double v = score_of(sg[j].x, f[e]);
-        if (v >= bound && v > -INFINITY) best_push(best, v, sg[j].x * a.V + sg[j].y + lane * E + e);
+        if (v >= bound && v > -INFINITY) best_push(best, v, sg[j].x * a.V + sg[j].y - shift[j] + lane * E + e);
       }
     }
   }
@@ -546,9 +549,11 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
   auto element = [&](int i, int* at) {          // element i of the segments, one behind the other, then the done beams
     if (i >= segs * SEG) return ended(i - segs * SEG, at);
     const int2 sg = s_seg[i / SEG];
-    const int v = sg.y + i % SEG;
+    int shift;
+    const T* x = row_begin<T>(a, b * a.W + sg.x, &shift);
+    const int v = sg.y + i % SEG - shift;
     *at = sg.x * a.V + v;
-    return v < a.V ? score_of(sg.x, Logit<T>::get(row_of(sg.x) + v)) : -(double)INFINITY;
+    return v >= 0 && v < a.V ? score_of(sg.x, Logit<T>::get(x + shift + v)) : -(double)INFINITY;
   };
   const int n = s_count > PICK_CAP ? best_rounds<THREADS>(best, N, segs * SEG + (a.done ? a.W : 0), element) : best_rank<THREADS>(best, N);
   for (int i = tid; i < N; i += THREADS) {
@@ -564,25 +569,25 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
 
 // With a CTA to each part of a row 64 x 4 rows of 131071 took 20 us, as runs 15.  Neighbouring runs go to different CTAs, so that
 // beams that are skipped are spread over all.
-template <typename T, bool VEC>
+template <typename T>
 __global__ void __launch_bounds__(SCAN_THREADS, 4) beam_scan_kernel(const __grid_constant__ BeamArgs a) {
   pdl_launch_dependents();
   pdl_wait();
-  beam_scan<T, VEC>(a, 0, a.B * a.W, (threadIdx.x >> 5) * gridDim.x + blockIdx.x, a.seg_max, a.parts);
+  beam_scan<T>(a, 0, a.B * a.W, (threadIdx.x >> 5) * gridDim.x + blockIdx.x, a.seg_max, a.parts);
 }
-template <typename T, bool VEC, int THREADS>
+template <typename T, int THREADS>
 __global__ void __launch_bounds__(THREADS) beam_pick_kernel(const __grid_constant__ BeamArgs a) {
   __shared__ Beams s_beams;
   const int row = blockIdx.x * a.W;
   pdl_launch_dependents();
   pdl_wait();
   beams_load<THREADS>(a, blockIdx.x, s_beams);
-  beam_pick<T, VEC, THREADS>(a, blockIdx.x, row, s_beams, a.seg_max + (long long)row * a.n_seg, a.parts + (long long)row * a.max_parts);
+  beam_pick<T, THREADS>(a, blockIdx.x, row, s_beams, a.seg_max + (long long)row * a.n_seg, a.parts + (long long)row * a.max_parts);
 }
 // Both for little work, a cluster to a sequence: what the scan finds goes straight to the shared memory of the CTA that picks.
 // One prompt of 4 x 32000: 8.6 us as two launches in a graph and 16 one by one (the host's), 8.9 and 11.5 this way (through L2 9.9
 // and 12); eight of 8 x 32000 14.6 and 16.6 against 11.9 and 12.2.
-template <typename T, bool VEC>
+template <typename T>
 __global__ void __cluster_dims__(ONE_CTAS, 1, 1) __launch_bounds__(ONE_THREADS, 2) beam_one_kernel(const __grid_constant__ BeamArgs a) {
   __shared__ Beams s_beams;
   __shared__ float s_segs[ONE_RUN * ONE_WARPS * SCAN_SEGS];
@@ -593,9 +598,9 @@ __global__ void __cluster_dims__(ONE_CTAS, 1, 1) __launch_bounds__(ONE_THREADS, 
   cl.sync();   // (the CTA that picks has to be there before others write to it)
   pdl_wait();
   if (rank == 0) beams_load<ONE_THREADS>(a, b, s_beams);
-  beam_scan<T, VEC>(a, b * a.W, a.W, (threadIdx.x >> 5) * ONE_CTAS + rank, cl.map_shared_rank(s_segs, 0), cl.map_shared_rank(s_parts, 0));
+  beam_scan<T>(a, b * a.W, a.W, (threadIdx.x >> 5) * ONE_CTAS + rank, cl.map_shared_rank(s_segs, 0), cl.map_shared_rank(s_parts, 0));
   cl.sync();
-  if (rank == 0) beam_pick<T, VEC, ONE_THREADS>(a, b, 0, s_beams, s_segs, s_parts);
+  if (rank == 0) beam_pick<T, ONE_THREADS>(a, b, 0, s_beams, s_segs, s_parts);
 }
 
 int no(int code, const char* msg) {
@@ -604,16 +609,19 @@ int no(int code, const char* msg) {
 }
 const char* bad_shape(int B, int W, int V) {
   if (B < 0 || B > BEAM_MAX_B || W < 1 || W > BEAM_MAX_W || V < 1 || V > 1 << 24) return "beams: B must be 0 .. 8192, W 1 .. 128, V 1 .. 2^24";
-  if ((int64_t)W * V > INT_MAX || (int64_t)B * W * ((V + 511) / 512) > INT_MAX) return "beams: W x V must stay below 2^31, B x W x V below 2^40";
+  if ((int64_t)W * V > INT_MAX || (int64_t)B * W * ((V + 514) / 512) > INT_MAX) return "beams: W x V must stay below 2^31, B x W x V below 2^40";
   return nullptr;
 }
 int64_t up(int64_t n) { return (n + 255) / 256 * 256; }
 
-int max_parts(int V) { return (V + 511) / 512 + 1; }   // of fp32 rows, which have the most groups; a run is one group at least
-template <typename T, bool VEC>
+// of fp32 rows, which have the most, shifted by up to 3: segments, and parts (a run is one group at least)
+int64_t most_segs(int V) { return ((int64_t)V + 3 + 127) / 128; }
+int max_parts(int V) { return (int)((most_segs(V) + SCAN_SEGS - 1) / SCAN_SEGS) + 1; }
+template <typename T>
 cudaError_t beam_launch(BeamArgs& a, int num_sm, cudaStream_t st) {
-  constexpr int SEG = 32 * Logit<T>::E;
-  a.n_seg = (a.V + SEG - 1) / SEG;
+  constexpr int E = Logit<T>::E, SEG = 32 * E;
+  const bool aligned = (((uintptr_t)a.logits | (uintptr_t)(a.row_stride * (int64_t)sizeof(T))) & 15) == 0;
+  a.n_seg = (a.V + (aligned ? 0 : E - 1) + SEG - 1) / SEG;
   a.groups = (a.n_seg + SCAN_SEGS - 1) / SCAN_SEGS;
   a.max_parts = max_parts(a.V);
   auto steps = [&](int threads) { a.step_w = threads / a.n_seg; a.step_r = threads % a.n_seg; };
@@ -623,26 +631,20 @@ cudaError_t beam_launch(BeamArgs& a, int num_sm, cudaStream_t st) {
     a.run = (a.W * a.groups + ONE_WARPS - 1) / ONE_WARPS;
     a.max_parts = (a.groups + a.run - 1) / a.run + 1;   // W of them: ONE_WARPS + 2 W at most
     steps(ONE_THREADS);
-    return launch_k(beam_one_kernel<T, VEC>, dim3(a.B * ONE_CTAS), dim3(ONE_THREADS), 0, st, a);
+    return launch_k(beam_one_kernel<T>, dim3(a.B * ONE_CTAS), dim3(ONE_THREADS), 0, st, a);
   }
   a.run = (int)((all + warps - 1) / warps);
   const long long runs = (all + a.run - 1) / a.run;
-  cudaError_t e = launch_k(beam_scan_kernel<T, VEC>, dim3((unsigned)((runs + SCAN_WARPS - 1) / SCAN_WARPS)), dim3(SCAN_THREADS), 0, st, a);
+  cudaError_t e = launch_k(beam_scan_kernel<T>, dim3((unsigned)((runs + SCAN_WARPS - 1) / SCAN_WARPS)), dim3(SCAN_THREADS), 0, st, a);
   if (e != cudaSuccess) return e;
   // a small CTA for few segments: what each warp does for itself then costs less than the walk over them
   if ((long long)a.W * a.n_seg <= 2048) {
     steps(512);
-    return launch_k(beam_pick_kernel<T, VEC, 512>, dim3(a.B), dim3(512), 0, st, a);
+    return launch_k(beam_pick_kernel<T, 512>, dim3(a.B), dim3(512), 0, st, a);
   }
   steps(1024);
-  return launch_k(beam_pick_kernel<T, VEC, 1024>, dim3(a.B), dim3(1024), 0, st, a);
+  return launch_k(beam_pick_kernel<T, 1024>, dim3(a.B), dim3(1024), 0, st, a);
 }
-template <typename T>
-cudaError_t beam_types(BeamArgs& a, int num_sm, cudaStream_t st) {
-  const bool vec = (((uintptr_t)a.logits | (uintptr_t)(a.row_stride * (int64_t)sizeof(T))) & 15) == 0;
-  return vec ? beam_launch<T, true>(a, num_sm, st) : beam_launch<T, false>(a, num_sm, st);
-}
-
 }  // namespace
 
 extern "C" {
@@ -650,7 +652,7 @@ extern "C" {
 int64_t sps_beam_select_workspace_bytes(int32_t B, int32_t W, int32_t V) {
   if (const char* why = bad_shape(B, W, V)) { no(SPS_EINVAL, why); return -1; }
   const int64_t rows = (int64_t)B * W;
-  return up(rows * (((int64_t)V + 127) / 128) * 4) + up(rows * max_parts(V) * 8);
+  return up(rows * most_segs(V) * 4) + up(rows * max_parts(V) * 8);
 }
 
 int sps_beam_select(const void* logits, int32_t dtype, int64_t row_stride, int32_t B, int32_t W, int32_t V, double temperature,
@@ -676,8 +678,8 @@ int sps_beam_select(const void* logits, int32_t dtype, int64_t row_stride, int32
   a.t = temperature; a.inv_t = 1.0 / temperature; a.inv_t32 = (float)a.inv_t; a.c = c; a.scores = scores; a.done = done; a.end_token = end_token;
   a.out_scores = out_scores; a.out_parents = out_parents; a.out_tokens = out_tokens; a.out_done = out_done;
   a.seg_max = (float*)workspace;
-  a.parts = (float2*)((char*)workspace + up((int64_t)B * W * (((int64_t)V + 127) / 128) * 4));
-  const cudaError_t e = dtype == 0 ? beam_types<float>(a, paged_sms(), (cudaStream_t)stream) : beam_types<__nv_bfloat16>(a, paged_sms(), (cudaStream_t)stream);
+  a.parts = (float2*)((char*)workspace + up((int64_t)B * W * most_segs(V) * 4));
+  const cudaError_t e = dtype == 0 ? beam_launch<float>(a, paged_sms(), (cudaStream_t)stream) : beam_launch<__nv_bfloat16>(a, paged_sms(), (cudaStream_t)stream);
   return e == cudaSuccess ? SPS_OK : no(SPS_ECUDA, cudaGetErrorString(e));
 }
 
