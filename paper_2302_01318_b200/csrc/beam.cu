@@ -24,7 +24,7 @@ namespace {
 
 constexpr int SCAN_THREADS = 256, SCAN_WARPS = 8, SCAN_SEGS = 4;       // segments of a group: a warp's load
 constexpr int ONE_RUN = 8, ONE_CTAS = 8, ONE_THREADS = 512, ONE_WARPS = ONE_CTAS * ONE_THREADS / 32;   // the kernel for little work
-constexpr int PICK_CAP = 1024, PICK_COUNTED = 128, PICK_SPLIT = 8, PICK_PER = 8;   // entries of a list, of one ranked by counting, threads that rank one; segments a thread holds
+constexpr int PICK_CAP = 1024, PICK_COUNTED = 128, PICK_SPLIT = 8, PICK_PER = 4;   // entries of a list, of one ranked by counting, threads that rank one; segments a thread holds
 constexpr int BEAM_MAX_B = 8192, BEAM_MAX_W = 128, BEAM_MAX_N = 128;
 
 struct BeamArgs {
@@ -41,7 +41,6 @@ struct BeamArgs {
   float* seg_max;            // [B W][n_seg]
   float2* parts;             // [B W][max_parts]: maximum, sum of exponentials
   int n_seg, groups, run, max_parts;   // segments and groups of a row, groups of a run, parts a row may have
-  int step_w, step_r;        // the picking CTA's threads over n_seg, and what is left
 };
 
 __device__ __forceinline__ float ex2(float x) {
@@ -249,6 +248,12 @@ __device__ __forceinline__ void beam_scan(const BeamArgs& a, int first_row, int 
   }
 }
 
+// log s to 2^-25, for s >= 2^-126: the fp32 function of a number next to 1, whose logarithm is below 0.35, and the exponent's share
+__device__ __forceinline__ double log_of(float s) {
+  const int i = __float_as_int(s), e = (i - 0x3f3504f3) >> 23;   // s 2^-e in 0.707 .. 1.414
+  return fma((double)e, 0.6931471805599453, (double)logf(__int_as_float(i - (e << 23))));
+}
+
 // Picking: candidates are (score, place) pairs, ties falling to the lowest place, so that all differ.  A list takes those that
 // reach a bound which at least N reach; only where more reach it than the list holds (ties by the hundred, rising rows) is the
 // stream taken in rounds, the list cut to its N best whenever it might overflow.
@@ -399,18 +404,23 @@ template <typename T, int THREADS>
 __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, const Beams& beams, const float* seg_max, const float2* all_parts) {
   constexpr int E = Logit<T>::E, SEG = 32 * E, WARPS = THREADS / 32, PER = PICK_PER;
   __shared__ double s_key[PICK_CAP], s_keep[BEAM_MAX_N], s_base[BEAM_MAX_W];
-  __shared__ float s_max[BEAM_MAX_W], s_base32[BEAM_MAX_W];
+  __shared__ float s_max[BEAM_MAX_W];
+  __shared__ float2 s_line[BEAM_MAX_W];   // a beam's score_of as a line in fp32: what a logit of 0 would have, and what that is off by
   __shared__ int s_thread[THREADS + WARPS], s_at[PICK_CAP], s_keep_at[BEAM_MAX_N], s_tops[BEAM_MAX_N + 2 * WARPS], s_count, s_bound;
   __shared__ int2 s_seg[BEAM_MAX_N];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, N = a.N;
   const Best best{s_key, s_at, s_keep, s_keep_at, &s_count, s_thread, s_tops, &s_bound};
   const int all = a.W * a.n_seg;
-  float held[PER];   // the first segments' maxima are on their way while the beams are looked at
+  // A warp takes the segments of one beam, 32 PER at a time; those of the first time round are on their way while the beams are looked at
+  const int chunks = (a.n_seg + 32 * PER - 1) / (32 * PER), units = a.W * chunks;
+  float held[PER];
+  auto load = [&](int unit) {
+    const int w = unit / chunks, r0 = (unit - w * chunks) * 32 * PER + lane;
 #pragma unroll
-  for (int j = 0; j < PER; ++j) {
-    const int i = tid + j * THREADS;
-    held[j] = i < all ? seg_max[i] : -INFINITY;
-  }
+    for (int j = 0; j < PER; ++j) held[j] = r0 + 32 * j < a.n_seg ? seg_max[(long long)w * a.n_seg + r0 + 32 * j] : -INFINITY;
+    return make_int2(w, r0);
+  };
+  int2 place = warp < units ? load(warp) : make_int2(0, 0);
   // a beam's part of its candidates' scores, -inf where it has none: c = base + (l - max) / T
   auto parts_of = [&](int w) { return ((first + w) * a.groups + a.groups - 1) / a.run - (first + w) * a.groups / a.run + 1; };
   float2 ahead = make_float2(-INFINITY, 0.f);   // (so is a warp's first part)
@@ -431,62 +441,40 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
     if (lane == 0) {
       const float score = beams.score[w];
       const bool live = !beams.done[w] && isfinite(score) && isfinite(m) && s > 0.f && s < INFINITY;   // (else its parts were not written)
-      const double base = live ? (double)score - log((double)s) : -INFINITY;
+      const double base = live ? (double)score - log_of(s) : -INFINITY;
+      const float at0 = (float)(base - (double)m * a.inv_t);
       s_base[w] = base;
-      s_base32[w] = (float)base;
       s_max[w] = m;
+      // (-inf: no beam; a start outside fp32's range: nothing is known of the scores)
+      s_line[w] = !live ? make_float2(-INFINITY, 0.f) : (isfinite(at0) ? make_float2(at0, fmaf(fabsf(at0), 4.7683716e-7f, 1e-36f)) : make_float2(0.f, INFINITY));
     }
   }
   if (tid == 0) s_count = 0;
   __syncthreads();
   auto score_of = [&](int w, float l) { return s_base[w] > -INFINITY ? s_base[w] + ((double)l - (double)s_max[w]) * a.inv_t : -INFINITY; };
-  // score_of in fp32, less and more than what its roundings (base, difference, 1 / T, product, sum: 2^-24 each of a term, once more
-  // of the sum) may come to; where the product leaves fp32's range, anything below the base
-  auto about = [&](int w, float l) {
-    const float base = s_base32[w], t = (l - s_max[w]) * a.inv_t32;
-    if (!(base > -INFINITY) || !(l > -INFINITY)) return make_float2(-INFINITY, -INFINITY);
-    const float v = base + t, e = fmaf(fabsf(base) + fabsf(t), 4.7683716e-7f, 1e-36f);   // 2^-21
-    return t > -INFINITY ? make_float2(v - e, v + e) : make_float2(-INFINITY, fmaf(fabsf(base), 4.7683716e-7f, base));
-  };
-  // The N best segments.  Scores are first taken in fp32 with what these may be off by, below and above: at least N reach the
-  // bound with what they have at least, and only those that may reach it are scored in 64 bits
-  const int w_first = tid / a.n_seg, r_first = tid - w_first * a.n_seg;
-  float high[PER], top = -INFINITY;
-  {
-    int w = w_first, r = r_first;
+  // The N best segments.  Scores are first taken in fp32, a line in the logit, with what their roundings may come to (the line's
+  // start, 1 / T, one of the fused operation: 2^-24 each of numbers no larger than the score's and the start's together): at
+  // least N reach the bound with the least that they may be, and only those that may reach it are scored in 64 bits
+  float top = -INFINITY;
+  for (int u = warp; u < units; u += WARPS) {
+    if (u != warp) place = load(u);
+    const float2 line = s_line[place.x];
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-      high[j] = -INFINITY;
-      if (j * THREADS >= all) continue;
-      if (tid + j * THREADS < all) {
-        const float2 v = about(w, held[j]);
-        high[j] = v.y;
-        top = fmaxf(top, v.x);
-      }
-      w += a.step_w; r += a.step_r;
-      if (r >= a.n_seg) { r -= a.n_seg; ++w; }
-    }
-    for (int i = tid + PER * THREADS; i < all; i += THREADS) {
-      top = fmaxf(top, about(w, seg_max[i]).x);
-      w += a.step_w; r += a.step_r;
-      if (r >= a.n_seg) { r -= a.n_seg; ++w; }
+      const float v = fmaf(held[j], a.inv_t32, line.x);
+      top = fmaxf(top, v - fmaf(fabsf(v), 4.7683716e-7f, line.y));   // (NaN, from a score of -inf, is left out)
     }
   }
   const float least = best_bound<THREADS>(best, top, N);
-  {
-    int w = w_first, r = r_first;
+  for (int u = warp; u < units; u += WARPS) {
+    if (units > WARPS) place = load(u);
+    const float2 line = s_line[place.x];
+    if (!(line.x > -INFINITY)) continue;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
-      if (j * THREADS >= all) continue;
-      if (high[j] >= least && high[j] > -INFINITY) best_push(best, score_of(w, held[j]), tid + j * THREADS);
-      w += a.step_w; r += a.step_r;
-      if (r >= a.n_seg) { r -= a.n_seg; ++w; }
-    }
-    for (int i = tid + PER * THREADS; i < all; i += THREADS) {
-      const float l = seg_max[i], h = about(w, l).y;
-      if (h >= least && h > -INFINITY) best_push(best, score_of(w, l), i);
-      w += a.step_w; r += a.step_r;
-      if (r >= a.n_seg) { r -= a.n_seg; ++w; }
+      const float v = fmaf(held[j], a.inv_t32, line.x);
+      // (what left fp32's range may be anything)
+      if (held[j] > -INFINITY && !(v + fmaf(fabsf(v), 4.7683716e-7f, line.y) < least)) best_push(best, score_of(place.x, held[j]), place.x * a.n_seg + place.y + 32 * j);
     }
   }
   __syncthreads();
@@ -624,13 +612,11 @@ cudaError_t beam_launch(BeamArgs& a, int num_sm, cudaStream_t st) {
   a.n_seg = (a.V + (aligned ? 0 : E - 1) + SEG - 1) / SEG;
   a.groups = (a.n_seg + SCAN_SEGS - 1) / SCAN_SEGS;
   a.max_parts = max_parts(a.V);
-  auto steps = [&](int threads) { a.step_w = threads / a.n_seg; a.step_r = threads % a.n_seg; };
   const long long all = (long long)a.B * a.W * a.groups, warps = (long long)num_sm * 4 * SCAN_WARPS;
   // little work, no more than ONE_RUN groups to a warp and clusters that fit beside one another: one launch
   if ((long long)a.W * a.groups <= ONE_RUN * ONE_WARPS && a.B * ONE_CTAS <= num_sm) {
     a.run = (a.W * a.groups + ONE_WARPS - 1) / ONE_WARPS;
     a.max_parts = (a.groups + a.run - 1) / a.run + 1;   // W of them: ONE_WARPS + 2 W at most
-    steps(ONE_THREADS);
     return launch_k(beam_one_kernel<T>, dim3(a.B * ONE_CTAS), dim3(ONE_THREADS), 0, st, a);
   }
   a.run = (int)((all + warps - 1) / warps);
@@ -638,11 +624,7 @@ cudaError_t beam_launch(BeamArgs& a, int num_sm, cudaStream_t st) {
   cudaError_t e = launch_k(beam_scan_kernel<T>, dim3((unsigned)((runs + SCAN_WARPS - 1) / SCAN_WARPS)), dim3(SCAN_THREADS), 0, st, a);
   if (e != cudaSuccess) return e;
   // a small CTA for few segments: what each warp does for itself then costs less than the walk over them
-  if ((long long)a.W * a.n_seg <= 2048) {
-    steps(512);
-    return launch_k(beam_pick_kernel<T, 512>, dim3(a.B), dim3(512), 0, st, a);
-  }
-  steps(1024);
+  if ((long long)a.W * a.n_seg <= 2048) return launch_k(beam_pick_kernel<T, 512>, dim3(a.B), dim3(512), 0, st, a);
   return launch_k(beam_pick_kernel<T, 1024>, dim3(a.B), dim3(1024), 0, st, a);
 }
 }  // namespace

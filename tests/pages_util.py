@@ -161,7 +161,7 @@ def select64(logits, scores, done, end, N, T):
         logp = below - torch.log(torch.exp(below).sum())
         c = s + logp
         far = float((torch.exp(logp) * (-below).clamp(max=1e30)).sum())
-        tols[-1] = (6 * far + 8 + logits.shape[1] / 256 + 32 + 13) * 2.0 ** -24
+        tols[-1] = (6 * far + 8 + logits.shape[1] / 256 + 32 + 13 + 1) * 2.0 ** -24
         k = min(N, x.shape[0])
         cut = c.topk(k).values[-1]
         at = ((c >= cut) & (x > -math.inf)).nonzero()[:, 0]

@@ -203,6 +203,13 @@ def test_large_and_small_logits():
         run_and_check(normal((2, 2, 3000), seed=10, std=scale), beams(2, 2), N=5)
 
 
+@pytest.mark.parametrize("std,T", [(100.0, 1e-36), (100.0, 1e-30), (3.0, 1e-3), (3.0, 1e30), (1e30, 1e30)])
+def test_temperatures_at_both_ends(std, T):
+    """Scaled logits beyond fp32's range, and logits that temperature levels."""
+    run_and_check(normal((3, 4, 3000), seed=13, std=std), beams(3, 4), N=7, T=T)
+    run_and_check(normal((30, 4, 3000), seed=14, std=std), beams(30, 4), N=7, T=T)
+
+
 def test_in_place_scores_and_done():
     B, W, V = 5, 4, 3000
     x, s = normal((B, W, V), seed=11), beams(B, W)
