@@ -15,8 +15,8 @@ namespace cg = cooperative_groups;
 // segment of 512 bytes.  A row's order is its logits', so the N best elements lie in the N segments whose maxima score
 // best (ties to the lower segment: any element outside has N better ones in them) -- whatever the numbers are.  The pick, a
 // CTA per sequence, finds those segments (or a few more), reads them again (N x 512 bytes, from L2) and picks the N best elements.
-// The scan is bound by HBM with many rows; the pick by latency, a chain of a dozen short steps between barriers (7 us): 256 rows of
-// 131071 in bf16 (67 MB) 23 us, 512 of 32000 in fp32 20 us, of which the bytes' floor is 10.
+// The scan is bound by HBM with many rows; the pick by latency, a chain of a dozen short steps between barriers (6 us): 256 rows of
+// 131071 in bf16 (67 MB) 22.5 us, 512 of 32000 in fp32 20 us, of which the bytes' floor is 10.
 // Candidates are compared in 64 bits, from exact logits and a sum of fp32 exponentials (relative error about 2^-22), so that
 // far scores keep the order of their last bits; results are rounded once.
 // ------------------------------------------------------------------------------------------------------------------
@@ -573,8 +573,8 @@ __global__ void __launch_bounds__(THREADS) beam_pick_kernel(const __grid_constan
   beam_pick<T, THREADS>(a, blockIdx.x, row, s_beams, a.seg_max + (long long)row * a.n_seg, a.parts + (long long)row * a.max_parts);
 }
 // Both for little work, a cluster to a sequence: what the scan finds goes straight to the shared memory of the CTA that picks.
-// One prompt of 4 x 32000: 8.6 us as two launches in a graph and 16 one by one (the host's), 8.9 and 11.5 this way (through L2 9.9
-// and 12); eight of 8 x 32000 14.6 and 16.6 against 11.9 and 12.2.
+// One prompt of 4 x 32000: 8.6 us as two launches in a graph and 16 one by one (the host's), 9.0 and 11.5 this way (1 more through
+// L2); eight of 8 x 32000 14.6 and 16.6 against 12.1 and 12.6.
 template <typename T>
 __global__ void __cluster_dims__(ONE_CTAS, 1, 1) __launch_bounds__(ONE_THREADS, 2) beam_one_kernel(const __grid_constant__ BeamArgs a) {
   __shared__ Beams s_beams;
