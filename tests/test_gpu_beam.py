@@ -210,6 +210,26 @@ def test_temperatures_at_both_ends(std, T):
     run_and_check(normal((30, 4, 3000), seed=14, std=std), beams(30, 4), N=7, T=T)
 
 
+def test_rows_that_lie_far_apart():
+    """Offsets that pass 2^31 elements."""
+    store = torch.empty(2 ** 31 + 4096, dtype=BF16, device=DEV)
+    x = store.as_strided((1, 3, 2000), (3 * 2 ** 30, 2 ** 30, 1))
+    x.copy_(normal((1, 3, 2000), BF16, 17))
+    run_and_check(x, beams(1, 3), N=6)
+
+
+@pytest.mark.skipif(torch.cuda.device_count() < 2, reason="needs two visible GPUs")
+def test_on_a_device_that_is_not_the_current_one():
+    x, s = normal((2, 3, 4000), seed=18), beams(2, 3)
+    want = run_select(x, s, N=4)
+    o = [torch.zeros((2, 4), device="cuda:1")] + [torch.zeros((2, 4), dtype=I32, device="cuda:1") for _ in range(2)]
+    ws = torch.zeros(sps.sps_beam_select_workspace_bytes(2, 3, 4000), dtype=torch.uint8, device="cuda:1")
+    sps.sps_beam_select(x.to("cuda:1"), s.to("cuda:1"), *o, ws)
+    assert all(torch.equal(a, b.to(DEV)) for a, b in zip(want, o))
+    with pytest.raises(ValueError):
+        sps.sps_beam_select(x, s, *o, ws)
+
+
 def test_in_place_scores_and_done():
     B, W, V = 5, 4, 3000
     x, s = normal((B, W, V), seed=11), beams(B, W)

@@ -109,6 +109,33 @@ def test_tables_without_rows(n_pages):
     assert int(d.pool.status) == sps.PAGED_BAD_LENGTH and d.t.held.tolist() == [0, 0, 0]
 
 
+@pytest.mark.parametrize("n_pages", [60, 30000])
+def test_want_may_be_the_lengths_themselves(n_pages):
+    """What was reserved ahead is given up: the lengths are both kept and wanted."""
+    m, d = grown(n_pages, 8, [60, 41, 7, 0], ld=16)
+    m.reserve([90, 41, 50, 3])
+    d.reserve([90, 41, 50, 3])
+    m.reserve([60, 41, 7, 0])
+    sps.sps_paged_reserve(d.pool, d.t, d.t.lens, d.moves, d.ws)
+    d.check(m)
+
+
+@pytest.mark.skipif(torch.cuda.device_count() < 2, reason="needs two visible GPUs")
+def test_on_a_device_that_is_not_the_current_one():
+    m, d = grown(64, 8, [21, 13], ld=9)
+    to = lambda t: t.to("cuda:1")
+    pool = sps.PagePool(to(d.pool.refs), 8)
+    tables = [sps.PageTable(to(t.pages), to(t.held), to(t.lens)) for t in d.tables]
+    moves, ws = sps.PageMoves(to(d.moves.list), to(d.moves.count)), to(d.ws)
+    sps.sps_paged_fork(pool, tables[0], tables[1], to(ints([1, 1])))
+    sps.sps_paged_reserve(pool, tables[1], to(ints([14, 20])), moves, ws)
+    m.fork([1, 1])
+    want, _ = m.reserve([14, 20])
+    assert moves.list[:int(moves.count)].tolist() == want and pool.refs.tolist() == m.refs
+    with pytest.raises(ValueError):
+        sps.sps_paged_fork(d.pool, tables[0], d.tables[1], ints([1, 1]))
+
+
 def test_two_pools_at_once_on_streams_of_their_own():
     ms = [grown(n, 8, [60, 41, 7, 0], ld=16, seed=n) for n in (200, 40000)]
     streams = [torch.cuda.Stream() for _ in ms]
