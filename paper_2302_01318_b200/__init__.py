@@ -761,6 +761,9 @@ def sps_beam_select_workspace_bytes(B, W, V):
     return n
 
 
+_beam_bytes = {}   # the workspace that a shape needs
+
+
 def sps_beam_select(logits, scores, out_scores, out_parents, out_tokens, workspace, done=None, out_done=None, end_token=-1,
                     temperature=1.0, stream=None):
     """The N best continuations of each sequence's beams.  logits CUDA [B, W, V], fp32 or bf16 (rows of any one stride); scores CUDA
@@ -775,26 +778,32 @@ def sps_beam_select(logits, scores, out_scores, out_parents, out_tokens, workspa
     sb, sw, sv = logits.stride()
     if (sv != 1 and V > 1) or (W > 1 and B > 1 and sb != W * sw):
         raise ValueError("the rows of logits must be contiguous, one stride apart")
-    out = out_scores.shape
+    beams, out = (B, W), out_scores.shape
     ints, f32 = _Torch.int32, _Torch.float32
-    if scores.dtype is not f32 or scores.shape != shape[:2] or not scores.is_contiguous() or scores.get_device() != index:
-        raise ValueError("scores is contiguous float32 [B, W] on the logits' device")
-    if out_scores.dtype is not f32 or len(out) != 2 or out[0] != B or not out_scores.is_contiguous() or out_scores.get_device() != index:
-        raise ValueError("out_scores is contiguous float32 [B, N] on the logits' device")
-    if out_parents.dtype is not ints or out_parents.shape != out or not out_parents.is_contiguous() or out_parents.get_device() != index or \
-            out_tokens.dtype is not ints or out_tokens.shape != out or not out_tokens.is_contiguous() or out_tokens.get_device() != index:
-        raise ValueError("out_parents and out_tokens are contiguous int32 [B, N] on the logits' device")
+    if scores.dtype is not f32 or scores.shape != beams or out_scores.dtype is not f32 or len(out) != 2 or out[0] != B or \
+            not (scores.is_contiguous() and out_scores.is_contiguous()):
+        raise ValueError("scores and out_scores are contiguous float32 [B, W] and [B, N]")
+    if out_parents.dtype is not ints or out_parents.shape != out or out_tokens.dtype is not ints or out_tokens.shape != out or \
+            not (out_parents.is_contiguous() and out_tokens.is_contiguous()):
+        raise ValueError("out_parents and out_tokens are contiguous int32 [B, N]")
     done_p = over_p = None
     if done is not None:
-        if done.dtype is not ints or done.shape != shape[:2] or not done.is_contiguous() or done.get_device() != index:
+        if done.dtype is not ints or done.shape != beams or not done.is_contiguous() or done.get_device() != index:
             raise ValueError("done is contiguous int32 [B, W] on the logits' device")
         done_p = done.data_ptr()
     if out_done is not None:
         if out_done.dtype is not ints or out_done.shape != out or not out_done.is_contiguous() or out_done.get_device() != index:
             raise ValueError("out_done is contiguous int32 [B, N] on the logits' device")
         over_p = out_done.data_ptr()
+    if not (scores.get_device() == out_scores.get_device() == out_parents.get_device() == out_tokens.get_device() == workspace.get_device() == index):
+        raise ValueError("all tensors must be on one CUDA device")
     L = lib()
-    if workspace.nbytes < L.sps_beam_select_workspace_bytes(B, W, V) or workspace.get_device() != index or not workspace.is_contiguous():
-        raise ValueError("workspace: on the logits' device, contiguous, of sps_beam_select_workspace_bytes")
+    need = _beam_bytes.get((B, W, V))
+    if need is None:
+        if len(_beam_bytes) > 1000:
+            _beam_bytes.clear()
+        need = _beam_bytes[(B, W, V)] = L.sps_beam_select_workspace_bytes(B, W, V)
+    if workspace.nbytes < need or not workspace.is_contiguous():
+        raise ValueError("workspace not contiguous, or smaller than sps_beam_select_workspace_bytes")
     _on(index, L.sps_beam_select, stream, logits.data_ptr(), code, sw if W > 1 else sb, B, W, V, temperature, scores.data_ptr(), done_p, end_token, out[1],
         out_scores.data_ptr(), out_parents.data_ptr(), out_tokens.data_ptr(), over_p, workspace.data_ptr())
