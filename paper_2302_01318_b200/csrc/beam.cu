@@ -23,7 +23,7 @@ namespace cg = cooperative_groups;
 namespace {
 
 constexpr int SCAN_THREADS = 256, SCAN_WARPS = 8, SCAN_SEGS = 4;       // segments of a group: a warp's load
-constexpr int ONE_RUN = 8, ONE_CTAS = 8, ONE_THREADS = 512, ONE_WARPS = ONE_CTAS * ONE_THREADS / 32;   // the kernel for little work
+constexpr int ONE_RUN = 4, ONE_CTAS = 8, ONE_THREADS = 1024, ONE_PICK = 512, ONE_WARPS = ONE_CTAS * ONE_THREADS / 32;   // the kernel for little work; ONE_PICK: threads that pick
 constexpr int PICK_CAP = 1024, PICK_COUNTED = 128, PICK_SPLIT = 8, PICK_PER = 4;   // entries of a list, of one ranked by counting, threads that rank one; segments a thread holds
 constexpr int BEAM_MAX_B = 8192, BEAM_MAX_W = 128, BEAM_MAX_N = 128;
 
@@ -257,6 +257,8 @@ __device__ __forceinline__ double log_of(float s) {
 // Picking: candidates are (score, place) pairs, ties falling to the lowest place, so that all differ.  A list takes those that
 // reach a bound which at least N reach; only where more reach it than the list holds (ties by the hundred, rising rows) is the
 // stream taken in rounds, the list cut to its N best whenever it might overflow.
+template <int THREADS>
+__device__ __forceinline__ void pick_sync() { asm volatile("bar.sync 1, %0;" ::"n"(THREADS) : "memory"); }   // of the threads that pick
 struct Best {
   double* key;        // [PICK_CAP]
   int* at;
@@ -278,14 +280,14 @@ __device__ __forceinline__ float best_bound(const Best& b, float top, int N) {
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, k = (N + WARPS - 1) / WARPS + 1, mine_at = lane * WARPS + warp;
   b.thread[tid + tid / 32] = ordered(top);
   if (tid == 0) *b.bound = INT_MIN;
-  __syncthreads();
+  pick_sync<THREADS>();
   int mine = b.thread[mine_at + mine_at / 32];
   for (int j = 0; j < k; ++j) {
     const int v = __reduce_max_sync(0xffffffffu, mine);
     if (lane == 0) b.tops[warp * k + j] = v;
     if (__ffs(__ballot_sync(0xffffffffu, mine == v)) - 1 == lane) mine = INT_MIN;
   }
-  __syncthreads();
+  pick_sync<THREADS>();
   for (int i = tid; i < k * WARPS; i += THREADS) {
     const int v = b.tops[i];
     int r = 0;
@@ -293,7 +295,7 @@ __device__ __forceinline__ float best_bound(const Best& b, float top, int N) {
     for (int j = 0; j < k * WARPS; ++j) r += b.tops[j] > v || (b.tops[j] == v && j < i);
     if (r == N - 1) *b.bound = v;
   }
-  __syncthreads();
+  pick_sync<THREADS>();
   return unordered(max(*b.bound, ordered(-INFINITY)));
 }
 
@@ -320,11 +322,11 @@ __device__ __forceinline__ int best_rank(const Best& b, int N) {
     }
     const float least = best_bound<THREADS>(b, top, N);
     if (tid == 0) *b.count = 0;
-    __syncthreads();
+    pick_sync<THREADS>();
 #pragma unroll
     for (int j = 0; j < PER; ++j)
       if (k[j] > -INFINITY && k[j] >= (double)least) best_push(b, k[j], p[j]);
-    __syncthreads();
+    pick_sync<THREADS>();
     n = *b.count;
   }
   if (n <= 2 * PICK_COUNTED) {
@@ -345,7 +347,7 @@ __device__ __forceinline__ int best_rank(const Best& b, int N) {
     int size = 4 * PICK_COUNTED;
     while (size < n) size *= 2;
     for (int i = n + tid; i < size; i += THREADS) { b.key[i] = -INFINITY; b.at[i] = INT_MAX; }
-    __syncthreads();
+    pick_sync<THREADS>();
     for (int run = 2; run <= size; run *= 2)
       for (int step = run / 2; step > 0; step /= 2) {
         if (tid < size / 2) {
@@ -355,24 +357,24 @@ __device__ __forceinline__ int best_rank(const Best& b, int N) {
           if (better(kj, aj, ki, ai) == ((i & run) == 0)) { b.key[i] = kj; b.at[i] = aj; b.key[j] = ki; b.at[j] = ai; }
         }
         // the next step's pairs lie within what a warp has, unless its step is above 32
-        if (step > 32 || (step == 1 && run > 32)) __syncthreads();
+        if (step > 32 || (step == 1 && run > 32)) pick_sync<THREADS>();
         else __syncwarp();
       }
-    __syncthreads();
+    pick_sync<THREADS>();
     for (int i = tid; i < N; i += THREADS) { b.keep_key[i] = b.key[i]; b.keep_at[i] = b.at[i]; }   // (N <= PICK_COUNTED < n)
   }
-  __syncthreads();
+  pick_sync<THREADS>();
   return found;
 }
 // the N best of item(0 .. all - 1) -> (key, place), -inf keys left out, in rounds
 template <int THREADS, class Item>
 __device__ __noinline__ int best_rounds(const Best& b, int N, int all, Item item) {
   int have = 0;
-  __syncthreads();
+  pick_sync<THREADS>();
   for (int i0 = 0; i0 < all; i0 += PICK_CAP - BEAM_MAX_N) {
     for (int i = threadIdx.x; i < have; i += THREADS) { b.key[i] = b.keep_key[i]; b.at[i] = b.keep_at[i]; }
     if (threadIdx.x == 0) *b.count = have;
-    __syncthreads();
+    pick_sync<THREADS>();
     const double bound = have == N ? b.key[N - 1] : -INFINITY;
     const int bound_at = have == N ? b.at[N - 1] : 0;
     for (int i = i0 + threadIdx.x; i < min(i0 + PICK_CAP - BEAM_MAX_N, all); i += THREADS) {
@@ -380,7 +382,7 @@ __device__ __noinline__ int best_rounds(const Best& b, int N, int all, Item item
       const double k = item(i, &at);
       if (better(k, at, bound, bound_at)) best_push(b, k, at);
     }
-    __syncthreads();
+    pick_sync<THREADS>();
     have = best_rank<THREADS>(b, N);
   }
   return have;
@@ -425,7 +427,7 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
   auto parts_of = [&](int w) { return ((first + w) * a.groups + a.groups - 1) / a.run - (first + w) * a.groups / a.run + 1; };
   float2 ahead = make_float2(-INFINITY, 0.f);   // (so is a warp's first part)
   if (warp < a.W && lane < a.max_parts) ahead = all_parts[(long long)warp * a.max_parts + lane];   // (those behind its own are not used)
-  __syncthreads();   // (`beams` is there)
+  pick_sync<THREADS>();   // (`beams` is there)
   for (int w = warp; w < a.W; w += WARPS) {
     const float2* parts = all_parts + (long long)w * a.max_parts;
     const int n_parts = parts_of(w);
@@ -450,7 +452,7 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
     }
   }
   if (tid == 0) s_count = 0;
-  __syncthreads();
+  pick_sync<THREADS>();
   auto score_of = [&](int w, float l) { return s_base[w] > -INFINITY ? s_base[w] + ((double)l - (double)s_max[w]) * a.inv_t : -INFINITY; };
   // The N best segments.  Scores are first taken in fp32, a line in the logit, with what their roundings may come to (the line's
   // start, 1 / T, one of the fused operation: 2^-24 each of numbers no larger than the score's and the start's together): at
@@ -477,7 +479,7 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
       if (held[j] > -INFINITY && !(v + fmaf(fabsf(v), 4.7683716e-7f, line.y) < least)) best_push(best, score_of(place.x, held[j]), place.x * a.n_seg + place.y + 32 * j);
     }
   }
-  __syncthreads();
+  pick_sync<THREADS>();
   // few more than N: all are read, else the N best
   int segs = s_count;
   const bool all_read = segs <= BEAM_MAX_N;
@@ -492,9 +494,9 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
     const int w = from[i] / a.n_seg;
     s_seg[i] = make_int2(w, (from[i] - w * a.n_seg) * SEG);
   }
-  __syncthreads();
+  pick_sync<THREADS>();
   if (tid == 0) s_count = 0;
-  __syncthreads();
+  pick_sync<THREADS>();
   // their elements that reach the bound, and the beams that are done
   auto ended = [&](int w, int* at) {            // beam w's candidate, if it is done
     const float s = beams.done[w] ? beams.score[w] : -INFINITY;
@@ -533,7 +535,7 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
     const double v = ended(tid, &at);
     if (v >= bound && v > -INFINITY) best_push(best, v, at);
   }
-  __syncthreads();
+  pick_sync<THREADS>();
   auto element = [&](int i, int* at) {          // element i of the segments, one behind the other, then the done beams
     if (i >= segs * SEG) return ended(i - segs * SEG, at);
     const int2 sg = s_seg[i / SEG];
@@ -572,11 +574,11 @@ __global__ void __launch_bounds__(THREADS) beam_pick_kernel(const __grid_constan
   beams_load<THREADS>(a, blockIdx.x, s_beams);
   beam_pick<T, THREADS>(a, blockIdx.x, row, s_beams, a.seg_max + (long long)row * a.n_seg, a.parts + (long long)row * a.max_parts);
 }
-// Both for little work, a cluster to a sequence: what the scan finds goes straight to the shared memory of the CTA that picks.
-// One prompt of 4 x 32000: 8.6 us as two launches in a graph and 16 one by one (the host's), 9.0 and 11.5 this way (1 more through
-// L2); eight of 8 x 32000 14.6 and 16.6 against 12.1 and 12.6.
+// Both for little work, a cluster to a sequence: what the scan finds goes straight to the shared memory of the CTA that picks (half
+// of its threads do: the pick's steps cost by the warp).  One prompt of 4 x 32000: 8.6 us as two launches in a graph and 16 one by
+// one (the host's), 8.6 and 10.5 this way; eight of 8 x 32000 14.6 and 16.6 against 10.6 and 11.3.
 template <typename T>
-__global__ void __cluster_dims__(ONE_CTAS, 1, 1) __launch_bounds__(ONE_THREADS, 2) beam_one_kernel(const __grid_constant__ BeamArgs a) {
+__global__ void __cluster_dims__(ONE_CTAS, 1, 1) __launch_bounds__(ONE_THREADS) beam_one_kernel(const __grid_constant__ BeamArgs a) {
   __shared__ Beams s_beams;
   __shared__ float s_segs[ONE_RUN * ONE_WARPS * SCAN_SEGS];
   __shared__ float2 s_parts[ONE_WARPS + 2 * BEAM_MAX_W];
@@ -588,7 +590,7 @@ __global__ void __cluster_dims__(ONE_CTAS, 1, 1) __launch_bounds__(ONE_THREADS, 
   if (rank == 0) beams_load<ONE_THREADS>(a, b, s_beams);
   beam_scan<T>(a, b * a.W, a.W, (threadIdx.x >> 5) * ONE_CTAS + rank, cl.map_shared_rank(s_segs, 0), cl.map_shared_rank(s_parts, 0));
   cl.sync();
-  if (rank == 0) beam_pick<T, ONE_THREADS>(a, b, 0, s_beams, s_segs, s_parts);
+  if (rank == 0 && threadIdx.x < ONE_PICK) beam_pick<T, ONE_PICK>(a, b, 0, s_beams, s_segs, s_parts);
 }
 
 int no(int code, const char* msg) {
