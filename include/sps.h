@@ -488,8 +488,8 @@ int64_t sps_paged_attention_workspace_bytes(const sps_paged_cache* cache, int32_
  * sequence; these calls serve programs that decode several continuations of a prompt, admit and drop sequences, and roll
  * rejected drafts back.  One table serves all layers: page p is page p of every layer's cache.
  *
- * All calls only enqueue on `stream` (one kernel each, sps_paged_compact of a large pool or table two, sps_paged_copy one per 64 layers), read and write
- * their state on the device -- so that a captured call can be replayed -- and allocate nothing.  A pool's, a table's or a
+ * All calls only enqueue on `stream` (one kernel each; sps_paged_compact of a large pool or table two, sps_paged_copy one per 64
+ * layers, sps_beam_select of much work two), read and write their state on the device -- so that a captured call can be replayed -- and allocate nothing.  A pool's, a table's or a
  * workspace's calls must not run at the same time.  Results do not depend on timing: of free pages the lowest are taken, rows are
  * served in their order.  What does not fit is skipped, never followed, and sets a bit of the pool's status: page numbers
  * outside the pool (SPS_PAGED_BAD_PAGE; a fork and a compaction keep such an entry), counts outside their row
@@ -498,7 +498,7 @@ int64_t sps_paged_attention_workspace_bytes(const sps_paged_cache* cache, int32_
 #define SPS_PAGED_NO_PAGE 8    /* more bits of *status: a row was left without the pages that it wanted */
 #define SPS_PAGED_BAD_ROW 16
 typedef struct {
-  int32_t* refs;     /* device [n_pages]: table rows that hold the page, 0 = free           */
+  int32_t* refs;     /* device [n_pages]: table rows that hold the page, 0 = free (all zeros: an empty pool) */
   int32_t* status;   /* device [1], SPS_PAGED_* bits, never cleared by the calls; may be NULL */
   int32_t n_pages, page_size;   /* n_pages: up to 2^20; page_size: tokens, a power of two, 8 .. 512 */
 } sps_page_pool;
@@ -532,31 +532,32 @@ int sps_paged_fork(const sps_page_pool* pool, const sps_page_table* src, const s
  *   is added to `moves` -- unless all who hold it exchange it in this call: then the first of them keeps it;
  *   fresh pages are appended up to ceil(want / page_size) entries.
  * Fresh pages are the free ones in ascending order.  A row whose pages are no longer to be had gets none of them, nor does any
- * row behind it that needs some: it keeps its n tokens, held tells so, and SPS_PAGED_NO_PAGE is set.  held and len (= n) are
- * written.  Before the row's new tokens are appended, the moves are to be carried out (sps_paged_copy).
- * moves->capacity >= B.  workspace: device scratch of sps_paged_pool_workspace_bytes(n_pages) bytes, 16-byte aligned, zero-filled
+ * row behind it that needs some: it keeps its n tokens and the pages that they are in, and SPS_PAGED_NO_PAGE is set.  held
+ * and len (= n) are written.  room: device [B], may be NULL (and may be want): the tokens that the row may be written up to -- want,
+ * or n where it went without (its last page may then be shared still: nothing is to be appended to it).  Before new tokens
+ * are appended, the moves are to be carried out (sps_paged_copy).  moves->capacity >= B.  workspace: device scratch of sps_paged_pool_workspace_bytes(n_pages) bytes, 16-byte aligned, zero-filled
  * once before its first use (every call leaves it ready for the next). */
-int sps_paged_reserve(const sps_page_pool* pool, const sps_page_table* table, const int32_t* want, const sps_page_moves* moves, void* workspace,
-                      void* stream);
+int sps_paged_reserve(const sps_page_pool* pool, const sps_page_table* table, const int32_t* want, int32_t* room, const sps_page_moves* moves,
+                      void* workspace, void* stream);
 int64_t sps_paged_pool_workspace_bytes(int32_t n_pages);
 
 /* Compact: with U pages in use, those numbered U and above move to the free ones below U, the i-th such page to the i-th such
  * hole, at most moves->capacity of them, lowest first; afterwards (without that limit) pages 0 .. U - 1 are in use and the rest
  * of the pool can be given back.  src must be the only table that holds pages of the pool.  dst receives the table, refs_out
- * (device [n_pages]) the references, `moves` the copies to carry out, whole pages.  In place: dst may share src's arrays (the same ld), refs_out may be
- * pool->refs; else src and pool->refs stay as they are.  workspace: as for sps_paged_reserve (the same one will do). */
+ * (device [n_pages]) the references, `moves` the copies to carry out, whole pages.  In place: dst may share src's
+ * arrays (the same ld), refs_out may be pool->refs; else src and pool->refs stay as they are.  workspace: as for sps_paged_reserve (the same one will do). */
 int sps_paged_compact(const sps_page_pool* pool, const sps_page_table* src, const sps_page_table* dst, int32_t* refs_out, const sps_page_moves* moves,
                       void* workspace, void* stream);
 
-/* Copy: the listed pages' first slots, in the keys and values of every layer; slots behind them are left as they were.  layers: HOST array of n_layers caches of
- * one shape, dtype and strides.  Items of the list outside the caches are skipped, slots clipped to page_size.  No page may be
+/* Copy: the listed pages' first slots, in the keys and values of every layer; slots behind them are left as they were.  layers: HOST
+ * array of n_layers caches of one shape, dtype and strides.  Items of the list outside the caches are skipped, slots clipped to page_size.  No page may be
  * the destination of two items, or a source and a destination (what the calls above list is of that kind). */
 int sps_paged_copy(const sps_paged_cache* layers, int32_t n_layers, const sps_page_moves* moves, void* stream);
 
 /* The selection of a beam step: for each of B sequences the N best continuations of its W beams, best first,
  *   c[w, v] = scores[w] + logits[w, v] / T - log sum_u exp(logits[w, u] / T),
- * equal ones in the order of w V + v.  The paper samples; this is the search its Related Work's decoding methods set beside it, over the
- * same logits, and with sps_paged_fork over the same cache.
+ * equal ones in the order of w V + v.  (The paper samples; beam search is another way to decode from the same logits, and with
+ * sps_paged_fork over the same cache.)
  *   logits        device, dtype 0 fp32 / 1 bf16: row b W + w at logits + (b W + w) row_stride (elements), V of them; any alignment
  *                 of the rows
  *   scores        device fp32 [B][W]: log-probability of each beam so far; -inf: there is no such beam (the first step after

@@ -149,7 +149,7 @@ def lib():
         L.sps_paged_attention_workspace_bytes.argtypes = [vp, i32, i32]
         L.sps_paged_attention_workspace_bytes.restype = i64
         L.sps_paged_fork.argtypes = [vp, vp, vp, vp, vp]
-        L.sps_paged_reserve.argtypes = [vp, vp, vp, vp, vp, vp]
+        L.sps_paged_reserve.argtypes = [vp, vp, vp, vp, vp, vp, vp]
         L.sps_paged_pool_workspace_bytes.argtypes = [i32]
         L.sps_paged_pool_workspace_bytes.restype = i64
         L.sps_paged_compact.argtypes = [vp, vp, vp, vp, vp, vp, vp]
@@ -730,12 +730,14 @@ def sps_paged_fork(pool, src, dst, parents, stream=None):
     _on(index, lib().sps_paged_fork, stream, pool._p, src._p, dst._p, _ints(parents, (dst.B,), index, "parents"))
 
 
-def sps_paged_reserve(pool, table, want, moves, workspace, stream=None):
-    """Every row keeps min(len, want) tokens and gets room for want of them; `moves` are then to be copied."""
+def sps_paged_reserve(pool, table, want, moves, workspace, room=None, stream=None):
+    """Every row keeps min(len, want) tokens and gets room for want of them; `moves` are then to be copied.  room (CUDA int32 [B]): the
+    tokens that each row may then be written up to, want or, where the pool ran out, those kept."""
     index = pool.index
     if table.index != index or moves.index != index:
         raise ValueError("all tensors must be on one CUDA device")
-    _on(index, lib().sps_paged_reserve, stream, pool._p, table._p, _ints(want, (table.B,), index, "want"), moves._p, _pool_workspace(pool, workspace))
+    _on(index, lib().sps_paged_reserve, stream, pool._p, table._p, _ints(want, (table.B,), index, "want"),
+        _ints(room, (table.B,), index, "room") if room is not None else None, moves._p, _pool_workspace(pool, workspace))
 
 
 def sps_paged_compact(pool, src, dst, refs_out, moves, workspace, stream=None):

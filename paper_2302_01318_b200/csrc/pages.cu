@@ -236,12 +236,13 @@ struct ReserveArgs {
   Pool pool;
   Table t;
   const int32_t* want;
+  int32_t* room;              // or null
   Moves moves;
   int32_t *writers, *first;   // [n_pages], zero
   int32_t* fresh;             // [n_pages]: the pages handed out
 };
 
-struct RowPlan { int n, keep, to, give, q; };   // tokens and pages kept, pages wanted, entries given up, the page about to be written (-1: none)
+struct RowPlan { int n, keep, want, to, give, q; };   // tokens and pages kept, tokens and pages wanted, entries given up, the page about to be written (-1: none)
 __device__ __forceinline__ RowPlan row_plan(const ReserveArgs& a, int b) {
   RowPlan r;
   const int held0 = a.t.held[b], len0 = a.t.len[b], want0 = a.want[b];
@@ -250,6 +251,7 @@ __device__ __forceinline__ RowPlan row_plan(const ReserveArgs& a, int b) {
   if (held != held0 || len0 > room || want0 > cap) paged_flag(a.pool.status, SPS_PAGED_BAD_LENGTH);
   r.n = min(min(max(len0, 0), room), want);
   r.keep = (r.n + a.pool.page_size - 1) >> a.pool.page_shift;
+  r.want = want;
   r.to = (want + a.pool.page_size - 1) >> a.pool.page_shift;
   r.give = held - r.keep;
   r.q = -1;
@@ -274,7 +276,7 @@ __global__ void __launch_bounds__(POOL_THREADS) reserve_kernel(const __grid_cons
   pdl_wait();
 
   // (1) the row's plan, and what it gives up
-  const auto [n, keep, to, give, q] = row ? row_plan(a, b) : RowPlan{0, 0, 0, 0, -1};
+  const auto [n, keep, want, to, give, q] = row ? row_plan(a, b) : RowPlan{0, 0, 0, 0, 0, -1};
   s_from[tid] = keep;
   if (tid == 0) s_free = 0;
   for_entries(give, s_end, s_count, s_warp, [&](int r, int i) { return a.t.pages[(long long)(rank * per + r) * a.t.ld + s_from[r] + i]; }, [&](int, int, int p) {
@@ -337,6 +339,7 @@ __global__ void __launch_bounds__(POOL_THREADS) reserve_kernel(const __grid_cons
   if (row) {
     a.t.held[b] = served ? max(to, keep) : keep;
     a.t.len[b] = n;
+    if (a.room) a.room[b] = served || need == 0 ? want : n;
     if (served && swap) {
       atomicAdd(a.pool.refs + q, -1);
       int32_t* m = a.moves.list + 3ll * (moves_end - 1);
@@ -391,7 +394,7 @@ __global__ void __launch_bounds__(POOL_THREADS) reserve_small_kernel(const __gri
   } else {
     for (int i = tid; i < words * 32; i += POOL_THREADS) s_refs[i] = i < n_pages ? a.pool.refs[i] : 1;
   }
-  const auto [n, keep, to, give, q] = row ? row_plan(a, tid) : RowPlan{0, 0, 0, 0, -1};
+  const auto [n, keep, want, to, give, q] = row ? row_plan(a, tid) : RowPlan{0, 0, 0, 0, 0, -1};
   s_from[tid] = keep;
   if (tid == 0) { s_free = 0; s_need = 0; s_moves = 0; }
   __syncthreads();
@@ -437,6 +440,7 @@ __global__ void __launch_bounds__(POOL_THREADS) reserve_small_kernel(const __gri
   if (row) {
     a.t.held[tid] = served ? max(to, keep) : keep;
     a.t.len[tid] = n;
+    if (a.room) a.room[tid] = served || need == 0 ? want : n;
     if (served && swap) {
       atomicAdd(a.pool.refs + q, -1);
       int32_t* m = a.moves.list + 3ll * (ends.y - 1);
@@ -739,17 +743,18 @@ int sps_paged_fork(const sps_page_pool* pool, const sps_page_table* src, const s
   return done(launch_k(fork_kernel, table_grid(rows, src->ld), dim3(FORK_THREADS), 0, (cudaStream_t)stream, a));
 }
 
-int sps_paged_reserve(const sps_page_pool* pool, const sps_page_table* table, const int32_t* want, const sps_page_moves* moves, void* workspace,
-                      void* stream) {
+int sps_paged_reserve(const sps_page_pool* pool, const sps_page_table* table, const int32_t* want, int32_t* room, const sps_page_moves* moves,
+                      void* workspace, void* stream) {
   const char* why = bad_pool(pool);
   if (!why) why = bad_table(table);
   if (!why) why = bad_moves(moves);
   if (!why) why = bad_workspace(workspace);
   if (why) return no(SPS_EINVAL, why);
   if ((table->B > 0 && !want) || ((uintptr_t)want & 3)) return no(SPS_EINVAL, "want null or not 4-byte aligned");
+  if ((uintptr_t)room & 3) return no(SPS_EINVAL, "room not 4-byte aligned");
   if (moves->capacity < table->B) return no(SPS_EINVAL, "moves: a row may need one, capacity is smaller than the table's B");
   ReserveArgs a{};
-  a.pool = pool_of(pool); a.t = table_of(table); a.want = want; a.moves = moves_of(moves);
+  a.pool = pool_of(pool); a.t = table_of(table); a.want = want; a.room = room; a.moves = moves_of(moves);
   const int64_t n = ((int64_t)pool->n_pages + 63) / 64 * 64;
   a.writers = (int32_t*)((char*)workspace + 256);
   a.first = a.writers + n;

@@ -33,8 +33,9 @@ class Model:
         self.rows = rows
 
     def reserve(self, want):
-        """Returns (moves, a row went without)."""
+        """Returns (moves, a row went without); self.room: the tokens that each row may be written up to."""
         ps = self.page
+        self.room = [max(w, 0) for w in want]
         for i, w in enumerate(want):
             self.lens[i] = min(self.lens[i], max(w, 0))
             while len(self.rows[i]) * ps >= self.lens[i] + ps:
@@ -56,6 +57,7 @@ class Model:
                 continue
             if short or need > len(free):
                 short = True
+                self.room[i] = self.lens[i]
                 continue
             mine, free = free[:need], free[need:]
             if fresh[i]:
@@ -84,7 +86,7 @@ class Device:
         self.n_pages, self.page, self.B, self.ld = n_pages, page, B, ld
         self.pool = sps.PagePool(torch.zeros(n_pages, dtype=I32, device=DEV), page)
         self.tables = [self.table(B, ld), self.table(B, ld)]
-        self.at = 0
+        self.at, self.reserved = 0, False                      # reserved: the last call, whose room is to be checked
         cap = max(B, n_pages // 2 + 1) if capacity is None else capacity
         self.moves = sps.PageMoves(torch.full((cap, 3), -7, dtype=I32, device=DEV), torch.zeros(1, dtype=I32, device=DEV))
         self.ws = torch.zeros(sps.sps_paged_pool_workspace_bytes(n_pages), dtype=torch.uint8, device=DEV)
@@ -107,14 +109,18 @@ class Device:
         self.t.lens.copy_(ints(model.lens))
         self.pool.refs.copy_(ints(model.refs))
 
-    def fork(self, parents, stream=None):
-        sps.sps_paged_fork(self.pool, self.t, self.tables[1 - self.at], ints(parents), stream=stream)
+    def fork(self, parents):
+        self.reserved = False
+        sps.sps_paged_fork(self.pool, self.t, self.tables[1 - self.at], ints(parents))
         self.at = 1 - self.at
 
     def reserve(self, want):
-        sps.sps_paged_reserve(self.pool, self.t, ints(want), self.moves, self.ws)
+        self.reserved = True
+        self.room = torch.full((self.B,), -4, dtype=I32, device=DEV)
+        sps.sps_paged_reserve(self.pool, self.t, ints(want), self.moves, self.ws, room=self.room)
 
     def compact(self):
+        self.reserved = False
         sps.sps_paged_compact(self.pool, self.t, self.t, self.pool.refs, self.moves, self.ws)
 
     def listed(self):
@@ -125,6 +131,8 @@ class Device:
         assert rows == model.rows
         assert self.t.lens.tolist() == model.lens and self.t.held.tolist() == [len(r) for r in model.rows]
         assert self.pool.refs.tolist() == model.refs
+        if self.reserved:
+            assert self.room.tolist() == model.room
         assert int(self.pool.status) == status
         assert not self.ws[256:256 + 8 * ((self.n_pages + 63) // 64 * 64)].any()   # marks are zero between calls
 

@@ -116,7 +116,7 @@ def test_want_may_be_the_lengths_themselves(n_pages):
     m.reserve([90, 41, 50, 3])
     d.reserve([90, 41, 50, 3])
     m.reserve([60, 41, 7, 0])
-    sps.sps_paged_reserve(d.pool, d.t, d.t.lens, d.moves, d.ws)
+    sps.sps_paged_reserve(d.pool, d.t, d.t.lens, d.moves, d.ws, room=d.room)
     d.check(m)
 
 
@@ -237,7 +237,10 @@ def test_a_row_left_without_its_copy_still_shares():
     d.reserve([13, 13])
     assert short and moves == [] and d.listed() == []
     d.check(m, sps.PAGED_NO_PAGE)
-    assert m.rows[0] == m.rows[1]
+    assert m.rows[0] == m.rows[1] and d.room.tolist() == [13, 12]
+    want = ints([13, 13])
+    sps.sps_paged_reserve(d.pool, d.t, want, d.moves, d.ws, room=want)   # (room may be want)
+    assert want.tolist() == [13, 12]
 
 
 @pytest.mark.parametrize("B,n_pages", [(1, 1), (1025, 4096), (2500, 4097), (8192, 70001)])

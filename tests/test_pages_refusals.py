@@ -42,8 +42,8 @@ def fork(p=None, s=None, d=None, parents=P):
     return sps.lib().sps_paged_fork(ref(p or pool()), ref(s or table()), ref(d or other()), parents, None)
 
 
-def reserve(p=None, t=None, want=P, m=None, ws=P):
-    return sps.lib().sps_paged_reserve(ref(p or pool()), ref(t or table()), want, ref(m or moves()), ws, None)
+def reserve(p=None, t=None, want=P, m=None, ws=P, room=None):
+    return sps.lib().sps_paged_reserve(ref(p or pool()), ref(t or table()), want, room, ref(m or moves()), ws, None)
 
 
 def compact(p=None, s=None, d=None, refs=P, m=None, ws=P):
@@ -95,6 +95,7 @@ def test_combinations():
     refused(fork(parents=P + 2), "parents")
     refused(reserve(want=None), "want")
     refused(reserve(want=P + 1), "want")
+    refused(reserve(room=P + 2), "room")
     refused(reserve(m=moves(capacity=3)), "capacity")
     refused(reserve(ws=None), "workspace")
     refused(reserve(ws=P + 8), "workspace")
@@ -105,7 +106,7 @@ def test_combinations():
     refused(compact(ws=P + 4), "workspace")
     L = sps.lib()
     assert L.sps_paged_fork(None, None, None, None, None) == sps.SPS_EINVAL
-    assert L.sps_paged_reserve(None, None, None, None, None, None) == sps.SPS_EINVAL
+    assert L.sps_paged_reserve(None, None, None, None, None, None, None) == sps.SPS_EINVAL
     assert L.sps_paged_compact(None, None, None, None, None, None, None) == sps.SPS_EINVAL
     assert L.sps_paged_copy(None, 1, None, None) == sps.SPS_EINVAL
     assert L.sps_paged_pool_workspace_bytes(0) == -1 and L.sps_paged_pool_workspace_bytes((1 << 20) + 1) == -1
