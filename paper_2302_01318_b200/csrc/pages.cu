@@ -188,35 +188,48 @@ __device__ __forceinline__ void for_pages(const PoolPart& p, const uint32_t* s_b
 }
 
 // use(row, i, load(row, i)) for i < count of every row of the CTA (a row per thread), by threads of a warp for neighbouring i: rows of
-// one or two by their own thread, the others in runs of 256 that go round the warps
+// one or two by their own thread, the others, listed in any order, by a warp each or, where one of them is long, in runs of
+// 256 that go round the warps.  *s_rows: 0, and left so
 template <class Load, class Use>
-__device__ __forceinline__ void for_entries(int count, int* s_end, int* s_count, int2* s_warp, Load load, Use use) {
-  const int tid = threadIdx.x;
+__device__ __forceinline__ void for_entries(int count, int* s_rows, int* s_end, int* s_count, int2* s_warp, Load load, Use use) {
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
   const bool few = count <= 2;
   if (few && count > 0) {
     const int v0 = load(tid, 0), v1 = count > 1 ? load(tid, 1) : 0;
     use(tid, 0, v0);
     if (count > 1) use(tid, 1, v1);
   }
-  const int runs = few ? 0 : (count + 255) / 256;
-  if (!__syncthreads_or(runs)) return;
-  int2 all;
-  s_end[tid] = block_scan(make_int2(runs, 0), s_warp, &all).x;
   s_count[tid] = count;
+  if (!few) s_end[atomicAdd(s_rows, 1)] = tid;
+  if (!__syncthreads_or(!few)) return;
+  const int rows = *s_rows;
+  auto run = [&](int r, int i0, int n) {
+    int v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = i0 + 32 * j < n ? load(r, i0 + 32 * j) : 0;
+#pragma unroll
+    for (int j = 0; j < 8; ++j)
+      if (i0 + 32 * j < n) use(r, i0 + 32 * j, v[j]);
+  };
+  const bool any_long = __syncthreads_or(count > 1024);
+  if (tid == 0) *s_rows = 0;
+  if (!any_long) {
+    for (int x = warp; x < rows; x += POOL_WARPS) {
+      const int r = s_end[x], n = s_count[r];
+      for (int i0 = lane; i0 - lane < n; i0 += 256) run(r, i0, n);
+    }
+    return;
+  }
+  int2 all;
+  s_end[tid] = block_scan(make_int2(few ? 0 : (count + 255) / 256, 0), s_warp, &all).x;
   __syncthreads();
-  for (int u = tid >> 5; u < all.x; u += POOL_WARPS) {
+  for (int u = warp; u < all.x; u += POOL_WARPS) {
     int x = 0, y = POOL_THREADS - 1;   // the row of the u-th run: the first whose runs end behind it
     while (x < y) {
       const int m = (x + y) >> 1;
       if (s_end[m] > u) y = m; else x = m + 1;
     }
-    const int i0 = (u - (x ? s_end[x - 1] : 0)) * 256 + (tid & 31), n = s_count[x];
-    int v[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = i0 + 32 * j < n ? load(x, i0 + 32 * j) : 0;
-#pragma unroll
-    for (int j = 0; j < 8; ++j)
-      if (i0 + 32 * j < n) use(x, i0 + 32 * j, v[j]);
+    run(x, (u - (x ? s_end[x - 1] : 0)) * 256 + lane, s_count[x]);
   }
 }
 
@@ -266,7 +279,7 @@ __global__ void __launch_bounds__(POOL_THREADS) reserve_kernel(const __grid_cons
   __shared__ int s_end[POOL_THREADS], s_count[POOL_THREADS], s_from[POOL_THREADS], s_at[POOL_THREADS];
   __shared__ int2 s_warp[POOL_WARPS];
   __shared__ uint32_t s_bits[POOL_WORDS];
-  __shared__ int s_free, s_met, s_sums[3][8];   // this CTA's free pages; what is met where not all is; every CTA's free pages, needs and moves
+  __shared__ int s_rows, s_free, s_met, s_sums[3][8];   // this CTA's free pages; what is met where not all is; every CTA's free pages, needs and moves
   cg::cluster_group cl = cg::this_cluster();   // (at the first barrier every CTA is there to be written to)
   const int rank = (int)cl.block_rank(), parts = (int)cl.num_blocks(), tid = threadIdx.x, B = a.t.B;
   const int per = (B + parts - 1) / parts, b = rank * per + tid;
@@ -278,8 +291,9 @@ __global__ void __launch_bounds__(POOL_THREADS) reserve_kernel(const __grid_cons
   // (1) the row's plan, and what it gives up
   const auto [n, keep, want, to, give, q] = row ? row_plan(a, b) : RowPlan{0, 0, 0, 0, 0, -1};
   s_from[tid] = keep;
-  if (tid == 0) s_free = 0;
-  for_entries(give, s_end, s_count, s_warp, [&](int r, int i) { return a.t.pages[(long long)(rank * per + r) * a.t.ld + s_from[r] + i]; }, [&](int, int, int p) {
+  if (tid == 0) { s_free = 0; s_rows = 0; }
+  __syncthreads();
+  for_entries(give, &s_rows, s_end, s_count, s_warp, [&](int r, int i) { return a.t.pages[(long long)(rank * per + r) * a.t.ld + s_from[r] + i]; }, [&](int, int, int p) {
     if (p < 0 || p >= a.pool.n_pages) paged_flag(a.pool.status, SPS_PAGED_BAD_PAGE);
     else atomicAdd(a.pool.refs + p, -1);
   });
@@ -365,15 +379,16 @@ __global__ void __launch_bounds__(POOL_THREADS) reserve_kernel(const __grid_cons
   const int take = served ? need : 0;
   s_from[tid] = end - need;
   s_at[tid] = keep - swap;
-  for_entries(take, s_end, s_count, s_warp, [&](int r, int i) { return __ldcg(a.fresh + s_from[r] + i); },
+  for_entries(take, &s_rows, s_end, s_count, s_warp, [&](int r, int i) { return __ldcg(a.fresh + s_from[r] + i); },
               [&](int r, int i, int p) { a.t.pages[(long long)(rank * per + r) * a.t.ld + s_at[r] + i] = p; });
   if (served && swap) a.moves.list[3ll * (moves_end - 1) + 1] = __ldcg(a.fresh + end - need);
 }
 
 // The same for pools whose references fit a CTA's shared memory, and a table of a row per thread: the steps' counts, marks and
 // list are kept there, and trips to L2 are only the rows, the references and the entries.  A beam step of 4 rows takes 9.5 us with
-// this kernel and 12.2 with the cluster's, one of 64 rows in a pool of 700 pages 23.1 and 26.3; with 20700 pages the two are
-// level (6.4 us).  Changes of references go to both places.
+// this kernel and 12.2 with the cluster's, one of 64 rows in a pool of 700 pages 23.1 and 26.3.  64 rows with a scoring pass's room:
+// 3.9 us and 5.9 in a pool of 830 pages, 5.6 and 6.8 of 16606; with half of them coming and going 6.3 and 7.9, 11.6 and 10.6.  Changes
+// of references go to both places.
 constexpr int SMALL_PAGES = 24576;   // two words each
 
 __global__ void __launch_bounds__(POOL_THREADS) reserve_small_kernel(const __grid_constant__ ReserveArgs a) {
@@ -381,7 +396,7 @@ __global__ void __launch_bounds__(POOL_THREADS) reserve_small_kernel(const __gri
   __shared__ int s_end[POOL_THREADS], s_count[POOL_THREADS], s_from[POOL_THREADS], s_at[POOL_THREADS];
   __shared__ int2 s_warp[POOL_WARPS];
   __shared__ uint32_t s_bits[SMALL_PAGES / 32];
-  __shared__ int s_free, s_need, s_moves;
+  __shared__ int s_rows, s_free, s_need, s_moves;
   const int tid = threadIdx.x, lane = tid & 31, B = a.t.B, n_pages = a.pool.n_pages, words = (n_pages + 31) / 32;
   int* const s_refs = (int*)s_dyn;             // [words * 32]
   int* const s_first = s_refs + words * 32;    // first of those who write to a page; then the list of fresh pages
@@ -396,9 +411,9 @@ __global__ void __launch_bounds__(POOL_THREADS) reserve_small_kernel(const __gri
   }
   const auto [n, keep, want, to, give, q] = row ? row_plan(a, tid) : RowPlan{0, 0, 0, 0, 0, -1};
   s_from[tid] = keep;
-  if (tid == 0) { s_free = 0; s_need = 0; s_moves = 0; }
+  if (tid == 0) { s_rows = 0; s_free = 0; s_need = 0; s_moves = 0; }
   __syncthreads();
-  for_entries(give, s_end, s_count, s_warp, [&](int r, int i) { return a.t.pages[(long long)r * a.t.ld + s_from[r] + i]; }, [&](int, int, int p) {
+  for_entries(give, &s_rows, s_end, s_count, s_warp, [&](int r, int i) { return a.t.pages[(long long)r * a.t.ld + s_from[r] + i]; }, [&](int, int, int p) {
     if (p < 0 || p >= n_pages) { paged_flag(a.pool.status, SPS_PAGED_BAD_PAGE); return; }
     atomicAdd(s_refs + p, -1);
     atomicAdd(a.pool.refs + p, -1);
@@ -461,7 +476,7 @@ __global__ void __launch_bounds__(POOL_THREADS) reserve_small_kernel(const __gri
   s_from[tid] = ends.x - need;
   s_at[tid] = keep - swap;
   __syncthreads();
-  for_entries(served ? need : 0, s_end, s_count, s_warp, [&](int r, int i) { return s_first[s_from[r] + i]; },
+  for_entries(served ? need : 0, &s_rows, s_end, s_count, s_warp, [&](int r, int i) { return s_first[s_from[r] + i]; },
               [&](int r, int i, int p) { a.t.pages[(long long)r * a.t.ld + s_at[r] + i] = p; });
   if (served && swap) a.moves.list[3ll * (ends.y - 1) + 1] = s_first[ends.x - need];
 }
