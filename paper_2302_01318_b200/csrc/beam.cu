@@ -23,7 +23,7 @@ namespace cg = cooperative_groups;
 namespace {
 
 constexpr int SCAN_THREADS = 256, SCAN_WARPS = 8, SCAN_SEGS = 4;       // segments of a group: a warp's load
-constexpr int ONE_RUN = 4, ONE_CTAS = 8, ONE_THREADS = 1024, ONE_PICK = 512, ONE_WARPS = ONE_CTAS * ONE_THREADS / 32;   // the kernel for little work; ONE_PICK: threads that pick
+constexpr int ONE_RUN = 2, ONE_CTAS = 8, ONE_THREADS = 1024, ONE_PICK = 512, ONE_WARPS = ONE_CTAS * ONE_THREADS / 32;   // the kernel for little work; ONE_PICK: threads that pick
 constexpr int PICK_CAP = 1024, PICK_COUNTED = 128, PICK_SPLIT = 8, PICK_PER = 4;   // entries of a list, of one ranked by counting, threads that rank one; segments a thread holds
 constexpr int BEAM_MAX_B = 8192, BEAM_MAX_W = 128, BEAM_MAX_N = 128;
 
@@ -575,8 +575,9 @@ __global__ void __launch_bounds__(THREADS) beam_pick_kernel(const __grid_constan
   beam_pick<T, THREADS>(a, blockIdx.x, row, s_beams, a.seg_max + (long long)row * a.n_seg, a.parts + (long long)row * a.max_parts);
 }
 // Both for little work, a cluster to a sequence: what the scan finds goes straight to the shared memory of the CTA that picks (half
-// of its threads do: the pick's steps cost by the warp).  One prompt of 4 x 32000: 8.6 us as two launches in a graph and 16 one by
-// one (the host's), 8.6 and 10.5 this way; eight of 8 x 32000 14.6 and 16.6 against 10.6 and 11.3.
+// of its threads do: the pick's steps cost by the warp).  It saves a launch, which is the host's time: one prompt of 4 x 32000 takes 9.0
+// us a call (8.6 replayed from a graph), of 8 x 32000 10.5 (10.1), eight of those 10.9 (10.5); as two launches 10.9 (8.7) and
+// 11.1 (10.7), and 16 where the host is slow.
 template <typename T>
 __global__ void __cluster_dims__(ONE_CTAS, 1, 1) __launch_bounds__(ONE_THREADS) beam_one_kernel(const __grid_constant__ BeamArgs a) {
   __shared__ Beams s_beams;
@@ -615,8 +616,9 @@ cudaError_t beam_launch(BeamArgs& a, int num_sm, cudaStream_t st) {
   a.groups = (a.n_seg + SCAN_SEGS - 1) / SCAN_SEGS;
   a.max_parts = max_parts(a.V);
   const long long all = (long long)a.B * a.W * a.groups, warps = (long long)num_sm * 4 * SCAN_WARPS;
-  // little work, no more than ONE_RUN groups to a warp and clusters that fit beside one another: one launch
-  if ((long long)a.W * a.groups <= ONE_RUN * ONE_WARPS && a.B * ONE_CTAS <= num_sm) {
+  // little work, no more than ONE_RUN groups to a warp, and clusters that fit beside one another (with 18 of 8 x 32000 they do not:
+  // 15.5 us against 12.6): one launch
+  if ((long long)a.W * a.groups <= ONE_RUN * ONE_WARPS && a.B * ONE_CTAS <= num_sm / 2) {
     a.run = (a.W * a.groups + ONE_WARPS - 1) / ONE_WARPS;
     a.max_parts = (a.groups + a.run - 1) / a.run + 1;   // W of them: ONE_WARPS + 2 W at most
     return launch_k(beam_one_kernel<T>, dim3(a.B * ONE_CTAS), dim3(ONE_THREADS), 0, st, a);
