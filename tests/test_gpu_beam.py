@@ -81,6 +81,17 @@ def test_rows_of_any_alignment(offset, dtype):
     run_and_check(flat[offset:].view(B, W, V), beams(B, W), N=6)
 
 
+@pytest.mark.parametrize("V", [1, 7, 250, 4093])
+@pytest.mark.parametrize("dtype,pad,offset", [(F32, 1, 1), (F32, 5, 0), (BF16, 13, 3), (BF16, 8, 0), (BF16, 1, 7)])
+def test_what_lies_between_the_rows_never_matters(V, dtype, pad, offset):
+    """NaN ahead of the first row, between rows and behind the last one; both forms of the call."""
+    for B, W in ((2, 3), (40, 3)):
+        store = torch.full((offset + B * W * (V + pad) + 8,), math.nan, dtype=dtype, device=DEV)
+        x = store[offset:offset + B * W * (V + pad)].view(B, W, V + pad)[..., :V]
+        x.copy_(normal((B, W, V), dtype, V))
+        run_and_check(x, beams(B, W), N=5)
+
+
 def test_one_beam_rows_may_lie_a_batch_stride_apart():
     x = normal((4, 3, 500))[:, 1:2]
     run_and_check(x, beams(4, 1), N=3)
