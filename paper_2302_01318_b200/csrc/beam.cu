@@ -265,7 +265,7 @@ struct Best {
   double* keep_key;   // [BEAM_MAX_N]: the N best, in order
   int* keep_at;
   int* count;
-  int *thread, *tops, *bound;   // [THREADS + WARPS], [BEAM_MAX_N + 2 WARPS], [1]: for best_bound
+  int *thread, *tops, *bound;   // [THREADS], [BEAM_MAX_N + 2 WARPS], [1]: for best_bound
 };
 __device__ __forceinline__ bool better(double k, int i, double k1, int i1) { return k > k1 || (k == k1 && i < i1); }
 __device__ __forceinline__ void best_push(const Best& b, double k, int i) {
@@ -273,15 +273,16 @@ __device__ __forceinline__ void best_push(const Best& b, double k, int i) {
   if (n < PICK_CAP) { b.key[n] = k; b.at[n] = i; }
 }
 // a number that at least N of the threads' numbers reach (-inf: they may be fewer): the N-th of the groups' best, k from each, a
-// group being every WARPS-th thread (so that neighbours, which may all be of one beam, are in groups of their own)
+// group having one lane of 32, or two, of every warp, another one in each (a warp's numbers may all be of one beam, and only its first
+// lanes have any where a beam has few segments)
 template <int THREADS>
 __device__ __forceinline__ float best_bound(const Best& b, float top, int N) {
   constexpr int WARPS = THREADS / 32;
-  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, k = (N + WARPS - 1) / WARPS + 1, mine_at = lane * WARPS + warp;
-  b.thread[tid + tid / 32] = ordered(top);
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, k = (N + WARPS - 1) / WARPS + 1;
+  b.thread[tid] = ordered(top);
   if (tid == 0) *b.bound = INT_MIN;
   pick_sync<THREADS>();
-  int mine = b.thread[mine_at + mine_at / 32];
+  int mine = b.thread[lane % WARPS * 32 + ((warp - lane) & (WARPS - 1)) + lane / WARPS * WARPS];
   for (int j = 0; j < k; ++j) {
     const int v = __reduce_max_sync(0xffffffffu, mine);
     if (lane == 0) b.tops[warp * k + j] = v;
@@ -299,76 +300,99 @@ __device__ __forceinline__ float best_bound(const Best& b, float top, int N) {
   return unordered(max(*b.bound, ordered(-INFINITY)));
 }
 
+// A list of n, above PICK_COUNTED (few segments with many candidates), cut to what reaches a bound; what is long even then (ties by
+// the hundred) is sorted, a bitonic network over the next power of two, of which a warp has 64 neighbours to itself.  Returns
+// how many are left at its head: all of the N best, at most 2 PICK_COUNTED.  (Out of line, like all that is rarely run: the pick is a
+// walk through code that has to be fetched.)
+template <int THREADS>
+__device__ __noinline__ int best_shorten(const Best& b, int N, int n) {
+  constexpr int PER = (PICK_CAP + THREADS - 1) / THREADS;
+  const int tid = threadIdx.x;
+  double k[PER];
+  int p[PER];
+  float top = -INFINITY;
+#pragma unroll
+  for (int j = 0; j < PER; ++j) {
+    const int i = tid + j * THREADS;
+    k[j] = i < n ? b.key[i] : -INFINITY;
+    p[j] = i < n ? b.at[i] : 0;
+    top = fmaxf(top, __double2float_rd(k[j]));
+  }
+  const float least = best_bound<THREADS>(b, top, N);
+  if (tid == 0) *b.count = 0;
+  pick_sync<THREADS>();
+#pragma unroll
+  for (int j = 0; j < PER; ++j)
+    if (k[j] > -INFINITY && k[j] >= (double)least) best_push(b, k[j], p[j]);
+  pick_sync<THREADS>();
+  n = *b.count;
+  if (n <= 2 * PICK_COUNTED) return n;
+  int size = 4 * PICK_COUNTED;
+  while (size < n) size *= 2;
+  for (int i = n + tid; i < size; i += THREADS) { b.key[i] = -INFINITY; b.at[i] = INT_MAX; }
+  pick_sync<THREADS>();
+  for (int run = 2; run <= size; run *= 2)
+    for (int step = run / 2; step > 0; step /= 2) {
+      if (tid < size / 2) {
+        const int i = 2 * tid - (tid & (step - 1)), j = i + step;
+        const double ki = b.key[i], kj = b.key[j];
+        const int ai = b.at[i], aj = b.at[j];
+        if (better(kj, aj, ki, ai) == ((i & run) == 0)) { b.key[i] = kj; b.at[i] = aj; b.key[j] = ki; b.at[j] = ai; }
+      }
+      // the next step's pairs lie within what a warp has, unless its step is above 32
+      if (step > 32 || (step == 1 && run > 32)) pick_sync<THREADS>();
+      else __syncwarp();
+    }
+  pick_sync<THREADS>();
+  return 2 * PICK_COUNTED;
+}
 // The list's N best to keep_key / keep_at in order; returns how many there are (every thread of the CTA calls it, the list is
-// complete).  Every entry counts those before it, PICK_SPLIT threads to an entry.  A long list (few segments with many candidates)
-// is first cut to what reaches a bound; what is long even then (ties by the hundred) is sorted, a bitonic network over the next power
-// of two, of which a warp has 64 neighbours to itself.  Counting 1000 entries would take 50 us, sorting them 10, the cut 1.
+// complete).  Every entry counts those before it, PICK_SPLIT threads to an entry.  Counting 1000 entries would take 50 us, sorting
+// them 10, cutting them 1.
 template <int THREADS>
 __device__ __forceinline__ int best_rank(const Best& b, int N) {
-  const int tid = threadIdx.x;
+  const int tid = threadIdx.x, sub = tid % PICK_SPLIT;
   int n = min(*b.count, PICK_CAP);
   const int found = min(n, N);
-  if (n > PICK_COUNTED) {
-    constexpr int PER = (PICK_CAP + THREADS - 1) / THREADS;
-    double k[PER];
-    int p[PER];
-    float top = -INFINITY;
-#pragma unroll
-    for (int j = 0; j < PER; ++j) {
-      const int i = tid + j * THREADS;
-      k[j] = i < n ? b.key[i] : -INFINITY;
-      p[j] = i < n ? b.at[i] : 0;
-      top = fmaxf(top, __double2float_rd(k[j]));
-    }
-    const float least = best_bound<THREADS>(b, top, N);
-    if (tid == 0) *b.count = 0;
-    pick_sync<THREADS>();
-#pragma unroll
-    for (int j = 0; j < PER; ++j)
-      if (k[j] > -INFINITY && k[j] >= (double)least) best_push(b, k[j], p[j]);
-    pick_sync<THREADS>();
-    n = *b.count;
-  }
-  if (n <= 2 * PICK_COUNTED) {
-    const int sub = tid % PICK_SPLIT;
-    for (int i0 = 0; i0 < n; i0 += THREADS / PICK_SPLIT) {
-      const int i = i0 + tid / PICK_SPLIT;
-      const double k = i < n ? b.key[i] : 0.0;
-      const int p = i < n ? b.at[i] : 0;
-      int r = 0;
-      if (i < n)
+  if (n > PICK_COUNTED) n = best_shorten<THREADS>(b, N, n);
+#pragma unroll 1
+  for (int i0 = 0; i0 < n; i0 += THREADS / PICK_SPLIT) {
+    const int i = i0 + tid / PICK_SPLIT;
+    const double k = i < n ? b.key[i] : 0.0;
+    const int p = i < n ? b.at[i] : 0;
+    int r = 0;
+    if (i < n)
 #pragma unroll 4
-        for (int j = sub; j < n; j += PICK_SPLIT) r += better(b.key[j], b.at[j], k, p);
+      for (int j = sub; j < n; j += PICK_SPLIT) r += better(b.key[j], b.at[j], k, p);
 #pragma unroll
-      for (int o = PICK_SPLIT / 2; o > 0; o >>= 1) r += __shfl_xor_sync(0xffffffffu, r, o);
-      if (i < n && sub == 0 && r < N) { b.keep_key[r] = k; b.keep_at[r] = p; }
-    }
-  } else {
-    int size = 4 * PICK_COUNTED;
-    while (size < n) size *= 2;
-    for (int i = n + tid; i < size; i += THREADS) { b.key[i] = -INFINITY; b.at[i] = INT_MAX; }
-    pick_sync<THREADS>();
-    for (int run = 2; run <= size; run *= 2)
-      for (int step = run / 2; step > 0; step /= 2) {
-        if (tid < size / 2) {
-          const int i = 2 * tid - (tid & (step - 1)), j = i + step;
-          const double ki = b.key[i], kj = b.key[j];
-          const int ai = b.at[i], aj = b.at[j];
-          if (better(kj, aj, ki, ai) == ((i & run) == 0)) { b.key[i] = kj; b.at[i] = aj; b.key[j] = ki; b.at[j] = ai; }
-        }
-        // the next step's pairs lie within what a warp has, unless its step is above 32
-        if (step > 32 || (step == 1 && run > 32)) pick_sync<THREADS>();
-        else __syncwarp();
-      }
-    pick_sync<THREADS>();
-    for (int i = tid; i < N; i += THREADS) { b.keep_key[i] = b.key[i]; b.keep_at[i] = b.at[i]; }   // (N <= PICK_COUNTED < n)
+    for (int o = PICK_SPLIT / 2; o > 0; o >>= 1) r += __shfl_xor_sync(0xffffffffu, r, o);
+    if (i < n && sub == 0 && r < N) { b.keep_key[r] = k; b.keep_at[r] = p; }
   }
   pick_sync<THREADS>();
   return found;
 }
-// the N best of item(0 .. all - 1) -> (key, place), -inf keys left out, in rounds
+// The N best of item(0 .. all - 1) -> (key, place), -inf keys left out: those that reach a bound from the items themselves (a bound
+// from segments' maxima says little where few have them), or, where the list does not hold these either, in rounds.  20 x 15000 and
+// 127 candidates took 140 us in rounds alone, 51 so; rows of equal logits, which the bound does not thin, 97 and 122.
 template <int THREADS, class Item>
 __device__ __noinline__ int best_rounds(const Best& b, int N, int all, Item item) {
+  float top = -INFINITY;
+#pragma unroll 4
+  for (int i = threadIdx.x; i < all; i += THREADS) {
+    int at;
+    top = fmaxf(top, __double2float_rd(item(i, &at)));
+  }
+  const float least = best_bound<THREADS>(b, top, N);
+  if (threadIdx.x == 0) *b.count = 0;
+  pick_sync<THREADS>();
+#pragma unroll 4
+  for (int i = threadIdx.x; i < all; i += THREADS) {
+    int at;
+    const double k = item(i, &at);
+    if (k > -INFINITY && k >= (double)least) best_push(b, k, at);
+  }
+  pick_sync<THREADS>();
+  if (*b.count <= PICK_CAP) return best_rank<THREADS>(b, N);
   int have = 0;
   pick_sync<THREADS>();
   for (int i0 = 0; i0 < all; i0 += PICK_CAP - BEAM_MAX_N) {
@@ -408,12 +432,13 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
   __shared__ double s_key[PICK_CAP], s_keep[BEAM_MAX_N], s_base[BEAM_MAX_W];
   __shared__ float s_max[BEAM_MAX_W];
   __shared__ float2 s_line[BEAM_MAX_W];   // a beam's score_of as a line in fp32: what a logit of 0 would have, and what that is off by
-  __shared__ int s_thread[THREADS + WARPS], s_at[PICK_CAP], s_keep_at[BEAM_MAX_N], s_tops[BEAM_MAX_N + 2 * WARPS], s_count, s_bound;
-  __shared__ int2 s_seg[BEAM_MAX_N];
+  __shared__ int s_thread[THREADS], s_at[PICK_CAP], s_keep_at[BEAM_MAX_N], s_tops[BEAM_MAX_N + 2 * WARPS], s_count, s_bound;
+  __shared__ int3 s_seg[BEAM_MAX_N];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, N = a.N;
   const Best best{s_key, s_at, s_keep, s_keep_at, &s_count, s_thread, s_tops, &s_bound};
   const int all = a.W * a.n_seg;
-  // A warp takes the segments of one beam, 32 PER at a time; those of the first time round are on their way while the beams are looked at
+  // A warp takes the segments of one beam, 32 PER at a time; those of the first time round are on their way while the beams are
+  // looked at.  (Fewer at a time where there are warps enough: 8.7 us became 9.1 for 4 x 32000.)
   const int chunks = (a.n_seg + 32 * PER - 1) / (32 * PER), units = a.W * chunks;
   float held[PER];
   auto load = [&](int unit) {
@@ -472,11 +497,17 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
     if (units > WARPS) place = load(u);
     const float2 line = s_line[place.x];
     if (!(line.x > -INFINITY)) continue;
+    unsigned pass = 0;
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
       const float v = fmaf(held[j], a.inv_t32, line.x);
       // (what left fp32's range may be anything)
-      if (held[j] > -INFINITY && !(v + fmaf(fabsf(v), 4.7683716e-7f, line.y) < least)) best_push(best, score_of(place.x, held[j]), place.x * a.n_seg + place.y + 32 * j);
+      if (held[j] > -INFINITY && !(v + fmaf(fabsf(v), 4.7683716e-7f, line.y) < least)) pass |= 1u << j;
+    }
+#pragma unroll 1
+    for (; pass; pass &= pass - 1) {
+      const int i = place.x * a.n_seg + place.y + 32 * (__ffs(pass) - 1);
+      best_push(best, score_of(place.x, seg_max[i]), i);
     }
   }
   pick_sync<THREADS>();
@@ -490,12 +521,12 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
     bound = segs == N ? s_keep[N - 1] : -INFINITY;
   }
   const int* const from = all_read ? s_at : s_keep_at;
-  for (int i = tid; i < segs; i += THREADS) {
+  for (int i = tid; i < segs; i += THREADS) {   // each one's beam, and the token that it begins with (the row's first, or some before it)
     const int w = from[i] / a.n_seg;
-    s_seg[i] = make_int2(w, (from[i] - w * a.n_seg) * SEG);
+    int shift;
+    row_begin<T>(a, b * a.W + w, &shift);
+    s_seg[i] = make_int3(w, (from[i] - w * a.n_seg) * SEG - shift, 0);
   }
-  pick_sync<THREADS>();
-  if (tid == 0) s_count = 0;
   pick_sync<THREADS>();
   // their elements that reach the bound, and the beams that are done
   auto ended = [&](int w, int* at) {            // beam w's candidate, if it is done
@@ -503,31 +534,40 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
     *at = w * a.V + a.end_token;
     return isfinite(s) ? (double)s : -(double)INFINITY;
   };
+  auto row_of = [&](int w) { return reinterpret_cast<const T*>(a.logits) + (long long)(b * a.W + w) * a.row_stride; };
+  if (tid == 0) s_count = 0;
+  for (int i = tid; i < segs; i += THREADS) {   // the least logit that may reach the bound, rounded down, by which nearly all are told
+    const double base = s_base[s_seg[i].x], m = s_max[s_seg[i].x], off = (bound - base) * a.t;
+    const float low = __double2float_rd(m + off - (fabs(m) + fabs(off) + fabs(base) * a.t) * 1e-12);
+    s_seg[i].z = __float_as_int(fmaxf(low, -3.4028235e38f));   // (-inf is no candidate)
+  }
+  pick_sync<THREADS>();
+#pragma unroll 1
   for (int i0 = warp; i0 < segs; i0 += 4 * WARPS) {
     uint4 u[4];
-    int2 sg[4];
-    int shift[4];
+    unsigned pass = 0;
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       if (i0 + j * WARPS >= segs) continue;
-      sg[j] = s_seg[i0 + j * WARPS];
-      const T* x = row_begin<T>(a, b * a.W + sg[j].x, &shift[j]);
-      u[j] = load_piece(x, sg[j].y + lane * E, shift[j], a.V);
+      const int3 sg = s_seg[i0 + j * WARPS];
+      u[j] = load_piece(row_of(sg.x), sg.y + lane * E, 0, a.V);
     }
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
       if (i0 + j * WARPS >= segs) continue;
+      const float low = __int_as_float(s_seg[i0 + j * WARPS].z);
       float f[E];
       Logit<T>::unpack(u[j], f);
-      // the least logit that may reach the bound, rounded down: nearly all are told from it by one comparison
-      const double base = s_base[sg[j].x], m = s_max[sg[j].x], off = (bound - base) * a.t;
-      const float low = __double2float_rd(m + off - (fabs(m) + fabs(off) + fabs(base) * a.t) * 1e-12);
 #pragma unroll
-      for (int e = 0; e < E; ++e) {
-        if (!(f[e] >= low)) continue;
-        const double v = score_of(sg[j].x, f[e]);
-        if (v >= bound && v > -INFINITY) best_push(best, v, sg[j].x * a.V + sg[j].y - shift[j] + lane * E + e);
-      }
+      for (int e = 0; e < E; ++e) pass |= (f[e] >= low ? 1u : 0u) << (j * E + e);
+    }
+#pragma unroll 1
+    for (; pass; pass &= pass - 1) {
+      const int bit = __ffs(pass) - 1;
+      const int3 sg = s_seg[i0 + bit / E * WARPS];
+      const int token = sg.y + lane * E + bit % E;
+      const double v = score_of(sg.x, Logit<T>::get(row_of(sg.x) + token));
+      if (v >= bound) best_push(best, v, sg.x * a.V + token);
     }
   }
   if (a.done && tid < a.W) {
@@ -538,12 +578,10 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
   pick_sync<THREADS>();
   auto element = [&](int i, int* at) {          // element i of the segments, one behind the other, then the done beams
     if (i >= segs * SEG) return ended(i - segs * SEG, at);
-    const int2 sg = s_seg[i / SEG];
-    int shift;
-    const T* x = row_begin<T>(a, b * a.W + sg.x, &shift);
-    const int v = sg.y + i % SEG - shift;
+    const int3 sg = s_seg[i / SEG];
+    const int v = sg.y + i % SEG;
     *at = sg.x * a.V + v;
-    return v >= 0 && v < a.V ? score_of(sg.x, Logit<T>::get(x + shift + v)) : -(double)INFINITY;
+    return v >= 0 && v < a.V ? score_of(sg.x, Logit<T>::get(row_of(sg.x) + v)) : -(double)INFINITY;
   };
   const int n = s_count > PICK_CAP ? best_rounds<THREADS>(best, N, segs * SEG + (a.done ? a.W : 0), element) : best_rank<THREADS>(best, N);
   for (int i = tid; i < N; i += THREADS) {

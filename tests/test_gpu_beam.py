@@ -42,6 +42,16 @@ def test_many_sequences_wide_beams_and_unaligned_rows_in_both_forms(B, W, V, N, 
     run_and_check(normal((B, W, V), dtype, B + V, pad=pad), beams(B, W, V), N=N)
 
 
+@pytest.mark.parametrize("B,W,V,N,dtype", [(3, 15, 873, 13, BF16), (20, 15, 873, 13, BF16), (2, 1, 15000, 128, F32), (20, 1, 15000, 127, F32), (2, 3, 500, 100, BF16),
+                                           (20, 2, 4097, 64, F32), (1, 1, 9000, 65, BF16)])
+def test_fewer_segments_than_candidates_or_about_as_many(B, W, V, N, dtype):
+    """The segments' maxima then say little, or nothing, about the N-th candidate; one beam may hold them all."""
+    s = beams(B, W, V)
+    run_and_check(normal((B, W, V), dtype, B + V), s, N=N)
+    s[:, 0] += 40
+    run_and_check(normal((B, W, V), dtype, B + V + 1, std=0.5), s, N=N)
+
+
 def test_sequences_of_which_many_beams_are_dead_or_done():
     """Whole runs of rows are skipped, and parts begin and end beside them."""
     B, W, V = 60, 16, 3001
