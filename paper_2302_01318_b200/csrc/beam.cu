@@ -613,8 +613,8 @@ __global__ void __launch_bounds__(THREADS) beam_pick_kernel(const __grid_constan
   beam_pick<T, THREADS>(a, blockIdx.x, row, s_beams, a.seg_max + (long long)row * a.n_seg, a.parts + (long long)row * a.max_parts);
 }
 // Both for little work, a cluster to a sequence: what the scan finds goes straight to the shared memory of the CTA that picks (half
-// of its threads do: the pick's steps cost by the warp).  It saves a launch, which is the host's time: one prompt of 4 x 32000 takes 9.0
-// us a call (8.6 replayed from a graph), of 8 x 32000 10.5 (10.1), eight of those 10.9 (10.5); as two launches 10.9 (8.7) and
+// of its threads do: the pick's steps cost by the warp).  It saves a launch, which is the host's time: one prompt of 4 x 32000 takes 9.2
+// us a call (8.7 replayed from a graph), of 8 x 32000 10.5 (10.1), eight of those 10.9 (10.5); as two launches 10.9 (8.7) and
 // 11.1 (10.7), and 16 where the host is slow.
 template <typename T>
 __global__ void __cluster_dims__(ONE_CTAS, 1, 1) __launch_bounds__(ONE_THREADS) beam_one_kernel(const __grid_constant__ BeamArgs a) {
