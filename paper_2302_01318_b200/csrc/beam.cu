@@ -24,7 +24,7 @@ namespace {
 
 constexpr int SCAN_THREADS = 256, SCAN_WARPS = 8, SCAN_SEGS = 4;       // segments of a group: a warp's load
 constexpr int ONE_RUN = 2, ONE_CTAS = 8, ONE_THREADS = 1024, ONE_PICK = 512, ONE_WARPS = ONE_CTAS * ONE_THREADS / 32;   // the kernel for little work; ONE_PICK: threads that pick
-constexpr int PICK_CAP = 1024, PICK_COUNTED = 128, PICK_SPLIT = 8, PICK_PER = 4;   // entries of a list, of one ranked by counting, threads that rank one; segments a thread holds
+constexpr int PICK_CAP = 1024, PICK_COUNTED = 128, PICK_SPLIT = 8, PICK_PER = 4, PICK_FEW = 4;   // entries of a list, of one ranked by counting, threads that rank one; segments a thread holds, to a candidate that are few
 constexpr int BEAM_MAX_B = 8192, BEAM_MAX_W = 128, BEAM_MAX_N = 128;
 
 struct BeamArgs {
@@ -372,8 +372,9 @@ __device__ __forceinline__ int best_rank(const Best& b, int N) {
   return found;
 }
 // The N best of item(0 .. all - 1) -> (key, place), -inf keys left out: those that reach a bound from the items themselves (a bound
-// from segments' maxima says little where few have them), or, where the list does not hold these either, in rounds.  20 x 15000 and
-// 127 candidates took 140 us in rounds alone, 51 so; rows of equal logits, which the bound does not thin, 97 and 122.
+// from segments' maxima says little where they are of one beam), or, where the list does not hold these either, in rounds.  15 x 873
+// with a beam far ahead of the others, 13 candidates, took 50 us in rounds alone, 16 so; equal logits, which a bound does not
+// thin, 104 and 40.
 template <int THREADS, class Item>
 __device__ __noinline__ int best_rounds(const Best& b, int N, int all, Item item) {
   float top = -INFINITY;
@@ -410,6 +411,14 @@ __device__ __noinline__ int best_rounds(const Best& b, int N, int all, Item item
     have = best_rank<THREADS>(b, N);
   }
   return have;
+}
+// best_bound from top(i, lane) of the segments i < segs, a warp to a segment
+template <int THREADS, class Top>
+__device__ __noinline__ float best_elements(const Best& b, int N, int segs, Top top) {
+  float t = -INFINITY;
+#pragma unroll 1
+  for (int i = threadIdx.x >> 5; i < segs; i += THREADS / 32) t = fmaxf(t, top(i, threadIdx.x & 31));
+  return best_bound<THREADS>(b, t, N);
 }
 
 // a sequence's beams, where the pick finds them
@@ -535,6 +544,14 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
     return isfinite(s) ? (double)s : -(double)INFINITY;
   };
   auto row_of = [&](int w) { return reinterpret_cast<const T*>(a.logits) + (long long)(b * a.W + w) * a.row_stride; };
+  // Where there are few segments to a candidate their maxima hardly thin the elements, and a bound from the elements does: 9 x 13 x 147,
+  // 25 candidates 17.1 -> 10.7 us, 56 x 2 x 255, 6 candidates 13.5 -> 11.2, 20 x 15000, 127 candidates 51 -> 24, 60 drawn selections 10.45 -> 10.0 in the mean; 39 x 466, 3
+  // candidates, where the maxima would have done, 8.5 -> 9.9
+  if (N > 1 && all < PICK_FEW * N)
+    bound = fmax(bound, (double)best_elements<THREADS>(best, N, segs, [&](int i, int lane) {
+      const int3 sg = s_seg[i];
+      return __double2float_rd(score_of(sg.x, Logit<T>::top(load_piece(row_of(sg.x), sg.y + lane * E, 0, a.V))));
+    }));
   if (tid == 0) s_count = 0;
   for (int i = tid; i < segs; i += THREADS) {   // the least logit that may reach the bound, rounded down, by which nearly all are told
     const double base = s_base[s_seg[i].x], m = s_max[s_seg[i].x], off = (bound - base) * a.t;
@@ -614,7 +631,7 @@ __global__ void __launch_bounds__(THREADS) beam_pick_kernel(const __grid_constan
 }
 // Both for little work, a cluster to a sequence: what the scan finds goes straight to the shared memory of the CTA that picks (half
 // of its threads do: the pick's steps cost by the warp).  It saves a launch, which is the host's time: one prompt of 4 x 32000 takes 9.2
-// us a call (8.7 replayed from a graph), of 8 x 32000 10.5 (10.1), eight of those 10.9 (10.5); as two launches 10.9 (8.7) and
+// us a call (8.9 replayed from a graph), of 8 x 32000 10.5 (10.1), eight of those 10.9 (10.5); as two launches 10.9 (8.7) and
 // 11.1 (10.7), and 16 where the host is slow.
 template <typename T>
 __global__ void __cluster_dims__(ONE_CTAS, 1, 1) __launch_bounds__(ONE_THREADS) beam_one_kernel(const __grid_constant__ BeamArgs a) {
