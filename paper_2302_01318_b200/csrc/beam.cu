@@ -374,7 +374,7 @@ __device__ __forceinline__ int best_rank(const Best& b, int N) {
 // The N best of item(0 .. all - 1) -> (key, place), -inf keys left out: those that reach a bound from the items themselves (a bound
 // from segments' maxima says little where they are of one beam), or, where the list does not hold these either, in rounds.  15 x 873
 // with a beam far ahead of the others, 13 candidates, took 50 us in rounds alone, 16 so; equal logits, which a bound does not
-// thin, 104 and 40.
+// thin, 42 and 61 (64 x 4 x 32000, 8 candidates).
 template <int THREADS, class Item>
 __device__ __noinline__ int best_rounds(const Best& b, int N, int all, Item item) {
   float top = -INFINITY;
