@@ -529,14 +529,16 @@ int sps_paged_fork(const sps_page_pool* pool, const sps_page_table* src, const s
  *   the entries behind ceil(n / page_size) are given up (want = 0: the whole row);
  * then, where want > n, row after row:
  *   the page of token n, if n is inside it and other rows hold it too, is exchanged for a fresh one, and (old, fresh, n % page_size)
- *   is added to `moves` -- unless all who hold it exchange it in this call: then the first of them keeps it;
+ *   is added to `moves` -- unless all who hold it go on in this call: then the first of them keeps it, or, if the pool has too few
+ *   pages for all rows of the call, the one that has the most tokens in it, the first of those;
  *   fresh pages are appended up to ceil(want / page_size) entries.
  * Fresh pages are the free ones in ascending order.  A row whose pages are no longer to be had gets none of them, nor does any
- * row behind it that needs some: it keeps its n tokens and the pages that they are in, and SPS_PAGED_NO_PAGE is set.  held
- * and len (= n) are written.  room: device [B], may be NULL (and may be want): the tokens that the row may be written up to -- want,
- * or n where it went without (its last page may then be shared still: nothing is to be appended to it).  Before new tokens
- * are appended, the moves are to be carried out (sps_paged_copy).  moves->capacity >= B.  workspace: device scratch of sps_paged_pool_workspace_bytes(n_pages) bytes, 16-byte aligned, zero-filled
- * once before its first use (every call leaves it ready for the next). */
+ * row behind it that needs some: it keeps its n tokens and the pages that they are in -- no other row's room reaches into them --,
+ * and SPS_PAGED_NO_PAGE is set.  held and len (= n) are written.  room: device [B], may be NULL (and may be want): the tokens that
+ * the row may be written up to -- want, or n where it went without (its last page may then be shared still: nothing is to be
+ * appended to it).  Before new tokens are appended, the moves are to be carried out (sps_paged_copy).  moves->capacity >= B.
+ * workspace: device scratch of sps_paged_pool_workspace_bytes(n_pages) bytes, 16-byte aligned, zero-filled once before its first
+ * use (every call leaves it ready for the next). */
 int sps_paged_reserve(const sps_page_pool* pool, const sps_page_table* table, const int32_t* want, int32_t* room, const sps_page_moves* moves,
                       void* workspace, void* stream);
 int64_t sps_paged_pool_workspace_bytes(int32_t n_pages);

@@ -236,14 +236,18 @@ __device__ __forceinline__ void for_entries(int count, int* s_rows, int* s_end, 
 // ------------------------------------------------------------------------------------------------------------------
 // Reserve.  With n = min(len, want) tokens kept in k = ceil(n / page) pages, a row (1) gives up its entries behind k, (2)
 // exchanges entry k - 1 for a fresh page if it is partly filled, about to be written and held by others too -- unless all who
-// hold it write to it and this row is the first of them --, and (3) takes fresh pages up to want tokens.  Fresh pages are the
+// hold it write to it and this row is the one of them that keeps it --, and (3) takes fresh pages up to want tokens.  Fresh pages are the
 // lowest free ones, handed out row after row: a prefix sum over the rows' needs and one over the pool's free pages meet in
 // a list of the pages handed out.
+// Who keeps it: where all rows get what they need, the first, since the others' copies are made before anyone appends.  Where
+// pages are short one of the others may go without and keep its tokens there: then the one with the most tokens, the first of
+// those, which writes behind what the others have.  The needs' total is the same either way, so that is known beforehand.
 //
 // One cluster does it all, a thread to a row (its state stays in registers), a part of the pool to a CTA, the steps divided by
 // cluster barriers: giving up -> marks at shared last pages, free pages -> needs -> list -> entries.  What it costs is those
 // steps' trips to L2, one behind the other; the references are read once (4 bytes a page).
-// Marks: per page the number of rows about to write to it and B - (the first of them), in the workspace, zero between calls.
+// Marks: per page the number of rows about to write to it and B - (the first of them), where pages are short the one with the most
+// tokens; in the workspace, zero between calls.
 // ------------------------------------------------------------------------------------------------------------------
 struct ReserveArgs {
   Pool pool;
@@ -254,6 +258,9 @@ struct ReserveArgs {
   int32_t *writers, *first;   // [n_pages], zero
   int32_t* fresh;             // [n_pages]: the pages handed out
 };
+
+// a row's claim to keep a page of which it has n tokens (above 0): the largest keeps it
+__device__ __forceinline__ int keep_claim(int n, int page_size, int row) { return (n & (page_size - 1)) * PAGES_MAX_ROWS + PAGES_MAX_ROWS - 1 - row; }
 
 struct RowPlan { int n, keep, want, to, give, q; };   // tokens and pages kept, tokens and pages wanted, entries given up, the page about to be written (-1: none)
 __device__ __forceinline__ RowPlan row_plan(const ReserveArgs& a, int b) {
@@ -315,24 +322,39 @@ __global__ void __launch_bounds__(POOL_THREADS) reserve_kernel(const __grid_cons
   block_add(free_pages, &s_free);
   cl.sync();
   // (3) needs, summed in the rows' order, and every CTA told the others' sums
-  const bool swap = shared > 1 && !(__ldcg(a.writers + q) == shared && __ldcg(a.first + q) == B - b);
-  const int need = row ? max(to - keep, 0) + swap : 0;
+  const int more = row ? max(to - keep, 0) : 0;   // pages behind those that it has
+  const bool all_write = shared > 1 && __ldcg(a.writers + q) == shared;
+  bool swap = shared > 1 && !(all_write && __ldcg(a.first + q) == B - b);
   int2 sum;
-  const int2 ends = block_scan(make_int2(need, swap), s_warp, &sum);
-  if (tid < parts) {
-    int* const s = cl.map_shared_rank(&s_sums[0][0], tid);
-    s[rank] = s_free; s[8 + rank] = sum.x; s[16 + rank] = sum.y;
-  }
-  cl.sync();
-  int end = ends.x, moves_end = ends.y, free_before = 0, free_all = 0, need_all = 0, moves_all = 0;
+  int need, end, moves_end, free_before, free_all, need_all, moves_all;
+  auto add_up = [&]() {
+    need = more + swap;
+    const int2 ends = block_scan(make_int2(need, swap), s_warp, &sum);
+    if (tid < parts) {
+      int* const s = cl.map_shared_rank(&s_sums[0][0], tid);
+      s[rank] = s_free; s[8 + rank] = sum.x; s[16 + rank] = sum.y;
+    }
+    cl.sync();
+    end = ends.x; moves_end = ends.y;
+    free_before = free_all = need_all = moves_all = 0;
 #pragma unroll
-  for (int c = 0; c < 8; ++c) {
-    if (c >= parts) break;
-    const int f = s_sums[0][c], n0 = s_sums[1][c], m = s_sums[2][c];
-    if (c < rank) { free_before += f; end += n0; moves_end += m; }
-    free_all += f; need_all += n0; moves_all += m;
-  }
-  if (need_all > free_all) {   // the rows behind the first that goes without do so too: what the ones before it need, and their moves
+    for (int c = 0; c < 8; ++c) {
+      if (c >= parts) break;
+      const int f = s_sums[0][c], n0 = s_sums[1][c], m = s_sums[2][c];
+      if (c < rank) { free_before += f; end += n0; moves_end += m; }
+      free_all += f; need_all += n0; moves_all += m;
+    }
+  };
+  add_up();
+  if (need_all > free_all) {
+    if (all_write) a.first[q] = 0;   // (all have read it)
+    cl.sync();
+    const int claim = keep_claim(n, a.pool.page_size, b);
+    if (all_write) atomicMax(a.first + q, claim);
+    cl.sync();
+    swap = shared > 1 && !(all_write && __ldcg(a.first + q) == claim);
+    add_up();
+    // the rows behind the first that goes without do so too: what the ones before it need, and their moves
     if (row && need > 0 && end > free_all) paged_flag(a.pool.status, SPS_PAGED_NO_PAGE);
     s_met = 0;
     __syncthreads();
@@ -428,12 +450,14 @@ __global__ void __launch_bounds__(POOL_THREADS) reserve_small_kernel(const __gri
     atomicMin(s_first + q, tid);
   }
   __syncthreads();
-  const bool swap = writes && !(s_refs[q] == 0 && s_first[q] == tid);
-  const int need = row ? max(to - keep, 0) + swap : 0;
+  const bool all_write = writes && s_refs[q] == 0;
+  bool swap = writes && !(all_write && s_first[q] == tid);
+  const int more = row ? max(to - keep, 0) : 0;   // pages behind those that it has
+  int need = more + swap;
   __syncthreads();
   if (writes && !swap) s_refs[q] = 1;
   int2 all;
-  const int2 ends = block_scan(make_int2(need, swap), s_warp, &all);   // (its barriers: s_refs is complete, s_first free)
+  int2 ends = block_scan(make_int2(need, swap), s_warp, &all);   // (its barriers: s_refs is complete, s_first free)
   int free_pages = 0;
   for (int w = tid >> 5; w < words; w += POOL_WARPS) {
     const uint32_t v = __ballot_sync(0xffffffffu, s_refs[w * 32 + lane] == 0);
@@ -444,7 +468,16 @@ __global__ void __launch_bounds__(POOL_THREADS) reserve_small_kernel(const __gri
   __syncthreads();
   const int free_all = s_free;
   int need_all = all.x, moves_all = all.y;
-  if (need_all > free_all) {   // what the rows ahead of the first that goes without need, and their moves
+  if (need_all > free_all) {
+    if (all_write) s_first[q] = 0;
+    __syncthreads();
+    const int claim = keep_claim(n, a.pool.page_size, tid);
+    if (all_write) atomicMax(s_first + q, claim);
+    __syncthreads();
+    swap = writes && !(all_write && s_first[q] == claim);
+    need = more + swap;
+    ends = block_scan(make_int2(need, swap), s_warp, &all);
+    // what the rows ahead of the first that goes without need, and their moves
     if (need > 0 && ends.x > free_all) paged_flag(a.pool.status, SPS_PAGED_NO_PAGE);
     if (row && ends.x <= free_all) { atomicMax(&s_need, ends.x); atomicMax(&s_moves, ends.y); }
     __syncthreads();
