@@ -558,7 +558,8 @@ int sps_paged_copy(const sps_paged_cache* layers, int32_t n_layers, const sps_pa
 
 /* The selection of a beam step: for each of B sequences the N best continuations of its W beams, best first,
  *   c[w, v] = scores[w] + logits[w, v] / T - log sum_u exp(logits[w, u] / T),
- * equal ones in the order of w V + v.  (The paper samples; beam search is another way to decode from the same logits, and with
+ * equal ones in the order of w V + v: so are a beam's equal logits, and the candidates of alike beams, which have one score and the
+ * same logits, wherever their rows lie.  (The paper samples; beam search is another way to decode from the same logits, and with
  * sps_paged_fork over the same cache.)
  *   logits        device, dtype 0 fp32 / 1 bf16: row b W + w at logits + (b W + w) row_stride (elements), V of them; any alignment
  *                 of the rows

@@ -434,6 +434,90 @@ __device__ __forceinline__ void beams_load(const BeamArgs& a, int b, Beams& beam
   }
 }
 
+// Alike beams, of one score and the same logits, tie in every candidate, and places decide.  Their sums of exponentials were added
+// up in the parts that the runs and the rows' alignment made, and may differ in the last bits: the later ones take the first's.
+// It is the rows that are compared, where score and maximum are the same: sums that are close say nothing.  A warp looks for each beam's
+// first earlier one by the rows' first pieces, then all threads compare what was found to the end.  Rare (a search that starts from
+// beams of one score), and then a second reading by one CTA: 4 alike beams of 32000 fp32 logits take 15 us, where unlike ones take 9; 64 x
+// 4 of 131071 in bf16 52, else 22.  Where it is not run it costs 0.1 us (0.2 - 0.3 out of line: the call's registers).
+// base, top, line: the beams', as in beam_pick; like, differ: scratch, [BEAM_MAX_W]
+template <typename T, int THREADS>
+__device__ __forceinline__ void alike_beams(const BeamArgs& a, int first_row, const Beams& beams, double* base, const float* top, float2* line, int* like, int* differ) {
+  constexpr int E = Logit<T>::E, WARPS = THREADS / 32, PER = 4;
+  const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5;
+  // whether two rows differ in what a thread compares: the elements below n, `step` threads sharing them (it is number t of them)
+  auto unlike = [&](int w, int r, int n, int t, int step) {
+    int sw, sr;
+    const T *x = row_begin<T>(a, first_row + w, &sw), *y = row_begin<T>(a, first_row + r, &sr);
+    bool no = false;
+    int whole = 0;   // elements in 16-byte pieces, behind the first `ahead` ones
+    const int ahead = sw ? E - sw : 0;
+    if (sw == sr) whole = max(n - ahead, 0) / E * E;
+    for (int i0 = t; i0 < whole / E; i0 += PER * step) {
+      uint4 u[PER], v[PER];
+#pragma unroll
+      for (int j = 0; j < PER; ++j) {
+        const int at = sw + ahead + min(i0 + j * step, whole / E - 1) * E;
+        u[j] = *reinterpret_cast<const uint4*>(x + at);
+        v[j] = *reinterpret_cast<const uint4*>(y + at);
+      }
+#pragma unroll
+      for (int j = 0; j < PER; ++j) {
+        float f[E], g[E];
+        Logit<T>::unpack(u[j], f);
+        Logit<T>::unpack(v[j], g);
+#pragma unroll
+        for (int e = 0; e < E; ++e) no |= f[e] != g[e];
+      }
+    }
+    // the others: those ahead of the pieces and behind them, or, where the rows' alignment differs, all
+    for (int i0 = t; i0 < n - whole; i0 += PER * step) {
+      T f[PER], g[PER];
+#pragma unroll
+      for (int j = 0; j < PER; ++j) {
+        const int i = min(i0 + j * step, n - whole - 1), at = i < ahead ? i : i + whole;
+        f[j] = x[sw + at];
+        g[j] = y[sr + at];
+      }
+#pragma unroll
+      for (int j = 0; j < PER; ++j) no |= Logit<T>::get(f + j) != Logit<T>::get(g + j);
+    }
+    return no;
+  };
+  // the first beam of r0 .. w - 1 whose score, maximum and first n logits are w's (w: none), by a warp
+  auto search = [&](int w, int r0, int n) {
+    for (; r0 < w; r0 += 32) {
+      const int r = min(r0 + lane, w);
+      unsigned may = __ballot_sync(0xffffffffu, r < w && base[w] > -INFINITY && base[r] > -INFINITY && beams.score[r] == beams.score[w] && top[r] == top[w]);
+      for (; may; may &= may - 1) {
+        const int at = r0 + __ffs(may) - 1;
+        if (!__any_sync(0xffffffffu, unlike(w, at, n, lane, 32))) return at;
+      }
+    }
+    return w;
+  };
+  const int first = a.V <= 4096 ? a.V : 32 * E;   // (short rows to their end)
+  for (int w = warp; w < a.W; w += WARPS) {
+    const int r = search(w, 0, first);
+    if (lane == 0) { like[w] = r; differ[w] = 0; }
+  }
+  pick_sync<THREADS>();
+  if (first < a.V) {
+    for (int w = 0; w < a.W; ++w)
+      if (like[w] < w && unlike(w, like[w], a.V, tid, THREADS)) differ[w] = 1;
+    pick_sync<THREADS>();
+    for (int w = warp; w < a.W; w += WARPS)   // (alike at first only: the next one that is so to the end)
+      if (differ[w]) {
+        const int r = search(w, like[w] + 1, a.V);
+        if (lane == 0) like[w] = r;
+      }
+    pick_sync<THREADS>();
+  }
+  // (who is found is the first of its kind: what it has stays)
+  if (tid < a.W && like[tid] < tid) { base[tid] = base[like[tid]]; line[tid] = line[like[tid]]; }
+  pick_sync<THREADS>();
+}
+
 // the pick of sequence b by a CTA; first: its first row in the list that was cut into runs, seg_max and parts: from there on
 template <typename T, int THREADS>
 __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, const Beams& beams, const float* seg_max, const float2* all_parts) {
@@ -441,7 +525,7 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
   __shared__ double s_key[PICK_CAP], s_keep[BEAM_MAX_N], s_base[BEAM_MAX_W];
   __shared__ float s_max[BEAM_MAX_W];
   __shared__ float2 s_line[BEAM_MAX_W];   // a beam's score_of as a line in fp32: what a logit of 0 would have, and what that is off by
-  __shared__ int s_thread[THREADS], s_at[PICK_CAP], s_keep_at[BEAM_MAX_N], s_tops[BEAM_MAX_N + 2 * WARPS], s_count, s_bound;
+  __shared__ int s_thread[THREADS], s_at[PICK_CAP], s_keep_at[BEAM_MAX_N], s_tops[BEAM_MAX_N + 2 * WARPS], s_count, s_bound, s_one_score;
   __shared__ int3 s_seg[BEAM_MAX_N];
   const int tid = threadIdx.x, lane = tid & 31, warp = tid >> 5, N = a.N;
   const Best best{s_key, s_at, s_keep, s_keep_at, &s_count, s_thread, s_tops, &s_bound};
@@ -461,7 +545,13 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
   auto parts_of = [&](int w) { return ((first + w) * a.groups + a.groups - 1) / a.run - (first + w) * a.groups / a.run + 1; };
   float2 ahead = make_float2(-INFINITY, 0.f);   // (so is a warp's first part)
   if (warp < a.W && lane < a.max_parts) ahead = all_parts[(long long)warp * a.max_parts + lane];   // (those behind its own are not used)
+  if (tid == 0) s_one_score = 0;
   pick_sync<THREADS>();   // (`beams` is there)
+  if (warp == WARPS - 1) {   // beams of one score may be alike (beyond 32 that is left to be found out)
+    const float s = lane < a.W ? beams.score[lane] + 0.f : INFINITY;
+    const unsigned same = __match_any_sync(0xffffffffu, isfinite(s) ? __float_as_uint(s) : 0x7fc00000u | lane);
+    if (a.W > 32 || same != 1u << lane) s_one_score = 1;
+  }
   for (int w = warp; w < a.W; w += WARPS) {
     const float2* parts = all_parts + (long long)w * a.max_parts;
     const int n_parts = parts_of(w);
@@ -487,6 +577,7 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
   }
   if (tid == 0) s_count = 0;
   pick_sync<THREADS>();
+  if (__builtin_expect(s_one_score, 0)) alike_beams<T, THREADS>(a, b * a.W, beams, s_base, s_max, s_line, s_at, s_thread);
   auto score_of = [&](int w, float l) { return s_base[w] > -INFINITY ? s_base[w] + ((double)l - (double)s_max[w]) * a.inv_t : -INFINITY; };
   // The N best segments.  Scores are first taken in fp32, a line in the logit, with what their roundings may come to (the line's
   // start, 1 / T, one of the fused operation: 2^-24 each of numbers no larger than the score's and the start's together): at
