@@ -268,7 +268,7 @@ __device__ __forceinline__ RowPlan row_plan(const ReserveArgs& a, int b) {
   const int held0 = a.t.held[b], len0 = a.t.len[b], want0 = a.want[b];
   const int cap = (int)min((long long)a.t.ld << a.pool.page_shift, (long long)INT_MAX - a.pool.page_size);
   const int held = min(max(held0, 0), a.t.ld), room = (int)min((long long)held << a.pool.page_shift, (long long)cap), want = min(max(want0, 0), cap);
-  if (held != held0 || len0 > room || want0 > cap) paged_flag(a.pool.status, SPS_PAGED_BAD_LENGTH);
+  if (held != held0 || len0 < 0 || len0 > room || want0 < 0 || want0 > cap) paged_flag(a.pool.status, SPS_PAGED_BAD_LENGTH);
   r.n = min(min(max(len0, 0), room), want);
   r.keep = (r.n + a.pool.page_size - 1) >> a.pool.page_shift;
   r.want = want;

@@ -1,0 +1,21 @@
+"""The pool's status: each thing that does not fit sets its bit by itself, and what fits sets none."""
+import pytest
+import torch
+
+import paper_2302_01318_b200 as sps
+from pages_util import DEV, I32, Device, ints
+from test_gpu_pages import grown
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.mark.parametrize("n_pages", [40, 24577])
+@pytest.mark.parametrize("lens,want,bit", [((-1, 9), (0, 9), sps.PAGED_BAD_LENGTH), ((-2 ** 31, 9), (3, 9), sps.PAGED_BAD_LENGTH), ((30, 9), (-1, 9), sps.PAGED_BAD_LENGTH),
+                                           ((30, 9), (30, -2 ** 31), sps.PAGED_BAD_LENGTH), ((33, 9), (33, 9), sps.PAGED_BAD_LENGTH), ((30, 9), (49, 9), sps.PAGED_BAD_LENGTH),
+                                           ((32, 16), (0, 48), 0), ((0, 0), (0, 0), 0)])
+def test_reserve_tells_of_each_count_outside_its_row(n_pages, lens, want, bit):
+    m, d = grown(n_pages, 8, [30, 9], ld=6)
+    d.t.lens.copy_(ints(lens))
+    d.reserve(list(want))
+    assert int(d.pool.status) == bit
+    assert d.t.lens.tolist() == [min(max(n, 0), 8 * len(r), max(w, 0)) for n, r, w in zip(lens, m.rows, want)]
