@@ -69,7 +69,7 @@ __global__ void __launch_bounds__(FORK_THREADS) fork_kernel(const __grid_constan
     for (int b0 = 0; b0 < a.dst.B; b0 += FORK_THREADS) children += __syncthreads_count(b0 + tid < a.dst.B && a.parents[b0 + tid] == row);
   if (is_dst) {
     if (blockIdx.y == 0 && tid == 0) {
-      if (parent >= a.src.B) paged_flag(a.pool.status, SPS_PAGED_BAD_ROW);
+      if (parent < -1 || parent >= a.src.B) paged_flag(a.pool.status, SPS_PAGED_BAD_ROW);
       a.dst.held[row] = gets;
       a.dst.len[row] = there ? a.src.len[parent] : 0;
     }

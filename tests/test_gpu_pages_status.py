@@ -19,3 +19,12 @@ def test_reserve_tells_of_each_count_outside_its_row(n_pages, lens, want, bit):
     d.reserve(list(want))
     assert int(d.pool.status) == bit
     assert d.t.lens.tolist() == [min(max(n, 0), 8 * len(r), max(w, 0)) for n, r, w in zip(lens, m.rows, want)]
+
+
+@pytest.mark.parametrize("parents,bit", [((0, 1, -1), 0), ((0, 1, -2), sps.PAGED_BAD_ROW), ((-2 ** 31, 1, 0), sps.PAGED_BAD_ROW), ((0, 3, 1), sps.PAGED_BAD_ROW),
+                                         ((0, 1, 2 ** 31 - 1), sps.PAGED_BAD_ROW)])
+def test_fork_tells_of_each_parent_outside_the_table(parents, bit):
+    m, d = grown(40, 8, [30, 9, 17])
+    m.fork([p if 0 <= p < 3 else -1 for p in parents])
+    d.fork(list(parents))
+    d.check(m, bit)
