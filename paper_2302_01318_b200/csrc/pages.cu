@@ -78,13 +78,14 @@ __global__ void __launch_bounds__(FORK_THREADS) fork_kernel(const __grid_constan
     for (int i = 0; i < FORK_PER; ++i)
       if (e0 + i * FORK_THREADS < gets) to[e0 + i * FORK_THREADS] = v[i];
   }
+  unsigned top = 0;   // (what is not there is page 0; below 0 is far above)
+#pragma unroll
+  for (int i = 0; i < FORK_PER; ++i) top = max(top, (unsigned)u[i]);
+  if (top >= (unsigned)a.pool.n_pages) paged_flag(a.pool.status, SPS_PAGED_BAD_PAGE);
   if (is_src && children != 1) {
 #pragma unroll
-    for (int i = 0; i < FORK_PER; ++i) {
-      if (e0 + i * FORK_THREADS >= gives) continue;
-      if (u[i] < 0 || u[i] >= a.pool.n_pages) paged_flag(a.pool.status, SPS_PAGED_BAD_PAGE);
-      else atomicAdd(a.pool.refs + u[i], children - 1);
-    }
+    for (int i = 0; i < FORK_PER; ++i)
+      if (e0 + i * FORK_THREADS < gives && (unsigned)u[i] < (unsigned)a.pool.n_pages) atomicAdd(a.pool.refs + u[i], children - 1);
   }
 }
 

@@ -28,3 +28,16 @@ def test_fork_tells_of_each_parent_outside_the_table(parents, bit):
     m.fork([p if 0 <= p < 3 else -1 for p in parents])
     d.fork(list(parents))
     d.check(m, bit)
+
+
+@pytest.mark.parametrize("parents", [(0, 1, 2), (2, 0, 1), (0, 0, 0), (1, 1, 2), (-1, -1, -1)])
+@pytest.mark.parametrize("page", [40, -1, 2 ** 31 - 1])
+@pytest.mark.parametrize("row,entry", [(0, 0), (0, 3), (2, 1)])
+def test_fork_tells_of_a_page_outside_the_pool_however_many_children_its_row_has(parents, page, row, entry):
+    m, d = grown(40, 8, [30, 9, 17])
+    d.t.pages[row, entry] = page
+    d.fork(list(parents))
+    assert int(d.pool.status) == sps.PAGED_BAD_PAGE
+    for i, p in enumerate(parents):
+        if p == row:
+            assert int(d.t.pages[i, entry]) == page
