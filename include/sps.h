@@ -492,8 +492,9 @@ int64_t sps_paged_attention_workspace_bytes(const sps_paged_cache* cache, int32_
  * layers, sps_beam_select of much work two), read and write their state on the device -- so that a captured call can be replayed -- and allocate nothing.  A pool's, a table's or a
  * workspace's calls must not run at the same time.  Results do not depend on timing: of free pages the lowest are taken, rows are
  * served in their order.  What does not fit is skipped, never followed, and sets a bit of the pool's status: page numbers
- * outside the pool (SPS_PAGED_BAD_PAGE; a fork and a compaction keep such an entry), counts outside their row
- * (SPS_PAGED_BAD_LENGTH; they are clipped), parents outside their table (SPS_PAGED_BAD_ROW; none).
+ * outside the pool (SPS_PAGED_BAD_PAGE; a fork and a compaction keep such an entry), counts outside their row -- held, and in
+ * sps_paged_reserve len and want; a fork and a compaction hand len on as it is -- (SPS_PAGED_BAD_LENGTH; they are clipped),
+ * parents outside their table, -1 apart (SPS_PAGED_BAD_ROW; none).  Entries that a call does not read are not looked at.
  * ------------------------------------------------------------------------------------------------------------- */
 #define SPS_PAGED_NO_PAGE 8    /* more bits of *status: a row was left without the pages that it wanted */
 #define SPS_PAGED_BAD_ROW 16

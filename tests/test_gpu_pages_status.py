@@ -41,3 +41,21 @@ def test_fork_tells_of_a_page_outside_the_pool_however_many_children_its_row_has
     for i, p in enumerate(parents):
         if p == row:
             assert int(d.t.pages[i, entry]) == page
+
+
+def test_fork_and_compact_hand_a_length_on_as_it_is():
+    m, d = grown(40, 8, [30, 9, 17])
+    d.t.lens.copy_(ints([-5, 1000, 17]))
+    d.fork([2, 1, 0])
+    assert d.t.lens.tolist() == [17, 1000, -5] and int(d.pool.status) == 0
+    d.compact()
+    assert d.t.lens.tolist() == [17, 1000, -5] and int(d.pool.status) == 0
+
+
+def test_a_pool_without_a_status_takes_what_does_not_fit_just_so():
+    m, d = grown(40, 8, [30, 9, 17])
+    d.pool._c.status = None
+    d.t.pages[0, 0] = 41
+    d.fork([0, -7, 9])
+    d.reserve([31, -3, 2 ** 31 - 1])
+    assert int(d.pool.status) == 0 and d.t.held.tolist()[:2] == [4, 0]
