@@ -17,8 +17,9 @@ namespace cg = cooperative_groups;
 // CTA per sequence, finds those segments (or a few more), reads them again (N x 512 bytes, from L2) and picks the N best elements.
 // The scan is bound by HBM with many rows; the pick by latency, a chain of a dozen short steps between barriers (6 us): 256 rows of
 // 131071 in bf16 (67 MB) 22.5 us, 512 of 32000 in fp32 20 us, of which the bytes' floor is 10.
-// Candidates are compared in 64 bits, from exact logits and a sum of fp32 exponentials (relative error about 2^-22), so that
-// far scores keep the order of their last bits; results are rounded once.
+// Candidates are compared in 64 bits, from exact logits and a sum of fp32 exponentials, so that a beam's far scores keep the order of
+// their last bits; results are rounded to fp32 at the end.  The sum's relative error, found with scores that make c about 0: 1 - 2 10^-7
+// for 1000 .. 131071 logits, at most 4.6 10^-7 = 2^-21 (5120 rows of 10^6, 2000 x 8 of 32000, 2^24 logits).
 // ------------------------------------------------------------------------------------------------------------------
 namespace {
 
