@@ -580,8 +580,8 @@ int sps_paged_copy(const sps_paged_cache* layers, int32_t n_layers, const sps_pa
  * A logit of -inf is no candidate.  A beam whose score is not finite, or whose logits hold a NaN or +inf or nothing above -inf, offers
  * none; a sequence that has fewer than N candidates gets (-inf, -1, -1, 0) for the rest.
  * With N = W, out_scores may be scores and out_done may be done.  B up to 8192, W and N up to 128, V up to 2^24, W V below 2^31.
- * workspace: device scratch of sps_beam_select_workspace_bytes bytes, 16-byte aligned, zero-filled once before its first use (every
- * call leaves it ready for the next; calls that share one must not run at the same time, captured ones included). */
+ * workspace: device scratch of sps_beam_select_workspace_bytes bytes, 16-byte aligned, whatever is in it (calls that share one must
+ * not run at the same time, captured ones included). */
 int sps_beam_select(const void* logits, int32_t dtype, int64_t row_stride, int32_t B, int32_t W, int32_t V, double temperature,
                     const float* scores, const int32_t* done, int32_t end_token, int32_t N, float* out_scores, int32_t* out_parents,
                     int32_t* out_tokens, int32_t* out_done, void* workspace, void* stream);

@@ -770,7 +770,7 @@ def sps_beam_select(logits, scores, out_scores, out_parents, out_tokens, workspa
                     temperature=1.0, stream=None):
     """The N best continuations of each sequence's beams.  logits CUDA [B, W, V], fp32 or bf16 (rows of any one stride); scores CUDA
     float32 [B, W]; done CUDA int32 [B, W]; out_scores float32, out_parents (rows b W + w), out_tokens, out_done int32, all
-    [B, N]; workspace CUDA uint8 (zeroed once) of sps_beam_select_workspace_bytes."""
+    [B, N]; workspace CUDA uint8 of sps_beam_select_workspace_bytes."""
     code = _dtype_of(logits)
     index = logits.get_device()
     shape = logits.shape
