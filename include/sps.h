@@ -573,8 +573,8 @@ int sps_paged_copy(const sps_paged_cache* layers, int32_t n_layers, const sps_pa
  *   out_parents   device int32 [B][N]: row b W + w of the continued beam -- the parents of sps_paged_fork when N = W
  *   out_tokens    device int32 [B][N]
  *   out_done      device int32 [B][N], may be NULL: 1 where the token is end_token, else 0
- * c is worked out and compared in 64 bits, but the sum under its logarithm is of fp32 exponentials added up in fp32: its relative
- * error, which is c's error, is about 2^-22 (2^-21 was the largest found, over vocabularies of 1000 .. 2^24).  Within a beam that
+ * c is worked out and compared in 64 bits, but the sum under its logarithm is of fp32 exponentials added up in fp32: by its
+ * relative error, about 2^-22 (2^-21 was the largest found, over vocabularies of 1000 .. 2^24), c is off.  Within a beam that
  * changes no order; candidates of unlike beams that are closer than this may change places.  The order of the additions follows from
  * the shape of the call and the rows' alignment: the same beams in another batch may get scores that differ by as much.
  * A logit of -inf is no candidate.  A beam whose score is not finite, or whose logits hold a NaN or +inf or nothing above -inf, offers
