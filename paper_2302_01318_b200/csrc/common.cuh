@@ -5,6 +5,9 @@
 #include <cuda_runtime.h>
 #include <stdint.h>
 
+#include <atomic>
+#include <mutex>
+
 #define SPS_MAX_ROWS 16   // activation rows one pass may carry (two 8-column MMA tiles)
 #define SPS_NUM_SM_FALLBACK 148
 
@@ -65,12 +68,13 @@ inline cudaError_t launch_k(void (*kern)(KArgs...), dim3 grid, dim3 block, size_
 
 // ------------------------------------------------------------------------------------------------
 // cudaFuncSetAttribute is per device: what a launcher remembers about it is kept per device too, so that
-// handles on several GPUs of one process each set the attribute on their own device.
+// handles on several GPUs of one process each set the attribute on their own device.  It only ever grows: of two threads that ask
+// for unlike sizes neither may leave the other's launch with less than it asked for.
 // ------------------------------------------------------------------------------------------------
 #define SPS_MAX_DEVICES 64
 struct DevSmemCache {
-  size_t bytes[SPS_MAX_DEVICES];
-  bool init;
+  std::atomic<size_t> bytes[SPS_MAX_DEVICES];   // (statics: 0 at first)
+  std::mutex growing;
 };
 template <class Kern>
 inline cudaError_t sps_ensure_smem(Kern k, size_t bytes, DevSmemCache& c) {
@@ -79,10 +83,11 @@ inline cudaError_t sps_ensure_smem(Kern k, size_t bytes, DevSmemCache& c) {
   if (e != cudaSuccess) return e;
   if (dev < 0 || dev >= SPS_MAX_DEVICES) return cudaErrorInvalidDevice;
   // 48 KB is the limit for static and dynamic shared memory TOGETHER unless the attribute says more: set it from 32 KB on
-  if (!c.init) { for (size_t& b : c.bytes) b = 32 * 1024; c.init = true; }
-  if (bytes <= c.bytes[dev]) return cudaSuccess;
+  if (bytes <= 32 * 1024 || bytes <= c.bytes[dev].load(std::memory_order_acquire)) return cudaSuccess;
+  std::lock_guard<std::mutex> one(c.growing);
+  if (bytes <= c.bytes[dev].load(std::memory_order_relaxed)) return cudaSuccess;
   e = cudaFuncSetAttribute(k, cudaFuncAttributeMaxDynamicSharedMemorySize, (int)bytes);
-  if (e == cudaSuccess) c.bytes[dev] = bytes;
+  if (e == cudaSuccess) c.bytes[dev].store(bytes, std::memory_order_release);
   return e;
 }
 // one-time (per device) attribute calls: true the first time on the current device
