@@ -148,7 +148,7 @@ typedef struct {
  * and rotary tables on cfg->device.  *out receives the handle. */
 int sps_create(const sps_weights* target_w, const sps_weights* draft_w, const sps_cfg* cfg, sps_handle** out);
 int sps_destroy(sps_handle* h);
-/* NUL-terminated text owned by the handle (or by the library when h is NULL). */
+/* NUL-terminated text owned by the handle (or by the library when h is NULL: what the calling thread was told last). */
 const char* sps_last_error(sps_handle* h);
 
 /* Algorithm 2 (K >= 1) or Algorithm 1 (K == 0) for one sequence: ingest the

@@ -14,7 +14,7 @@
 
 namespace {
 
-std::string g_err;  // last error of the handle-less entry points
+thread_local std::string g_err;  // last error of the handle-less entry points, of the thread that called them
 
 struct ModelDev {
   sps_model_cfg cfg{};
