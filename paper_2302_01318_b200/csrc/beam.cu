@@ -440,7 +440,8 @@ __device__ __forceinline__ void beams_load(const BeamArgs& a, int b, Beams& beam
 // It is the rows that are compared, where score and maximum are the same: sums that are close say nothing.  A warp looks for each beam's
 // first earlier one by the rows' first pieces, then all threads compare what was found to the end.  Rare (a search that starts from
 // beams of one score), and then a second reading by one CTA: 4 alike beams of 32000 fp32 logits take 15 us, where unlike ones take 9; 64 x
-// 4 of 131071 in bf16 52, else 22.  Where it is not run it costs 0.1 us (0.2 - 0.3 out of line: the call's registers).
+// 4 of 131071 in bf16 52, else 22.  Where it is not run it and the look at the scores cost 0.1 - 0.2 us (0.2 - 0.3 with it
+// out of line: the call's registers), with 128 beams 1 - 2 of 38.
 // base, top, line: the beams', as in beam_pick; like, differ: scratch, [BEAM_MAX_W]
 template <typename T, int THREADS>
 __device__ __forceinline__ void alike_beams(const BeamArgs& a, int first_row, const Beams& beams, double* base, const float* top, float2* line, int* like, int* differ) {
@@ -548,10 +549,12 @@ __device__ __forceinline__ void beam_pick(const BeamArgs& a, int b, int first, c
   if (warp < a.W && lane < a.max_parts) ahead = all_parts[(long long)warp * a.max_parts + lane];   // (those behind its own are not used)
   if (tid == 0) s_one_score = 0;
   pick_sync<THREADS>();   // (`beams` is there)
-  if (warp == WARPS - 1) {   // beams of one score may be alike (beyond 32 that is left to be found out)
-    const float s = lane < a.W ? beams.score[lane] + 0.f : INFINITY;
-    const unsigned same = __match_any_sync(0xffffffffu, isfinite(s) ? __float_as_uint(s) : 0x7fc00000u | lane);
-    if (a.W > 32 || same != 1u << lane) s_one_score = 1;
+  // beams of one score may be alike: a thread compares one with 32 others (the last warps, which have no parts to add up, where there are few)
+  if (const int w = (THREADS - 1 - tid) % BEAM_MAX_W, r0 = (THREADS - 1 - tid) / BEAM_MAX_W * 32; w < a.W && isfinite(beams.score[w])) {
+    bool same = false;
+#pragma unroll 4
+    for (int r = r0; r < min(r0 + 32, w); ++r) same |= beams.score[r] == beams.score[w];
+    if (same) s_one_score = 1;
   }
   for (int w = warp; w < a.W; w += WARPS) {
     const float2* parts = all_parts + (long long)w * a.max_parts;
